@@ -395,6 +395,105 @@ int32_t odb_measure_bulk_read_bandwidth(const void* buf, size_t bytes, int32_t r
  * visible cached positions per sequence (weights once + K/V once); used by the benchmark. */
 double odb_step_algorithmic_bytes(const odb_config* cfg, int32_t keys);
 
+/* ---- paged K/V cache ---------------------------------------------------------------------
+ * Operators for programs that run layers of their own over requests of different lengths (the session above keeps one
+ * contiguous region per sequence): a pool of K/V pages, block tables and slot maps built on the GPU, a fused norm /
+ * rotation / store of a projection's rows, and attention over the pages with grouped heads, a window and first tokens
+ * that stay visible.  Section 4.1's length prediction shortens responses while they are decoded; here their pages go
+ * back to the pool.
+ *
+ * The pool is bf16 [n_layers][2][n_pages][n_kv_heads][page_size][head_dim] (index 1: 0 = K, 1 = V), caller-owned.  A
+ * request of `len` positions holds ceil(len / page_size) pages, the front entries of its row of the table; the pages
+ * nobody holds are the front entries of the free list.  The slot of a position is page * page_size + position %
+ * page_size.
+ *
+ * Requirements: head_dim in {64, 128}; n_heads a multiple of n_kv_heads, up to 1024; page_size a power of two, 16 ..
+ * 1024; fewer than 2^31 slots and pool rows (n_layers * 2 * n_pages * n_kv_heads * page_size); up to 1024 requests in a
+ * forward; table rows of less than 2^30 positions.
+ *
+ * A handle's calls go to the stream they are given and are asynchronous.  They share the handle's workspace: use one
+ * stream at a time (calls on two streams have to be ordered by the caller).  They can be captured into a CUDA graph.
+ * What the device finds wrong is recorded in the handle's status word (odb_paged_status); nothing outside the buffers
+ * named in a call is read or written, whatever the lengths, tables and maps hold. */
+typedef struct odb_paged_config {
+    int32_t n_layers, n_heads, n_kv_heads, head_dim, page_size, n_pages;
+} odb_paged_config;
+
+/* One forward: device arrays, and what the host knows.  A call reads the fields that it names. */
+typedef struct odb_paged_batch {
+    int32_t n_seqs;             /* requests */
+    int32_t max_rows;           /* length of row_seq / row_pos / row_slot and rows of q, k, v and outputs */
+    int32_t max_new;            /* rows of the longest request, as far as the host knows: picks a kernel, never a result */
+    int32_t table_stride;       /* entries of a table row */
+    const int32_t* len_before;  /* [n_seqs] positions whose pages are held before the forward */
+    const int32_t* len_after;   /* [n_seqs] positions held, and keys, from the forward on */
+    const int32_t* first;       /* [n_seqs] position of the request's first row */
+    const int32_t* count;       /* [n_seqs] rows of the request */
+    int32_t* table;             /* [n_seqs][table_stride] page ids */
+    int32_t* free_pages;        /* [n_pages] page ids, the first n_pages - sum(held) are free */
+    int32_t* row_start;         /* [n_seqs + 1] rows before a request */
+    int32_t* row_seq;           /* [max_rows] request of a row, -1 behind the last */
+    int32_t* row_pos;           /* [max_rows] position, -1 behind the last */
+    int32_t* row_slot;          /* [max_rows] slot, -1 behind the last */
+} odb_paged_batch;
+
+typedef struct odb_paged odb_paged;
+
+size_t odb_paged_kv_bytes(const odb_paged_config* cfg);          /* 0: a configuration odb_paged_create would refuse */
+size_t odb_paged_workspace_bytes(const odb_paged_config* cfg);
+/* kv and workspace: device buffers, 256-byte aligned, borrowed until the handle is destroyed; the device current during
+ * this call is the handle's (calls with another one current return ODB_ERR_STATE).  Clears the workspace's control words
+ * on the stream and waits for it; the pool is left as it is. */
+int32_t odb_paged_create(const odb_paged_config* cfg, void* kv, size_t kv_bytes, void* workspace, size_t ws_bytes, void* stream,
+                         odb_paged** out);
+int32_t odb_paged_destroy(odb_paged* h);
+/* Reads and clears the status word: ODB_OK, or what a call on the device found since - ODB_ERR_ARG (lengths or rows that
+ * are negative, too long for a table row, or behind the length), ODB_ERR_WORKSPACE (the pool has too few pages),
+ * ODB_ERR_SHAPE (more rows than max_rows), ODB_ERR_STATE (a page id that is none), ODB_ERR_TIMEOUT.  Synchronous. */
+int32_t odb_paged_status(odb_paged* h, void* stream);
+
+/* Tables and maps of the forward: every request's table grows or shrinks from ceil(len_before / page_size) to
+ * ceil(len_after / page_size) pages, and rows first .. first + count - 1 of every request get their places.
+ * With n free pages, G given back (requests in order, then table order) and appended to them, T taken (requests in order,
+ * then table order): page j that is taken is entry n + G - 1 - j; the first n + G - T entries remain.  Table entries
+ * behind the pages held are left as they are.  Reads len_before, len_after, first, count; updates table, free_pages;
+ * writes row_start, row_seq, row_pos, row_slot.  A forward that does not fit changes no table and has no rows (row_start
+ * all zero), see odb_paged_status.  The next call's len_before is this one's len_after. */
+int32_t odb_paged_layout(odb_paged* h, const odb_paged_batch* b, void* stream);
+
+/* Rotation frequencies.  plain: theta^(-2i / rot_dim) radians per position for pair i; linear: divided by factor
+ * (position interpolation); ntk: theta * factor^(rot_dim / (rot_dim - 2)); yarn (arXiv 2309.00071, Section 3): by parts,
+ * f * (keep + (1 - keep) / factor), keep = clamp((original_len * f / (2 pi) - beta_slow) / (beta_fast - beta_slow), 0, 1),
+ * and cosine and sine multiplied by 0.1 ln(factor) + 1.  turns_host[i], i < rot_dim / 2: the fraction of a turn per
+ * position as a multiple of 2^-64 (position x turns in 64-bit integers drops the whole turns).  Host call. */
+enum { ODB_ROPE_PLAIN = 0, ODB_ROPE_LINEAR = 1, ODB_ROPE_NTK = 2, ODB_ROPE_YARN = 3 };
+int32_t odb_rope_frequencies(int32_t rot_dim, double theta, int32_t scaling, double factor, double original_len, double beta_slow,
+                             double beta_fast, uint64_t* turns_host, float* magnitude);
+
+/* For every row r < max_rows with row_pos[r] >= 0: q_out = rotate(norm(q)), and K := rotate(norm(k)), V := v at
+ * row_slot[r] (a slot that is none, -1 for one, stores nothing).  norm: x / sqrt(mean(x^2) + eps) * gain over a head's
+ * head_dim values, gains fp32 [head_dim], NULL: no norm (of q, of k).  rotate: pairs (i, i + rot_dim / 2), or (2i, 2i + 1)
+ * where interleaved, of the first rot_dim values (a multiple of 8 up to head_dim, 0: none) by position x frequency
+ * (turns: device copy of odb_rope_frequencies' numbers); the other values pass.  fp32, rounded once.
+ * q [max_rows][n_heads][head_dim], k and v [max_rows][n_kv_heads][head_dim], bf16 on 8-byte boundaries, strides in
+ * elements between rows (multiples of 4; the three may be slices of one projection's output).  q_out may be q itself
+ * (same stride).  Two rows with the same slot: one of them is stored. */
+int32_t odb_paged_norm_rope_store(odb_paged* h, int32_t layer, const odb_paged_batch* b, const void* q, int64_t q_stride, const void* k,
+                                  int64_t k_stride, const void* v, int64_t v_stride, const float* q_gain, const float* k_gain, float eps,
+                                  const uint64_t* turns, int32_t rot_dim, int32_t interleaved, float magnitude, void* q_out,
+                                  int64_t out_stride, void* stream);
+
+/* out[r][h] = sum_j softmax_j(scale * q[r][h] . K[j][h / group]) V[j][h / group] over the keys j that row r at position
+ * p = first + (r - row_start) sees: j < len_after, j <= p + right, and j >= p - left or j < sinks (left, right: -1 = no
+ * limit; causal: right = 0).  The row's own K and V are in the pool before (odb_paged_norm_rope_store).  scale 0 means
+ * 1 / sqrt(head_dim).  lse (fp32 [max_rows][n_heads], may be NULL): ln of the sum of exponentials.  A row that sees no key
+ * gets zeros and -infinity.  What pages hold at positions nobody sees never reaches a result, not even as NaN.
+ * Reads len_after, first, row_start, table; rows from row_start[n_seqs] on are left as they are.  q and out on 16-byte
+ * boundaries with row strides that are multiples of 8 elements; out must not overlap q.  Fixed order of sums: the same
+ * call gives the same bits. */
+int32_t odb_paged_attention(odb_paged* h, int32_t layer, const odb_paged_batch* b, const void* q, int64_t q_stride, void* out,
+                            int64_t out_stride, float* lse, float scale, int32_t left, int32_t right, int32_t sinks, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -54,6 +54,16 @@ class odb_result(C.Structure):
                 ("block_end", C.c_int32), ("accepted_pos", C.c_int32 * 64), ("accepted_tok", C.c_int32 * 64)]
 
 
+class odb_paged_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_heads", "n_kv_heads", "head_dim", "page_size", "n_pages")]
+
+
+class odb_paged_batch(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_seqs", "max_rows", "max_new", "table_stride")] + \
+               [(n, C.c_void_p) for n in ("len_before", "len_after", "first", "count", "table", "free_pages", "row_start",
+                                          "row_seq", "row_pos", "row_slot")]
+
+
 # name -> (restype, argtypes); the list the header declares
 SIGNATURES = {
     "odb_status_string": (C.c_char_p, [C.c_int32]),
@@ -101,6 +111,20 @@ SIGNATURES = {
     "odb_measure_read_bandwidth": (C.c_int32, [C.c_void_p, C.c_size_t, C.c_int32, C.c_void_p, C.POINTER(C.c_double)]),
     "odb_measure_bulk_read_bandwidth": (C.c_int32, [C.c_void_p, C.c_size_t, C.c_int32, C.c_void_p, C.POINTER(C.c_double)]),
     "odb_step_algorithmic_bytes": (C.c_double, [C.POINTER(odb_config), C.c_int32]),
+    "odb_paged_kv_bytes": (C.c_size_t, [C.POINTER(odb_paged_config)]),
+    "odb_paged_workspace_bytes": (C.c_size_t, [C.POINTER(odb_paged_config)]),
+    "odb_paged_create": (C.c_int32, [C.POINTER(odb_paged_config), C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t, C.c_void_p,
+                                     C.POINTER(C.c_void_p)]),
+    "odb_paged_destroy": (C.c_int32, [C.c_void_p]),
+    "odb_paged_status": (C.c_int32, [C.c_void_p, C.c_void_p]),
+    "odb_paged_layout": (C.c_int32, [C.c_void_p, C.POINTER(odb_paged_batch), C.c_void_p]),
+    "odb_rope_frequencies": (C.c_int32, [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double,
+                                         C.POINTER(C.c_uint64), C.POINTER(C.c_float)]),
+    "odb_paged_norm_rope_store": (C.c_int32, [C.c_void_p, C.c_int32, C.POINTER(odb_paged_batch), C.c_void_p, C.c_int64, C.c_void_p,
+                                              C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p,
+                                              C.c_int32, C.c_int32, C.c_float, C.c_void_p, C.c_int64, C.c_void_p]),
+    "odb_paged_attention": (C.c_int32, [C.c_void_p, C.c_int32, C.POINTER(odb_paged_batch), C.c_void_p, C.c_int64, C.c_void_p,
+                                        C.c_int64, C.c_void_p, C.c_float, C.c_int32, C.c_int32, C.c_int32, C.c_void_p]),
 }
 
 _lib = None

@@ -21,6 +21,12 @@ int32_t cuda_fail(cudaError_t e) {
     return ODB_ERR_CUDA;
 }
 
+}  // namespace
+
+int32_t odb::record_cuda_error(cudaError_t e) { return cuda_fail(e); }
+
+namespace {
+
 #define ODB_CUDA(call)                                   \
     do {                                                 \
         cudaError_t e__ = (call);                        \

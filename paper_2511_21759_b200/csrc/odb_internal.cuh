@@ -157,6 +157,8 @@ constexpr int kRowDecoded = 1;   // row_flags bit: the row's position is decoded
 // kernel launchers (each enqueues on `st`; returns cudaError_t of the launch)
 // ---------------------------------------------------------------------------------------
 
+int32_t record_cuda_error(cudaError_t e);   // keeps the text for odb_last_cuda_error; returns ODB_ERR_CUDA
+
 struct TmaEncoder;   // wraps the driver's tensor-map encode entry point
 
 // The row scalar of an RMSNorm folded behind a projection, kept as the partial sums of x^2 its producer
@@ -374,6 +376,9 @@ cudaError_t launch_tp_wait(const TpWait& tw, cudaStream_t st);
 cudaError_t make_weight_maps(WeightMaps* out, const void* w_packed, int N, int K);
 // bf16 [rows][cols] row-major; box = 64 columns x box_rows rows, 128-byte swizzle, rows beyond `rows` read as zero
 cudaError_t make_rows_tmap(CUtensorMap* out, const void* base, int rows, int cols, int box_rows);
+// the K/V pool bf16 [rows][hd] as boxes of box_rows rows: in shared memory [hd / 64][box_rows][64], 128-byte swizzle; rows beyond
+// `rows` read as zero
+cudaError_t make_pool_tmap(CUtensorMap* out, const void* kv, unsigned long long rows, int hd, int box_rows);
 size_t packed_weight_bytes(int N, int K);
 size_t packed_gate_up_bytes(int F, int K);
 cudaError_t make_gate_up_maps(WeightMaps* out, const void* w_packed, int F, int K);

@@ -1,0 +1,506 @@
+// Attention of the rows of each request over its pages of the K/V pool: few packed rows (query rows x heads of a group).
+//
+//   o = sum_j p_j v_j / sum_j p_j,  p_j = 2^(s_j - m),  s_j = log2(e) * scale * q.k_j,  lse = ln 2 * (m + log2 sum_j p_j)
+//
+// over the visible keys j < len, j <= pos + right, (j >= pos - left or j < sinks).  One pass over the keys with the running
+// maximum m and sum in fp32; P is rounded to bf16 for the second product (the sum keeps the unrounded values: the rounding's
+// relative error of up to 2^-8 per key is independent from key to key and ends below the output's own rounding).
+//
+// Work: see paged.cuh; every CTA takes the same number of key tiles of 64 positions.  One warp loads (TMA, a box per page of
+// a tile, 128-byte swizzle, a ring of stages with a full and an empty barrier each), four warps multiply (mma.sync m16n8k16):
+// ROWS / 16 groups of rows x 64 / ROWS groups of keys, each warp with a running maximum, sum and output of its own, which
+// meet when the item ends.  An item that several CTAs share leaves unnormalised parts in the workspace; the CTA that arrives
+// last adds them up in the order of the CTAs, whoever it is: the same bits every time.
+//
+// Rows of V behind the last visible key are whatever the page held before: their P is zero, but zero times an infinity or NaN
+// there is not, so they are set to zero in shared memory first.  A key that some rows of the tile see and others do not is
+// treated by the element: V's values that are not finite are taken out of the tile and given to the rows that see them.
+#include "paged.cuh"
+
+namespace odb {
+
+namespace {
+
+constexpr int kKT = 64;                    // keys per tile
+constexpr int kMmaWarps = 4;
+constexpr int kThreads = 32 * (kMmaWarps + 1);
+template <int HD> constexpr int kStages = HD == 128 ? 3 : 6;
+template <int HD> constexpr uint32_t kTileBytes = kKT * HD * 2;            // K or V of a tile
+template <int HD> constexpr uint32_t kMergeBytes = 2 * 16 * HD * 4;        // two warps' outputs
+template <int HD> constexpr uint32_t kSmem = 1024 + kStages<HD> * 2 * kTileBytes<HD> + kMergeBytes<HD> + 1024;
+
+struct Barriers {
+    uint64_t full[6], empty[6];
+    float ml[kMmaWarps][16][2];
+    int last, abort;
+};
+static_assert(sizeof(Barriers) <= 1024, "the barriers end inside the allocation");
+
+__device__ __forceinline__ void mbar_init(uint64_t* bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count));
+}
+__device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// a box of rows of the pool: all head dims of a row, 64 at a time
+__device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* tmap, uint64_t* bar, int row) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(smem_u32(bar)), "r"(0), "r"(row), "r"(0)
+        : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ void mma_warps_barrier() { asm volatile("bar.sync 1, %0;" ::"r"(32 * kMmaWarps) : "memory"); }
+// the warps with the same keys and other rows
+template <int WR>
+__device__ __forceinline__ void key_group_barrier(int wk) {
+    if constexpr (WR > 1) asm volatile("bar.sync %0, %1;" ::"r"(2 + wk), "r"(32 * WR) : "memory");
+    else __syncwarp();
+}
+__device__ __forceinline__ float quad_max(float x) {
+    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+    return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+    x += __shfl_xor_sync(0xffffffffu, x, 1);
+    return x + __shfl_xor_sync(0xffffffffu, x, 2);
+}
+// 2^(m - M) with M the larger of the two; a side that has seen nothing counts nothing
+__device__ __forceinline__ float weight(float m, float M) { return m == -INFINITY ? 0.f : ex2(m - M); }
+__device__ __forceinline__ bool odd_bf16(uint32_t two) {   // one of the two is an infinity or NaN
+    return (two & 0x7f80u) == 0x7f80u || (two & 0x7f800000u) == 0x7f800000u;
+}
+
+template <int HD, int ROWS>
+__global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __grid_constant__ CUtensorMap tm, const PagedAttnArgs a) {
+    constexpr int WR = ROWS / 16, WK = kMmaWarps / WR, KW = kKT / WK;   // warps along the rows and the keys, keys of a warp
+    constexpr int kAtoms = HD / 64, NS = KW / 8, ND = HD / 8;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    float* merge = reinterpret_cast<float*>(smem + kStages<HD> * 2 * kTileBytes<HD>);
+    Barriers* sh = reinterpret_cast<Barriers*>(smem + kStages<HD> * 2 * kTileBytes<HD> + kMergeBytes<HD>);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    volatile int* cta_abort = &sh->abort;
+
+    if (tid == 0) {
+        for (int i = 0; i < kStages<HD>; ++i) {
+            mbar_init(&sh->full[i], 1);
+            mbar_init(&sh->empty[i], kMmaWarps);
+        }
+        sh->abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    pdl_launch_dependents();
+    pdl_wait();
+    // the ring's memory holds the sums until the start is found
+    static_assert(sizeof(PagedScratch) <= 2 * kTileBytes<64>, "the scratch fits the ring");
+    PagedStart start;
+    const bool any = paged_find_start<kThreads, ROWS, kKT>(a, *reinterpret_cast<PagedScratch*>(smem), 2, start);
+    if (!any) return;                                           // block-uniform
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the scratch's writes before the copies that take its place
+    __syncthreads();
+
+    PagedWalk<ROWS, kKT> w(a, start);
+    const int box_shift = min(a.page_shift, 6), box = 1 << box_shift;   // rows of a copy
+    int stage = 0;
+    uint32_t phase = 0;
+
+    if (warp == kMmaWarps) {
+        // ================= loader =================
+        bool ok = true;
+        int issued = 0;
+        do {
+            for (int t = w.t0; t < w.t1 && ok; ++t) {
+                const int k0 = w.k.tile(t) << 6;
+                const int boxes = max(0, (min(kKT, w.k.hi - k0) + box - 1) >> box_shift);
+                // lanes 0 .. boxes - 1: K, the next ones: V
+                int row = a.pool_rows;                          // behind the pool: zeros
+                const bool mine = lane < 2 * boxes, is_v = lane >= boxes;
+                const int sub = is_v ? lane - boxes : lane;
+                if (mine) {
+                    const int pos = k0 + (sub << box_shift);
+                    const int page = a.table[static_cast<size_t>(w.seq) * a.table_stride + (pos >> a.page_shift)];
+                    if (page >= 0 && page < a.n_pages)
+                        row = (is_v ? a.v_row0 : a.k_row0) + ((page * a.KV + w.head) << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
+                }
+                if (issued >= kStages<HD>) ok = mbar_wait_bounded(&sh->empty[stage], phase ^ 1u, cta_abort, a.status);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                const uint32_t bytes = static_cast<uint32_t>(boxes) * box * HD * 2;
+                if (lane == 0) mbar_expect_tx(&sh->full[stage], 2 * bytes);
+                __syncwarp();
+                if (mine)
+                    tma_rows(smem_u32(smem) + (stage * 2 + (is_v ? 1 : 0)) * kTileBytes<HD> + sub * box * HD * 2, &tm, &sh->full[stage], row);
+                ++issued;
+                if (++stage == kStages<HD>) { stage = 0; phase ^= 1u; }
+            }
+        } while (ok && w.next());
+        if (!ok) {   // copies in flight land before the memory goes away
+            const long long t0 = clock64();
+            for (int j = max(0, issued - kStages<HD>); j < issued; ++j)
+                while (!mbar_try_wait_parity(&sh->full[j % kStages<HD>], static_cast<uint32_t>(j / kStages<HD>) & 1u) && clock64() - t0 < kWaitLimitCycles / 8) {
+                }
+        }
+        return;
+    }
+
+    // ================= the products =================
+    const int wr = warp % WR, wk = warp / WR;
+    const int r_lo = wr * 16 + (lane >> 2);                     // this thread's rows of the tile: r_lo and r_lo + 8
+    do {
+        const int rows = min(ROWS, w.q.n * a.G - w.rt * ROWS);  // packed rows of this item
+        uint32_t qf[HD / 16][4];
+        int pos[2];
+        size_t at[2];                                           // row of q, out and lse, in heads
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = min(r_lo + 8 * e, rows - 1), idx = w.rt * ROWS + r, i = idx / a.G;   // rows behind the last repeat it
+            pos[e] = w.q.first + i;
+            at[e] = static_cast<size_t>(w.q.row0 + i);
+            const __nv_bfloat16* qp = a.q + at[e] * a.q_stride + (w.head * a.G + idx - i * a.G) * HD + (lane & 3) * 2;
+#pragma unroll
+            for (int kk = 0; kk < HD / 16; ++kk) {
+                qf[kk][e] = *reinterpret_cast<const uint32_t*>(qp + kk * 16);
+                qf[kk][2 + e] = *reinterpret_cast<const uint32_t*>(qp + kk * 16 + 8);
+            }
+        }
+        const int idx_last = w.rt * ROWS + rows - 1;
+        const int p_min = w.q.first + w.rt * ROWS / a.G, p_max = w.q.first + idx_last / a.G;
+        float o[ND][4];
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[d][j] = 0.f;
+
+        for (int t = w.t0; t < w.t1; ++t) {
+            const int k0 = (w.k.tile(t) << 6) + wk * KW;        // this warp's first key
+            // Behind an expired wait the warp goes on through the tiles without their products: it must not be missing at a barrier.
+            const bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh->full[stage], phase, cta_abort, a.status));
+            const uint32_t sk = smem_u32(smem) + stage * 2 * kTileBytes<HD>, sv = sk + kTileBytes<HD>;
+            // key c of the tile, atom h: box (c >> box_shift), then [atom][row of the box][128 bytes]
+            auto key_at = [&](int c, int h) -> uint32_t {
+                return static_cast<uint32_t>((((c >> box_shift) * kAtoms + h) << box_shift) + (c & (box - 1))) * 128u;
+            };
+            const bool any_key = k0 < w.k.hi && (k0 + KW > w.k.lo || k0 < a.sinks);   // some row of the item sees some key
+            if (ok && any_key) {
+                float s[NS][4];
+#pragma unroll
+                for (int nb = 0; nb < NS; ++nb) s[nb][0] = s[nb][1] = s[nb][2] = s[nb][3] = 0.f;
+                const uint32_t sw = static_cast<uint32_t>(lane & 7) << 4;
+#pragma unroll
+                for (int nb = 0; nb < NS; nb += 2) {
+                    const int c = wk * KW + nb * 8 + (lane & 7) + ((lane >> 4) << 3);
+#pragma unroll
+                    for (int kk = 0; kk < HD / 16; ++kk) {
+                        uint32_t b[4];
+                        ldsm4(sk + key_at(c, kk >> 2) + (((kk & 3) * 32 + ((lane >> 3) & 1) * 16) ^ sw), b);
+                        mma(s[nb], qf[kk], b[0], b[1]);
+                        mma(s[nb + 1], qf[kk], b[2], b[3]);
+                    }
+                }
+                const bool whole = k0 + KW <= min(static_cast<long long>(w.q.len), static_cast<long long>(p_min) + a.right + 1) &&
+                                   (k0 >= p_max - a.left || k0 + KW <= a.sinks);
+                float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                for (int nb = 0; nb < NS; ++nb)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float x = s[nb][j] * a.scale_log2;
+                        if (!whole) {
+                            const int key = k0 + nb * 8 + (lane & 3) * 2 + (j & 1), p = pos[j >> 1];
+                            const bool seen = key < w.q.len && key - a.right <= p && (key + a.left >= p || key < a.sinks);
+                            x = seen ? x : -INFINITY;
+                        }
+                        s[nb][j] = x;
+                        top[j >> 1] = fmaxf(top[j >> 1], x);
+                    }
+                float factor[2], shift[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float mn = fmaxf(m[e], quad_max(top[e]));
+                    shift[e] = mn == -INFINITY ? 0.f : mn;
+                    factor[e] = weight(m[e], shift[e]);
+                    m[e] = mn;
+                }
+                float sum[2] = {0.f, 0.f};
+                uint32_t p[NS][2];
+#pragma unroll
+                for (int nb = 0; nb < NS; ++nb) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        s[nb][j] = ex2(s[nb][j] - shift[j >> 1]);
+                        sum[j >> 1] += s[nb][j];
+                    }
+                    p[nb][0] = pack_bf16(s[nb][0], s[nb][1]);
+                    p[nb][1] = pack_bf16(s[nb][2], s[nb][3]);
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) l[e] = l[e] * factor[e] + sum[e];
+                if (__any_sync(0xffffffffu, factor[0] != 1.f || factor[1] != 1.f)) {
+#pragma unroll
+                    for (int d = 0; d < ND; ++d)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) o[d][j] *= factor[j >> 1];
+                }
+                if (!whole) {
+                    // V in places that a row does not see: zero where no row sees it, by the element where it is not finite
+                    constexpr int kChunks = KW * HD / 8 / 32;   // 16-byte chunks of a lane
+                    bool odd = false;
+#pragma unroll 4
+                    for (int i = 0; i < kChunks; ++i) {
+                        const int c16 = i * 32 + lane, c = wk * KW + c16 / (HD / 8), ch = c16 % (HD / 8);
+                        const int key = k0 + c16 / (HD / 8);
+                        const uint32_t ad = sv + key_at(c, ch >> 3) + (((ch & 7) ^ (c & 7)) << 4);
+                        uint32_t v[4];
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(ad) : "memory");
+                        const bool out = key >= w.k.hi || (key < w.k.lo && key >= a.sinks);
+                        if (out)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(ad), "r"(0) : "memory");
+                        else
+                            odd = odd || odd_bf16(v[0]) || odd_bf16(v[1]) || odd_bf16(v[2]) || odd_bf16(v[3]);
+                    }
+                    odd = __any_sync(0xffffffffu, odd);
+                    key_group_barrier<WR>(wk);                  // all have looked
+                    if (odd) {
+#pragma unroll 1
+                        for (int kc = 0; kc < KW; ++kc) {       // rare: an infinity or NaN in V, seen by some of the rows
+                            const int key = k0 + kc, c = wk * KW + kc;
+                            float pr[2];
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {       // P of this thread's rows and this key, from the lane that has it
+                                float x = 0.f;
+#pragma unroll
+                                for (int nb = 0; nb < NS; ++nb)
+#pragma unroll
+                                    for (int j = 0; j < 2; ++j)
+                                        if (nb == kc >> 3 && j == (kc & 1)) x = s[nb][e * 2 + j];
+                                pr[e] = __shfl_sync(0xffffffffu, x, (lane & ~3) | ((kc & 7) >> 1));
+                            }
+#pragma unroll
+                            for (int d = 0; d < ND; ++d) {
+                                const int ch = d;
+                                const uint32_t ad = sv + key_at(c, ch >> 3) + (((ch & 7) ^ (c & 7)) << 4) + (lane & 3) * 4;
+                                uint32_t v;
+                                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(ad) : "memory");
+                                if (odd_bf16(v)) {
+                                    const float v0 = __uint_as_float(v << 16), v1 = __uint_as_float(v & 0xffff0000u);
+#pragma unroll
+                                    for (int e = 0; e < 2; ++e) {
+                                        const bool seen = key < w.q.len && key - a.right <= pos[e] && (key + a.left >= pos[e] || key < a.sinks);
+                                        if (seen && !isfinite(v0)) o[d][e * 2] += pr[e] * v0;
+                                        if (seen && !isfinite(v1)) o[d][e * 2 + 1] += pr[e] * v1;
+                                    }
+                                }
+                            }
+                        }
+                        key_group_barrier<WR>(wk);
+#pragma unroll 1
+                        for (int i = 0; i < KW * HD / 2 / 32; ++i) {
+                            const int c2 = i * 32 + lane, kc = c2 / (HD / 2), dd = c2 % (HD / 2), c = wk * KW + kc;
+                            const uint32_t ad = sv + key_at(c, dd >> 5) + ((((dd >> 2) & 7) ^ (c & 7)) << 4) + (dd & 3) * 4;
+                            uint32_t v;
+                            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(ad) : "memory");
+                            if ((v & 0x7f80u) == 0x7f80u) v &= 0xffff0000u;
+                            if ((v & 0x7f800000u) == 0x7f800000u) v &= 0xffffu;
+                            asm volatile("st.shared.b32 [%0], %1;" ::"r"(ad), "r"(v) : "memory");
+                        }
+                        key_group_barrier<WR>(wk);
+                    }
+                    __syncwarp();
+                }
+#pragma unroll
+                for (int kb = 0; kb < KW / 16; ++kb) {
+                    const uint32_t pa[4] = {p[2 * kb][0], p[2 * kb][1], p[2 * kb + 1][0], p[2 * kb + 1][1]};
+                    const int c = wk * KW + kb * 16 + (lane & 15);
+#pragma unroll
+                    for (int d = 0; d < ND; d += 2) {
+                        uint32_t b[4];
+                        ldsm4_t(sv + key_at(c, d >> 3) + ((((d & 7) + (lane >> 4)) * 16) ^ sw), b);
+                        mma(o[d], pa, b[0], b[1]);
+                        mma(o[d + 1], pa, b[2], b[3]);
+                    }
+                }
+                if (!whole) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // this warp's writes to V before the next copy into it
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh->empty[stage]);
+            if (++stage == kStages<HD>) { stage = 0; phase ^= 1u; }
+        }
+
+        // ---- the warps that share the rows meet ----
+#pragma unroll
+        for (int e = 0; e < 2; ++e) l[e] = quad_sum(l[e]);
+        if constexpr (WK > 1) {
+            if ((lane & 3) == 0) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    sh->ml[warp][(lane >> 2) + 8 * e][0] = m[e];
+                    sh->ml[warp][(lane >> 2) + 8 * e][1] = l[e];
+                }
+            }
+            mma_warps_barrier();
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float M = -INFINITY, L = 0.f;
+#pragma unroll
+                for (int g = 0; g < WK; ++g) M = fmaxf(M, sh->ml[g * WR + wr][(lane >> 2) + 8 * e][0]);
+#pragma unroll
+                for (int g = 0; g < WK; ++g) {
+                    const float* x = sh->ml[g * WR + wr][(lane >> 2) + 8 * e];
+                    L += weight(x[0], M) * x[1];
+                }
+                const float f = weight(m[e], M);
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    o[d][2 * e] *= f;
+                    o[d][2 * e + 1] *= f;
+                }
+                m[e] = M;
+                l[e] = L;
+            }
+#pragma unroll
+            for (int half = WK / 2; half >= 1; half >>= 1) {     // the upper half of the key groups hands over to the lower
+                float* mb = merge + (((wk % half) * WR + wr) * ND * 4) * 32 + lane;
+                if (wk >= half && wk < 2 * half) {
+#pragma unroll
+                    for (int d = 0; d < ND; ++d)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) mb[(d * 4 + j) * 32] = o[d][j];
+                }
+                mma_warps_barrier();
+                if (wk < half) {
+#pragma unroll
+                    for (int d = 0; d < ND; ++d)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) o[d][j] += mb[(d * 4 + j) * 32];
+                }
+                mma_warps_barrier();
+            }
+        }
+
+        // ---- results, or this CTA's part of them ----
+        const bool final = w.t0 == 0 && w.t1 == w.k.n;
+        const int slot = w.t0 > 0 ? 0 : 1;
+        const size_t part = (static_cast<size_t>(blockIdx.x) * kPagedMaxParts + slot) * ROWS;
+        if (wk == 0) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = r_lo + 8 * e;
+                if (r >= rows) continue;
+                if (final) {
+                    const int idx = w.rt * ROWS + r, head = w.head * a.G + idx % a.G;
+                    const float inv = l[e] == 0.f ? 0.f : 1.0f / l[e];
+                    __nv_bfloat16* op = a.out + at[e] * a.out_stride + head * HD + (lane & 3) * 2;
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) *reinterpret_cast<uint32_t*>(op + d * 8) = pack_bf16(o[d][2 * e] * inv, o[d][2 * e + 1] * inv);
+                    if (a.lse && (lane & 3) == 0) a.lse[at[e] * a.H + head] = l[e] == 0.f ? -INFINITY : (m[e] + log2f(l[e])) * 0.6931471805599453f;
+                } else {
+                    float* op = a.part_o + (part + r) * HD + (lane & 3) * 2;
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) *reinterpret_cast<float2*>(op + d * 8) = make_float2(o[d][2 * e], o[d][2 * e + 1]);
+                    if ((lane & 3) == 0) *reinterpret_cast<float2*>(a.part_ml + (part + r) * 2) = make_float2(m[e], l[e]);
+                }
+            }
+        }
+        if (!final) {
+            __threadfence();
+            mma_warps_barrier();
+            const long long ub = w.item_begin();
+            const int c0 = paged_owner(ub, start.total, start.ctas), c1 = paged_owner(ub + w.k.n - 1, start.total, start.ctas);
+            if (tid == 0) {
+                const bool last = atomicAdd(a.arrivals + c0, 1u) == static_cast<unsigned>(c1 - c0);
+                if (last) a.arrivals[c0] = 0;                    // for the next launch; an item is counted at the CTA it begins in
+                __threadfence();
+                sh->last = last;
+            }
+            mma_warps_barrier();
+            if (sh->last) {
+                constexpr int V = HD / 32;                       // dims of a lane
+                for (int r = warp; r < rows; r += kMmaWarps) {
+                    auto slot_of = [&](int c) { return (static_cast<size_t>(c) * kPagedMaxParts + (c == c0 ? 1 : 0)) * ROWS + r; };
+                    float M = -INFINITY;
+                    for (int c = c0 + lane; c <= c1; c += 32) M = fmaxf(M, __ldcg(a.part_ml + slot_of(c) * 2));
+#pragma unroll
+                    for (int d = 16; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+                    float L = 0.f, acc[V];
+#pragma unroll
+                    for (int j = 0; j < V; ++j) acc[j] = 0.f;
+#pragma unroll 4
+                    for (int c = c0; c <= c1; ++c) {
+                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(a.part_ml + slot_of(c) * 2));
+                        const float f = weight(ml.x, M);
+                        L += f * ml.y;
+                        const float* po = a.part_o + slot_of(c) * HD + lane * V;
+                        if constexpr (V == 4) {
+                            const float4 x = __ldcg(reinterpret_cast<const float4*>(po));
+                            acc[0] += f * x.x; acc[1] += f * x.y; acc[2] += f * x.z; acc[3] += f * x.w;
+                        } else {
+                            const float2 x = __ldcg(reinterpret_cast<const float2*>(po));
+                            acc[0] += f * x.x; acc[1] += f * x.y;
+                        }
+                    }
+                    const int idx = w.rt * ROWS + r, i = idx / a.G, head = w.head * a.G + idx - i * a.G;
+                    const size_t row = static_cast<size_t>(w.q.row0 + i);
+                    const float inv = L == 0.f ? 0.f : 1.0f / L;
+                    uint32_t* op = reinterpret_cast<uint32_t*>(a.out + row * a.out_stride + head * HD + lane * V);
+#pragma unroll
+                    for (int j = 0; j < V; j += 2) op[j / 2] = pack_bf16(acc[j] * inv, acc[j + 1] * inv);
+                    if (a.lse && lane == 0) a.lse[row * a.H + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+                }
+                mma_warps_barrier();                             // sh->last has been read by all
+            }
+        }
+    } while (w.next());
+}
+
+template <int HD, int ROWS>
+cudaError_t launch_few(const PagedAttnArgs& a, const CUtensorMap& tmap, int sms, cudaStream_t st) {
+    static std::atomic<unsigned long long> attr_done{0};
+    cudaError_t e = set_smem_limit_once(attr_done, paged_attention_kernel<HD, ROWS>, static_cast<int>(kSmem<HD>));
+    if (e != cudaSuccess) return e;
+    return launch_kernel(paged_attention_kernel<HD, ROWS>, dim3(2 * sms), dim3(kThreads), kSmem<HD>, st, tmap, a);
+}
+
+template <int HD>
+cudaError_t launch_hd(const PagedAttnArgs& a, const CUtensorMap& tmap, int max_new, int sms, cudaStream_t st) {
+    const long long rows = static_cast<long long>(max_new) * a.G;
+    if (rows <= 16) return launch_few<HD, 16>(a, tmap, sms, st);
+    if (rows <= 32) return launch_few<HD, 32>(a, tmap, sms, st);
+    return launch_few<HD, 64>(a, tmap, sms, st);
+}
+
+}  // namespace
+
+size_t paged_part_bytes(int hd) { return static_cast<size_t>(kPagedMaxCtas) * kPagedMaxParts * 64 * (hd + 2) * sizeof(float); }
+
+cudaError_t launch_paged_attention(const PagedAttnArgs& a, const CUtensorMap& tmap, int hd, int max_new, int sms, cudaStream_t st) {
+    if (sms < 1 || 2 * sms > kPagedMaxCtas) return cudaErrorInvalidValue;
+    return hd == 128 ? launch_hd<128>(a, tmap, max_new, sms, st) : launch_hd<64>(a, tmap, max_new, sms, st);
+}
+
+}  // namespace odb

@@ -1,0 +1,196 @@
+"""Object layer of the paged K/V cache (odb_paged_* of include/odb.h): owns or borrows the device buffers, checks what a
+pointer cannot say (types, devices, shapes, strides) and marshals arguments.  No arithmetic happens in this file.
+
+A forward over requests of different lengths, one layer after the other:
+
+    cache = PagedCache(n_layers, n_heads, n_kv_heads, head_dim, page_size, n_pages)
+    batch = Batch(cache, table=..., free_pages=..., len_before=..., len_after=..., first=..., count=..., max_rows=...)
+    cache.layout(batch)                                       # tables, slots, row maps: once a forward
+    for layer in range(n_layers):
+        q = cache.norm_rope_store(layer, batch, q, k, v, rope, q_gain=..., k_gain=...)
+        o = cache.attention(layer, batch, q, right=0)
+
+Every call is enqueued on the current stream of the cache's device and returns at once; status() waits and says what the
+device found.  A cache is used on one stream at a time: a call on another stream than the one before waits for that one.
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional
+
+import torch
+
+from . import binding as B
+
+SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+
+
+class Rope:
+    """Rotation of the first rot_dim values of a head: pairs (i, i + rot_dim / 2), or (2i, 2i + 1) where interleaved.
+    scaling: "none", "linear", "ntk" or "yarn" with a factor (odb_rope_frequencies)."""
+
+    def __init__(self, rot_dim: int, theta: float = 500000.0, *, interleaved: bool = False, scaling: str = "none", factor: float = 1.0,
+                 original_len: float = 8192, beta_slow: float = 1.0, beta_fast: float = 32.0, device="cuda"):
+        if scaling not in SCALINGS:
+            raise ValueError(f"scaling {scaling!r}: one of {', '.join(SCALINGS)}")
+        host = (C.c_uint64 * max(1, rot_dim // 2))()
+        mag = C.c_float()
+        B.check(B.lib().odb_rope_frequencies(rot_dim, theta, SCALINGS[scaling], factor, original_len, beta_slow, beta_fast, host,
+                                             C.byref(mag)), "odb_rope_frequencies")
+        self.rot_dim, self.interleaved, self.magnitude = rot_dim, interleaved, mag.value
+        # fractions of a turn per position, 64-bit patterns
+        self.turns = torch.tensor([C.c_int64(v).value for v in host], dtype=torch.int64, device=device)
+        self._tail = (self.turns.data_ptr(), rot_dim, 1 if interleaved else 0, mag.value)
+
+
+class Batch:
+    """The device arrays of one forward (odb_paged_batch); arrays that a call needs and that are not given are made here,
+    those that are given are used as they are: int32, contiguous, on the cache's device.  max_rows: rows of the forward
+    (known where row arrays are given); max_new: rows of the longest request, a hint (max_rows where not given)."""
+
+    _INPUTS = ("len_before", "len_after", "first", "count", "table", "free_pages", "row_start", "row_seq", "row_pos", "row_slot")
+
+    def __init__(self, cache: "PagedCache", *, table=None, free_pages=None, len_before=None, len_after=None, first=None, count=None,
+                 row_start=None, row_seq=None, row_pos=None, row_slot=None, max_rows: Optional[int] = None, max_new: Optional[int] = None):
+        given = dict(len_before=len_before, len_after=len_after, first=first, count=count, table=table, free_pages=free_pages,
+                     row_start=row_start, row_seq=row_seq, row_pos=row_pos, row_slot=row_slot)
+        for name, t in given.items():
+            if t is not None and (not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or t.device != cache.device or not t.is_contiguous()):
+                raise ValueError(f"{name}: a contiguous int32 tensor on {cache.device} is wanted")
+        seqs = {name: given[name].shape for name in ("len_before", "len_after", "first", "count") if given[name] is not None}
+        if table is not None:
+            if table.dim() != 2 or (table.shape[0] and table.shape[1] < 1):
+                raise ValueError("table: [requests][pages of the longest request]")
+            seqs["table"] = table.shape[:1]
+        if row_start is not None:
+            seqs["row_start"] = torch.Size([row_start.numel() - 1]) if row_start.dim() == 1 else row_start.shape
+        if len(set(seqs.values())) > 1 or any(len(v) != 1 for v in seqs.values()):
+            raise ValueError(f"one entry a request is wanted: {({k: tuple(v) for k, v in seqs.items()})}")
+        n_seqs = next(iter(seqs.values()))[0] if seqs else 0
+        rows = {given[n].numel() for n in ("row_seq", "row_pos", "row_slot") if given[n] is not None}
+        if len(rows | ({max_rows} - {None})) > 1:
+            raise ValueError("row_seq, row_pos and row_slot have max_rows entries")
+        if free_pages is not None and free_pages.numel() < cache.n_pages:
+            raise ValueError(f"free_pages: {cache.n_pages} entries are wanted")
+        self.n_seqs = n_seqs
+        self.max_rows = rows.pop() if rows else (max_rows or 0)
+        self.max_new = self.max_rows if max_new is None else max_new
+        new = lambda n: torch.empty(n, dtype=torch.int32, device=cache.device)
+        if given["row_start"] is None and seqs:
+            given["row_start"] = new(n_seqs + 1)
+        for name in ("row_seq", "row_pos", "row_slot"):
+            if given[name] is None:
+                given[name] = new(self.max_rows)
+        for name, t in given.items():
+            setattr(self, name, t)
+        self.cache = cache
+        self._c = B.odb_paged_batch(n_seqs, self.max_rows, self.max_new, table.shape[1] if table is not None else 1,
+                                    *[None if given[n] is None else given[n].data_ptr() for n in self._INPUTS])
+        self._ref = C.byref(self._c)
+
+
+class PagedCache:
+    """A pool of K/V pages (bf16 [n_layers][2][n_pages][n_kv_heads][page_size][head_dim]) and the calls over it.  kv: a
+    tensor of that shape to use; otherwise one is allocated (not cleared: what no request has written reaches no result)."""
+
+    def __init__(self, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, *, kv=None, device=None):
+        lib = B.lib()
+        self.cfg = B.odb_paged_config(n_layers, n_heads, n_kv_heads, head_dim, page_size, n_pages)
+        self.n_layers, self.n_heads, self.n_kv_heads, self.head_dim, self.page_size, self.n_pages = \
+            n_layers, n_heads, n_kv_heads, head_dim, page_size, n_pages
+        self.handle = C.c_void_p()
+        if not lib.odb_paged_kv_bytes(C.byref(self.cfg)):
+            raise B.OdbError(B.ODB_ERR_SHAPE, "odb_paged_create")
+        shape = (n_layers, 2, n_pages, n_kv_heads, page_size, head_dim)
+        if kv is None:
+            kv = torch.empty(shape, dtype=torch.bfloat16, device=device or "cuda")
+        elif tuple(kv.shape) != shape or kv.dtype != torch.bfloat16 or not kv.is_cuda or not kv.is_contiguous():
+            raise ValueError(f"kv: a contiguous bfloat16 CUDA tensor of shape {shape} is wanted")
+        self.kv = kv
+        self.device = kv.device
+        self.workspace = torch.empty(lib.odb_paged_workspace_bytes(C.byref(self.cfg)), dtype=torch.uint8, device=self.device)
+        stream = torch.cuda.current_stream(self.device)
+        with torch.cuda.device(self.device):
+            B.check(lib.odb_paged_create(C.byref(self.cfg), kv.data_ptr(), kv.numel() * 2, self.workspace.data_ptr(),
+                                         self.workspace.numel(), C.c_void_p(stream.cuda_stream), C.byref(self.handle)), "odb_paged_create")
+        self._stream = stream
+        self._layout, self._store, self._attention = lib.odb_paged_layout, lib.odb_paged_norm_rope_store, lib.odb_paged_attention
+
+    def close(self):
+        if self.handle:
+            B.lib().odb_paged_destroy(self.handle)
+            self.handle = C.c_void_p()
+
+    def _current(self) -> int:
+        """The current stream's handle; behind a call on another stream, that one's work comes first."""
+        st = torch.cuda.current_stream(self.device)
+        if st != self._stream:
+            if not torch.cuda.is_current_stream_capturing():
+                st.wait_stream(self._stream)
+            self._stream = st
+        return st.cuda_stream
+
+    def _rows(self, t, what: str, heads: int, rows: int):
+        """(pointer, elements from row to row) of [rows][heads][head_dim], the last two dims together or apart."""
+        width = heads * self.head_dim
+        if t.dtype is not torch.bfloat16 or t.device != self.device:
+            raise ValueError(f"{what}: a bfloat16 tensor on {self.device} is wanted")
+        shape, stride = t.shape, t.stride()
+        if len(shape) == 2:
+            ok = shape[1] == width and (width == 1 or stride[1] == 1)
+        else:
+            ok = len(shape) == 3 and shape[1] == heads and shape[2] == self.head_dim and stride[2] == 1 and (heads == 1 or stride[1] == self.head_dim)
+        if not ok or shape[0] != rows:
+            raise ValueError(f"{what}: [{rows}][{heads}][{self.head_dim}] with a row's values together is wanted, got {tuple(shape)} by {stride}")
+        return t.data_ptr(), stride[0] if rows > 1 else max(stride[0], width)
+
+    def _gain(self, t, what: str):
+        if t is None:
+            return None
+        if t.dtype is not torch.float32 or t.device != self.device or t.shape != (self.head_dim,) or not t.is_contiguous():
+            raise ValueError(f"{what}: a contiguous float32 tensor of {self.head_dim} values on {self.device} is wanted")
+        return t.data_ptr()
+
+    def layout(self, batch: Batch):
+        """Block tables, free list and row maps of the forward (odb_paged_layout); the batch's arrays are updated."""
+        B.check(self._layout(self.handle, batch._ref, self._current()), "odb_paged_layout")
+
+    def norm_rope_store(self, layer: int, batch: Batch, q, k, v, rope: Rope, *, q_gain=None, k_gain=None, eps: float = 1e-6, q_out=None):
+        """Norm of every q and k head (where a gain is given), rotation by row_pos, K and V into row_slot
+        (odb_paged_norm_rope_store).  q, k, v: [max_rows][heads][head_dim] or [max_rows][heads * head_dim], slices of one
+        projection's output as they are.  Returns q_out (a new tensor where none is given; q itself may be given)."""
+        rows = batch.max_rows
+        if q_out is None:
+            q_out = torch.empty(rows, self.n_heads, self.head_dim, dtype=torch.bfloat16, device=self.device)
+        if rope.turns.device != self.device:
+            raise ValueError(f"rope: on {self.device} it is wanted")
+        qp, qs = self._rows(q, "q", self.n_heads, rows)
+        kp, ks = self._rows(k, "k", self.n_kv_heads, rows)
+        vp, vs = self._rows(v, "v", self.n_kv_heads, rows)
+        op, os_ = self._rows(q_out, "q_out", self.n_heads, rows)
+        B.check(self._store(self.handle, layer, batch._ref, qp, qs, kp, ks, vp, vs, self._gain(q_gain, "q_gain"), self._gain(k_gain, "k_gain"),
+                            eps, *rope._tail, op, os_, self._current()), "odb_paged_norm_rope_store")
+        return q_out
+
+    def attention(self, layer: int, batch: Batch, q, *, left: int = -1, right: int = -1, sinks: int = 0, scale: float = 0.0, out=None, lse=None):
+        """Attention of the batch's rows over their requests' pages (odb_paged_attention): a row at position p sees the
+        keys j < len_after with j <= p + right and (j >= p - left or j < sinks); -1: no limit; causal: right=0.
+        scale 0: 1 / sqrt(head_dim).  lse: float32 [max_rows][n_heads] to be filled.  Returns out (a new tensor where none
+        is given)."""
+        rows = batch.max_rows
+        if out is None:
+            out = torch.empty(rows, self.n_heads, self.head_dim, dtype=torch.bfloat16, device=self.device)
+        qp, qs = self._rows(q, "q", self.n_heads, rows)
+        op, os_ = self._rows(out, "out", self.n_heads, rows)
+        lp = None
+        if lse is not None:
+            if lse.dtype is not torch.float32 or lse.device != self.device or lse.shape != (rows, self.n_heads) or not lse.is_contiguous():
+                raise ValueError(f"lse: a contiguous float32 tensor [{rows}][{self.n_heads}] on {self.device} is wanted")
+            lp = lse.data_ptr()
+        B.check(self._attention(self.handle, layer, batch._ref, qp, qs, op, os_, lp, scale, left, right, sinks, self._current()),
+                "odb_paged_attention")
+        return out
+
+    def status(self) -> int:
+        """Waits for the current stream; ODB_OK or what the device has found since the last call (read and cleared)."""
+        return B.lib().odb_paged_status(self.handle, self._current())
