@@ -376,9 +376,11 @@ cudaError_t launch_tp_wait(const TpWait& tw, cudaStream_t st);
 cudaError_t make_weight_maps(WeightMaps* out, const void* w_packed, int N, int K);
 // bf16 [rows][cols] row-major; box = 64 columns x box_rows rows, 128-byte swizzle, rows beyond `rows` read as zero
 cudaError_t make_rows_tmap(CUtensorMap* out, const void* base, int rows, int cols, int box_rows);
-// the K/V pool bf16 [rows][hd] as boxes of box_rows rows: in shared memory [hd / 64][box_rows][64], 128-byte swizzle; rows beyond
-// `rows` read as zero
-cudaError_t make_pool_tmap(CUtensorMap* out, const void* kv, unsigned long long rows, int hd, int box_rows);
+// the K/V pool bf16 [rows][hd] as boxes of box_rows rows x atoms 64 values: in shared memory [atom][box_rows][64], 128-byte swizzle;
+// rows beyond `rows` read as zero
+cudaError_t make_pool_tmap(CUtensorMap* out, const void* kv, unsigned long long rows, int hd, int box_rows, int atoms);
+// query rows bf16 [rows][heads][hd], `stride` elements from row to row, as boxes of `tokens` rows x `group` heads x 64 values
+cudaError_t make_group_tmap(CUtensorMap* out, const void* q, int rows, long long stride, int heads, int hd, int group, int tokens);
 size_t packed_weight_bytes(int N, int K);
 size_t packed_gate_up_bytes(int F, int K);
 cudaError_t make_gate_up_maps(WeightMaps* out, const void* w_packed, int F, int K);

@@ -8,6 +8,7 @@ namespace odb {
 
 constexpr int kPagedMaxSeqs = 1024;        // requests of one forward
 constexpr int kPagedMaxCtas = 304;         // CTAs of an attention launch, at most: two on each of the 148 SMs and a few
+constexpr int kPagedPartRows = 128;         // rows of a part with two CTAs on an SM; twice that with one
 constexpr int kPagedMaxParts = 2;          // unfinished segments a CTA leaves behind: of its first item and of its last
 constexpr int kPagedUnlimited = 1 << 30;   // a window side without limit; lengths and positions stay below it
 
@@ -48,16 +49,25 @@ struct PagedAttnArgs {
     float scale_log2;                                     // softmax scale x log2(e)
     int* status;
     unsigned int* arrivals;                               // [kPagedMaxCtas], zero between launches
-    float* part_o;                                        // [ctas][2][rows of a tile][HD]
-    float* part_ml;                                       // [ctas][2][rows of a tile][2]
+    float* part_o;                                        // [ctas][2][part_rows][HD]
+    float* part_ml;                                       // [ctas][2][part_rows][2]
+    int part_rows;                                        // rows of a tile
+    int tile_rows, tile_tokens;                           // many rows: packed rows of an item, query rows of a Q tile
+};
+// the pool's two maps: boxes of whole rows, and of 64 values of a row
+struct PagedMaps {
+    CUtensorMap rows, atoms;
 };
 // max_new: rows of the longest request; a hint that picks the kernel
-cudaError_t launch_paged_attention(const PagedAttnArgs& a, const CUtensorMap& tmap, int hd, int max_new, int sms, cudaStream_t st);
+cudaError_t launch_paged_attention(PagedAttnArgs a, const PagedMaps& maps, int hd, int max_new, int sms, cudaStream_t st);
+// many packed rows on the tensor cores (paged_attention_tc.cu); q_tiles: Q tiles of 128 rows a CTA takes
+cudaError_t launch_paged_attention_tc(PagedAttnArgs a, const PagedMaps& maps, int hd, int q_tiles, int sms, cudaStream_t st);
+constexpr int kPagedTcMaxGroup = 128;   // heads of a group that fit a Q tile
 size_t paged_part_bytes(int hd);
 
 #ifdef __CUDACC__
 // ---------------------------------------------------------------------------------------
-// The attention's work.  An item is one tile of up to ROWS packed rows (row i of a request and query head g of the
+// The attention's work.  An item is one tile of up to `rows` packed rows (row i of a request and query head g of the
 // group: packed row i * G + g) of one K/V head; its keys are cut into tiles of KT positions.  All key tiles of all
 // items in the order head, request, row tile, key tile are one line, which is divided evenly over the CTAs: whatever
 // the lengths, every CTA gets the same number of key tiles.
@@ -67,8 +77,7 @@ struct PagedSeq {
     int row0, n, first, len, n_rt;
 };
 
-template <int ROWS>
-__device__ __forceinline__ PagedSeq paged_seq(const PagedAttnArgs& a, int s) {
+__device__ __forceinline__ PagedSeq paged_seq(const PagedAttnArgs& a, int s, int rows) {
     PagedSeq q;
     const int r0 = min(max(a.row_start[s], 0), a.max_rows), r1 = min(a.row_start[s + 1], a.max_rows);
     q.row0 = r0;
@@ -76,7 +85,7 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedAttnArgs& a, int s) {
     q.first = min(max(a.first[s], -kPagedUnlimited), kPagedUnlimited - 1);
     // the table bounds the keys whatever the length says
     q.len = static_cast<int>(min(static_cast<long long>(max(a.len[s], 0)), static_cast<long long>(a.table_stride) << a.page_shift));
-    q.n_rt = static_cast<int>((static_cast<long long>(q.n) * a.G + ROWS - 1) / ROWS);
+    q.n_rt = static_cast<int>((static_cast<unsigned>(q.n) * static_cast<unsigned>(a.G) + rows - 1) / static_cast<unsigned>(rows));
     return q;
 }
 
@@ -88,9 +97,9 @@ struct PagedKeys {
     __device__ __forceinline__ int tile(int t) const { return t < sink_tiles ? t : first_tile + t - sink_tiles; }
 };
 
-template <int ROWS, int KT>
-__device__ __forceinline__ PagedKeys paged_keys(const PagedAttnArgs& a, const PagedSeq& q, int rt) {
-    const int i0 = rt * ROWS / a.G, i1 = min(q.n - 1, (rt * ROWS + ROWS - 1) / a.G);
+template <int KT>
+__device__ __forceinline__ PagedKeys paged_keys(const PagedAttnArgs& a, const PagedSeq& q, int rt, int rows) {
+    const int i0 = rt * rows / a.G, i1 = min(q.n - 1, (rt * rows + rows - 1) / a.G);
     PagedKeys k;
     k.hi = static_cast<int>(max(0ll, min(static_cast<long long>(q.len), static_cast<long long>(q.first) + i1 + a.right + 1)));
     k.lo = static_cast<int>(max(0ll, min(static_cast<long long>(k.hi), static_cast<long long>(q.first) + i0 - a.left)));
@@ -151,18 +160,18 @@ __device__ __forceinline__ int paged_upper(const int* v, int n, int x) {   // th
 
 // Called by all THREADS threads of the block; false: there is nothing for this CTA to do.
 // min_units: key tiles a CTA takes at least where there are fewer than the grid could share.
-template <int THREADS, int ROWS, int KT>
-__device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int min_units, PagedStart& st) {
+template <int THREADS, int KT>
+__device__ bool paged_find_start(const PagedAttnArgs& a, int rows, PagedScratch& sc, int min_units, PagedStart& st) {
     const int tid = threadIdx.x;
     long long total;
     {
         const int per = (a.n_seqs + THREADS - 1) / THREADS, s0 = min(tid * per, a.n_seqs), s1 = min(s0 + per, a.n_seqs);
         long long mine = 0;
-        for (int s = s0; s < s1; ++s) mine += paged_seq<ROWS>(a, s).n_rt;
+        for (int s = s0; s < s1; ++s) mine += paged_seq(a, s, rows).n_rt;
         long long at = paged_block_scan<THREADS>(mine, sc.warp_sum, total);
         for (int s = s0; s < s1; ++s) {
             sc.rt0[s] = static_cast<int>(at);
-            at += paged_seq<ROWS>(a, s).n_rt;
+            at += paged_seq(a, s, rows).n_rt;
         }
         if (tid == 0) sc.rt0[a.n_seqs] = static_cast<int>(total);
     }
@@ -175,13 +184,13 @@ __device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int m
         long long mine = 0;
         if (e0 < e1) {
             int s = paged_upper(sc.rt0, a.n_seqs + 1, e0 * group);
-            PagedSeq q = paged_seq<ROWS>(a, s);
+            PagedSeq q = paged_seq(a, s, rows);
             int rt = e0 * group - sc.rt0[s];
             for (int e = e0; e < e1; ++e) {
                 sc.sum[e] = static_cast<int>(mine);
                 for (int j = e * group; j < min((e + 1) * group, n_rt); ++j, ++rt) {
-                    while (rt >= q.n_rt) { q = paged_seq<ROWS>(a, ++s); rt = 0; }
-                    mine += paged_keys<ROWS, KT>(a, q, rt).n;
+                    while (rt >= q.n_rt) { q = paged_seq(a, ++s, rows); rt = 0; }
+                    mine += paged_keys<KT>(a, q, rt, rows).n;
                 }
             }
         }
@@ -202,11 +211,11 @@ __device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int m
     const int e = paged_upper(sc.sum, entries, rem);
     int j = e * group, left = rem - sc.sum[e];
     st.seq = paged_upper(sc.rt0, a.n_seqs + 1, j);
-    PagedSeq q = paged_seq<ROWS>(a, st.seq);
+    PagedSeq q = paged_seq(a, st.seq, rows);
     st.rt = j - sc.rt0[st.seq];
     for (;;) {
-        while (st.rt >= q.n_rt) { q = paged_seq<ROWS>(a, ++st.seq); st.rt = 0; }
-        const int n = paged_keys<ROWS, KT>(a, q, st.rt).n;
+        while (st.rt >= q.n_rt) { q = paged_seq(a, ++st.seq, rows); st.rt = 0; }
+        const int n = paged_keys<KT>(a, q, st.rt, rows).n;
         if (left < n) break;
         left -= n;
         ++st.rt;
@@ -217,19 +226,20 @@ __device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int m
 }
 
 // The items of a CTA's share, one after the other.
-template <int ROWS, int KT>
+template <int KT>
 struct PagedWalk {
     const PagedAttnArgs& a;
+    const int rows;
     PagedSeq q;
     PagedKeys k;
     int head, seq, rt;
     int t0, t1;                      // this CTA's key tiles of the item
     long long u, u1;                 // units left: [u, u1) from t0 on
 
-    __device__ __forceinline__ PagedWalk(const PagedAttnArgs& args, const PagedStart& st)
-        : a(args), head(st.head), seq(st.seq), rt(st.rt), t0(st.tile), u(st.u0), u1(st.u1) {
-        q = paged_seq<ROWS>(a, seq);
-        k = paged_keys<ROWS, KT>(a, q, rt);
+    __device__ __forceinline__ PagedWalk(const PagedAttnArgs& args, const PagedStart& st, int tile_rows)
+        : a(args), rows(tile_rows), head(st.head), seq(st.seq), rt(st.rt), t0(st.tile), u(st.u0), u1(st.u1) {
+        q = paged_seq(a, seq, rows);
+        k = paged_keys<KT>(a, q, rt, rows);
         t1 = static_cast<int>(min(static_cast<long long>(k.n), t0 + (u1 - u)));
     }
     __device__ __forceinline__ long long item_begin() const { return u - t0; }
@@ -241,14 +251,71 @@ struct PagedWalk {
         while (rt >= q.n_rt) {
             rt = 0;
             if (++seq == a.n_seqs) { seq = 0; ++head; }
-            q = paged_seq<ROWS>(a, seq);
+            q = paged_seq(a, seq, rows);
         }
-        k = paged_keys<ROWS, KT>(a, q, rt);
+        k = paged_keys<KT>(a, q, rt, rows);
         t0 = 0;
         t1 = static_cast<int>(min(static_cast<long long>(k.n), u1 - u));
         return true;
     }
 };
+
+// 2^x for x <= 0 on the special-function unit (flushes to zero far below zero, which is the wanted value)
+__device__ __forceinline__ float paged_ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// 2^(m - M) with M the larger of the two; a side that has seen nothing counts nothing
+__device__ __forceinline__ float paged_weight(float m, float M) { return m == -INFINITY ? 0.f : paged_ex2(m - M); }
+// log-sum-exp of a row from its shift in the log2 domain and its sum
+__device__ __forceinline__ float paged_lse(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f; }
+__device__ __forceinline__ uint32_t paged_bf16x2(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// A CTA's place for its part of an item that other CTAs share: parts [CTA][first or last item][row of the tile].
+__device__ __forceinline__ size_t paged_part(const PagedAttnArgs& a, int cta, bool begins) {
+    return (static_cast<size_t>(cta) * kPagedMaxParts + (begins ? 1 : 0)) * a.part_rows;
+}
+// Rows warp, warp + warps .. of an item's parts, which CTAs c0 .. c1 have written, added up in the order of the CTAs.
+template <int HD>
+__device__ __forceinline__ void paged_merge(const PagedAttnArgs& a, int row0, int head, int first_idx, int rows, int c0, int c1, int warp, int warps) {
+    constexpr int V = HD / 32;                       // dims of a lane
+    const int lane = threadIdx.x & 31;
+    for (int r = warp; r < rows; r += warps) {
+        auto slot_of = [&](int c) { return paged_part(a, c, c == c0) + r; };
+        float M = -INFINITY;
+        for (int c = c0 + lane; c <= c1; c += 32) M = fmaxf(M, __ldcg(a.part_ml + slot_of(c) * 2));
+#pragma unroll
+        for (int d = 16; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+        float L = 0.f, acc[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] = 0.f;
+#pragma unroll 4
+        for (int c = c0; c <= c1; ++c) {
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(a.part_ml + slot_of(c) * 2));
+            const float f = paged_weight(ml.x, M);
+            L += f * ml.y;
+            const float* po = a.part_o + slot_of(c) * HD + lane * V;
+            if constexpr (V == 4) {
+                const float4 x = __ldcg(reinterpret_cast<const float4*>(po));
+                acc[0] += f * x.x; acc[1] += f * x.y; acc[2] += f * x.z; acc[3] += f * x.w;
+            } else {
+                const float2 x = __ldcg(reinterpret_cast<const float2*>(po));
+                acc[0] += f * x.x; acc[1] += f * x.y;
+            }
+        }
+        const int idx = first_idx + r, i = idx / a.G, h = head * a.G + idx - i * a.G;
+        const size_t row = static_cast<size_t>(row0 + i);
+        const float inv = L == 0.f ? 0.f : 1.0f / L;
+        uint32_t* op = reinterpret_cast<uint32_t*>(a.out + row * a.out_stride + h * HD + lane * V);
+#pragma unroll
+        for (int j = 0; j < V; j += 2) op[j / 2] = paged_bf16x2(acc[j] * inv, acc[j + 1] * inv);
+        if (a.lse && lane == 0) a.lse[row * a.H + h] = paged_lse(M, L);
+    }
+}
 
 // the CTA whose share holds unit u
 __device__ __forceinline__ int paged_owner(long long u, long long total, int ctas) {

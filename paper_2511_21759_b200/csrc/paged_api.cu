@@ -15,7 +15,7 @@ struct odb_paged {
     unsigned int* arrivals;
     float *part_o, *part_ml;
     int pool_rows, layer_rows;      // rows of head_dim values: of the whole pool, of the K or the V of a layer
-    CUtensorMap tmap;
+    PagedMaps maps;
 };
 
 namespace {
@@ -83,7 +83,8 @@ int32_t odb_paged_create(const odb_paged_config* cfg, void* kv, size_t kv_bytes,
     cudaError_t e = cudaGetDevice(&h->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, h->device);
     if (e == cudaSuccess && 2 * h->sms > kPagedMaxCtas) h->sms = kPagedMaxCtas / 2;
-    if (e == cudaSuccess) e = make_pool_tmap(&h->tmap, kv, h->pool_rows, cfg->head_dim, cfg->page_size < 64 ? cfg->page_size : 64);
+    if (e == cudaSuccess) e = make_pool_tmap(&h->maps.rows, kv, h->pool_rows, cfg->head_dim, cfg->page_size < 64 ? cfg->page_size : 64, cfg->head_dim / 64);
+    if (e == cudaSuccess) e = make_pool_tmap(&h->maps.atoms, kv, h->pool_rows, cfg->head_dim, cfg->page_size < 64 ? cfg->page_size : 64, 1);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (e == cudaSuccess) e = cudaMemsetAsync(ws, 0, kStatusBytes + kArrivalBytes, st);
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
@@ -217,7 +218,7 @@ int32_t odb_paged_attention(odb_paged* h, int32_t layer, const odb_paged_batch* 
     a.sinks = sinks > kPagedUnlimited ? kPagedUnlimited : sinks;
     a.scale_log2 = (scale != 0.f ? scale : 1.0f / sqrtf(static_cast<float>(c.head_dim))) * 1.4426950408889634f;
     a.status = h->status; a.arrivals = h->arrivals; a.part_o = h->part_o; a.part_ml = h->part_ml;
-    return enqueued(launch_paged_attention(a, h->tmap, c.head_dim, b->max_new, h->sms, static_cast<cudaStream_t>(stream)));
+    return enqueued(launch_paged_attention(a, h->maps, c.head_dim, b->max_new, h->sms, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -65,15 +65,6 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
 __device__ __forceinline__ void mma_warps_barrier() { asm volatile("bar.sync 1, %0;" ::"r"(32 * kMmaWarps) : "memory"); }
 // the warps with the same keys and other rows
 template <int WR>
@@ -89,8 +80,6 @@ __device__ __forceinline__ float quad_sum(float x) {
     x += __shfl_xor_sync(0xffffffffu, x, 1);
     return x + __shfl_xor_sync(0xffffffffu, x, 2);
 }
-// 2^(m - M) with M the larger of the two; a side that has seen nothing counts nothing
-__device__ __forceinline__ float weight(float m, float M) { return m == -INFINITY ? 0.f : ex2(m - M); }
 __device__ __forceinline__ bool odd_bf16(uint32_t two) {   // one of the two is an infinity or NaN
     return (two & 0x7f80u) == 0x7f80u || (two & 0x7f800000u) == 0x7f800000u;
 }
@@ -119,12 +108,12 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
     // the ring's memory holds the sums until the start is found
     static_assert(sizeof(PagedScratch) <= 2 * kTileBytes<64>, "the scratch fits the ring");
     PagedStart start;
-    const bool any = paged_find_start<kThreads, ROWS, kKT>(a, *reinterpret_cast<PagedScratch*>(smem), 2, start);
+    const bool any = paged_find_start<kThreads, kKT>(a, ROWS, *reinterpret_cast<PagedScratch*>(smem), 2, start);
     if (!any) return;                                           // block-uniform
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the scratch's writes before the copies that take its place
     __syncthreads();
 
-    PagedWalk<ROWS, kKT> w(a, start);
+    PagedWalk<kKT> w(a, start, ROWS);
     const int box_shift = min(a.page_shift, 6), box = 1 << box_shift;   // rows of a copy
     int stage = 0;
     uint32_t phase = 0;
@@ -244,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                 for (int e = 0; e < 2; ++e) {
                     const float mn = fmaxf(m[e], quad_max(top[e]));
                     shift[e] = mn == -INFINITY ? 0.f : mn;
-                    factor[e] = weight(m[e], shift[e]);
+                    factor[e] = paged_weight(m[e], shift[e]);
                     m[e] = mn;
                 }
                 float sum[2] = {0.f, 0.f};
@@ -253,11 +242,11 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                 for (int nb = 0; nb < NS; ++nb) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        s[nb][j] = ex2(s[nb][j] - shift[j >> 1]);
+                        s[nb][j] = paged_ex2(s[nb][j] - shift[j >> 1]);
                         sum[j >> 1] += s[nb][j];
                     }
-                    p[nb][0] = pack_bf16(s[nb][0], s[nb][1]);
-                    p[nb][1] = pack_bf16(s[nb][2], s[nb][3]);
+                    p[nb][0] = paged_bf16x2(s[nb][0], s[nb][1]);
+                    p[nb][1] = paged_bf16x2(s[nb][2], s[nb][3]);
                 }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) l[e] = l[e] * factor[e] + sum[e];
@@ -372,9 +361,9 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
 #pragma unroll
                 for (int g = 0; g < WK; ++g) {
                     const float* x = sh->ml[g * WR + wr][(lane >> 2) + 8 * e];
-                    L += weight(x[0], M) * x[1];
+                    L += paged_weight(x[0], M) * x[1];
                 }
-                const float f = weight(m[e], M);
+                const float f = paged_weight(m[e], M);
 #pragma unroll
                 for (int d = 0; d < ND; ++d) {
                     o[d][2 * e] *= f;
@@ -405,8 +394,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
 
         // ---- results, or this CTA's part of them ----
         const bool final = w.t0 == 0 && w.t1 == w.k.n;
-        const int slot = w.t0 > 0 ? 0 : 1;
-        const size_t part = (static_cast<size_t>(blockIdx.x) * kPagedMaxParts + slot) * ROWS;
+        const size_t part = paged_part(a, blockIdx.x, w.t0 == 0);
         if (wk == 0) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -417,8 +405,8 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                     const float inv = l[e] == 0.f ? 0.f : 1.0f / l[e];
                     __nv_bfloat16* op = a.out + at[e] * a.out_stride + head * HD + (lane & 3) * 2;
 #pragma unroll
-                    for (int d = 0; d < ND; ++d) *reinterpret_cast<uint32_t*>(op + d * 8) = pack_bf16(o[d][2 * e] * inv, o[d][2 * e + 1] * inv);
-                    if (a.lse && (lane & 3) == 0) a.lse[at[e] * a.H + head] = l[e] == 0.f ? -INFINITY : (m[e] + log2f(l[e])) * 0.6931471805599453f;
+                    for (int d = 0; d < ND; ++d) *reinterpret_cast<uint32_t*>(op + d * 8) = paged_bf16x2(o[d][2 * e] * inv, o[d][2 * e + 1] * inv);
+                    if (a.lse && (lane & 3) == 0) a.lse[at[e] * a.H + head] = paged_lse(m[e], l[e]);
                 } else {
                     float* op = a.part_o + (part + r) * HD + (lane & 3) * 2;
 #pragma unroll
@@ -440,38 +428,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
             }
             mma_warps_barrier();
             if (sh->last) {
-                constexpr int V = HD / 32;                       // dims of a lane
-                for (int r = warp; r < rows; r += kMmaWarps) {
-                    auto slot_of = [&](int c) { return (static_cast<size_t>(c) * kPagedMaxParts + (c == c0 ? 1 : 0)) * ROWS + r; };
-                    float M = -INFINITY;
-                    for (int c = c0 + lane; c <= c1; c += 32) M = fmaxf(M, __ldcg(a.part_ml + slot_of(c) * 2));
-#pragma unroll
-                    for (int d = 16; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-                    float L = 0.f, acc[V];
-#pragma unroll
-                    for (int j = 0; j < V; ++j) acc[j] = 0.f;
-#pragma unroll 4
-                    for (int c = c0; c <= c1; ++c) {
-                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(a.part_ml + slot_of(c) * 2));
-                        const float f = weight(ml.x, M);
-                        L += f * ml.y;
-                        const float* po = a.part_o + slot_of(c) * HD + lane * V;
-                        if constexpr (V == 4) {
-                            const float4 x = __ldcg(reinterpret_cast<const float4*>(po));
-                            acc[0] += f * x.x; acc[1] += f * x.y; acc[2] += f * x.z; acc[3] += f * x.w;
-                        } else {
-                            const float2 x = __ldcg(reinterpret_cast<const float2*>(po));
-                            acc[0] += f * x.x; acc[1] += f * x.y;
-                        }
-                    }
-                    const int idx = w.rt * ROWS + r, i = idx / a.G, head = w.head * a.G + idx - i * a.G;
-                    const size_t row = static_cast<size_t>(w.q.row0 + i);
-                    const float inv = L == 0.f ? 0.f : 1.0f / L;
-                    uint32_t* op = reinterpret_cast<uint32_t*>(a.out + row * a.out_stride + head * HD + lane * V);
-#pragma unroll
-                    for (int j = 0; j < V; j += 2) op[j / 2] = pack_bf16(acc[j] * inv, acc[j + 1] * inv);
-                    if (a.lse && lane == 0) a.lse[row * a.H + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
-                }
+                paged_merge<HD>(a, w.q.row0, w.head, w.rt * ROWS, rows, c0, c1, warp, kMmaWarps);
                 mma_warps_barrier();                             // sh->last has been read by all
             }
         }
@@ -487,8 +444,7 @@ cudaError_t launch_few(const PagedAttnArgs& a, const CUtensorMap& tmap, int sms,
 }
 
 template <int HD>
-cudaError_t launch_hd(const PagedAttnArgs& a, const CUtensorMap& tmap, int max_new, int sms, cudaStream_t st) {
-    const long long rows = static_cast<long long>(max_new) * a.G;
+cudaError_t launch_hd(const PagedAttnArgs& a, const CUtensorMap& tmap, long long rows, int sms, cudaStream_t st) {
     if (rows <= 16) return launch_few<HD, 16>(a, tmap, sms, st);
     if (rows <= 32) return launch_few<HD, 32>(a, tmap, sms, st);
     return launch_few<HD, 64>(a, tmap, sms, st);
@@ -496,11 +452,14 @@ cudaError_t launch_hd(const PagedAttnArgs& a, const CUtensorMap& tmap, int max_n
 
 }  // namespace
 
-size_t paged_part_bytes(int hd) { return static_cast<size_t>(kPagedMaxCtas) * kPagedMaxParts * 64 * (hd + 2) * sizeof(float); }
+size_t paged_part_bytes(int hd) { return static_cast<size_t>(kPagedMaxCtas) * kPagedMaxParts * kPagedPartRows * (hd + 2) * sizeof(float); }
 
-cudaError_t launch_paged_attention(const PagedAttnArgs& a, const CUtensorMap& tmap, int hd, int max_new, int sms, cudaStream_t st) {
+cudaError_t launch_paged_attention(PagedAttnArgs a, const PagedMaps& maps, int hd, int max_new, int sms, cudaStream_t st) {
     if (sms < 1 || 2 * sms > kPagedMaxCtas) return cudaErrorInvalidValue;
-    return hd == 128 ? launch_hd<128>(a, tmap, max_new, sms, st) : launch_hd<64>(a, tmap, max_new, sms, st);
+    const long long rows = static_cast<long long>(max_new) * a.G;
+    if (rows > 64 && a.G <= kPagedTcMaxGroup) return launch_paged_attention_tc(a, maps, hd, rows > 128 ? 2 : 1, sms, st);
+    a.part_rows = 64;
+    return hd == 128 ? launch_hd<128>(a, maps.rows, rows, sms, st) : launch_hd<64>(a, maps.rows, rows, sms, st);
 }
 
 }  // namespace odb

@@ -298,6 +298,14 @@ ATT = [  # lens, rows (0: all), H, KV, D, page, mask
     ([130, 65, 64], 0, 6, 2, 64, 16, dict(right=0)),
     ([300], 0, 8, 2, 128, 256, dict(left=50, right=0, sinks=2)),
     ([210], 0, 3, 1, 128, 16, dict(left=40, right=40)),
+    ([1000, 33, 200], 32, 8, 2, 128, 32, {}),                      # 128 packed rows
+    ([700, 100], 25, 10, 2, 64, 16, dict(right=0)),                # 125 packed rows, groups of five
+    ([900, 64, 129], 20, 8, 2, 64, 128, dict(left=100, right=3, sinks=70)),
+    ([520], 0, 10, 2, 128, 64, dict(right=0)),
+    ([2000], 40, 4, 1, 64, 64, dict(left=300, right=0, sinks=130)),
+    ([300, 290], 0, 1, 1, 64, 32, dict(right=0)),
+    ([40], 0, 71, 1, 64, 16, dict(right=0)),
+    ([30], 0, 130, 1, 64, 16, dict(right=0)),                      # more heads in a group than a Q tile has rows
 ]
 
 
@@ -321,7 +329,7 @@ def test_attention(case):
 
 
 @requires_gpu
-@pytest.mark.parametrize("max_new", [1, 8, 64, 5000])
+@pytest.mark.parametrize("max_new", [1, 8, 16, 20, 64, 5000])
 def test_the_hint_decides_no_result(max_new):
     rng = np.random.default_rng(9)
     lens, counts = [90, 300, 20], [1, 37, 5]
@@ -354,7 +362,7 @@ def test_attention_rows_that_see_nothing_and_requests_without_rows_or_keys(new, 
 
 
 @requires_gpu
-@pytest.mark.parametrize("new,G", [(1, 4), (5, 2), (20, 1), (9, 4), (16, 4), (70, 2)])
+@pytest.mark.parametrize("new,G", [(1, 4), (5, 2), (20, 1), (9, 4), (16, 4), (20, 4), (70, 1), (70, 2), (100, 3)])
 @pytest.mark.parametrize("D", [64, 128])
 def test_attention_infinities_and_nan_reach_only_the_rows_that_see_them(new, G, D):
     rng = np.random.default_rng(new + D)
