@@ -279,42 +279,71 @@ __device__ __forceinline__ uint32_t paged_bf16x2(float a, float b) {
 __device__ __forceinline__ size_t paged_part(const PagedAttnArgs& a, int cta, bool begins) {
     return (static_cast<size_t>(cta) * kPagedMaxParts + (begins ? 1 : 0)) * a.part_rows;
 }
-// Rows warp, warp + warps .. of an item's parts, which CTAs c0 .. c1 have written, added up in the order of the CTAs.
-template <int HD>
-__device__ __forceinline__ void paged_merge(const PagedAttnArgs& a, int row0, int head, int first_idx, int rows, int c0, int c1, int warp, int warps) {
+// Rows of an item's parts, which CTAs c0 .. c1 have written, added up in the order of the CTAs with a running maximum: RB rows
+// of a warp at a time, so that their loads are in flight together.
+template <int HD, int RB>
+__device__ __forceinline__ void paged_merge_rows(const PagedAttnArgs& a, int row0, int head, int first_idx, int rows, int c0, int c1, int r0, int step) {
     constexpr int V = HD / 32;                       // dims of a lane
     const int lane = threadIdx.x & 31;
-    for (int r = warp; r < rows; r += warps) {
-        auto slot_of = [&](int c) { return paged_part(a, c, c == c0) + r; };
-        float M = -INFINITY;
-        for (int c = c0 + lane; c <= c1; c += 32) M = fmaxf(M, __ldcg(a.part_ml + slot_of(c) * 2));
+    float M[RB], L[RB], acc[RB][V];
 #pragma unroll
-        for (int d = 16; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-        float L = 0.f, acc[V];
+    for (int k = 0; k < RB; ++k) {
+        M[k] = -INFINITY;
+        L[k] = 0.f;
 #pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] = 0.f;
-#pragma unroll 4
-        for (int c = c0; c <= c1; ++c) {
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(a.part_ml + slot_of(c) * 2));
-            const float f = paged_weight(ml.x, M);
-            L += f * ml.y;
-            const float* po = a.part_o + slot_of(c) * HD + lane * V;
-            if constexpr (V == 4) {
-                const float4 x = __ldcg(reinterpret_cast<const float4*>(po));
-                acc[0] += f * x.x; acc[1] += f * x.y; acc[2] += f * x.z; acc[3] += f * x.w;
-            } else {
-                const float2 x = __ldcg(reinterpret_cast<const float2*>(po));
-                acc[0] += f * x.x; acc[1] += f * x.y;
+        for (int j = 0; j < V; ++j) acc[k][j] = 0.f;
+    }
+    constexpr int CU = 8 / RB;                       // parts in flight
+    for (int c = c0; c <= c1; c += CU) {
+        float2 ml[CU][RB];
+        float x[CU][RB][V];
+#pragma unroll
+        for (int u = 0; u < CU; ++u)
+#pragma unroll
+            for (int k = 0; k < RB; ++k) {
+                const size_t slot = paged_part(a, min(c + u, c1), c + u == c0) + min(r0 + k * step, rows - 1);
+                ml[u][k] = __ldcg(reinterpret_cast<const float2*>(a.part_ml + slot * 2));
+                const float* po = a.part_o + slot * HD + lane * V;
+                if constexpr (V == 4) {
+                    const float4 t = __ldcg(reinterpret_cast<const float4*>(po));
+                    x[u][k][0] = t.x; x[u][k][1] = t.y; x[u][k][2] = t.z; x[u][k][3] = t.w;
+                } else {
+                    const float2 t = __ldcg(reinterpret_cast<const float2*>(po));
+                    x[u][k][0] = t.x; x[u][k][1] = t.y;
+                }
+            }
+#pragma unroll
+        for (int u = 0; u < CU; ++u) {
+            if (c + u > c1) break;
+#pragma unroll
+            for (int k = 0; k < RB; ++k) {
+                const float m = fmaxf(M[k], ml[u][k].x), f = paged_weight(M[k], m), e = paged_weight(ml[u][k].x, m);
+                M[k] = m;
+                L[k] = L[k] * f + ml[u][k].y * e;
+#pragma unroll
+                for (int j = 0; j < V; ++j) acc[k][j] = acc[k][j] * f + x[u][k][j] * e;
             }
         }
+    }
+#pragma unroll
+    for (int k = 0; k < RB; ++k) {
+        const int r = r0 + k * step;
+        if (r >= rows) break;
         const int idx = first_idx + r, i = idx / a.G, h = head * a.G + idx - i * a.G;
         const size_t row = static_cast<size_t>(row0 + i);
-        const float inv = L == 0.f ? 0.f : 1.0f / L;
+        const float inv = L[k] == 0.f ? 0.f : 1.0f / L[k];
         uint32_t* op = reinterpret_cast<uint32_t*>(a.out + row * a.out_stride + h * HD + lane * V);
 #pragma unroll
-        for (int j = 0; j < V; j += 2) op[j / 2] = paged_bf16x2(acc[j] * inv, acc[j + 1] * inv);
-        if (a.lse && lane == 0) a.lse[row * a.H + h] = paged_lse(M, L);
+        for (int j = 0; j < V; j += 2) op[j / 2] = paged_bf16x2(acc[k][j] * inv, acc[k][j + 1] * inv);
+        if (a.lse && lane == 0) a.lse[row * a.H + h] = paged_lse(M[k], L[k]);
     }
+}
+template <int HD>
+__device__ __forceinline__ void paged_merge(const PagedAttnArgs& a, int row0, int head, int first_idx, int rows, int c0, int c1, int warp, int warps) {
+    if (rows > 4 * warps)
+        for (int r = warp; r < rows; r += 8 * warps) paged_merge_rows<HD, 8>(a, row0, head, first_idx, rows, c0, c1, r, warps);
+    else
+        for (int r = warp; r < rows; r += warps) paged_merge_rows<HD, 1>(a, row0, head, first_idx, rows, c0, c1, r, warps);
 }
 
 // the CTA whose share holds unit u

@@ -45,6 +45,12 @@ __device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
+// One lane of a converged warp: copies behind it take their operands from uniform registers at once.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t x;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(x));
+    return x != 0;
+}
 // a box of rows of the pool: all head dims of a row, 64 at a time
 __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* tmap, uint64_t* bar, int row) {
     asm volatile(
@@ -92,7 +98,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     float* merge = reinterpret_cast<float*>(smem + kStages<HD> * 2 * kTileBytes<HD>);
     Barriers* sh = reinterpret_cast<Barriers*>(smem + kStages<HD> * 2 * kTileBytes<HD> + kMergeBytes<HD>);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     volatile int* cta_abort = &sh->abort;
 
     if (tid == 0) {
@@ -140,10 +146,14 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 const uint32_t bytes = static_cast<uint32_t>(boxes) * box * HD * 2;
-                if (lane == 0) mbar_expect_tx(&sh->full[stage], 2 * bytes);
+                const uint32_t sg = __shfl_sync(0xffffffffu, stage, 0), dst = smem_u32(smem) + sg * 2 * kTileBytes<HD>;
+                if (elect_one()) mbar_expect_tx(&sh->full[sg], 2 * bytes);
                 __syncwarp();
-                if (mine)
-                    tma_rows(smem_u32(smem) + (stage * 2 + (is_v ? 1 : 0)) * kTileBytes<HD> + sub * box * HD * 2, &tm, &sh->full[stage], row);
+                for (int c = 0; c < 2 * boxes; ++c) {
+                    const int row_c = __shfl_sync(0xffffffffu, row, c);
+                    if (elect_one()) tma_rows(dst + (c < boxes ? c * box * HD * 2 : kTileBytes<HD> + (c - boxes) * box * HD * 2), &tm, &sh->full[sg], row_c);
+                    __syncwarp();
+                }
                 ++issued;
                 if (++stage == kStages<HD>) { stage = 0; phase ^= 1u; }
             }

@@ -61,6 +61,14 @@ __device__ __forceinline__ bool softmax_any(bool x) {
         : "memory");
     return r != 0;
 }
+// One lane of a converged warp.  The MMA and TMA instructions take their operands from uniform registers: behind elect, with
+// operands that every lane has, they follow one another without a detour (behind `lane == 0` an MMA took 110 cycles to issue, and
+// one of 128 x 64 x 16 runs for 32).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t x;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(x));
+    return x != 0;
+}
 template <int QT>
 __device__ __forceinline__ void softmax_barrier() { asm volatile("bar.sync 1, %0;" ::"r"(128 * QT) : "memory"); }
 
@@ -92,7 +100,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
     uint8_t* ring = sQ + QT * kQBytes<HD>;
     Shared* sh = reinterpret_cast<Shared*>(ring + kRing * kT);
     static_assert(kRing <= 16 && kB * kKT + HD <= static_cast<int>(kCols) && 4 * kPatch <= kQBytes<HD>, "ring, TMEM columns, patches");
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     volatile int* cta_abort = &sh->abort;
 
     if ((smem_u32(smem_raw) & 1023u) != 0) {                // the swizzled tiles need 1024-byte alignment
@@ -137,7 +145,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
     __syncthreads();
 
     auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait_bounded(bar, parity, cta_abort, a.status); };
-    const uint32_t tmem = sh->tmem_base;                    // per Q tile 256 columns: kB x 64 of S or P, then O
+    const uint32_t tmem = __shfl_sync(0xffffffffu, sh->tmem_base, 0);                    // per Q tile 256 columns: kB x 64 of S or P, then O
     auto tmem_o = [&](int g) { return tmem + g * kCols + kCols - HD; };
 
     if (any && warp == kSoftmaxWarps + 1) {
@@ -189,9 +197,14 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                     ok = __all_sync(0xffffffffu, wait(&sh->empty[slot], ph));
                     if (!ok) break;
                 }
-                if (lane == 0) mbar_expect_tx(&sh->full[slot], static_cast<uint32_t>(boxes) * box * 128);
+                const uint32_t sl = __shfl_sync(0xffffffffu, slot, 0), dst = smem_u32(ring) + sl * kT;
+                if (elect_one()) mbar_expect_tx(&sh->full[sl], static_cast<uint32_t>(boxes) * box * 128);
                 __syncwarp();
-                if (mine) tma_box_3d(smem_u32(ring) + slot * kT + at * kKT * 128 + sub * box * 128, &tm_kv, &sh->full[slot], 0, row, at);
+                for (int c = 0; c < boxes; ++c) {
+                    const int row_c = __shfl_sync(0xffffffffu, row, c), at_c = c % kAtoms, sub_c = c / kAtoms;
+                    if (elect_one()) tma_box_3d(dst + at_c * kKT * 128 + sub_c * box * 128, &tm_kv, &sh->full[sl], 0, row_c, at_c);
+                    __syncwarp();
+                }
                 ++issued;
                 if (++slot == kRing) { slot = 0; ph ^= 1u; }
             }
@@ -207,35 +220,36 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
             for (uint32_t j = issued > kRing ? issued - kRing : 0; j < issued; ++j) land(&sh->full[j % kRing], (j / kRing) & 1u);
         }
     } else if (any && warp == kSoftmaxWarps) {
-        // ================= MMA issuer =================
-        if (lane == 0) {
-            PagedWalk<kKT> w(a, start, a.tile_rows);
-            constexpr uint32_t idesc_s = instr_desc(kTQ, kKT, 0), idesc_o = instr_desc(kTQ, HD, 1);
-            const uint64_t q_desc = desc_k_major(smem_u32(sQ)), ring_k = desc_k_major(smem_u32(ring)), ring_v = desc_mn_major(smem_u32(ring), kKT * 128);
-            bool ok = true;
-            uint32_t item = 0, done = 0;                         // key tiles of the items before
-            int slot = 0;
-            uint32_t ph = 0;
-            auto next_slot = [&]() {
-                umma_commit(&sh->empty[slot]);
-                if (++slot == kRing) { slot = 0; ph ^= 1u; }
-            };
-            do {
-                const int n = w.t1 - w.t0;
-                if (item > 0) ok = wait(&sh->item_done, (item - 1) & 1u);   // O read; with it every MMA of the item has completed
-                if (ok) ok = wait(&sh->q_full, item & 1u);
-                // S of the item's tile t, for every Q tile: its buffer's P has been multiplied
-                auto issue_s = [&](int t) {
-                    if (!wait(&sh->full[slot], ph)) return false;
-                    const uint32_t gt = done + t, b = gt % kB;
-                    const uint64_t k_desc = ring_k + static_cast<uint32_t>(slot) * (kT >> 4);
+        // ================= MMA issuer: the whole warp walks and waits, one lane issues =================
+        PagedWalk<kKT> w(a, start, a.tile_rows);
+        constexpr uint32_t idesc_s = instr_desc(kTQ, kKT, 0), idesc_o = instr_desc(kTQ, HD, 1);
+        const uint64_t q_desc = desc_k_major(smem_u32(sQ)), ring_k = desc_k_major(smem_u32(ring)), ring_v = desc_mn_major(smem_u32(ring), kKT * 128);
+        bool ok = true;
+        uint32_t item = 0, done = 0;                             // key tiles of the items before
+        int slot = 0;
+        uint32_t ph = 0;
+        auto uniform = [](uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); };
+        auto all_wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
+        auto next_slot = [&]() {
+            if (++slot == kRing) { slot = 0; ph ^= 1u; }
+        };
+        do {
+            const int n = w.t1 - w.t0;
+            if (item > 0) ok = all_wait(&sh->item_done, (item - 1) & 1u);   // O read; with it every MMA of the item has completed
+            if (ok) ok = all_wait(&sh->q_full, item & 1u);
+            // S of the item's tile t, for every Q tile: its buffer's P has been multiplied
+            auto issue_s = [&](int t) {
+                if (!all_wait(&sh->full[slot], ph)) return false;
+                const uint32_t gt = done + t, b = uniform(gt % kB), sl = uniform(slot);
+                const uint64_t k_desc = ring_k + sl * (kT >> 4);
 #pragma unroll
-                    for (int g = 0; g < QT; ++g) {
-                        if (t >= kB) {
-                            const uint32_t pv = gt - kB;
-                            if (!wait(&sh->pv_done[g][pv & 1u], (pv >> 1) & 1u)) return false;
-                        }
-                        tc_fence_after();
+                for (int g = 0; g < QT; ++g) {
+                    if (t >= kB) {
+                        const uint32_t pv = gt - kB;
+                        if (!all_wait(&sh->pv_done[g][pv & 1u], (pv >> 1) & 1u)) return false;
+                    }
+                    tc_fence_after();
+                    if (elect_one()) {
 #pragma unroll
                         for (int kk = 0; kk < HD / 16; ++kk) {
                             const uint32_t atom = kk >> 2, within = (kk & 3) * 32;
@@ -243,35 +257,40 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                                  k_desc + ((atom * (kKT * 128) + within) >> 4), idesc_s, kk > 0 ? 1u : 0u);
                         }
                         umma_commit(&sh->s_full[g][b]);
+                        if (g == QT - 1) umma_commit(&sh->empty[sl]);
                     }
-                    next_slot();
-                    return true;
-                };
-                for (int t = 0; t < kFirst && t < n && ok; ++t) ok = issue_s(t);
-                for (int t = 0; t < n && ok; ++t) {
-                    if (t + kFirst < n) ok = issue_s(t + kFirst);
-                    if (ok) ok = wait(&sh->full[slot], ph);
-                    const uint32_t gt = done + t, b = gt % kB;
-                    const uint64_t v_desc = ring_v + static_cast<uint32_t>(slot) * (kT >> 4);
+                    __syncwarp();
+                }
+                next_slot();
+                return true;
+            };
+            for (int t = 0; t < kFirst && t < n && ok; ++t) ok = issue_s(t);
+            for (int t = 0; t < n && ok; ++t) {
+                if (t + kFirst < n) ok = issue_s(t + kFirst);
+                if (ok) ok = all_wait(&sh->full[slot], ph);
+                const uint32_t gt = done + t, b = uniform(gt % kB), sl = uniform(slot), last = t + 1 == n;
+                const uint64_t v_desc = ring_v + sl * (kT >> 4);
 #pragma unroll
-                    for (int g = 0; g < QT; ++g) {
-                        if (ok) ok = wait(&sh->p_full[g][b], (gt / kB) & 1u);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint32_t keep = t > 0 || *const_cast<volatile int*>(&sh->keep_o[g]) ? 1u : 0u;
+                for (int g = 0; g < QT; ++g) {
+                    if (ok) ok = all_wait(&sh->p_full[g][b], (gt / kB) & 1u);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t keep = uniform(t > 0 || *const_cast<volatile int*>(&sh->keep_o[g]) ? 1u : 0u);
+                    if (elect_one()) {
 #pragma unroll
                         for (int kk = 0; kk < kKT / 16; ++kk)
                             umma_ts(tmem_o(g), tmem + g * kCols + b * kKT + kk * 8, v_desc + kk * (2048 >> 4), idesc_o, kk > 0 ? 1u : keep);
                         umma_commit(&sh->pv_done[g][gt & 1u]);
-                        if (t + 1 == n) umma_commit(&sh->o_full[g]);
+                        if (last) umma_commit(&sh->o_full[g]);
+                        if (g == QT - 1) umma_commit(&sh->empty[sl]);
                     }
-                    if (ok) next_slot();
+                    __syncwarp();
                 }
-                done += n;
-                ++item;
-            } while (ok && w.next());
-        }
-        __syncwarp();
+                if (ok) next_slot();
+            }
+            done += n;
+            ++item;
+        } while (ok && w.next());
     } else if (any) {
         // ================= softmax: thread r of Q tile g = packed row r = TMEM lane r =================
         PagedWalk<kKT> w(a, start, a.tile_rows);
@@ -453,6 +472,13 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
             const uint32_t patch = smem_u32(sQ) + g * kQBytes<HD> + gw * kPatch;   // every MMA that reads this Q tile has completed
             const bool final = w.t0 == 0 && w.t1 == w.k.n;
             if (final) {
+                int at[8];                                               // head of rows lane / 8, lane / 8 + 4 .. of the warp, from the Q tile's first
+#pragma unroll
+                for (int it = 0; it < 8; ++it) {
+                    const int idx = row_w + it * 4 + (lane >> 3), i = idx / a.G;
+                    at[it] = i * static_cast<int>(a.out_stride / 8) + (idx - i * a.G) * (HD / 8);
+                }
+                uint4* out = reinterpret_cast<uint4*>(a.out + static_cast<size_t>(w.q.row0 + tok0) * a.out_stride + w.head * a.G * HD);
                 const float inv = l_row == 0.f ? 0.f : 1.0f / l_row;
                 if (a.lse && lane < left) {
                     const int idx = row_w + lane, i = idx / a.G;
@@ -468,9 +494,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
 #pragma unroll
                         for (int j = 0; j < 32; ++j) x[j] = 0u;
                     turn_rows(patch, lane, x, [&](int rr, int ch, const uint4& y) {
-                        const int idx = row_w + rr, i = idx / a.G;
-                        if (rr < left)
-                            *reinterpret_cast<uint4*>(a.out + static_cast<size_t>(w.q.row0 + tok0 + i) * a.out_stride + (w.head * a.G + idx - i * a.G) * HD + c * 64 + ch * 8) = y;
+                        if (rr < left) out[at[rr >> 2] + c * 8 + ch] = y;
                     });
                 }
             } else {
