@@ -37,6 +37,22 @@ struct PagedStoreArgs {
 cudaError_t launch_paged_store(const PagedStoreArgs& a, cudaStream_t st);
 
 // ---- attention (paged_attention.cu) ----
+// n / d for 0 <= n < 2^31 by a product: with l = ceil(log2 d) and m = floor(2^(31 + l) / d) + 1, which fits 32 bits, n m 2^-(31 + l)
+// exceeds n / d by less than 1 / d (Granlund and Montgomery, PLDI 1994).
+struct PagedDiv {
+    unsigned int mul, shift;
+    __host__ static PagedDiv by(unsigned int d) {
+        unsigned int l = 0;
+        while ((1ull << l) < d) ++l;
+        return PagedDiv{static_cast<unsigned int>((1ull << (31 + l)) / d + (d == 1 ? 0 : 1)), 31 + l};
+    }
+#ifdef __CUDACC__
+    __device__ __forceinline__ int operator()(int n) const {
+        return static_cast<int>((static_cast<unsigned long long>(static_cast<unsigned int>(n)) * mul) >> shift);
+    }
+#endif
+};
+
 struct PagedAttnArgs {
     const __nv_bfloat16* q;
     __nv_bfloat16* out;
@@ -52,6 +68,7 @@ struct PagedAttnArgs {
     float* part_o;                                        // [ctas][2][part_rows][HD]
     float* part_ml;                                       // [ctas][2][part_rows][2]
     int part_rows;                                        // rows of a tile
+    PagedDiv by_group, by_rows;                           // divisions by G and by the packed rows of an item
     int tile_rows, tile_tokens;                           // many rows: packed rows of an item, query rows of a Q tile
 };
 // the pool's two maps: boxes of whole rows, and of 64 values of a row
@@ -67,25 +84,27 @@ size_t paged_part_bytes(int hd);
 
 #ifdef __CUDACC__
 // ---------------------------------------------------------------------------------------
-// The attention's work.  An item is one tile of up to `rows` packed rows (row i of a request and query head g of the
+// The attention's work.  An item is one tile of up to a.tile_rows packed rows (row i of a request and query head g of the
 // group: packed row i * G + g) of one K/V head; its keys are cut into tiles of KT positions.  All key tiles of all
 // items in the order head, request, row tile, key tile are one line, which is divided evenly over the CTAs: whatever
-// the lengths, every CTA gets the same number of key tiles.
+// the lengths, every CTA gets the same share.  An item's first key tile has E units in front of it that stand for what
+// an item costs beside its tiles (fetching Q, writing results): a share that ends among them leaves the item to the next.
 // ---------------------------------------------------------------------------------------
 
 struct PagedSeq {
     int row0, n, first, len, n_rt;
+    __device__ __forceinline__ void tiles(const PagedAttnArgs& a) { n_rt = a.by_rows(n * a.G + a.tile_rows - 1); }
 };
 
-__device__ __forceinline__ PagedSeq paged_seq(const PagedAttnArgs& a, int s, int rows) {
+__device__ __forceinline__ PagedSeq paged_seq(const PagedAttnArgs& a, int s) {
     PagedSeq q;
     const int r0 = min(max(a.row_start[s], 0), a.max_rows), r1 = min(a.row_start[s + 1], a.max_rows);
     q.row0 = r0;
     q.n = max(r1 - r0, 0);
     q.first = min(max(a.first[s], -kPagedUnlimited), kPagedUnlimited - 1);
-    // the table bounds the keys whatever the length says
-    q.len = static_cast<int>(min(static_cast<long long>(max(a.len[s], 0)), static_cast<long long>(a.table_stride) << a.page_shift));
-    q.n_rt = static_cast<int>((static_cast<unsigned>(q.n) * static_cast<unsigned>(a.G) + rows - 1) / static_cast<unsigned>(rows));
+    // the table bounds the keys whatever the length says (its rows hold fewer than 2^30 positions)
+    q.len = min(max(a.len[s], 0), a.table_stride << a.page_shift);
+    q.tiles(a);
     return q;
 }
 
@@ -98,11 +117,14 @@ struct PagedKeys {
 };
 
 template <int KT>
-__device__ __forceinline__ PagedKeys paged_keys(const PagedAttnArgs& a, const PagedSeq& q, int rt, int rows) {
-    const int i0 = rt * rows / a.G, i1 = min(q.n - 1, (rt * rows + rows - 1) / a.G);
+__device__ __forceinline__ PagedKeys paged_keys(const PagedAttnArgs& a, const PagedSeq& q, int rt) {
+    const int i0 = a.by_group(rt * a.tile_rows), i1 = min(q.n - 1, a.by_group(rt * a.tile_rows + a.tile_rows - 1));
     PagedKeys k;
-    k.hi = static_cast<int>(max(0ll, min(static_cast<long long>(q.len), static_cast<long long>(q.first) + i1 + a.right + 1)));
-    k.lo = static_cast<int>(max(0ll, min(static_cast<long long>(k.hi), static_cast<long long>(q.first) + i0 - a.left)));
+    // first + i + right + 1 stays below 2^30 + 2^30 + rows and may pass 2^31: as unsigned it does not wrap
+    k.hi = max(0, q.first + i1 < 0 ? q.first + i1 + a.right + 1
+                                   : static_cast<int>(min(static_cast<unsigned>(q.len), static_cast<unsigned>(q.first + i1) + a.right + 1u)));
+    k.hi = min(k.hi, q.len);
+    k.lo = max(0, min(k.hi, q.first + i0 - a.left));
     const int end = (k.hi + KT - 1) / KT;
     k.first_tile = k.lo < k.hi ? k.lo / KT : end;
     k.sink_tiles = min((min(a.sinks, k.hi) + KT - 1) / KT, k.first_tile);
@@ -110,38 +132,38 @@ __device__ __forceinline__ PagedKeys paged_keys(const PagedAttnArgs& a, const Pa
     return k;
 }
 
-// Where a CTA's share of the line begins.
+// Where a CTA's share of the line begins: `off` units into an item; units [u0, u1), `chunk` a CTA.
 struct PagedStart {
-    int head, seq, rt, tile;         // the item, and the key tile inside it
-    long long u0, u1;                // its units [u0, u1) of
-    long long total;                 // this many, divided over
-    int ctas;                        // this many CTAs
+    int head, seq, rt, off;
+    int u0, u1, chunk;
 };
 
-constexpr int kPagedEntries = 1024;   // sums of key tiles kept while a CTA finds its start
+constexpr int kPagedEntries = 1024;   // sums of units kept while a CTA finds its start
 struct PagedScratch {
+    int4 seq[kPagedMaxSeqs];          // a request's row0, n, first, len
     int rt0[kPagedMaxSeqs + 1];       // row tiles before a request
-    int sum[kPagedEntries + 1];       // key tiles before a group of row tiles
+    int sum[kPagedEntries + 1];       // units before a group of row tiles
     long long warp_sum[32];
 };
 
 // exclusive sum over the block; every thread gets the total
-template <int THREADS>
-__device__ __forceinline__ long long paged_block_scan(long long v, long long* warp_sum, long long& total) {
+template <int THREADS, typename T>
+__device__ __forceinline__ T paged_block_scan(T v, long long* sums, T& total) {
+    T* warp_sum = reinterpret_cast<T*>(sums);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    long long x = v;
+    T x = v;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const long long y = __shfl_up_sync(0xffffffffu, x, d);
+        const T y = __shfl_up_sync(0xffffffffu, x, d);
         if (lane >= d) x += y;
     }
     __syncthreads();                  // the previous scan's sums have been read
     if (lane == 31) warp_sum[warp] = x;
     __syncthreads();
-    long long before = 0, all = 0;
+    T before = 0, all = 0;
 #pragma unroll
     for (int w = 0; w < THREADS / 32; ++w) {
-        const long long t = warp_sum[w];
+        const T t = warp_sum[w];
         if (w < warp) before += t;
         all += t;
     }
@@ -159,106 +181,147 @@ __device__ __forceinline__ int paged_upper(const int* v, int n, int x) {   // th
 }
 
 // Called by all THREADS threads of the block; false: there is nothing for this CTA to do.
-// min_units: key tiles a CTA takes at least where there are fewer than the grid could share.
-template <int THREADS, int KT>
-__device__ bool paged_find_start(const PagedAttnArgs& a, int rows, PagedScratch& sc, int min_units, PagedStart& st) {
+// min_units: what a CTA takes at least (more than E) where there is less than the grid could share.
+// The launcher's bounds on rows, requests and keys keep every sum below 2^31.
+template <int THREADS, int KT, int E>
+__device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int min_units, PagedStart& st) {
     const int tid = threadIdx.x;
-    long long total;
+    int n_rt;
+    auto kept = [&](int s) {          // the request's numbers, loaded once
+        const int4 v = sc.seq[s];
+        PagedSeq q{v.x, v.y, v.z, v.w, 0};
+        q.tiles(a);
+        return q;
+    };
     {
         const int per = (a.n_seqs + THREADS - 1) / THREADS, s0 = min(tid * per, a.n_seqs), s1 = min(s0 + per, a.n_seqs);
-        long long mine = 0;
-        for (int s = s0; s < s1; ++s) mine += paged_seq(a, s, rows).n_rt;
-        long long at = paged_block_scan<THREADS>(mine, sc.warp_sum, total);
+        int mine = 0;
+#pragma unroll 4
         for (int s = s0; s < s1; ++s) {
-            sc.rt0[s] = static_cast<int>(at);
-            at += paged_seq(a, s, rows).n_rt;
+            const PagedSeq q = paged_seq(a, s);
+            sc.seq[s] = make_int4(q.row0, q.n, q.first, q.len);
+            mine += q.n_rt;
         }
-        if (tid == 0) sc.rt0[a.n_seqs] = static_cast<int>(total);
+        int at = paged_block_scan<THREADS>(mine, sc.warp_sum, n_rt);
+        for (int s = s0; s < s1; ++s) {
+            sc.rt0[s] = at;
+            at += kept(s).n_rt;
+        }
+        if (tid == 0) sc.rt0[a.n_seqs] = n_rt;
     }
-    const int n_rt = static_cast<int>(total);      // rows x group fits: max_rows * H < 2^31
     if (n_rt == 0) return false;
     __syncthreads();
-    const int group = (n_rt + kPagedEntries - 1) / kPagedEntries, entries = (n_rt + group - 1) / group;
+    const int group = (n_rt + kPagedEntries - 1) / kPagedEntries, entries = group == 1 ? n_rt : (n_rt + group - 1) / group;
+    int per_head;
     {
         const int per = (entries + THREADS - 1) / THREADS, e0 = min(tid * per, entries), e1 = min(e0 + per, entries);
-        long long mine = 0;
+        int mine = 0;
         if (e0 < e1) {
             int s = paged_upper(sc.rt0, a.n_seqs + 1, e0 * group);
-            PagedSeq q = paged_seq(a, s, rows);
+            PagedSeq q = kept(s);
             int rt = e0 * group - sc.rt0[s];
             for (int e = e0; e < e1; ++e) {
-                sc.sum[e] = static_cast<int>(mine);
+                sc.sum[e] = mine;
                 for (int j = e * group; j < min((e + 1) * group, n_rt); ++j, ++rt) {
-                    while (rt >= q.n_rt) { q = paged_seq(a, ++s, rows); rt = 0; }
-                    mine += paged_keys<KT>(a, q, rt, rows).n;
+                    while (rt >= q.n_rt) { q = kept(++s); rt = 0; }
+                    mine += paged_keys<KT>(a, q, rt).n + E;
                 }
             }
         }
-        const long long before = paged_block_scan<THREADS>(mine, sc.warp_sum, total);
-        for (int e = e0; e < e1; ++e) sc.sum[e] += static_cast<int>(before);
+        const int before = paged_block_scan<THREADS>(mine, sc.warp_sum, per_head);
+        for (int e = e0; e < e1; ++e) sc.sum[e] += before;
         __syncthreads();
     }
-    // total key tiles of one head fit 31 bits: at most 2^31 / KT a row tile's keys and 2^31 packed rows would not, but the
-    // launcher bounds rows x keys
-    const long long per_head = total;
-    st.total = per_head * a.KV;
-    st.ctas = static_cast<int>(max(1ll, min(static_cast<long long>(gridDim.x), st.total / min_units)));
-    if (static_cast<int>(blockIdx.x) >= st.ctas) return false;
-    st.u0 = st.total * blockIdx.x / st.ctas;
-    st.u1 = st.total * (blockIdx.x + 1) / st.ctas;
-    st.head = static_cast<int>(st.u0 / per_head);
-    const int rem = static_cast<int>(st.u0 - st.head * per_head);
+    const int total = per_head * a.KV;
+    st.chunk = max(min_units, static_cast<int>((static_cast<unsigned>(total) + gridDim.x - 1) / gridDim.x));
+    if (static_cast<long long>(st.chunk) * blockIdx.x >= total) return false;
+    st.u0 = st.chunk * blockIdx.x;
+    st.u1 = total - st.u0 < st.chunk ? total : st.u0 + st.chunk;
+    st.head = st.u0 / per_head;
+    const int rem = st.u0 - st.head * per_head;
     const int e = paged_upper(sc.sum, entries, rem);
-    int j = e * group, left = rem - sc.sum[e];
+    const int j = e * group;
+    int left = rem - sc.sum[e];
     st.seq = paged_upper(sc.rt0, a.n_seqs + 1, j);
-    PagedSeq q = paged_seq(a, st.seq, rows);
+    PagedSeq q = kept(st.seq);
     st.rt = j - sc.rt0[st.seq];
     for (;;) {
-        while (st.rt >= q.n_rt) { q = paged_seq(a, ++st.seq, rows); st.rt = 0; }
-        const int n = paged_keys<KT>(a, q, st.rt, rows).n;
+        while (st.rt >= q.n_rt) { q = kept(++st.seq); st.rt = 0; }
+        const int n = paged_keys<KT>(a, q, st.rt).n + E;
         if (left < n) break;
         left -= n;
         ++st.rt;
     }
-    st.tile = left;
+    st.off = left;
     __syncthreads();                  // the scratch may be overwritten now
-    return st.u1 > st.u0;
+    return true;
 }
 
 // The items of a CTA's share, one after the other.
-template <int KT>
+template <int KT, int E>
 struct PagedWalk {
     const PagedAttnArgs& a;
-    const int rows;
     PagedSeq q;
     PagedKeys k;
     int head, seq, rt;
     int t0, t1;                      // this CTA's key tiles of the item
-    long long u, u1;                 // units left: [u, u1) from t0 on
+    int begin;                       // the unit of the item's first key tile
+    int u1, chunk;
 
-    __device__ __forceinline__ PagedWalk(const PagedAttnArgs& args, const PagedStart& st, int tile_rows)
-        : a(args), rows(tile_rows), head(st.head), seq(st.seq), rt(st.rt), t0(st.tile), u(st.u0), u1(st.u1) {
-        q = paged_seq(a, seq, rows);
-        k = paged_keys<KT>(a, q, rt, rows);
-        t1 = static_cast<int>(min(static_cast<long long>(k.n), t0 + (u1 - u)));
+    __device__ __forceinline__ PagedWalk(const PagedAttnArgs& args, const PagedStart& st)
+        : a(args), head(st.head), seq(st.seq), rt(st.rt), begin(st.u0 - st.off + E), u1(st.u1), chunk(st.chunk) {
+        q = paged_seq(a, seq);
+        k = paged_keys<KT>(a, q, rt);
+        t0 = max(0, st.off - E);
+        t1 = min(k.n, u1 - begin);
     }
-    __device__ __forceinline__ long long item_begin() const { return u - t0; }
     // to the next item; false: the share has ended
     __device__ __forceinline__ bool next() {
-        u += t1 - t0;
-        if (u >= u1) return false;
+        begin += k.n + E;
+        if (begin >= u1) return false;
         ++rt;
         while (rt >= q.n_rt) {
             rt = 0;
             if (++seq == a.n_seqs) { seq = 0; ++head; }
-            q = paged_seq(a, seq, rows);
+            q = paged_seq(a, seq);
         }
-        k = paged_keys<KT>(a, q, rt, rows);
+        k = paged_keys<KT>(a, q, rt);
         t0 = 0;
-        t1 = static_cast<int>(min(static_cast<long long>(k.n), u1 - u));
+        t1 = min(k.n, u1 - begin);
         return true;
     }
+    __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == k.n; }
+    // the CTAs that share the item
+    __device__ __forceinline__ int first_cta() const { return begin / chunk; }
+    __device__ __forceinline__ int last_cta() const { return (begin + k.n - 1) / chunk; }
 };
+
+// The pages of a request as a warp sees them: 32 entries of its table row at a time, one a lane.  Every lane calls row() with the
+// same position and gets the pool row of it (of head 0 behind `base`, the layer's K or V); of a page that is none, the row
+// behind the pool, which reads as zeros.
+struct PagedPages {
+    int seq = -1, first = 0, entry = 0;
+    __device__ __forceinline__ int row(const PagedAttnArgs& a, int s, int head, int pos, int base) {
+        const int p = pos >> a.page_shift;
+        if (s != seq || p < first || p >= first + 32) {
+            seq = s;
+            first = p;
+            const int mine = p + static_cast<int>(threadIdx.x & 31);
+            entry = mine < a.table_stride ? a.table[static_cast<size_t>(s) * a.table_stride + mine] : -1;
+        }
+        const int page = __shfl_sync(0xffffffffu, entry, p - first);
+        return page >= 0 && page < a.n_pages ? base + ((page * a.KV + head) << a.page_shift) + (pos & ((1 << a.page_shift) - 1)) : a.pool_rows;
+    }
+};
+
+// One lane of a converged warp.  TMA copies and MMAs take their operands from uniform registers: behind elect, with operands that
+// every lane has, they follow one another without a detour (behind `lane == 0` an MMA took 110 cycles to issue, and one of
+// 128 x 64 x 16 runs for 32).
+__device__ __forceinline__ bool paged_elect() {
+    uint32_t x;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(x));
+    return x != 0;
+}
 
 // 2^x for x <= 0 on the special-function unit (flushes to zero far below zero, which is the wanted value)
 __device__ __forceinline__ float paged_ex2(float x) {
@@ -293,7 +356,7 @@ __device__ __forceinline__ void paged_merge_rows(const PagedAttnArgs& a, int row
 #pragma unroll
         for (int j = 0; j < V; ++j) acc[k][j] = 0.f;
     }
-    constexpr int CU = 8 / RB;                       // parts in flight
+    constexpr int CU = RB == 1 ? 8 : 16 / RB;        // parts in flight
     for (int c = c0; c <= c1; c += CU) {
         float2 ml[CU][RB];
         float x[CU][RB][V];
@@ -329,7 +392,7 @@ __device__ __forceinline__ void paged_merge_rows(const PagedAttnArgs& a, int row
     for (int k = 0; k < RB; ++k) {
         const int r = r0 + k * step;
         if (r >= rows) break;
-        const int idx = first_idx + r, i = idx / a.G, h = head * a.G + idx - i * a.G;
+        const int idx = first_idx + r, i = a.by_group(idx), h = head * a.G + idx - i * a.G;
         const size_t row = static_cast<size_t>(row0 + i);
         const float inv = L[k] == 0.f ? 0.f : 1.0f / L[k];
         uint32_t* op = reinterpret_cast<uint32_t*>(a.out + row * a.out_stride + h * HD + lane * V);
@@ -346,10 +409,6 @@ __device__ __forceinline__ void paged_merge(const PagedAttnArgs& a, int row0, in
         for (int r = warp; r < rows; r += warps) paged_merge_rows<HD, 1>(a, row0, head, first_idx, rows, c0, c1, r, warps);
 }
 
-// the CTA whose share holds unit u
-__device__ __forceinline__ int paged_owner(long long u, long long total, int ctas) {
-    return static_cast<int>(((u + 1) * ctas - 1) / total);
-}
 #endif
 
 }  // namespace odb

@@ -198,11 +198,11 @@ int32_t odb_paged_attention(odb_paged* h, int32_t layer, const odb_paged_batch* 
     if (!q || !out || !b->len_after || !b->first || !b->row_start || !b->table) return ODB_ERR_ARG;
     const int64_t qw = static_cast<int64_t>(c.n_heads) * c.head_dim;
     if (q_stride < qw || out_stride < qw || ((q_stride | out_stride) & 7) || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4)) return ODB_ERR_ARG;
-    // sums of row tiles over the requests and of key tiles over the row tiles are 32-bit numbers
+    // sums of row tiles over the requests and of key tiles over the row tiles and heads are 32-bit numbers
     const int G = c.n_heads / c.n_kv_heads;
     const double tiles = static_cast<double>(b->max_rows) * G / 16 + 1;
     if (static_cast<double>(b->max_rows) * c.n_heads >= 2147483648.0 || tiles * b->n_seqs >= 2147483648.0 ||
-        (tiles + b->n_seqs) * (longest / 64 + 2) >= 2147483648.0)
+        (tiles + b->n_seqs) * c.n_kv_heads * (longest / 64 + 8) >= 2147483648.0)
         return ODB_ERR_SHAPE;
     PagedAttnArgs a{};
     a.q = static_cast<const __nv_bfloat16*>(q);

@@ -22,6 +22,7 @@ namespace odb {
 namespace {
 
 constexpr int kKT = 64;                    // keys per tile
+constexpr int kItem = 2;                    // key tiles that an item costs beside its own
 constexpr int kMmaWarps = 4;
 constexpr int kThreads = 32 * (kMmaWarps + 1);
 template <int HD> constexpr int kStages = HD == 128 ? 3 : 6;
@@ -44,12 +45,6 @@ __device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
 }
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-// One lane of a converged warp: copies behind it take their operands from uniform registers at once.
-__device__ __forceinline__ bool elect_one() {
-    uint32_t x;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(x));
-    return x != 0;
 }
 // a box of rows of the pool: all head dims of a row, 64 at a time
 __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* tmap, uint64_t* bar, int row) {
@@ -112,14 +107,14 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
     pdl_launch_dependents();
     pdl_wait();
     // the ring's memory holds the sums until the start is found
-    static_assert(sizeof(PagedScratch) <= 2 * kTileBytes<64>, "the scratch fits the ring");
+    static_assert(sizeof(PagedScratch) <= kStages<64> * 2 * kTileBytes<64>, "the scratch fits the ring");
     PagedStart start;
-    const bool any = paged_find_start<kThreads, kKT>(a, ROWS, *reinterpret_cast<PagedScratch*>(smem), 2, start);
+    const bool any = paged_find_start<kThreads, kKT, kItem>(a, *reinterpret_cast<PagedScratch*>(smem), kItem + 2, start);
     if (!any) return;                                           // block-uniform
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the scratch's writes before the copies that take its place
     __syncthreads();
 
-    PagedWalk<kKT> w(a, start, ROWS);
+    PagedWalk<kKT, kItem> w(a, start);
     const int box_shift = min(a.page_shift, 6), box = 1 << box_shift;   // rows of a copy
     int stage = 0;
     uint32_t phase = 0;
@@ -128,30 +123,22 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
         // ================= loader =================
         bool ok = true;
         int issued = 0;
+        PagedPages pages;
         do {
             for (int t = w.t0; t < w.t1 && ok; ++t) {
                 const int k0 = w.k.tile(t) << 6;
                 const int boxes = max(0, (min(kKT, w.k.hi - k0) + box - 1) >> box_shift);
-                // lanes 0 .. boxes - 1: K, the next ones: V
-                int row = a.pool_rows;                          // behind the pool: zeros
-                const bool mine = lane < 2 * boxes, is_v = lane >= boxes;
-                const int sub = is_v ? lane - boxes : lane;
-                if (mine) {
-                    const int pos = k0 + (sub << box_shift);
-                    const int page = a.table[static_cast<size_t>(w.seq) * a.table_stride + (pos >> a.page_shift)];
-                    if (page >= 0 && page < a.n_pages)
-                        row = (is_v ? a.v_row0 : a.k_row0) + ((page * a.KV + w.head) << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
-                }
-                if (issued >= kStages<HD>) ok = mbar_wait_bounded(&sh->empty[stage], phase ^ 1u, cta_abort, a.status);
-                ok = __all_sync(0xffffffffu, ok);
+                if (issued >= kStages<HD>) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh->empty[stage], phase ^ 1u, cta_abort, a.status));
                 if (!ok) break;
-                const uint32_t bytes = static_cast<uint32_t>(boxes) * box * HD * 2;
                 const uint32_t sg = __shfl_sync(0xffffffffu, stage, 0), dst = smem_u32(smem) + sg * 2 * kTileBytes<HD>;
-                if (elect_one()) mbar_expect_tx(&sh->full[sg], 2 * bytes);
+                if (paged_elect()) mbar_expect_tx(&sh->full[sg], 2u * boxes * box * HD * 2);
                 __syncwarp();
-                for (int c = 0; c < 2 * boxes; ++c) {
-                    const int row_c = __shfl_sync(0xffffffffu, row, c);
-                    if (elect_one()) tma_rows(dst + (c < boxes ? c * box * HD * 2 : kTileBytes<HD> + (c - boxes) * box * HD * 2), &tm, &sh->full[sg], row_c);
+                for (int c = 0; c < boxes; ++c) {
+                    const int row = pages.row(a, w.seq, w.head, k0 + (c << box_shift), a.k_row0), row_v = row == a.pool_rows ? row : row + (a.v_row0 - a.k_row0);
+                    if (paged_elect()) {
+                        tma_rows(dst + c * box * HD * 2, &tm, &sh->full[sg], row);
+                        tma_rows(dst + kTileBytes<HD> + c * box * HD * 2, &tm, &sh->full[sg], row_v);
+                    }
                     __syncwarp();
                 }
                 ++issued;
@@ -177,7 +164,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
         size_t at[2];                                           // row of q, out and lse, in heads
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const int r = min(r_lo + 8 * e, rows - 1), idx = w.rt * ROWS + r, i = idx / a.G;   // rows behind the last repeat it
+            const int r = min(r_lo + 8 * e, rows - 1), idx = w.rt * ROWS + r, i = a.by_group(idx);   // rows behind the last repeat it
             pos[e] = w.q.first + i;
             at[e] = static_cast<size_t>(w.q.row0 + i);
             const __nv_bfloat16* qp = a.q + at[e] * a.q_stride + (w.head * a.G + idx - i * a.G) * HD + (lane & 3) * 2;
@@ -188,7 +175,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
             }
         }
         const int idx_last = w.rt * ROWS + rows - 1;
-        const int p_min = w.q.first + w.rt * ROWS / a.G, p_max = w.q.first + idx_last / a.G;
+        const int p_min = w.q.first + a.by_group(w.rt * ROWS), p_max = w.q.first + a.by_group(idx_last);
         float o[ND][4];
         float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
@@ -403,7 +390,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
         }
 
         // ---- results, or this CTA's part of them ----
-        const bool final = w.t0 == 0 && w.t1 == w.k.n;
+        const bool final = w.whole();
         const size_t part = paged_part(a, blockIdx.x, w.t0 == 0);
         if (wk == 0) {
 #pragma unroll
@@ -411,7 +398,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                 const int r = r_lo + 8 * e;
                 if (r >= rows) continue;
                 if (final) {
-                    const int idx = w.rt * ROWS + r, head = w.head * a.G + idx % a.G;
+                    const int idx = w.rt * ROWS + r, head = w.head * a.G + idx - a.by_group(idx) * a.G;
                     const float inv = l[e] == 0.f ? 0.f : 1.0f / l[e];
                     __nv_bfloat16* op = a.out + at[e] * a.out_stride + head * HD + (lane & 3) * 2;
 #pragma unroll
@@ -428,8 +415,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
         if (!final) {
             __threadfence();
             mma_warps_barrier();
-            const long long ub = w.item_begin();
-            const int c0 = paged_owner(ub, start.total, start.ctas), c1 = paged_owner(ub + w.k.n - 1, start.total, start.ctas);
+            const int c0 = w.first_cta(), c1 = w.last_cta();
             if (tid == 0) {
                 const bool last = atomicAdd(a.arrivals + c0, 1u) == static_cast<unsigned>(c1 - c0);
                 if (last) a.arrivals[c0] = 0;                    // for the next launch; an item is counted at the CTA it begins in
@@ -446,10 +432,12 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
 }
 
 template <int HD, int ROWS>
-cudaError_t launch_few(const PagedAttnArgs& a, const CUtensorMap& tmap, int sms, cudaStream_t st) {
+cudaError_t launch_few(PagedAttnArgs a, const CUtensorMap& tmap, int sms, cudaStream_t st) {
     static std::atomic<unsigned long long> attr_done{0};
     cudaError_t e = set_smem_limit_once(attr_done, paged_attention_kernel<HD, ROWS>, static_cast<int>(kSmem<HD>));
     if (e != cudaSuccess) return e;
+    a.tile_rows = ROWS;
+    a.by_rows = PagedDiv::by(ROWS);
     return launch_kernel(paged_attention_kernel<HD, ROWS>, dim3(2 * sms), dim3(kThreads), kSmem<HD>, st, tmap, a);
 }
 
@@ -466,6 +454,7 @@ size_t paged_part_bytes(int hd) { return static_cast<size_t>(kPagedMaxCtas) * kP
 
 cudaError_t launch_paged_attention(PagedAttnArgs a, const PagedMaps& maps, int hd, int max_new, int sms, cudaStream_t st) {
     if (sms < 1 || 2 * sms > kPagedMaxCtas) return cudaErrorInvalidValue;
+    a.by_group = PagedDiv::by(a.G);
     const long long rows = static_cast<long long>(max_new) * a.G;
     if (rows > 64 && a.G <= kPagedTcMaxGroup) return launch_paged_attention_tc(a, maps, hd, rows > 128 ? 2 : 1, sms, st);
     a.part_rows = 64;

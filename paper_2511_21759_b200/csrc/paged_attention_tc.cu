@@ -24,24 +24,30 @@ namespace {
 
 constexpr int kTQ = 128;   // packed rows of a Q tile (MMA M)
 constexpr int kKT = 64;    // keys of a tile
-template <int QT> constexpr int kThreads = 32 * (4 * QT + 2);
+template <int QT> constexpr int kThreads = 32 * (5 * QT + 1);   // four softmax warps and an MMA warp a Q tile, a loader
+constexpr int kItem = 4;   // key tiles that an item costs beside its own
 template <int HD> constexpr uint32_t kQBytes = kTQ * HD * 2;
 template <int HD> constexpr uint32_t kTileBytes = kKT * HD * 2;
-template <int HD, int QT> constexpr int kSlots = HD == 128 ? (QT == 1 ? 5 : 10) : (QT == 1 ? 10 : 16);
-template <int HD, int QT> constexpr uint32_t kSmem = QT * kQBytes<HD> + kSlots<HD, QT> * kTileBytes<HD> + 512;
+// Q buffers: with two the next item's Q tiles and first scores are there when an item ends; the larger Q tiles of two CTAs on an SM
+// leave no room for it.  K and V tiles in rings of their own.
+template <int HD, int QT> constexpr int kQBufs = HD == 128 && QT == 1 ? 1 : 2;
+template <int HD, int QT> constexpr int kKSlots = HD == 128 ? 3 : (QT == 1 ? 5 : 8);
+template <int HD, int QT> constexpr int kVSlots = HD == 128 ? (QT == 1 ? 2 : 3) : (QT == 1 ? 5 : 8);
+template <int HD, int QT>
+constexpr uint32_t kSmem = kQBufs<HD, QT> * QT * kQBytes<HD> + (kKSlots<HD, QT> + kVSlots<HD, QT>) * kTileBytes<HD> + 512;
 template <int HD> constexpr int kBufs = HD == 128 ? 2 : 3;   // S / P buffers of a Q tile: 256 columns, of which O takes HD
 constexpr uint32_t kCols = 256;
 constexpr uint32_t kPatch = 4096;                            // per softmax warp, in the Q tile: 32 rows x 128 bytes of output
 
 struct alignas(8) Shared {
-    uint64_t q_full;             // the item's Q tiles landed                     (loader -> MMA)
-    uint64_t full[16];           // K or V tile landed in the ring's slot         (loader -> MMA, softmax)
-    uint64_t empty[16];          // the MMAs have read the slot                   (MMA -> loader)
-    uint64_t s_full[2][3];       // S of Q tile g into buffer i has completed     (MMA -> softmax)
-    uint64_t p_full[2][3];       // P has taken its place                         (softmax -> MMA, 4 arrivals)
-    uint64_t pv_done[2][2];      // O += P V of an even / odd tile has completed  (MMA -> MMA, softmax)
-    uint64_t o_full[2];          // the item's last one has                       (MMA -> softmax)
-    uint64_t item_done;          // O and the Q tiles may be overwritten          (softmax -> loader, MMA, 4 QT arrivals)
+    uint64_t q_full[2];                // an item's Q tiles landed in the buffer          (loader -> MMA)
+    uint64_t k_full[8], v_full[8];     // K or V tile landed in the ring's slot           (loader -> MMA, softmax)
+    uint64_t k_empty[8], v_empty[8];   // the MMAs have read the slot                     (MMA -> loader, QT arrivals)
+    uint64_t s_full[2][3];             // S of Q tile g into buffer i has completed       (MMA -> softmax)
+    uint64_t p_full[2][3];             // P has taken its place                           (softmax -> MMA, 4 arrivals)
+    uint64_t pv_done[2][2];            // O += P V of an even / odd tile has completed    (MMA -> MMA, softmax)
+    uint64_t o_full[2];                // the item's last one has                         (MMA -> softmax)
+    uint64_t item_done[2];             // the Q buffer may be overwritten                 (softmax -> loader, 4 QT arrivals)
     uint32_t tmem_base;
     int abort, last, keep_o[2];
 };
@@ -60,14 +66,6 @@ __device__ __forceinline__ bool softmax_any(bool x) {
         : "r"(static_cast<int>(x)), "r"(128 * QT)
         : "memory");
     return r != 0;
-}
-// One lane of a converged warp.  The MMA and TMA instructions take their operands from uniform registers: behind elect, with
-// operands that every lane has, they follow one another without a detour (behind `lane == 0` an MMA took 110 cycles to issue, and
-// one of 128 x 64 x 16 runs for 32).
-__device__ __forceinline__ bool elect_one() {
-    uint32_t x;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(x));
-    return x != 0;
 }
 template <int QT>
 __device__ __forceinline__ void softmax_barrier() { asm volatile("bar.sync 1, %0;" ::"r"(128 * QT) : "memory"); }
@@ -91,15 +89,17 @@ __device__ __forceinline__ bool not_finite(uint32_t bf) { return (bf & 0x7f80u) 
 
 template <int HD, int QT>
 __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
-    paged_attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_kv, const PagedAttnArgs a) {
+    paged_attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_rows,
+                              const __grid_constant__ CUtensorMap tm_atoms, const PagedAttnArgs a) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
-    constexpr int kRing = kSlots<HD, QT>, kB = kBufs<HD>, kFirst = kB - 1, kAtoms = HD / 64;
+    constexpr int NQ = kQBufs<HD, QT>, KS = kKSlots<HD, QT>, VS = kVSlots<HD, QT>, kB = kBufs<HD>, kFirst = kB - 1, kAtoms = HD / 64;
     constexpr uint32_t kT = kTileBytes<HD>;
     constexpr int kSoftmaxWarps = 4 * QT;
-    uint8_t* sQ = smem_raw;
-    uint8_t* ring = sQ + QT * kQBytes<HD>;
-    Shared* sh = reinterpret_cast<Shared*>(ring + kRing * kT);
-    static_assert(kRing <= 16 && kB * kKT + HD <= static_cast<int>(kCols) && 4 * kPatch <= kQBytes<HD>, "ring, TMEM columns, patches");
+    uint8_t* sQ = smem_raw;                                  // [buffer][Q tile]
+    uint8_t* sK = sQ + NQ * QT * kQBytes<HD>;
+    uint8_t* sV = sK + KS * kT;
+    Shared* sh = reinterpret_cast<Shared*>(sV + VS * kT);
+    static_assert(KS <= 8 && VS <= 8 && kB * kKT + HD <= static_cast<int>(kCols) && 4 * kPatch <= kQBytes<HD>, "rings, TMEM columns, patches");
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     volatile int* cta_abort = &sh->abort;
 
@@ -109,10 +109,17 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
         return;
     }
     if (tid == 0) {
-        mbar_init(&sh->q_full, 1);
-        for (int i = 0; i < kRing; ++i) {
-            mbar_init(&sh->full[i], 1);
-            mbar_init(&sh->empty[i], 1);
+        for (int i = 0; i < NQ; ++i) {
+            mbar_init(&sh->q_full[i], 1);
+            mbar_init(&sh->item_done[i], kSoftmaxWarps);
+        }
+        for (int i = 0; i < KS; ++i) {
+            mbar_init(&sh->k_full[i], 1);
+            mbar_init(&sh->k_empty[i], QT);
+        }
+        for (int i = 0; i < VS; ++i) {
+            mbar_init(&sh->v_full[i], 1);
+            mbar_init(&sh->v_empty[i], QT);
         }
         for (int g = 0; g < QT; ++g) {
             for (int b = 0; b < kB; ++b) {
@@ -123,7 +130,6 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
             mbar_init(&sh->o_full[g], 1);
             sh->keep_o[g] = 0;
         }
-        mbar_init(&sh->item_done, kSoftmaxWarps);
         sh->abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -139,8 +145,8 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
     pdl_wait();
 
     PagedStart start;
-    static_assert(sizeof(PagedScratch) <= kQBytes<64>, "the scratch fits a Q tile");
-    const bool any = paged_find_start<kThreads<QT>, kKT>(a, a.tile_rows, *reinterpret_cast<PagedScratch*>(sQ), 2, start);
+    static_assert(sizeof(PagedScratch) <= kSmem<64, 1> - 512, "the scratch fits the tiles");
+    const bool any = paged_find_start<kThreads<QT>, kKT, kItem>(a, *reinterpret_cast<PagedScratch*>(sQ), kItem + 2, start);
     proxy_fence();                                          // the scratch's writes before the copies that take its place
     __syncthreads();
 
@@ -148,152 +154,164 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
     const uint32_t tmem = __shfl_sync(0xffffffffu, sh->tmem_base, 0);                    // per Q tile 256 columns: kB x 64 of S or P, then O
     auto tmem_o = [&](int g) { return tmem + g * kCols + kCols - HD; };
 
-    if (any && warp == kSoftmaxWarps + 1) {
+    if (any && warp == kSoftmaxWarps + QT) {
         // ================= loader =================
-        PagedWalk<kKT> w(a, start, a.tile_rows);
-        const int box_shift = min(a.page_shift, 6), box = 1 << box_shift, boxes_all = kKT >> box_shift;
-        bool ok = true;
-        uint32_t item = 0, issued = 0;
-        int slot = 0;
-        uint32_t ph = 1;                                         // a slot's first load waits for nothing
-        do {
-            const int n = w.t1 - w.t0, n_loads = 2 * n, q_at = min(n_loads, kRing);
-            // Load i: K(0) .. K(kFirst - 1), then K(t + kFirst), V(t) by turns, then the last V (the order of the MMAs).
-            const int head_k = min(kFirst, n), turns = 2 * (n - head_k);
-            for (int i = 0; i <= n_loads && ok; ++i) {
-                if (i == q_at) {                                 // Q behind the first K and V tiles: they need no Q to be let in
-                    if (item > 0) ok = wait(&sh->item_done, (item - 1) & 1u);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    const uint32_t bytes = static_cast<uint32_t>(a.tile_tokens) * a.G * 128;
-                    if (lane == 0) mbar_expect_tx(&sh->q_full, QT * kAtoms * bytes);
-                    __syncwarp();
-                    if (lane < QT * kAtoms) {
-                        const int g = lane / kAtoms, at = lane % kAtoms;
-                        tma_box_3d(smem_u32(sQ) + g * kQBytes<HD> + at * kTQ * 128, &tm_q, &sh->q_full, 64 * at, w.head * a.G,
-                                   w.q.row0 + (w.rt * QT + g) * a.tile_tokens);
+        // K of tile i + kFirst, V of tile i by turns, whatever item they belong to; Q of an item while its predecessor's first
+        // tiles are on the way (two buffers), or when its predecessor has ended.
+        PagedWalk<kKT, kItem> wk(a, start), wv(a, start), wq(a, start);
+        // pages of 64 rows and more: a copy a tile; smaller ones: a copy per page and 64 values, in their places of the operand layout
+        const int box_shift = min(a.page_shift, 6), box = 1 << box_shift;
+        PagedPages k_pages, v_pages;
+        bool ok = true, have_k = true, have_q = true;
+        uint32_t nk = 0, nv = 0, nq = 0;                         // loads issued
+        int tk = wk.t0;
+        auto all_wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
+        auto load_tile = [&](const PagedWalk<kKT, kItem>& w, int t, PagedPages& pages, int base, uint8_t* to, uint64_t* bar) {
+            const int k0 = w.k.tile(t) << 6, boxes = max(0, (min(kKT, w.k.hi - k0) + box - 1) >> box_shift);
+            const uint32_t dst = __shfl_sync(0xffffffffu, smem_u32(to), 0);
+            if (paged_elect()) mbar_expect_tx(bar, static_cast<uint32_t>(boxes) * box * HD * 2);
+            __syncwarp();
+            for (int c = 0; c < boxes; ++c) {
+                const int row = pages.row(a, w.seq, w.head, k0 + (c << box_shift), base);
+                if (paged_elect()) {
+                    if (box == kKT) {
+                        tma_box_3d(dst, &tm_rows, bar, 0, row, 0);
+                    } else {
+#pragma unroll
+                        for (int at = 0; at < kAtoms; ++at) tma_box_3d(dst + at * kKT * 128 + c * box * 128, &tm_atoms, bar, 0, row, at);
                     }
                 }
-                if (i == n_loads) break;
-                int tile = i;
-                bool v = false;
-                if (i >= head_k) {
-                    const int j = i - head_k;
-                    v = j >= turns || (j & 1);
-                    tile = j >= turns ? j - turns / 2 : (j >> 1) + (v ? 0 : kFirst);
-                }
-                const int k0 = w.k.tile(w.t0 + tile) << 6;
-                const int sub = lane / kAtoms, at = lane % kAtoms;
-                const bool mine = sub < boxes_all && k0 + (sub << box_shift) < w.k.hi;
-                const int boxes = __popc(__ballot_sync(0xffffffffu, mine));
-                int row = a.pool_rows;                           // behind the pool: zeros
-                if (mine) {
-                    const int pos = k0 + (sub << box_shift);
-                    const int page = a.table[static_cast<size_t>(w.seq) * a.table_stride + (pos >> a.page_shift)];
-                    if (page >= 0 && page < a.n_pages)
-                        row = (v ? a.v_row0 : a.k_row0) + ((page * a.KV + w.head) << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
-                }
-                if (issued >= kRing) {
-                    ok = __all_sync(0xffffffffu, wait(&sh->empty[slot], ph));
-                    if (!ok) break;
-                }
-                const uint32_t sl = __shfl_sync(0xffffffffu, slot, 0), dst = smem_u32(ring) + sl * kT;
-                if (elect_one()) mbar_expect_tx(&sh->full[sl], static_cast<uint32_t>(boxes) * box * 128);
                 __syncwarp();
-                for (int c = 0; c < boxes; ++c) {
-                    const int row_c = __shfl_sync(0xffffffffu, row, c), at_c = c % kAtoms, sub_c = c / kAtoms;
-                    if (elect_one()) tma_box_3d(dst + at_c * kKT * 128 + sub_c * box * 128, &tm_kv, &sh->full[sl], 0, row_c, at_c);
-                    __syncwarp();
-                }
-                ++issued;
-                if (++slot == kRing) { slot = 0; ph ^= 1u; }
             }
-            ++item;
-        } while (ok && w.next());
+        };
+        auto load_k = [&]() {
+            if (!ok || !have_k) return;
+            const uint32_t slot = nk % KS;
+            if (nk >= KS) ok = all_wait(&sh->k_empty[slot], (nk / KS - 1) & 1u);
+            if (!ok) return;
+            load_tile(wk, tk, k_pages, a.k_row0, sK + slot * kT, &sh->k_full[slot]);
+            ++nk;
+            if (++tk == wk.t1) {
+                have_k = wk.next();
+                tk = wk.t0;
+            }
+        };
+        auto load_v = [&](int t) {
+            const uint32_t slot = nv % VS;
+            if (nv >= VS) ok = ok && all_wait(&sh->v_empty[slot], (nv / VS - 1) & 1u);
+            if (!ok) return;
+            load_tile(wv, t, v_pages, a.v_row0, sV + slot * kT, &sh->v_full[slot]);
+            ++nv;
+        };
+        auto load_q = [&]() {
+            if (!ok || !have_q) return;
+            const uint32_t buf = nq % NQ;
+            if (nq >= NQ) ok = all_wait(&sh->item_done[buf], (nq / NQ - 1) & 1u);
+            if (!ok) return;
+            if (paged_elect()) mbar_expect_tx(&sh->q_full[buf], QT * kAtoms * static_cast<uint32_t>(a.tile_tokens) * a.G * 128);
+            __syncwarp();
+            if (paged_elect()) {
+#pragma unroll
+                for (int g = 0; g < QT; ++g)
+#pragma unroll
+                    for (int at = 0; at < kAtoms; ++at)
+                        tma_box_3d(smem_u32(sQ) + (buf * QT + g) * kQBytes<HD> + at * kTQ * 128, &tm_q, &sh->q_full[buf], 64 * at, wq.head * a.G,
+                                   wq.q.row0 + (wq.rt * QT + g) * a.tile_tokens);
+            }
+            __syncwarp();
+            ++nq;
+            have_q = wq.next();
+        };
+        for (int i = 0; i < kFirst; ++i) load_k();
+        if (NQ == 2) load_q();
+        do {
+            if (NQ == 1) load_q();
+            for (int t = wv.t0; t < wv.t1 && ok; ++t) {
+                load_k();
+                load_v(t);
+                // behind the item's third tile: the epilogue in front of it, which frees the buffer, is on its way by then
+                if (NQ == 2 && t == min(wv.t0 + 2, wv.t1 - 1)) load_q();
+            }
+        } while (ok && wv.next());
         if (*cta_abort && lane == 0) {   // copies in flight land before the CTA's shared memory goes away
             const long long t0 = clock64();
-            auto land = [&](uint64_t* bar, uint32_t parity) {
-                while (!mbar_try_wait_parity(bar, parity) && clock64() - t0 < kWaitLimitCycles / 8) {
-                }
+            auto land = [&](uint64_t* bars, uint32_t n, uint32_t slots) {
+                for (uint32_t j = n > slots ? n - slots : 0; j < n; ++j)
+                    while (!mbar_try_wait_parity(&bars[j % slots], (j / slots) & 1u) && clock64() - t0 < kWaitLimitCycles / 8) {
+                    }
             };
-            land(&sh->q_full, (item - 1) & 1u);
-            for (uint32_t j = issued > kRing ? issued - kRing : 0; j < issued; ++j) land(&sh->full[j % kRing], (j / kRing) & 1u);
+            land(sh->q_full, nq, NQ);
+            land(sh->k_full, nk, KS);
+            land(sh->v_full, nv, VS);
         }
-    } else if (any && warp == kSoftmaxWarps) {
-        // ================= MMA issuer: the whole warp walks and waits, one lane issues =================
-        PagedWalk<kKT> w(a, start, a.tile_rows);
+    } else if (any && warp >= kSoftmaxWarps) {
+        // ================= MMA issuer of Q tile g: the whole warp walks and waits, one lane issues =================
+        // S of tile i + kFirst, P V of tile i by turns; with two Q buffers into the next item, so that its first scores are ready when
+        // the softmax warps have written the one in front of it.  (P of an item's first tile says that O has been read.)
+        PagedWalk<kKT, kItem> ws(a, start), wv(a, start);
+        const int g = warp - kSoftmaxWarps;
         constexpr uint32_t idesc_s = instr_desc(kTQ, kKT, 0), idesc_o = instr_desc(kTQ, HD, 1);
-        const uint64_t q_desc = desc_k_major(smem_u32(sQ)), ring_k = desc_k_major(smem_u32(ring)), ring_v = desc_mn_major(smem_u32(ring), kKT * 128);
-        bool ok = true;
-        uint32_t item = 0, done = 0;                             // key tiles of the items before
-        int slot = 0;
-        uint32_t ph = 0;
+        const uint32_t cols = tmem + g * kCols;
+        const uint64_t q_desc = desc_k_major(smem_u32(sQ) + g * kQBytes<HD>), k_desc = desc_k_major(smem_u32(sK)),
+                       v_desc = desc_mn_major(smem_u32(sV), kKT * 128);
+        bool ok = true, have_s = true;
+        uint32_t ns = 0, nv = 0, is = 0, iv = 0;                 // S and P V issued, the items of the next ones
+        int ts = ws.t0;
         auto uniform = [](uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); };
         auto all_wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
-        auto next_slot = [&]() {
-            if (++slot == kRing) { slot = 0; ph ^= 1u; }
+        auto issue_s = [&]() {
+            const uint32_t b = uniform(ns % kB), slot = uniform(ns % KS), buf = uniform(is % NQ);
+            if (ts == ws.t0) ok = all_wait(&sh->q_full[buf], (is / NQ) & 1u);
+            if (ok) ok = all_wait(&sh->k_full[slot], (ns / KS) & 1u);
+            // P in this buffer, of tile ns - kB <= nv - 1, has been multiplied
+            if (ok && nv > 0) ok = all_wait(&sh->pv_done[g][(nv - 1) & 1u], ((nv - 1) >> 1) & 1u);
+            if (!ok) return;
+            tc_fence_after();
+            const uint64_t q = q_desc + buf * (QT * kQBytes<HD> >> 4), k = k_desc + slot * (kT >> 4);
+            if (paged_elect()) {
+#pragma unroll
+                for (int kk = 0; kk < HD / 16; ++kk) {
+                    const uint32_t atom = kk >> 2, within = (kk & 3) * 32;
+                    umma(cols + b * kKT, q + ((atom * (kTQ * 128) + within) >> 4), k + ((atom * (kKT * 128) + within) >> 4), idesc_s, kk > 0 ? 1u : 0u);
+                }
+                umma_commit(&sh->s_full[g][b]);
+                umma_commit(&sh->k_empty[slot]);
+            }
+            __syncwarp();
+            ++ns;
+            if (++ts == ws.t1) {
+                have_s = ws.next();
+                ts = ws.t0;
+                ++is;
+            }
         };
         do {
-            const int n = w.t1 - w.t0;
-            if (item > 0) ok = all_wait(&sh->item_done, (item - 1) & 1u);   // O read; with it every MMA of the item has completed
-            if (ok) ok = all_wait(&sh->q_full, item & 1u);
-            // S of the item's tile t, for every Q tile: its buffer's P has been multiplied
-            auto issue_s = [&](int t) {
-                if (!all_wait(&sh->full[slot], ph)) return false;
-                const uint32_t gt = done + t, b = uniform(gt % kB), sl = uniform(slot);
-                const uint64_t k_desc = ring_k + sl * (kT >> 4);
-#pragma unroll
-                for (int g = 0; g < QT; ++g) {
-                    if (t >= kB) {
-                        const uint32_t pv = gt - kB;
-                        if (!all_wait(&sh->pv_done[g][pv & 1u], (pv >> 1) & 1u)) return false;
-                    }
-                    tc_fence_after();
-                    if (elect_one()) {
-#pragma unroll
-                        for (int kk = 0; kk < HD / 16; ++kk) {
-                            const uint32_t atom = kk >> 2, within = (kk & 3) * 32;
-                            umma(tmem + g * kCols + b * kKT, q_desc + ((g * kQBytes<HD> + atom * (kTQ * 128) + within) >> 4),
-                                 k_desc + ((atom * (kKT * 128) + within) >> 4), idesc_s, kk > 0 ? 1u : 0u);
-                        }
-                        umma_commit(&sh->s_full[g][b]);
-                        if (g == QT - 1) umma_commit(&sh->empty[sl]);
-                    }
-                    __syncwarp();
-                }
-                next_slot();
-                return true;
-            };
-            for (int t = 0; t < kFirst && t < n && ok; ++t) ok = issue_s(t);
+            const int n = wv.t1 - wv.t0;
             for (int t = 0; t < n && ok; ++t) {
-                if (t + kFirst < n) ok = issue_s(t + kFirst);
-                if (ok) ok = all_wait(&sh->full[slot], ph);
-                const uint32_t gt = done + t, b = uniform(gt % kB), sl = uniform(slot), last = t + 1 == n;
-                const uint64_t v_desc = ring_v + sl * (kT >> 4);
+                while (ok && have_s && ns <= nv + kFirst && is < iv + NQ) issue_s();
+                const uint32_t b = uniform(nv % kB), slot = uniform(nv % VS), last = t + 1 == n;
+                if (ok) ok = all_wait(&sh->v_full[slot], (nv / VS) & 1u);
+                if (ok) ok = all_wait(&sh->p_full[g][b], (nv / kB) & 1u);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t keep = uniform(t > 0 || *const_cast<volatile int*>(&sh->keep_o[g]) ? 1u : 0u);
+                const uint64_t v = v_desc + slot * (kT >> 4);
+                if (paged_elect()) {
 #pragma unroll
-                for (int g = 0; g < QT; ++g) {
-                    if (ok) ok = all_wait(&sh->p_full[g][b], (gt / kB) & 1u);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t keep = uniform(t > 0 || *const_cast<volatile int*>(&sh->keep_o[g]) ? 1u : 0u);
-                    if (elect_one()) {
-#pragma unroll
-                        for (int kk = 0; kk < kKT / 16; ++kk)
-                            umma_ts(tmem_o(g), tmem + g * kCols + b * kKT + kk * 8, v_desc + kk * (2048 >> 4), idesc_o, kk > 0 ? 1u : keep);
-                        umma_commit(&sh->pv_done[g][gt & 1u]);
-                        if (last) umma_commit(&sh->o_full[g]);
-                        if (g == QT - 1) umma_commit(&sh->empty[sl]);
-                    }
-                    __syncwarp();
+                    for (int kk = 0; kk < kKT / 16; ++kk)
+                        umma_ts(tmem_o(g), cols + b * kKT + kk * 8, v + kk * (2048 >> 4), idesc_o, kk > 0 ? 1u : keep);
+                    umma_commit(&sh->pv_done[g][nv & 1u]);
+                    umma_commit(&sh->v_empty[slot]);
+                    if (last) umma_commit(&sh->o_full[g]);
                 }
-                if (ok) next_slot();
+                __syncwarp();
+                ++nv;
             }
-            done += n;
-            ++item;
-        } while (ok && w.next());
+            ++iv;
+        } while (ok && wv.next());
     } else if (any) {
         // ================= softmax: thread r of Q tile g = packed row r = TMEM lane r =================
-        PagedWalk<kKT> w(a, start, a.tile_rows);
+        PagedWalk<kKT, kItem> w(a, start);
         const int g = warp >> 2, gw = warp & 3, r = tid & 127;
         const uint32_t lane_base = static_cast<uint32_t>(gw * 32) << 16;   // this warp's TMEM lanes
         const uint32_t s_base = tmem + g * kCols + lane_base, o_base = tmem_o(g) + lane_base;
@@ -301,24 +319,26 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
         constexpr float kSlack = 4.0f;
         const uint64_t scale2 = pack2f(a.scale_log2, a.scale_log2);
         bool ok = true;
-        uint32_t item = 0, done = 0, loads = 0;                  // key tiles and loads of the items before
+        uint32_t item = 0, done = 0;                             // key tiles of the items before
         do {
-            const int n = w.t1 - w.t0, head_k = min(kFirst, n);
+            const int n = w.t1 - w.t0;
             const int tok0 = (w.rt * QT + g) * a.tile_tokens;    // the Q tile's first query row
-            const int pos = w.q.first + tok0 + min(r, rows_g - 1) / a.G;
-            const int p_lo = w.q.first + tok0, p_hi = p_lo + a.tile_tokens - 1;
+            const int pos = w.q.first + tok0 + a.by_group(min(r, rows_g - 1));
+            // keys from .._lo on and below .._hi are seen by all rows of the Q tile, of the item
+            auto low = [&](int tok) { return static_cast<int>(max(-1ll, static_cast<long long>(w.q.first) + tok - a.left)); };
+            auto high = [&](int tok) { return static_cast<int>(max(0ll, min(static_cast<long long>(w.q.len), static_cast<long long>(w.q.first) + tok + a.right + 1))); };
+            const int all_lo = low(tok0 + a.tile_tokens - 1), all_hi = high(tok0);
+            const int item_lo = low((w.rt + 1) * QT * a.tile_tokens - 1), item_hi = high(w.rt * QT * a.tile_tokens);
+            const int left = min(rows_g, (w.q.n - tok0) * a.G);          // rows of the Q tile (may be negative); others hold anything
+            const bool mine = r < left;
             float M_row = -INFINITY, l_row = 0.f;
             for (int t = 0; t < n; ++t) {
                 const uint32_t gt = done + t, b = gt % kB;
                 const uint32_t ts = s_base + b * kKT;
                 const int k0 = w.k.tile(w.t0 + t) << 6;
-                // seen by every row of the Q tile / tiles with rows of V that need care, the same for all Q tiles of the item
-                const bool whole = k0 + kKT <= min(static_cast<long long>(w.q.len), static_cast<long long>(p_lo) + a.right + 1) &&
-                                   (k0 >= p_hi - a.left || k0 + kKT <= a.sinks);
-                const int item_lo = w.q.first + w.rt * QT * a.tile_tokens, item_hi = item_lo + QT * a.tile_tokens - 1;
-                const bool whole_item = QT == 1 ? whole
-                    : k0 + kKT <= min(static_cast<long long>(w.q.len), static_cast<long long>(item_lo) + a.right + 1) &&
-                          (k0 >= item_hi - a.left || k0 + kKT <= a.sinks);
+                // seen by every row of the Q tile, of all Q tiles of the item (others have rows of V that need care)
+                const bool whole = k0 + kKT <= all_hi && (k0 >= all_lo || k0 + kKT <= a.sinks);
+                const bool whole_item = QT == 1 ? whole : k0 + kKT <= item_hi && (k0 >= item_lo || k0 + kKT <= a.sinks);
                 ok = __all_sync(0xffffffffu, wait(&sh->s_full[g][b], (gt / kB) & 1u));
                 tc_fence_after();
                 uint32_t sv[64];                                         // the row's scores
@@ -348,7 +368,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                         else sv[j] = 0x7f800000u;                        // times the scale: minus infinity
                 }
                 float factor = 1.0f;                                     // what O and the row sum so far are multiplied by
-                const float mt_log2 = mask ? m0 * a.scale_log2 : -INFINITY;
+                const float mt_log2 = mine && mask ? m0 * a.scale_log2 : -INFINITY;   // rows that are none turn nothing for the warp's others
                 if (mt_log2 > M_row + kSlack) {                          // also the first visible key (M_row = -inf)
                     const float M_new = ceilf(mt_log2);
                     if (M_row != -INFINITY) factor = exp2f(M_row - M_new);   // an exact power of two
@@ -383,12 +403,11 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                 bool odd = false;
                 uint32_t vt = 0;
                 if (!whole_item) {
-                    // V in places that a row does not see, once it has landed (its place in the loader's order: behind K(t + kFirst)).
-                    // The parity is not ambiguous: the load before it in this slot is a K or V tile multiplied before S(t) was, the one
-                    // behind it waits for P V(t).
-                    const uint32_t i = loads + (t < n - head_k ? head_k + 2 * t + 1 : n + t), slot = i % kRing;
-                    ok = __all_sync(0xffffffffu, wait(&sh->full[slot], (i / kRing) & 1u)) && ok;
-                    vt = smem_u32(ring) + slot * kT;
+                    // V in places that a row does not see, once it has landed.  The parity is not ambiguous: the tile before it in this
+                    // slot was multiplied before S(t) was, the one behind it waits for P V(t).
+                    const uint32_t slot = gt % VS;
+                    ok = __all_sync(0xffffffffu, wait(&sh->v_full[slot], (gt / VS) & 1u)) && ok;
+                    vt = smem_u32(sV) + slot * kT;
 #pragma unroll
                     for (int at = 0; at < kAtoms; ++at)
                         for (uint32_t off = tid * 16; off < kKT * 128; off += 128 * QT * 16) {
@@ -463,25 +482,23 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                 if (lane == 0) mbar_arrive(&sh->p_full[g][b]);
             }
             done += n;
-            loads += 2 * n;
             const float m_log2 = M_row == -INFINITY ? 0.f : M_row;      // the shift the row's sum and output carry
             ok = __all_sync(0xffffffffu, wait(&sh->o_full[g], item & 1u)) && ok;
             tc_fence_after();
             const int row_w = gw * 32;                                   // the warp's first row of the Q tile
-            const int left = min(rows_g, (w.q.n - tok0) * a.G) - row_w;   // rows of the Q tile from there on (may be negative)
-            const uint32_t patch = smem_u32(sQ) + g * kQBytes<HD> + gw * kPatch;   // every MMA that reads this Q tile has completed
-            const bool final = w.t0 == 0 && w.t1 == w.k.n;
+            const uint32_t patch = smem_u32(sQ) + ((item % NQ) * QT + g) * kQBytes<HD> + gw * kPatch;   // every MMA that reads this Q tile has completed
+            const bool final = w.whole();
             if (final) {
                 int at[8];                                               // head of rows lane / 8, lane / 8 + 4 .. of the warp, from the Q tile's first
 #pragma unroll
                 for (int it = 0; it < 8; ++it) {
-                    const int idx = row_w + it * 4 + (lane >> 3), i = idx / a.G;
+                    const int idx = row_w + it * 4 + (lane >> 3), i = a.by_group(idx);
                     at[it] = i * static_cast<int>(a.out_stride / 8) + (idx - i * a.G) * (HD / 8);
                 }
                 uint4* out = reinterpret_cast<uint4*>(a.out + static_cast<size_t>(w.q.row0 + tok0) * a.out_stride + w.head * a.G * HD);
                 const float inv = l_row == 0.f ? 0.f : 1.0f / l_row;
-                if (a.lse && lane < left) {
-                    const int idx = row_w + lane, i = idx / a.G;
+                if (a.lse && row_w + lane < left) {
+                    const int idx = row_w + lane, i = a.by_group(idx);
                     a.lse[static_cast<size_t>(w.q.row0 + tok0 + i) * a.H + w.head * a.G + idx - i * a.G] = paged_lse(m_log2, l_row);
                 }
 #pragma unroll 1
@@ -494,12 +511,12 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
 #pragma unroll
                         for (int j = 0; j < 32; ++j) x[j] = 0u;
                     turn_rows(patch, lane, x, [&](int rr, int ch, const uint4& y) {
-                        if (rr < left) out[at[rr >> 2] + c * 8 + ch] = y;
+                        if (row_w + rr < left) out[at[rr >> 2] + c * 8 + ch] = y;
                     });
                 }
             } else {
                 const size_t pr = paged_part(a, blockIdx.x, w.t0 == 0) + g * rows_g + row_w;
-                if (lane < left) *reinterpret_cast<float2*>(a.part_ml + (pr + lane) * 2) = make_float2(m_log2, l_row);
+                if (row_w + lane < left) *reinterpret_cast<float2*>(a.part_ml + (pr + lane) * 2) = make_float2(m_log2, l_row);
 #pragma unroll 1
                 for (int c = 0; c < HD / 32; ++c) {
                     uint32_t v[32];
@@ -508,19 +525,18 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] = 0u;
                     turn_rows(patch, lane, v, [&](int rr, int ch, const uint4& y) {
-                        if (rr < left) *reinterpret_cast<uint4*>(a.part_o + (pr + rr) * HD + c * 32 + ch * 4) = y;
+                        if (row_w + rr < left) *reinterpret_cast<uint4*>(a.part_o + (pr + rr) * HD + c * 32 + ch * 4) = y;
                     });
                 }
             }
             proxy_fence();                                               // the patches before the next Q
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sh->item_done);
+            if (lane == 0) mbar_arrive(&sh->item_done[item % NQ]);
             if (!final) {
                 __threadfence();
                 softmax_barrier<QT>();
-                const long long ub = w.item_begin();
-                const int c0 = paged_owner(ub, start.total, start.ctas), c1 = paged_owner(ub + w.k.n - 1, start.total, start.ctas);
+                const int c0 = w.first_cta(), c1 = w.last_cta();
                 if (tid == 0) {
                     const bool last = atomicAdd(a.arrivals + c0, 1u) == static_cast<unsigned>(c1 - c0);
                     if (last) a.arrivals[c0] = 0;                        // for the next launch; an item is counted at the CTA it begins in
@@ -545,11 +561,11 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
 }
 
 template <int HD, int QT>
-cudaError_t launch(const PagedAttnArgs& a, const CUtensorMap& tm_q, const CUtensorMap& tm_kv, int sms, cudaStream_t st) {
+cudaError_t launch(const PagedAttnArgs& a, const CUtensorMap& tm_q, const PagedMaps& maps, int sms, cudaStream_t st) {
     static std::atomic<unsigned long long> attr_done{0};
     const cudaError_t e = set_smem_limit_once(attr_done, paged_attention_tc_kernel<HD, QT>, static_cast<int>(kSmem<HD, QT>));
     if (e != cudaSuccess) return e;
-    return launch_kernel(paged_attention_tc_kernel<HD, QT>, dim3(QT == 1 ? 2 * sms : sms), dim3(kThreads<QT>), kSmem<HD, QT>, st, tm_q, tm_kv, a);
+    return launch_kernel(paged_attention_tc_kernel<HD, QT>, dim3(QT == 1 ? 2 * sms : sms), dim3(kThreads<QT>), kSmem<HD, QT>, st, tm_q, maps.rows, maps.atoms, a);
 }
 
 }  // namespace
@@ -557,12 +573,13 @@ cudaError_t launch(const PagedAttnArgs& a, const CUtensorMap& tm_q, const CUtens
 cudaError_t launch_paged_attention_tc(PagedAttnArgs a, const PagedMaps& maps, int hd, int q_tiles, int sms, cudaStream_t st) {
     a.tile_tokens = kTQ / a.G;
     a.tile_rows = q_tiles * a.tile_tokens * a.G;
+    a.by_rows = PagedDiv::by(a.tile_rows);
     a.part_rows = q_tiles * kPagedPartRows;
     CUtensorMap tm_q;
     const cudaError_t e = make_group_tmap(&tm_q, a.q, a.max_rows, a.q_stride, a.H, hd, a.G, a.tile_tokens);
     if (e != cudaSuccess) return e;
-    if (q_tiles == 1) return hd == 128 ? launch<128, 1>(a, tm_q, maps.atoms, sms, st) : launch<64, 1>(a, tm_q, maps.atoms, sms, st);
-    return hd == 128 ? launch<128, 2>(a, tm_q, maps.atoms, sms, st) : launch<64, 2>(a, tm_q, maps.atoms, sms, st);
+    if (q_tiles == 1) return hd == 128 ? launch<128, 1>(a, tm_q, maps, sms, st) : launch<64, 1>(a, tm_q, maps, sms, st);
+    return hd == 128 ? launch<128, 2>(a, tm_q, maps, sms, st) : launch<64, 2>(a, tm_q, maps, sms, st);
 }
 
 }  // namespace odb

@@ -329,6 +329,29 @@ def test_attention(case):
 
 
 @requires_gpu
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("new,G", [(1, 4), (30, 4), (60, 4)])
+def test_attention_of_many_requests_of_a_tile_or_two(new, G, D):
+    """More items than CTAs, each of one to three key tiles: shares of many items, and items cut in two."""
+    rng = np.random.default_rng(new + D)
+    seqs = 230
+    lens = [int(n) for n in rng.integers(1, 150, seqs)]
+    counts = [min(n, new) for n in lens]
+    firsts = [n - c for n, c in zip(lens, counts)]
+    cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, 2 * G, 2, D, 16)
+    lse = torch.empty(sum(counts), 2 * G, device="cuda")
+    out = cache.attention(0, b, q, right=0, lse=lse)
+    assert cache.status() == 0
+    got, gl = out.float().cpu().numpy(), lse.cpu().numpy()
+    for s in range(0, seqs, 1 if new == 1 else 9):                 # the oracle takes its time
+        rows = slice(start[s], start[s + 1])
+        _check(torch.from_numpy(got[rows]), torch.from_numpy(gl[rows]), qf[rows], keys[s:s + 1], values[s:s + 1],
+               np.array([0, counts[s]]), firsts[s:s + 1], D, right=0)
+    assert np.isfinite(got).all() and torch.equal(cache.attention(0, b, q, right=0), out)
+    cache.close()
+
+
+@requires_gpu
 @pytest.mark.parametrize("max_new", [1, 8, 16, 20, 64, 5000])
 def test_the_hint_decides_no_result(max_new):
     rng = np.random.default_rng(9)
