@@ -53,6 +53,11 @@ struct PagedDiv {
 #endif
 };
 
+// An item that begins in a CTA and ends in CTA `last_cta`: its rows, or none.
+struct PagedShared {
+    int row0, head, first_idx, rows, last_cta;
+};
+
 struct PagedAttnArgs {
     const __nv_bfloat16* q;
     __nv_bfloat16* out;
@@ -68,6 +73,7 @@ struct PagedAttnArgs {
     float* part_o;                                        // [ctas][2][part_rows][HD]
     float* part_ml;                                       // [ctas][2][part_rows][2]
     int part_rows;                                        // rows of a tile
+    struct PagedShared* shared;                           // [kPagedMaxCtas], of the last launch that adds up in a kernel of its own
     PagedDiv by_group, by_rows;                           // divisions by G and by the packed rows of an item
     int tile_rows, tile_tokens;                           // many rows: packed rows of an item, query rows of a Q tile
 };

@@ -13,6 +13,7 @@ struct odb_paged {
     __nv_bfloat16* kv;
     int* status;
     unsigned int* arrivals;
+    PagedShared* shared;
     float *part_o, *part_ml;
     int pool_rows, layer_rows;      // rows of head_dim values: of the whole pool, of the K or the V of a layer
     PagedMaps maps;
@@ -22,6 +23,7 @@ namespace {
 
 constexpr size_t kStatusBytes = 256;
 constexpr size_t kArrivalBytes = (kPagedMaxCtas * sizeof(unsigned int) + 255) / 256 * 256;
+constexpr size_t kSharedBytes = (kPagedMaxCtas * sizeof(PagedShared) + 255) / 256 * 256;
 
 int32_t check_config(const odb_paged_config* c) {
     if (!c) return ODB_ERR_ARG;
@@ -59,7 +61,7 @@ size_t odb_paged_kv_bytes(const odb_paged_config* c) {
 
 size_t odb_paged_workspace_bytes(const odb_paged_config* c) {
     if (check_config(c) != ODB_OK) return 0;
-    return kStatusBytes + kArrivalBytes + paged_part_bytes(c->head_dim);
+    return kStatusBytes + kArrivalBytes + kSharedBytes + paged_part_bytes(c->head_dim);
 }
 
 int32_t odb_paged_create(const odb_paged_config* cfg, void* kv, size_t kv_bytes, void* workspace, size_t ws_bytes, void* stream,
@@ -78,7 +80,8 @@ int32_t odb_paged_create(const odb_paged_config* cfg, void* kv, size_t kv_bytes,
     char* ws = static_cast<char*>(workspace);
     h->status = reinterpret_cast<int*>(ws);
     h->arrivals = reinterpret_cast<unsigned int*>(ws + kStatusBytes);
-    h->part_o = reinterpret_cast<float*>(ws + kStatusBytes + kArrivalBytes);
+    h->part_o = reinterpret_cast<float*>(ws + kStatusBytes + kArrivalBytes + kSharedBytes);
+    h->shared = reinterpret_cast<PagedShared*>(ws + kStatusBytes + kArrivalBytes);
     h->part_ml = h->part_o + paged_part_bytes(cfg->head_dim) / sizeof(float) / (cfg->head_dim + 2) * cfg->head_dim;
     cudaError_t e = cudaGetDevice(&h->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, h->device);
@@ -218,6 +221,7 @@ int32_t odb_paged_attention(odb_paged* h, int32_t layer, const odb_paged_batch* 
     a.sinks = sinks > kPagedUnlimited ? kPagedUnlimited : sinks;
     a.scale_log2 = (scale != 0.f ? scale : 1.0f / sqrtf(static_cast<float>(c.head_dim))) * 1.4426950408889634f;
     a.status = h->status; a.arrivals = h->arrivals; a.part_o = h->part_o; a.part_ml = h->part_ml;
+    a.shared = h->shared;
     return enqueued(launch_paged_attention(a, h->maps, c.head_dim, b->max_new, h->sms, static_cast<cudaStream_t>(stream)));
 }
 

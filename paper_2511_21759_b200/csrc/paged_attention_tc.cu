@@ -49,7 +49,7 @@ struct alignas(8) Shared {
     uint64_t o_full[2];                // the item's last one has                         (MMA -> softmax)
     uint64_t item_done[2];             // the Q buffer may be overwritten                 (softmax -> loader, 4 QT arrivals)
     uint32_t tmem_base;
-    int abort, last, keep_o[2];
+    int abort, keep_o[2];
 };
 static_assert(sizeof(Shared) <= 512, "the barriers end inside the allocation");
 
@@ -86,6 +86,18 @@ __device__ __forceinline__ void tmem_st1(uint32_t taddr, uint32_t v) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};\n\ttcgen05.wait::st.sync.aligned;" ::"r"(taddr), "r"(v) : "memory");
 }
 __device__ __forceinline__ bool not_finite(uint32_t bf) { return (bf & 0x7f80u) == 0x7f80u; }
+
+// Turns of the two Q tiles' softmax warps gw: Q tile 0 first.
+__device__ __forceinline__ void turn_begin(int g, int gw) { asm volatile("bar.sync %0, 64;" ::"r"(2 + 4 * g + gw) : "memory"); }
+__device__ __forceinline__ void turn_end(int g, int gw) { asm volatile("bar.arrive %0, 64;" ::"r"(2 + 4 * (g ^ 1) + gw) : "memory"); }
+
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
+        "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
 
 template <int HD, int QT>
 __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
@@ -153,6 +165,8 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
     auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait_bounded(bar, parity, cta_abort, a.status); };
     const uint32_t tmem = __shfl_sync(0xffffffffu, sh->tmem_base, 0);                    // per Q tile 256 columns: kB x 64 of S or P, then O
     auto tmem_o = [&](int g) { return tmem + g * kCols + kCols - HD; };
+
+    if (tid == 0) a.shared[blockIdx.x].rows = 0;            // thread 0 writes it again where an item begins here and ends elsewhere
 
     if (any && warp == kSoftmaxWarps + QT) {
         // ================= loader =================
@@ -320,6 +334,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
         const uint64_t scale2 = pack2f(a.scale_log2, a.scale_log2);
         bool ok = true;
         uint32_t item = 0, done = 0;                             // key tiles of the items before
+        if (QT == 2 && g == 1) turn_end(1, gw);
         do {
             const int n = w.t1 - w.t0;
             const int tok0 = (w.rt * QT + g) * a.tile_tokens;    // the Q tile's first query row
@@ -352,14 +367,15 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                     for (int j = 0; j < 64; ++j)
                         if (!((mask >> j) & 1ull)) sv[j] = 0xff800000u;
                 }
-                float m0 = __uint_as_float(sv[0]), m1 = __uint_as_float(sv[32]);   // largest visible score of the tile
+                float mx[4];                                             // largest visible score of the tile, in four chains
 #pragma unroll
-                for (int j = 1; j < 31; j += 2) {
-                    m0 = max3(m0, __uint_as_float(sv[j]), __uint_as_float(sv[j + 1]));
-                    m1 = max3(m1, __uint_as_float(sv[32 + j]), __uint_as_float(sv[33 + j]));
+                for (int c = 0; c < 4; ++c) {
+                    mx[c] = __uint_as_float(sv[16 * c]);
+#pragma unroll
+                    for (int j = 1; j < 15; j += 2) mx[c] = max3(mx[c], __uint_as_float(sv[16 * c + j]), __uint_as_float(sv[16 * c + j + 1]));
                 }
-                m0 = max3(m0, m1, __uint_as_float(sv[31]));
-                m0 = fmaxf(m0, __uint_as_float(sv[63]));
+                float m0 = fmaxf(max3(mx[0], mx[1], __uint_as_float(sv[15])), max3(mx[2], mx[3], __uint_as_float(sv[31])));
+                m0 = max3(m0, __uint_as_float(sv[47]), __uint_as_float(sv[63]));
                 if (a.scale_log2 < 0.f) {                                // a negative scale turns the order around
                     m0 = INFINITY;
 #pragma unroll
@@ -369,17 +385,17 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                 }
                 float factor = 1.0f;                                     // what O and the row sum so far are multiplied by
                 const float mt_log2 = mine && mask ? m0 * a.scale_log2 : -INFINITY;   // rows that are none turn nothing for the warp's others
-                if (mt_log2 > M_row + kSlack) {                          // also the first visible key (M_row = -inf)
-                    const float M_new = ceilf(mt_log2);
-                    if (M_row != -INFINITY) factor = exp2f(M_row - M_new);   // an exact power of two
-                    M_row = M_new;
-                }
                 // The exponentials take a score's exact product with the scale, the shift comes from the rounded one: from 2^22 on
                 // they lie up to 0.25 and more apart, and the scores are rounded first.
                 const bool far = fabsf(mt_log2) >= 0x1p22f && mt_log2 != -INFINITY;
                 bool rescale = false;
                 uint64_t mult2 = scale2;
-                if (__any_sync(0xffffffffu, factor != 1.0f || far)) {
+                if (__any_sync(0xffffffffu, mt_log2 > M_row + kSlack || far)) {
+                    if (mt_log2 > M_row + kSlack) {                      // also the first visible key (M_row = -inf)
+                        const float M_new = ceilf(mt_log2);
+                        if (M_row != -INFINITY) factor = exp2f(M_row - M_new);   // an exact power of two
+                        M_row = M_new;
+                    }
                     rescale = __any_sync(0xffffffffu, factor != 1.0f);
                     if (__any_sync(0xffffffffu, far)) {
 #pragma unroll
@@ -390,15 +406,22 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                 const float m_log2 = M_row == -INFINITY ? 0.f : M_row;   // a row that has seen no key: every P is 0
                 const uint64_t shift2 = pack2f(-m_log2, -m_log2);
                 uint64_t sum[2] = {0ull, 0ull};
-                uint32_t pb[32];                                         // the row's P: 64 keys as bf16 pairs
+                // The two softmax warps of a scheduler take turns at the exponentials: left alone they fall into step, share the
+                // special-function unit for twice as long and leave it idle together for the rest of the tile.
+                if (QT == 2) turn_begin(g, gw);
 #pragma unroll
-                for (int u = 0; u < 32; ++u) {
-                    const float2 x = unpack2f(fma2(pack2u(sv[2 * u], sv[2 * u + 1]), mult2, shift2));
-                    const float p0 = ex2_approx(x.x), p1 = ex2_approx(x.y);
-                    sum[u & 1] = add2(sum[u & 1], pack2f(p0, p1));
-                    pb[u] = paged_bf16x2(p0, p1);
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t pb[16];                                     // P of 32 keys as bf16 pairs
+#pragma unroll
+                    for (int u = 0; u < 16; ++u) {
+                        const float2 x = unpack2f(fma2(pack2u(sv[32 * half + 2 * u], sv[32 * half + 2 * u + 1]), mult2, shift2));
+                        const float p0 = ex2_approx(x.x), p1 = ex2_approx(x.y);
+                        sum[u & 1] = add2(sum[u & 1], pack2f(p0, p1));
+                        pb[u] = paged_bf16x2(p0, p1);
+                    }
+                    tmem_st16(ts + 16 * half, pb);
                 }
-                tmem_st32(ts, pb);
+                if (QT == 2) turn_end(g, gw);
                 const float2 s0 = unpack2f(add2(sum[0], sum[1]));
                 bool odd = false;
                 uint32_t vt = 0;
@@ -533,23 +556,17 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh->item_done[item % NQ]);
-            if (!final) {
-                __threadfence();
-                softmax_barrier<QT>();
-                const int c0 = w.first_cta(), c1 = w.last_cta();
-                if (tid == 0) {
-                    const bool last = atomicAdd(a.arrivals + c0, 1u) == static_cast<unsigned>(c1 - c0);
-                    if (last) a.arrivals[c0] = 0;                        // for the next launch; an item is counted at the CTA it begins in
-                    __threadfence();
-                    sh->last = last;
-                }
-                softmax_barrier<QT>();
-                if (sh->last)
-                    paged_merge<HD>(a, w.q.row0, w.head, w.rt * a.tile_rows, min(a.tile_rows, w.q.n * a.G - w.rt * a.tile_rows), c0, c1, warp, kSoftmaxWarps);
-                softmax_barrier<QT>();                                   // sh->last has been read by all
+            if (!final && w.t0 == 0 && tid == 0) {
+                PagedShared& d = a.shared[blockIdx.x];
+                d.row0 = w.q.row0;
+                d.head = w.head;
+                d.first_idx = w.rt * a.tile_rows;
+                d.last_cta = w.last_cta();
+                d.rows = min(a.tile_rows, w.q.n * a.G - w.rt * a.tile_rows);
             }
             ++item;
         } while (w.next());
+        if (QT == 2 && g == 0) turn_begin(0, gw);                // the other's last word
     }
     tc_fence_before();
     __syncthreads();
@@ -560,12 +577,26 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
     }
 }
 
+// Adds up the parts of the items that several CTAs share, 32 rows a block: with the whole GPU behind it 4 us, where the last CTA of
+// an item took up to 27 us for 128 rows of five parts.
+template <int HD>
+__global__ void __launch_bounds__(128) paged_merge_kernel(const PagedAttnArgs a) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const PagedShared d = a.shared[blockIdx.x];
+    const int warp = threadIdx.x >> 5, r0 = blockIdx.y * 32 + warp;
+    if (r0 < d.rows) paged_merge_rows<HD, 8>(a, d.row0, d.head, d.first_idx, d.rows, blockIdx.x, d.last_cta, r0, 4);
+}
+
 template <int HD, int QT>
 cudaError_t launch(const PagedAttnArgs& a, const CUtensorMap& tm_q, const PagedMaps& maps, int sms, cudaStream_t st) {
     static std::atomic<unsigned long long> attr_done{0};
-    const cudaError_t e = set_smem_limit_once(attr_done, paged_attention_tc_kernel<HD, QT>, static_cast<int>(kSmem<HD, QT>));
+    cudaError_t e = set_smem_limit_once(attr_done, paged_attention_tc_kernel<HD, QT>, static_cast<int>(kSmem<HD, QT>));
     if (e != cudaSuccess) return e;
-    return launch_kernel(paged_attention_tc_kernel<HD, QT>, dim3(QT == 1 ? 2 * sms : sms), dim3(kThreads<QT>), kSmem<HD, QT>, st, tm_q, maps.rows, maps.atoms, a);
+    const dim3 grid(QT == 1 ? 2 * sms : sms);
+    e = launch_kernel(paged_attention_tc_kernel<HD, QT>, grid, dim3(kThreads<QT>), kSmem<HD, QT>, st, tm_q, maps.rows, maps.atoms, a);
+    if (e != cudaSuccess) return e;
+    return launch_kernel(paged_merge_kernel<HD>, dim3(grid.x, QT * kPagedPartRows / 32), dim3(128), 0, st, a);
 }
 
 }  // namespace
