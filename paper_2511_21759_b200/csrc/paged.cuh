@@ -7,8 +7,8 @@
 namespace odb {
 
 constexpr int kPagedMaxSeqs = 1024;        // requests of one forward
-constexpr int kPagedMaxCtas = 304;         // CTAs of an attention launch, at most: two on each of the 148 SMs and a few
-constexpr int kPagedPartRows = 128;         // rows of a part with two CTAs on an SM; twice that with one
+constexpr int kPagedMaxCtas = 4864;        // CTAs of an attention launch, at most (of 16 rows; in proportion fewer with more)
+constexpr int kPagedPartRows = 16 * kPagedMaxCtas;   // rows that the workspace holds of all CTAs' first or last items
 constexpr int kPagedMaxParts = 2;          // unfinished segments a CTA leaves behind: of its first item and of its last
 constexpr int kPagedUnlimited = 1 << 30;   // a window side without limit; lengths and positions stay below it
 
@@ -72,6 +72,8 @@ struct PagedAttnArgs {
     unsigned int* arrivals;                               // [kPagedMaxCtas], zero between launches
     float* part_o;                                        // [ctas][2][part_rows][HD]
     float* part_ml;                                       // [ctas][2][part_rows][2]
+    int merge_later;                                      // 1: shared items are added up by a kernel of its own
+    int at_once;                                          // CTAs that run at one time
     int part_rows;                                        // rows of a tile
     struct PagedShared* shared;                           // [kPagedMaxCtas], of the last launch that adds up in a kernel of its own
     PagedDiv by_group, by_rows;                           // divisions by G and by the packed rows of an item
@@ -187,35 +189,62 @@ __device__ __forceinline__ int paged_upper(const int* v, int n, int x) {   // th
 }
 
 // Called by all THREADS threads of the block; false: there is nothing for this CTA to do.
-// min_units: what a CTA takes at least (more than E) where there is less than the grid could share.
+// min_units: what a CTA takes at least (more than E); full_units: what it takes at least as long as `at_once` CTAs, those that run
+// at one time, have work.
 // The launcher's bounds on rows, requests and keys keep every sum below 2^31.
 template <int THREADS, int KT, int E>
-__device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int min_units, PagedStart& st) {
+__device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int min_units, int full_units, int at_once, PagedStart& st) {
     const int tid = threadIdx.x;
-    int n_rt;
     auto kept = [&](int s) {          // the request's numbers, loaded once
         const int4 v = sc.seq[s];
         PagedSeq q{v.x, v.y, v.z, v.w, 0};
         q.tiles(a);
         return q;
     };
-    {
-        const int per = (a.n_seqs + THREADS - 1) / THREADS, s0 = min(tid * per, a.n_seqs), s1 = min(s0 + per, a.n_seqs);
-        int mine = 0;
+    auto share = [&](int per_head, int& rem) {   // this CTA's part of the line, and its place within a head's
+        const int total = per_head * a.KV;
+        const int even = static_cast<int>((static_cast<unsigned>(total) + gridDim.x - 1) / gridDim.x);
+        st.chunk = max(max(even, min_units), min(full_units, static_cast<int>((static_cast<unsigned>(total) + at_once - 1) / at_once)));
+        if (static_cast<long long>(st.chunk) * blockIdx.x >= total) return false;
+        st.u0 = st.chunk * blockIdx.x;
+        st.u1 = total - st.u0 < st.chunk ? total : st.u0 + st.chunk;
+        st.head = st.u0 / per_head;
+        rem = st.u0 - st.head * per_head;
+        return true;
+    };
+    const int per_s = (a.n_seqs + THREADS - 1) / THREADS, s0 = min(tid * per_s, a.n_seqs), s1 = min(s0 + per_s, a.n_seqs);
+    int n_rt, mine_rt = 0, units = 0, rem;
+    bool several = false;
 #pragma unroll 4
-        for (int s = s0; s < s1; ++s) {
-            const PagedSeq q = paged_seq(a, s);
-            sc.seq[s] = make_int4(q.row0, q.n, q.first, q.len);
-            mine += q.n_rt;
-        }
-        int at = paged_block_scan<THREADS>(mine, sc.warp_sum, n_rt);
+    for (int s = s0; s < s1; ++s) {
+        const PagedSeq q = paged_seq(a, s);
+        sc.seq[s] = make_int4(q.row0, q.n, q.first, q.len);
+        mine_rt += q.n_rt;
+        several = several || q.n_rt > 1;
+        sc.sum[s] = units;
+        if (q.n_rt > 0) units += paged_keys<KT>(a, q, 0).n + E;
+    }
+    if (!__syncthreads_or(several)) {   // no request has more than a row tile (single tokens, short blocks): sums over the requests do
+        int per_head;
+        const int before = paged_block_scan<THREADS>(units, sc.warp_sum, per_head);
+        if (per_head == 0) return false;
+        for (int s = s0; s < s1; ++s) sc.sum[s] += before;
+        if (!share(per_head, rem)) return false;
+        __syncthreads();
+        st.seq = paged_upper(sc.sum, a.n_seqs, rem);
+        st.rt = 0;
+        st.off = rem - sc.sum[st.seq];
+        __syncthreads();                // the scratch may be overwritten now
+        return true;
+    }
+    {
+        int at = paged_block_scan<THREADS>(mine_rt, sc.warp_sum, n_rt);
         for (int s = s0; s < s1; ++s) {
             sc.rt0[s] = at;
             at += kept(s).n_rt;
         }
         if (tid == 0) sc.rt0[a.n_seqs] = n_rt;
     }
-    if (n_rt == 0) return false;
     __syncthreads();
     const int group = (n_rt + kPagedEntries - 1) / kPagedEntries, entries = group == 1 ? n_rt : (n_rt + group - 1) / group;
     int per_head;
@@ -238,13 +267,7 @@ __device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int m
         for (int e = e0; e < e1; ++e) sc.sum[e] += before;
         __syncthreads();
     }
-    const int total = per_head * a.KV;
-    st.chunk = max(min_units, static_cast<int>((static_cast<unsigned>(total) + gridDim.x - 1) / gridDim.x));
-    if (static_cast<long long>(st.chunk) * blockIdx.x >= total) return false;
-    st.u0 = st.chunk * blockIdx.x;
-    st.u1 = total - st.u0 < st.chunk ? total : st.u0 + st.chunk;
-    st.head = st.u0 / per_head;
-    const int rem = st.u0 - st.head * per_head;
+    if (!share(per_head, rem)) return false;
     const int e = paged_upper(sc.sum, entries, rem);
     const int j = e * group;
     int left = rem - sc.sum[e];
@@ -348,57 +371,62 @@ __device__ __forceinline__ uint32_t paged_bf16x2(float a, float b) {
 __device__ __forceinline__ size_t paged_part(const PagedAttnArgs& a, int cta, bool begins) {
     return (static_cast<size_t>(cta) * kPagedMaxParts + (begins ? 1 : 0)) * a.part_rows;
 }
-// Rows of an item's parts, which CTAs c0 .. c1 have written, added up in the order of the CTAs with a running maximum: RB rows
-// of a warp at a time, so that their loads are in flight together.
+// Parts of RB rows (r0, r0 + step ..) of an item that begins in CTA c0, added up in the order of the CTAs with a running maximum;
+// all rows' loads of several parts are in flight together.
 template <int HD, int RB>
-__device__ __forceinline__ void paged_merge_rows(const PagedAttnArgs& a, int row0, int head, int first_idx, int rows, int c0, int c1, int r0, int step) {
-    constexpr int V = HD / 32;                       // dims of a lane
-    const int lane = threadIdx.x & 31;
+struct PagedSum {
+    static constexpr int V = HD / 32;                // dims of a lane
     float M[RB], L[RB], acc[RB][V];
+
+    __device__ __forceinline__ PagedSum() {
 #pragma unroll
-    for (int k = 0; k < RB; ++k) {
-        M[k] = -INFINITY;
-        L[k] = 0.f;
+        for (int k = 0; k < RB; ++k) {
+            M[k] = -INFINITY;
+            L[k] = 0.f;
 #pragma unroll
-        for (int j = 0; j < V; ++j) acc[k][j] = 0.f;
+            for (int j = 0; j < V; ++j) acc[k][j] = 0.f;
+        }
     }
-    constexpr int CU = RB == 1 ? 8 : 16 / RB;        // parts in flight
-    for (int c = c0; c <= c1; c += CU) {
-        float2 ml[CU][RB];
-        float x[CU][RB][V];
+    __device__ __forceinline__ void add(int k, float m, float l, const float (&x)[V]) {
+        const float top = fmaxf(M[k], m), f = paged_weight(M[k], top), e = paged_weight(m, top);
+        M[k] = top;
+        L[k] = L[k] * f + l * e;
 #pragma unroll
-        for (int u = 0; u < CU; ++u)
+        for (int j = 0; j < V; ++j) acc[k][j] = acc[k][j] * f + x[j] * e;
+    }
+    __device__ __forceinline__ void parts(const PagedAttnArgs& a, int c0, int from, int to, int r0, int step, int rows) {   // CTAs [from, to)
+        const int lane = threadIdx.x & 31;
+        constexpr int CU = 16 / RB;                  // parts in flight
+        for (int c = from; c < to; c += CU) {
+            float2 ml[CU][RB];
+            float x[CU][RB][V];
 #pragma unroll
-            for (int k = 0; k < RB; ++k) {
-                const size_t slot = paged_part(a, min(c + u, c1), c + u == c0) + min(r0 + k * step, rows - 1);
-                ml[u][k] = __ldcg(reinterpret_cast<const float2*>(a.part_ml + slot * 2));
-                const float* po = a.part_o + slot * HD + lane * V;
-                if constexpr (V == 4) {
-                    const float4 t = __ldcg(reinterpret_cast<const float4*>(po));
-                    x[u][k][0] = t.x; x[u][k][1] = t.y; x[u][k][2] = t.z; x[u][k][3] = t.w;
-                } else {
-                    const float2 t = __ldcg(reinterpret_cast<const float2*>(po));
-                    x[u][k][0] = t.x; x[u][k][1] = t.y;
+            for (int u = 0; u < CU; ++u)
+#pragma unroll
+                for (int k = 0; k < RB; ++k) {
+                    const int cta = min(c + u, to - 1);
+                    const size_t slot = paged_part(a, cta, cta == c0) + min(r0 + k * step, rows - 1);
+                    ml[u][k] = __ldcg(reinterpret_cast<const float2*>(a.part_ml + slot * 2));
+                    const float* po = a.part_o + slot * HD + lane * V;
+                    if constexpr (V == 4) {
+                        const float4 t = __ldcg(reinterpret_cast<const float4*>(po));
+                        x[u][k][0] = t.x; x[u][k][1] = t.y; x[u][k][2] = t.z; x[u][k][3] = t.w;
+                    } else {
+                        const float2 t = __ldcg(reinterpret_cast<const float2*>(po));
+                        x[u][k][0] = t.x; x[u][k][1] = t.y;
+                    }
                 }
-            }
 #pragma unroll
-        for (int u = 0; u < CU; ++u) {
-            if (c + u > c1) break;
+            for (int u = 0; u < CU; ++u) {
+                if (c + u >= to) break;
 #pragma unroll
-            for (int k = 0; k < RB; ++k) {
-                const float m = fmaxf(M[k], ml[u][k].x), f = paged_weight(M[k], m), e = paged_weight(ml[u][k].x, m);
-                M[k] = m;
-                L[k] = L[k] * f + ml[u][k].y * e;
-#pragma unroll
-                for (int j = 0; j < V; ++j) acc[k][j] = acc[k][j] * f + x[u][k][j] * e;
+                for (int k = 0; k < RB; ++k) add(k, ml[u][k].x, ml[u][k].y, x[u][k]);
             }
         }
     }
-#pragma unroll
-    for (int k = 0; k < RB; ++k) {
-        const int r = r0 + k * step;
-        if (r >= rows) break;
-        const int idx = first_idx + r, i = a.by_group(idx), h = head * a.G + idx - i * a.G;
+    // output of packed row idx of the request whose rows begin at row0
+    __device__ __forceinline__ void write(const PagedAttnArgs& a, int k, int row0, int head, int idx) const {
+        const int lane = threadIdx.x & 31, i = a.by_group(idx), h = head * a.G + idx - i * a.G;
         const size_t row = static_cast<size_t>(row0 + i);
         const float inv = L[k] == 0.f ? 0.f : 1.0f / L[k];
         uint32_t* op = reinterpret_cast<uint32_t*>(a.out + row * a.out_stride + h * HD + lane * V);
@@ -406,14 +434,7 @@ __device__ __forceinline__ void paged_merge_rows(const PagedAttnArgs& a, int row
         for (int j = 0; j < V; j += 2) op[j / 2] = paged_bf16x2(acc[k][j] * inv, acc[k][j + 1] * inv);
         if (a.lse && lane == 0) a.lse[row * a.H + h] = paged_lse(M[k], L[k]);
     }
-}
-template <int HD>
-__device__ __forceinline__ void paged_merge(const PagedAttnArgs& a, int row0, int head, int first_idx, int rows, int c0, int c1, int warp, int warps) {
-    if (rows > 4 * warps)
-        for (int r = warp; r < rows; r += 8 * warps) paged_merge_rows<HD, 8>(a, row0, head, first_idx, rows, c0, c1, r, warps);
-    else
-        for (int r = warp; r < rows; r += warps) paged_merge_rows<HD, 1>(a, row0, head, first_idx, rows, c0, c1, r, warps);
-}
+};
 
 #endif
 

@@ -85,7 +85,7 @@ int32_t odb_paged_create(const odb_paged_config* cfg, void* kv, size_t kv_bytes,
     h->part_ml = h->part_o + paged_part_bytes(cfg->head_dim) / sizeof(float) / (cfg->head_dim + 2) * cfg->head_dim;
     cudaError_t e = cudaGetDevice(&h->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, h->device);
-    if (e == cudaSuccess && 2 * h->sms > kPagedMaxCtas) h->sms = kPagedMaxCtas / 2;
+    if (e == cudaSuccess && h->sms > 148) h->sms = 148;         // what the workspace has parts for
     if (e == cudaSuccess) e = make_pool_tmap(&h->maps.rows, kv, h->pool_rows, cfg->head_dim, cfg->page_size < 64 ? cfg->page_size : 64, cfg->head_dim / 64);
     if (e == cudaSuccess) e = make_pool_tmap(&h->maps.atoms, kv, h->pool_rows, cfg->head_dim, cfg->page_size < 64 ? cfg->page_size : 64, 1);
     cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -23,12 +23,15 @@ namespace {
 
 constexpr int kKT = 64;                    // keys per tile
 constexpr int kItem = 2;                    // key tiles that an item costs beside its own
+constexpr int kMinUnits = 4, kFullUnits = 24;   // units of a CTA, at least; where all places on the SMs have work
+constexpr int kWaves = 3;                   // CTAs for each place on the SMs
 constexpr int kMmaWarps = 4;
 constexpr int kThreads = 32 * (kMmaWarps + 1);
 template <int HD> constexpr int kStages = HD == 128 ? 3 : 6;
 template <int HD> constexpr uint32_t kTileBytes = kKT * HD * 2;            // K or V of a tile
 template <int HD> constexpr uint32_t kMergeBytes = 2 * 16 * HD * 4;        // two warps' outputs
-template <int HD> constexpr uint32_t kSmem = 1024 + kStages<HD> * 2 * kTileBytes<HD> + kMergeBytes<HD> + 1024;
+template <int HD> constexpr uint32_t kSmem = kStages<HD> * 2 * kTileBytes<HD> + kMergeBytes<HD> + 1024;
+static_assert(2 * (kSmem<128> + 1024) <= 228 * 1024 && 2 * (kSmem<64> + 1024) <= 228 * 1024, "two CTAs share an SM");
 
 struct Barriers {
     uint64_t full[6], empty[6];
@@ -89,13 +92,18 @@ template <int HD, int ROWS>
 __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __grid_constant__ CUtensorMap tm, const PagedAttnArgs a) {
     constexpr int WR = ROWS / 16, WK = kMmaWarps / WR, KW = kKT / WK;   // warps along the rows and the keys, keys of a warp
     constexpr int kAtoms = HD / 64, NS = KW / 8, ND = HD / 8;
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    uint8_t* smem = smem_raw;
     float* merge = reinterpret_cast<float*>(smem + kStages<HD> * 2 * kTileBytes<HD>);
     Barriers* sh = reinterpret_cast<Barriers*>(smem + kStages<HD> * 2 * kTileBytes<HD> + kMergeBytes<HD>);
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     volatile int* cta_abort = &sh->abort;
 
+    if ((smem_u32(smem_raw) & 1023u) != 0) {                    // the swizzled tiles need 1024-byte alignment
+        if (tid == 0) atomicExch(a.status, ODB_ERR_CUDA);
+        pdl_wait();
+        return;
+    }
     if (tid == 0) {
         for (int i = 0; i < kStages<HD>; ++i) {
             mbar_init(&sh->full[i], 1);
@@ -109,7 +117,8 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
     // the ring's memory holds the sums until the start is found
     static_assert(sizeof(PagedScratch) <= kStages<64> * 2 * kTileBytes<64>, "the scratch fits the ring");
     PagedStart start;
-    const bool any = paged_find_start<kThreads, kKT, kItem>(a, *reinterpret_cast<PagedScratch*>(smem), kItem + 2, start);
+    const bool any = paged_find_start<kThreads, kKT, kItem>(a, *reinterpret_cast<PagedScratch*>(smem), kMinUnits, kFullUnits, a.at_once, start);
+    if (a.merge_later && tid == 0) a.shared[blockIdx.x].rows = 0;   // thread 0 writes it again where an item begins here and ends elsewhere
     if (!any) return;                                           // block-uniform
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the scratch's writes before the copies that take its place
     __syncthreads();
@@ -412,7 +421,16 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                 }
             }
         }
-        if (!final) {
+        if (!final && a.merge_later) {
+            if (w.t0 == 0 && tid == 0) {
+                PagedShared& d = a.shared[blockIdx.x];
+                d.row0 = w.q.row0;
+                d.head = w.head;
+                d.first_idx = w.rt * ROWS;
+                d.last_cta = w.last_cta();
+                d.rows = rows;
+            }
+        } else if (!final) {
             __threadfence();
             mma_warps_barrier();
             const int c0 = w.first_cta(), c1 = w.last_cta();
@@ -424,11 +442,56 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
             }
             mma_warps_barrier();
             if (sh->last) {
-                paged_merge<HD>(a, w.q.row0, w.head, w.rt * ROWS, rows, c0, c1, warp, kMmaWarps);
+                for (int r = warp; r < rows; r += kMmaWarps) {
+                    PagedSum<HD, 1> sum;
+                    sum.parts(a, c0, c0, c1 + 1, r, 0, rows);
+                    sum.write(a, 0, w.q.row0, w.head, w.rt * ROWS + r);
+                }
                 mma_warps_barrier();                             // sh->last has been read by all
             }
         }
     } while (w.next());
+}
+
+// Adds up the parts of the items that several CTAs share, a block an item: several warps a row where there are few rows.
+constexpr int kMergeWarps = 16;
+template <int HD>
+__global__ void __launch_bounds__(32 * kMergeWarps) paged_merge_kernel(const PagedAttnArgs a) {
+    __shared__ float ml[kMergeWarps][2], part[kMergeWarps][HD];
+    constexpr int V = HD / 32;
+    pdl_launch_dependents();
+    pdl_wait();
+    const PagedShared d = a.shared[blockIdx.x];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c0 = blockIdx.x, n = d.last_cta + 1 - c0;
+    if (d.rows == 0) return;
+    const int split = max(1, kMergeWarps / d.rows);                 // warps of a row, each with its share of the parts
+    for (int r = warp / split; r < d.rows; r += kMergeWarps / split) {
+        const int piece = warp % split;
+        PagedSum<HD, 1> sum;
+        sum.parts(a, c0, c0 + n * piece / split, c0 + n * (piece + 1) / split, r, 0, d.rows);
+        if (split == 1) {
+            sum.write(a, 0, d.row0, d.head, d.first_idx + r);
+            continue;
+        }
+        if (lane == 0) {
+            ml[warp][0] = sum.M[0];
+            ml[warp][1] = sum.L[0];
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) part[warp][lane * V + j] = sum.acc[0][j];
+    }
+    if (split == 1) return;                                         // block-uniform
+    __syncthreads();
+    if (warp % split == 0 && warp / split < d.rows) {               // with several warps a row there is one row a warp
+        PagedSum<HD, 1> sum;
+        for (int p = 0; p < split; ++p) {
+            float x[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) x[j] = part[warp + p][lane * V + j];
+            sum.add(0, ml[warp + p][0], ml[warp + p][1], x);
+        }
+        sum.write(a, 0, d.row0, d.head, d.first_idx + warp / split);
+    }
 }
 
 template <int HD, int ROWS>
@@ -438,7 +501,19 @@ cudaError_t launch_few(PagedAttnArgs a, const CUtensorMap& tmap, int sms, cudaSt
     if (e != cudaSuccess) return e;
     a.tile_rows = ROWS;
     a.by_rows = PagedDiv::by(ROWS);
-    return launch_kernel(paged_attention_kernel<HD, ROWS>, dim3(2 * sms), dim3(kThreads), kSmem<HD>, st, tmap, a);
+    a.part_rows = ROWS;
+    a.at_once = 2 * sms;
+    // Several CTAs for each place on the SMs: under a full memory system some SMs run a third slower than others, and the shares of
+    // a grid of just two CTAs an SM end far apart.  No more than the table's width leaves work for.
+    const long long tiles = (static_cast<long long>(a.table_stride) << a.page_shift) / kKT + 1 + kItem,
+                    most = (static_cast<long long>(a.max_rows) * a.G / ROWS + a.n_seqs) * a.KV * tiles / kMinUnits + 1;
+    const int grid = static_cast<int>(most < kWaves * 2 * sms ? most : kWaves * 2 * sms);
+    // A small grid's parts are added up by the CTA that arrives last, without a second launch; with a full memory system behind its
+    // loads that took it up to 55 us for 55 parts.
+    a.merge_later = grid > 2 * sms;
+    e = launch_kernel(paged_attention_kernel<HD, ROWS>, dim3(grid), dim3(kThreads), kSmem<HD>, st, tmap, a);
+    if (e != cudaSuccess || !a.merge_later) return e;
+    return launch_kernel(paged_merge_kernel<HD>, dim3(grid), dim3(32 * kMergeWarps), 0, st, a);
 }
 
 template <int HD>
@@ -450,14 +525,13 @@ cudaError_t launch_hd(const PagedAttnArgs& a, const CUtensorMap& tmap, long long
 
 }  // namespace
 
-size_t paged_part_bytes(int hd) { return static_cast<size_t>(kPagedMaxCtas) * kPagedMaxParts * kPagedPartRows * (hd + 2) * sizeof(float); }
+size_t paged_part_bytes(int hd) { return static_cast<size_t>(kPagedMaxParts) * kPagedPartRows * (hd + 2) * sizeof(float); }
 
 cudaError_t launch_paged_attention(PagedAttnArgs a, const PagedMaps& maps, int hd, int max_new, int sms, cudaStream_t st) {
-    if (sms < 1 || 2 * sms > kPagedMaxCtas) return cudaErrorInvalidValue;
+    if (sms < 1 || kWaves * 2 * sms * 64 > kPagedPartRows) return cudaErrorInvalidValue;   // every kernel's parts fit the workspace
     a.by_group = PagedDiv::by(a.G);
     const long long rows = static_cast<long long>(max_new) * a.G;
     if (rows > 64 && a.G <= kPagedTcMaxGroup) return launch_paged_attention_tc(a, maps, hd, rows > 128 ? 2 : 1, sms, st);
-    a.part_rows = 64;
     return hd == 128 ? launch_hd<128>(a, maps.rows, rows, sms, st) : launch_hd<64>(a, maps.rows, rows, sms, st);
 }
 

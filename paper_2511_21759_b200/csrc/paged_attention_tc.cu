@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
 
     PagedStart start;
     static_assert(sizeof(PagedScratch) <= kSmem<64, 1> - 512, "the scratch fits the tiles");
-    const bool any = paged_find_start<kThreads<QT>, kKT, kItem>(a, *reinterpret_cast<PagedScratch*>(sQ), kItem + 2, start);
+    const bool any = paged_find_start<kThreads<QT>, kKT, kItem>(a, *reinterpret_cast<PagedScratch*>(sQ), kItem + 2, 0, gridDim.x, start);
     proxy_fence();                                          // the scratch's writes before the copies that take its place
     __syncthreads();
 
@@ -585,7 +585,12 @@ __global__ void __launch_bounds__(128) paged_merge_kernel(const PagedAttnArgs a)
     pdl_wait();
     const PagedShared d = a.shared[blockIdx.x];
     const int warp = threadIdx.x >> 5, r0 = blockIdx.y * 32 + warp;
-    if (r0 < d.rows) paged_merge_rows<HD, 8>(a, d.row0, d.head, d.first_idx, d.rows, blockIdx.x, d.last_cta, r0, 4);
+    if (r0 >= d.rows) return;
+    PagedSum<HD, 8> sum;
+    sum.parts(a, blockIdx.x, blockIdx.x, d.last_cta + 1, r0, 4, d.rows);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        if (r0 + 4 * k < d.rows) sum.write(a, k, d.row0, d.head, d.first_idx + r0 + 4 * k);
 }
 
 template <int HD, int QT>
@@ -596,7 +601,7 @@ cudaError_t launch(const PagedAttnArgs& a, const CUtensorMap& tm_q, const PagedM
     const dim3 grid(QT == 1 ? 2 * sms : sms);
     e = launch_kernel(paged_attention_tc_kernel<HD, QT>, grid, dim3(kThreads<QT>), kSmem<HD, QT>, st, tm_q, maps.rows, maps.atoms, a);
     if (e != cudaSuccess) return e;
-    return launch_kernel(paged_merge_kernel<HD>, dim3(grid.x, QT * kPagedPartRows / 32), dim3(128), 0, st, a);
+    return launch_kernel(paged_merge_kernel<HD>, dim3(grid.x, QT * kTQ / 32), dim3(128), 0, st, a);
 }
 
 }  // namespace
@@ -605,7 +610,7 @@ cudaError_t launch_paged_attention_tc(PagedAttnArgs a, const PagedMaps& maps, in
     a.tile_tokens = kTQ / a.G;
     a.tile_rows = q_tiles * a.tile_tokens * a.G;
     a.by_rows = PagedDiv::by(a.tile_rows);
-    a.part_rows = q_tiles * kPagedPartRows;
+    a.part_rows = q_tiles * kTQ;
     CUtensorMap tm_q;
     const cudaError_t e = make_group_tmap(&tm_q, a.q, a.max_rows, a.q_stride, a.H, hd, a.G, a.tile_tokens);
     if (e != cudaSuccess) return e;

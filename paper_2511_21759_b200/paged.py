@@ -22,6 +22,7 @@ import torch
 
 from . import binding as B
 
+_BF16, _F32 = torch.bfloat16, torch.float32
 SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 
 
@@ -40,6 +41,7 @@ class Rope:
         self.rot_dim, self.interleaved, self.magnitude = rot_dim, interleaved, mag.value
         # fractions of a turn per position, 64-bit patterns
         self.turns = torch.tensor([C.c_int64(v).value for v in host], dtype=torch.int64, device=device)
+        self.index = self.turns.get_device()
         self._tail = (self.turns.data_ptr(), rot_dim, 1 if interleaved else 0, mag.value)
 
 
@@ -87,6 +89,11 @@ class Batch:
         self._c = B.odb_paged_batch(n_seqs, self.max_rows, self.max_new, table.shape[1] if table is not None else 1,
                                     *[None if given[n] is None else given[n].data_ptr() for n in self._INPUTS])
         self._ref = C.byref(self._c)
+        # shapes of its rows, heads apart and together
+        n, d = self.max_rows, cache.head_dim
+        self._q = (torch.Size((n, cache.n_heads, d)), torch.Size((n, cache.n_heads * d)))
+        self._kv = (torch.Size((n, cache.n_kv_heads, d)), torch.Size((n, cache.n_kv_heads * d)))
+        self._lse = torch.Size((n, cache.n_heads))
 
 
 class PagedCache:
@@ -113,7 +120,7 @@ class PagedCache:
         with torch.cuda.device(self.device):
             B.check(lib.odb_paged_create(C.byref(self.cfg), kv.data_ptr(), kv.numel() * 2, self.workspace.data_ptr(),
                                          self.workspace.numel(), C.c_void_p(stream.cuda_stream), C.byref(self.handle)), "odb_paged_create")
-        self._stream = stream
+        self._stream, self._raw, self._index = stream, stream.cuda_stream, self.device.index
         self._layout, self._store, self._attention = lib.odb_paged_layout, lib.odb_paged_norm_rope_store, lib.odb_paged_attention
 
     def close(self):
@@ -123,53 +130,63 @@ class PagedCache:
 
     def _current(self) -> int:
         """The current stream's handle; behind a call on another stream, that one's work comes first."""
-        st = torch.cuda.current_stream(self.device)
-        if st != self._stream:
+        raw = torch._C._cuda_getCurrentRawStream(self._index)
+        if raw != self._raw:
+            st = torch.cuda.current_stream(self.device)
             if not torch.cuda.is_current_stream_capturing():
                 st.wait_stream(self._stream)
-            self._stream = st
-        return st.cuda_stream
+            self._stream, self._raw = st, raw
+        return raw
 
-    def _rows(self, t, what: str, heads: int, rows: int):
-        """(pointer, elements from row to row) of [rows][heads][head_dim], the last two dims together or apart."""
-        width = heads * self.head_dim
-        if t.dtype is not torch.bfloat16 or t.device != self.device:
-            raise ValueError(f"{what}: a bfloat16 tensor on {self.device} is wanted")
-        shape, stride = t.shape, t.stride()
-        if len(shape) == 2:
-            ok = shape[1] == width and (width == 1 or stride[1] == 1)
-        else:
-            ok = len(shape) == 3 and shape[1] == heads and shape[2] == self.head_dim and stride[2] == 1 and (heads == 1 or stride[1] == self.head_dim)
-        if not ok or shape[0] != rows:
-            raise ValueError(f"{what}: [{rows}][{heads}][{self.head_dim}] with a row's values together is wanted, got {tuple(shape)} by {stride}")
-        return t.data_ptr(), stride[0] if rows > 1 else max(stride[0], width)
+    def _wrong(self, t, what: str, heads: int, rows: int):
+        if not isinstance(t, torch.Tensor) or t.dtype is not torch.bfloat16 or t.device != self.device:
+            return ValueError(f"{what}: a bfloat16 tensor on {self.device} is wanted")
+        return ValueError(f"{what}: [{rows}][{heads}][{self.head_dim}] with a row's values together is wanted, got {tuple(t.shape)} by {t.stride()}")
+
+    # The checks of a tensor are most of what a small call costs on the host: each question is asked once, of the tensor's own methods.
+    def _rows(self, t, what: str, heads: int, shapes):
+        """(pointer, elements from row to row) of [rows][heads][head_dim], the last two dims together or apart; shapes: the two."""
+        if t.dtype is _BF16 and t.get_device() == self._index:
+            shape = t.shape
+            if shape == shapes[0]:
+                stride, head, last = t.stride()
+                if last == 1 and (heads == 1 or head == self.head_dim):
+                    return t.data_ptr(), stride if shape[0] > 1 else shapes[1][1]     # of one row: any number
+            elif shape == shapes[1]:
+                stride, last = t.stride()
+                if last == 1:
+                    return t.data_ptr(), stride if shape[0] > 1 else shapes[1][1]
+        raise self._wrong(t, what, heads, shapes[0][0])
 
     def _gain(self, t, what: str):
         if t is None:
             return None
-        if t.dtype is not torch.float32 or t.device != self.device or t.shape != (self.head_dim,) or not t.is_contiguous():
-            raise ValueError(f"{what}: a contiguous float32 tensor of {self.head_dim} values on {self.device} is wanted")
-        return t.data_ptr()
+        if t.dtype is _F32 and t.get_device() == self._index and t.shape == (self.head_dim,) and t.is_contiguous():
+            return t.data_ptr()
+        raise ValueError(f"{what}: a contiguous float32 tensor of {self.head_dim} values on {self.device} is wanted")
 
     def layout(self, batch: Batch):
         """Block tables, free list and row maps of the forward (odb_paged_layout); the batch's arrays are updated."""
-        B.check(self._layout(self.handle, batch._ref, self._current()), "odb_paged_layout")
+        status = self._layout(self.handle, batch._ref, self._current())
+        if status:
+            raise B.OdbError(status, "odb_paged_layout")
 
     def norm_rope_store(self, layer: int, batch: Batch, q, k, v, rope: Rope, *, q_gain=None, k_gain=None, eps: float = 1e-6, q_out=None):
         """Norm of every q and k head (where a gain is given), rotation by row_pos, K and V into row_slot
         (odb_paged_norm_rope_store).  q, k, v: [max_rows][heads][head_dim] or [max_rows][heads * head_dim], slices of one
         projection's output as they are.  Returns q_out (a new tensor where none is given; q itself may be given)."""
-        rows = batch.max_rows
         if q_out is None:
-            q_out = torch.empty(rows, self.n_heads, self.head_dim, dtype=torch.bfloat16, device=self.device)
-        if rope.turns.device != self.device:
+            q_out = torch.empty(batch._q[0], dtype=torch.bfloat16, device=self.device)
+        if rope.index != self._index:
             raise ValueError(f"rope: on {self.device} it is wanted")
-        qp, qs = self._rows(q, "q", self.n_heads, rows)
-        kp, ks = self._rows(k, "k", self.n_kv_heads, rows)
-        vp, vs = self._rows(v, "v", self.n_kv_heads, rows)
-        op, os_ = self._rows(q_out, "q_out", self.n_heads, rows)
-        B.check(self._store(self.handle, layer, batch._ref, qp, qs, kp, ks, vp, vs, self._gain(q_gain, "q_gain"), self._gain(k_gain, "k_gain"),
-                            eps, *rope._tail, op, os_, self._current()), "odb_paged_norm_rope_store")
+        qp, qs = self._rows(q, "q", self.n_heads, batch._q)
+        kp, ks = self._rows(k, "k", self.n_kv_heads, batch._kv)
+        vp, vs = self._rows(v, "v", self.n_kv_heads, batch._kv)
+        op, os_ = (qp, qs) if q_out is q else self._rows(q_out, "q_out", self.n_heads, batch._q)
+        status = self._store(self.handle, layer, batch._ref, qp, qs, kp, ks, vp, vs, self._gain(q_gain, "q_gain"), self._gain(k_gain, "k_gain"),
+                             eps, *rope._tail, op, os_, self._current())
+        if status:
+            raise B.OdbError(status, "odb_paged_norm_rope_store")
         return q_out
 
     def attention(self, layer: int, batch: Batch, q, *, left: int = -1, right: int = -1, sinks: int = 0, scale: float = 0.0, out=None, lse=None):
@@ -177,18 +194,18 @@ class PagedCache:
         keys j < len_after with j <= p + right and (j >= p - left or j < sinks); -1: no limit; causal: right=0.
         scale 0: 1 / sqrt(head_dim).  lse: float32 [max_rows][n_heads] to be filled.  Returns out (a new tensor where none
         is given)."""
-        rows = batch.max_rows
         if out is None:
-            out = torch.empty(rows, self.n_heads, self.head_dim, dtype=torch.bfloat16, device=self.device)
-        qp, qs = self._rows(q, "q", self.n_heads, rows)
-        op, os_ = self._rows(out, "out", self.n_heads, rows)
+            out = torch.empty(batch._q[0], dtype=torch.bfloat16, device=self.device)
+        qp, qs = self._rows(q, "q", self.n_heads, batch._q)
+        op, os_ = self._rows(out, "out", self.n_heads, batch._q)
         lp = None
         if lse is not None:
-            if lse.dtype is not torch.float32 or lse.device != self.device or lse.shape != (rows, self.n_heads) or not lse.is_contiguous():
-                raise ValueError(f"lse: a contiguous float32 tensor [{rows}][{self.n_heads}] on {self.device} is wanted")
+            if lse.dtype is not _F32 or lse.get_device() != self._index or lse.shape != batch._lse or not lse.is_contiguous():
+                raise ValueError(f"lse: a contiguous float32 tensor {list(batch._lse)} on {self.device} is wanted")
             lp = lse.data_ptr()
-        B.check(self._attention(self.handle, layer, batch._ref, qp, qs, op, os_, lp, scale, left, right, sinks, self._current()),
-                "odb_paged_attention")
+        status = self._attention(self.handle, layer, batch._ref, qp, qs, op, os_, lp, scale, left, right, sinks, self._current())
+        if status:
+            raise B.OdbError(status, "odb_paged_attention")
         return out
 
     def status(self) -> int:
