@@ -72,7 +72,6 @@ struct PagedAttnArgs {
     unsigned int* arrivals;                               // [kPagedMaxCtas], zero between launches
     float* part_o;                                        // [ctas][2][part_rows][HD]
     float* part_ml;                                       // [ctas][2][part_rows][2]
-    int merge_later;                                      // 1: shared items are added up by a kernel of its own
     int at_once;                                          // CTAs that run at one time
     int part_rows;                                        // rows of a tile
     struct PagedShared* shared;                           // [kPagedMaxCtas], of the last launch that adds up in a kernel of its own
@@ -140,10 +139,53 @@ __device__ __forceinline__ PagedKeys paged_keys(const PagedAttnArgs& a, const Pa
     return k;
 }
 
-// Where a CTA's share of the line begins: `off` units into an item; units [u0, u1), `chunk` a CTA.
+// The line's division: `waves` times as many CTAs as run at one time, of shares that grow smaller from wave to wave (the sizes are
+// of each wave's CTAs; a line that ends early leaves the later ones without work).
+constexpr int kPagedWaves = 4;
+struct PagedShares {
+    int size[kPagedWaves], at_once;
+    __device__ __forceinline__ void divide(int total, int waves, int min_units, int full_units) {
+        // 45, 27, 17 and 11 of a hundred: see the launcher of the few rows' kernel
+        constexpr int kPart[kPagedWaves] = {115, 69, 44, 28};
+        const int most = static_cast<int>((static_cast<unsigned>(total) + at_once - 1) / at_once), least = max(min_units, min(full_units, most));
+        int left = total;
+#pragma unroll
+        for (int w = 0; w < kPagedWaves; ++w) {
+            const int all = static_cast<int>((static_cast<unsigned>(max(left, 0)) + at_once - 1) / at_once);
+            const int part = w + 1 < waves ? static_cast<int>(static_cast<unsigned>(most) * kPart[w] / 256) + 1 : all;
+            size[w] = max(min(part, all), least);
+            left -= min(left, size[w] * at_once);
+        }
+    }
+    __device__ __forceinline__ long long begin(int cta) const {
+        long long u = 0;
+        int i = cta;
+#pragma unroll
+        for (int w = 0; w < kPagedWaves; ++w) {
+            const int n = min(i, at_once);
+            u += static_cast<long long>(n) * size[w];
+            i -= n;
+        }
+        return i > 0 ? 0x7fffffffffffll : u;
+    }
+    __device__ __forceinline__ int owner(int u) const {
+        int cta = 0;
+#pragma unroll
+        for (int w = 0; w < kPagedWaves; ++w) {
+            const long long all = static_cast<long long>(size[w]) * at_once;
+            if (u < all || w + 1 == kPagedWaves) return cta + u / size[w];
+            u -= static_cast<int>(all);
+            cta += at_once;
+        }
+        return cta;
+    }
+};
+
+// Where a CTA's share of the line begins: `off` units into an item; units [u0, u1).
 struct PagedStart {
     int head, seq, rt, off;
-    int u0, u1, chunk;
+    int u0, u1;
+    PagedShares shares;
 };
 
 constexpr int kPagedEntries = 1024;   // sums of units kept while a CTA finds its start
@@ -189,11 +231,11 @@ __device__ __forceinline__ int paged_upper(const int* v, int n, int x) {   // th
 }
 
 // Called by all THREADS threads of the block; false: there is nothing for this CTA to do.
-// min_units: what a CTA takes at least (more than E); full_units: what it takes at least as long as `at_once` CTAs, those that run
-// at one time, have work.
+// waves: CTAs of the grid for each of the `at_once` that run at one time.  min_units: what a CTA takes at least (more than E);
+// full_units: what it takes at least as long as `at_once` CTAs have work.
 // The launcher's bounds on rows, requests and keys keep every sum below 2^31.
 template <int THREADS, int KT, int E>
-__device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int min_units, int full_units, int at_once, PagedStart& st) {
+__device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int waves, int min_units, int full_units, int at_once, PagedStart& st) {
     const int tid = threadIdx.x;
     auto kept = [&](int s) {          // the request's numbers, loaded once
         const int4 v = sc.seq[s];
@@ -203,11 +245,12 @@ __device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int m
     };
     auto share = [&](int per_head, int& rem) {   // this CTA's part of the line, and its place within a head's
         const int total = per_head * a.KV;
-        const int even = static_cast<int>((static_cast<unsigned>(total) + gridDim.x - 1) / gridDim.x);
-        st.chunk = max(max(even, min_units), min(full_units, static_cast<int>((static_cast<unsigned>(total) + at_once - 1) / at_once)));
-        if (static_cast<long long>(st.chunk) * blockIdx.x >= total) return false;
-        st.u0 = st.chunk * blockIdx.x;
-        st.u1 = total - st.u0 < st.chunk ? total : st.u0 + st.chunk;
+        st.shares.at_once = at_once;
+        st.shares.divide(total, waves, min_units, full_units);
+        const long long u0 = st.shares.begin(blockIdx.x), u1 = st.shares.begin(blockIdx.x + 1);
+        if (u0 >= total) return false;
+        st.u0 = static_cast<int>(u0);
+        st.u1 = static_cast<int>(min(u1, static_cast<long long>(total)));
         st.head = st.u0 / per_head;
         rem = st.u0 - st.head * per_head;
         return true;
@@ -295,10 +338,11 @@ struct PagedWalk {
     int head, seq, rt;
     int t0, t1;                      // this CTA's key tiles of the item
     int begin;                       // the unit of the item's first key tile
-    int u1, chunk;
+    int u1;
+    const PagedShares& shares;
 
     __device__ __forceinline__ PagedWalk(const PagedAttnArgs& args, const PagedStart& st)
-        : a(args), head(st.head), seq(st.seq), rt(st.rt), begin(st.u0 - st.off + E), u1(st.u1), chunk(st.chunk) {
+        : a(args), head(st.head), seq(st.seq), rt(st.rt), begin(st.u0 - st.off + E), u1(st.u1), shares(st.shares) {
         q = paged_seq(a, seq);
         k = paged_keys<KT>(a, q, rt);
         t0 = max(0, st.off - E);
@@ -321,8 +365,8 @@ struct PagedWalk {
     }
     __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == k.n; }
     // the CTAs that share the item
-    __device__ __forceinline__ int first_cta() const { return begin / chunk; }
-    __device__ __forceinline__ int last_cta() const { return (begin + k.n - 1) / chunk; }
+    __device__ __forceinline__ int first_cta() const { return shares.owner(begin); }
+    __device__ __forceinline__ int last_cta() const { return shares.owner(begin + k.n - 1); }
 };
 
 // The pages of a request as a warp sees them: 32 entries of its table row at a time, one a lane.  Every lane calls row() with the
@@ -394,6 +438,51 @@ struct PagedSum {
 #pragma unroll
         for (int j = 0; j < V; ++j) acc[k][j] = acc[k][j] * f + x[j] * e;
     }
+    __device__ __forceinline__ void load(const float* p, float (&x)[V]) const {
+        if constexpr (V == 4) {
+            const float4 t = __ldcg(reinterpret_cast<const float4*>(p));
+            x[0] = t.x; x[1] = t.y; x[2] = t.z; x[3] = t.w;
+        } else {
+            const float2 t = __ldcg(reinterpret_cast<const float2*>(p));
+            x[0] = t.x; x[1] = t.y;
+        }
+    }
+    // One row of many parts: 32 parts' maxima and sums at once, one a lane, then their outputs, sixteen in flight.
+    __device__ __forceinline__ void row(const PagedAttnArgs& a, int c0, int c1, int r) {
+        static_assert(RB == 1, "one row");
+        const int lane = threadIdx.x & 31;
+        for (int c = c0; c <= c1; c += 32) {
+            const int n = min(32, c1 + 1 - c), mine = c + min(lane, n - 1);
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(a.part_ml + (paged_part(a, mine, mine == c0) + r) * 2));
+            float top = ml.x;
+#pragma unroll
+            for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            top = fmaxf(top, M[0]);
+            const float w = lane < n ? paged_weight(ml.x, top) : 0.f, f = paged_weight(M[0], top);
+            float l = w * ml.y;
+#pragma unroll
+            for (int d = 16; d >= 1; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+            M[0] = top;
+            L[0] = L[0] * f + l;
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[0][j] *= f;
+            for (int u0 = 0; u0 < n; u0 += 16) {
+                float x[16][V];
+#pragma unroll
+                for (int u = 0; u < 16; ++u) {
+                    const int cta = c + min(u0 + u, n - 1);
+                    load(a.part_o + (paged_part(a, cta, cta == c0) + r) * HD + lane * V, x[u]);
+                }
+#pragma unroll
+                for (int u = 0; u < 16; ++u) {
+                    const float e = __shfl_sync(0xffffffffu, w, (u0 + u) & 31);   // zero behind the last
+                    if (u0 + u < n)
+#pragma unroll
+                        for (int j = 0; j < V; ++j) acc[0][j] += e * x[u][j];
+                }
+            }
+        }
+    }
     __device__ __forceinline__ void parts(const PagedAttnArgs& a, int c0, int from, int to, int r0, int step, int rows) {   // CTAs [from, to)
         const int lane = threadIdx.x & 31;
         constexpr int CU = 16 / RB;                  // parts in flight
@@ -407,14 +496,7 @@ struct PagedSum {
                     const int cta = min(c + u, to - 1);
                     const size_t slot = paged_part(a, cta, cta == c0) + min(r0 + k * step, rows - 1);
                     ml[u][k] = __ldcg(reinterpret_cast<const float2*>(a.part_ml + slot * 2));
-                    const float* po = a.part_o + slot * HD + lane * V;
-                    if constexpr (V == 4) {
-                        const float4 t = __ldcg(reinterpret_cast<const float4*>(po));
-                        x[u][k][0] = t.x; x[u][k][1] = t.y; x[u][k][2] = t.z; x[u][k][3] = t.w;
-                    } else {
-                        const float2 t = __ldcg(reinterpret_cast<const float2*>(po));
-                        x[u][k][0] = t.x; x[u][k][1] = t.y;
-                    }
+                    load(a.part_o + slot * HD + lane * V, x[u][k]);
                 }
 #pragma unroll
             for (int u = 0; u < CU; ++u) {

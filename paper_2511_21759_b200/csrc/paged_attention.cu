@@ -7,7 +7,7 @@
 // relative error of up to 2^-8 per key is independent from key to key and ends below the output's own rounding).
 //
 // Work: see paged.cuh; every CTA takes the same number of key tiles of 64 positions.  One warp loads (TMA, a box per page of
-// a tile, 128-byte swizzle, a ring of stages with a full and an empty barrier each), four warps multiply (mma.sync m16n8k16):
+// a tile, 128-byte swizzle, rings of K and of V tiles with a full and an empty barrier each), four warps multiply (mma.sync m16n8k16):
 // ROWS / 16 groups of rows x 64 / ROWS groups of keys, each warp with a running maximum, sum and output of its own, which
 // meet when the item ends.  An item that several CTAs share leaves unnormalised parts in the workspace; the CTA that arrives
 // last adds them up in the order of the CTAs, whoever it is: the same bits every time.
@@ -24,17 +24,16 @@ namespace {
 constexpr int kKT = 64;                    // keys per tile
 constexpr int kItem = 2;                    // key tiles that an item costs beside its own
 constexpr int kMinUnits = 4, kFullUnits = 24;   // units of a CTA, at least; where all places on the SMs have work
-constexpr int kWaves = 3;                   // CTAs for each place on the SMs
 constexpr int kMmaWarps = 4;
 constexpr int kThreads = 32 * (kMmaWarps + 1);
-template <int HD> constexpr int kStages = HD == 128 ? 3 : 6;
+template <int HD> constexpr int kKSlots = HD == 128 ? 3 : 7;                // K tiles on the way or in use
+template <int HD> constexpr int kVSlots = HD == 128 ? 4 : 7;
 template <int HD> constexpr uint32_t kTileBytes = kKT * HD * 2;            // K or V of a tile
-template <int HD> constexpr uint32_t kMergeBytes = 2 * 16 * HD * 4;        // two warps' outputs
-template <int HD> constexpr uint32_t kSmem = kStages<HD> * 2 * kTileBytes<HD> + kMergeBytes<HD> + 1024;
+template <int HD> constexpr uint32_t kSmem = (kKSlots<HD> + kVSlots<HD>) * kTileBytes<HD> + 1024;
 static_assert(2 * (kSmem<128> + 1024) <= 228 * 1024 && 2 * (kSmem<64> + 1024) <= 228 * 1024, "two CTAs share an SM");
 
 struct Barriers {
-    uint64_t full[6], empty[6];
+    uint64_t k_full[8], v_full[8], k_empty[8], v_empty[8];
     float ml[kMmaWarps][16][2];
     int last, abort;
 };
@@ -94,8 +93,9 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
     constexpr int kAtoms = HD / 64, NS = KW / 8, ND = HD / 8;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t* smem = smem_raw;
-    float* merge = reinterpret_cast<float*>(smem + kStages<HD> * 2 * kTileBytes<HD>);
-    Barriers* sh = reinterpret_cast<Barriers*>(smem + kStages<HD> * 2 * kTileBytes<HD> + kMergeBytes<HD>);
+    constexpr int KS = kKSlots<HD>, VS = kVSlots<HD>;
+    const uint32_t k_tiles = smem_u32(smem), v_tiles = k_tiles + KS * kTileBytes<HD>;
+    Barriers* sh = reinterpret_cast<Barriers*>(smem + (KS + VS) * kTileBytes<HD>);
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     volatile int* cta_abort = &sh->abort;
 
@@ -105,9 +105,13 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
         return;
     }
     if (tid == 0) {
-        for (int i = 0; i < kStages<HD>; ++i) {
-            mbar_init(&sh->full[i], 1);
-            mbar_init(&sh->empty[i], kMmaWarps);
+        for (int i = 0; i < KS; ++i) {
+            mbar_init(&sh->k_full[i], 1);
+            mbar_init(&sh->k_empty[i], kMmaWarps);
+        }
+        for (int i = 0; i < VS; ++i) {
+            mbar_init(&sh->v_full[i], 1);
+            mbar_init(&sh->v_empty[i], kMmaWarps);
         }
         sh->abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -115,18 +119,22 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
     pdl_launch_dependents();
     pdl_wait();
     // the ring's memory holds the sums until the start is found
-    static_assert(sizeof(PagedScratch) <= kStages<64> * 2 * kTileBytes<64>, "the scratch fits the ring");
+    static_assert(sizeof(PagedScratch) <= kSmem<64> - 1024, "the scratch fits the rings");
     PagedStart start;
-    const bool any = paged_find_start<kThreads, kKT, kItem>(a, *reinterpret_cast<PagedScratch*>(smem), kMinUnits, kFullUnits, a.at_once, start);
-    if (a.merge_later && tid == 0) a.shared[blockIdx.x].rows = 0;   // thread 0 writes it again where an item begins here and ends elsewhere
+    const bool any = paged_find_start<kThreads, kKT, kItem>(a, *reinterpret_cast<PagedScratch*>(smem), kPagedWaves, kMinUnits, kFullUnits, a.at_once, start);
     if (!any) return;                                           // block-uniform
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the scratch's writes before the copies that take its place
     __syncthreads();
 
     PagedWalk<kKT, kItem> w(a, start);
     const int box_shift = min(a.page_shift, 6), box = 1 << box_shift;   // rows of a copy
-    int stage = 0;
-    uint32_t phase = 0;
+    struct Ring {
+        int slot = 0;
+        uint32_t phase = 0;
+        __device__ __forceinline__ void next(int slots) {
+            if (++slot == slots) { slot = 0; phase ^= 1u; }
+        }
+    } kr, vr;
 
     if (warp == kMmaWarps) {
         // ================= loader =================
@@ -137,28 +145,35 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
             for (int t = w.t0; t < w.t1 && ok; ++t) {
                 const int k0 = w.k.tile(t) << 6;
                 const int boxes = max(0, (min(kKT, w.k.hi - k0) + box - 1) >> box_shift);
-                if (issued >= kStages<HD>) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh->empty[stage], phase ^ 1u, cta_abort, a.status));
-                if (!ok) break;
-                const uint32_t sg = __shfl_sync(0xffffffffu, stage, 0), dst = smem_u32(smem) + sg * 2 * kTileBytes<HD>;
-                if (paged_elect()) mbar_expect_tx(&sh->full[sg], 2u * boxes * box * HD * 2);
-                __syncwarp();
-                for (int c = 0; c < boxes; ++c) {
-                    const int row = pages.row(a, w.seq, w.head, k0 + (c << box_shift), a.k_row0), row_v = row == a.pool_rows ? row : row + (a.v_row0 - a.k_row0);
-                    if (paged_elect()) {
-                        tma_rows(dst + c * box * HD * 2, &tm, &sh->full[sg], row);
-                        tma_rows(dst + kTileBytes<HD> + c * box * HD * 2, &tm, &sh->full[sg], row_v);
-                    }
+                const uint32_t bytes = static_cast<uint32_t>(boxes) * box * HD * 2;
+                auto load = [&](Ring& r, int slots, uint64_t* empty, uint64_t* full, uint32_t tiles, int base) {
+                    if (issued >= slots) ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(&empty[r.slot], r.phase ^ 1u, cta_abort, a.status));
+                    if (!ok) return;
+                    const uint32_t slot = __shfl_sync(0xffffffffu, r.slot, 0), to = tiles + slot * kTileBytes<HD>;
+                    if (paged_elect()) mbar_expect_tx(&full[slot], bytes);
                     __syncwarp();
-                }
+                    for (int c = 0; c < boxes; ++c) {
+                        const int row = pages.row(a, w.seq, w.head, k0 + (c << box_shift), base);
+                        if (paged_elect()) tma_rows(to + c * box * HD * 2, &tm, &full[slot], row);
+                        __syncwarp();
+                    }
+                    r.next(slots);
+                };
+                load(kr, KS, sh->k_empty, sh->k_full, k_tiles, a.k_row0);
+                load(vr, VS, sh->v_empty, sh->v_full, v_tiles, a.v_row0);
+                if (!ok) break;
                 ++issued;
-                if (++stage == kStages<HD>) { stage = 0; phase ^= 1u; }
             }
         } while (ok && w.next());
         if (!ok) {   // copies in flight land before the memory goes away
             const long long t0 = clock64();
-            for (int j = max(0, issued - kStages<HD>); j < issued; ++j)
-                while (!mbar_try_wait_parity(&sh->full[j % kStages<HD>], static_cast<uint32_t>(j / kStages<HD>) & 1u) && clock64() - t0 < kWaitLimitCycles / 8) {
-                }
+            auto land = [&](uint64_t* full, int slots) {
+                for (int j = max(0, issued + 1 - slots); j <= issued; ++j)   // the last one may have a K tile only
+                    while (!mbar_try_wait_parity(&full[j % slots], static_cast<uint32_t>(j / slots) & 1u) && clock64() - t0 < kWaitLimitCycles / 8) {
+                    }
+            };
+            land(sh->k_full, KS);
+            land(sh->v_full, VS);
         }
         return;
     }
@@ -185,6 +200,9 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
         }
         const int idx_last = w.rt * ROWS + rows - 1;
         const int p_min = w.q.first + a.by_group(w.rt * ROWS), p_max = w.q.first + a.by_group(idx_last);
+        // keys from all_lo on and below all_hi are seen by all rows of the item
+        const int all_hi = static_cast<int>(max(0ll, min(static_cast<long long>(w.q.len), static_cast<long long>(p_min) + a.right + 1)));
+        const int all_lo = static_cast<int>(max(-1ll, static_cast<long long>(p_max) - a.left));
         float o[ND][4];
         float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
@@ -195,8 +213,15 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
         for (int t = w.t0; t < w.t1; ++t) {
             const int k0 = (w.k.tile(t) << 6) + wk * KW;        // this warp's first key
             // Behind an expired wait the warp goes on through the tiles without their products: it must not be missing at a barrier.
-            const bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh->full[stage], phase, cta_abort, a.status));
-            const uint32_t sk = smem_u32(smem) + stage * 2 * kTileBytes<HD>, sv = sk + kTileBytes<HD>;
+            bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh->k_full[kr.slot], kr.phase, cta_abort, a.status));
+            bool k_read = false;
+            auto k_done = [&]() {                               // K's place is free again before the softmax
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh->k_empty[kr.slot]);
+                kr.next(KS);
+                k_read = true;
+            };
+            const uint32_t sk = k_tiles + kr.slot * kTileBytes<HD>, sv = v_tiles + vr.slot * kTileBytes<HD>;
             // key c of the tile, atom h: box (c >> box_shift), then [atom][row of the box][128 bytes]
             auto key_at = [&](int c, int h) -> uint32_t {
                 return static_cast<uint32_t>((((c >> box_shift) * kAtoms + h) << box_shift) + (c & (box - 1))) * 128u;
@@ -210,16 +235,27 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
 #pragma unroll
                 for (int nb = 0; nb < NS; nb += 2) {
                     const int c = wk * KW + nb * 8 + (lane & 7) + ((lane >> 4) << 3);
+                    float odd[2][4] = {};                       // every other step in sums of its own: half as long a chain of products
 #pragma unroll
                     for (int kk = 0; kk < HD / 16; ++kk) {
                         uint32_t b[4];
                         ldsm4(sk + key_at(c, kk >> 2) + (((kk & 3) * 32 + ((lane >> 3) & 1) * 16) ^ sw), b);
-                        mma(s[nb], qf[kk], b[0], b[1]);
-                        mma(s[nb + 1], qf[kk], b[2], b[3]);
+                        if (NS == 2 && (kk & 1)) {
+                            mma(odd[0], qf[kk], b[0], b[1]);
+                            mma(odd[1], qf[kk], b[2], b[3]);
+                        } else {
+                            mma(s[nb], qf[kk], b[0], b[1]);
+                            mma(s[nb + 1], qf[kk], b[2], b[3]);
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        s[nb][j] += odd[0][j];
+                        s[nb + 1][j] += odd[1][j];
                     }
                 }
-                const bool whole = k0 + KW <= min(static_cast<long long>(w.q.len), static_cast<long long>(p_min) + a.right + 1) &&
-                                   (k0 >= p_max - a.left || k0 + KW <= a.sinks);
+                k_done();
+                const bool whole = k0 + KW <= all_hi && (k0 >= all_lo || k0 + KW <= a.sinks);
                 float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
                 for (int nb = 0; nb < NS; ++nb)
@@ -262,6 +298,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
 #pragma unroll
                         for (int j = 0; j < 4; ++j) o[d][j] *= factor[j >> 1];
                 }
+                ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh->v_full[vr.slot], vr.phase, cta_abort, a.status));
                 if (!whole) {
                     // V in places that a row does not see: zero where no row sees it, by the element where it is not finite
                     constexpr int kChunks = KW * HD / 8 / 32;   // 16-byte chunks of a lane
@@ -342,9 +379,14 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                 }
                 if (!whole) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // this warp's writes to V before the next copy into it
             }
+            if (!k_read) {                                      // nothing to multiply: in step with the loader all the same
+                k_done();
+                mbar_wait_bounded(&sh->v_full[vr.slot], vr.phase, cta_abort, a.status);
+            }
+            if (WK > 1 && t + 1 == w.t1) break;                 // the item's last V tile stays: its place is where the warps meet
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sh->empty[stage]);
-            if (++stage == kStages<HD>) { stage = 0; phase ^= 1u; }
+            if (lane == 0) mbar_arrive(&sh->v_empty[vr.slot]);
+            vr.next(VS);
         }
 
         // ---- the warps that share the rows meet ----
@@ -358,7 +400,9 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                     sh->ml[warp][(lane >> 2) + 8 * e][1] = l[e];
                 }
             }
-            mma_warps_barrier();
+            mma_warps_barrier();                                // all have read the last V tile
+            float* merge = reinterpret_cast<float*>(smem + (KS + vr.slot) * kTileBytes<HD>);
+            static_assert(2 * 16 * HD * 4 <= kTileBytes<HD>, "two warps' outputs fit a tile");
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 float M = -INFINITY, L = 0.f;
@@ -396,6 +440,10 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                 }
                 mma_warps_barrier();
             }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh->v_empty[vr.slot]);
+            vr.next(VS);
         }
 
         // ---- results, or this CTA's part of them ----
@@ -421,16 +469,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                 }
             }
         }
-        if (!final && a.merge_later) {
-            if (w.t0 == 0 && tid == 0) {
-                PagedShared& d = a.shared[blockIdx.x];
-                d.row0 = w.q.row0;
-                d.head = w.head;
-                d.first_idx = w.rt * ROWS;
-                d.last_cta = w.last_cta();
-                d.rows = rows;
-            }
-        } else if (!final) {
+        if (!final) {
             __threadfence();
             mma_warps_barrier();
             const int c0 = w.first_cta(), c1 = w.last_cta();
@@ -444,54 +483,13 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
             if (sh->last) {
                 for (int r = warp; r < rows; r += kMmaWarps) {
                     PagedSum<HD, 1> sum;
-                    sum.parts(a, c0, c0, c1 + 1, r, 0, rows);
+                    sum.row(a, c0, c1, r);
                     sum.write(a, 0, w.q.row0, w.head, w.rt * ROWS + r);
                 }
                 mma_warps_barrier();                             // sh->last has been read by all
             }
         }
     } while (w.next());
-}
-
-// Adds up the parts of the items that several CTAs share, a block an item: several warps a row where there are few rows.
-constexpr int kMergeWarps = 16;
-template <int HD>
-__global__ void __launch_bounds__(32 * kMergeWarps) paged_merge_kernel(const PagedAttnArgs a) {
-    __shared__ float ml[kMergeWarps][2], part[kMergeWarps][HD];
-    constexpr int V = HD / 32;
-    pdl_launch_dependents();
-    pdl_wait();
-    const PagedShared d = a.shared[blockIdx.x];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c0 = blockIdx.x, n = d.last_cta + 1 - c0;
-    if (d.rows == 0) return;
-    const int split = max(1, kMergeWarps / d.rows);                 // warps of a row, each with its share of the parts
-    for (int r = warp / split; r < d.rows; r += kMergeWarps / split) {
-        const int piece = warp % split;
-        PagedSum<HD, 1> sum;
-        sum.parts(a, c0, c0 + n * piece / split, c0 + n * (piece + 1) / split, r, 0, d.rows);
-        if (split == 1) {
-            sum.write(a, 0, d.row0, d.head, d.first_idx + r);
-            continue;
-        }
-        if (lane == 0) {
-            ml[warp][0] = sum.M[0];
-            ml[warp][1] = sum.L[0];
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j) part[warp][lane * V + j] = sum.acc[0][j];
-    }
-    if (split == 1) return;                                         // block-uniform
-    __syncthreads();
-    if (warp % split == 0 && warp / split < d.rows) {               // with several warps a row there is one row a warp
-        PagedSum<HD, 1> sum;
-        for (int p = 0; p < split; ++p) {
-            float x[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) x[j] = part[warp + p][lane * V + j];
-            sum.add(0, ml[warp + p][0], ml[warp + p][1], x);
-        }
-        sum.write(a, 0, d.row0, d.head, d.first_idx + warp / split);
-    }
 }
 
 template <int HD, int ROWS>
@@ -503,17 +501,13 @@ cudaError_t launch_few(PagedAttnArgs a, const CUtensorMap& tmap, int sms, cudaSt
     a.by_rows = PagedDiv::by(ROWS);
     a.part_rows = ROWS;
     a.at_once = 2 * sms;
-    // Several CTAs for each place on the SMs: under a full memory system some SMs run a third slower than others, and the shares of
-    // a grid of just two CTAs an SM end far apart.  No more than the table's width leaves work for.
+    // Under a full memory system some SMs run a third slower than others, and so does the second CTA of an SM: of one share for each
+    // place the last ended a third behind the mean.  So four waves of CTAs, taken by whichever place is free, of shares that grow
+    // smaller to the end.  No more CTAs than the table's width leaves work for.
     const long long tiles = (static_cast<long long>(a.table_stride) << a.page_shift) / kKT + 1 + kItem,
                     most = (static_cast<long long>(a.max_rows) * a.G / ROWS + a.n_seqs) * a.KV * tiles / kMinUnits + 1;
-    const int grid = static_cast<int>(most < kWaves * 2 * sms ? most : kWaves * 2 * sms);
-    // A small grid's parts are added up by the CTA that arrives last, without a second launch; with a full memory system behind its
-    // loads that took it up to 55 us for 55 parts.
-    a.merge_later = grid > 2 * sms;
-    e = launch_kernel(paged_attention_kernel<HD, ROWS>, dim3(grid), dim3(kThreads), kSmem<HD>, st, tmap, a);
-    if (e != cudaSuccess || !a.merge_later) return e;
-    return launch_kernel(paged_merge_kernel<HD>, dim3(grid), dim3(32 * kMergeWarps), 0, st, a);
+    const int grid = static_cast<int>(most < kPagedWaves * 2 * sms ? most : kPagedWaves * 2 * sms);
+    return launch_kernel(paged_attention_kernel<HD, ROWS>, dim3(grid), dim3(kThreads), kSmem<HD>, st, tmap, a);
 }
 
 template <int HD>
@@ -528,7 +522,7 @@ cudaError_t launch_hd(const PagedAttnArgs& a, const CUtensorMap& tmap, long long
 size_t paged_part_bytes(int hd) { return static_cast<size_t>(kPagedMaxParts) * kPagedPartRows * (hd + 2) * sizeof(float); }
 
 cudaError_t launch_paged_attention(PagedAttnArgs a, const PagedMaps& maps, int hd, int max_new, int sms, cudaStream_t st) {
-    if (sms < 1 || kWaves * 2 * sms * 64 > kPagedPartRows) return cudaErrorInvalidValue;   // every kernel's parts fit the workspace
+    if (sms < 1 || kPagedWaves * 2 * sms * 64 > kPagedPartRows) return cudaErrorInvalidValue;   // every kernel's parts fit the workspace
     a.by_group = PagedDiv::by(a.G);
     const long long rows = static_cast<long long>(max_new) * a.G;
     if (rows > 64 && a.G <= kPagedTcMaxGroup) return launch_paged_attention_tc(a, maps, hd, rows > 128 ? 2 : 1, sms, st);

@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
 
     PagedStart start;
     static_assert(sizeof(PagedScratch) <= kSmem<64, 1> - 512, "the scratch fits the tiles");
-    const bool any = paged_find_start<kThreads<QT>, kKT, kItem>(a, *reinterpret_cast<PagedScratch*>(sQ), kItem + 2, 0, gridDim.x, start);
+    const bool any = paged_find_start<kThreads<QT>, kKT, kItem>(a, *reinterpret_cast<PagedScratch*>(sQ), 1, kItem + 2, 0, gridDim.x, start);
     proxy_fence();                                          // the scratch's writes before the copies that take its place
     __syncthreads();
 
