@@ -472,9 +472,9 @@ int32_t odb_rope_frequencies(int32_t rot_dim, double theta, int32_t scaling, dou
 
 /* For every row r < max_rows with row_pos[r] >= 0: q_out = rotate(norm(q)), and K := rotate(norm(k)), V := v at
  * row_slot[r] (a slot that is none, -1 for one, stores nothing).  norm: x / sqrt(mean(x^2) + eps) * gain over a head's
- * head_dim values, gains fp32 [head_dim], NULL: no norm (of q, of k).  rotate: pairs (i, i + rot_dim / 2), or (2i, 2i + 1)
+ * head_dim values, gains fp32 [head_dim], on 16-byte boundaries, NULL: no norm (of q, of k).  rotate: pairs (i, i + rot_dim / 2), or (2i, 2i + 1)
  * where interleaved, of the first rot_dim values (a multiple of 8 up to head_dim, 0: none) by position x frequency
- * (turns: device copy of odb_rope_frequencies' numbers); the other values pass.  fp32, rounded once.
+ * (turns: device copy of odb_rope_frequencies' numbers, on a 16-byte boundary); the other values pass.  fp32, rounded once.
  * q [max_rows][n_heads][head_dim], k and v [max_rows][n_kv_heads][head_dim], bf16 on 8-byte boundaries, strides in
  * elements between rows (multiples of 4; the three may be slices of one projection's output).  q_out may be q itself
  * (same stride).  Two rows with the same slot: one of them is stored. */

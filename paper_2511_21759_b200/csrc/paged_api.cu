@@ -168,7 +168,7 @@ int32_t odb_paged_norm_rope_store(odb_paged* h, int32_t layer, const odb_paged_b
     const int64_t qw = static_cast<int64_t>(c.n_heads) * c.head_dim, kw = static_cast<int64_t>(c.n_kv_heads) * c.head_dim;
     if (q_stride < qw || out_stride < qw || k_stride < kw || v_stride < kw) return ODB_ERR_ARG;
     if (!aligned(q, 8) || !aligned(k, 8) || !aligned(v, 8) || !aligned(q_out, 8) || !aligned(q_gain, 16) || !aligned(k_gain, 16) ||
-        !aligned(turns, 8) || ((q_stride | k_stride | v_stride | out_stride) & 3))
+        !aligned(turns, 16) || ((q_stride | k_stride | v_stride | out_stride) & 3))
         return ODB_ERR_ARG;
     if (static_cast<double>(b->max_rows) * (c.n_heads + 2 * c.n_kv_heads) >= 2147483648.0) return ODB_ERR_SHAPE;
     PagedStoreArgs a{};

@@ -7,10 +7,12 @@
 // per position, so that the integer product's upper half is the angle with its whole turns already gone: exact to 2^-32 of
 // a turn at every position (fp32 position x frequency is off by 4e-3 rad at position 131072).
 //
-// HD / 8 threads take a head, each two chunks of four values that hold four whole pairs (values 4 l .. and rot / 2 + 4 l ..,
-// or 8 l .. of interleaved pairs; behind `rot` the next ones), so no value changes threads but for the sum of squares.  A
-// thread takes the same place of HG heads: one set of sines for all of them, and HG pairs of loads in flight.  Bound by
-// HBM: every value read and written once.
+// A unit is a row and up to 8 heads of one kind (q, k or v); HD / 8 threads take it, each the same place of all its heads: two chunks
+// of four values that hold four whole pairs (values 4 l .. and rot / 2 + 4 l .., or 8 l .. of interleaved pairs; behind `rot` the
+// next ones, turned by nothing), so that no value changes threads but for the sum of squares, the sines are computed once and all
+// heads' loads are in flight together.  Arithmetic on pairs of floats (f32x2).
+// Every value is read and written once: HBM is the bound.  With the kinds mixed in a unit of four heads and single floats it was the
+// issue slots: 241 instructions a head and warp, 164 us for 25568 rows of 32 + 2 x 8 heads of 128 (628 MB).
 #include "paged.cuh"
 
 namespace odb {
@@ -18,125 +20,204 @@ namespace odb {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kHeads = 8;                                     // heads of a unit
 
-__device__ __forceinline__ float4 widen(uint2 v) {
-    return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
+typedef unsigned long long f2;                                // two floats
+__device__ __forceinline__ f2 pair(float a, float b) {
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
 }
-__device__ __forceinline__ uint2 narrow(float4 v) {
-    const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
-    return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+__device__ __forceinline__ float2 floats(f2 x) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+    return r;
 }
-__device__ __forceinline__ void turn(float& a, float& b, float c, float s) {
-    const float x = a * c - b * s;
-    b = b * c + a * s;
-    a = x;
+__device__ __forceinline__ f2 mul(f2 a, f2 b) {
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 fma(f2 a, f2 b, f2 c) {
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float low(uint32_t x) { return __uint_as_float(x << 16); }
+__device__ __forceinline__ float high(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
+__device__ __forceinline__ uint32_t bf16x2(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-template <int HD, int HG>
-__global__ void __launch_bounds__(kThreads) paged_store_kernel(const PagedStoreArgs p) {
-    constexpr int kLanes = HD / 8;                            // threads of a head
+// Sine and cosine of two angles of t / 2^32 turns.  The nearest quarter turn is taken off in integers, which leaves |x| <= pi / 4;
+// there the Taylor polynomials up to x^9 and x^8 end within 2e-9 and 3e-8.  (A quarter of the instructions of the library's call,
+// which for eight heads a thread were 40 % of all.)
+__device__ __forceinline__ void sincos_turns(uint32_t t0, uint32_t t1, float (&sn)[2], float (&cs)[2]) {
+    const uint32_t q0 = t0 + 0x20000000u, q1 = t1 + 0x20000000u;   // the quarter in the two highest bits
+    constexpr float kUnit = 1.4629180792671596e-9f;                // 2 pi / 2^32
+    const f2 x = mul(pair(static_cast<float>(static_cast<int>(t0 - (q0 & 0xc0000000u))), static_cast<float>(static_cast<int>(t1 - (q1 & 0xc0000000u)))),
+                     pair(kUnit, kUnit));
+    auto both = [](float v) { return pair(v, v); };
+    const f2 z = mul(x, x);
+    const f2 s = fma(mul(x, z), fma(z, fma(z, fma(z, both(1.f / 362880.f), both(-1.f / 5040.f)), both(1.f / 120.f)), both(-1.f / 6.f)), x);
+    const f2 c = fma(z, fma(z, fma(z, fma(z, both(1.f / 40320.f), both(-1.f / 720.f)), both(1.f / 24.f)), both(-0.5f)), both(1.f));
+    const float2 sf = floats(s), cf = floats(c);
+    auto place = [](uint32_t q, float s0, float c0, float& so, float& co) {   // quarters 0 .. 3: (s, c), (c, -s), (-s, -c), (-c, s)
+        const bool swap = q & 0x40000000u;
+        const float a = swap ? c0 : s0, b = swap ? s0 : c0;
+        so = __uint_as_float(__float_as_uint(a) ^ (q & 0x80000000u));
+        co = __uint_as_float(__float_as_uint(b) ^ ((q + 0x40000000u) & 0x80000000u));
+    };
+    place(q0, sf.x, cf.x, sn[0], cs[0]);
+    place(q1, sf.y, cf.y, sn[1], cs[1]);
+}
+
+// Four pairs (a_j, b_j) of a thread from its two chunks' words, and back.
+template <bool INTER>
+__device__ __forceinline__ void widen(uint2 va, uint2 vb, f2 (&a)[2], f2 (&b)[2]) {
+    if (INTER) {
+        a[0] = pair(low(va.x), low(va.y)); b[0] = pair(high(va.x), high(va.y));
+        a[1] = pair(low(vb.x), low(vb.y)); b[1] = pair(high(vb.x), high(vb.y));
+    } else {
+        a[0] = pair(low(va.x), high(va.x)); a[1] = pair(low(va.y), high(va.y));
+        b[0] = pair(low(vb.x), high(vb.x)); b[1] = pair(low(vb.y), high(vb.y));
+    }
+}
+template <bool INTER>
+__device__ __forceinline__ void narrow(const f2 (&a)[2], const f2 (&b)[2], uint2& va, uint2& vb) {
+    const float2 a0 = floats(a[0]), a1 = floats(a[1]), b0 = floats(b[0]), b1 = floats(b[1]);
+    if (INTER) {
+        va = make_uint2(bf16x2(a0.x, b0.x), bf16x2(a0.y, b0.y));
+        vb = make_uint2(bf16x2(a1.x, b1.x), bf16x2(a1.y, b1.y));
+    } else {
+        va = make_uint2(bf16x2(a0.x, a0.y), bf16x2(a1.x, a1.y));
+        vb = make_uint2(bf16x2(b0.x, b0.y), bf16x2(b1.x, b1.y));
+    }
+}
+
+template <int HD, bool INTER>
+__global__ void __launch_bounds__(kThreads, 2) paged_store_kernel(const PagedStoreArgs p) {
+    constexpr int kLanes = HD / 8;                            // threads of a unit
     pdl_launch_dependents();
     pdl_wait();
-    const int n_heads = p.H + 2 * p.KV, groups = (n_heads + HG - 1) / HG;
+    const int q_units = (p.H + kHeads - 1) / kHeads, k_units = (p.KV + kHeads - 1) / kHeads, units = q_units + 2 * k_units;
     const int l = threadIdx.x % kLanes;
-    // chunk places
-    const int rot_lanes = p.rot / 8;
-    const bool turned = l < rot_lanes;
-    const int ca = turned ? (p.interleaved ? 8 * l : 4 * l) : 8 * l;
-    const int cb = turned ? (p.interleaved ? 8 * l + 4 : p.rot / 2 + 4 * l) : 8 * l + 4;
-
-    const long long units = static_cast<long long>(p.rows) * groups;
     const long long unit = static_cast<long long>(blockIdx.x) * (kThreads / kLanes) + threadIdx.x / kLanes;
-    const unsigned mask = __ballot_sync(0xffffffffu, unit < units);   // a head's lanes are in one warp
-    if (unit >= units) return;
-    const int row = static_cast<int>(unit / groups), grp = static_cast<int>(unit - static_cast<long long>(row) * groups);
+    const unsigned mask = __ballot_sync(0xffffffffu, unit < static_cast<long long>(p.rows) * units);   // a unit's lanes are in one warp
+    if (unit >= static_cast<long long>(p.rows) * units) return;
+    const int row = p.rows * units < 0x7fffffff ? static_cast<int>(static_cast<unsigned>(unit) / static_cast<unsigned>(units)) : static_cast<int>(unit / units);
+    const int part = static_cast<int>(unit - static_cast<long long>(row) * units);
+    const bool is_q = part < q_units, is_v = part >= q_units + k_units;
+    const int h0 = (is_q ? part : is_v ? part - q_units - k_units : part - q_units) * kHeads, n = min(kHeads, (is_q ? p.H : p.KV) - h0);
     const int pos = p.row_pos[row], slot = p.row_slot[row];
+    const int page = slot >> p.page_shift, off = slot & ((1 << p.page_shift) - 1);
+    const bool stored = is_q ? pos >= 0 : slot >= 0 && page < p.n_pages;
+    // from head to head: HD values in q, a page's rows in the pool
+    const size_t step = is_q ? HD : static_cast<size_t>(HD) << p.page_shift;
+    __nv_bfloat16* dst = is_q ? p.q_out + row * p.out_stride + h0 * HD
+                              : (is_v ? p.v_pool : p.k_pool) + (((static_cast<size_t>(page) * p.KV + h0) << p.page_shift) + off) * HD;
 
-    uint2 va[HG], vb[HG];
+    if (is_v) {
+        const __nv_bfloat16* src = p.v + row * p.v_stride + h0 * HD + 4 * l;
+        uint2 v[kHeads][2];
 #pragma unroll
-    for (int i = 0; i < HG; ++i) {
-        const int h = grp + i * groups;
+        for (int i = 0; i < kHeads; ++i)
+            if (i < n) {
+                v[i][0] = *reinterpret_cast<const uint2*>(src + i * HD);
+                v[i][1] = *reinterpret_cast<const uint2*>(src + i * HD + HD / 2);
+            }
+        if (!stored) return;
+#pragma unroll
+        for (int i = 0; i < kHeads; ++i)
+            if (i < n) {
+                *reinterpret_cast<uint2*>(dst + i * step + 4 * l) = v[i][0];
+                *reinterpret_cast<uint2*>(dst + i * step + 4 * l + HD / 2) = v[i][1];
+            }
+        return;
+    }
+    const bool turned = l < p.rot / 8;
+    const int ca = turned && !INTER ? 4 * l : 8 * l, cb = turned && !INTER ? p.rot / 2 + 4 * l : 8 * l + 4;
+    const __nv_bfloat16* src = (is_q ? p.q + row * p.q_stride : p.k + row * p.k_stride) + h0 * HD;
+    uint2 va[kHeads], vb[kHeads];
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i) {
         va[i] = vb[i] = make_uint2(0u, 0u);
-        if (h < n_heads) {
-            const __nv_bfloat16* src = h < p.H ? p.q + row * p.q_stride + h * HD
-                                     : h < p.H + p.KV ? p.k + row * p.k_stride + (h - p.H) * HD
-                                                      : p.v + row * p.v_stride + (h - p.H - p.KV) * HD;
-            va[i] = *reinterpret_cast<const uint2*>(src + ca);
-            vb[i] = *reinterpret_cast<const uint2*>(src + cb);
+        if (i < n) {
+            va[i] = *reinterpret_cast<const uint2*>(src + i * HD + ca);
+            vb[i] = *reinterpret_cast<const uint2*>(src + i * HD + cb);
         }
     }
-    float c[4], s[4];
+    f2 c[2], s[2], ms[2];
+    c[0] = c[1] = pair(1.f, 1.f);
+    s[0] = s[1] = ms[0] = ms[1] = pair(0.f, 0.f);
     if (turned) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const unsigned long long t = p.turns[4 * l + j] * static_cast<unsigned long long>(static_cast<long long>(pos));
-            sincospif(static_cast<float>(static_cast<int>(t >> 32)) * 0x1p-31f, &s[j], &c[j]);
-            s[j] *= p.magnitude;
-            c[j] *= p.magnitude;
+        for (int j = 0; j < 2; ++j) {
+            const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(p.turns + 4 * l + 2 * j);
+            const long long at = pos;
+            float sn[2], cs[2];
+            sincos_turns(static_cast<uint32_t>(f.x * static_cast<unsigned long long>(at) >> 32), static_cast<uint32_t>(f.y * static_cast<unsigned long long>(at) >> 32), sn, cs);
+            c[j] = pair(cs[0] * p.magnitude, cs[1] * p.magnitude);
+            s[j] = pair(sn[0] * p.magnitude, sn[1] * p.magnitude);
+            ms[j] = pair(-sn[0] * p.magnitude, -sn[1] * p.magnitude);
         }
     }
-    const bool row_ok = pos >= 0, slot_ok = slot >= 0 && (slot >> p.page_shift) < p.n_pages;
-    const int page = slot >> p.page_shift, off = slot & ((1 << p.page_shift) - 1);
+    const float* gain = is_q ? p.q_gain : p.k_gain;
+    f2 ga[2], gb[2];
+    if (gain) {
+        const float4 u = *reinterpret_cast<const float4*>(gain + ca), v = *reinterpret_cast<const float4*>(gain + cb);
+        if (INTER) {
+            ga[0] = pair(u.x, u.z); gb[0] = pair(u.y, u.w);
+            ga[1] = pair(v.x, v.z); gb[1] = pair(v.y, v.w);
+        } else {
+            ga[0] = pair(u.x, u.y); ga[1] = pair(u.z, u.w);
+            gb[0] = pair(v.x, v.y); gb[1] = pair(v.z, v.w);
+        }
+    }
 #pragma unroll
-    for (int i = 0; i < HG; ++i) {
-        const int h = grp + i * groups;
-        const bool have = h < n_heads, is_q = h < p.H, is_v = h >= p.H + p.KV;
-        const float* gain = is_q ? p.q_gain : p.k_gain;
-        float4 x = widen(va[i]), y = widen(vb[i]);
-        if (p.q_gain || p.k_gain) {                           // uniform
-            float ss = x.x * x.x + x.y * x.y + x.z * x.z + x.w * x.w + y.x * y.x + y.y * y.y + y.z * y.z + y.w * y.w;
+    for (int i = 0; i < kHeads; ++i) {
+        f2 a[2], b[2];
+        widen<INTER>(va[i], vb[i], a, b);
+        if (gain) {
+            const float2 sq = floats(fma(a[0], a[0], fma(a[1], a[1], fma(b[0], b[0], mul(b[1], b[1])))));
+            float ss = sq.x + sq.y;
 #pragma unroll
             for (int d = kLanes / 2; d >= 1; d >>= 1) ss += __shfl_xor_sync(mask, ss, d);
-            if (have && !is_v && gain) {
-                const float r = 1.0f / sqrtf(ss * (1.0f / HD) + p.eps);
-                const float4 ga = *reinterpret_cast<const float4*>(gain + ca), gb = *reinterpret_cast<const float4*>(gain + cb);
-                x = make_float4(x.x * r * ga.x, x.y * r * ga.y, x.z * r * ga.z, x.w * r * ga.w);
-                y = make_float4(y.x * r * gb.x, y.y * r * gb.y, y.z * r * gb.z, y.w * r * gb.w);
+            const float r = rsqrtf(ss * (1.0f / HD) + p.eps);       // within 2 ulp
+            const f2 rr = pair(r, r);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                a[j] = mul(mul(a[j], rr), ga[j]);
+                b[j] = mul(mul(b[j], rr), gb[j]);
             }
         }
-        if (!have) continue;
-        if (turned && !is_v) {
-            if (p.interleaved) {
-                turn(x.x, x.y, c[0], s[0]);
-                turn(x.z, x.w, c[1], s[1]);
-                turn(y.x, y.y, c[2], s[2]);
-                turn(y.z, y.w, c[3], s[3]);
-            } else {
-                turn(x.x, y.x, c[0], s[0]);
-                turn(x.y, y.y, c[1], s[1]);
-                turn(x.z, y.z, c[2], s[2]);
-                turn(x.w, y.w, c[3], s[3]);
-            }
+        f2 u[2], v[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            u[j] = fma(a[j], c[j], mul(b[j], ms[j]));
+            v[j] = fma(b[j], c[j], mul(a[j], s[j]));
         }
-        __nv_bfloat16* dst;
-        if (is_q) {
-            if (!row_ok) continue;
-            dst = p.q_out + row * p.out_stride + h * HD;
-        } else {
-            if (!slot_ok) continue;
-            const int kh = is_v ? h - p.H - p.KV : h - p.H;
-            dst = (is_v ? p.v_pool : p.k_pool) + (((static_cast<size_t>(page) * p.KV + kh) << p.page_shift) + off) * HD;
-        }
-        if (is_v) {
-            *reinterpret_cast<uint2*>(dst + ca) = va[i];
-            *reinterpret_cast<uint2*>(dst + cb) = vb[i];
-        } else {
-            *reinterpret_cast<uint2*>(dst + ca) = narrow(x);
-            *reinterpret_cast<uint2*>(dst + cb) = narrow(y);
+        if (i < n && stored) {
+            uint2 x, y;
+            narrow<INTER>(u, v, x, y);
+            *reinterpret_cast<uint2*>(dst + i * step + ca) = x;
+            *reinterpret_cast<uint2*>(dst + i * step + cb) = y;
         }
     }
 }
 
-template <int HD, int HG>
+template <int HD, bool INTER>
 cudaError_t launch(const PagedStoreArgs& a, cudaStream_t st) {
-    const long long groups = (a.H + 2 * a.KV + HG - 1) / HG, units = a.rows * groups, per = kThreads / (HD / 8);
-    return launch_kernel(paged_store_kernel<HD, HG>, dim3(static_cast<unsigned>((units + per - 1) / per)), dim3(kThreads), 0, st, a);
+    const long long units = static_cast<long long>(a.rows) * ((a.H + kHeads - 1) / kHeads + 2 * ((a.KV + kHeads - 1) / kHeads)), per = kThreads / (HD / 8);
+    return launch_kernel(paged_store_kernel<HD, INTER>, dim3(static_cast<unsigned>((units + per - 1) / per)), dim3(kThreads), 0, st, a);
 }
 
 }  // namespace
 
 cudaError_t launch_paged_store(const PagedStoreArgs& a, cudaStream_t st) {
-    return a.HD == 128 ? launch<128, 4>(a, st) : launch<64, 4>(a, st);
+    if (a.interleaved) return a.HD == 128 ? launch<128, true>(a, st) : launch<64, true>(a, st);
+    return a.HD == 128 ? launch<128, false>(a, st) : launch<64, false>(a, st);
 }
 
 }  // namespace odb
