@@ -23,9 +23,40 @@ constexpr int kPer = kPagedMaxSeqs / kThreads;   // requests of a thread
 struct Sums {
     int row0[kPagedMaxSeqs + 1], take0[kPagedMaxSeqs + 1], give0[kPagedMaxSeqs + 1];
     int held[kPagedMaxSeqs], need[kPagedMaxSeqs];
-    long long warp_sum[32];
+    long long warp_sum[kThreads / 32][4];
     int bad;
 };
+
+// exclusive sums of four numbers over the block at once; every thread gets the totals
+__device__ __forceinline__ void scan4(long long (&v)[4], long long (*warp_sum)[4], long long (&total)[4]) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    long long x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = v[k];
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const long long y = __shfl_up_sync(0xffffffffu, x[k], d);
+            if (lane >= d) x[k] += y;
+        }
+    if (lane == 31)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) warp_sum[warp][k] = x[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        long long before = 0;
+        total[k] = 0;
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) {
+            const long long t = warp_sum[w][k];
+            if (w < warp) before += t;
+            total[k] += t;
+        }
+        v[k] = before + x[k] - v[k];
+    }
+}
 
 __global__ void __launch_bounds__(kThreads) paged_layout_kernel(const PagedLayoutArgs a) {
     __shared__ Sums sm;
@@ -37,54 +68,56 @@ __global__ void __launch_bounds__(kThreads) paged_layout_kernel(const PagedLayou
 
     const long long P = 1ll << a.page_shift, longest = static_cast<long long>(a.table_stride) << a.page_shift;
     const int per = (a.n_seqs + kThreads - 1) / kThreads, s0 = min(tid * per, a.n_seqs), s1 = min(s0 + per, a.n_seqs);
-    long long rows = 0, take = 0, give = 0, held_all = 0;
+    long long at[4] = {0, 0, 0, 0}, all[4];        // rows, pages taken, pages given, pages held
     bool bad_arg = false;
+    int counts[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        counts[i] = 0;
+        const int s = s0 + i;
+        if (i < per && s < s1) {
+            const long long before = a.len_before[s], after = a.len_after[s], first = a.first[s], count = a.count[s];
+            if (before < 0 || before > longest || after < 0 || after > longest || count < 0 || first < 0 || (count > 0 && first + count > after)) {
+                bad_arg = true;
+            } else {
+                const long long held = (before + P - 1) >> a.page_shift, need = (after + P - 1) >> a.page_shift;
+                sm.held[s] = static_cast<int>(held);
+                sm.need[s] = static_cast<int>(need);
+                counts[i] = static_cast<int>(count);
+                at[0] += count;
+                at[1] += max(0ll, need - held);
+                at[2] += max(0ll, held - need);
+                at[3] += held;
+            }
+        }
+    }
+    if (bad_arg) atomicExch(&sm.bad, ODB_ERR_ARG);
+    scan4(at, sm.warp_sum, all);
+    int bad = sm.bad;
+    if (!bad && (all[3] > a.n_pages || all[3] + all[1] - all[2] > a.n_pages)) bad = ODB_ERR_WORKSPACE;
+    if (!bad && all[0] > a.max_rows) bad = ODB_ERR_SHAPE;
+    if (bad) {
+        if (blockIdx.x == 0 && tid == 0) atomicExch(a.status, bad);
+        all[0] = all[1] = all[2] = 0;
+    }
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int s = s0 + i;
-        if (i >= per || s >= s1) break;
-        const long long before = a.len_before[s], after = a.len_after[s], first = a.first[s], count = a.count[s];
-        if (before < 0 || before > longest || after < 0 || after > longest || count < 0 || first < 0 || (count > 0 && first + count > after)) {
-            bad_arg = true;
-            break;
+        if (i < per && s < s1) {
+            sm.row0[s] = bad ? 0 : static_cast<int>(at[0]);
+            if (!bad) {
+                sm.take0[s] = static_cast<int>(at[1]);
+                sm.give0[s] = static_cast<int>(at[2]);
+                const int held = sm.held[s], need = sm.need[s];
+                at[0] += counts[i];
+                at[1] += max(0, need - held);
+                at[2] += max(0, held - need);
+            }
+            if (blockIdx.x == 0) a.row_start[s] = sm.row0[s];
         }
-        const long long held = (before + P - 1) >> a.page_shift, need = (after + P - 1) >> a.page_shift;
-        sm.held[s] = static_cast<int>(held);
-        sm.need[s] = static_cast<int>(need);
-        rows += count;
-        take += max(0ll, need - held);
-        give += max(0ll, held - need);
-        held_all += held;
     }
-    if (bad_arg) atomicExch(&sm.bad, ODB_ERR_ARG);
-    long long all_rows, all_take, all_give, all_held;
-    long long row0 = paged_block_scan<kThreads>(rows, sm.warp_sum, all_rows);
-    long long take0 = paged_block_scan<kThreads>(take, sm.warp_sum, all_take);
-    long long give0 = paged_block_scan<kThreads>(give, sm.warp_sum, all_give);
-    paged_block_scan<kThreads>(held_all, sm.warp_sum, all_held);
-    int bad = sm.bad;
-    if (!bad && (all_held > a.n_pages || all_held + all_take - all_give > a.n_pages)) bad = ODB_ERR_WORKSPACE;
-    if (!bad && all_rows > a.max_rows) bad = ODB_ERR_SHAPE;
-    if (bad) {
-        if (blockIdx.x == 0 && tid == 0) atomicExch(a.status, bad);
-        all_rows = all_take = all_give = 0;
-    }
-    for (int s = s0; s < s1; ++s) {
-        if (bad) {
-            sm.row0[s] = 0;
-        } else {
-            sm.row0[s] = static_cast<int>(row0);
-            sm.take0[s] = static_cast<int>(take0);
-            sm.give0[s] = static_cast<int>(give0);
-            const int held = sm.held[s], need = sm.need[s];
-            row0 += a.count[s];
-            take0 += max(0, need - held);
-            give0 += max(0, held - need);
-        }
-        if (blockIdx.x == 0) a.row_start[s] = sm.row0[s];
-    }
-    const int n_rows = static_cast<int>(all_rows), T = static_cast<int>(all_take), G = static_cast<int>(all_give);
-    const int n_free = a.n_pages - static_cast<int>(bad ? 0 : all_held);
+    const int n_rows = static_cast<int>(all[0]), T = static_cast<int>(all[1]), G = static_cast<int>(all[2]);
+    const int n_free = a.n_pages - static_cast<int>(bad ? 0 : all[3]);
     if (tid == 0) {
         sm.row0[a.n_seqs] = n_rows;
         sm.take0[a.n_seqs] = T;
@@ -103,6 +136,7 @@ __global__ void __launch_bounds__(kThreads) paged_layout_kernel(const PagedLayou
         return i < n_free ? a.free_pages[i] : given(i - n_free);
     };
     const int step = gridDim.x * kThreads, t0 = blockIdx.x * kThreads + tid;
+#pragma unroll 4
     for (int r = t0; r < a.max_rows; r += step) {
         int seq = -1, pos = -1, slot = -1;
         if (r < n_rows) {

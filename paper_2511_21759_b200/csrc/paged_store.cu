@@ -19,7 +19,7 @@ namespace odb {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 64;
 constexpr int kHeads = 8;                                     // heads of a unit
 
 typedef unsigned long long f2;                                // two floats
@@ -97,7 +97,7 @@ __device__ __forceinline__ void narrow(const f2 (&a)[2], const f2 (&b)[2], uint2
 }
 
 template <int HD, bool INTER>
-__global__ void __launch_bounds__(kThreads, 2) paged_store_kernel(const PagedStoreArgs p) {
+__global__ void __launch_bounds__(kThreads, 14) paged_store_kernel(const PagedStoreArgs p) {
     constexpr int kLanes = HD / 8;                            // threads of a unit
     pdl_launch_dependents();
     pdl_wait();
