@@ -72,6 +72,7 @@ struct PagedAttnArgs {
     unsigned int* arrivals;                               // [kPagedMaxCtas], zero between launches
     float* part_o;                                        // [ctas][2][part_rows][HD]
     float* part_ml;                                       // [ctas][2][part_rows][2]
+    int negate;                                           // many rows: the scale's sign, which scale_log2 no longer has
     int at_once;                                          // CTAs that run at one time
     int part_rows;                                        // rows of a tile
     struct PagedShared* shared;                           // [kPagedMaxCtas], of the last launch that adds up in a kernel of its own

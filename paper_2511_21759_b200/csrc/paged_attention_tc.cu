@@ -24,7 +24,8 @@ namespace {
 
 constexpr int kTQ = 128;   // packed rows of a Q tile (MMA M)
 constexpr int kKT = 64;    // keys of a tile
-template <int QT> constexpr int kThreads = 32 * (5 * QT + 1);   // four softmax warps and an MMA warp a Q tile, a loader
+template <int QT> constexpr int kLoaders = QT;   // one warp for K and V, or one each (the SM has room for a twelfth warp, two CTAs' registers not for two more)
+template <int QT> constexpr int kThreads = 32 * (5 * QT + kLoaders<QT>);   // four softmax warps and an MMA warp a Q tile
 constexpr int kItem = 4;   // key tiles that an item costs beside its own
 template <int HD> constexpr uint32_t kQBytes = kTQ * HD * 2;
 template <int HD> constexpr uint32_t kTileBytes = kKT * HD * 2;
@@ -168,85 +169,109 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
 
     if (tid == 0) a.shared[blockIdx.x].rows = 0;            // thread 0 writes it again where an item begins here and ends elsewhere
 
-    if (any && warp == kSoftmaxWarps + QT) {
-        // ================= loader =================
-        // K of tile i + kFirst, V of tile i by turns, whatever item they belong to; Q of an item while its predecessor's first
-        // tiles are on the way (two buffers), or when its predecessor has ended.
-        PagedWalk<kKT, kItem> wk(a, start), wv(a, start), wq(a, start);
-        // pages of 64 rows and more: a copy a tile; smaller ones: a copy per page and 64 values, in their places of the operand layout
+    if (any && warp >= kSoftmaxWarps + QT) {
+        // ================= loaders =================
+        // K tiles, with Q before its item's first tile or (one Q buffer) where the item in front has ended, and V tiles; each walks
+        // the share by itself.  A single warp takes them by turns, K kFirst tiles ahead.
         const int box_shift = min(a.page_shift, 6), box = 1 << box_shift;
-        PagedPages k_pages, v_pages;
-        bool ok = true, have_k = true, have_q = true;
-        uint32_t nk = 0, nv = 0, nq = 0;                         // loads issued
-        int tk = wk.t0;
+        bool ok = true;
         auto all_wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
-        auto load_tile = [&](const PagedWalk<kKT, kItem>& w, int t, PagedPages& pages, int base, uint8_t* to, uint64_t* bar) {
-            const int k0 = w.k.tile(t) << 6, boxes = max(0, (min(kKT, w.k.hi - k0) + box - 1) >> box_shift);
-            const uint32_t dst = __shfl_sync(0xffffffffu, smem_u32(to), 0);
-            if (paged_elect()) mbar_expect_tx(bar, static_cast<uint32_t>(boxes) * box * HD * 2);
-            __syncwarp();
-            for (int c = 0; c < boxes; ++c) {
-                const int row = pages.row(a, w.seq, w.head, k0 + (c << box_shift), base);
+        struct Tiles {
+            PagedWalk<kKT, kItem> w;
+            PagedPages pages;
+            int t, base, slots;
+            uint32_t slot = 0, ph = 1, issued = 0, at;
+            uint64_t *full, *empty;
+            bool have = true;
+        };
+        Tiles k{PagedWalk<kKT, kItem>(a, start)}, v{PagedWalk<kKT, kItem>(a, start)};
+        k.t = v.t = k.w.t0;
+        k.base = a.k_row0; v.base = a.v_row0;
+        k.slots = KS; v.slots = VS;
+        k.at = __shfl_sync(0xffffffffu, smem_u32(sK), 0); v.at = __shfl_sync(0xffffffffu, smem_u32(sV), 0);
+        k.full = sh->k_full; k.empty = sh->k_empty;
+        v.full = sh->v_full; v.empty = sh->v_empty;
+        // pages of 64 rows and more: a copy a tile; smaller ones: a copy per page and 64 values, in their places of the operand layout
+        auto load = [&](Tiles& x) {
+            if (!ok || !x.have) return;
+            const int k0 = x.w.k.tile(x.t) << 6, keys = min(kKT, x.w.k.hi - k0);
+            const int row = x.pages.row(a, x.w.seq, x.w.head, k0, x.base);
+            if (x.issued >= static_cast<uint32_t>(x.slots)) ok = all_wait(&x.empty[x.slot], x.ph);
+            if (!ok) return;
+            const uint32_t dst = x.at + x.slot * kT;
+            uint64_t* bar = &x.full[x.slot];
+            if (box == kKT) {
                 if (paged_elect()) {
-                    if (box == kKT) {
-                        tma_box_3d(dst, &tm_rows, bar, 0, row, 0);
-                    } else {
-#pragma unroll
-                        for (int at = 0; at < kAtoms; ++at) tma_box_3d(dst + at * kKT * 128 + c * box * 128, &tm_atoms, bar, 0, row, at);
-                    }
+                    mbar_expect_tx(bar, keys > 0 ? kT : 0u);
+                    if (keys > 0) tma_box_3d(dst, &tm_rows, bar, 0, row, 0);
                 }
                 __syncwarp();
+            } else {
+                const int boxes = max(0, (keys + box - 1) >> box_shift);
+                if (paged_elect()) mbar_expect_tx(bar, static_cast<uint32_t>(boxes) * box * HD * 2);
+                __syncwarp();
+                for (int c = 0; c < boxes; ++c) {
+                    const int row_c = x.pages.row(a, x.w.seq, x.w.head, k0 + (c << box_shift), x.base);
+                    if (paged_elect()) {
+#pragma unroll
+                        for (int at = 0; at < kAtoms; ++at) tma_box_3d(dst + at * kKT * 128 + c * box * 128, &tm_atoms, bar, 0, row_c, at);
+                    }
+                    __syncwarp();
+                }
+            }
+            ++x.issued;
+            if (++x.slot == static_cast<uint32_t>(x.slots)) { x.slot = 0; x.ph ^= 1u; }
+            if (++x.t == x.w.t1) {
+                x.have = x.w.next();
+                x.t = x.w.t0;
             }
         };
-        auto load_k = [&]() {
-            if (!ok || !have_k) return;
-            const uint32_t slot = nk % KS;
-            if (nk >= KS) ok = all_wait(&sh->k_empty[slot], (nk / KS - 1) & 1u);
-            if (!ok) return;
-            load_tile(wk, tk, k_pages, a.k_row0, sK + slot * kT, &sh->k_full[slot]);
-            ++nk;
-            if (++tk == wk.t1) {
-                have_k = wk.next();
-                tk = wk.t0;
-            }
-        };
-        auto load_v = [&](int t) {
-            const uint32_t slot = nv % VS;
-            if (nv >= VS) ok = ok && all_wait(&sh->v_empty[slot], (nv / VS - 1) & 1u);
-            if (!ok) return;
-            load_tile(wv, t, v_pages, a.v_row0, sV + slot * kT, &sh->v_full[slot]);
-            ++nv;
-        };
-        auto load_q = [&]() {
-            if (!ok || !have_q) return;
+        uint32_t nq = 0;
+        auto load_q = [&](const PagedWalk<kKT, kItem>& w) {
             const uint32_t buf = nq % NQ;
-            if (nq >= NQ) ok = all_wait(&sh->item_done[buf], (nq / NQ - 1) & 1u);
+            if (nq >= NQ) ok = ok && all_wait(&sh->item_done[buf], (nq / NQ - 1) & 1u);
             if (!ok) return;
-            if (paged_elect()) mbar_expect_tx(&sh->q_full[buf], QT * kAtoms * static_cast<uint32_t>(a.tile_tokens) * a.G * 128);
-            __syncwarp();
+            const uint32_t dst = __shfl_sync(0xffffffffu, smem_u32(sQ) + buf * QT * kQBytes<HD>, 0);
+            const int row = w.q.row0 + w.rt * QT * a.tile_tokens;
             if (paged_elect()) {
+                mbar_expect_tx(&sh->q_full[buf], QT * kAtoms * static_cast<uint32_t>(a.tile_tokens) * a.G * 128);
 #pragma unroll
                 for (int g = 0; g < QT; ++g)
 #pragma unroll
                     for (int at = 0; at < kAtoms; ++at)
-                        tma_box_3d(smem_u32(sQ) + (buf * QT + g) * kQBytes<HD> + at * kTQ * 128, &tm_q, &sh->q_full[buf], 64 * at, wq.head * a.G,
-                                   wq.q.row0 + (wq.rt * QT + g) * a.tile_tokens);
+                        tma_box_3d(dst + g * kQBytes<HD> + at * kTQ * 128, &tm_q, &sh->q_full[buf], 64 * at, w.head * a.G, row + g * a.tile_tokens);
             }
             __syncwarp();
             ++nq;
-            have_q = wq.next();
         };
-        for (int i = 0; i < kFirst; ++i) load_k();
-        if (NQ == 2) load_q();
-        do {
-            if (NQ == 1) load_q();
-            for (int t = wv.t0; t < wv.t1 && ok; ++t) {
-                load_k();
-                load_v(t);
+        if (kLoaders<QT> == 2) {
+            static_assert(kLoaders<QT> == 1 || NQ == 2, "K waits for its item's Q buffer, V does not");
+            if (warp == kSoftmaxWarps + QT)
+                while (ok && k.have) {
+                    if (k.t == k.w.t0) load_q(k.w);
+                    load(k);
+                }
+            else
+                while (ok && v.have) load(v);
+        } else {
+            PagedWalk<kKT, kItem> wq(a, start);
+            bool have_q = true;
+            auto next_q = [&]() {
+                if (!have_q) return;
+                load_q(wq);
+                have_q = wq.next();
+            };
+            for (int i = 0; i < kFirst; ++i) load(k);
+            if (NQ == 2) next_q();
+            while (ok && v.have) {
+                if (NQ == 1 && v.t == v.w.t0) next_q();
                 // behind the item's third tile: the epilogue in front of it, which frees the buffer, is on its way by then
-                if (NQ == 2 && t == min(wv.t0 + 2, wv.t1 - 1)) load_q();
+                const bool then_q = NQ == 2 && v.t == min(v.w.t0 + 2, v.w.t1 - 1);
+                load(k);
+                load(v);
+                if (then_q) next_q();
             }
-        } while (ok && wv.next());
+        }
         if (*cta_abort && lane == 0) {   // copies in flight land before the CTA's shared memory goes away
             const long long t0 = clock64();
             auto land = [&](uint64_t* bars, uint32_t n, uint32_t slots) {
@@ -255,8 +280,8 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                     }
             };
             land(sh->q_full, nq, NQ);
-            land(sh->k_full, nk, KS);
-            land(sh->v_full, nv, VS);
+            land(sh->k_full, k.issued, KS);
+            land(sh->v_full, v.issued, VS);
         }
     } else if (any && warp >= kSoftmaxWarps) {
         // ================= MMA issuer of Q tile g: the whole warp walks and waits, one lane issues =================
@@ -264,7 +289,8 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
         // the softmax warps have written the one in front of it.  (P of an item's first tile says that O has been read.)
         PagedWalk<kKT, kItem> ws(a, start), wv(a, start);
         const int g = warp - kSoftmaxWarps;
-        constexpr uint32_t idesc_s = instr_desc(kTQ, kKT, 0), idesc_o = instr_desc(kTQ, HD, 1);
+        const uint32_t idesc_s = instr_desc(kTQ, kKT, 0) | (a.negate ? 1u << 13 : 0u);   // bit 13: the product's A is taken with its sign turned
+        constexpr uint32_t idesc_o = instr_desc(kTQ, HD, 1);
         const uint32_t cols = tmem + g * kCols;
         const uint64_t q_desc = desc_k_major(smem_u32(sQ) + g * kQBytes<HD>), k_desc = desc_k_major(smem_u32(sK)),
                        v_desc = desc_mn_major(smem_u32(sV), kKT * 128);
@@ -376,13 +402,6 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                 }
                 float m0 = fmaxf(max3(mx[0], mx[1], __uint_as_float(sv[15])), max3(mx[2], mx[3], __uint_as_float(sv[31])));
                 m0 = max3(m0, __uint_as_float(sv[47]), __uint_as_float(sv[63]));
-                if (a.scale_log2 < 0.f) {                                // a negative scale turns the order around
-                    m0 = INFINITY;
-#pragma unroll
-                    for (int j = 0; j < 64; ++j)
-                        if ((mask >> j) & 1ull) m0 = fminf(m0, __uint_as_float(sv[j]));
-                        else sv[j] = 0x7f800000u;                        // times the scale: minus infinity
-                }
                 float factor = 1.0f;                                     // what O and the row sum so far are multiplied by
                 const float mt_log2 = mine && mask ? m0 * a.scale_log2 : -INFINITY;   // rows that are none turn nothing for the warp's others
                 // The exponentials take a score's exact product with the scale, the shift comes from the rounded one: from 2^22 on
@@ -607,6 +626,8 @@ cudaError_t launch(const PagedAttnArgs& a, const CUtensorMap& tm_q, const PagedM
 }  // namespace
 
 cudaError_t launch_paged_attention_tc(PagedAttnArgs a, const PagedMaps& maps, int hd, int q_tiles, int sms, cudaStream_t st) {
+    a.negate = a.scale_log2 < 0.f;                           // the softmax below takes the largest score for the largest exponent
+    a.scale_log2 = fabsf(a.scale_log2);
     a.tile_tokens = kTQ / a.G;
     a.tile_rows = q_tiles * a.tile_tokens * a.G;
     a.by_rows = PagedDiv::by(a.tile_rows);

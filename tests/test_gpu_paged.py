@@ -279,6 +279,22 @@ def _check(out, lse, qf, keys, values, start, firsts, D, scale=None, **mask):
             assert (err <= (d[..., 0] + 2.0 ** -21 * (1 + np.abs(wl)))[~gone]).all(), (s, err.max())
 
 
+def _check_scaled(out, lse, qf, keys, values, start, firsts, D, scale, **mask):
+    """As _check where the scores' own error d is not small: the weights are off by up to e^(2 d) - 1 each, the output at most by
+    the largest value; log-sum-exp in relative terms of the scores it comes from."""
+    out, lse = out.float().cpu().numpy(), lse.cpu().numpy()
+    for s in range(len(keys)):
+        rows = slice(start[s], start[s + 1])
+        pos = firsts[s] + np.arange(start[s + 1] - start[s])
+        want, wl, mag, size = O.attention(qf[rows], keys[s], values[s], pos, scale, **mask)
+        d = D * 2.0 ** -24 * size + 2.0 ** -23 * size              # the sum of products, and its own rounding after the scale
+        grow = np.minimum(np.expm1(np.minimum(2 * d, 50.0)), 1e6)[..., None]
+        top = max(np.abs(v).max() for v in values)
+        tol = U * np.abs(want) + np.minimum((U + grow + 2.0 ** -20) * mag * 1.01, 2.02 * top)
+        assert (np.abs(out[rows] - want) <= tol).all(), (s, np.abs(out[rows] - want).max())
+        assert (np.abs(lse[rows] - wl) <= d + 2.0 ** -21 * (1 + np.abs(wl))).all(), (s, np.abs(lse[rows] - wl).max())
+
+
 ATT = [  # lens, rows (0: all), H, KV, D, page, mask
     ([1], 1, 1, 1, 64, 16, {}),
     ([577], 1, 32, 8, 128, 16, {}),
@@ -424,15 +440,19 @@ def test_attention_infinities_and_nan_reach_only_the_rows_that_see_them(new, G, 
 
 
 @requires_gpu
-def test_attention_of_large_scores_and_another_scale():
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("new", [3, 45, 90])
+def test_attention_of_large_scores_and_another_scale(new, D):
     rng = np.random.default_rng(21)
-    lens, counts, firsts = [333, 64], [3, 3], [330, 61]
-    cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, 4, 2, 128, 16, scale=30.0)
-    for scale in (0.0, 0.25, 1e-4, -0.05):
-        lse = torch.empty(6, 4, device="cuda")
-        out = cache.attention(0, b, q, lse=lse, scale=scale)
-        _check(out, lse, qf, keys, values, start, firsts, 128, scale or None)
-    cache.close()
+    lens, counts = [333, 94], [new, new]
+    firsts = [n - c for n, c in zip(lens, counts)]
+    for scale in (0.0, 0.25, 1e-4, -0.05, 3e4):
+        for size in (1.0, 30.0):
+            cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, 4, 2, D, 16, scale=size)
+            lse = torch.empty(2 * new, 4, device="cuda")
+            out = cache.attention(0, b, q, lse=lse, scale=scale, right=0)
+            _check_scaled(out, lse, qf, keys, values, start, firsts, D, scale or None, right=0)
+            cache.close()
 
 
 @requires_gpu
