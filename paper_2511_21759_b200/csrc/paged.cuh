@@ -76,7 +76,7 @@ struct PagedAttnArgs {
     int at_once;                                          // CTAs that run at one time
     int part_rows;                                        // rows of a tile
     struct PagedShared* shared;                           // [kPagedMaxCtas], of the last launch that adds up in a kernel of its own
-    PagedDiv by_group, by_rows;                           // divisions by G and by the packed rows of an item
+    PagedDiv by_group, by_rows, by_once;                  // divisions by G, by the packed rows of an item, by at_once
     int tile_rows, tile_tokens;                           // many rows: packed rows of an item, query rows of a Q tile
 };
 // the pool's two maps: boxes of whole rows, and of 64 values of a row
@@ -145,14 +145,14 @@ __device__ __forceinline__ PagedKeys paged_keys(const PagedAttnArgs& a, const Pa
 constexpr int kPagedWaves = 4;
 struct PagedShares {
     int size[kPagedWaves], at_once;
-    __device__ __forceinline__ void divide(int total, int waves, int min_units, int full_units) {
+    __device__ __forceinline__ void divide(int total, int waves, int min_units, int full_units, const PagedDiv& by_once) {
         // 45, 27, 17 and 11 of a hundred: see the launcher of the few rows' kernel
         constexpr int kPart[kPagedWaves] = {115, 69, 44, 28};
-        const int most = static_cast<int>((static_cast<unsigned>(total) + at_once - 1) / at_once), least = max(min_units, min(full_units, most));
+        const int most = by_once(total + at_once - 1), least = max(min_units, min(full_units, most));
         int left = total;
 #pragma unroll
         for (int w = 0; w < kPagedWaves; ++w) {
-            const int all = static_cast<int>((static_cast<unsigned>(max(left, 0)) + at_once - 1) / at_once);
+            const int all = by_once(left + at_once - 1);
             const int part = w + 1 < waves ? static_cast<int>(static_cast<unsigned>(most) * kPart[w] / 256) + 1 : all;
             size[w] = max(min(part, all), least);
             left -= min(left, size[w] * at_once);
@@ -232,11 +232,11 @@ __device__ __forceinline__ int paged_upper(const int* v, int n, int x) {   // th
 }
 
 // Called by all THREADS threads of the block; false: there is nothing for this CTA to do.
-// waves: CTAs of the grid for each of the `at_once` that run at one time.  min_units: what a CTA takes at least (more than E);
-// full_units: what it takes at least as long as `at_once` CTAs have work.
+// waves: CTAs of the grid for each of the a.at_once that run at one time.  min_units: what a CTA takes at least (more than E);
+// full_units: what it takes at least as long as those have work.
 // The launcher's bounds on rows, requests and keys keep every sum below 2^31.
 template <int THREADS, int KT, int E>
-__device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int waves, int min_units, int full_units, int at_once, PagedStart& st) {
+__device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int waves, int min_units, int full_units, PagedStart& st) {
     const int tid = threadIdx.x;
     auto kept = [&](int s) {          // the request's numbers, loaded once
         const int4 v = sc.seq[s];
@@ -246,8 +246,8 @@ __device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int w
     };
     auto share = [&](int per_head, int& rem) {   // this CTA's part of the line, and its place within a head's
         const int total = per_head * a.KV;
-        st.shares.at_once = at_once;
-        st.shares.divide(total, waves, min_units, full_units);
+        st.shares.at_once = a.at_once;
+        st.shares.divide(total, waves, min_units, full_units, a.by_once);
         const long long u0 = st.shares.begin(blockIdx.x), u1 = st.shares.begin(blockIdx.x + 1);
         if (u0 >= total) return false;
         st.u0 = static_cast<int>(u0);
@@ -486,7 +486,7 @@ struct PagedSum {
     }
     __device__ __forceinline__ void parts(const PagedAttnArgs& a, int c0, int from, int to, int r0, int step, int rows) {   // CTAs [from, to)
         const int lane = threadIdx.x & 31;
-        constexpr int CU = 16 / RB;                  // parts in flight
+        constexpr int CU = 8 / RB;                   // parts in flight
         for (int c = from; c < to; c += CU) {
             float2 ml[CU][RB];
             float x[CU][RB][V];

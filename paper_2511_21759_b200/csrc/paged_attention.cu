@@ -22,8 +22,8 @@ namespace odb {
 namespace {
 
 constexpr int kKT = 64;                    // keys per tile
-constexpr int kItem = 2;                    // key tiles that an item costs beside its own
-constexpr int kMinUnits = 4, kFullUnits = 24;   // units of a CTA, at least; where all places on the SMs have work
+constexpr int kItem = 1;                    // key tiles that an item costs beside its own
+constexpr int kMinUnits = 2, kFullUnits = 24;   // units of a CTA, at least; where all places on the SMs have work
 constexpr int kMmaWarps = 4;
 constexpr int kThreads = 32 * (kMmaWarps + 1);
 template <int HD> constexpr int kKSlots = HD == 128 ? 3 : 7;                // K tiles on the way or in use
@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
     // the ring's memory holds the sums until the start is found
     static_assert(sizeof(PagedScratch) <= kSmem<64> - 1024, "the scratch fits the rings");
     PagedStart start;
-    const bool any = paged_find_start<kThreads, kKT, kItem>(a, *reinterpret_cast<PagedScratch*>(smem), kPagedWaves, kMinUnits, kFullUnits, a.at_once, start);
+    const bool any = paged_find_start<kThreads, kKT, kItem>(a, *reinterpret_cast<PagedScratch*>(smem), kPagedWaves, kMinUnits, kFullUnits, start);
     if (!any) return;                                           // block-uniform
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the scratch's writes before the copies that take its place
     __syncthreads();
@@ -501,6 +501,7 @@ cudaError_t launch_few(PagedAttnArgs a, const CUtensorMap& tmap, int sms, cudaSt
     a.by_rows = PagedDiv::by(ROWS);
     a.part_rows = ROWS;
     a.at_once = 2 * sms;
+    a.by_once = PagedDiv::by(a.at_once);
     // Under a full memory system some SMs run a third slower than others, and so does the second CTA of an SM: of one share for each
     // place the last ended a third behind the mean.  So four waves of CTAs, taken by whichever place is free, of shares that grow
     // smaller to the end.  No more CTAs than the table's width leaves work for.

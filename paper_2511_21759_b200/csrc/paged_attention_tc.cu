@@ -77,6 +77,77 @@ __device__ __forceinline__ void tma_box_3d(uint32_t dst, const CUtensorMap* tmap
         "l"(reinterpret_cast<uint64_t>(tmap)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
         : "memory");
 }
+// The products with descriptors as their low words (address, and what stands below bit 32) and the high word that all tiles here
+// share: one 32-bit addition from product to product.
+__device__ __forceinline__ void umma_lo(uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+        "mov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n\t}" ::"r"(tmem_d),
+        "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void umma_ts_lo(uint32_t tmem_d, uint32_t tmem_a, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\t"
+        "mov.b64 b, {%2, %3};\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}" ::"r"(tmem_d),
+        "r"(tmem_a), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void commit_at(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// whether the phase has completed for all lanes of a converged warp
+__device__ __forceinline__ bool try_all(uint32_t bar, uint32_t parity) {
+    uint32_t x;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "vote.sync.all.pred p, p, 0xffffffff;\n\t"
+        "selp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(x)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return x != 0;
+}
+
+// 64 TMEM columns asked for, and (with whatever else was asked for) there
+__device__ __forceinline__ void tmem_ask64(uint32_t taddr, uint32_t (&v)[64]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+        "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+        "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
+          "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
+          "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31]), "=r"(v[32]),
+          "=r"(v[33]), "=r"(v[34]), "=r"(v[35]), "=r"(v[36]), "=r"(v[37]), "=r"(v[38]), "=r"(v[39]), "=r"(v[40]),
+          "=r"(v[41]), "=r"(v[42]), "=r"(v[43]), "=r"(v[44]), "=r"(v[45]), "=r"(v[46]), "=r"(v[47]), "=r"(v[48]),
+          "=r"(v[49]), "=r"(v[50]), "=r"(v[51]), "=r"(v[52]), "=r"(v[53]), "=r"(v[54]), "=r"(v[55]), "=r"(v[56]),
+          "=r"(v[57]), "=r"(v[58]), "=r"(v[59]), "=r"(v[60]), "=r"(v[61]), "=r"(v[62]), "=r"(v[63])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_got64(uint32_t (&v)[64]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int j = 0; j < 64; ++j) asm volatile("" : "+r"(v[j]));       // no use of them moves in front of the wait
+}
+__device__ __forceinline__ void tmem_ld16_now(uint32_t taddr, uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(taddr)
+        : "memory");
+}
 // one TMEM column of a warp's lanes
 __device__ __forceinline__ uint32_t tmem_ld1(uint32_t taddr) {
     uint32_t v;
@@ -159,7 +230,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
 
     PagedStart start;
     static_assert(sizeof(PagedScratch) <= kSmem<64, 1> - 512, "the scratch fits the tiles");
-    const bool any = paged_find_start<kThreads<QT>, kKT, kItem>(a, *reinterpret_cast<PagedScratch*>(sQ), 1, kItem + 2, 0, gridDim.x, start);
+    const bool any = paged_find_start<kThreads<QT>, kKT, kItem>(a, *reinterpret_cast<PagedScratch*>(sQ), 1, kItem + 2, 0, start);
     proxy_fence();                                          // the scratch's writes before the copies that take its place
     __syncthreads();
 
@@ -292,62 +363,78 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
         const uint32_t idesc_s = instr_desc(kTQ, kKT, 0) | (a.negate ? 1u << 13 : 0u);   // bit 13: the product's A is taken with its sign turned
         constexpr uint32_t idesc_o = instr_desc(kTQ, HD, 1);
         const uint32_t cols = tmem + g * kCols;
-        const uint64_t q_desc = desc_k_major(smem_u32(sQ) + g * kQBytes<HD>), k_desc = desc_k_major(smem_u32(sK)),
-                       v_desc = desc_mn_major(smem_u32(sV), kKT * 128);
+        const uint32_t q_lo = static_cast<uint32_t>(desc_k_major(smem_u32(sQ) + g * kQBytes<HD>)), k_lo = static_cast<uint32_t>(desc_k_major(smem_u32(sK))),
+                       v_lo = static_cast<uint32_t>(desc_mn_major(smem_u32(sV), kKT * 128));
+        const uint32_t hi = static_cast<uint32_t>(desc_k_major(0) >> 32);    // desc_mn_major's too
+        const uint32_t bars = smem_u32(sh);
+        auto bar_of = [&](const uint64_t* first, uint32_t i) { return bars + static_cast<uint32_t>(reinterpret_cast<const char*>(first) - reinterpret_cast<const char*>(sh)) + i * 8; };
+        // Places and phases are counted along: what a tile takes here is what bounds the whole where products and exponentials overlap.
         bool ok = true, have_s = true;
-        uint32_t ns = 0, nv = 0, is = 0, iv = 0;                 // S and P V issued, the items of the next ones
+        int s_ahead = 0, i_ahead = 0;                            // S issued beyond P V, items beyond P V's that the next S is
         int ts = ws.t0;
-        auto uniform = [](uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); };
-        auto all_wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
-        auto issue_s = [&]() {
-            const uint32_t b = uniform(ns % kB), slot = uniform(ns % KS), buf = uniform(is % NQ);
-            if (ts == ws.t0) ok = all_wait(&sh->q_full[buf], (is / NQ) & 1u);
-            if (ok) ok = all_wait(&sh->k_full[slot], (ns / KS) & 1u);
-            // P in this buffer, of tile ns - kB <= nv - 1, has been multiplied
-            if (ok && nv > 0) ok = all_wait(&sh->pv_done[g][(nv - 1) & 1u], ((nv - 1) >> 1) & 1u);
+        uint32_t k_slot = 0, k_ph = 0, s_buf = 0, q_buf = 0, q_ph = 0;
+        uint32_t v_slot = 0, v_ph = 0, p_buf = 0, p_ph = 0;
+        uint32_t pv_bar = 1, pv_ph = 1;                          // of the last P V: barrier and phase
+        auto all_wait = [&](uint64_t* first, uint32_t i, uint32_t parity) {
+            if (!try_all(bar_of(first, i), parity)) ok = __all_sync(0xffffffffu, wait(first + i, parity));
+        };
+        auto issue_s = [&](bool first_pv) {
+            const uint32_t q = q_lo + q_buf * (QT * kQBytes<HD> >> 4), k = k_lo + k_slot * (kT >> 4), d = cols + s_buf * kKT;
+            const uint32_t full = bar_of(sh->s_full[g], s_buf), empty = bar_of(sh->k_empty, k_slot);
+            if (ts == ws.t0) all_wait(sh->q_full, q_buf, q_ph);
+            if (ok) all_wait(sh->k_full, k_slot, k_ph);
+            // the last P V has been done, and with it the one that read P in this S's place
+            if (ok && !first_pv) all_wait(sh->pv_done[g], pv_bar, pv_ph);
             if (!ok) return;
             tc_fence_after();
-            const uint64_t q = q_desc + buf * (QT * kQBytes<HD> >> 4), k = k_desc + slot * (kT >> 4);
             if (paged_elect()) {
 #pragma unroll
                 for (int kk = 0; kk < HD / 16; ++kk) {
                     const uint32_t atom = kk >> 2, within = (kk & 3) * 32;
-                    umma(cols + b * kKT, q + ((atom * (kTQ * 128) + within) >> 4), k + ((atom * (kKT * 128) + within) >> 4), idesc_s, kk > 0 ? 1u : 0u);
+                    umma_lo(d, q + ((atom * (kTQ * 128) + within) >> 4), k + ((atom * (kKT * 128) + within) >> 4), hi, idesc_s, kk > 0 ? 1u : 0u);
                 }
-                umma_commit(&sh->s_full[g][b]);
-                umma_commit(&sh->k_empty[slot]);
+                commit_at(full);
+                commit_at(empty);
             }
             __syncwarp();
-            ++ns;
+            ++s_ahead;
+            if (++k_slot == KS) { k_slot = 0; k_ph ^= 1u; }
+            if (++s_buf == kB) s_buf = 0;
             if (++ts == ws.t1) {
                 have_s = ws.next();
                 ts = ws.t0;
-                ++is;
+                ++i_ahead;
+                if (++q_buf == NQ) { q_buf = 0; q_ph ^= 1u; }
             }
         };
+        bool first_pv = true;
         do {
             const int n = wv.t1 - wv.t0;
             for (int t = 0; t < n && ok; ++t) {
-                while (ok && have_s && ns <= nv + kFirst && is < iv + NQ) issue_s();
-                const uint32_t b = uniform(nv % kB), slot = uniform(nv % VS), last = t + 1 == n;
-                if (ok) ok = all_wait(&sh->v_full[slot], (nv / VS) & 1u);
-                if (ok) ok = all_wait(&sh->p_full[g][b], (nv / kB) & 1u);
+                while (ok && have_s && s_ahead <= kFirst && i_ahead < NQ) issue_s(first_pv);
+                const uint32_t v = v_lo + v_slot * (kT >> 4), o = tmem_o(g), pa = cols + p_buf * kKT;
+                pv_bar ^= 1u;
+                if (pv_bar == 0) pv_ph ^= 1u;
+                const uint32_t done_bar = bar_of(sh->pv_done[g], pv_bar), empty = bar_of(sh->v_empty, v_slot), o_bar = bar_of(sh->o_full, g);
+                if (ok) all_wait(sh->v_full, v_slot, v_ph);
+                if (ok) all_wait(sh->p_full[g], p_buf, p_ph);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t keep = uniform(t > 0 || *const_cast<volatile int*>(&sh->keep_o[g]) ? 1u : 0u);
-                const uint64_t v = v_desc + slot * (kT >> 4);
+                const uint32_t keep = t > 0 ? 1u : __shfl_sync(0xffffffffu, *const_cast<volatile int*>(&sh->keep_o[g]), 0);
                 if (paged_elect()) {
 #pragma unroll
-                    for (int kk = 0; kk < kKT / 16; ++kk)
-                        umma_ts(tmem_o(g), cols + b * kKT + kk * 8, v + kk * (2048 >> 4), idesc_o, kk > 0 ? 1u : keep);
-                    umma_commit(&sh->pv_done[g][nv & 1u]);
-                    umma_commit(&sh->v_empty[slot]);
-                    if (last) umma_commit(&sh->o_full[g]);
+                    for (int kk = 0; kk < kKT / 16; ++kk) umma_ts_lo(o, pa + kk * 8, v + kk * (2048 >> 4), hi, idesc_o, kk > 0 ? 1u : keep);
+                    commit_at(done_bar);
+                    commit_at(empty);
+                    if (t + 1 == n) commit_at(o_bar);
                 }
                 __syncwarp();
-                ++nv;
+                first_pv = false;
+                --s_ahead;
+                if (++v_slot == VS) { v_slot = 0; v_ph ^= 1u; }
+                if (++p_buf == kB) { p_buf = 0; p_ph ^= 1u; }
             }
-            ++iv;
+            --i_ahead;
         } while (ok && wv.next());
     } else if (any) {
         // ================= softmax: thread r of Q tile g = packed row r = TMEM lane r =================
@@ -373,19 +460,20 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
             const int left = min(rows_g, (w.q.n - tok0) * a.G);          // rows of the Q tile (may be negative); others hold anything
             const bool mine = r < left;
             float M_row = -INFINITY, l_row = 0.f;
-            for (int t = 0; t < n; ++t) {
+            uint32_t sv[64];                                             // the row's scores of the tile at hand
+            auto ask = [&](int t) {                                      // for those of tile t, once they are there
+                const uint32_t gt = done + t, b = gt % kB;
+                if (!try_all(smem_u32(&sh->s_full[g][b]), (gt / kB) & 1u)) ok = __all_sync(0xffffffffu, wait(&sh->s_full[g][b], (gt / kB) & 1u)) && ok;
+                tc_fence_after();
+                tmem_ask64(s_base + b * kKT, sv);
+            };
+            // One tile.  care: some row of the item does not see all of its keys.
+            auto tile = [&](bool care, int t, int k0) {
                 const uint32_t gt = done + t, b = gt % kB;
                 const uint32_t ts = s_base + b * kKT;
-                const int k0 = w.k.tile(w.t0 + t) << 6;
-                // seen by every row of the Q tile, of all Q tiles of the item (others have rows of V that need care)
-                const bool whole = k0 + kKT <= all_hi && (k0 >= all_lo || k0 + kKT <= a.sinks);
-                const bool whole_item = QT == 1 ? whole : k0 + kKT <= item_hi && (k0 >= item_lo || k0 + kKT <= a.sinks);
-                ok = __all_sync(0xffffffffu, wait(&sh->s_full[g][b], (gt / kB) & 1u));
-                tc_fence_after();
-                uint32_t sv[64];                                         // the row's scores
-                tmem_ld64(ts, sv);
+                tmem_got64(sv);
                 unsigned long long mask = ~0ull;                         // the keys of the tile that the row sees
-                if (!whole) {
+                if (care && !(k0 + kKT <= all_hi && (k0 >= all_lo || k0 + kKT <= a.sinks))) {
                     auto below = [](long long x) { return x >= 64 ? ~0ull : x <= 0 ? 0ull : (1ull << x) - 1ull; };
                     mask = below(min(static_cast<long long>(w.q.len), static_cast<long long>(pos) + a.right + 1) - k0) &
                            (~below(static_cast<long long>(pos) - a.left - k0) | below(static_cast<long long>(a.sinks) - k0));
@@ -402,13 +490,13 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                 }
                 float m0 = fmaxf(max3(mx[0], mx[1], __uint_as_float(sv[15])), max3(mx[2], mx[3], __uint_as_float(sv[31])));
                 m0 = max3(m0, __uint_as_float(sv[47]), __uint_as_float(sv[63]));
-                float factor = 1.0f;                                     // what O and the row sum so far are multiplied by
                 const float mt_log2 = mine && mask ? m0 * a.scale_log2 : -INFINITY;   // rows that are none turn nothing for the warp's others
                 // The exponentials take a score's exact product with the scale, the shift comes from the rounded one: from 2^22 on
                 // they lie up to 0.25 and more apart, and the scores are rounded first.
                 const bool far = fabsf(mt_log2) >= 0x1p22f && mt_log2 != -INFINITY;
-                bool rescale = false;
                 uint64_t mult2 = scale2;
+                float factor = 1.0f;                                     // what O and the row sum so far are multiplied by
+                bool rescale = false;
                 if (__any_sync(0xffffffffu, mt_log2 > M_row + kSlack || far)) {
                     if (mt_log2 > M_row + kSlack) {                      // also the first visible key (M_row = -inf)
                         const float M_new = ceilf(mt_log2);
@@ -421,10 +509,25 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                         for (int j = 0; j < 64; ++j) sv[j] = __float_as_uint(__uint_as_float(sv[j]) * a.scale_log2);
                         mult2 = pack2f(1.0f, 1.0f);
                     }
+                    if (rescale && t > 0) {                              // warp-uniform; rows that keep their shift multiply by 1
+                        // P V(t - 1) has been added to O.  The parity is not ambiguous: S(t) was issued behind P V(t - kB), so P V(t - 3),
+                        // which the same barrier counts, has completed; P V(t + 1) cannot have, it is behind this P.
+                        ok = __all_sync(0xffffffffu, wait(&sh->pv_done[g][(gt - 1) & 1u], ((gt - 1) >> 1) & 1u)) && ok;
+                        tc_fence_after();
+                        l_row *= factor;
+#pragma unroll 1
+                        for (int c = 0; c < HD / 16; ++c) {
+                            uint32_t v[16];
+                            tmem_ld16_now(o_base + c * 16, v);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * factor);
+                            tmem_st16(o_base + c * 16, v);
+                        }
+                    }
                 }
                 const float m_log2 = M_row == -INFINITY ? 0.f : M_row;   // a row that has seen no key: every P is 0
                 const uint64_t shift2 = pack2f(-m_log2, -m_log2);
-                uint64_t sum[2] = {0ull, 0ull};
+                uint64_t sum[4] = {0ull, 0ull, 0ull, 0ull};
                 // The two softmax warps of a scheduler take turns at the exponentials: left alone they fall into step, share the
                 // special-function unit for twice as long and leave it idle together for the rest of the tile.
                 if (QT == 2) turn_begin(g, gw);
@@ -435,21 +538,21 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                     for (int u = 0; u < 16; ++u) {
                         const float2 x = unpack2f(fma2(pack2u(sv[32 * half + 2 * u], sv[32 * half + 2 * u + 1]), mult2, shift2));
                         const float p0 = ex2_approx(x.x), p1 = ex2_approx(x.y);
-                        sum[u & 1] = add2(sum[u & 1], pack2f(p0, p1));
+                        sum[u & 3] = add2(sum[u & 3], pack2f(p0, p1));
                         pb[u] = paged_bf16x2(p0, p1);
                     }
                     tmem_st16(ts + 16 * half, pb);
                 }
                 if (QT == 2) turn_end(g, gw);
-                const float2 s0 = unpack2f(add2(sum[0], sum[1]));
-                bool odd = false;
-                uint32_t vt = 0;
-                if (!whole_item) {
+                const float2 s0 = unpack2f(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
+                l_row += s0.x + s0.y;
+                if (care) {
                     // V in places that a row does not see, once it has landed.  The parity is not ambiguous: the tile before it in this
                     // slot was multiplied before S(t) was, the one behind it waits for P V(t).
                     const uint32_t slot = gt % VS;
                     ok = __all_sync(0xffffffffu, wait(&sh->v_full[slot], (gt / VS) & 1u)) && ok;
-                    vt = smem_u32(sV) + slot * kT;
+                    const uint32_t vt = smem_u32(sV) + slot * kT;
+                    bool odd = false;
 #pragma unroll
                     for (int at = 0; at < kAtoms; ++at)
                         for (uint32_t off = tid * 16; off < kKT * 128; off += 128 * QT * 16) {
@@ -464,34 +567,17 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                             }
                         }
                     proxy_fence();
-                }
-                if (rescale || !whole_item) {
-                    // P V(t - 1) has been added to O.  The parity is not ambiguous: S(t) was issued behind P V(t - kB), so P V(t - 3),
-                    // which the same barrier counts, has completed; P V(t + 1) cannot have, it is behind this P.
-                    if (t > 0) ok = __all_sync(0xffffffffu, wait(&sh->pv_done[g][(gt - 1) & 1u], ((gt - 1) >> 1) & 1u)) && ok;
-                    tc_fence_after();
-                }
-                if (rescale && t > 0) {                                  // warp-uniform; rows that keep their shift multiply by 1
-#pragma unroll 1
-                    for (int c = 0; c < HD / 32; ++c) {
-                        uint32_t v[32];
-                        tmem_ld32(o_base + c * 32, v);
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * factor);
-                        tmem_st32(o_base + c * 32, v);
-                    }
-                }
-                bool given = false;                                      // values of V are added to O here
-                if (!whole_item) {
-                    given = softmax_any<QT>(odd);                        // all have looked and cleared: they share the V tile
-                    if (given) {                                         // rare
+                    const bool given = softmax_any<QT>(odd);             // all have looked and cleared: they share the V tile
+                    if (given) {                                         // rare: values of V are added to O here
+                        if (t > 0) ok = __all_sync(0xffffffffu, wait(&sh->pv_done[g][(gt - 1) & 1u], ((gt - 1) >> 1) & 1u)) && ok;
+                        tc_fence_after();
                         tmem_wait_st();
                         if (t == 0) {
-                            uint32_t z[32];
+                            uint32_t z[16];
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) z[j] = 0u;
+                            for (int j = 0; j < 16; ++j) z[j] = 0u;
 #pragma unroll 1
-                            for (int c = 0; c < HD / 32; ++c) tmem_st32(o_base + c * 32, z);
+                            for (int c = 0; c < HD / 16; ++c) tmem_st16(o_base + c * 16, z);
                             tmem_wait_st();
                         }
 #pragma unroll 1
@@ -514,14 +600,22 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                         }
                         proxy_fence();
                         softmax_barrier<QT>();
+                        if (t == 0 && r == 0) sh->keep_o[g] = 1;
                     }
                 }
-                if (t == 0 && r == 0) sh->keep_o[g] = given;
-                l_row = l_row * factor + (s0.x + s0.y);
+                // The next scores are asked for before P is waited for: one latency instead of two.  They depend on P of the tile before
+                // this one only.
+                if (t + 1 < n) ask(t + 1);
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh->p_full[g][b]);
+            };
+            if (r == 0) sh->keep_o[g] = 0;
+            ask(0);
+            for (int t = 0; t < n; ++t) {
+                const int k0 = w.k.tile(w.t0 + t) << 6;
+                tile(!(k0 + kKT <= item_hi && (k0 >= item_lo || k0 + kKT <= a.sinks)), t, k0);
             }
             done += n;
             const float m_log2 = M_row == -INFINITY ? 0.f : M_row;      // the shift the row's sum and output carry
@@ -596,31 +690,34 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
     }
 }
 
-// Adds up the parts of the items that several CTAs share, 32 rows a block: with the whole GPU behind it 4 us, where the last CTA of
-// an item took up to 27 us for 128 rows of five parts.
+// Adds up the parts of the items that several CTAs share: 16 rows a block, two at a time a warp, few registers, so that the blocks of
+// all items are on the SMs at once and one latency after the other is hidden.  (By the last CTA of an item, which alone has too few
+// loads in flight, up to 27 us for 128 rows of five parts; in blocks of 32 rows with eight at a time, two to a wave, 12 us.)
+constexpr int kMergeRows = 16;
 template <int HD>
-__global__ void __launch_bounds__(128) paged_merge_kernel(const PagedAttnArgs a) {
+__global__ void __launch_bounds__(128, 8) paged_merge_kernel(const PagedAttnArgs a) {
     pdl_launch_dependents();
     pdl_wait();
     const PagedShared d = a.shared[blockIdx.x];
-    const int warp = threadIdx.x >> 5, r0 = blockIdx.y * 32 + warp;
-    if (r0 >= d.rows) return;
-    PagedSum<HD, 8> sum;
-    sum.parts(a, blockIdx.x, blockIdx.x, d.last_cta + 1, r0, 4, d.rows);
+#pragma unroll 1
+    for (int r0 = blockIdx.y * kMergeRows + (threadIdx.x >> 5); r0 < min(d.rows, static_cast<int>(blockIdx.y + 1) * kMergeRows); r0 += 8) {
+        PagedSum<HD, 2> sum;
+        sum.parts(a, blockIdx.x, blockIdx.x, d.last_cta + 1, r0, 4, d.rows);
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-        if (r0 + 4 * k < d.rows) sum.write(a, k, d.row0, d.head, d.first_idx + r0 + 4 * k);
+        for (int k = 0; k < 2; ++k)
+            if (r0 + 4 * k < d.rows) sum.write(a, k, d.row0, d.head, d.first_idx + r0 + 4 * k);
+    }
 }
 
 template <int HD, int QT>
-cudaError_t launch(const PagedAttnArgs& a, const CUtensorMap& tm_q, const PagedMaps& maps, int sms, cudaStream_t st) {
+cudaError_t launch(const PagedAttnArgs& a, const CUtensorMap& tm_q, const PagedMaps& maps, cudaStream_t st) {
     static std::atomic<unsigned long long> attr_done{0};
     cudaError_t e = set_smem_limit_once(attr_done, paged_attention_tc_kernel<HD, QT>, static_cast<int>(kSmem<HD, QT>));
     if (e != cudaSuccess) return e;
-    const dim3 grid(QT == 1 ? 2 * sms : sms);
+    const dim3 grid(a.at_once);
     e = launch_kernel(paged_attention_tc_kernel<HD, QT>, grid, dim3(kThreads<QT>), kSmem<HD, QT>, st, tm_q, maps.rows, maps.atoms, a);
     if (e != cudaSuccess) return e;
-    return launch_kernel(paged_merge_kernel<HD>, dim3(grid.x, QT * kTQ / 32), dim3(128), 0, st, a);
+    return launch_kernel(paged_merge_kernel<HD>, dim3(grid.x, QT * kTQ / kMergeRows), dim3(128), 0, st, a);
 }
 
 }  // namespace
@@ -631,12 +728,14 @@ cudaError_t launch_paged_attention_tc(PagedAttnArgs a, const PagedMaps& maps, in
     a.tile_tokens = kTQ / a.G;
     a.tile_rows = q_tiles * a.tile_tokens * a.G;
     a.by_rows = PagedDiv::by(a.tile_rows);
+    a.at_once = q_tiles == 1 ? 2 * sms : sms;
+    a.by_once = PagedDiv::by(a.at_once);
     a.part_rows = q_tiles * kTQ;
     CUtensorMap tm_q;
     const cudaError_t e = make_group_tmap(&tm_q, a.q, a.max_rows, a.q_stride, a.H, hd, a.G, a.tile_tokens);
     if (e != cudaSuccess) return e;
-    if (q_tiles == 1) return hd == 128 ? launch<128, 1>(a, tm_q, maps, sms, st) : launch<64, 1>(a, tm_q, maps, sms, st);
-    return hd == 128 ? launch<128, 2>(a, tm_q, maps, sms, st) : launch<64, 2>(a, tm_q, maps, sms, st);
+    if (q_tiles == 1) return hd == 128 ? launch<128, 1>(a, tm_q, maps, st) : launch<64, 1>(a, tm_q, maps, st);
+    return hd == 128 ? launch<128, 2>(a, tm_q, maps, st) : launch<64, 2>(a, tm_q, maps, st);
 }
 
 }  // namespace odb
