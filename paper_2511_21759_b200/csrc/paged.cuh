@@ -7,8 +7,8 @@
 namespace odb {
 
 constexpr int kPagedMaxSeqs = 1024;        // requests of one forward
-constexpr int kPagedMaxCtas = 4864;        // CTAs of an attention launch, at most (of 16 rows; in proportion fewer with more)
-constexpr int kPagedPartRows = 16 * kPagedMaxCtas;   // rows that the workspace holds of all CTAs' first or last items
+constexpr int kPagedMaxCtas = 1216;        // CTAs of an attention launch, at most: four waves of two on each of the 148 SMs
+constexpr int kPagedPartRows = 304 * 128;  // rows that the workspace holds of all CTAs' first or last items, whatever the kernel
 constexpr int kPagedMaxParts = 2;          // unfinished segments a CTA leaves behind: of its first item and of its last
 constexpr int kPagedUnlimited = 1 << 30;   // a window side without limit; lengths and positions stay below it
 

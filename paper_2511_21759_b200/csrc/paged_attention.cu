@@ -6,11 +6,15 @@
 // maximum m and sum in fp32; P is rounded to bf16 for the second product (the sum keeps the unrounded values: the rounding's
 // relative error of up to 2^-8 per key is independent from key to key and ends below the output's own rounding).
 //
-// Work: see paged.cuh; every CTA takes the same number of key tiles of 64 positions.  One warp loads (TMA, a box per page of
-// a tile, 128-byte swizzle, rings of K and of V tiles with a full and an empty barrier each), four warps multiply (mma.sync m16n8k16):
-// ROWS / 16 groups of rows x 64 / ROWS groups of keys, each warp with a running maximum, sum and output of its own, which
-// meet when the item ends.  An item that several CTAs share leaves unnormalised parts in the workspace; the CTA that arrives
-// last adds them up in the order of the CTAs, whoever it is: the same bits every time.
+// Work: see paged.cuh; items of 16 packed rows, key tiles of 64 positions.  One warp loads (TMA, a box per page of a tile, 128-byte
+// swizzle, rings of K and of V tiles with a full and an empty barrier each), four warps multiply (mma.sync m16n8k16), 16 keys of a
+// tile each with a running maximum, sum and output of their own, which meet in the last V tile's place when the item ends.  An item
+// that several CTAs share leaves unnormalised parts in the workspace; the CTA that arrives last adds them up in the order of the
+// CTAs, whoever it is: the same bits every time.
+//
+// Bound by HBM where there is work for all SMs (a pool read once; the products of 16 rows take a third of a tile's time): one token
+// of 48 requests, 905 MB, 156 us = 5.8 TB/s, of two of 131072 keys, 1.02 GB, 170 us = 6.0 TB/s; the rest is the start (2 us to find
+// the share), the parts and the slowest SMs' tail.  Small calls are bound by latency: one token of 577 keys 10 us.
 //
 // Rows of V behind the last visible key are whatever the page held before: their P is zero, but zero times an infinity or NaN
 // there is not, so they are set to zero in shared memory first.  A key that some rows of the tile see and others do not is
@@ -24,6 +28,7 @@ namespace {
 constexpr int kKT = 64;                    // keys per tile
 constexpr int kItem = 1;                    // key tiles that an item costs beside its own
 constexpr int kMinUnits = 2, kFullUnits = 24;   // units of a CTA, at least; where all places on the SMs have work
+constexpr int kRows = 16;                   // packed rows of an item
 constexpr int kMmaWarps = 4;
 constexpr int kThreads = 32 * (kMmaWarps + 1);
 template <int HD> constexpr int kKSlots = HD == 128 ? 3 : 7;                // K tiles on the way or in use
@@ -69,12 +74,6 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma_warps_barrier() { asm volatile("bar.sync 1, %0;" ::"r"(32 * kMmaWarps) : "memory"); }
-// the warps with the same keys and other rows
-template <int WR>
-__device__ __forceinline__ void key_group_barrier(int wk) {
-    if constexpr (WR > 1) asm volatile("bar.sync %0, %1;" ::"r"(2 + wk), "r"(32 * WR) : "memory");
-    else __syncwarp();
-}
 __device__ __forceinline__ float quad_max(float x) {
     x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
     return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
@@ -87,9 +86,9 @@ __device__ __forceinline__ bool odd_bf16(uint32_t two) {   // one of the two is 
     return (two & 0x7f80u) == 0x7f80u || (two & 0x7f800000u) == 0x7f800000u;
 }
 
-template <int HD, int ROWS>
+template <int HD>
 __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __grid_constant__ CUtensorMap tm, const PagedAttnArgs a) {
-    constexpr int WR = ROWS / 16, WK = kMmaWarps / WR, KW = kKT / WK;   // warps along the rows and the keys, keys of a warp
+    constexpr int KW = kKT / kMmaWarps;                         // keys of a warp
     constexpr int kAtoms = HD / 64, NS = KW / 8, ND = HD / 8;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t* smem = smem_raw;
@@ -179,16 +178,15 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
     }
 
     // ================= the products =================
-    const int wr = warp % WR, wk = warp / WR;
-    const int r_lo = wr * 16 + (lane >> 2);                     // this thread's rows of the tile: r_lo and r_lo + 8
+    const int r_lo = lane >> 2;                     // this thread's rows of the tile: r_lo and r_lo + 8
     do {
-        const int rows = min(ROWS, w.q.n * a.G - w.rt * ROWS);  // packed rows of this item
+        const int rows = min(kRows, w.q.n * a.G - w.rt * kRows);  // packed rows of this item
         uint32_t qf[HD / 16][4];
         int pos[2];
         size_t at[2];                                           // row of q, out and lse, in heads
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const int r = min(r_lo + 8 * e, rows - 1), idx = w.rt * ROWS + r, i = a.by_group(idx);   // rows behind the last repeat it
+            const int r = min(r_lo + 8 * e, rows - 1), idx = w.rt * kRows + r, i = a.by_group(idx);   // rows behind the last repeat it
             pos[e] = w.q.first + i;
             at[e] = static_cast<size_t>(w.q.row0 + i);
             const __nv_bfloat16* qp = a.q + at[e] * a.q_stride + (w.head * a.G + idx - i * a.G) * HD + (lane & 3) * 2;
@@ -198,8 +196,8 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                 qf[kk][2 + e] = *reinterpret_cast<const uint32_t*>(qp + kk * 16 + 8);
             }
         }
-        const int idx_last = w.rt * ROWS + rows - 1;
-        const int p_min = w.q.first + a.by_group(w.rt * ROWS), p_max = w.q.first + a.by_group(idx_last);
+        const int idx_last = w.rt * kRows + rows - 1;
+        const int p_min = w.q.first + a.by_group(w.rt * kRows), p_max = w.q.first + a.by_group(idx_last);
         // keys from all_lo on and below all_hi are seen by all rows of the item
         const int all_hi = static_cast<int>(max(0ll, min(static_cast<long long>(w.q.len), static_cast<long long>(p_min) + a.right + 1)));
         const int all_lo = static_cast<int>(max(-1ll, static_cast<long long>(p_max) - a.left));
@@ -211,7 +209,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
             for (int j = 0; j < 4; ++j) o[d][j] = 0.f;
 
         for (int t = w.t0; t < w.t1; ++t) {
-            const int k0 = (w.k.tile(t) << 6) + wk * KW;        // this warp's first key
+            const int k0 = (w.k.tile(t) << 6) + warp * KW;        // this warp's first key
             // Behind an expired wait the warp goes on through the tiles without their products: it must not be missing at a barrier.
             bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh->k_full[kr.slot], kr.phase, cta_abort, a.status));
             bool k_read = false;
@@ -234,7 +232,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                 const uint32_t sw = static_cast<uint32_t>(lane & 7) << 4;
 #pragma unroll
                 for (int nb = 0; nb < NS; nb += 2) {
-                    const int c = wk * KW + nb * 8 + (lane & 7) + ((lane >> 4) << 3);
+                    const int c = warp * KW + nb * 8 + (lane & 7) + ((lane >> 4) << 3);
                     float odd[2][4] = {};                       // every other step in sums of its own: half as long a chain of products
 #pragma unroll
                     for (int kk = 0; kk < HD / 16; ++kk) {
@@ -305,7 +303,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                     bool odd = false;
 #pragma unroll 4
                     for (int i = 0; i < kChunks; ++i) {
-                        const int c16 = i * 32 + lane, c = wk * KW + c16 / (HD / 8), ch = c16 % (HD / 8);
+                        const int c16 = i * 32 + lane, c = warp * KW + c16 / (HD / 8), ch = c16 % (HD / 8);
                         const int key = k0 + c16 / (HD / 8);
                         const uint32_t ad = sv + key_at(c, ch >> 3) + (((ch & 7) ^ (c & 7)) << 4);
                         uint32_t v[4];
@@ -317,11 +315,11 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                             odd = odd || odd_bf16(v[0]) || odd_bf16(v[1]) || odd_bf16(v[2]) || odd_bf16(v[3]);
                     }
                     odd = __any_sync(0xffffffffu, odd);
-                    key_group_barrier<WR>(wk);                  // all have looked
+                    __syncwarp();                  // all have looked
                     if (odd) {
 #pragma unroll 1
                         for (int kc = 0; kc < KW; ++kc) {       // rare: an infinity or NaN in V, seen by some of the rows
-                            const int key = k0 + kc, c = wk * KW + kc;
+                            const int key = k0 + kc, c = warp * KW + kc;
                             float pr[2];
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {       // P of this thread's rows and this key, from the lane that has it
@@ -350,10 +348,10 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                                 }
                             }
                         }
-                        key_group_barrier<WR>(wk);
+                        __syncwarp();
 #pragma unroll 1
                         for (int i = 0; i < KW * HD / 2 / 32; ++i) {
-                            const int c2 = i * 32 + lane, kc = c2 / (HD / 2), dd = c2 % (HD / 2), c = wk * KW + kc;
+                            const int c2 = i * 32 + lane, kc = c2 / (HD / 2), dd = c2 % (HD / 2), c = warp * KW + kc;
                             const uint32_t ad = sv + key_at(c, dd >> 5) + ((((dd >> 2) & 7) ^ (c & 7)) << 4) + (dd & 3) * 4;
                             uint32_t v;
                             asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(ad) : "memory");
@@ -361,14 +359,14 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                             if ((v & 0x7f800000u) == 0x7f800000u) v &= 0xffffu;
                             asm volatile("st.shared.b32 [%0], %1;" ::"r"(ad), "r"(v) : "memory");
                         }
-                        key_group_barrier<WR>(wk);
+                        __syncwarp();
                     }
                     __syncwarp();
                 }
 #pragma unroll
                 for (int kb = 0; kb < KW / 16; ++kb) {
                     const uint32_t pa[4] = {p[2 * kb][0], p[2 * kb][1], p[2 * kb + 1][0], p[2 * kb + 1][1]};
-                    const int c = wk * KW + kb * 16 + (lane & 15);
+                    const int c = warp * KW + kb * 16 + (lane & 15);
 #pragma unroll
                     for (int d = 0; d < ND; d += 2) {
                         uint32_t b[4];
@@ -383,7 +381,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                 k_done();
                 mbar_wait_bounded(&sh->v_full[vr.slot], vr.phase, cta_abort, a.status);
             }
-            if (WK > 1 && t + 1 == w.t1) break;                 // the item's last V tile stays: its place is where the warps meet
+            if (t + 1 == w.t1) break;                 // the item's last V tile stays: its place is where the warps meet
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh->v_empty[vr.slot]);
             vr.next(VS);
@@ -392,7 +390,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
         // ---- the warps that share the rows meet ----
 #pragma unroll
         for (int e = 0; e < 2; ++e) l[e] = quad_sum(l[e]);
-        if constexpr (WK > 1) {
+        {
             if ((lane & 3) == 0) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
@@ -407,10 +405,10 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
             for (int e = 0; e < 2; ++e) {
                 float M = -INFINITY, L = 0.f;
 #pragma unroll
-                for (int g = 0; g < WK; ++g) M = fmaxf(M, sh->ml[g * WR + wr][(lane >> 2) + 8 * e][0]);
+                for (int g = 0; g < kMmaWarps; ++g) M = fmaxf(M, sh->ml[g][(lane >> 2) + 8 * e][0]);
 #pragma unroll
-                for (int g = 0; g < WK; ++g) {
-                    const float* x = sh->ml[g * WR + wr][(lane >> 2) + 8 * e];
+                for (int g = 0; g < kMmaWarps; ++g) {
+                    const float* x = sh->ml[g][(lane >> 2) + 8 * e];
                     L += paged_weight(x[0], M) * x[1];
                 }
                 const float f = paged_weight(m[e], M);
@@ -423,16 +421,16 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                 l[e] = L;
             }
 #pragma unroll
-            for (int half = WK / 2; half >= 1; half >>= 1) {     // the upper half of the key groups hands over to the lower
-                float* mb = merge + (((wk % half) * WR + wr) * ND * 4) * 32 + lane;
-                if (wk >= half && wk < 2 * half) {
+            for (int half = kMmaWarps / 2; half >= 1; half >>= 1) {   // the upper half of the warps hands over to the lower
+                float* mb = merge + (warp % half) * ND * 4 * 32 + lane;
+                if (warp >= half && warp < 2 * half) {
 #pragma unroll
                     for (int d = 0; d < ND; ++d)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) mb[(d * 4 + j) * 32] = o[d][j];
                 }
                 mma_warps_barrier();
-                if (wk < half) {
+                if (warp < half) {
 #pragma unroll
                     for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -449,13 +447,13 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
         // ---- results, or this CTA's part of them ----
         const bool final = w.whole();
         const size_t part = paged_part(a, blockIdx.x, w.t0 == 0);
-        if (wk == 0) {
+        if (warp == 0) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int r = r_lo + 8 * e;
                 if (r >= rows) continue;
                 if (final) {
-                    const int idx = w.rt * ROWS + r, head = w.head * a.G + idx - a.by_group(idx) * a.G;
+                    const int idx = w.rt * kRows + r, head = w.head * a.G + idx - a.by_group(idx) * a.G;
                     const float inv = l[e] == 0.f ? 0.f : 1.0f / l[e];
                     __nv_bfloat16* op = a.out + at[e] * a.out_stride + head * HD + (lane & 3) * 2;
 #pragma unroll
@@ -484,7 +482,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                 for (int r = warp; r < rows; r += kMmaWarps) {
                     PagedSum<HD, 1> sum;
                     sum.row(a, c0, c1, r);
-                    sum.write(a, 0, w.q.row0, w.head, w.rt * ROWS + r);
+                    sum.write(a, 0, w.q.row0, w.head, w.rt * kRows + r);
                 }
                 mma_warps_barrier();                             // sh->last has been read by all
             }
@@ -492,42 +490,41 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
     } while (w.next());
 }
 
-template <int HD, int ROWS>
-cudaError_t launch_few(PagedAttnArgs a, const CUtensorMap& tmap, int sms, cudaStream_t st) {
+template <int HD>
+cudaError_t launch(PagedAttnArgs a, const CUtensorMap& tmap, int sms, cudaStream_t st) {
     static std::atomic<unsigned long long> attr_done{0};
-    cudaError_t e = set_smem_limit_once(attr_done, paged_attention_kernel<HD, ROWS>, static_cast<int>(kSmem<HD>));
+    cudaError_t e = set_smem_limit_once(attr_done, paged_attention_kernel<HD>, static_cast<int>(kSmem<HD>));
     if (e != cudaSuccess) return e;
-    a.tile_rows = ROWS;
-    a.by_rows = PagedDiv::by(ROWS);
-    a.part_rows = ROWS;
+    a.tile_rows = kRows;
+    a.by_rows = PagedDiv::by(kRows);
+    a.part_rows = kRows;
     a.at_once = 2 * sms;
     a.by_once = PagedDiv::by(a.at_once);
     // Under a full memory system some SMs run a third slower than others, and so does the second CTA of an SM: of one share for each
     // place the last ended a third behind the mean.  So four waves of CTAs, taken by whichever place is free, of shares that grow
     // smaller to the end.  No more CTAs than the table's width leaves work for.
     const long long tiles = (static_cast<long long>(a.table_stride) << a.page_shift) / kKT + 1 + kItem,
-                    most = (static_cast<long long>(a.max_rows) * a.G / ROWS + a.n_seqs) * a.KV * tiles / kMinUnits + 1;
-    const int grid = static_cast<int>(most < kPagedWaves * 2 * sms ? most : kPagedWaves * 2 * sms);
-    return launch_kernel(paged_attention_kernel<HD, ROWS>, dim3(grid), dim3(kThreads), kSmem<HD>, st, tmap, a);
-}
-
-template <int HD>
-cudaError_t launch_hd(const PagedAttnArgs& a, const CUtensorMap& tmap, long long rows, int sms, cudaStream_t st) {
-    if (rows <= 16) return launch_few<HD, 16>(a, tmap, sms, st);
-    if (rows <= 32) return launch_few<HD, 32>(a, tmap, sms, st);
-    return launch_few<HD, 64>(a, tmap, sms, st);
+                    most = (static_cast<long long>(a.max_rows) * a.G / kRows + a.n_seqs) * a.KV * tiles / kMinUnits + 1;
+    static_assert(kPagedMaxCtas * kRows <= kPagedPartRows, "parts");
+    const int grid = static_cast<int>(most < kPagedWaves * a.at_once ? most : kPagedWaves * a.at_once);
+    return launch_kernel(paged_attention_kernel<HD>, dim3(grid), dim3(kThreads), kSmem<HD>, st, tmap, a);
 }
 
 }  // namespace
 
 size_t paged_part_bytes(int hd) { return static_cast<size_t>(kPagedMaxParts) * kPagedPartRows * (hd + 2) * sizeof(float); }
 
+// Which kernel, by the packed rows of the longest request.  us, few rows' kernel / tensor cores with one Q tile / with two, 8 K/V heads
+// of 128:
+//   4 packed rows, 1 request of 577 keys 10 / 20 / 18, 2 of 131072 174 / 170 / 249, 48 of up to 8192 155 / 150 / 222
+//   16 packed rows, 16 requests of 4096 keys 55 / 49 / 66, 2 of them 23 / 25 / 27;   32, 16 requests 87 / 49 / 65, of 600 keys 27 / 22 / 26
+//   128 packed rows, 16 requests of 4096 keys - / 54 / 66;   192: - / 79 / 72;   256: - / 86 / 78;   a prompt of 4096: - / 180 / 176
 cudaError_t launch_paged_attention(PagedAttnArgs a, const PagedMaps& maps, int hd, int max_new, int sms, cudaStream_t st) {
-    if (sms < 1 || kPagedWaves * 2 * sms * 64 > kPagedPartRows) return cudaErrorInvalidValue;   // every kernel's parts fit the workspace
+    if (sms < 1 || 2 * sms * 128 > kPagedPartRows || kPagedWaves * 2 * sms > kPagedMaxCtas) return cudaErrorInvalidValue;   // the workspace's size
     a.by_group = PagedDiv::by(a.G);
     const long long rows = static_cast<long long>(max_new) * a.G;
-    if (rows > 64 && a.G <= kPagedTcMaxGroup) return launch_paged_attention_tc(a, maps, hd, rows > 128 ? 2 : 1, sms, st);
-    return hd == 128 ? launch_hd<128>(a, maps.rows, rows, sms, st) : launch_hd<64>(a, maps.rows, rows, sms, st);
+    if (rows > kRows && a.G <= kPagedTcMaxGroup) return launch_paged_attention_tc(a, maps, hd, rows > 128 ? 2 : 1, sms, st);
+    return hd == 128 ? launch<128>(a, maps.rows, sms, st) : launch<64>(a, maps.rows, sms, st);
 }
 
 }  // namespace odb

@@ -48,7 +48,8 @@ class Rope:
 class Batch:
     """The device arrays of one forward (odb_paged_batch); arrays that a call needs and that are not given are made here,
     those that are given are used as they are: int32, contiguous, on the cache's device.  max_rows: rows of the forward
-    (known where row arrays are given); max_new: rows of the longest request, a hint (max_rows where not given)."""
+    (known where row arrays are given); max_new: rows of the longest request, a hint that picks the attention's kernel (where
+    not given, rows divided by requests)."""
 
     _INPUTS = ("len_before", "len_after", "first", "count", "table", "free_pages", "row_start", "row_seq", "row_pos", "row_slot")
 
@@ -76,7 +77,7 @@ class Batch:
             raise ValueError(f"free_pages: {cache.n_pages} entries are wanted")
         self.n_seqs = n_seqs
         self.max_rows = rows.pop() if rows else (max_rows or 0)
-        self.max_new = self.max_rows if max_new is None else max_new
+        self.max_new = -(-self.max_rows // max(1, n_seqs)) if max_new is None else max_new
         new = lambda n: torch.empty(n, dtype=torch.int32, device=cache.device)
         if given["row_start"] is None and seqs:
             given["row_start"] = new(n_seqs + 1)
