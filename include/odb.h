@@ -470,18 +470,31 @@ enum { ODB_ROPE_PLAIN = 0, ODB_ROPE_LINEAR = 1, ODB_ROPE_NTK = 2, ODB_ROPE_YARN 
 int32_t odb_rope_frequencies(int32_t rot_dim, double theta, int32_t scaling, double factor, double original_len, double beta_slow,
                              double beta_fast, uint64_t* turns_host, float* magnitude);
 
+/* What norm_rope_store reads and writes: bf16 rows on 8-byte boundaries, strides in elements between rows (multiples of 4;
+ * q, k and v may be slices of one projection's output).  q_out may be q itself (same stride). */
+typedef struct odb_paged_rows {
+    const void* q; int64_t q_stride;            /* [max_rows][n_heads][head_dim] */
+    const void* k; int64_t k_stride;            /* [max_rows][n_kv_heads][head_dim] */
+    const void* v; int64_t v_stride;
+    void* q_out; int64_t out_stride;
+    const float* q_gain;                        /* fp32 [head_dim] on a 16-byte boundary; NULL: q is not normed */
+    const float* k_gain;
+} odb_paged_rows;
+
+/* Rotation of the first rot_dim values of a head (a multiple of 8 up to head_dim, 0: none). */
+typedef struct odb_rope {
+    const uint64_t* turns;                      /* device copy of odb_rope_frequencies' numbers, on a 16-byte boundary */
+    int32_t rot_dim;
+    int32_t interleaved;                        /* 0: pairs (i, i + rot_dim / 2), otherwise (2i, 2i + 1) */
+    float magnitude;                            /* odb_rope_frequencies' */
+} odb_rope;
+
 /* For every row r < max_rows with row_pos[r] >= 0: q_out = rotate(norm(q)), and K := rotate(norm(k)), V := v at
  * row_slot[r] (a slot that is none, -1 for one, stores nothing).  norm: x / sqrt(mean(x^2) + eps) * gain over a head's
- * head_dim values, gains fp32 [head_dim], on 16-byte boundaries, NULL: no norm (of q, of k).  rotate: pairs (i, i + rot_dim / 2), or (2i, 2i + 1)
- * where interleaved, of the first rot_dim values (a multiple of 8 up to head_dim, 0: none) by position x frequency
- * (turns: device copy of odb_rope_frequencies' numbers, on a 16-byte boundary); the other values pass.  fp32, rounded once.
- * q [max_rows][n_heads][head_dim], k and v [max_rows][n_kv_heads][head_dim], bf16 on 8-byte boundaries, strides in
- * elements between rows (multiples of 4; the three may be slices of one projection's output).  q_out may be q itself
- * (same stride).  Two rows with the same slot: one of them is stored. */
-int32_t odb_paged_norm_rope_store(odb_paged* h, int32_t layer, const odb_paged_batch* b, const void* q, int64_t q_stride, const void* k,
-                                  int64_t k_stride, const void* v, int64_t v_stride, const float* q_gain, const float* k_gain, float eps,
-                                  const uint64_t* turns, int32_t rot_dim, int32_t interleaved, float magnitude, void* q_out,
-                                  int64_t out_stride, void* stream);
+ * head_dim values.  rotate: by position x frequency; values behind rot_dim pass.  fp32, rounded once.  Two rows with the
+ * same slot: one of them is stored.  Reads row_pos and row_slot. */
+int32_t odb_paged_norm_rope_store(odb_paged* h, int32_t layer, const odb_paged_batch* b, const odb_paged_rows* rows, const odb_rope* rope,
+                                  float eps, void* stream);
 
 /* out[r][h] = sum_j softmax_j(scale * q[r][h] . K[j][h / group]) V[j][h / group] over the keys j that row r at position
  * p = first + (r - row_start) sees: j < len_after, j <= p + right, and j >= p - left or j < sinks (left, right: -1 = no

@@ -64,6 +64,15 @@ class odb_paged_batch(C.Structure):
                                           "row_seq", "row_pos", "row_slot")]
 
 
+class odb_paged_rows(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_stride", C.c_int64), ("k", C.c_void_p), ("k_stride", C.c_int64), ("v", C.c_void_p),
+                ("v_stride", C.c_int64), ("q_out", C.c_void_p), ("out_stride", C.c_int64), ("q_gain", C.c_void_p), ("k_gain", C.c_void_p)]
+
+
+class odb_rope(C.Structure):
+    _fields_ = [("turns", C.c_void_p), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("magnitude", C.c_float)]
+
+
 # name -> (restype, argtypes); the list the header declares
 SIGNATURES = {
     "odb_status_string": (C.c_char_p, [C.c_int32]),
@@ -120,9 +129,8 @@ SIGNATURES = {
     "odb_paged_layout": (C.c_int32, [C.c_void_p, C.POINTER(odb_paged_batch), C.c_void_p]),
     "odb_rope_frequencies": (C.c_int32, [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double,
                                          C.POINTER(C.c_uint64), C.POINTER(C.c_float)]),
-    "odb_paged_norm_rope_store": (C.c_int32, [C.c_void_p, C.c_int32, C.POINTER(odb_paged_batch), C.c_void_p, C.c_int64, C.c_void_p,
-                                              C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p,
-                                              C.c_int32, C.c_int32, C.c_float, C.c_void_p, C.c_int64, C.c_void_p]),
+    "odb_paged_norm_rope_store": (C.c_int32, [C.c_void_p, C.c_int32, C.POINTER(odb_paged_batch), C.POINTER(odb_paged_rows),
+                                              C.POINTER(odb_rope), C.c_float, C.c_void_p]),
     "odb_paged_attention": (C.c_int32, [C.c_void_p, C.c_int32, C.POINTER(odb_paged_batch), C.c_void_p, C.c_int64, C.c_void_p,
                                         C.c_int64, C.c_void_p, C.c_float, C.c_int32, C.c_int32, C.c_int32, C.c_void_p]),
 }

@@ -153,38 +153,36 @@ int32_t odb_rope_frequencies(int32_t rot_dim, double theta, int32_t scaling, dou
     return ODB_OK;
 }
 
-int32_t odb_paged_norm_rope_store(odb_paged* h, int32_t layer, const odb_paged_batch* b, const void* q, int64_t q_stride, const void* k,
-                                  int64_t k_stride, const void* v, int64_t v_stride, const float* q_gain, const float* k_gain, float eps,
-                                  const uint64_t* turns, int32_t rot_dim, int32_t interleaved, float magnitude, void* q_out,
-                                  int64_t out_stride, void* stream) {
+int32_t odb_paged_norm_rope_store(odb_paged* h, int32_t layer, const odb_paged_batch* b, const odb_paged_rows* r, const odb_rope* rope,
+                                  float eps, void* stream) {
     const int32_t rc = check_call(h, layer);
     if (rc != ODB_OK) return rc;
-    if (!b || b->max_rows < 0) return ODB_ERR_ARG;
+    if (!b || !r || !rope || b->max_rows < 0) return ODB_ERR_ARG;
     const odb_paged_config& c = h->cfg;
-    if (rot_dim < 0 || rot_dim > c.head_dim || rot_dim % 8) return ODB_ERR_SHAPE;
+    if (rope->rot_dim < 0 || rope->rot_dim > c.head_dim || rope->rot_dim % 8) return ODB_ERR_SHAPE;
     if (b->max_rows == 0) return ODB_OK;
-    if (!q || !k || !v || !q_out || !b->row_pos || !b->row_slot || (rot_dim && !turns)) return ODB_ERR_ARG;
-    if (!(eps >= 0.f) || !isfinite(eps) || !isfinite(magnitude)) return ODB_ERR_ARG;
+    if (!r->q || !r->k || !r->v || !r->q_out || !b->row_pos || !b->row_slot || (rope->rot_dim && !rope->turns)) return ODB_ERR_ARG;
+    if (!(eps >= 0.f) || !isfinite(eps) || !isfinite(rope->magnitude)) return ODB_ERR_ARG;
     const int64_t qw = static_cast<int64_t>(c.n_heads) * c.head_dim, kw = static_cast<int64_t>(c.n_kv_heads) * c.head_dim;
-    if (q_stride < qw || out_stride < qw || k_stride < kw || v_stride < kw) return ODB_ERR_ARG;
-    if (!aligned(q, 8) || !aligned(k, 8) || !aligned(v, 8) || !aligned(q_out, 8) || !aligned(q_gain, 16) || !aligned(k_gain, 16) ||
-        !aligned(turns, 16) || ((q_stride | k_stride | v_stride | out_stride) & 3))
+    if (r->q_stride < qw || r->out_stride < qw || r->k_stride < kw || r->v_stride < kw) return ODB_ERR_ARG;
+    if (!aligned(r->q, 8) || !aligned(r->k, 8) || !aligned(r->v, 8) || !aligned(r->q_out, 8) || !aligned(r->q_gain, 16) || !aligned(r->k_gain, 16) ||
+        !aligned(rope->turns, 16) || ((r->q_stride | r->k_stride | r->v_stride | r->out_stride) & 3))
         return ODB_ERR_ARG;
     if (static_cast<double>(b->max_rows) * (c.n_heads + 2 * c.n_kv_heads) >= 2147483648.0) return ODB_ERR_SHAPE;
     PagedStoreArgs a{};
-    a.q = static_cast<const __nv_bfloat16*>(q);
-    a.k = static_cast<const __nv_bfloat16*>(k);
-    a.v = static_cast<const __nv_bfloat16*>(v);
-    a.q_out = static_cast<__nv_bfloat16*>(q_out);
-    a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride; a.out_stride = out_stride;
-    a.q_gain = q_gain; a.k_gain = k_gain; a.eps = eps;
-    a.turns = reinterpret_cast<const unsigned long long*>(turns);
-    a.magnitude = magnitude;
+    a.q = static_cast<const __nv_bfloat16*>(r->q);
+    a.k = static_cast<const __nv_bfloat16*>(r->k);
+    a.v = static_cast<const __nv_bfloat16*>(r->v);
+    a.q_out = static_cast<__nv_bfloat16*>(r->q_out);
+    a.q_stride = r->q_stride; a.k_stride = r->k_stride; a.v_stride = r->v_stride; a.out_stride = r->out_stride;
+    a.q_gain = r->q_gain; a.k_gain = r->k_gain; a.eps = eps;
+    a.turns = reinterpret_cast<const unsigned long long*>(rope->turns);
+    a.magnitude = rope->magnitude;
     a.row_pos = b->row_pos; a.row_slot = b->row_slot;
     a.k_pool = h->kv + static_cast<size_t>(2 * layer) * h->layer_rows * c.head_dim;
     a.v_pool = a.k_pool + static_cast<size_t>(h->layer_rows) * c.head_dim;
     a.rows = b->max_rows; a.H = c.n_heads; a.KV = c.n_kv_heads; a.HD = c.head_dim;
-    a.rot = rot_dim; a.interleaved = interleaved != 0; a.page_shift = h->page_shift; a.n_pages = c.n_pages;
+    a.rot = rope->rot_dim; a.interleaved = rope->interleaved != 0; a.page_shift = h->page_shift; a.n_pages = c.n_pages;
     return enqueued(launch_paged_store(a, static_cast<cudaStream_t>(stream)));
 }
 

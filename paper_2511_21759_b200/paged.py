@@ -11,11 +11,13 @@ A forward over requests of different lengths, one layer after the other:
         o = cache.attention(layer, batch, q, right=0)
 
 Every call is enqueued on the current stream of the cache's device and returns at once; status() waits and says what the
-device found.  A cache is used on one stream at a time: a call on another stream than the one before waits for that one.
+device found.  A cache is used by one thread and on one stream at a time: a call on another stream than the one before waits for
+that one.
 """
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from typing import Optional
 
 import torch
@@ -23,6 +25,7 @@ import torch
 from . import binding as B
 
 _BF16, _F32 = torch.bfloat16, torch.float32
+_ROWS = struct.Struct("=QqQqQqQqQQ")          # odb_paged_rows, filled in one go
 SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 
 
@@ -42,7 +45,8 @@ class Rope:
         # fractions of a turn per position, 64-bit patterns
         self.turns = torch.tensor([C.c_int64(v).value for v in host], dtype=torch.int64, device=device)
         self.index = self.turns.get_device()
-        self._tail = (self.turns.data_ptr(), rot_dim, 1 if interleaved else 0, mag.value)
+        self._c = B.odb_rope(self.turns.data_ptr(), rot_dim, 1 if interleaved else 0, mag.value)
+        self._ref = C.byref(self._c)
 
 
 class Batch:
@@ -122,6 +126,9 @@ class PagedCache:
             B.check(lib.odb_paged_create(C.byref(self.cfg), kv.data_ptr(), kv.numel() * 2, self.workspace.data_ptr(),
                                          self.workspace.numel(), C.c_void_p(stream.cuda_stream), C.byref(self.handle)), "odb_paged_create")
         self._stream, self._raw, self._index = stream, stream.cuda_stream, self.device.index
+        self._gain_shape = torch.Size((head_dim,))
+        self._rows_c = B.odb_paged_rows()
+        self._rows_ref = C.byref(self._rows_c)
         self._layout, self._store, self._attention = lib.odb_paged_layout, lib.odb_paged_norm_rope_store, lib.odb_paged_attention
 
     def close(self):
@@ -161,8 +168,8 @@ class PagedCache:
 
     def _gain(self, t, what: str):
         if t is None:
-            return None
-        if t.dtype is _F32 and t.get_device() == self._index and t.shape == (self.head_dim,) and t.is_contiguous():
+            return 0
+        if t.dtype is _F32 and t.get_device() == self._index and t.shape == self._gain_shape and t.is_contiguous():
             return t.data_ptr()
         raise ValueError(f"{what}: a contiguous float32 tensor of {self.head_dim} values on {self.device} is wanted")
 
@@ -184,8 +191,8 @@ class PagedCache:
         kp, ks = self._rows(k, "k", self.n_kv_heads, batch._kv)
         vp, vs = self._rows(v, "v", self.n_kv_heads, batch._kv)
         op, os_ = (qp, qs) if q_out is q else self._rows(q_out, "q_out", self.n_heads, batch._q)
-        status = self._store(self.handle, layer, batch._ref, qp, qs, kp, ks, vp, vs, self._gain(q_gain, "q_gain"), self._gain(k_gain, "k_gain"),
-                             eps, *rope._tail, op, os_, self._current())
+        _ROWS.pack_into(self._rows_c, 0, qp, qs, kp, ks, vp, vs, op, os_, self._gain(q_gain, "q_gain"), self._gain(k_gain, "k_gain"))
+        status = self._store(self.handle, layer, batch._ref, self._rows_ref, rope._ref, eps, self._current())
         if status:
             raise B.OdbError(status, "odb_paged_norm_rope_store")
         return q_out

@@ -122,9 +122,10 @@ def test_null_arguments_are_refused():
     batch = b.odb_paged_batch()
     assert lib.odb_paged_layout(None, C.byref(batch), None) == b.ODB_ERR_ARG
     assert lib.odb_paged_attention(None, 0, C.byref(batch), None, 0, None, 0, None, 0.0, -1, -1, 0, None) == b.ODB_ERR_ARG
-    assert lib.odb_paged_norm_rope_store(None, 0, C.byref(batch), None, 0, None, 0, None, 0, None, None, 0.0, None, 0, 0, 1.0, None, 0, None) == b.ODB_ERR_ARG
+    assert lib.odb_paged_norm_rope_store(None, 0, C.byref(batch), None, None, 0.0, None) == b.ODB_ERR_ARG
     assert lib.odb_paged_status(None, None) == b.ODB_ERR_ARG and lib.odb_paged_destroy(None) == b.ODB_OK
     assert C.sizeof(b.odb_paged_config) == 6 * 4 and C.sizeof(b.odb_paged_batch) == 4 * 4 + 10 * C.sizeof(C.c_void_p)
+    assert C.sizeof(b.odb_paged_rows) == 10 * 8 and C.sizeof(b.odb_rope) == 24
 
 
 def test_division_by_a_product():
