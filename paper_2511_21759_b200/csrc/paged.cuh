@@ -65,6 +65,7 @@ struct PagedAttnArgs {
     long long q_stride, out_stride;
     const int32_t *table, *len, *first, *row_start;
     int n_seqs, max_rows, H, KV, G, page_shift, n_pages, table_stride;
+    const unsigned short* pool;                           // bf16 [pool_rows][hd]
     int k_row0, v_row0, pool_rows;                        // rows of hd values of the whole pool: this layer's K, its V, all of them
     int left, right, sinks;
     float scale_log2;                                     // softmax scale x log2(e)
@@ -416,29 +417,12 @@ __device__ __forceinline__ uint32_t paged_bf16x2(float a, float b) {
 __device__ __forceinline__ size_t paged_part(const PagedAttnArgs& a, int cta, bool begins) {
     return (static_cast<size_t>(cta) * kPagedMaxParts + (begins ? 1 : 0)) * a.part_rows;
 }
-// Parts of RB rows (r0, r0 + step ..) of an item that begins in CTA c0, added up in the order of the CTAs with a running maximum;
-// all rows' loads of several parts are in flight together.
-template <int HD, int RB>
+// The parts of row r of an item that begins in CTA c0, added up in the order of the CTAs.
+template <int HD>
 struct PagedSum {
     static constexpr int V = HD / 32;                // dims of a lane
-    float M[RB], L[RB], acc[RB][V];
+    float M = -INFINITY, L = 0.f, acc[V] = {};
 
-    __device__ __forceinline__ PagedSum() {
-#pragma unroll
-        for (int k = 0; k < RB; ++k) {
-            M[k] = -INFINITY;
-            L[k] = 0.f;
-#pragma unroll
-            for (int j = 0; j < V; ++j) acc[k][j] = 0.f;
-        }
-    }
-    __device__ __forceinline__ void add(int k, float m, float l, const float (&x)[V]) {
-        const float top = fmaxf(M[k], m), f = paged_weight(M[k], top), e = paged_weight(m, top);
-        M[k] = top;
-        L[k] = L[k] * f + l * e;
-#pragma unroll
-        for (int j = 0; j < V; ++j) acc[k][j] = acc[k][j] * f + x[j] * e;
-    }
     __device__ __forceinline__ void load(const float* p, float (&x)[V]) const {
         if constexpr (V == 4) {
             const float4 t = __ldcg(reinterpret_cast<const float4*>(p));
@@ -450,7 +434,6 @@ struct PagedSum {
     }
     // One row of many parts: 32 parts' maxima and sums at once, one a lane, then their outputs, sixteen in flight.
     __device__ __forceinline__ void row(const PagedAttnArgs& a, int c0, int c1, int r) {
-        static_assert(RB == 1, "one row");
         const int lane = threadIdx.x & 31;
         for (int c = c0; c <= c1; c += 32) {
             const int n = min(32, c1 + 1 - c), mine = c + min(lane, n - 1);
@@ -458,15 +441,15 @@ struct PagedSum {
             float top = ml.x;
 #pragma unroll
             for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-            top = fmaxf(top, M[0]);
-            const float w = lane < n ? paged_weight(ml.x, top) : 0.f, f = paged_weight(M[0], top);
+            top = fmaxf(top, M);
+            const float w = lane < n ? paged_weight(ml.x, top) : 0.f, f = paged_weight(M, top);
             float l = w * ml.y;
 #pragma unroll
             for (int d = 16; d >= 1; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-            M[0] = top;
-            L[0] = L[0] * f + l;
+            M = top;
+            L = L * f + l;
 #pragma unroll
-            for (int j = 0; j < V; ++j) acc[0][j] *= f;
+            for (int j = 0; j < V; ++j) acc[j] *= f;
             for (int u0 = 0; u0 < n; u0 += 16) {
                 float x[16][V];
 #pragma unroll
@@ -479,43 +462,20 @@ struct PagedSum {
                     const float e = __shfl_sync(0xffffffffu, w, (u0 + u) & 31);   // zero behind the last
                     if (u0 + u < n)
 #pragma unroll
-                        for (int j = 0; j < V; ++j) acc[0][j] += e * x[u][j];
+                        for (int j = 0; j < V; ++j) acc[j] += e * x[u][j];
                 }
-            }
-        }
-    }
-    __device__ __forceinline__ void parts(const PagedAttnArgs& a, int c0, int from, int to, int r0, int step, int rows) {   // CTAs [from, to)
-        const int lane = threadIdx.x & 31;
-        constexpr int CU = 8 / RB;                   // parts in flight
-        for (int c = from; c < to; c += CU) {
-            float2 ml[CU][RB];
-            float x[CU][RB][V];
-#pragma unroll
-            for (int u = 0; u < CU; ++u)
-#pragma unroll
-                for (int k = 0; k < RB; ++k) {
-                    const int cta = min(c + u, to - 1);
-                    const size_t slot = paged_part(a, cta, cta == c0) + min(r0 + k * step, rows - 1);
-                    ml[u][k] = __ldcg(reinterpret_cast<const float2*>(a.part_ml + slot * 2));
-                    load(a.part_o + slot * HD + lane * V, x[u][k]);
-                }
-#pragma unroll
-            for (int u = 0; u < CU; ++u) {
-                if (c + u >= to) break;
-#pragma unroll
-                for (int k = 0; k < RB; ++k) add(k, ml[u][k].x, ml[u][k].y, x[u][k]);
             }
         }
     }
     // output of packed row idx of the request whose rows begin at row0
-    __device__ __forceinline__ void write(const PagedAttnArgs& a, int k, int row0, int head, int idx) const {
+    __device__ __forceinline__ void write(const PagedAttnArgs& a, int row0, int head, int idx) const {
         const int lane = threadIdx.x & 31, i = a.by_group(idx), h = head * a.G + idx - i * a.G;
         const size_t row = static_cast<size_t>(row0 + i);
-        const float inv = L[k] == 0.f ? 0.f : 1.0f / L[k];
+        const float inv = L == 0.f ? 0.f : 1.0f / L;
         uint32_t* op = reinterpret_cast<uint32_t*>(a.out + row * a.out_stride + h * HD + lane * V);
 #pragma unroll
-        for (int j = 0; j < V; j += 2) op[j / 2] = paged_bf16x2(acc[k][j] * inv, acc[k][j + 1] * inv);
-        if (a.lse && lane == 0) a.lse[row * a.H + h] = paged_lse(M[k], L[k]);
+        for (int j = 0; j < V; j += 2) op[j / 2] = paged_bf16x2(acc[j] * inv, acc[j + 1] * inv);
+        if (a.lse && lane == 0) a.lse[row * a.H + h] = paged_lse(M, L);
     }
 };
 

@@ -213,6 +213,7 @@ int32_t odb_paged_attention(odb_paged* h, int32_t layer, const odb_paged_batch* 
     a.table = b->table; a.len = b->len_after; a.first = b->first; a.row_start = b->row_start;
     a.n_seqs = b->n_seqs; a.max_rows = b->max_rows; a.H = c.n_heads; a.KV = c.n_kv_heads; a.G = G;
     a.page_shift = h->page_shift; a.n_pages = c.n_pages; a.table_stride = b->table_stride;
+    a.pool = reinterpret_cast<const unsigned short*>(h->kv);
     a.k_row0 = 2 * layer * h->layer_rows; a.v_row0 = a.k_row0 + h->layer_rows; a.pool_rows = h->pool_rows;
     a.left = left < 0 || left > kPagedUnlimited ? kPagedUnlimited : left;
     a.right = right < 0 || right > kPagedUnlimited ? kPagedUnlimited : right;

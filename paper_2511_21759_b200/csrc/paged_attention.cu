@@ -480,9 +480,9 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
             mma_warps_barrier();
             if (sh->last) {
                 for (int r = warp; r < rows; r += kMmaWarps) {
-                    PagedSum<HD, 1> sum;
+                    PagedSum<HD> sum;
                     sum.row(a, c0, c1, r);
-                    sum.write(a, 0, w.q.row0, w.head, w.rt * kRows + r);
+                    sum.write(a, w.q.row0, w.head, w.rt * kRows + r);
                 }
                 mma_warps_barrier();                             // sh->last has been read by all
             }

@@ -26,7 +26,7 @@ constexpr int kTQ = 128;   // packed rows of a Q tile (MMA M)
 constexpr int kKT = 64;    // keys of a tile
 template <int QT> constexpr int kLoaders = QT;   // one warp for K and V, or one each (the SM has room for a twelfth warp, two CTAs' registers not for two more)
 template <int QT> constexpr int kThreads = 32 * (5 * QT + kLoaders<QT>);   // four softmax warps and an MMA warp a Q tile
-constexpr int kItem = 4;   // key tiles that an item costs beside its own
+constexpr int kItem = 3;   // key tiles that an item costs beside its own
 template <int HD> constexpr uint32_t kQBytes = kTQ * HD * 2;
 template <int HD> constexpr uint32_t kTileBytes = kKT * HD * 2;
 // Q buffers: with two the next item's Q tiles and first scores are there when an item ends; the larger Q tiles of two CTAs on an SM
@@ -35,7 +35,7 @@ template <int HD, int QT> constexpr int kQBufs = HD == 128 && QT == 1 ? 1 : 2;
 template <int HD, int QT> constexpr int kKSlots = HD == 128 ? 3 : (QT == 1 ? 5 : 8);
 template <int HD, int QT> constexpr int kVSlots = HD == 128 ? (QT == 1 ? 2 : 3) : (QT == 1 ? 5 : 8);
 template <int HD, int QT>
-constexpr uint32_t kSmem = kQBufs<HD, QT> * QT * kQBytes<HD> + (kKSlots<HD, QT> + kVSlots<HD, QT>) * kTileBytes<HD> + 512;
+constexpr uint32_t kSmem = kQBufs<HD, QT> * QT * kQBytes<HD> + (kKSlots<HD, QT> + kVSlots<HD, QT>) * kTileBytes<HD> + 1024;
 template <int HD> constexpr int kBufs = HD == 128 ? 2 : 3;   // S / P buffers of a Q tile: 256 columns, of which O takes HD
 constexpr uint32_t kCols = 256;
 constexpr uint32_t kPatch = 4096;                            // per softmax warp, in the Q tile: 32 rows x 128 bytes of output
@@ -43,6 +43,7 @@ constexpr uint32_t kPatch = 4096;                            // per softmax warp
 struct alignas(8) Shared {
     uint64_t q_full[2];                // an item's Q tiles landed in the buffer          (loader -> MMA)
     uint64_t k_full[8], v_full[8];     // K or V tile landed in the ring's slot           (loader -> MMA, softmax)
+    uint64_t v_seen[8];                // V at keys that not all rows see has been looked at (loader -> softmax)
     uint64_t k_empty[8], v_empty[8];   // the MMAs have read the slot                     (MMA -> loader, QT arrivals)
     uint64_t s_full[2][3];             // S of Q tile g into buffer i has completed       (MMA -> softmax)
     uint64_t p_full[2][3];             // P has taken its place                           (softmax -> MMA, 4 arrivals)
@@ -51,31 +52,23 @@ struct alignas(8) Shared {
     uint64_t item_done[2];             // the Q buffer may be overwritten                 (softmax -> loader, 4 QT arrivals)
     uint32_t tmem_base;
     int abort, keep_o[2];
+    int odd[8];                        // V in the slot has values that are not finite where only some rows see them
 };
-static_assert(sizeof(Shared) <= 512, "the barriers end inside the allocation");
-
-// whether any softmax thread of the CTA says so
-template <int QT>
-__device__ __forceinline__ bool softmax_any(bool x) {
-    int r;
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t"
-        "setp.ne.b32 p, %1, 0;\n\t"
-        "barrier.cta.red.or.pred q, 1, %2, p;\n\t"
-        "selp.b32 %0, 1, 0, q;\n\t}"
-        : "=r"(r)
-        : "r"(static_cast<int>(x)), "r"(128 * QT)
-        : "memory");
-    return r != 0;
-}
-template <int QT>
-__device__ __forceinline__ void softmax_barrier() { asm volatile("bar.sync 1, %0;" ::"r"(128 * QT) : "memory"); }
+static_assert(sizeof(Shared) <= 1024, "the barriers end inside the allocation");
 
 __device__ __forceinline__ void tma_box_3d(uint32_t dst, const CUtensorMap* tmap, uint64_t* bar, int c0, int c1, int c2) {
     asm volatile(
         "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
         "l"(reinterpret_cast<uint64_t>(tmap)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
         : "memory");
+}
+__device__ __forceinline__ void tma_store_box_3d(const CUtensorMap* tmap, uint32_t src, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(reinterpret_cast<uint64_t>(tmap)), "r"(src),
+                 "r"(c0), "r"(c1), "r"(c2)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_prefetch_map(const CUtensorMap* tmap) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tmap)) : "memory");
 }
 // The products with descriptors as their low words (address, and what stands below bit 32) and the high word that all tiles here
 // share: one 32-bit addition from product to product.
@@ -158,6 +151,21 @@ __device__ __forceinline__ void tmem_st1(uint32_t taddr, uint32_t v) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};\n\ttcgen05.wait::st.sync.aligned;" ::"r"(taddr), "r"(v) : "memory");
 }
 __device__ __forceinline__ bool not_finite(uint32_t bf) { return (bf & 0x7f80u) == 0x7f80u; }
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+// Keys from lo on and below hi are seen by all of the query rows tok .. tok + n - 1 of a request.
+struct SeenByAll {
+    int lo, hi;
+    __device__ __forceinline__ SeenByAll(const PagedAttnArgs& a, const PagedSeq& q, int tok, int n)
+        : lo(static_cast<int>(max(-1ll, static_cast<long long>(q.first) + tok + n - 1 - a.left))),
+          hi(static_cast<int>(max(0ll, min(static_cast<long long>(q.len), static_cast<long long>(q.first) + tok + a.right + 1)))) {}
+    // the tile from k0 on
+    __device__ __forceinline__ bool tile(const PagedAttnArgs& a, int k0) const { return k0 + kKT <= hi && (k0 >= lo || k0 + kKT <= a.sinks); }
+};
 
 // Turns of the two Q tiles' softmax warps gw: Q tile 0 first.
 __device__ __forceinline__ void turn_begin(int g, int gw) { asm volatile("bar.sync %0, 64;" ::"r"(2 + 4 * g + gw) : "memory"); }
@@ -174,7 +182,7 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16
 template <int HD, int QT>
 __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
     paged_attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_rows,
-                              const __grid_constant__ CUtensorMap tm_atoms, const PagedAttnArgs a) {
+                              const __grid_constant__ CUtensorMap tm_atoms, const __grid_constant__ CUtensorMap tm_out, const PagedAttnArgs a) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     constexpr int NQ = kQBufs<HD, QT>, KS = kKSlots<HD, QT>, VS = kVSlots<HD, QT>, kB = kBufs<HD>, kFirst = kB - 1, kAtoms = HD / 64;
     constexpr uint32_t kT = kTileBytes<HD>;
@@ -193,6 +201,8 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
         return;
     }
     if (tid == 0) {
+        tma_prefetch_map(&tm_q);
+        tma_prefetch_map(a.page_shift >= 6 ? &tm_rows : &tm_atoms);
         for (int i = 0; i < NQ; ++i) {
             mbar_init(&sh->q_full[i], 1);
             mbar_init(&sh->item_done[i], kSoftmaxWarps);
@@ -203,6 +213,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
         }
         for (int i = 0; i < VS; ++i) {
             mbar_init(&sh->v_full[i], 1);
+            mbar_init(&sh->v_seen[i], 1);
             mbar_init(&sh->v_empty[i], QT);
         }
         for (int g = 0; g < QT; ++g) {
@@ -229,7 +240,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
     pdl_wait();
 
     PagedStart start;
-    static_assert(sizeof(PagedScratch) <= kSmem<64, 1> - 512, "the scratch fits the tiles");
+    static_assert(sizeof(PagedScratch) <= kSmem<64, 1> - 1024, "the scratch fits the tiles");
     const bool any = paged_find_start<kThreads<QT>, kKT, kItem>(a, *reinterpret_cast<PagedScratch*>(sQ), 1, kItem + 2, 0, start);
     proxy_fence();                                          // the scratch's writes before the copies that take its place
     __syncthreads();
@@ -262,6 +273,42 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
         k.at = __shfl_sync(0xffffffffu, smem_u32(sK), 0); v.at = __shfl_sync(0xffffffffu, smem_u32(sV), 0);
         k.full = sh->k_full; k.empty = sh->k_empty;
         v.full = sh->v_full; v.empty = sh->v_empty;
+        // V in places that a row does not see: zero where no row sees it, and values that are not finite where some do, which the softmax
+        // warps add to O of the rows that see them.  Here, once the tile has landed: nobody waits for it on the way.
+        auto look = [&](const Tiles& x, int k0) {
+            if (!SeenByAll(a, x.w.q, x.w.rt * QT * a.tile_tokens, QT * a.tile_tokens).tile(a, k0)) {
+                ok = all_wait(&x.full[x.slot], x.ph ^ 1u);
+                if (!ok) return;
+                const uint32_t vt = x.at + x.slot * kT;
+                uint32_t top = 0;                               // largest magnitudes of both halves of the words
+#pragma unroll 8
+                for (uint32_t off = lane * 16; off < kT; off += 512) {
+                    const int key = k0 + ((off >> 7) & (kKT - 1));
+                    const bool hidden = key >= x.w.k.hi || (key < x.w.k.lo && key >= a.sinks);
+                    uint32_t v[4];
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(vt + off) : "memory");
+                    uint32_t m = 0;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) m = max_u16x2(m, v[j] & 0x7fff7fffu);
+                    if (hidden) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(vt + off), "r"(0) : "memory");
+                    else top = max_u16x2(top, m);
+                }
+                const bool odd = __any_sync(0xffffffffu, not_finite(top) || not_finite(top >> 16));
+                if (odd) {                                      // rare
+#pragma unroll 1
+                    for (uint32_t off = lane * 2; off < kT; off += 64) {
+                        unsigned short bits;
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(bits) : "r"(vt + off) : "memory");
+                        if (not_finite(bits)) asm volatile("st.shared.u16 [%0], %1;" ::"r"(vt + off), "h"(static_cast<unsigned short>(0)) : "memory");
+                    }
+                }
+                if (lane == 0) *const_cast<volatile int*>(&sh->odd[x.slot]) = odd;
+                proxy_fence();
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh->v_seen[x.slot]);
+            __syncwarp();
+        };
         // pages of 64 rows and more: a copy a tile; smaller ones: a copy per page and 64 values, in their places of the operand layout
         auto load = [&](Tiles& x) {
             if (!ok || !x.have) return;
@@ -290,6 +337,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                     __syncwarp();
                 }
             }
+            if (x.full == sh->v_full) look(x, k0);
             ++x.issued;
             if (++x.slot == static_cast<uint32_t>(x.slots)) { x.slot = 0; x.ph ^= 1u; }
             if (++x.t == x.w.t1) {
@@ -447,16 +495,22 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
         const uint64_t scale2 = pack2f(a.scale_log2, a.scale_log2);
         bool ok = true;
         uint32_t item = 0, done = 0;                             // key tiles of the items before
+        bool storing = false;                                    // the last item's output is on its way from the Q tile's place
+        auto q_free = [&]() {                                    // it has left that place
+            if (!storing) return;
+            if (lane == 0) {
+                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                mbar_arrive(&sh->item_done[(item - 1) % NQ]);
+            }
+            __syncwarp();
+            storing = false;
+        };
         if (QT == 2 && g == 1) turn_end(1, gw);
         do {
             const int n = w.t1 - w.t0;
             const int tok0 = (w.rt * QT + g) * a.tile_tokens;    // the Q tile's first query row
             const int pos = w.q.first + tok0 + a.by_group(min(r, rows_g - 1));
-            // keys from .._lo on and below .._hi are seen by all rows of the Q tile, of the item
-            auto low = [&](int tok) { return static_cast<int>(max(-1ll, static_cast<long long>(w.q.first) + tok - a.left)); };
-            auto high = [&](int tok) { return static_cast<int>(max(0ll, min(static_cast<long long>(w.q.len), static_cast<long long>(w.q.first) + tok + a.right + 1))); };
-            const int all_lo = low(tok0 + a.tile_tokens - 1), all_hi = high(tok0);
-            const int item_lo = low((w.rt + 1) * QT * a.tile_tokens - 1), item_hi = high(w.rt * QT * a.tile_tokens);
+            const SeenByAll by_tile(a, w.q, tok0, a.tile_tokens), by_item(a, w.q, w.rt * QT * a.tile_tokens, QT * a.tile_tokens);
             const int left = min(rows_g, (w.q.n - tok0) * a.G);          // rows of the Q tile (may be negative); others hold anything
             const bool mine = r < left;
             float M_row = -INFINITY, l_row = 0.f;
@@ -473,7 +527,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                 const uint32_t ts = s_base + b * kKT;
                 tmem_got64(sv);
                 unsigned long long mask = ~0ull;                         // the keys of the tile that the row sees
-                if (care && !(k0 + kKT <= all_hi && (k0 >= all_lo || k0 + kKT <= a.sinks))) {
+                if (care && !by_tile.tile(a, k0)) {
                     auto below = [](long long x) { return x >= 64 ? ~0ull : x <= 0 ? 0ull : (1ull << x) - 1ull; };
                     mask = below(min(static_cast<long long>(w.q.len), static_cast<long long>(pos) + a.right + 1) - k0) &
                            (~below(static_cast<long long>(pos) - a.left - k0) | below(static_cast<long long>(a.sinks) - k0));
@@ -547,28 +601,11 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                 const float2 s0 = unpack2f(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
                 l_row += s0.x + s0.y;
                 if (care) {
-                    // V in places that a row does not see, once it has landed.  The parity is not ambiguous: the tile before it in this
-                    // slot was multiplied before S(t) was, the one behind it waits for P V(t).
+                    // The parity is not ambiguous: the tile before it in this slot was multiplied before S(t) was, the one behind it waits
+                    // for P V(t).
                     const uint32_t slot = gt % VS;
-                    ok = __all_sync(0xffffffffu, wait(&sh->v_full[slot], (gt / VS) & 1u)) && ok;
-                    const uint32_t vt = smem_u32(sV) + slot * kT;
-                    bool odd = false;
-#pragma unroll
-                    for (int at = 0; at < kAtoms; ++at)
-                        for (uint32_t off = tid * 16; off < kKT * 128; off += 128 * QT * 16) {
-                            const int key = k0 + (off >> 7);
-                            uint32_t v[4];
-                            if (key >= w.k.hi || (key < w.k.lo && key >= a.sinks)) {
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(vt + at * kKT * 128 + off), "r"(0) : "memory");
-                            } else {
-                                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(vt + at * kKT * 128 + off) : "memory");
-#pragma unroll
-                                for (int j = 0; j < 4; ++j) odd = odd || not_finite(v[j]) || not_finite(v[j] >> 16);
-                            }
-                        }
-                    proxy_fence();
-                    const bool given = softmax_any<QT>(odd);             // all have looked and cleared: they share the V tile
-                    if (given) {                                         // rare: values of V are added to O here
+                    ok = __all_sync(0xffffffffu, wait(&sh->v_seen[slot], (gt / VS) & 1u)) && ok;
+                    if (ok && *const_cast<volatile int*>(&sh->odd[slot])) {   // rare: values of V, from the pool, are added to O here
                         if (t > 0) ok = __all_sync(0xffffffffu, wait(&sh->pv_done[g][(gt - 1) & 1u], ((gt - 1) >> 1) & 1u)) && ok;
                         tc_fence_after();
                         tmem_wait_st();
@@ -580,26 +617,24 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                             for (int c = 0; c < HD / 16; ++c) tmem_st16(o_base + c * 16, z);
                             tmem_wait_st();
                         }
+                        PagedPages pages;
 #pragma unroll 1
-                        for (int e = 0; e < kKT * HD; ++e) {
-                            const int key = e / HD, d = e % HD;
-                            unsigned short bits;
-                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(bits)
-                                         : "r"(vt + (d >> 6) * kKT * 128 + key * 128 + ((((d >> 3) & 7) ^ (key & 7)) << 4) + (d & 7) * 2) : "memory");
-                            if (!not_finite(bits)) continue;             // the same for all lanes
-                            const uint32_t p2 = tmem_ld1(ts + key / 2);
-                            const float p = __uint_as_float(key & 1 ? p2 & 0xffff0000u : p2 << 16), o = __uint_as_float(tmem_ld1(o_base + d));
-                            tmem_st1(o_base + d, __float_as_uint((mask >> key) & 1ull ? o + p * __uint_as_float(static_cast<uint32_t>(bits) << 16) : o));
-                        }
-                        softmax_barrier<QT>();
+                        for (int e = 0; e < kKT; ++e) {
+                            const int key = k0 + e;
+                            if (key >= w.k.hi || (key < w.k.lo && key >= a.sinks)) continue;
+                            const int row = pages.row(a, w.seq, w.head, key, a.v_row0);
+                            if (row >= a.pool_rows) continue;
+                            const unsigned short* v = a.pool + static_cast<size_t>(row) * HD;
+                            const uint32_t p2 = tmem_ld1(ts + e / 2);
+                            const float p = __uint_as_float(e & 1 ? p2 & 0xffff0000u : p2 << 16);
 #pragma unroll 1
-                        for (uint32_t off = tid * 2; off < kT; off += 128 * QT * 2) {
-                            unsigned short bits;
-                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(bits) : "r"(vt + off) : "memory");
-                            if (not_finite(bits)) asm volatile("st.shared.u16 [%0], %1;" ::"r"(vt + off), "h"(static_cast<unsigned short>(0)) : "memory");
+                            for (int d = 0; d < HD; ++d) {
+                                const uint32_t bits = v[d];
+                                if (!not_finite(bits)) continue;             // the same for all lanes
+                                const float o = __uint_as_float(tmem_ld1(o_base + d));
+                                tmem_st1(o_base + d, __float_as_uint((mask >> e) & 1ull ? o + p * __uint_as_float(bits << 16) : o));
+                            }
                         }
-                        proxy_fence();
-                        softmax_barrier<QT>();
                         if (t == 0 && r == 0) sh->keep_o[g] = 1;
                     }
                 }
@@ -615,16 +650,52 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
             ask(0);
             for (int t = 0; t < n; ++t) {
                 const int k0 = w.k.tile(w.t0 + t) << 6;
-                tile(!(k0 + kKT <= item_hi && (k0 >= item_lo || k0 + kKT <= a.sinks)), t, k0);
+                tile(!by_item.tile(a, k0), t, k0);
+                if (t == 0) q_free();
             }
             done += n;
             const float m_log2 = M_row == -INFINITY ? 0.f : M_row;      // the shift the row's sum and output carry
             ok = __all_sync(0xffffffffu, wait(&sh->o_full[g], item & 1u)) && ok;
             tc_fence_after();
             const int row_w = gw * 32;                                   // the warp's first row of the Q tile
-            const uint32_t patch = smem_u32(sQ) + ((item % NQ) * QT + g) * kQBytes<HD> + gw * kPatch;   // every MMA that reads this Q tile has completed
+            const uint32_t place = smem_u32(sQ) + ((item % NQ) * QT + g) * kQBytes<HD>;   // every MMA that reads this Q tile has completed
+            const uint32_t patch = place + gw * kPatch;
             const bool final = w.whole();
-            if (final) {
+            const float inv = l_row == 0.f ? 0.f : 1.0f / l_row;
+            if (final && a.lse && row_w + lane < left) {
+                const int idx = row_w + lane, i = a.by_group(idx);
+                a.lse[static_cast<size_t>(w.q.row0 + tok0 + i) * a.H + w.head * a.G + idx - i * a.G] = paged_lse(m_log2, l_row);
+            }
+            // 64 values of the row as pairs of bf16
+            auto result = [&](int c, uint32_t (&x)[32]) {
+                uint32_t v[64];
+                tmem_ld64(o_base + c * 64, v);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) x[j] = paged_bf16x2(__uint_as_float(v[2 * j]) * inv, __uint_as_float(v[2 * j + 1]) * inv);
+                if (l_row == 0.f)                                        // no visible key: whatever O holds
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) x[j] = 0u;
+            };
+            if (final && left == rows_g) {                               // a Q tile without gaps: stored as it was loaded
+#pragma unroll 1
+                for (int c = 0; c < HD / 64; ++c) {
+                    uint32_t x[32];
+                    result(c, x);
+#pragma unroll
+                    for (int ch = 0; ch < 8; ++ch)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(place + c * kTQ * 128 + r * 128 + ((ch ^ (r & 7)) << 4)), "r"(x[4 * ch]),
+                                     "r"(x[4 * ch + 1]), "r"(x[4 * ch + 2]), "r"(x[4 * ch + 3])
+                                     : "memory");
+                }
+                proxy_fence();
+                asm volatile("bar.sync %0, 128;" ::"r"(10 + g) : "memory");
+                if (gw == 0 && lane == 0) {
+#pragma unroll
+                    for (int c = 0; c < kAtoms; ++c) tma_store_box_3d(&tm_out, place + c * kTQ * 128, 64 * c, w.head * a.G, w.q.row0 + tok0);
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                }
+                storing = gw == 0;
+            } else if (final) {
                 int at[8];                                               // head of rows lane / 8, lane / 8 + 4 .. of the warp, from the Q tile's first
 #pragma unroll
                 for (int it = 0; it < 8; ++it) {
@@ -632,27 +703,19 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                     at[it] = i * static_cast<int>(a.out_stride / 8) + (idx - i * a.G) * (HD / 8);
                 }
                 uint4* out = reinterpret_cast<uint4*>(a.out + static_cast<size_t>(w.q.row0 + tok0) * a.out_stride + w.head * a.G * HD);
-                const float inv = l_row == 0.f ? 0.f : 1.0f / l_row;
-                if (a.lse && row_w + lane < left) {
-                    const int idx = row_w + lane, i = a.by_group(idx);
-                    a.lse[static_cast<size_t>(w.q.row0 + tok0 + i) * a.H + w.head * a.G + idx - i * a.G] = paged_lse(m_log2, l_row);
-                }
 #pragma unroll 1
                 for (int c = 0; c < HD / 64; ++c) {
-                    uint32_t v[64], x[32];
-                    tmem_ld64(o_base + c * 64, v);
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) x[j] = paged_bf16x2(__uint_as_float(v[2 * j]) * inv, __uint_as_float(v[2 * j + 1]) * inv);
-                    if (l_row == 0.f)                                    // no visible key: whatever O holds
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) x[j] = 0u;
+                    uint32_t x[32];
+                    result(c, x);
                     turn_rows(patch, lane, x, [&](int rr, int ch, const uint4& y) {
                         if (row_w + rr < left) out[at[rr >> 2] + c * 8 + ch] = y;
                     });
                 }
             } else {
-                const size_t pr = paged_part(a, blockIdx.x, w.t0 == 0) + g * rows_g + row_w;
-                if (row_w + lane < left) *reinterpret_cast<float2*>(a.part_ml + (pr + lane) * 2) = make_float2(m_log2, l_row);
+                // [16 bytes of a row][row]: a warp's store is 512 bytes in one piece, and so is a load of the kernel that adds up
+                const size_t part = paged_part(a, blockIdx.x, w.t0 == 0) + g * kTQ;
+                float* po = a.part_o + part * HD + r * 4;
+                if (r < left) *reinterpret_cast<float2*>(a.part_ml + (part + r) * 2) = make_float2(M_row, l_row);
 #pragma unroll 1
                 for (int c = 0; c < HD / 32; ++c) {
                     uint32_t v[32];
@@ -660,15 +723,16 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                     if (l_row == 0.f)
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] = 0u;
-                    turn_rows(patch, lane, v, [&](int rr, int ch, const uint4& y) {
-                        if (row_w + rr < left) *reinterpret_cast<uint4*>(a.part_o + (pr + rr) * HD + c * 32 + ch * 4) = y;
-                    });
+                    if (r < left)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            *reinterpret_cast<uint4*>(po + (c * 8 + j) * kTQ * 4) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
                 }
             }
             proxy_fence();                                               // the patches before the next Q
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sh->item_done[item % NQ]);
+            if (!storing && lane == 0) mbar_arrive(&sh->item_done[item % NQ]);
             if (!final && w.t0 == 0 && tid == 0) {
                 PagedShared& d = a.shared[blockIdx.x];
                 d.row0 = w.q.row0;
@@ -678,7 +742,9 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                 d.rows = min(a.tile_rows, w.q.n * a.G - w.rt * a.tile_rows);
             }
             ++item;
+            if (NQ == 1) q_free();                               // the next item's Q tile has no other place
         } while (w.next());
+        if (gw == 0 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         if (QT == 2 && g == 0) turn_begin(0, gw);                // the other's last word
     }
     tc_fence_before();
@@ -690,34 +756,67 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
     }
 }
 
-// Adds up the parts of the items that several CTAs share: 16 rows a block, two at a time a warp, few registers, so that the blocks of
-// all items are on the SMs at once and one latency after the other is hidden.  (By the last CTA of an item, which alone has too few
-// loads in flight, up to 27 us for 128 rows of five parts; in blocks of 32 rows with eight at a time, two to a wave, 12 us.)
-constexpr int kMergeRows = 16;
+// Adds up the parts of the items that several CTAs share, in the order of the CTAs with a running maximum: a thread takes kMergeDims
+// values of a row, a block the rows of a Q tile, eight parts in flight.
+constexpr int kMergeDims = 8;
 template <int HD>
-__global__ void __launch_bounds__(128, 8) paged_merge_kernel(const PagedAttnArgs a) {
+__global__ void __launch_bounds__(kTQ) paged_merge_kernel(const PagedAttnArgs a) {
     pdl_launch_dependents();
     pdl_wait();
     const PagedShared d = a.shared[blockIdx.x];
-#pragma unroll 1
-    for (int r0 = blockIdx.y * kMergeRows + (threadIdx.x >> 5); r0 < min(d.rows, static_cast<int>(blockIdx.y + 1) * kMergeRows); r0 += 8) {
-        PagedSum<HD, 2> sum;
-        sum.parts(a, blockIdx.x, blockIdx.x, d.last_cta + 1, r0, 4, d.rows);
+    const int g = blockIdx.y / (HD / kMergeDims), dim0 = blockIdx.y % (HD / kMergeDims) * kMergeDims, r = threadIdx.x;
+    const int rows_g = a.tile_tokens * a.G, at = g * rows_g + r;
+    if (r >= rows_g || at >= d.rows) return;
+    float M = -INFINITY, L = 0.f, acc[kMergeDims];
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-            if (r0 + 4 * k < d.rows) sum.write(a, k, d.row0, d.head, d.first_idx + r0 + 4 * k);
+    for (int j = 0; j < kMergeDims; ++j) acc[j] = 0.f;
+    constexpr int kU = 8;
+    for (int c = blockIdx.x; c <= d.last_cta; c += kU) {
+        float2 ml[kU];
+        float4 x[kU][kMergeDims / 4];
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            if (c + u > d.last_cta) break;
+            const size_t part = paged_part(a, c + u, c + u == static_cast<int>(blockIdx.x)) + g * kTQ;
+            ml[u] = __ldcg(reinterpret_cast<const float2*>(a.part_ml + (part + r) * 2));
+#pragma unroll
+            for (int j = 0; j < kMergeDims / 4; ++j) x[u][j] = __ldcg(reinterpret_cast<const float4*>(a.part_o + part * HD + ((dim0 / 4 + j) * kTQ + r) * 4));
+        }
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            if (c + u > d.last_cta) break;
+            const float top = fmaxf(M, ml[u].x), f = paged_weight(M, top), e = paged_weight(ml[u].x, top);
+            M = top;
+            L = L * f + ml[u].y * e;
+#pragma unroll
+            for (int j = 0; j < kMergeDims / 4; ++j) {
+                acc[4 * j] = acc[4 * j] * f + x[u][j].x * e;
+                acc[4 * j + 1] = acc[4 * j + 1] * f + x[u][j].y * e;
+                acc[4 * j + 2] = acc[4 * j + 2] * f + x[u][j].z * e;
+                acc[4 * j + 3] = acc[4 * j + 3] * f + x[u][j].w * e;
+            }
+        }
     }
+    const int idx = d.first_idx + at, i = a.by_group(idx), h = d.head * a.G + idx - i * a.G;
+    const size_t row = static_cast<size_t>(d.row0 + i);
+    const float inv = L == 0.f ? 0.f : 1.0f / L;
+    uint32_t o[kMergeDims / 2];
+#pragma unroll
+    for (int j = 0; j < kMergeDims / 2; ++j) o[j] = paged_bf16x2(acc[2 * j] * inv, acc[2 * j + 1] * inv);
+    static_assert(kMergeDims == 8, "a store of 16 bytes");
+    *reinterpret_cast<uint4*>(a.out + row * a.out_stride + h * HD + dim0) = make_uint4(o[0], o[1], o[2], o[3]);
+    if (a.lse && dim0 == 0) a.lse[row * a.H + h] = paged_lse(M, L);
 }
 
 template <int HD, int QT>
-cudaError_t launch(const PagedAttnArgs& a, const CUtensorMap& tm_q, const PagedMaps& maps, cudaStream_t st) {
+cudaError_t launch(const PagedAttnArgs& a, const CUtensorMap& tm_q, const CUtensorMap& tm_out, const PagedMaps& maps, cudaStream_t st) {
     static std::atomic<unsigned long long> attr_done{0};
     cudaError_t e = set_smem_limit_once(attr_done, paged_attention_tc_kernel<HD, QT>, static_cast<int>(kSmem<HD, QT>));
     if (e != cudaSuccess) return e;
     const dim3 grid(a.at_once);
-    e = launch_kernel(paged_attention_tc_kernel<HD, QT>, grid, dim3(kThreads<QT>), kSmem<HD, QT>, st, tm_q, maps.rows, maps.atoms, a);
+    e = launch_kernel(paged_attention_tc_kernel<HD, QT>, grid, dim3(kThreads<QT>), kSmem<HD, QT>, st, tm_q, maps.rows, maps.atoms, tm_out, a);
     if (e != cudaSuccess) return e;
-    return launch_kernel(paged_merge_kernel<HD>, dim3(grid.x, QT * kTQ / kMergeRows), dim3(128), 0, st, a);
+    return launch_kernel(paged_merge_kernel<HD>, dim3(grid.x, QT * HD / kMergeDims), dim3(kTQ), 0, st, a);
 }
 
 }  // namespace
@@ -731,11 +830,12 @@ cudaError_t launch_paged_attention_tc(PagedAttnArgs a, const PagedMaps& maps, in
     a.at_once = q_tiles == 1 ? 2 * sms : sms;
     a.by_once = PagedDiv::by(a.at_once);
     a.part_rows = q_tiles * kTQ;
-    CUtensorMap tm_q;
-    const cudaError_t e = make_group_tmap(&tm_q, a.q, a.max_rows, a.q_stride, a.H, hd, a.G, a.tile_tokens);
+    CUtensorMap tm_q, tm_out;
+    cudaError_t e = make_group_tmap(&tm_q, a.q, a.max_rows, a.q_stride, a.H, hd, a.G, a.tile_tokens);
+    if (e == cudaSuccess) e = make_group_tmap(&tm_out, a.out, a.max_rows, a.out_stride, a.H, hd, a.G, a.tile_tokens);
     if (e != cudaSuccess) return e;
-    if (q_tiles == 1) return hd == 128 ? launch<128, 1>(a, tm_q, maps, st) : launch<64, 1>(a, tm_q, maps, st);
-    return hd == 128 ? launch<128, 2>(a, tm_q, maps, st) : launch<64, 2>(a, tm_q, maps, st);
+    if (q_tiles == 1) return hd == 128 ? launch<128, 1>(a, tm_q, tm_out, maps, st) : launch<64, 1>(a, tm_q, tm_out, maps, st);
+    return hd == 128 ? launch<128, 2>(a, tm_q, tm_out, maps, st) : launch<64, 2>(a, tm_q, tm_out, maps, st);
 }
 
 }  // namespace odb

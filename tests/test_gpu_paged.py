@@ -456,6 +456,23 @@ def test_attention_of_large_scores_and_another_scale(new, D):
 
 
 @requires_gpu
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("lens,new,G", [([1500], 1500, 4), ([700, 90], 90, 1), ([2600], 30, 4), ([3000], 1, 4)])
+def test_attention_of_scores_far_below_zero_in_parts(lens, new, G, D):
+    """Rows whose scores all lie hundreds below zero, some of whose item's parts hold no key that they see."""
+    rng = np.random.default_rng(22)
+    counts = [new] * len(lens)
+    firsts = [n - new for n in lens]
+    cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, 2 * G, 2, D, 16)
+    cache.kv[:, 0].abs_()
+    for mask in (dict(right=0), dict(left=70, right=0)):
+        lse = torch.empty(len(qf), 2 * G, device="cuda")
+        out = cache.attention(0, b, q.abs(), lse=lse, scale=-8.0, **mask)
+        _check_scaled(out, lse, np.abs(qf), [np.abs(k) for k in keys], values, start, firsts, D, -8.0, **mask)
+    cache.close()
+
+
+@requires_gpu
 def test_attention_reads_strided_rows_and_other_layers_and_leaves_rows_behind_the_last():
     rng = np.random.default_rng(4)
     lens, counts, firsts = [50, 90], [2, 5], [48, 85]
