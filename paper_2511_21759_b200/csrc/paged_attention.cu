@@ -104,6 +104,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
         return;
     }
     if (tid == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tm)) : "memory");
         for (int i = 0; i < KS; ++i) {
             mbar_init(&sh->k_full[i], 1);
             mbar_init(&sh->k_empty[i], kMmaWarps);
@@ -196,6 +197,8 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                 qf[kk][2 + e] = *reinterpret_cast<const uint32_t*>(qp + kk * 16 + 8);
             }
         }
+        const bool final = w.whole();
+        const int c0 = final ? 0 : w.first_cta(), c1 = final ? 0 : w.last_cta();   // while K is on its way
         const int idx_last = w.rt * kRows + rows - 1;
         const int p_min = w.q.first + a.by_group(w.rt * kRows), p_max = w.q.first + a.by_group(idx_last);
         // keys from all_lo on and below all_hi are seen by all rows of the item
@@ -445,7 +448,6 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
         }
 
         // ---- results, or this CTA's part of them ----
-        const bool final = w.whole();
         const size_t part = paged_part(a, blockIdx.x, w.t0 == 0);
         if (warp == 0) {
 #pragma unroll
@@ -468,13 +470,13 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
             }
         }
         if (!final) {
-            __threadfence();
             mma_warps_barrier();
-            const int c0 = w.first_cta(), c1 = w.last_cta();
             if (tid == 0) {
-                const bool last = atomicAdd(a.arrivals + c0, 1u) == static_cast<unsigned>(c1 - c0);
+                // releases what the barrier has put in front of it, and acquires what the other CTAs have released
+                unsigned before;
+                asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(a.arrivals + c0) : "memory");
+                const bool last = before == static_cast<unsigned>(c1 - c0);
                 if (last) a.arrivals[c0] = 0;                    // for the next launch; an item is counted at the CTA it begins in
-                __threadfence();
                 sh->last = last;
             }
             mma_warps_barrier();
