@@ -232,11 +232,12 @@ __device__ __forceinline__ int paged_upper(const int* v, int n, int x) {   // th
     return lo;
 }
 
-// Called by all THREADS threads of the block; false: there is nothing for this CTA to do.
+// WARPS: for kernels of few rows, whose requests have a row tile each (the others only lose by the question: blocks of 32 rows
+// 47.9 -> 49.0 us).  Called by all THREADS threads of the block; false: there is nothing for this CTA to do.
 // waves: CTAs of the grid for each of the a.at_once that run at one time.  min_units: what a CTA takes at least (more than E);
 // full_units: what it takes at least as long as those have work.
 // The launcher's bounds on rows, requests and keys keep every sum below 2^31.
-template <int THREADS, int KT, int E>
+template <int THREADS, int KT, int E, bool WARPS>
 __device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int waves, int min_units, int full_units, PagedStart& st) {
     const int tid = threadIdx.x;
     auto kept = [&](int s) {          // the request's numbers, loaded once
@@ -257,6 +258,30 @@ __device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int w
         rem = st.u0 - st.head * per_head;
         return true;
     };
+    // Few requests of one row tile each: every warp by itself, a request a lane, without a barrier (577 keys 9.5 -> 9.2 us).
+    if (WARPS && a.n_seqs <= 32) {
+        const int s = tid & 31;
+        int units = 0, n_rt = 0, rem;
+        if (s < a.n_seqs) {
+            const PagedSeq q = paged_seq(a, s);
+            n_rt = q.n_rt;
+            if (n_rt > 0) units = paged_keys<KT>(a, q, 0).n + E;
+        }
+        if (!__any_sync(0xffffffffu, n_rt > 1)) {
+            int sum = units;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int x = __shfl_up_sync(0xffffffffu, sum, d);
+                if (s >= d) sum += x;
+            }
+            const int per_head = __shfl_sync(0xffffffffu, sum, 31);
+            if (per_head == 0 || !share(per_head, rem)) return false;
+            st.seq = __ffs(__ballot_sync(0xffffffffu, sum > rem)) - 1;
+            st.rt = 0;
+            st.off = rem - __shfl_sync(0xffffffffu, sum - units, st.seq);
+            return true;
+        }
+    }
     const int per_s = (a.n_seqs + THREADS - 1) / THREADS, s0 = min(tid * per_s, a.n_seqs), s1 = min(s0 + per_s, a.n_seqs);
     int n_rt, mine_rt = 0, units = 0, rem;
     bool several = false;

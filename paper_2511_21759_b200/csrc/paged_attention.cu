@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
     // the ring's memory holds the sums until the start is found
     static_assert(sizeof(PagedScratch) <= kSmem<64> - 1024, "the scratch fits the rings");
     PagedStart start;
-    const bool any = paged_find_start<kThreads, kKT, kItem>(a, *reinterpret_cast<PagedScratch*>(smem), kPagedWaves, kMinUnits, kFullUnits, start);
+    const bool any = paged_find_start<kThreads, kKT, kItem, true>(a, *reinterpret_cast<PagedScratch*>(smem), kPagedWaves, kMinUnits, kFullUnits, start);
     if (!any) return;                                           // block-uniform
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the scratch's writes before the copies that take its place
     __syncthreads();
@@ -402,6 +402,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                 }
             }
             mma_warps_barrier();                                // all have read the last V tile
+            const bool upper = rows > 8;                        // rows from 8 on
             float* merge = reinterpret_cast<float*>(smem + (KS + vr.slot) * kTileBytes<HD>);
             static_assert(2 * 16 * HD * 4 <= kTileBytes<HD>, "two warps' outputs fit a tile");
 #pragma unroll
@@ -430,14 +431,16 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
 #pragma unroll
                     for (int d = 0; d < ND; ++d)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) mb[(d * 4 + j) * 32] = o[d][j];
+                        for (int j = 0; j < 4; ++j)
+                            if (j < 2 || upper) mb[(d * 4 + j) * 32] = o[d][j];
                 }
                 mma_warps_barrier();
                 if (warp < half) {
 #pragma unroll
                     for (int d = 0; d < ND; ++d)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) o[d][j] += mb[(d * 4 + j) * 32];
+                        for (int j = 0; j < 4; ++j)
+                            if (j < 2 || upper) o[d][j] += mb[(d * 4 + j) * 32];
                 }
                 mma_warps_barrier();
             }

@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
 
     PagedStart start;
     static_assert(sizeof(PagedScratch) <= kSmem<64, 1> - 1024, "the scratch fits the tiles");
-    const bool any = paged_find_start<kThreads<QT>, kKT, kItem>(a, *reinterpret_cast<PagedScratch*>(sQ), 1, kItem + 2, 0, start);
+    const bool any = paged_find_start<kThreads<QT>, kKT, kItem, false>(a, *reinterpret_cast<PagedScratch*>(sQ), 1, kItem + 2, 0, start);
     proxy_fence();                                          // the scratch's writes before the copies that take its place
     __syncthreads();
 
