@@ -127,6 +127,7 @@ class PagedCache:
                                          self.workspace.numel(), C.c_void_p(stream.cuda_stream), C.byref(self.handle)), "odb_paged_create")
         self._stream, self._raw, self._index = stream, stream.cuda_stream, self.device.index
         self._gain_shape = torch.Size((head_dim,))
+        self._new, self._width = kv.new_empty, n_heads * head_dim       # outputs: bf16 on the cache's device (1.4 us; torch.empty 3.1)
         self._rows_c = B.odb_paged_rows()
         self._rows_ref = C.byref(self._rows_c)
         self._layout, self._store, self._attention = lib.odb_paged_layout, lib.odb_paged_norm_rope_store, lib.odb_paged_attention
@@ -183,14 +184,16 @@ class PagedCache:
         """Norm of every q and k head (where a gain is given), rotation by row_pos, K and V into row_slot
         (odb_paged_norm_rope_store).  q, k, v: [max_rows][heads][head_dim] or [max_rows][heads * head_dim], slices of one
         projection's output as they are.  Returns q_out (a new tensor where none is given; q itself may be given)."""
-        if q_out is None:
-            q_out = torch.empty(batch._q[0], dtype=torch.bfloat16, device=self.device)
         if rope.index != self._index:
             raise ValueError(f"rope: on {self.device} it is wanted")
         qp, qs = self._rows(q, "q", self.n_heads, batch._q)
         kp, ks = self._rows(k, "k", self.n_kv_heads, batch._kv)
         vp, vs = self._rows(v, "v", self.n_kv_heads, batch._kv)
-        op, os_ = (qp, qs) if q_out is q else self._rows(q_out, "q_out", self.n_heads, batch._q)
+        if q_out is None:
+            q_out = self._new(batch.max_rows, self.n_heads, self.head_dim)
+            op, os_ = q_out.data_ptr(), self._width
+        else:
+            op, os_ = (qp, qs) if q_out is q else self._rows(q_out, "q_out", self.n_heads, batch._q)
         _ROWS.pack_into(self._rows_c, 0, qp, qs, kp, ks, vp, vs, op, os_, self._gain(q_gain, "q_gain"), self._gain(k_gain, "k_gain"))
         status = self._store(self.handle, layer, batch._ref, self._rows_ref, rope._ref, eps, self._current())
         if status:
@@ -202,10 +205,12 @@ class PagedCache:
         keys j < len_after with j <= p + right and (j >= p - left or j < sinks); -1: no limit; causal: right=0.
         scale 0: 1 / sqrt(head_dim).  lse: float32 [max_rows][n_heads] to be filled.  Returns out (a new tensor where none
         is given)."""
-        if out is None:
-            out = torch.empty(batch._q[0], dtype=torch.bfloat16, device=self.device)
         qp, qs = self._rows(q, "q", self.n_heads, batch._q)
-        op, os_ = self._rows(out, "out", self.n_heads, batch._q)
+        if out is None:
+            out = self._new(batch.max_rows, self.n_heads, self.head_dim)
+            op, os_ = out.data_ptr(), self._width
+        else:
+            op, os_ = self._rows(out, "out", self.n_heads, batch._q)
         lp = None
         if lse is not None:
             if lse.dtype is not _F32 or lse.get_device() != self._index or lse.shape != batch._lse or not lse.is_contiguous():
