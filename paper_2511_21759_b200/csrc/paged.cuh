@@ -442,11 +442,12 @@ __device__ __forceinline__ uint32_t paged_bf16x2(float a, float b) {
 __device__ __forceinline__ size_t paged_part(const PagedAttnArgs& a, int cta, bool begins) {
     return (static_cast<size_t>(cta) * kPagedMaxParts + (begins ? 1 : 0)) * a.part_rows;
 }
-// The parts of row r of an item that begins in CTA c0, added up in the order of the CTAs.
-template <int HD>
+// The parts of RB rows of an item that begins in CTA c0, added up in the order of the CTAs: 32 parts' maxima and sums at once, one a
+// lane, then their outputs, 16 loads in flight.
+template <int HD, int RB>
 struct PagedSum {
-    static constexpr int V = HD / 32;                // dims of a lane
-    float M = -INFINITY, L = 0.f, acc[V] = {};
+    static constexpr int V = HD / 32, CU = 16 / RB;  // dims of a lane; parts at once
+    float M[RB], L[RB], acc[RB][V];
 
     __device__ __forceinline__ void load(const float* p, float (&x)[V]) const {
         if constexpr (V == 4) {
@@ -457,50 +458,71 @@ struct PagedSum {
             x[0] = t.x; x[1] = t.y;
         }
     }
-    // One row of many parts: 32 parts' maxima and sums at once, one a lane, then their outputs, sixteen in flight.
-    __device__ __forceinline__ void row(const PagedAttnArgs& a, int c0, int c1, int r) {
+    // rows r0, r0 + step ..; those behind the last repeat it
+    __device__ __forceinline__ void rows(const PagedAttnArgs& a, int c0, int c1, int r0, int step, int n_rows) {
         const int lane = threadIdx.x & 31;
+        int r[RB];
+#pragma unroll
+        for (int k = 0; k < RB; ++k) {
+            r[k] = min(r0 + k * step, n_rows - 1);
+            M[k] = -INFINITY;
+            L[k] = 0.f;
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[k][j] = 0.f;
+        }
         for (int c = c0; c <= c1; c += 32) {
             const int n = min(32, c1 + 1 - c), mine = c + min(lane, n - 1);
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(a.part_ml + (paged_part(a, mine, mine == c0) + r) * 2));
-            float top = ml.x;
+            float2 ml[RB];
+            float w[RB];
 #pragma unroll
-            for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-            top = fmaxf(top, M);
-            const float w = lane < n ? paged_weight(ml.x, top) : 0.f, f = paged_weight(M, top);
-            float l = w * ml.y;
+            for (int k = 0; k < RB; ++k) ml[k] = __ldcg(reinterpret_cast<const float2*>(a.part_ml + (paged_part(a, mine, mine == c0) + r[k]) * 2));
 #pragma unroll
-            for (int d = 16; d >= 1; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-            M = top;
-            L = L * f + l;
+            for (int k = 0; k < RB; ++k) {
+                float top = ml[k].x;
 #pragma unroll
-            for (int j = 0; j < V; ++j) acc[j] *= f;
-            for (int u0 = 0; u0 < n; u0 += 16) {
-                float x[16][V];
+                for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                top = fmaxf(top, M[k]);
+                w[k] = lane < n ? paged_weight(ml[k].x, top) : 0.f;
+                const float f = paged_weight(M[k], top);
+                float l = w[k] * ml[k].y;
 #pragma unroll
-                for (int u = 0; u < 16; ++u) {
+                for (int d = 16; d >= 1; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+                M[k] = top;
+                L[k] = L[k] * f + l;
+#pragma unroll
+                for (int j = 0; j < V; ++j) acc[k][j] *= f;
+            }
+            for (int u0 = 0; u0 < n; u0 += CU) {
+                float x[CU][RB][V];
+#pragma unroll
+                for (int u = 0; u < CU; ++u) {
                     const int cta = c + min(u0 + u, n - 1);
-                    load(a.part_o + (paged_part(a, cta, cta == c0) + r) * HD + lane * V, x[u]);
+                    const float* part = a.part_o + paged_part(a, cta, cta == c0) * HD + lane * V;
+#pragma unroll
+                    for (int k = 0; k < RB; ++k) load(part + r[k] * HD, x[u][k]);
                 }
 #pragma unroll
-                for (int u = 0; u < 16; ++u) {
-                    const float e = __shfl_sync(0xffffffffu, w, (u0 + u) & 31);   // zero behind the last
-                    if (u0 + u < n)
+                for (int u = 0; u < CU; ++u) {
 #pragma unroll
-                        for (int j = 0; j < V; ++j) acc[j] += e * x[u][j];
+                    for (int k = 0; k < RB; ++k) {
+                        const float e = __shfl_sync(0xffffffffu, w[k], (u0 + u) & 31);   // zero behind the last
+                        if (u0 + u < n)
+#pragma unroll
+                            for (int j = 0; j < V; ++j) acc[k][j] += e * x[u][k][j];
+                    }
                 }
             }
         }
     }
-    // output of packed row idx of the request whose rows begin at row0
-    __device__ __forceinline__ void write(const PagedAttnArgs& a, int row0, int head, int idx) const {
+    // output of row k, packed row idx of the request whose rows begin at row0
+    __device__ __forceinline__ void write(const PagedAttnArgs& a, int k, int row0, int head, int idx) const {
         const int lane = threadIdx.x & 31, i = a.by_group(idx), h = head * a.G + idx - i * a.G;
         const size_t row = static_cast<size_t>(row0 + i);
-        const float inv = L == 0.f ? 0.f : 1.0f / L;
+        const float inv = L[k] == 0.f ? 0.f : 1.0f / L[k];
         uint32_t* op = reinterpret_cast<uint32_t*>(a.out + row * a.out_stride + h * HD + lane * V);
 #pragma unroll
-        for (int j = 0; j < V; j += 2) op[j / 2] = paged_bf16x2(acc[j] * inv, acc[j + 1] * inv);
-        if (a.lse && lane == 0) a.lse[row * a.H + h] = paged_lse(M, L);
+        for (int j = 0; j < V; j += 2) op[j / 2] = paged_bf16x2(acc[k][j] * inv, acc[k][j + 1] * inv);
+        if (a.lse && lane == 0) a.lse[row * a.H + h] = paged_lse(M[k], L[k]);
     }
 };
 

@@ -484,11 +484,17 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
             }
             mma_warps_barrier();
             if (sh->last) {
-                for (int r = warp; r < rows; r += kMmaWarps) {
-                    PagedSum<HD> sum;
-                    sum.row(a, c0, c1, r);
-                    sum.write(a, w.q.row0, w.head, w.rt * kRows + r);
-                }
+                auto add_up = [&](auto sum) {
+                    constexpr int RB = sizeof(sum.M) / sizeof(float);
+                    if (warp >= rows) return;
+                    sum.rows(a, c0, c1, warp, kMmaWarps, rows);
+#pragma unroll
+                    for (int k = 0; k < RB; ++k)
+                        if (warp + k * kMmaWarps < rows) sum.write(a, k, w.q.row0, w.head, w.rt * kRows + warp + k * kMmaWarps);
+                };
+                if (rows <= kMmaWarps) add_up(PagedSum<HD, 1>{});
+                else if (rows <= 2 * kMmaWarps) add_up(PagedSum<HD, 2>{});
+                else add_up(PagedSum<HD, 4>{});
                 mma_warps_barrier();                             // sh->last has been read by all
             }
         }
