@@ -757,10 +757,12 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
 }
 
 // Adds up the parts of the items that several CTAs share, in the order of the CTAs with a running maximum: a thread takes kMergeDims
-// values of a row, a block the rows of a Q tile, eight parts in flight.
-constexpr int kMergeDims = 8;
+// values of a row, a block the rows of a Q tile, four parts in flight.  Most items have two or three parts: with eight in flight the
+// registers leave half as many blocks on an SM (blocks of 32 rows 48.2 us, a prompt of 4096 rows 153.7; with four 46.4 and 150.3; with
+// two 45.9 and 149.3, but twice the latency of items of many parts).
+constexpr int kMergeDims = 8, kMergeParts = 4;
 template <int HD>
-__global__ void __launch_bounds__(kTQ) paged_merge_kernel(const PagedAttnArgs a) {
+__global__ void __launch_bounds__(kTQ, 8) paged_merge_kernel(const PagedAttnArgs a) {
     pdl_launch_dependents();
     pdl_wait();
     const PagedShared d = a.shared[blockIdx.x];
@@ -770,12 +772,11 @@ __global__ void __launch_bounds__(kTQ) paged_merge_kernel(const PagedAttnArgs a)
     float M = -INFINITY, L = 0.f, acc[kMergeDims];
 #pragma unroll
     for (int j = 0; j < kMergeDims; ++j) acc[j] = 0.f;
-    constexpr int kU = 8;
-    for (int c = blockIdx.x; c <= d.last_cta; c += kU) {
-        float2 ml[kU];
-        float4 x[kU][kMergeDims / 4];
+    for (int c = blockIdx.x; c <= d.last_cta; c += kMergeParts) {
+        float2 ml[kMergeParts];
+        float4 x[kMergeParts][kMergeDims / 4];
 #pragma unroll
-        for (int u = 0; u < kU; ++u) {
+        for (int u = 0; u < kMergeParts; ++u) {
             if (c + u > d.last_cta) break;
             const size_t part = paged_part(a, c + u, c + u == static_cast<int>(blockIdx.x)) + g * kTQ;
             ml[u] = __ldcg(reinterpret_cast<const float2*>(a.part_ml + (part + r) * 2));
@@ -783,7 +784,7 @@ __global__ void __launch_bounds__(kTQ) paged_merge_kernel(const PagedAttnArgs a)
             for (int j = 0; j < kMergeDims / 4; ++j) x[u][j] = __ldcg(reinterpret_cast<const float4*>(a.part_o + part * HD + ((dim0 / 4 + j) * kTQ + r) * 4));
         }
 #pragma unroll
-        for (int u = 0; u < kU; ++u) {
+        for (int u = 0; u < kMergeParts; ++u) {
             if (c + u > d.last_cta) break;
             const float top = fmaxf(M, ml[u].x), f = paged_weight(M, top), e = paged_weight(ml[u].x, top);
             M = top;
