@@ -13,8 +13,9 @@
 // CTAs, whoever it is: the same bits every time.
 //
 // Bound by HBM where there is work for all SMs (a pool read once; the products of 16 rows take a third of a tile's time): one token
-// of 48 requests, 905 MB, 156 us = 5.8 TB/s, of two of 131072 keys, 1.02 GB, 170 us = 6.0 TB/s; the rest is the start (2 us to find
-// the share), the parts and the slowest SMs' tail.  Small calls are bound by latency: one token of 577 keys 10 us.
+// of 48 requests, 905 MB, 154 us = 5.9 TB/s, of two of 131072 keys, 1.02 GB, 170 us = 6.0 TB/s; the rest is the start (a microsecond to
+// find the share, two until the first tile is there), the parts and the slowest SMs' tail.  Small calls are bound by latency: one token
+// of 577 keys 9.2 us, 16 requests with a window of 4096 keys of 64 (67 MB) 24 us.
 //
 // Rows of V behind the last visible key are whatever the page held before: their P is zero, but zero times an infinity or NaN
 // there is not, so they are set to zero in shared memory first.  A key that some rows of the tile see and others do not is
@@ -527,9 +528,10 @@ size_t paged_part_bytes(int hd) { return static_cast<size_t>(kPagedMaxParts) * k
 
 // Which kernel, by the packed rows of the longest request.  us, few rows' kernel / tensor cores with one Q tile / with two, 8 K/V heads
 // of 128:
-//   4 packed rows, 1 request of 577 keys 10 / 20 / 18, 2 of 131072 174 / 170 / 249, 48 of up to 8192 155 / 150 / 222
-//   16 packed rows, 16 requests of 4096 keys 55 / 49 / 66, 2 of them 23 / 25 / 27;   32, 16 requests 87 / 49 / 65, of 600 keys 27 / 22 / 26
-//   128 packed rows, 16 requests of 4096 keys - / 54 / 66;   192: - / 79 / 72;   256: - / 86 / 78;   a prompt of 4096: - / 180 / 176
+//   4 packed rows, 1 request of 577 keys 9.0 / 17.0 / 19.7, 16 of up to 600 15 / 20 / 26, 16 of up to 4096 47 / 48 / 68, 2 of 131072
+//   170 / 165 / 235;   16 rows, 1 of 577 12 / 19 / -, 1 of 4096 18 / 20 / -, 16 of up to 4096 50 / 50 / 67
+//   32 packed rows, 16 requests of up to 4096 keys 86 / 48 / 62, of up to 600 28 / 21 / 23
+//   128 packed rows, 16 requests of up to 4096 - / 54 / 64;   192: - / 78 / 70;   256: - / 85 / 76;   refresh of 4 x 1300 rows - / 173 / 152
 cudaError_t launch_paged_attention(PagedAttnArgs a, const PagedMaps& maps, int hd, int max_new, int sms, cudaStream_t st) {
     if (sms < 1 || 2 * sms * 128 > kPagedPartRows || kPagedWaves * 2 * sms > kPagedMaxCtas) return cudaErrorInvalidValue;   // the workspace's size
     a.by_group = PagedDiv::by(a.G);

@@ -1,5 +1,7 @@
 """The paged cache's host side and its oracle on a machine without a GPU."""
 import ctypes as C
+import os
+import re
 
 import numpy as np
 import pytest
@@ -136,3 +138,12 @@ def test_division_by_a_product():
         assert m < 1 << 32
         ns = sorted({n for q in (0, 1, 2, 3, 1000, 65535, (2 ** 31 - 1) // d) for n in (q * d - 1, q * d, q * d + 1, q * d + d - 1) if 0 <= n < 2 ** 31} | {2 ** 31 - 1, 2 ** 30})
         assert all((n * m) >> (31 + l) == n // d for n in ns), d
+
+
+def test_the_paged_attentions_successor_starts_behind_its_tmem_allocation():
+    """tcgen05.alloc blocks until columns are free; a successor's CTAs that held them while they wait for this kernel would never
+    give them back."""
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2511_21759_b200", "csrc")
+    text = re.sub(r"//[^\n]*", "", open(os.path.join(csrc, "paged_attention_tc.cu")).read())
+    body = text.split("__global__")[1]
+    assert 0 < body.find("tmem_alloc(") < body.find("pdl_launch_dependents()") < body.find("PagedStart start;")
