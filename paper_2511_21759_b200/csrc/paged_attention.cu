@@ -532,11 +532,17 @@ size_t paged_part_bytes(int hd) { return static_cast<size_t>(kPagedMaxParts) * k
 //   170 / 165 / 235;   16 rows, 1 of 577 12 / 19 / -, 1 of 4096 18 / 20 / -, 16 of up to 4096 50 / 50 / 67
 //   32 packed rows, 16 requests of up to 4096 keys 86 / 48 / 62, of up to 600 28 / 21 / 23
 //   128 packed rows, 16 requests of up to 4096 - / 54 / 64;   192: - / 78 / 70;   256: - / 85 / 76;   refresh of 4 x 1300 rows - / 173 / 152
+// Two Q tiles take requests that are alike, the longest up to three times the mean: beside a prompt of 2048 rows 47 single tokens of up
+// to 8192 keys leave the second one empty, and two CTAs on an SM hide more: - / 165 / 215 (head dim 64: 125 / 172); 512 rows and 8 tokens
+// 48 / 61; 4096 rows and 8 tokens 179 / 171.
 cudaError_t launch_paged_attention(PagedAttnArgs a, const PagedMaps& maps, int hd, int max_new, int sms, cudaStream_t st) {
     if (sms < 1 || 2 * sms * 128 > kPagedPartRows || kPagedWaves * 2 * sms > kPagedMaxCtas) return cudaErrorInvalidValue;   // the workspace's size
     a.by_group = PagedDiv::by(a.G);
     const long long rows = static_cast<long long>(max_new) * a.G;
-    if (rows > kRows && a.G <= kPagedTcMaxGroup) return launch_paged_attention_tc(a, maps, hd, rows > 128 ? 2 : 1, sms, st);
+    if (rows > kRows && a.G <= kPagedTcMaxGroup) {
+        const bool alike = static_cast<long long>(max_new) * a.n_seqs <= 3ll * a.max_rows;
+        return launch_paged_attention_tc(a, maps, hd, rows > 128 && alike ? 2 : 1, sms, st);
+    }
     return hd == 128 ? launch<128>(a, maps.rows, sms, st) : launch<64>(a, maps.rows, sms, st);
 }
 

@@ -473,6 +473,25 @@ def test_attention_of_scores_far_below_zero_in_parts(lens, new, G, D):
 
 
 @requires_gpu
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G", [1, 4])
+def test_attention_of_prompts_blocks_and_single_tokens_in_one_forward(G, D):
+    """Requests of one, a few and many row tiles by turns, so that shares begin and end in each kind."""
+    rng = np.random.default_rng(23)
+    lens = [700, 577, 90, 1, 2000, 64, 300, 1500, 129, 520]
+    counts = [300, 1, 1, 1, 33, 64, 300, 1, 129, 2]
+    firsts = [n - c for n, c in zip(lens, counts)]
+    for mask in (dict(right=0), dict(left=200, right=0, sinks=5), dict()):
+        cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, 2 * G, 2, D, 32)
+        lse = torch.empty(len(qf), 2 * G, device="cuda")
+        out = cache.attention(0, b, q, lse=lse, **mask)
+        _check(out, lse, qf, keys, values, start, firsts, D, **mask)
+        again = cache.attention(0, b, q, **mask)
+        assert torch.equal(out, again)
+        cache.close()
+
+
+@requires_gpu
 def test_attention_reads_strided_rows_and_other_layers_and_leaves_rows_behind_the_last():
     rng = np.random.default_rng(4)
     lens, counts, firsts = [50, 90], [2, 5], [48, 85]
