@@ -1,4 +1,4 @@
-// Attention of the rows of each request over its pages of the K/V pool: few packed rows (query rows x heads of a group).
+// Attention of the rows of each request over its pages of the K/V pool: few packed rows (query rows x heads of a group), or little work.
 //
 //   o = sum_j p_j v_j / sum_j p_j,  p_j = 2^(s_j - m),  s_j = log2(e) * scale * q.k_j,  lse = ln 2 * (m + log2 sum_j p_j)
 //
@@ -30,6 +30,7 @@ constexpr int kKT = 64;                    // keys per tile
 constexpr int kItem = 1;                    // key tiles that an item costs beside its own
 constexpr int kMinUnits = 2, kFullUnits = 24;   // units of a CTA, at least; where all places on the SMs have work
 constexpr int kRows = 16;                   // packed rows of an item
+constexpr int kSmallUnits = 1024;           // up to here few rows' kernel for any number of rows
 constexpr int kMmaWarps = 4;
 constexpr int kThreads = 32 * (kMmaWarps + 1);
 template <int HD> constexpr int kKSlots = HD == 128 ? 3 : 7;                // K tiles on the way or in use
@@ -526,8 +527,11 @@ cudaError_t launch(PagedAttnArgs a, const CUtensorMap& tmap, int sms, cudaStream
 
 size_t paged_part_bytes(int hd) { return static_cast<size_t>(kPagedMaxParts) * kPagedPartRows * (hd + 2) * sizeof(float); }
 
-// Which kernel, by the packed rows of the longest request.  us, few rows' kernel / tensor cores with one Q tile / with two, 8 K/V heads
-// of 128:
+// Which kernel: by the work, then by the packed rows of the longest request.  Up to kSmallUnits key tiles of items of 16 packed rows (an
+// item's start counted as one), as far as the table's width bounds them, mma.sync without a second launch is faster,
+// however many rows: us, it / tensor cores with one Q tile, head dim 128: 192 units 12.6 / 16.0, 544 13.6 / 16.2, 1024 15.8 / 18.3, 1088
+// 17.2 / 17.0, 1536 18.9 / 19.2, 2112 22 / 18, 4352 31 / 18; head dim 64: 192 10.7 / 12.7, 528 12.1 / 14.2, 1088 14.3 / 13.9, 2112 19 / 15.
+// Above, 8 K/V heads of 128, one Q tile / two behind it:
 //   4 packed rows, 1 request of 577 keys 9.0 / 17.0 / 19.7, 16 of up to 600 15 / 20 / 26, 16 of up to 4096 47 / 48 / 68, 2 of 131072
 //   170 / 165 / 235;   16 rows, 1 of 577 12 / 19 / -, 1 of 4096 18 / 20 / -, 16 of up to 4096 50 / 50 / 67
 //   32 packed rows, 16 requests of up to 4096 keys 86 / 48 / 62, of up to 600 28 / 21 / 23
@@ -539,7 +543,10 @@ cudaError_t launch_paged_attention(PagedAttnArgs a, const PagedMaps& maps, int h
     if (sms < 1 || 2 * sms * 128 > kPagedPartRows || kPagedWaves * 2 * sms > kPagedMaxCtas) return cudaErrorInvalidValue;   // the workspace's size
     a.by_group = PagedDiv::by(a.G);
     const long long rows = static_cast<long long>(max_new) * a.G;
-    if (rows > kRows && a.G <= kPagedTcMaxGroup) {
+    const long long tiles = (static_cast<long long>(a.table_stride) << a.page_shift) / kKT + 1 + kItem;
+    const double units = static_cast<double>((static_cast<long long>(a.max_rows) * a.G + (kRows - 1ll) * a.n_seqs) / kRows) * a.KV *
+                         static_cast<double>(tiles);
+    if (rows > kRows && units > kSmallUnits && a.G <= kPagedTcMaxGroup) {
         const bool alike = static_cast<long long>(max_new) * a.n_seqs <= 3ll * a.max_rows;
         return launch_paged_attention_tc(a, maps, hd, rows > 128 && alike ? 2 : 1, sms, st);
     }

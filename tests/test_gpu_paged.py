@@ -229,16 +229,23 @@ def test_norm_rope_store_in_place_and_without_anything_to_do():
     cache.close()
 
 
+# The table's width is what the host knows of the keys, and with few of them every number of rows takes the kernel of few rows: the
+# same requests in a wide table take the tensor cores'.
+@pytest.fixture(params=["narrow", "wide"])
+def columns(request):
+    return {"narrow": 1, "wide": 5000}[request.param]
+
+
 # ---- attention --------------------------------------------------------------------------------------------------------
 
-def _setup(rng, lens, counts, firsts, H, KV, D, page, layers=1, layer=0, poison=True, scale=1.0, spare=2):
+def _setup(rng, lens, counts, firsts, H, KV, D, page, layers=1, layer=0, poison=True, scale=1.0, spare=2, columns=1):
     """A pool of shuffled pages; everything that is no key of a request is NaN, and so are pages nobody holds."""
     P = paged()
     held = [O.pages_of(n, page) for n in lens]
     n_pages = sum(held) + spare
     pool = torch.full((layers, 2, n_pages, KV, page, D), float("nan") if poison else 0.0, dtype=torch.bfloat16)
     order = rng.permutation(n_pages)
-    width = max(held + [1]) + 1
+    width = max(held + [1]) + columns
     table = np.full((len(lens), width), 10 ** 6, np.int32)
     keys, values = [], []
     at = 0
@@ -327,14 +334,14 @@ ATT = [  # lens, rows (0: all), H, KV, D, page, mask
 
 @requires_gpu
 @pytest.mark.parametrize("case", ATT)
-def test_attention(case):
+def test_attention(case, columns):
     lens, new, H, KV, D, page, mask = case
     rng = np.random.default_rng(len(lens) * 31 + H + D + page)
     counts = [min(n, new) if new else n for n in lens]
     firsts = [n - c for n, c in zip(lens, counts)]
     if not mask and new > 1:
         firsts = [max(0, f // 2) for f in firsts]                 # a block in the middle
-    cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, H, KV, D, page)
+    cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, H, KV, D, page, columns=columns)
     lse = torch.empty(sum(counts), H, device="cuda")
     out = cache.attention(0, b, q, lse=lse, **mask)
     assert cache.status() == 0
@@ -347,14 +354,14 @@ def test_attention(case):
 @requires_gpu
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("new,G", [(1, 4), (30, 4), (60, 4)])
-def test_attention_of_many_requests_of_a_tile_or_two(new, G, D):
+def test_attention_of_many_requests_of_a_tile_or_two(new, G, D, columns):
     """More items than CTAs, each of one to three key tiles: shares of many items, and items cut in two."""
     rng = np.random.default_rng(new + D)
     seqs = 230
     lens = [int(n) for n in rng.integers(1, 150, seqs)]
     counts = [min(n, new) for n in lens]
     firsts = [n - c for n, c in zip(lens, counts)]
-    cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, 2 * G, 2, D, 16)
+    cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, 2 * G, 2, D, 16, columns=columns)
     lse = torch.empty(sum(counts), 2 * G, device="cuda")
     out = cache.attention(0, b, q, right=0, lse=lse)
     assert cache.status() == 0
@@ -369,11 +376,11 @@ def test_attention_of_many_requests_of_a_tile_or_two(new, G, D):
 
 @requires_gpu
 @pytest.mark.parametrize("max_new", [1, 8, 16, 20, 64, 5000])
-def test_the_hint_decides_no_result(max_new):
+def test_the_hint_decides_no_result(max_new, columns):
     rng = np.random.default_rng(9)
     lens, counts = [90, 300, 20], [1, 37, 5]
     firsts = [n - c for n, c in zip(lens, counts)]
-    cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, 8, 2, 128, 32)
+    cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, 8, 2, 128, 32, columns=columns)
     b._c.max_new = max_new
     lse = torch.empty(sum(counts), 8, device="cuda")
     out = cache.attention(0, b, q, right=0, lse=lse)
@@ -385,11 +392,11 @@ def test_the_hint_decides_no_result(max_new):
 @requires_gpu
 @pytest.mark.parametrize("new", [1, 3, 20, 40])
 @pytest.mark.parametrize("D", [64, 128])
-def test_attention_rows_that_see_nothing_and_requests_without_rows_or_keys(new, D):
+def test_attention_rows_that_see_nothing_and_requests_without_rows_or_keys(new, D, columns):
     rng = np.random.default_rng(new + D)
     lens, counts = [0, 70, 0, 12, 33], [new, 0, 0, new, new]
     firsts = [0, 3, 0, 40, 60]                                     # 40 - left > 12: the window lies behind the keys
-    cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, 4, 2, D, 16)
+    cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, 4, 2, D, 16, columns=columns)
     for mask in (dict(), dict(right=0), dict(left=5, right=0), dict(left=5, right=0, sinks=3), dict(left=0, sinks=1)):
         lse = torch.full((sum(counts), 4), 3.0, device="cuda")
         out = torch.full((sum(counts), 4, D), 3.0, dtype=torch.bfloat16, device="cuda")
@@ -403,11 +410,11 @@ def test_attention_rows_that_see_nothing_and_requests_without_rows_or_keys(new, 
 @requires_gpu
 @pytest.mark.parametrize("new,G", [(1, 4), (5, 2), (20, 1), (9, 4), (16, 4), (20, 4), (70, 1), (70, 2), (100, 3)])
 @pytest.mark.parametrize("D", [64, 128])
-def test_attention_infinities_and_nan_reach_only_the_rows_that_see_them(new, G, D):
+def test_attention_infinities_and_nan_reach_only_the_rows_that_see_them(new, G, D, columns):
     rng = np.random.default_rng(new + D)
     n = 150
     first = n - new
-    cache, b, q, qf, keys, values, start = _setup(rng, [n], [new], [first], 2 * G, 2, D, 16)
+    cache, b, q, qf, keys, values, start = _setup(rng, [n], [new], [first], 2 * G, 2, D, 16, columns=columns)
     table = b.table.cpu().numpy()[0]
     mask = dict(left=60, right=0, sinks=2)
     clean = cache.attention(0, b, q, **mask).float().cpu().numpy()
@@ -442,13 +449,13 @@ def test_attention_infinities_and_nan_reach_only_the_rows_that_see_them(new, G, 
 @requires_gpu
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("new", [3, 45, 90])
-def test_attention_of_large_scores_and_another_scale(new, D):
+def test_attention_of_large_scores_and_another_scale(new, D, columns):
     rng = np.random.default_rng(21)
     lens, counts = [333, 94], [new, new]
     firsts = [n - c for n, c in zip(lens, counts)]
     for scale in (0.0, 0.25, 1e-4, -0.05, 3e4):
         for size in (1.0, 30.0):
-            cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, 4, 2, D, 16, scale=size)
+            cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, 4, 2, D, 16, scale=size, columns=columns)
             lse = torch.empty(2 * new, 4, device="cuda")
             out = cache.attention(0, b, q, lse=lse, scale=scale, right=0)
             _check_scaled(out, lse, qf, keys, values, start, firsts, D, scale or None, right=0)
@@ -458,12 +465,12 @@ def test_attention_of_large_scores_and_another_scale(new, D):
 @requires_gpu
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("lens,new,G", [([1500], 1500, 4), ([700, 90], 90, 1), ([2600], 30, 4), ([3000], 1, 4)])
-def test_attention_of_scores_far_below_zero_in_parts(lens, new, G, D):
+def test_attention_of_scores_far_below_zero_in_parts(lens, new, G, D, columns):
     """Rows whose scores all lie hundreds below zero, some of whose item's parts hold no key that they see."""
     rng = np.random.default_rng(22)
     counts = [new] * len(lens)
     firsts = [n - new for n in lens]
-    cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, 2 * G, 2, D, 16)
+    cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, 2 * G, 2, D, 16, columns=columns)
     cache.kv[:, 0].abs_()
     for mask in (dict(right=0), dict(left=70, right=0)):
         lse = torch.empty(len(qf), 2 * G, device="cuda")
@@ -475,14 +482,14 @@ def test_attention_of_scores_far_below_zero_in_parts(lens, new, G, D):
 @requires_gpu
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("G", [1, 4])
-def test_attention_of_prompts_blocks_and_single_tokens_in_one_forward(G, D):
+def test_attention_of_prompts_blocks_and_single_tokens_in_one_forward(G, D, columns):
     """Requests of one, a few and many row tiles by turns, so that shares begin and end in each kind."""
     rng = np.random.default_rng(23)
     lens = [700, 577, 90, 1, 2000, 64, 300, 1500, 129, 520]
     counts = [300, 1, 1, 1, 33, 64, 300, 1, 129, 2]
     firsts = [n - c for n, c in zip(lens, counts)]
     for mask in (dict(right=0), dict(left=200, right=0, sinks=5), dict()):
-        cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, 2 * G, 2, D, 32)
+        cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, 2 * G, 2, D, 32, columns=columns)
         lse = torch.empty(len(qf), 2 * G, device="cuda")
         out = cache.attention(0, b, q, lse=lse, **mask)
         _check(out, lse, qf, keys, values, start, firsts, D, **mask)
