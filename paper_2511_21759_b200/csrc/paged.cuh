@@ -71,7 +71,7 @@ struct PagedAttnArgs {
     float scale_log2;                                     // softmax scale x log2(e)
     int* status;
     unsigned int* arrivals;                               // [kPagedMaxCtas], zero between launches
-    float* part_o;                                        // [ctas][2][part_rows][HD]
+    float* part_o;                                        // [ctas][2][part_rows][HD]; many rows: [ctas][2][Q tile][HD / 4][128 rows][4]
     float* part_ml;                                       // [ctas][2][part_rows][2]
     int negate;                                           // many rows: the scale's sign, which scale_log2 no longer has
     int at_once;                                          // CTAs that run at one time
@@ -416,7 +416,7 @@ struct PagedPages {
 
 // One lane of a converged warp.  TMA copies and MMAs take their operands from uniform registers: behind elect, with operands that
 // every lane has, they follow one another without a detour (behind `lane == 0` an MMA took 110 cycles to issue, and one of
-// 128 x 64 x 16 runs for 32).
+// 128 x 64 x 16 runs for 51).
 __device__ __forceinline__ bool paged_elect() {
     uint32_t x;
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(x));
