@@ -13,9 +13,9 @@
 // CTAs, whoever it is: the same bits every time.
 //
 // Bound by HBM where there is work for all SMs (a pool read once; the products of 16 rows take a third of a tile's time): one token
-// of 48 requests, 905 MB, 154 us = 5.9 TB/s, of two of 131072 keys, 1.02 GB, 170 us = 6.0 TB/s; the rest is the start (a microsecond to
+// of 48 requests, 905 MB, 153 us = 5.9 TB/s, of two of 131072 keys, 1.02 GB, 168 us = 6.1 TB/s; the rest is the start (a microsecond to
 // find the share, two until the first tile is there), the parts and the slowest SMs' tail.  Small calls are bound by latency: one token
-// of 577 keys 9.2 us, 16 requests with a window of 4096 keys of 64 (67 MB) 24 us.
+// of 577 keys 9.2 us, 16 requests with a window of 4096 keys of 64 (67 MB) 23 us.
 //
 // Rows of V behind the last visible key are whatever the page held before: their P is zero, but zero times an infinity or NaN
 // there is not, so they are set to zero in shared memory first.  A key that some rows of the tile see and others do not is
@@ -532,13 +532,13 @@ size_t paged_part_bytes(int hd) { return static_cast<size_t>(kPagedMaxParts) * k
 // however many rows: us, it / tensor cores with one Q tile, head dim 128: 192 units 12.6 / 16.0, 544 13.6 / 16.2, 1024 15.8 / 18.3, 1088
 // 17.2 / 17.0, 1536 18.9 / 19.2, 2112 22 / 18, 4352 31 / 18; head dim 64: 192 10.7 / 12.7, 528 12.1 / 14.2, 1088 14.3 / 13.9, 2112 19 / 15.
 // Above, 8 K/V heads of 128, one Q tile / two behind it:
-//   4 packed rows, 1 request of 577 keys 9.0 / 17.0 / 19.7, 16 of up to 600 15 / 20 / 26, 16 of up to 4096 47 / 48 / 68, 2 of 131072
-//   170 / 165 / 235;   16 rows, 1 of 577 12 / 19 / -, 1 of 4096 18 / 20 / -, 16 of up to 4096 50 / 50 / 67
-//   32 packed rows, 16 requests of up to 4096 keys 86 / 48 / 62, of up to 600 28 / 21 / 23
-//   128 packed rows, 16 requests of up to 4096 - / 54 / 64;   192: - / 78 / 70;   256: - / 85 / 76;   refresh of 4 x 1300 rows - / 173 / 152
+//   4 packed rows, 1 request of 577 keys 9.1 / 17 / 20, 16 of up to 600 15 / 19 / 26, 16 of up to 4096 46 / 47 / 68, 2 of 131072
+//   168 / 165 / 235;   16 rows, 1 of 577 11 / 19 / -, 16 of up to 4096 49 / 48 / 67
+//   32 packed rows, 16 requests of up to 4096 keys 77 / 47 / 62, of up to 600 25 / 19 / 23
+//   128 packed rows, 16 requests of up to 4096 - / 52 / 62;   192: - / 75 / 65;   256: - / 82 / 70;   a causal prompt of 4096 rows - / 162 / 142
 // Two Q tiles take requests that are alike, the longest up to three times the mean: beside a prompt of 2048 rows 47 single tokens of up
-// to 8192 keys leave the second one empty, and two CTAs on an SM hide more: - / 165 / 215 (head dim 64: 125 / 172); 512 rows and 8 tokens
-// 48 / 61; 4096 rows and 8 tokens 179 / 171.
+// to 8192 keys leave the second one empty, and two CTAs on an SM hide more: - / 169 / 220 (head dim 64: 127 / 173); 512 rows and 8 tokens
+// 50 / 63; 4096 rows and 8 tokens 180 / 172.
 cudaError_t launch_paged_attention(PagedAttnArgs a, const PagedMaps& maps, int hd, int max_new, int sms, cudaStream_t st) {
     if (sms < 1 || 2 * sms * 128 > kPagedPartRows || kPagedWaves * 2 * sms > kPagedMaxCtas) return cudaErrorInvalidValue;   // the workspace's size
     a.by_group = PagedDiv::by(a.G);
