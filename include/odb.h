@@ -448,7 +448,8 @@ int32_t odb_paged_create(const odb_paged_config* cfg, void* kv, size_t kv_bytes,
                          odb_paged** out);
 int32_t odb_paged_destroy(odb_paged* h);
 /* Reads and clears the status word: ODB_OK, or what a call on the device found since - ODB_ERR_ARG (lengths or rows that
- * are negative, too long for a table row, or behind the length), ODB_ERR_WORKSPACE (the pool has too few pages),
+ * are negative, too long for a table row, or behind the length; in the attention a row_start that does not ascend from 0 or more to
+ * max_rows or less: such a call writes nothing), ODB_ERR_WORKSPACE (the pool has too few pages),
  * ODB_ERR_SHAPE (more rows than max_rows), ODB_ERR_STATE (a page id that is none), ODB_ERR_TIMEOUT.  Synchronous. */
 int32_t odb_paged_status(odb_paged* h, void* stream);
 

@@ -117,6 +117,14 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedAttnArgs& a, int s) {
     return q;
 }
 
+// Rows follow one another within those of the call.  Every sum below, the launcher's grid and the count of an item's parts rest on it:
+// requests whose rows overlap may have more work than the grid has CTAs for, and the item that is cut at its end would wait for parts
+// that nobody brings, in this launch and in the next ones.
+__device__ __forceinline__ bool paged_rows_follow(const PagedAttnArgs& a, int s) {
+    const int r0 = a.row_start[s], r1 = a.row_start[s + 1];
+    return 0 <= r0 && r0 <= r1 && r1 <= a.max_rows;
+}
+
 // The key tiles of a row tile: `sink_tiles` from the front, the others from tile `first_tile` on; `n` of them, at least
 // one (an item without a visible key still writes its rows).  Positions from `hi` on are seen by no row, nor are those
 // of [sinks, lo).
@@ -236,7 +244,8 @@ __device__ __forceinline__ int paged_upper(const int* v, int n, int x) {   // th
 // 47.9 -> 49.0 us).  Called by all THREADS threads of the block; false: there is nothing for this CTA to do.
 // waves: CTAs of the grid for each of the a.at_once that run at one time.  min_units: what a CTA takes at least (more than E);
 // full_units: what it takes at least as long as those have work.
-// The launcher's bounds on rows, requests and keys keep every sum below 2^31.
+// The launcher's bounds on rows, requests and keys keep every sum below 2^31, as long as the requests' rows follow one another; where
+// they do not, the call has no work and the status word says so.  (Sums that are formed until that is known may wrap and lead nowhere.)
 template <int THREADS, int KT, int E, bool WARPS>
 __device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int waves, int min_units, int full_units, PagedStart& st) {
     const int tid = threadIdx.x;
@@ -262,12 +271,14 @@ __device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int w
     if (WARPS && a.n_seqs <= 32) {
         const int s = tid & 31;
         int units = 0, n_rt = 0, rem;
+        bool wrong = false;
         if (s < a.n_seqs) {
             const PagedSeq q = paged_seq(a, s);
+            wrong = !paged_rows_follow(a, s);
             n_rt = q.n_rt;
             if (n_rt > 0) units = paged_keys<KT>(a, q, 0).n + E;
         }
-        if (!__any_sync(0xffffffffu, n_rt > 1)) {
+        if (!__any_sync(0xffffffffu, n_rt > 1 || wrong)) {
             int sum = units;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -284,17 +295,18 @@ __device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int w
     }
     const int per_s = (a.n_seqs + THREADS - 1) / THREADS, s0 = min(tid * per_s, a.n_seqs), s1 = min(s0 + per_s, a.n_seqs);
     int n_rt, mine_rt = 0, units = 0, rem;
-    bool several = false;
+    bool several = false, wrong = false;
 #pragma unroll 4
     for (int s = s0; s < s1; ++s) {
         const PagedSeq q = paged_seq(a, s);
+        wrong = wrong || !paged_rows_follow(a, s);
         sc.seq[s] = make_int4(q.row0, q.n, q.first, q.len);
         mine_rt += q.n_rt;
         several = several || q.n_rt > 1;
         sc.sum[s] = units;
         if (q.n_rt > 0) units += paged_keys<KT>(a, q, 0).n + E;
     }
-    if (!__syncthreads_or(several)) {   // no request has more than a row tile (single tokens, short blocks): sums over the requests do
+    if (!__syncthreads_or(several || wrong)) {   // no request has more than a row tile (single tokens, short blocks): sums over the requests do
         int per_head;
         const int before = paged_block_scan<THREADS>(units, sc.warp_sum, per_head);
         if (per_head == 0) return false;
@@ -306,6 +318,10 @@ __device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int w
         st.off = rem - sc.sum[st.seq];
         __syncthreads();                // the scratch may be overwritten now
         return true;
+    }
+    if (__syncthreads_or(wrong)) {
+        if (blockIdx.x == 0 && tid == 0) atomicExch(a.status, ODB_ERR_ARG);
+        return false;
     }
     {
         int at = paged_block_scan<THREADS>(mine_rt, sc.warp_sum, n_rt);
