@@ -12,7 +12,9 @@ A forward over requests of different lengths, one layer after the other:
 
 Every call is enqueued on the current stream of the cache's device and returns at once; status() waits and says what the
 device found.  A cache is used by one thread and on one stream at a time: a call on another stream than the one before waits for
-that one.
+that one, and so it does for the stream that its Batch was made or used on; the memory of these objects and of a Rope is not given back
+before the streams that used it are through.  In a graph's capture nothing is waited for: what the graph uses is to be kept, and its
+replays ordered, by its owner.  Tensors that are passed to a call follow torch's own rules for streams.
 """
 from __future__ import annotations
 
@@ -25,11 +27,27 @@ import torch
 from . import binding as B
 
 _BF16, _F32 = torch.bfloat16, torch.float32
+_raw_stream = torch._C._cuda_getCurrentRawStream
 _ROWS = struct.Struct("=QqQqQqQqQQ")          # odb_paged_rows, filled in one go
 SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 
 
-class Rope:
+class _OnStream:
+    """What is known of the memory that an object holds: the stream it was last used on."""
+
+    def _made(self, device, *tensors):
+        self._stream = torch.cuda.current_stream(device)
+        self._raw, self._memory = self._stream.cuda_stream, tensors
+
+    def _follow(self, st, raw: int):
+        """To stream st: the other one's work comes first, and the memory stays until st's is done too."""
+        st.wait_stream(self._stream)
+        for t in self._memory:
+            t.record_stream(st)
+        self._stream, self._raw = st, raw
+
+
+class Rope(_OnStream):
     """Rotation of the first rot_dim values of a head: pairs (i, i + rot_dim / 2), or (2i, 2i + 1) where interleaved.
     scaling: "none", "linear", "ntk" or "yarn" with a factor (odb_rope_frequencies)."""
 
@@ -45,11 +63,18 @@ class Rope:
         # fractions of a turn per position, 64-bit patterns
         self.turns = torch.tensor([C.c_int64(v).value for v in host], dtype=torch.int64, device=device)
         self.index = self.turns.get_device()
+        if self.turns.is_cuda:
+            self._made(self.turns.device, self.turns)
         self._c = B.odb_rope(self.turns.data_ptr(), rot_dim, 1 if interleaved else 0, mag.value)
         self._ref = C.byref(self._c)
 
+    def _follow(self, st, raw: int):
+        """The numbers were there when the constructor returned and are read only: caches on several streams wait for none."""
+        self.turns.record_stream(st)
+        self._stream, self._raw = st, raw
 
-class Batch:
+
+class Batch(_OnStream):
     """The device arrays of one forward (odb_paged_batch); arrays that a call needs and that are not given are made here,
     those that are given are used as they are: int32, contiguous, on the cache's device.  max_rows: rows of the forward
     (known where row arrays are given); max_new: rows of the longest request, a hint that picks the attention's kernel (where
@@ -88,6 +113,7 @@ class Batch:
         for name in ("row_seq", "row_pos", "row_slot"):
             if given[name] is None:
                 given[name] = new(self.max_rows)
+        self._made(cache.device, *(t for t in given.values() if t is not None))
         for name, t in given.items():
             setattr(self, name, t)
         self.cache = cache
@@ -101,7 +127,7 @@ class Batch:
         self._lse = torch.Size((n, cache.n_heads))
 
 
-class PagedCache:
+class PagedCache(_OnStream):
     """A pool of K/V pages (bf16 [n_layers][2][n_pages][n_kv_heads][page_size][head_dim]) and the calls over it.  kv: a
     tensor of that shape to use; otherwise one is allocated (not cleared: what no request has written reaches no result)."""
 
@@ -121,11 +147,11 @@ class PagedCache:
         self.kv = kv
         self.device = kv.device
         self.workspace = torch.empty(lib.odb_paged_workspace_bytes(C.byref(self.cfg)), dtype=torch.uint8, device=self.device)
-        stream = torch.cuda.current_stream(self.device)
+        self._made(self.device, self.workspace, kv)
+        self._index = self.device.index
         with torch.cuda.device(self.device):
             B.check(lib.odb_paged_create(C.byref(self.cfg), kv.data_ptr(), kv.numel() * 2, self.workspace.data_ptr(),
-                                         self.workspace.numel(), C.c_void_p(stream.cuda_stream), C.byref(self.handle)), "odb_paged_create")
-        self._stream, self._raw, self._index = stream, stream.cuda_stream, self.device.index
+                                         self.workspace.numel(), C.c_void_p(self._raw), C.byref(self.handle)), "odb_paged_create")
         self._gain_shape = torch.Size((head_dim,))
         self._new, self._width = kv.new_empty, n_heads * head_dim       # outputs: bf16 on the cache's device (1.4 us; torch.empty 3.1)
         self._rows_c = B.odb_paged_rows()
@@ -137,14 +163,14 @@ class PagedCache:
             B.lib().odb_paged_destroy(self.handle)
             self.handle = C.c_void_p()
 
-    def _current(self) -> int:
-        """The current stream's handle; behind a call on another stream, that one's work comes first."""
-        raw = torch._C._cuda_getCurrentRawStream(self._index)
-        if raw != self._raw:
+    def _current(self, a, b) -> int:
+        """The current stream's handle; it follows the streams that the cache and the objects a and b used with it come from."""
+        raw = _raw_stream(self._index)
+        if (raw != self._raw or raw != a._raw or raw != b._raw) and not torch.cuda.is_current_stream_capturing():
             st = torch.cuda.current_stream(self.device)
-            if not torch.cuda.is_current_stream_capturing():
-                st.wait_stream(self._stream)
-            self._stream, self._raw = st, raw
+            for x in (self, a, b):
+                if raw != x._raw:
+                    x._follow(st, raw)
         return raw
 
     def _wrong(self, t, what: str, heads: int, rows: int):
@@ -176,7 +202,7 @@ class PagedCache:
 
     def layout(self, batch: Batch):
         """Block tables, free list and row maps of the forward (odb_paged_layout); the batch's arrays are updated."""
-        status = self._layout(self.handle, batch._ref, self._current())
+        status = self._layout(self.handle, batch._ref, self._current(batch, batch))
         if status:
             raise B.OdbError(status, "odb_paged_layout")
 
@@ -195,7 +221,7 @@ class PagedCache:
         else:
             op, os_ = (qp, qs) if q_out is q else self._rows(q_out, "q_out", self.n_heads, batch._q)
         _ROWS.pack_into(self._rows_c, 0, qp, qs, kp, ks, vp, vs, op, os_, self._gain(q_gain, "q_gain"), self._gain(k_gain, "k_gain"))
-        status = self._store(self.handle, layer, batch._ref, self._rows_ref, rope._ref, eps, self._current())
+        status = self._store(self.handle, layer, batch._ref, self._rows_ref, rope._ref, eps, self._current(batch, rope))
         if status:
             raise B.OdbError(status, "odb_paged_norm_rope_store")
         return q_out
@@ -216,11 +242,11 @@ class PagedCache:
             if lse.dtype is not _F32 or lse.get_device() != self._index or lse.shape != batch._lse or not lse.is_contiguous():
                 raise ValueError(f"lse: a contiguous float32 tensor {list(batch._lse)} on {self.device} is wanted")
             lp = lse.data_ptr()
-        status = self._attention(self.handle, layer, batch._ref, qp, qs, op, os_, lp, scale, left, right, sinks, self._current())
+        status = self._attention(self.handle, layer, batch._ref, qp, qs, op, os_, lp, scale, left, right, sinks, self._current(batch, batch))
         if status:
             raise B.OdbError(status, "odb_paged_attention")
         return out
 
     def status(self) -> int:
         """Waits for the current stream; ODB_OK or what the device has found since the last call (read and cleared)."""
-        return B.lib().odb_paged_status(self.handle, self._current())
+        return B.lib().odb_paged_status(self.handle, self._current(self, self))

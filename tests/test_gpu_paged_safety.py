@@ -60,3 +60,110 @@ def test_a_row_start_that_does_not_ascend_is_no_work_and_leaves_nothing_behind(D
             assert torch.equal(cache.attention(0, b, q, right=0, lse=lse), want) and torch.equal(lse, want_lse), name
         assert cache.status() == B.ODB_OK
     cache.close()
+
+
+# ---- streams and memory -----------------------------------------------------------------------------------------------
+
+def _delay():
+    torch.cuda._sleep(400_000_000)                                # some 0.2 s of the current stream
+
+
+def _forward(cache, page=16):
+    """A small forward over the cache, everything but the cache itself made on the current stream: (batch, rope, qkv)."""
+    P = paged()
+    n, H, KV, D = 40, cache.n_heads, cache.n_kv_heads, cache.head_dim
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    table = torch.full((1, 4), -1, dtype=torch.int32, device="cuda")
+    free = torch.arange(cache.n_pages, dtype=torch.int32, device="cuda")
+    batch = P.Batch(cache, table=table, free_pages=free, len_before=i32([0]), len_after=i32([n]), first=i32([0]), count=i32([n]), max_rows=n)
+    qkv = torch.randn(n, (H + 2 * KV) * D, generator=g, device="cuda").to(torch.bfloat16)
+    return batch, P.Rope(D), qkv
+
+
+def _run(cache, batch, rope, qkv):
+    cache.layout(batch)
+    a, c = cache.n_heads * cache.head_dim, (cache.n_heads + cache.n_kv_heads) * cache.head_dim
+    q = cache.norm_rope_store(0, batch, qkv[:, :a], qkv[:, a:c], qkv[:, c:], rope)
+    return cache.attention(0, batch, q, right=0)
+
+
+@requires_gpu
+def test_memory_of_a_cache_a_batch_and_a_rope_is_not_given_back_before_another_stream_is_done_with_it():
+    P = paged()
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(one):
+        cache = P.PagedCache(1, 4, 2, 64, 16, 1024)
+        batch, rope, qkv = _forward(cache)
+        want = _run(cache, batch, rope, qkv)
+    torch.full((1,), 255, dtype=torch.uint8, device="cuda")      # loads the kernel: that may wait for the device
+    torch.cuda._sleep(1)
+    torch.cuda.synchronize()
+    mine = {"workspace": cache.workspace, "kv": cache.kv, "row_start": batch.row_start, "row_seq": batch.row_seq, "row_pos": batch.row_pos,
+            "row_slot": batch.row_slot, "turns": rope.turns}
+    sizes = {name: (t.numel() * t.element_size(), t.data_ptr()) for name, t in mine.items()}
+    del mine
+    with torch.cuda.stream(two):
+        batch.len_before.fill_(40)                               # its pages are held: the layout changes nothing
+        _delay()
+        got = _run(cache, batch, rope, qkv)
+    cache.close()
+    del cache, batch, rope
+    with torch.cuda.stream(one):                                 # stream two has not begun: none of that memory may come back
+        taken = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n, _ in sizes.values() for _ in range(3)]
+    assert not two.query()
+    spans = [(t.data_ptr(), t.data_ptr() + t.numel()) for t in taken]
+    for name, (n, p) in sizes.items():
+        assert all(p + n <= a or b <= p for a, b in spans), name
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+
+
+@requires_gpu
+def test_a_call_waits_for_the_stream_its_batch_was_used_on():
+    """Two caches share a forward's maps: what the first one's layout writes on its stream the second one reads on another."""
+    P = paged()
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    a, b = (P.PagedCache(1, 4, 2, 64, 16, 8, kv=torch.zeros(1, 2, 8, 2, 16, 64, dtype=torch.bfloat16, device="cuda")) for _ in range(2))
+    batch, rope, qkv = _forward(a)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(two):
+        b.status()
+    with torch.cuda.stream(one):
+        a.status()
+        batch.row_pos.fill_(-1)
+        batch.row_slot.fill_(-1)
+        _delay()
+        a.layout(batch)
+    with torch.cuda.stream(two):
+        q = b.norm_rope_store(0, batch, qkv[:, :256], qkv[:, 256:384], qkv[:, 384:], rope)
+        out = b.attention(0, batch, q, right=0)
+    torch.cuda.synchronize()
+    batch.len_before.fill_(40)
+    assert torch.equal(out, _run(a, batch, rope, qkv))
+    assert torch.equal(a.kv, b.kv)
+
+
+@requires_gpu
+def test_a_capture_leaves_the_order_of_the_calls_around_it():
+    """A call captured on another stream is no work of that stream: the next one still waits for the last that ran."""
+    P = paged()
+    one, two, three = torch.cuda.Stream(), torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(one):
+        cache = P.PagedCache(1, 4, 2, 64, 16, 8)
+        batch, rope, qkv = _forward(cache)
+        want = _run(cache, batch, rope, qkv)
+    torch.cuda.synchronize()
+    batch.len_before.fill_(40)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=two):
+        held = _run(cache, batch, rope, qkv)
+    assert cache._raw == one.cuda_stream
+    with torch.cuda.stream(three):
+        assert torch.equal(_run(cache, batch, rope, qkv), want)
+        assert cache._raw == batch._raw == three.cuda_stream
+    torch.cuda.synchronize()
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(held, want)
+    cache.close()
