@@ -75,8 +75,8 @@ class Rope(_OnStream):
 
 
 class Batch(_OnStream):
-    """The device arrays of one forward (odb_paged_batch); arrays that a call needs and that are not given are made here,
-    those that are given are used as they are: int32, contiguous, on the cache's device.  max_rows: rows of the forward
+    """The device arrays of one forward (odb_paged_batch); arrays that a call needs and that are not given are made here (without rows,
+    until layout fills them), those that are given are used as they are: int32, contiguous, on the cache's device.  max_rows: rows of the forward
     (known where row arrays are given); max_new: rows of the longest request, a hint that picks the attention's kernel (where
     not given, rows divided by requests)."""
 
@@ -107,12 +107,11 @@ class Batch(_OnStream):
         self.n_seqs = n_seqs
         self.max_rows = rows.pop() if rows else (max_rows or 0)
         self.max_new = -(-self.max_rows // max(1, n_seqs)) if max_new is None else max_new
-        new = lambda n: torch.empty(n, dtype=torch.int32, device=cache.device)
-        if given["row_start"] is None and seqs:
-            given["row_start"] = new(n_seqs + 1)
-        for name in ("row_seq", "row_pos", "row_slot"):
-            if given[name] is None:
-                given[name] = new(self.max_rows)
+        if row_start is None and seqs:
+            given["row_start"] = torch.zeros(n_seqs + 1, dtype=torch.int32, device=cache.device)
+        maps = [name for name in ("row_seq", "row_pos", "row_slot") if given[name] is None]
+        if maps:
+            given.update(zip(maps, torch.full((len(maps), self.max_rows), -1, dtype=torch.int32, device=cache.device)))
         self._made(cache.device, *(t for t in given.values() if t is not None))
         for name, t in given.items():
             setattr(self, name, t)

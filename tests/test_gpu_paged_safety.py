@@ -167,3 +167,41 @@ def test_a_capture_leaves_the_order_of_the_calls_around_it():
     torch.cuda.synchronize()
     assert torch.equal(held, want)
     cache.close()
+
+
+@requires_gpu
+def test_a_batch_without_a_layout_has_no_rows():
+    """What a batch makes itself holds nothing that was in that memory before."""
+    P = paged()
+    cache = P.PagedCache(1, 4, 2, 64, 16, 8, kv=torch.zeros(1, 2, 8, 2, 16, 64, dtype=torch.bfloat16, device="cuda"))
+    n = 24
+    for _ in range(40):                                          # what the allocator has next: plausible slots and row starts
+        torch.arange(n, dtype=torch.int32, device="cuda")
+    batch = P.Batch(cache, table=torch.zeros(n - 1, 1, dtype=torch.int32, device="cuda"), len_after=i32([16] * (n - 1)), first=i32([0] * (n - 1)), max_rows=n)
+    assert bool((batch.row_start == 0).all()) and all(bool((t == -1).all()) and t.shape == (n,) for t in (batch.row_seq, batch.row_pos, batch.row_slot))
+    x = torch.ones(n, 8 * 64, dtype=torch.bfloat16, device="cuda")
+    out = torch.full((n, 4, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    cache.norm_rope_store(0, batch, x[:, :256], x[:, 256:384], x[:, 384:], P.Rope(64), q_out=out)
+    cache.attention(0, batch, x[:, :256], out=out)
+    assert bool((out == 3.0).all()) and bool((cache.kv == 0).all()) and cache.status() == 0
+    cache.close()
+
+
+@requires_gpu
+def test_a_layout_comes_behind_the_making_of_its_batch_on_another_stream():
+    P = paged()
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    cache = P.PagedCache(1, 4, 2, 64, 16, 8)
+    ints = [i32(v) for v in ([0], [40], [0], [40])]
+    table, free = torch.full((1, 4), -1, dtype=torch.int32, device="cuda"), torch.arange(8, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(two):
+        cache.status()
+    with torch.cuda.stream(one):
+        _delay()
+        batch = P.Batch(cache, table=table, free_pages=free, **dict(zip(("len_before", "len_after", "first", "count"), ints)), max_rows=44)
+    with torch.cuda.stream(two):
+        cache.layout(batch)
+    torch.cuda.synchronize()
+    assert batch.row_start.cpu().tolist() == [0, 40] and batch.row_pos.cpu().tolist() == list(range(40)) + [-1] * 4
+    cache.close()
