@@ -546,7 +546,9 @@ cudaError_t launch_paged_attention(PagedAttnArgs a, const PagedMaps& maps, int h
     const long long tiles = (static_cast<long long>(a.table_stride) << a.page_shift) / kKT + 1 + kItem;
     const double units = static_cast<double>((static_cast<long long>(a.max_rows) * a.G + (kRows - 1ll) * a.n_seqs) / kRows) * a.KV *
                          static_cast<double>(tiles);
-    if (rows > kRows && units > kSmallUnits && a.G <= kPagedTcMaxGroup) {
+    // the many rows' kernel keeps a row's place within its Q tile in 32 bits, in units of 8 elements
+    const bool near = a.out_stride <= 1ll << 27;
+    if (rows > kRows && units > kSmallUnits && a.G <= kPagedTcMaxGroup && near) {
         const bool alike = static_cast<long long>(max_new) * a.n_seqs <= 3ll * a.max_rows;
         return launch_paged_attention_tc(a, maps, hd, rows > 128 && alike ? 2 : 1, sms, st);
     }

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from gpu_common import requires_gpu
-from test_gpu_paged import _setup, dev, paged
+from test_gpu_paged import _check, _setup, dev, paged
 
 
 def binding():
@@ -204,4 +204,25 @@ def test_a_layout_comes_behind_the_making_of_its_batch_on_another_stream():
         cache.layout(batch)
     torch.cuda.synchronize()
     assert batch.row_start.cpu().tolist() == [0, 40] and batch.row_pos.cpu().tolist() == list(range(40)) + [-1] * 4
+    cache.close()
+
+
+# ---- rows far apart ---------------------------------------------------------------------------------------------------
+
+@requires_gpu
+@pytest.mark.parametrize("rows,stride", [(17, 1 << 30), (100, (1 << 27) + 8), (100, 1 << 27)])
+def test_attention_writes_rows_that_are_far_apart(rows, stride):
+    """A row's offset within its tile passes 2^31 pieces of 16 bytes (34 GB from the first row to the last)."""
+    if torch.cuda.mem_get_info()[0] < 45 << 30:
+        pytest.skip("45 GB of free memory are wanted")
+    rng = np.random.default_rng(6)
+    cache, b, q, qf, keys, values, start = _setup(rng, [300], [rows], [300 - rows], 2, 2, 64, 16, columns=5000)
+    wide = torch.empty((rows - 1) * stride + 128, dtype=torch.bfloat16, device="cuda")
+    out = wide.as_strided((rows, 128), (stride, 1))
+    out.fill_(3.0)
+    cache.attention(0, b, q, right=0, out=out)
+    assert cache.status() == 0
+    _check(out.reshape(rows, 2, 64), None, qf, keys, values, start, [300 - rows], 64, right=0)
+    del wide, out
+    torch.cuda.empty_cache()
     cache.close()
