@@ -76,9 +76,9 @@ class Rope(_OnStream):
 
 class Batch(_OnStream):
     """The device arrays of one forward (odb_paged_batch); arrays that a call needs and that are not given are made here (without rows,
-    until layout fills them), those that are given are used as they are: int32, contiguous, on the cache's device.  max_rows: rows of the forward
-    (known where row arrays are given); max_new: rows of the longest request, a hint that picks the attention's kernel (where
-    not given, rows divided by requests)."""
+    until layout fills them), those that are given are used as they are: int32, contiguous, on the cache's device.  It serves every
+    cache of the same device, pages and heads.  max_rows: rows of the forward (known where row arrays are given); max_new: rows of
+    the longest request, a hint that picks the attention's kernel (where not given, rows divided by requests)."""
 
     _INPUTS = ("len_before", "len_after", "first", "count", "table", "free_pages", "row_start", "row_seq", "row_pos", "row_slot")
 
@@ -151,6 +151,7 @@ class PagedCache(_OnStream):
         with torch.cuda.device(self.device):
             B.check(lib.odb_paged_create(C.byref(self.cfg), kv.data_ptr(), kv.numel() * 2, self.workspace.data_ptr(),
                                          self.workspace.numel(), C.c_void_p(self._raw), C.byref(self.handle)), "odb_paged_create")
+        self._shape = (self.device, n_heads, n_kv_heads, head_dim, page_size, n_pages)     # what a batch depends on
         self._gain_shape = torch.Size((head_dim,))
         self._new, self._width = kv.new_empty, n_heads * head_dim       # outputs: bf16 on the cache's device (1.4 us; torch.empty 3.1)
         self._rows_c = B.odb_paged_rows()
@@ -171,6 +172,11 @@ class PagedCache(_OnStream):
                 if raw != x._raw:
                     x._follow(st, raw)
         return raw
+
+    def _other(self, batch: Batch):
+        """A batch that was made for another cache: its tensors were checked against that one's pages and heads."""
+        if batch.cache._shape != self._shape:
+            raise ValueError("the batch was made for a cache of other pages, heads or device")
 
     def _wrong(self, t, what: str, heads: int, rows: int):
         if not isinstance(t, torch.Tensor) or t.dtype is not torch.bfloat16 or t.device != self.device:
@@ -201,6 +207,8 @@ class PagedCache(_OnStream):
 
     def layout(self, batch: Batch):
         """Block tables, free list and row maps of the forward (odb_paged_layout); the batch's arrays are updated."""
+        if batch.cache is not self:
+            self._other(batch)
         status = self._layout(self.handle, batch._ref, self._current(batch, batch))
         if status:
             raise B.OdbError(status, "odb_paged_layout")
@@ -209,6 +217,8 @@ class PagedCache(_OnStream):
         """Norm of every q and k head (where a gain is given), rotation by row_pos, K and V into row_slot
         (odb_paged_norm_rope_store).  q, k, v: [max_rows][heads][head_dim] or [max_rows][heads * head_dim], slices of one
         projection's output as they are.  Returns q_out (a new tensor where none is given; q itself may be given)."""
+        if batch.cache is not self:
+            self._other(batch)
         if rope.index != self._index:
             raise ValueError(f"rope: on {self.device} it is wanted")
         qp, qs = self._rows(q, "q", self.n_heads, batch._q)
@@ -230,6 +240,8 @@ class PagedCache(_OnStream):
         keys j < len_after with j <= p + right and (j >= p - left or j < sinks); -1: no limit; causal: right=0.
         scale 0: 1 / sqrt(head_dim).  lse: float32 [max_rows][n_heads] to be filled.  Returns out (a new tensor where none
         is given)."""
+        if batch.cache is not self:
+            self._other(batch)
         qp, qs = self._rows(q, "q", self.n_heads, batch._q)
         if out is None:
             out = self._new(batch.max_rows, self.n_heads, self.head_dim)

@@ -226,3 +226,27 @@ def test_attention_writes_rows_that_are_far_apart(rows, stride):
     del wide, out
     torch.cuda.empty_cache()
     cache.close()
+
+
+# ---- a batch of another cache -----------------------------------------------------------------------------------------
+
+@requires_gpu
+def test_a_batch_made_for_a_cache_of_other_pages_or_heads_is_refused():
+    """Its arrays were checked against that cache: a free list of fewer pages, tensors of fewer heads would be passed on unseen."""
+    P = paged()
+    first = P.PagedCache(1, 4, 2, 64, 16, 8)
+    batch, rope, qkv = _forward(first)
+    q, k, v = qkv[:, :256], qkv[:, 256:384], qkv[:, 384:]
+    for other in (dict(n_pages=9), dict(n_pages=7), dict(n_heads=8), dict(n_kv_heads=4), dict(head_dim=128), dict(page_size=32)):
+        cache = P.PagedCache(**(dict(n_layers=1, n_heads=4, n_kv_heads=2, head_dim=64, page_size=16, n_pages=8) | other))
+        for call in (lambda: cache.layout(batch), lambda: cache.norm_rope_store(0, batch, q, k, v, rope), lambda: cache.attention(0, batch, q)):
+            with pytest.raises(ValueError):
+                call()
+        assert cache.status() == 0
+        cache.close()
+    like = P.PagedCache(3, 4, 2, 64, 16, 8)                       # another number of layers
+    want = _run(first, batch, rope, qkv)
+    batch.len_before.fill_(40)
+    assert torch.equal(_run(like, batch, rope, qkv), want)
+    like.close()
+    first.close()
