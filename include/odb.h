@@ -472,7 +472,8 @@ int32_t odb_rope_frequencies(int32_t rot_dim, double theta, int32_t scaling, dou
                              double beta_fast, uint64_t* turns_host, float* magnitude);
 
 /* What norm_rope_store reads and writes: bf16 rows on 8-byte boundaries, strides in elements between rows (multiples of 4;
- * q, k and v may be slices of one projection's output).  q_out may be q itself (same stride). */
+ * q, k and v may be slices of one projection's output).  q_out may be q itself (same stride); rows of it that overlap those of q, k or v
+ * in any other way are refused (ODB_ERR_ARG). */
 typedef struct odb_paged_rows {
     const void* q; int64_t q_stride;            /* [max_rows][n_heads][head_dim] */
     const void* k; int64_t k_stride;            /* [max_rows][n_kv_heads][head_dim] */
@@ -503,7 +504,7 @@ int32_t odb_paged_norm_rope_store(odb_paged* h, int32_t layer, const odb_paged_b
  * 1 / sqrt(head_dim).  lse (fp32 [max_rows][n_heads], may be NULL): ln of the sum of exponentials.  A row that sees no key
  * gets zeros and -infinity.  What pages hold at positions nobody sees never reaches a result, not even as NaN.
  * Reads len_after, first, row_start, table; rows from row_start[n_seqs] on are left as they are.  q and out on 16-byte
- * boundaries with row strides that are multiples of 8 elements; out must not overlap q.  Fixed order of sums: the same
+ * boundaries with row strides that are multiples of 8 elements; rows of out that overlap rows of q are refused (ODB_ERR_ARG).  Fixed order of sums: the same
  * call gives the same bits. */
 int32_t odb_paged_attention(odb_paged* h, int32_t layer, const odb_paged_batch* b, const void* q, int64_t q_stride, void* out,
                             int64_t out_stride, float* lse, float scale, int32_t left, int32_t right, int32_t sinks, void* stream);

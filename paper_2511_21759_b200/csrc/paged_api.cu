@@ -48,6 +48,30 @@ int32_t check_call(const odb_paged* h, int32_t layer) {
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
+// Rows of `width` elements of bf16, `stride` apart.
+struct Rows {
+    const void* at;
+    int64_t stride, width;
+};
+// Whether n rows of each have a byte in common (rows of one tensor's slices lie between one another without that).  A row at `from` bytes
+// behind b's first meets row k of b where from - (b's width) < k * (b's stride) < from + (a's width).
+bool overlap(const Rows& a, const Rows& b, int32_t n) {
+    typedef __int128 wide;                                  // strides are the caller's numbers
+    const wide sa = 2 * static_cast<wide>(a.stride), sb = 2 * static_cast<wide>(b.stride), wa = 2 * a.width, wb = 2 * b.width, last = n - 1;
+    const wide from = static_cast<wide>(reinterpret_cast<uintptr_t>(a.at)) - static_cast<wide>(reinterpret_cast<uintptr_t>(b.at));
+    auto meets = [&](wide d, wide lo, wide hi) {            // some row k of b with lo <= k <= hi
+        const wide x = d + wa - 1;
+        wide k = x >= 0 ? x / sb : -((sb - 1 - x) / sb);    // the largest k with k * sb <= x
+        if (k > hi) k = hi;
+        return k >= lo && k * sb > d - wb;
+    };
+    if (from + last * sa + wa <= 0 || from >= last * sb + wb) return false;
+    if (sa == sb) return meets(from, -last, last);
+    for (int32_t i = 0; i < n; ++i)
+        if (meets(from + i * sa, 0, last)) return true;
+    return false;
+}
+
 int32_t enqueued(cudaError_t e) { return e == cudaSuccess ? ODB_OK : record_cuda_error(e); }
 
 }  // namespace
@@ -168,6 +192,11 @@ int32_t odb_paged_norm_rope_store(odb_paged* h, int32_t layer, const odb_paged_b
     if (!aligned(r->q, 8) || !aligned(r->k, 8) || !aligned(r->v, 8) || !aligned(r->q_out, 8) || !aligned(r->q_gain, 16) || !aligned(r->k_gain, 16) ||
         !aligned(rope->turns, 16) || ((r->q_stride | r->k_stride | r->v_stride | r->out_stride) & 3))
         return ODB_ERR_ARG;
+    // other blocks read their rows after the first have written
+    const Rows out{r->q_out, r->out_stride, qw};
+    if (((r->q_out != r->q || r->out_stride != r->q_stride) && overlap(out, {r->q, r->q_stride, qw}, b->max_rows)) ||
+        overlap(out, {r->k, r->k_stride, kw}, b->max_rows) || overlap(out, {r->v, r->v_stride, kw}, b->max_rows))
+        return ODB_ERR_ARG;
     if (static_cast<double>(b->max_rows) * (c.n_heads + 2 * c.n_kv_heads) >= 2147483648.0) return ODB_ERR_SHAPE;
     PagedStoreArgs a{};
     a.q = static_cast<const __nv_bfloat16*>(r->q);
@@ -199,6 +228,7 @@ int32_t odb_paged_attention(odb_paged* h, int32_t layer, const odb_paged_batch* 
     if (!q || !out || !b->len_after || !b->first || !b->row_start || !b->table) return ODB_ERR_ARG;
     const int64_t qw = static_cast<int64_t>(c.n_heads) * c.head_dim;
     if (q_stride < qw || out_stride < qw || ((q_stride | out_stride) & 7) || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4)) return ODB_ERR_ARG;
+    if (overlap({out, out_stride, qw}, {q, q_stride, qw}, b->max_rows)) return ODB_ERR_ARG;   // some CTAs read Q after others have written
     // sums of row tiles over the requests and of key tiles over the row tiles and heads are 32-bit numbers
     const int G = c.n_heads / c.n_kv_heads;
     const double tiles = static_cast<double>(b->max_rows) * G / 16 + 1;

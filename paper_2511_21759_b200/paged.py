@@ -216,7 +216,8 @@ class PagedCache(_OnStream):
     def norm_rope_store(self, layer: int, batch: Batch, q, k, v, rope: Rope, *, q_gain=None, k_gain=None, eps: float = 1e-6, q_out=None):
         """Norm of every q and k head (where a gain is given), rotation by row_pos, K and V into row_slot
         (odb_paged_norm_rope_store).  q, k, v: [max_rows][heads][head_dim] or [max_rows][heads * head_dim], slices of one
-        projection's output as they are.  Returns q_out (a new tensor where none is given; q itself may be given)."""
+        projection's output as they are.  Returns q_out (a new tensor where none is given; q itself may be given, other rows that overlap
+        q, k or v are refused)."""
         if batch.cache is not self:
             self._other(batch)
         if rope.index != self._index:
@@ -239,7 +240,7 @@ class PagedCache(_OnStream):
         """Attention of the batch's rows over their requests' pages (odb_paged_attention): a row at position p sees the
         keys j < len_after with j <= p + right and (j >= p - left or j < sinks); -1: no limit; causal: right=0.
         scale 0: 1 / sqrt(head_dim).  lse: float32 [max_rows][n_heads] to be filled.  Returns out (a new tensor where none
-        is given)."""
+        is given; one whose rows overlap q's is refused)."""
         if batch.cache is not self:
             self._other(batch)
         qp, qs = self._rows(q, "q", self.n_heads, batch._q)

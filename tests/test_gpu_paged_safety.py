@@ -250,3 +250,71 @@ def test_a_batch_made_for_a_cache_of_other_pages_or_heads_is_refused():
     assert torch.equal(_run(like, batch, rope, qkv), want)
     like.close()
     first.close()
+
+
+# ---- outputs that overlap inputs --------------------------------------------------------------------------------------
+
+def _spans(t):
+    """The bytes of a [rows][width] bf16 tensor, by rows."""
+    return {(t.data_ptr() + 2 * r * t.stride(0) + 2 * i) for r in range(t.shape[0]) for i in range(t.shape[1])}
+
+
+def _views(flat, rows, width, unit):
+    """[rows][width] views of a buffer at offsets and strides that are multiples of `unit` elements, those on their own and those between others'."""
+    for stride in (width, width + unit, width + 2 * unit, 2 * width, 2 * width + unit, 3 * width):
+        for offset in (0, unit, 2 * unit, width - unit, width, width + unit, 2 * width, 2 * width + unit, rows * width, rows * width - unit, 3 * rows * width):
+            if offset + (rows - 1) * stride + width <= flat.numel():
+                yield flat.as_strided((rows, width), (stride, 1), offset)
+
+
+@requires_gpu
+@pytest.mark.parametrize("rows", [1, 2, 5])
+def test_attention_refuses_an_output_that_overlaps_its_queries_and_no_other(rows):
+    B = binding()
+    rng = np.random.default_rng(14)
+    cache, b, q0, *_ = _setup(rng, [60], [rows], [60 - rows], 1, 1, 64, 16)
+    want = cache.attention(0, b, q0, right=0).view(rows, 64)
+    flat = torch.zeros(8 * rows * 64, dtype=torch.bfloat16, device="cuda")
+    seen = {True: 0, False: 0}
+    for q in _views(flat, rows, 64, 8):
+        for out in _views(flat, rows, 64, 8):
+            q.copy_(q0.view(rows, 64))
+            clash = bool(_spans(q) & _spans(out))
+            seen[clash] += 1
+            if clash:
+                with pytest.raises(B.OdbError) as e:
+                    cache.attention(0, b, q, right=0, out=out)
+                assert e.value.status == B.ODB_ERR_ARG
+            else:
+                cache.attention(0, b, q, right=0, out=out)
+                assert torch.equal(out, want) and torch.equal(q, q0.view(rows, 64))
+    assert min(seen.values()) > 20
+    cache.close()
+
+
+@requires_gpu
+def test_norm_rope_store_refuses_an_output_that_overlaps_its_inputs_but_for_q_itself():
+    P, B = paged(), binding()
+    cache = P.PagedCache(1, 1, 1, 64, 16, 4)
+    rows = 3
+    b = P.Batch(cache, row_pos=i32([5, 6, 7]), row_slot=i32([5, 6, 7]))
+    rope = P.Rope(64)
+    flat = torch.zeros(8 * rows * 64, dtype=torch.bfloat16, device="cuda")
+    other = torch.ones(rows, 64, dtype=torch.bfloat16, device="cuda")
+    x = torch.randn(rows, 64, device="cuda").to(torch.bfloat16)
+    want = cache.norm_rope_store(0, b, x, other, other, rope).view(rows, 64)
+    for source in _views(flat, rows, 64, 4):
+        for out in _views(flat, rows, 64, 4):
+            same = source.data_ptr() == out.data_ptr() and source.stride() == out.stride()
+            clash = bool(_spans(source) & _spans(out))
+            for at in "qkv":
+                source.copy_(x)
+                args = [source if n == at else x if n == "q" else other for n in "qkv"]
+                if clash and not (same and at == "q"):
+                    with pytest.raises(B.OdbError) as e:
+                        cache.norm_rope_store(0, b, *args, rope, q_out=out)
+                    assert e.value.status == B.ODB_ERR_ARG
+                else:
+                    cache.norm_rope_store(0, b, *args, rope, q_out=out)
+                    assert torch.equal(out, want)
+    cache.close()
