@@ -447,10 +447,16 @@ size_t odb_paged_workspace_bytes(const odb_paged_config* cfg);
 int32_t odb_paged_create(const odb_paged_config* cfg, void* kv, size_t kv_bytes, void* workspace, size_t ws_bytes, void* stream,
                          odb_paged** out);
 int32_t odb_paged_destroy(odb_paged* h);
-/* Reads and clears the status word: ODB_OK, or what a call on the device found since - ODB_ERR_ARG (lengths or rows that
- * are negative, too long for a table row, or behind the length; in the attention a row_start that does not ascend from 0 or more to
- * max_rows or less: such a call writes nothing), ODB_ERR_WORKSPACE (the pool has too few pages),
- * ODB_ERR_SHAPE (more rows than max_rows), ODB_ERR_STATE (a page id that is none), ODB_ERR_TIMEOUT.  Synchronous. */
+/* Reads and clears the status word: ODB_OK, or the last of what calls on the device found since.  Synchronous.
+ *   ODB_ERR_ARG        layout: lengths or rows that are negative, too long for a table row, or behind the length; attention: a
+ *                      length that is negative or too long (it is cut to what the table has), or a row_start that does not ascend
+ *                      from 0 or more to max_rows or less (nothing is written)
+ *   ODB_ERR_WORKSPACE  layout: the pool has too few pages
+ *   ODB_ERR_SHAPE      layout: more rows than max_rows
+ *   ODB_ERR_STATE      a page id that is none: layout, of a row's position (it gets no slot); attention, of a position that some row
+ *                      sees (read as zeros)
+ *   ODB_ERR_TIMEOUT    a wait on the device ran out
+ * norm_rope_store records nothing: a slot that is none is a row that is not stored. */
 int32_t odb_paged_status(odb_paged* h, void* stream);
 
 /* Tables and maps of the forward: every request's table grows or shrinks from ceil(len_before / page_size) to

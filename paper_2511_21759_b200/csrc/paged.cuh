@@ -125,6 +125,12 @@ __device__ __forceinline__ bool paged_rows_follow(const PagedAttnArgs& a, int s)
     return 0 <= r0 && r0 <= r1 && r1 <= a.max_rows;
 }
 
+// The length is one that the table has entries for (where not, it is cut, and the status word says so).
+__device__ __forceinline__ bool paged_length_fits(const PagedAttnArgs& a, int s) {
+    const int len = a.len[s];
+    return 0 <= len && len <= a.table_stride << a.page_shift;
+}
+
 // The key tiles of a row tile: `sink_tiles` from the front, the others from tile `first_tile` on; `n` of them, at least
 // one (an item without a visible key still writes its rows).  Positions from `hi` on are seen by no row, nor are those
 // of [sinks, lo).
@@ -275,6 +281,7 @@ __device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int w
         if (s < a.n_seqs) {
             const PagedSeq q = paged_seq(a, s);
             wrong = !paged_rows_follow(a, s);
+            if (blockIdx.x == 0 && tid < 32 && !paged_length_fits(a, s)) atomicExch(a.status, ODB_ERR_ARG);
             n_rt = q.n_rt;
             if (n_rt > 0) units = paged_keys<KT>(a, q, 0).n + E;
         }
@@ -300,6 +307,7 @@ __device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int w
     for (int s = s0; s < s1; ++s) {
         const PagedSeq q = paged_seq(a, s);
         wrong = wrong || !paged_rows_follow(a, s);
+        if (blockIdx.x == 0 && !paged_length_fits(a, s)) atomicExch(a.status, ODB_ERR_ARG);
         sc.seq[s] = make_int4(q.row0, q.n, q.first, q.len);
         mine_rt += q.n_rt;
         several = several || q.n_rt > 1;
@@ -429,6 +437,12 @@ struct PagedPages {
         return page >= 0 && page < a.n_pages ? base + ((page * a.KV + head) << a.page_shift) + (pos & ((1 << a.page_shift) - 1)) : a.pool_rows;
     }
 };
+
+// Positions pos .. pos + n - 1 of an item, the first of them below the keys' end, lie in a page that is none: an error where some row
+// sees one of them (the page in front of a window may be gone).
+__device__ __forceinline__ void paged_no_page(const PagedAttnArgs& a, const PagedKeys& k, int pos, int n) {
+    if ((min(pos + n, k.hi) > k.lo || pos < a.sinks) && (threadIdx.x & 31) == 0) atomicExch(a.status, ODB_ERR_STATE);
+}
 
 // One lane of a converged warp.  TMA copies and MMAs take their operands from uniform registers: behind elect, with operands that
 // every lane has, they follow one another without a detour (behind `lane == 0` an MMA took 110 cycles to issue, and one of

@@ -156,6 +156,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                     __syncwarp();
                     for (int c = 0; c < boxes; ++c) {
                         const int row = pages.row(a, w.seq, w.head, k0 + (c << box_shift), base);
+                        if (row == a.pool_rows) paged_no_page(a, w.k, k0 + (c << box_shift), box);
                         if (paged_elect()) tma_rows(to + c * box * HD * 2, &tm, &full[slot], row);
                         __syncwarp();
                     }

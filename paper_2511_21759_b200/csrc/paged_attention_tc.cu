@@ -329,6 +329,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
             const uint32_t dst = x.at + x.slot * kT;
             uint64_t* bar = &x.full[x.slot];
             if (box == kKT) {
+                if (row == a.pool_rows && keys > 0) paged_no_page(a, x.w.k, k0, kKT);
                 if (paged_elect()) {
                     mbar_expect_tx(bar, keys > 0 ? kT : 0u);
                     if (keys > 0) tma_box_3d(dst, &tm_rows, bar, 0, row, 0);
@@ -340,6 +341,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                 __syncwarp();
                 for (int c = 0; c < boxes; ++c) {
                     const int row_c = x.pages.row(a, x.w.seq, x.w.head, k0 + (c << box_shift), x.base);
+                    if (row_c == a.pool_rows) paged_no_page(a, x.w.k, k0 + (c << box_shift), box);
                     if (paged_elect()) {
 #pragma unroll
                         for (int at = 0; at < kAtoms; ++at) tma_box_3d(dst + at * kKT * 128 + c * box * 128, &tm_atoms, bar, 0, row_c, at);

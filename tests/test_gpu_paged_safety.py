@@ -318,3 +318,81 @@ def test_norm_rope_store_refuses_an_output_that_overlaps_its_inputs_but_for_q_it
                     cache.norm_rope_store(0, b, *args, rope, q_out=out)
                     assert torch.equal(out, want)
     cache.close()
+
+
+# ---- what the attention's tables and lengths lead to ------------------------------------------------------------------
+
+WINDOW = dict(left=40, right=0, sinks=3)
+
+
+@requires_gpu
+@pytest.mark.parametrize("columns", [1, 5000])
+@pytest.mark.parametrize("page", [16, 64, 128])
+@pytest.mark.parametrize("new", [1, 9, 60])
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_page_that_is_none_sets_the_status_word_where_some_row_sees_it(D, new, page, columns):
+    B = binding()
+    rng = np.random.default_rng(new + page)
+    n = 700
+    cache, b, q, *_ = _setup(rng, [n, 80], [new, 1], [n - new, 79], 4, 1, D, page, columns=columns)
+    table = b.table.clone()
+    for mask in (dict(right=0), WINDOW):
+        want = cache.attention(0, b, q, **mask)
+        assert cache.status() == B.ODB_OK
+        lo = n - new - 40                                        # the first position that the window lets some row see
+        for p in range(-(-n // page)):
+            for none in (-1, cache.n_pages, 2 ** 31 - 1):
+                b.table.copy_(table)
+                b.table[0, p] = none
+                got = cache.attention(0, b, q, **mask)
+                seen = "left" not in mask or p == 0 or (p + 1) * page > lo
+                assert cache.status() == (B.ODB_ERR_STATE if seen else B.ODB_OK), (p, none)
+                if not seen:
+                    assert torch.equal(got, want), p
+                elif none == -1:                                 # zeros: as if the page were there and cleared
+                    b.table.copy_(table)
+                    keep = cache.kv[0, :, table[0, p]].clone()
+                    cache.kv[0, :, table[0, p]] = 0
+                    assert torch.equal(got, cache.attention(0, b, q, **mask)), p
+                    cache.kv[0, :, table[0, p]] = keep
+        b.table.copy_(table)
+        cache.status()
+    cache.close()
+
+
+@requires_gpu
+@pytest.mark.parametrize("columns", [1, 5000])
+@pytest.mark.parametrize("new", [1, 20])
+def test_a_window_behind_the_keys_needs_the_pages_of_the_sinks_only(new, columns):
+    """Rows at positions whose window begins behind the last key: the pages between the sinks and the end may be gone."""
+    B = binding()
+    rng = np.random.default_rng(new)
+    cache, b, q, *_ = _setup(rng, [40], [new], [200], 4, 1, 64, 16, columns=columns)
+    want = cache.attention(0, b, q, **WINDOW)
+    b.table[0, 1:3] = -1
+    assert torch.equal(cache.attention(0, b, q, **WINDOW), want) and cache.status() == B.ODB_OK
+    b.table[0, 0] = -1
+    assert bool((cache.attention(0, b, q, **WINDOW) == 0).all()) and cache.status() == B.ODB_ERR_STATE
+    cache.close()
+
+
+@requires_gpu
+@pytest.mark.parametrize("columns", [1, 5000])
+@pytest.mark.parametrize("seqs", [2, 40])
+@pytest.mark.parametrize("new", [1, 20])
+def test_a_length_that_the_table_has_no_entries_for_is_cut_and_sets_the_status_word(new, seqs, columns):
+    B = binding()
+    rng = np.random.default_rng(seqs)
+    n = 64
+    cache, b, q, *_ = _setup(rng, [n] * seqs, [new] * seqs, [n - new] * seqs, 4, 1, 64, 16, columns=columns)
+    b.table[:, 4:] = b.table[:, :1]                               # entries behind the length: pages all the same
+    width = b.table.shape[1] * 16
+    for len1, cut in ((width, width), (width + 1, width), (2 ** 31 - 1, width), (-1, 0), (-2 ** 31, 0)):
+        b.len_after.fill_(n)
+        b.len_after[seqs - 1] = cut
+        want = cache.attention(0, b, q, right=0)
+        assert cache.status() == B.ODB_OK
+        b.len_after[seqs - 1] = len1
+        assert torch.equal(cache.attention(0, b, q, right=0), want)
+        assert cache.status() == (B.ODB_OK if len1 == cut else B.ODB_ERR_ARG), len1
+    cache.close()
