@@ -409,7 +409,9 @@ double odb_step_algorithmic_bytes(const odb_config* cfg, int32_t keys);
  *
  * Requirements: head_dim in {64, 128}; n_heads a multiple of n_kv_heads, up to 1024; page_size a power of two, 16 ..
  * 1024; fewer than 2^31 slots and pool rows (n_layers * 2 * n_pages * n_kv_heads * page_size); up to 1024 requests in a
- * forward; table rows of less than 2^30 positions.
+ * forward; table rows of less than 2^30 positions; in an attention fewer than 2^31 - 65536 packed rows (max_rows * n_heads) and key
+ * tiles: (max_rows * group / R + n_seqs) * n_kv_heads * (positions of a table row / 64 + 4), R = 2 * group * floor(128 / group), or 16
+ * where a group has more than 128 heads (8 K/V heads of groups of four, a table row of a million positions: a million rows).
  *
  * A handle's calls go to the stream they are given and are asynchronous.  They share the handle's workspace: use one
  * stream at a time (calls on two streams have to be ordered by the caller).  They can be captured into a CUDA graph.

@@ -84,11 +84,14 @@ struct PagedAttnArgs {
 struct PagedMaps {
     CUtensorMap rows, atoms;
 };
-// max_new: rows of the longest request; a hint that picks the kernel
-cudaError_t launch_paged_attention(PagedAttnArgs a, const PagedMaps& maps, int hd, int max_new, int sms, cudaStream_t st);
+// The kernel of an attention over n_seqs requests with max_rows rows together, `longest` positions in a table row: 0 the few rows', 1 or 2
+// Q tiles of the many rows', -1: none, its sums would pass 32 bits.  max_new: rows of the longest request, a hint.
+int paged_attention_kernel_of(int n_seqs, int max_rows, int max_new, int group, int kv_heads, long long longest, long long out_stride);
+cudaError_t launch_paged_attention(PagedAttnArgs a, const PagedMaps& maps, int hd, int q_tiles, int sms, cudaStream_t st);
 // many packed rows on the tensor cores (paged_attention_tc.cu); q_tiles: Q tiles of 128 rows a CTA takes
 cudaError_t launch_paged_attention_tc(PagedAttnArgs a, const PagedMaps& maps, int hd, int q_tiles, int sms, cudaStream_t st);
 constexpr int kPagedTcMaxGroup = 128;   // heads of a group that fit a Q tile
+constexpr int kPagedTcItem = 3;         // key tiles that an item costs the many rows' kernel beside its own
 size_t paged_part_bytes(int hd);
 
 #ifdef __CUDACC__
@@ -251,7 +254,7 @@ __device__ __forceinline__ int paged_upper(const int* v, int n, int x) {   // th
 // waves: CTAs of the grid for each of the a.at_once that run at one time.  min_units: what a CTA takes at least (more than E);
 // full_units: what it takes at least as long as those have work.
 // The launcher's bounds on rows, requests and keys keep every sum below 2^31, as long as the requests' rows follow one another; where
-// they do not, the call has no work and the status word says so.  (Sums that are formed until that is known may wrap and lead nowhere.)
+// they do not, the call has no work and the status word says so.
 template <int THREADS, int KT, int E, bool WARPS>
 __device__ bool paged_find_start(const PagedAttnArgs& a, PagedScratch& sc, int waves, int min_units, int full_units, PagedStart& st) {
     const int tid = threadIdx.x;

@@ -229,12 +229,10 @@ int32_t odb_paged_attention(odb_paged* h, int32_t layer, const odb_paged_batch* 
     const int64_t qw = static_cast<int64_t>(c.n_heads) * c.head_dim;
     if (q_stride < qw || out_stride < qw || ((q_stride | out_stride) & 7) || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4)) return ODB_ERR_ARG;
     if (overlap({out, out_stride, qw}, {q, q_stride, qw}, b->max_rows)) return ODB_ERR_ARG;   // some CTAs read Q after others have written
-    // sums of row tiles over the requests and of key tiles over the row tiles and heads are 32-bit numbers
     const int G = c.n_heads / c.n_kv_heads;
-    const double tiles = static_cast<double>(b->max_rows) * G / 16 + 1;
-    if (static_cast<double>(b->max_rows) * c.n_heads >= 2147483648.0 || tiles * b->n_seqs >= 2147483648.0 ||
-        (tiles + b->n_seqs) * c.n_kv_heads * (longest / 64 + 8) >= 2147483648.0)
-        return ODB_ERR_SHAPE;
+    if (static_cast<double>(b->max_rows) * c.n_heads >= 2147483648.0 - 65536) return ODB_ERR_SHAPE;   // packed rows are 32-bit numbers
+    const int q_tiles = paged_attention_kernel_of(b->n_seqs, b->max_rows, b->max_new, G, c.n_kv_heads, longest, out_stride);
+    if (q_tiles < 0) return ODB_ERR_SHAPE;
     PagedAttnArgs a{};
     a.q = static_cast<const __nv_bfloat16*>(q);
     a.out = static_cast<__nv_bfloat16*>(out);
@@ -251,7 +249,7 @@ int32_t odb_paged_attention(odb_paged* h, int32_t layer, const odb_paged_batch* 
     a.scale_log2 = (scale != 0.f ? scale : 1.0f / sqrtf(static_cast<float>(c.head_dim))) * 1.4426950408889634f;
     a.status = h->status; a.arrivals = h->arrivals; a.part_o = h->part_o; a.part_ml = h->part_ml;
     a.shared = h->shared;
-    return enqueued(launch_paged_attention(a, h->maps, c.head_dim, b->max_new, h->sms, static_cast<cudaStream_t>(stream)));
+    return enqueued(launch_paged_attention(a, h->maps, c.head_dim, q_tiles, h->sms, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -540,19 +540,31 @@ size_t paged_part_bytes(int hd) { return static_cast<size_t>(kPagedMaxParts) * k
 // Two Q tiles take requests that are alike, the longest up to three times the mean: beside a prompt of 2048 rows 47 single tokens of up
 // to 8192 keys leave the second one empty, and two CTAs on an SM hide more: - / 169 / 220 (head dim 64: 127 / 173); 512 rows and 8 tokens
 // 50 / 63; 4096 rows and 8 tokens 180 / 172.
-cudaError_t launch_paged_attention(PagedAttnArgs a, const PagedMaps& maps, int hd, int max_new, int sms, cudaStream_t st) {
+int paged_attention_kernel_of(int n_seqs, int max_rows, int max_new, int group, int kv_heads, long long longest, long long out_stride) {
+    const long long all = static_cast<long long>(max_rows) * group, mine = static_cast<long long>(max_new) * group, tiles = longest / kKT + 1;
+    // units of all items together and what is added to them on the way, with rows that follow one another
+    auto fits = [&](int tile_rows, int item) {
+        return (static_cast<double>(all / tile_rows) + n_seqs) * kv_heads * static_cast<double>(tiles + item) < 2147483648.0 - 65536;
+    };
+    const bool few_fit = fits(kRows, kItem);
+    // the many rows' kernel keeps a row's place within its Q tile in 32 bits, in units of 8 elements
+    if (group <= kPagedTcMaxGroup && out_stride <= 1ll << 27) {
+        const int tile = kPagedTcMaxGroup / group * group;
+        const double units = static_cast<double>((all + (kRows - 1ll) * n_seqs) / kRows) * kv_heads * static_cast<double>(tiles + kItem);
+        if ((mine > kRows && units > kSmallUnits) || !few_fit) {
+            const bool alike = static_cast<long long>(max_new) * n_seqs <= 3ll * max_rows;
+            const int q_tiles = mine > 128 && alike ? 2 : 1;
+            if (fits(q_tiles * tile, kPagedTcItem)) return q_tiles;
+            return fits(2 * tile, kPagedTcItem) ? 2 : -1;
+        }
+    }
+    return few_fit ? 0 : -1;
+}
+
+cudaError_t launch_paged_attention(PagedAttnArgs a, const PagedMaps& maps, int hd, int q_tiles, int sms, cudaStream_t st) {
     if (sms < 1 || 2 * sms * 128 > kPagedPartRows || kPagedWaves * 2 * sms > kPagedMaxCtas) return cudaErrorInvalidValue;   // the workspace's size
     a.by_group = PagedDiv::by(a.G);
-    const long long rows = static_cast<long long>(max_new) * a.G;
-    const long long tiles = (static_cast<long long>(a.table_stride) << a.page_shift) / kKT + 1 + kItem;
-    const double units = static_cast<double>((static_cast<long long>(a.max_rows) * a.G + (kRows - 1ll) * a.n_seqs) / kRows) * a.KV *
-                         static_cast<double>(tiles);
-    // the many rows' kernel keeps a row's place within its Q tile in 32 bits, in units of 8 elements
-    const bool near = a.out_stride <= 1ll << 27;
-    if (rows > kRows && units > kSmallUnits && a.G <= kPagedTcMaxGroup && near) {
-        const bool alike = static_cast<long long>(max_new) * a.n_seqs <= 3ll * a.max_rows;
-        return launch_paged_attention_tc(a, maps, hd, rows > 128 && alike ? 2 : 1, sms, st);
-    }
+    if (q_tiles > 0) return launch_paged_attention_tc(a, maps, hd, q_tiles, sms, st);
     return hd == 128 ? launch<128>(a, maps.rows, sms, st) : launch<64>(a, maps.rows, sms, st);
 }
 

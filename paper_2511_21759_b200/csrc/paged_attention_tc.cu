@@ -37,7 +37,7 @@ constexpr int kTQ = 128;   // packed rows of a Q tile (MMA M)
 constexpr int kKT = 64;    // keys of a tile
 template <int QT> constexpr int kLoaders = QT;   // one warp for K and V, or one each (one CTA's registers have room for a twelfth warp, two CTAs' not for two more)
 template <int QT> constexpr int kThreads = 32 * (5 * QT + kLoaders<QT>);   // four softmax warps and an MMA warp a Q tile
-constexpr int kItem = 3;   // key tiles that an item costs beside its own
+constexpr int kItem = kPagedTcItem;
 template <int HD> constexpr uint32_t kQBytes = kTQ * HD * 2;
 template <int HD> constexpr uint32_t kTileBytes = kKT * HD * 2;
 // Q buffers: with two the next item's Q tiles and first scores are there when an item ends; the larger Q tiles of two CTAs on an SM

@@ -396,3 +396,33 @@ def test_a_length_that_the_table_has_no_entries_for_is_cut_and_sets_the_status_w
         assert torch.equal(cache.attention(0, b, q, right=0), want)
         assert cache.status() == (B.ODB_OK if len1 == cut else B.ODB_ERR_ARG), len1
     cache.close()
+
+
+# ---- very long prompts ------------------------------------------------------------------------------------------------
+
+@requires_gpu
+def test_attention_of_a_prompt_of_262144_rows():
+    """More key tiles of 16 packed rows than 32 bits count, of 256 far fewer; a window keeps the work small."""
+    P = paged()
+    n, H, KV, D, page = 262144, 32, 8, 64, 64
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    cache = P.PagedCache(1, H, KV, D, page, n // page)
+    cache.kv.normal_(generator=g)
+    q = torch.empty(n, H, D, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    table = torch.randperm(n // page, generator=g, device="cuda").to(torch.int32)[None]
+    batch = P.Batch(cache, table=table, len_after=i32([n]), first=i32([0]), row_start=i32([0, n]), max_rows=n, max_new=n)
+    lse = torch.empty(n, H, device="cuda")
+    out = cache.attention(0, batch, q, left=63, right=0, sinks=2, lse=lse)
+    assert cache.status() == 0 and bool(out.isfinite().all())
+    pages = table[0].cpu().numpy()
+    for a in (0, 61, 4095, 131071, 200001, n - 3):                # three rows each: the keys that they see, put together
+        rows = np.arange(a, a + 3)
+        lo = max(0, a - 63)
+        seen = np.concatenate([np.arange(min(2, lo)), np.arange(lo, a + 3)])
+        k, v = (cache.kv[0, i, pages[seen // page], :, seen % page].float().cpu().numpy() for i in (0, 1))
+        sinks = min(2, lo)
+        # the same differences of positions from the keys behind the sinks on: first key lo becomes number `sinks`
+        _check(out[rows], lse[rows], q[rows].float().cpu().numpy(), [k], [v], np.array([0, 3]), [a - lo + sinks], D, left=63, right=0, sinks=2)
+    del q, out, lse
+    cache.close()
