@@ -150,8 +150,7 @@ __global__ void __launch_bounds__(kThreads, 14) paged_store_kernel(const PagedSt
         }
     }
     f2 c[2], s[2], ms[2];
-    c[0] = c[1] = pair(1.f, 1.f);
-    s[0] = s[1] = ms[0] = ms[1] = pair(0.f, 0.f);
+    c[0] = c[1] = s[0] = s[1] = ms[0] = ms[1] = pair(0.f, 0.f);
     if (turned) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -193,15 +192,17 @@ __global__ void __launch_bounds__(kThreads, 14) paged_store_kernel(const PagedSt
                 b[j] = mul(mul(b[j], rr), gb[j]);
             }
         }
-        f2 u[2], v[2];
+        if (turned) {                                           // values behind rot pass: a product with zero would make NaN of their infinities
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            u[j] = fma(a[j], c[j], mul(b[j], ms[j]));
-            v[j] = fma(b[j], c[j], mul(a[j], s[j]));
+            for (int j = 0; j < 2; ++j) {
+                const f2 u = fma(a[j], c[j], mul(b[j], ms[j]));
+                b[j] = fma(b[j], c[j], mul(a[j], s[j]));
+                a[j] = u;
+            }
         }
         if (i < n && stored) {
             uint2 x, y;
-            narrow<INTER>(u, v, x, y);
+            narrow<INTER>(a, b, x, y);
             *reinterpret_cast<uint2*>(dst + i * step + ca) = x;
             *reinterpret_cast<uint2*>(dst + i * step + cb) = y;
         }

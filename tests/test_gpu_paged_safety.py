@@ -426,3 +426,37 @@ def test_attention_of_a_prompt_of_262144_rows():
         _check(out[rows], lse[rows], q[rows].float().cpu().numpy(), [k], [v], np.array([0, 3]), [a - lo + sinks], D, left=63, right=0, sinks=2)
     del q, out, lse
     cache.close()
+
+
+# ---- norm, rotation, store: what is not turned, not normed, not stored --------------------------------------------------
+
+@requires_gpu
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("rot", [0, 8, 24, 56])
+@pytest.mark.parametrize("inter", [False, True])
+def test_values_behind_the_turned_ones_pass_whatever_they_are(inter, rot, D):
+    """An infinity, a NaN or a negative zero behind rot_dim changes no other value and is stored as it is (a NaN as a NaN)."""
+    P = paged()
+    rng = np.random.default_rng(rot + D)
+    rows, H, KV = 9, 4, 2
+    clean = dev(rng.standard_normal((rows, H + 2 * KV, D)).astype(np.float32)).to(torch.bfloat16)
+    dirty, at = clean.clone(), torch.zeros_like(clean, dtype=torch.bool)
+    for r in range(rows):
+        for h in range(H + KV):
+            for x in (float("inf"), float("-inf"), float("nan"), -0.0):
+                j = int(rng.integers(rot, D))
+                dirty[r, h, j], at[r, h, j] = x, True
+    results = []
+    for x in (clean, dirty):
+        cache = P.PagedCache(1, H, KV, D, 16, 1, kv=torch.zeros(1, 2, 1, KV, 16, D, dtype=torch.bfloat16, device="cuda"))
+        b = P.Batch(cache, row_pos=i32(np.arange(rows) * 977), row_slot=i32(np.arange(rows)))
+        q = cache.norm_rope_store(0, b, x[:, :H].contiguous(), x[:, H:H + KV].contiguous(), x[:, H + KV:].contiguous(), P.Rope(rot, interleaved=inter))
+        results.append(torch.cat([q, cache.kv[0, 0, 0].transpose(0, 1)[:rows]], 1))
+        cache.close()
+    (a, b), poison = (t.view(torch.int16) for t in results), dirty[:, :H + KV]
+    at = at[:, :H + KV]
+    assert torch.equal(a[~at], b[~at])
+    got = results[1][at]
+    nan = poison[at].isnan()
+    assert bool(got[nan].isnan().all()) and torch.equal(got[~nan].view(torch.int16), poison[at][~nan].view(torch.int16))
+    assert torch.equal(results[0][..., rot:].contiguous().view(torch.int16), clean[:, :H + KV, rot:].contiguous().view(torch.int16))
