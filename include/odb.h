@@ -501,8 +501,8 @@ typedef struct odb_rope {
 
 /* For every row r < max_rows with row_pos[r] >= 0: q_out = rotate(norm(q)), and K := rotate(norm(k)), V := v at
  * row_slot[r] (a slot that is none, -1 for one, stores nothing).  norm: x / sqrt(mean(x^2) + eps) * gain over a head's
- * head_dim values.  rotate: by position x frequency; values behind rot_dim pass.  fp32, rounded once.  Two rows with the
- * same slot: one of them is stored.  Reads row_pos and row_slot. */
+ * head_dim values.  rotate: by position x frequency; values behind rot_dim pass.  fp32, rounded once.  Rows with
+ * the same slot are written over one another, in no order and in pieces of 8 bytes.  Reads row_pos and row_slot. */
 int32_t odb_paged_norm_rope_store(odb_paged* h, int32_t layer, const odb_paged_batch* b, const odb_paged_rows* rows, const odb_rope* rope,
                                   float eps, void* stream);
 

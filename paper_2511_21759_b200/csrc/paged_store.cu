@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(kThreads, 14) paged_store_kernel(const PagedSt
     const int h0 = (is_q ? part : is_v ? part - q_units - k_units : part - q_units) * kHeads, n = min(kHeads, (is_q ? p.H : p.KV) - h0);
     const int pos = p.row_pos[row], slot = p.row_slot[row];
     const int page = slot >> p.page_shift, off = slot & ((1 << p.page_shift) - 1);
-    const bool stored = is_q ? pos >= 0 : slot >= 0 && page < p.n_pages;
+    const bool stored = pos >= 0 && (is_q || (slot >= 0 && page < p.n_pages));
     // from head to head: HD values in q, a page's rows in the pool
     const size_t step = is_q ? HD : static_cast<size_t>(HD) << p.page_shift;
     __nv_bfloat16* dst = is_q ? p.q_out + row * p.out_stride + h0 * HD

@@ -460,3 +460,20 @@ def test_values_behind_the_turned_ones_pass_whatever_they_are(inter, rot, D):
     nan = poison[at].isnan()
     assert bool(got[nan].isnan().all()) and torch.equal(got[~nan].view(torch.int16), poison[at][~nan].view(torch.int16))
     assert torch.equal(results[0][..., rot:].contiguous().view(torch.int16), clean[:, :H + KV, rot:].contiguous().view(torch.int16))
+
+
+@requires_gpu
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_row_without_a_position_stores_nothing_whatever_its_slot(D):
+    P = paged()
+    rng = np.random.default_rng(D)
+    cache = P.PagedCache(1, 2, 2, D, 16, 1, kv=torch.full((1, 2, 1, 2, 16, D), 5.0, dtype=torch.bfloat16, device="cuda"))
+    x = dev(rng.standard_normal((6, 2, D)).astype(np.float32)).to(torch.bfloat16)
+    b = P.Batch(cache, row_pos=i32([3, -1, 0, -2 ** 31, 7, -1]), row_slot=i32([0, 1, 2, 3, -1, -1]))
+    out = torch.full_like(x, 7.0)
+    cache.norm_rope_store(0, b, x, x, x, P.Rope(D), q_out=out)
+    assert bool((out[[1, 3, 5]] == 7.0).all()) and not bool((out[[0, 2, 4]] == 7.0).any())
+    kept = cache.kv[0, :, 0].transpose(1, 2)                       # [K, V][position][head][value]
+    assert bool((kept[:, [1, 3, 4, 5]] == 5.0).all()) and bool((kept[:, 6:] == 5.0).all())
+    assert torch.equal(kept[1, [0, 2]], x[[0, 2]]) and torch.equal(kept[0, 2], x[2])     # position 0 turns nothing
+    cache.close()
