@@ -105,11 +105,14 @@ __global__ void __launch_bounds__(kThreads, 14) paged_store_kernel(const PagedSt
     const int q_units = (p.H + kHeads - 1) / kHeads, k_units = (p.KV + kHeads - 1) / kHeads, units = q_units + 2 * k_units;
     const int l = threadIdx.x % kLanes;
     const long long unit = static_cast<long long>(blockIdx.x) * (kThreads / kLanes) + threadIdx.x / kLanes;
-    const unsigned mask = __ballot_sync(0xffffffffu, unit < static_cast<long long>(p.rows) * units);   // a unit's lanes are in one warp
-    if (unit >= static_cast<long long>(p.rows) * units) return;
+    const bool any = unit < static_cast<long long>(p.rows) * units;
     const int row = p.rows * units < 0x7fffffff ? static_cast<int>(static_cast<unsigned>(unit) / static_cast<unsigned>(units)) : static_cast<int>(unit / units);
     const int part = static_cast<int>(unit - static_cast<long long>(row) * units);
     const bool is_q = part < q_units, is_v = part >= q_units + k_units;
+    const float* gain = is_q ? p.q_gain : p.k_gain;
+    // the lanes that will form sums of squares: those of a warp's other units (values, heads without a gain, none) are not waited for
+    const unsigned mask = __ballot_sync(0xffffffffu, any && !is_v && gain);
+    if (!any) return;
     const int h0 = (is_q ? part : is_v ? part - q_units - k_units : part - q_units) * kHeads, n = min(kHeads, (is_q ? p.H : p.KV) - h0);
     const int pos = p.row_pos[row], slot = p.row_slot[row];
     const int page = slot >> p.page_shift, off = slot & ((1 << p.page_shift) - 1);
@@ -163,7 +166,6 @@ __global__ void __launch_bounds__(kThreads, 14) paged_store_kernel(const PagedSt
             ms[j] = pair(-sn[0] * p.magnitude, -sn[1] * p.magnitude);
         }
     }
-    const float* gain = is_q ? p.q_gain : p.k_gain;
     f2 ga[2], gb[2];
     if (gain) {
         const float4 u = *reinterpret_cast<const float4*>(gain + ca), v = *reinterpret_cast<const float4*>(gain + cb);

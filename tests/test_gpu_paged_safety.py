@@ -477,3 +477,30 @@ def test_a_row_without_a_position_stores_nothing_whatever_its_slot(D):
     assert bool((kept[:, [1, 3, 4, 5]] == 5.0).all()) and bool((kept[:, 6:] == 5.0).all())
     assert torch.equal(kept[1, [0, 2]], x[[0, 2]]) and torch.equal(kept[0, 2], x[2])     # position 0 turns nothing
     cache.close()
+
+
+@requires_gpu
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,KV,rows", [(1, 1, 1), (2, 1, 33), (6, 2, 7), (16, 16, 20), (9, 3, 65)])
+def test_a_norm_of_the_queries_or_of_the_keys_alone(H, KV, rows, D):
+    """Units of queries, keys and values share a warp; those with a gain form their sums among themselves."""
+    P = paged()
+    rng = np.random.default_rng(H + rows)
+    x = dev(rng.standard_normal((rows, (H + 2 * KV) * D)).astype(np.float32)).to(torch.bfloat16)
+    pos, gain = i32(rng.integers(0, 5000, rows)), {n: dev((1 + 0.2 * rng.standard_normal(D)).astype(np.float32)) for n in "qk"}
+    rope, n_pages = P.Rope(D), -(-rows // 16)
+
+    def result(which):
+        cache = P.PagedCache(1, H, KV, D, 16, n_pages, kv=torch.zeros(1, 2, n_pages, KV, 16, D, dtype=torch.bfloat16, device="cuda"))
+        b = P.Batch(cache, row_pos=pos, row_slot=i32(np.arange(rows)))
+        q = cache.norm_rope_store(0, b, x[:, :H * D], x[:, H * D:(H + KV) * D], x[:, (H + KV) * D:], rope,
+                                  q_gain=gain["q"] if "q" in which else None, k_gain=gain["k"] if "k" in which else None)
+        assert cache.status() == 0
+        kv = cache.kv.clone()
+        cache.close()
+        return q, kv
+
+    both, none, q_only, k_only = (result(w) for w in ("qk", "", "q", "k"))     # both and neither are compared with the oracle elsewhere
+    assert not torch.equal(both[0], none[0]) and not torch.equal(both[1], none[1])
+    assert torch.equal(q_only[0], both[0]) and torch.equal(q_only[1], none[1])
+    assert torch.equal(k_only[0], none[0]) and torch.equal(k_only[1], both[1])
