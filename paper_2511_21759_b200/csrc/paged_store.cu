@@ -5,13 +5,15 @@
 //
 // in fp32, rounded once.  The angle of pair i is position x frequency; the frequencies come as 64-bit fractions of a turn
 // per position, so that the integer product's upper half is the angle with its whole turns already gone: exact to 2^-32 of
-// a turn at every position (fp32 position x frequency is off by 4e-3 rad at position 131072).
+// a turn (fp32 position x frequency is off by 4e-3 rad at position 131072) up to positions of some 10^7, from where on the rounding of
+// the frequencies themselves, which are computed as doubles, is more than that.
 //
 // A unit is a row and up to 8 heads of one kind (q, k or v); HD / 8 threads take it, each the same place of all its heads: two chunks
 // of four values that hold four whole pairs (values 4 l .. and rot / 2 + 4 l .., or 8 l .. of interleaved pairs; behind `rot` the
-// next ones, turned by nothing), so that no value changes threads but for the sum of squares, the sines are computed once and all
+// next ones, which pass), so that no value changes threads but for the sum of squares, the sines are computed once and all
 // heads' loads are in flight together.  Arithmetic on pairs of floats (f32x2).
-// Every value is read and written once: HBM is the bound.  25568 rows of 32 + 2 x 8 heads of 128 (628 MB) take 113 us = 5.6 TB/s.
+// Every value is read and written once: HBM is the bound.  25568 rows of 32 + 2 x 8 heads of 128 (628 MB) take 106 us = 5.9 TB/s, with
+// half of each head turned 111.  Whole heads have an instance of their own (ALL): in the one that asks every lane they take 112.
 // With the kinds mixed in a unit of four heads and single floats it was the issue slots: 241 instructions a head and warp, 164 us; in
 // blocks of 128 threads and more 118 us.  8 or 512 rows are the call's cost on the host, 13 us with three slices of a projection.
 #include "paged.cuh"
@@ -97,7 +99,7 @@ __device__ __forceinline__ void narrow(const f2 (&a)[2], const f2 (&b)[2], uint2
     }
 }
 
-template <int HD, bool INTER>
+template <int HD, bool INTER, bool ALL>
 __global__ void __launch_bounds__(kThreads, 14) paged_store_kernel(const PagedStoreArgs p) {
     constexpr int kLanes = HD / 8;                            // threads of a unit
     pdl_launch_dependents();
@@ -114,9 +116,9 @@ __global__ void __launch_bounds__(kThreads, 14) paged_store_kernel(const PagedSt
     const unsigned mask = __ballot_sync(0xffffffffu, any && !is_v && gain);
     if (!any) return;
     const int h0 = (is_q ? part : is_v ? part - q_units - k_units : part - q_units) * kHeads, n = min(kHeads, (is_q ? p.H : p.KV) - h0);
-    const int pos = p.row_pos[row], slot = p.row_slot[row];
+    const int pos = p.row_pos[row], slot = p.row_slot[row] | pos >> 31;   // without a position no slot
     const int page = slot >> p.page_shift, off = slot & ((1 << p.page_shift) - 1);
-    const bool stored = pos >= 0 && (is_q || (slot >= 0 && page < p.n_pages));
+    const bool stored = is_q ? pos >= 0 : slot >= 0 && page < p.n_pages;
     // from head to head: HD values in q, a page's rows in the pool
     const size_t step = is_q ? HD : static_cast<size_t>(HD) << p.page_shift;
     __nv_bfloat16* dst = is_q ? p.q_out + row * p.out_stride + h0 * HD
@@ -140,8 +142,8 @@ __global__ void __launch_bounds__(kThreads, 14) paged_store_kernel(const PagedSt
             }
         return;
     }
-    const bool turned = l < p.rot / 8;
-    const int ca = turned && !INTER ? 4 * l : 8 * l, cb = turned && !INTER ? p.rot / 2 + 4 * l : 8 * l + 4;
+    const bool turned = ALL || l < p.rot / 8;
+    const int ca = turned && !INTER ? 4 * l : 8 * l, cb = turned && !INTER ? (ALL ? HD : p.rot) / 2 + 4 * l : 8 * l + 4;
     const __nv_bfloat16* src = (is_q ? p.q + row * p.q_stride : p.k + row * p.k_stride) + h0 * HD;
     uint2 va[kHeads], vb[kHeads];
 #pragma unroll
@@ -194,13 +196,11 @@ __global__ void __launch_bounds__(kThreads, 14) paged_store_kernel(const PagedSt
                 b[j] = mul(mul(b[j], rr), gb[j]);
             }
         }
-        if (turned) {                                           // values behind rot pass: a product with zero would make NaN of their infinities
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const f2 u = fma(a[j], c[j], mul(b[j], ms[j]));
-                b[j] = fma(b[j], c[j], mul(a[j], s[j]));
-                a[j] = u;
-            }
+        for (int j = 0; j < 2; ++j) {                           // values behind rot pass: by cosine 1 and sine 0 an infinity would make NaN of its partner
+            const f2 u = fma(a[j], c[j], mul(b[j], ms[j])), v = fma(b[j], c[j], mul(a[j], s[j]));
+            a[j] = turned ? u : a[j];
+            b[j] = turned ? v : b[j];
         }
         if (i < n && stored) {
             uint2 x, y;
@@ -211,17 +211,22 @@ __global__ void __launch_bounds__(kThreads, 14) paged_store_kernel(const PagedSt
     }
 }
 
-template <int HD, bool INTER>
+template <int HD, bool INTER, bool ALL>
 cudaError_t launch(const PagedStoreArgs& a, cudaStream_t st) {
     const long long units = static_cast<long long>(a.rows) * ((a.H + kHeads - 1) / kHeads + 2 * ((a.KV + kHeads - 1) / kHeads)), per = kThreads / (HD / 8);
-    return launch_kernel(paged_store_kernel<HD, INTER>, dim3(static_cast<unsigned>((units + per - 1) / per)), dim3(kThreads), 0, st, a);
+    return launch_kernel(paged_store_kernel<HD, INTER, ALL>, dim3(static_cast<unsigned>((units + per - 1) / per)), dim3(kThreads), 0, st, a);
 }
 
 }  // namespace
 
 cudaError_t launch_paged_store(const PagedStoreArgs& a, cudaStream_t st) {
-    if (a.interleaved) return a.HD == 128 ? launch<128, true>(a, st) : launch<64, true>(a, st);
-    return a.HD == 128 ? launch<128, false>(a, st) : launch<64, false>(a, st);
+    const bool all = a.rot == a.HD;
+    if (a.interleaved) {
+        if (a.HD == 128) return all ? launch<128, true, true>(a, st) : launch<128, true, false>(a, st);
+        return all ? launch<64, true, true>(a, st) : launch<64, true, false>(a, st);
+    }
+    if (a.HD == 128) return all ? launch<128, false, true>(a, st) : launch<128, false, false>(a, st);
+    return all ? launch<64, false, true>(a, st) : launch<64, false, false>(a, st);
 }
 
 }  // namespace odb
