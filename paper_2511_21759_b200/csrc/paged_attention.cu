@@ -155,8 +155,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                     if (paged_elect()) mbar_expect_tx(&full[slot], bytes);
                     __syncwarp();
                     for (int c = 0; c < boxes; ++c) {
-                        const int row = pages.row(a, w.seq, w.head, k0 + (c << box_shift), base);
-                        if (row == a.pool_rows) paged_no_page(a, w.k, k0 + (c << box_shift), box);
+                        const int row = pages.row<true, true>(a, w.q, w.seq, w.head, k0 + (c << box_shift), base);
                         if (paged_elect()) tma_rows(to + c * box * HD * 2, &tm, &full[slot], row);
                         __syncwarp();
                     }

@@ -320,16 +320,15 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
             __syncwarp();
         };
         // pages of 64 rows and more: a copy a tile; smaller ones: a copy per page and 64 values, in their places of the operand layout
-        auto load = [&](Tiles& x) {
+        auto load = [&](Tiles& x, auto ask) {
             if (!ok || !x.have) return;
             const int k0 = x.w.k.tile(x.t) << 6, keys = min(kKT, x.w.k.hi - k0);
-            const int row = x.pages.row(a, x.w.seq, x.w.head, k0, x.base);
+            const int row = x.pages.template row<decltype(ask)::value>(a, x.w.q, x.w.seq, x.w.head, k0, x.base);
             if (x.issued >= static_cast<uint32_t>(x.slots)) ok = all_wait(&x.empty[x.slot], x.ph);
             if (!ok) return;
             const uint32_t dst = x.at + x.slot * kT;
             uint64_t* bar = &x.full[x.slot];
             if (box == kKT) {
-                if (row == a.pool_rows && keys > 0) paged_no_page(a, x.w.k, k0, kKT);
                 if (paged_elect()) {
                     mbar_expect_tx(bar, keys > 0 ? kT : 0u);
                     if (keys > 0) tma_box_3d(dst, &tm_rows, bar, 0, row, 0);
@@ -340,8 +339,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                 if (paged_elect()) mbar_expect_tx(bar, static_cast<uint32_t>(boxes) * box * HD * 2);
                 __syncwarp();
                 for (int c = 0; c < boxes; ++c) {
-                    const int row_c = x.pages.row(a, x.w.seq, x.w.head, k0 + (c << box_shift), x.base);
-                    if (row_c == a.pool_rows) paged_no_page(a, x.w.k, k0 + (c << box_shift), box);
+                    const int row_c = x.pages.template row<decltype(ask)::value>(a, x.w.q, x.w.seq, x.w.head, k0 + (c << box_shift), x.base);
                     if (paged_elect()) {
 #pragma unroll
                         for (int at = 0; at < kAtoms; ++at) tma_box_3d(dst + at * kKT * 128 + c * box * 128, &tm_atoms, bar, 0, row_c, at);
@@ -380,10 +378,10 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
             if (warp == kSoftmaxWarps + QT)
                 while (ok && k.have) {
                     if (k.t == k.w.t0) load_q(k.w);
-                    load(k);
+                    load(k, std::false_type());
                 }
             else
-                while (ok && v.have) load(v);
+                while (ok && v.have) load(v, std::true_type());
         } else {
             PagedWalk<kKT, kItem> wq(a, start);
             bool have_q = true;
@@ -392,14 +390,14 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                 load_q(wq);
                 have_q = wq.next();
             };
-            for (int i = 0; i < kFirst; ++i) load(k);
+            for (int i = 0; i < kFirst; ++i) load(k, std::false_type());
             if (NQ == 2) next_q();
             while (ok && v.have) {
                 if (NQ == 1 && v.t == v.w.t0) next_q();
                 // behind the item's third tile: the epilogue in front of it, which frees the buffer, is on its way by then
                 const bool then_q = NQ == 2 && v.t == min(v.w.t0 + 2, v.w.t1 - 1);
-                load(k);
-                load(v);
+                load(k, std::false_type());
+                load(v, std::true_type());
                 if (then_q) next_q();
             }
         }
@@ -634,7 +632,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                         for (int e = 0; e < kKT; ++e) {
                             const int key = k0 + e;
                             if (key >= w.k.hi || (key < w.k.lo && key >= a.sinks)) continue;
-                            const int row = pages.row(a, w.seq, w.head, key, a.v_row0);
+                            const int row = pages.template row<false>(a, w.q, w.seq, w.head, key, a.v_row0);
                             if (row >= a.pool_rows) continue;
                             const unsigned short* v = a.pool + static_cast<size_t>(row) * HD;
                             const uint32_t p2 = tmem_ld1(ts + e / 2);
