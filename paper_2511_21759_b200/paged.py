@@ -27,7 +27,7 @@ import torch
 from . import binding as B
 
 _BF16, _F32 = torch.bfloat16, torch.float32
-_raw_stream = torch._C._cuda_getCurrentRawStream
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 _ROWS = struct.Struct("=QqQqQqQqQQ")          # odb_paged_rows, filled in one go
 SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 
@@ -163,6 +163,11 @@ class PagedCache(_OnStream):
             B.lib().odb_paged_destroy(self.handle)
             self.handle = C.c_void_p()
 
+    def _there(self, call, *args, **kwargs):
+        """The call with the cache's device current: the library takes no other."""
+        with torch.cuda.device(self._index):
+            return call(*args, **kwargs)
+
     def _current(self, a, b) -> int:
         """The current stream's handle; it follows the streams that the cache and the objects a and b used with it come from."""
         raw = _raw_stream(self._index)
@@ -209,6 +214,8 @@ class PagedCache(_OnStream):
         """Block tables, free list and row maps of the forward (odb_paged_layout); the batch's arrays are updated."""
         if batch.cache is not self:
             self._other(batch)
+        if _current_device() != self._index:
+            return self._there(self.layout, batch)
         status = self._layout(self.handle, batch._ref, self._current(batch, batch))
         if status:
             raise B.OdbError(status, "odb_paged_layout")
@@ -218,6 +225,8 @@ class PagedCache(_OnStream):
         (odb_paged_norm_rope_store).  q, k, v: [max_rows][heads][head_dim] or [max_rows][heads * head_dim], slices of one
         projection's output as they are.  Returns q_out (a new tensor where none is given; q itself may be given, other rows that overlap
         q, k or v are refused)."""
+        if _current_device() != self._index:
+            return self._there(self.norm_rope_store, layer, batch, q, k, v, rope, q_gain=q_gain, k_gain=k_gain, eps=eps, q_out=q_out)
         if batch.cache is not self:
             self._other(batch)
         if rope.index != self._index:
@@ -241,6 +250,8 @@ class PagedCache(_OnStream):
         keys j < len_after with j <= p + right and (j >= p - left or j < sinks); -1: no limit; causal: right=0.
         scale 0: 1 / sqrt(head_dim).  lse: float32 [max_rows][n_heads] to be filled.  Returns out (a new tensor where none
         is given; one whose rows overlap q's is refused)."""
+        if _current_device() != self._index:
+            return self._there(self.attention, layer, batch, q, left=left, right=right, sinks=sinks, scale=scale, out=out, lse=lse)
         if batch.cache is not self:
             self._other(batch)
         qp, qs = self._rows(q, "q", self.n_heads, batch._q)
@@ -261,4 +272,6 @@ class PagedCache(_OnStream):
 
     def status(self) -> int:
         """Waits for the current stream; ODB_OK or what the device has found since the last call (read and cleared)."""
+        if _current_device() != self._index:
+            return self._there(self.status)
         return B.lib().odb_paged_status(self.handle, self._current(self, self))

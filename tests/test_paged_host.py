@@ -147,3 +147,51 @@ def test_the_paged_attentions_successor_starts_behind_its_tmem_allocation():
     text = re.sub(r"//[^\n]*", "", open(os.path.join(csrc, "paged_attention_tc.cu")).read())
     body = text.split("__global__")[1]
     assert 0 < body.find("tmem_alloc(") < body.find("pdl_launch_dependents()") < body.find("PagedStart start;")
+
+
+def test_calls_with_another_device_current_go_to_the_caches(monkeypatch):
+    """The library refuses a call while another device than the handle's is current: the object layer switches for it and back."""
+    import torch
+
+    from paper_2511_21759_b200 import paged as P
+    now, seen = [0], []
+
+    class Switch:
+        def __init__(self, device):
+            self.device = device
+
+        def __enter__(self):
+            self.before, now[0] = now[0], self.device
+
+        def __exit__(self, *_):
+            now[0] = self.before
+
+    monkeypatch.setattr(P, "_current_device", lambda: now[0])
+    monkeypatch.setattr(P, "_raw_stream", lambda index: 77)
+    monkeypatch.setattr(torch.cuda, "device", Switch)
+
+    class Lib:
+        def odb_paged_status(self, *_):
+            seen.append(("status", now[0]))
+            return 5
+
+    monkeypatch.setattr(P.B, "lib", lambda: Lib())
+    cache = object.__new__(P.PagedCache)
+    batch, rope = object.__new__(P.Batch), object.__new__(P.Rope)
+    cache._index, cache._raw, cache.handle, cache.device = 3, 77, None, torch.device("cpu")
+    cache.n_heads = cache.n_kv_heads = 1
+    cache.head_dim, cache._width, cache._rows_c, cache._rows_ref = 64, 64, P.B.odb_paged_rows(), None
+    batch.cache, batch._raw, batch._ref, batch.max_rows = cache, 77, None, 1
+    batch._q = batch._kv = (torch.Size((1, 1, 64)), torch.Size((1, 64)))
+    rope.index, rope._raw, rope._ref = 3, 77, None
+    for name in ("_layout", "_store", "_attention"):
+        setattr(cache, name, lambda *_, name=name: seen.append((name, now[0])) or 0)
+    monkeypatch.setattr(P.PagedCache, "_rows", lambda self, *_: (0, 64))
+    x = torch.zeros(1, 64, dtype=torch.bfloat16)
+    for device in (0, 3):
+        now[0] = device
+        cache.layout(batch)
+        assert cache.norm_rope_store(0, batch, x, x, x, rope, q_out=x) is x
+        assert cache.attention(0, batch, x, out=x) is x
+        assert cache.status() == 5 and now[0] == device
+    assert seen == [(name, 3) for name in ("_layout", "_store", "_attention", "status")] * 2
