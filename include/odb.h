@@ -425,7 +425,7 @@ typedef struct odb_paged_config {
 typedef struct odb_paged_batch {
     int32_t n_seqs;             /* requests */
     int32_t max_rows;           /* length of row_seq / row_pos / row_slot and rows of q, k, v and outputs */
-    int32_t max_new;            /* rows of the longest request, as far as the host knows: picks a kernel, never a result */
+    int32_t max_new;            /* rows of the longest request, 0 where the host does not know: picks a kernel, not the formula */
     int32_t table_stride;       /* entries of a table row */
     const int32_t* len_before;  /* [n_seqs] positions whose pages are held before the forward */
     const int32_t* len_after;   /* [n_seqs] positions held, and keys, from the forward on */

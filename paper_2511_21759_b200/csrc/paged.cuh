@@ -85,7 +85,7 @@ struct PagedMaps {
     CUtensorMap rows, atoms;
 };
 // The kernel of an attention over n_seqs requests with max_rows rows together, `longest` positions in a table row: 0 the few rows', 1 or 2
-// Q tiles of the many rows', -1: none, its sums would pass 32 bits.  max_new: rows of the longest request, a hint.
+// Q tiles of the many rows', -1: none, its sums would pass 32 bits.  max_new: rows of the longest request, a hint; 0: not known.
 int paged_attention_kernel_of(int n_seqs, int max_rows, int max_new, int group, int kv_heads, long long longest, long long out_stride);
 cudaError_t launch_paged_attention(PagedAttnArgs a, const PagedMaps& maps, int hd, int q_tiles, int sms, cudaStream_t st);
 // many packed rows on the tensor cores (paged_attention_tc.cu); q_tiles: Q tiles of 128 rows a CTA takes

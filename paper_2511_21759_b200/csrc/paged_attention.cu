@@ -31,6 +31,7 @@ constexpr int kItem = 1;                    // key tiles that an item costs besi
 constexpr int kMinUnits = 2, kFullUnits = 24;   // units of a CTA, at least; where all places on the SMs have work
 constexpr int kRows = 16;                   // packed rows of an item
 constexpr int kSmallUnits = 1024;           // up to here few rows' kernel for any number of rows
+constexpr int kManyRows = 1024;             // packed rows a request, on average, from which two Q tiles are right whatever the longest
 constexpr int kMmaWarps = 4;
 constexpr int kThreads = 32 * (kMmaWarps + 1);
 template <int HD> constexpr int kKSlots = HD == 128 ? 3 : 7;                // K tiles on the way or in use
@@ -539,8 +540,13 @@ size_t paged_part_bytes(int hd) { return static_cast<size_t>(kPagedMaxParts) * k
 // Two Q tiles take requests that are alike, the longest up to three times the mean: beside a prompt of 2048 rows 47 single tokens of up
 // to 8192 keys leave the second one empty, and two CTAs on an SM hide more: - / 169 / 220 (head dim 64: 127 / 173); 512 rows and 8 tokens
 // 50 / 63; 4096 rows and 8 tokens 180 / 172.
+// Where the longest is not known (max_new 0) the mean stands for it, and a mean says nothing of the mixture: of 1024 packed rows and
+// more on average two Q tiles are right for alike and unlike ones (4 of 1024 rows 127 / 113, 4096 rows and 15 tokens 198 / 197, 2 of
+// 2048 and 16 tokens, 916, 127 / 129), of fewer they gain a tenth where requests are alike and lose a third where they are not (16 of
+// 128 rows 95 / 83; 2048 rows and 47 tokens 177 / 237, 512 and 15 61 / 75; head dim 64 the same).
 int paged_attention_kernel_of(int n_seqs, int max_rows, int max_new, int group, int kv_heads, long long longest, long long out_stride) {
-    const long long all = static_cast<long long>(max_rows) * group, mine = static_cast<long long>(max_new) * group, tiles = longest / kKT + 1;
+    const long long all = static_cast<long long>(max_rows) * group, mean = (max_rows + n_seqs - 1ll) / n_seqs * group,
+                    mine = max_new > 0 ? static_cast<long long>(max_new) * group : mean, tiles = longest / kKT + 1;
     // units of all items together and what is added to them on the way, with rows that follow one another
     auto fits = [&](int tile_rows, int item) {
         return (static_cast<double>(all / tile_rows) + n_seqs) * kv_heads * static_cast<double>(tiles + item) < 2147483648.0 - 65536;
@@ -551,7 +557,7 @@ int paged_attention_kernel_of(int n_seqs, int max_rows, int max_new, int group, 
         const int tile = kPagedTcMaxGroup / group * group;
         const double units = static_cast<double>((all + (kRows - 1ll) * n_seqs) / kRows) * kv_heads * static_cast<double>(tiles + kItem);
         if ((mine > kRows && units > kSmallUnits) || !few_fit) {
-            const bool alike = static_cast<long long>(max_new) * n_seqs <= 3ll * max_rows;
+            const bool alike = max_new > 0 ? static_cast<long long>(max_new) * n_seqs <= 3ll * max_rows : n_seqs == 1 || mean >= kManyRows;
             const int q_tiles = mine > 128 && alike ? 2 : 1;
             if (fits(q_tiles * tile, kPagedTcItem)) return q_tiles;
             return fits(2 * tile, kPagedTcItem) ? 2 : -1;

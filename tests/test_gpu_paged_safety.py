@@ -504,3 +504,21 @@ def test_a_norm_of_the_queries_or_of_the_keys_alone(H, KV, rows, D):
     assert not torch.equal(both[0], none[0]) and not torch.equal(both[1], none[1])
     assert torch.equal(q_only[0], both[0]) and torch.equal(q_only[1], none[1])
     assert torch.equal(k_only[0], none[0]) and torch.equal(k_only[1], both[1])
+
+
+@requires_gpu
+@pytest.mark.parametrize("columns", [1, 5000])
+@pytest.mark.parametrize("counts", [[1, 37, 5], [300, 290], [310], [1, 1, 1]])
+def test_attention_without_a_hint(counts, columns):
+    """The longest request is not known: whatever kernel the mean picks."""
+    rng = np.random.default_rng(9)
+    lens = [320] * len(counts)
+    firsts = [n - c for n, c in zip(lens, counts)]
+    cache, b, q, qf, keys, values, start = _setup(rng, lens, counts, firsts, 8, 2, 128, 32, columns=columns)
+    batch = paged().Batch(cache, table=b.table, len_after=b.len_after, first=b.first, row_start=b.row_start, max_rows=sum(counts))
+    assert batch.max_new == 0 and batch._c.max_new == 0
+    lse = torch.empty(sum(counts), 8, device="cuda")
+    out = cache.attention(0, batch, q, right=0, lse=lse)
+    assert cache.status() == 0
+    _check(out, lse, qf, keys, values, start, firsts, 128, right=0)
+    cache.close()

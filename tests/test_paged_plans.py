@@ -40,3 +40,13 @@ def test_every_prompt_is_taken_that_some_kernel_can_count(n_seqs, max_rows, max_
 def test_rows_far_apart_take_the_kernel_of_few_rows():
     at = lambda stride: kernel(1, 4096, 4096, 4, 8, 4096, stride)
     assert at(1 << 27) == 2 and at((1 << 27) + 8) == 0 and at(1 << 40) == 0
+
+
+@pytest.mark.parametrize("n_seqs,max_rows,group,want", [
+    (48, 48, 4, 0), (16, 64, 4, 0), (16, 65, 4, 1),                   # the mean stands for the longest: few rows or many
+    (1, 4096, 4, 2), (1, 4096, 1, 2), (1, 33, 4, 2), (1, 20, 4, 1),   # one request: the mean is the longest
+    (48, 2048 + 47, 4, 1), (16, 512 + 15, 4, 1), (16, 2048, 4, 1),    # fewer than 1024 packed rows on average: one Q tile
+    (16, 4096 + 15, 4, 2), (4, 4096, 4, 2), (8, 8 * 256, 4, 2), (4, 4096, 1, 2), (5, 4096, 1, 1),
+])
+def test_kernel_of_requests_whose_longest_is_not_known(n_seqs, max_rows, group, want):
+    assert kernel(n_seqs, max_rows, 0, group, 8, 8192) == want
