@@ -18,7 +18,7 @@ def _kernels(source):
     assert r.returncode == 0, r.stderr[-2000:]
     out = {}
     for b in re.split(r"ptxas info\s*: Compiling entry function '", r.stderr)[1:]:
-        m = re.search(r"(paged_\w+?_kernel)(I(?:L[ib]\d+E)+E)?", b.split("'", 1)[0])
+        m = re.search(r".*\d(paged_[a-z_]+_kernel)(I(?:L[ib]\d+E)+E)?", b.split("'", 1)[0])
         key = (m.group(1), *map(int, re.findall(r"L[ib](\d+)E", m.group(2) or "")))
         assert key not in out
         out[key] = (int(re.search(r"Used (\d+) registers", b).group(1)), sum(int(x) for x in re.findall(r"(\d+) bytes spill", b)))
