@@ -35,16 +35,16 @@ SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 class _OnStream:
     """What is known of the memory that an object holds: the stream it was last used on."""
 
-    def _made(self, device, *tensors):
-        self._stream = torch.cuda.current_stream(device)
-        self._raw, self._memory = self._stream.cuda_stream, tensors
+    def _made(self, index: int, tensors):
+        self._raw, self._memory = _raw_stream(index), tensors
 
     def _follow(self, st, raw: int):
         """To stream st: the other one's work comes first, and the memory stays until st's is done too."""
-        st.wait_stream(self._stream)
+        st.wait_stream(torch.cuda.ExternalStream(self._raw, device=st.device))
         for t in self._memory:
-            t.record_stream(st)
-        self._stream, self._raw = st, raw
+            if t is not None:
+                t.record_stream(st)
+        self._raw = raw
 
 
 class Rope(_OnStream):
@@ -64,22 +64,24 @@ class Rope(_OnStream):
         self.turns = torch.tensor([C.c_int64(v).value for v in host], dtype=torch.int64, device=device)
         self.index = self.turns.get_device()
         if self.turns.is_cuda:
-            self._made(self.turns.device, self.turns)
+            self._made(self.index, (self.turns,))
         self._c = B.odb_rope(self.turns.data_ptr(), rot_dim, 1 if interleaved else 0, mag.value)
         self._ref = C.byref(self._c)
 
     def _follow(self, st, raw: int):
         """The numbers were there when the constructor returned and are read only: caches on several streams wait for none."""
         self.turns.record_stream(st)
-        self._stream, self._raw = st, raw
+        self._raw = raw
 
 
 class Batch(_OnStream):
-    """The device arrays of one forward (odb_paged_batch); arrays that a call needs and that are not given are made here (without rows,
-    until layout fills them), those that are given are used as they are: int32, contiguous, on the cache's device.  It serves every
-    cache of the same device, pages and heads.  max_rows: rows of the forward (known where row arrays are given); max_new: rows of
-    the longest request, a hint that picks the attention's kernel: worth giving where the requests' rows are known on the host (without
-    it up to a fifth slower, where several requests of 128 to 1024 rows x heads of a group are alike)."""
+    """The device arrays of one forward (odb_paged_batch); arrays that a call needs and that are not given are made here (-1 until
+    layout fills them: nothing is stored by such maps, and an attention is refused by the status word), those that are given are used
+    as they are: int32, contiguous, on the cache's device.  It serves every cache of the same device, pages and heads, and every
+    forward of the same requests and rows: its arrays may be written in place (one copy of all lengths takes 3 us on the host, a new
+    Batch 22, 11 with all arrays given).  max_rows: rows of the forward (known where row arrays are given); max_new: rows of the longest
+    request, a hint that picks the attention's kernel: worth giving where the requests' rows are known on the host (without it up to a
+    fifth slower, where several requests of 128 to 1024 rows x heads of a group are alike)."""
 
     _INPUTS = ("len_before", "len_after", "first", "count", "table", "free_pages", "row_start", "row_seq", "row_pos", "row_slot")
 
@@ -108,12 +110,14 @@ class Batch(_OnStream):
         self.n_seqs = n_seqs
         self.max_rows = rows.pop() if rows else (max_rows or 0)
         self.max_new = max_new or 0
-        if row_start is None and seqs:
-            given["row_start"] = torch.zeros(n_seqs + 1, dtype=torch.int32, device=cache.device)
         maps = [name for name in ("row_seq", "row_pos", "row_slot") if given[name] is None]
+        sizes = [self.max_rows] * len(maps)
+        if row_start is None and seqs:
+            maps.append("row_start")
+            sizes.append(n_seqs + 1)
         if maps:
-            given.update(zip(maps, torch.full((len(maps), self.max_rows), -1, dtype=torch.int32, device=cache.device)))
-        self._made(cache.device, *(t for t in given.values() if t is not None))
+            given.update(zip(maps, torch.full((sum(sizes),), -1, dtype=torch.int32, device=cache.device).split(sizes)))
+        self._made(cache._index, tuple(given.values()))
         for name, t in given.items():
             setattr(self, name, t)
         self.cache = cache
@@ -147,8 +151,8 @@ class PagedCache(_OnStream):
         self.kv = kv
         self.device = kv.device
         self.workspace = torch.empty(lib.odb_paged_workspace_bytes(C.byref(self.cfg)), dtype=torch.uint8, device=self.device)
-        self._made(self.device, self.workspace, kv)
         self._index = self.device.index
+        self._made(self._index, (self.workspace, kv))
         with torch.cuda.device(self.device):
             B.check(lib.odb_paged_create(C.byref(self.cfg), kv.data_ptr(), kv.numel() * 2, self.workspace.data_ptr(),
                                          self.workspace.numel(), C.c_void_p(self._raw), C.byref(self.handle)), "odb_paged_create")

@@ -178,12 +178,13 @@ def test_a_batch_without_a_layout_has_no_rows():
     for _ in range(40):                                          # what the allocator has next: plausible slots and row starts
         torch.arange(n, dtype=torch.int32, device="cuda")
     batch = P.Batch(cache, table=torch.zeros(n - 1, 1, dtype=torch.int32, device="cuda"), len_after=i32([16] * (n - 1)), first=i32([0] * (n - 1)), max_rows=n)
-    assert bool((batch.row_start == 0).all()) and all(bool((t == -1).all()) and t.shape == (n,) for t in (batch.row_seq, batch.row_pos, batch.row_slot))
+    assert bool((batch.row_start == -1).all()) and all(bool((t == -1).all()) and t.shape == (n,) for t in (batch.row_seq, batch.row_pos, batch.row_slot))
     x = torch.ones(n, 8 * 64, dtype=torch.bfloat16, device="cuda")
     out = torch.full((n, 4, 64), 3.0, dtype=torch.bfloat16, device="cuda")
     cache.norm_rope_store(0, batch, x[:, :256], x[:, 256:384], x[:, 384:], P.Rope(64), q_out=out)
+    assert cache.status() == 0
     cache.attention(0, batch, x[:, :256], out=out)
-    assert bool((out == 3.0).all()) and bool((cache.kv == 0).all()) and cache.status() == 0
+    assert bool((out == 3.0).all()) and bool((cache.kv == 0).all()) and cache.status() == binding().ODB_ERR_ARG
     cache.close()
 
 
