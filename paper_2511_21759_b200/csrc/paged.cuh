@@ -2,7 +2,7 @@
 // attention's work, which the kernels of few and of many rows have in common.
 #pragma once
 
-#include "odb_internal.cuh"
+#include "attention_tc.cuh"
 
 namespace odb {
 
@@ -466,14 +466,8 @@ __device__ __forceinline__ bool paged_elect() {
     return x != 0;
 }
 
-// 2^x for x <= 0 on the special-function unit (flushes to zero far below zero, which is the wanted value)
-__device__ __forceinline__ float paged_ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 // 2^(m - M) with M the larger of the two; a side that has seen nothing counts nothing
-__device__ __forceinline__ float paged_weight(float m, float M) { return m == -INFINITY ? 0.f : paged_ex2(m - M); }
+__device__ __forceinline__ float paged_weight(float m, float M) { return m == -INFINITY ? 0.f : ex2_approx(m - M); }
 // log-sum-exp of a row from its shift in the log2 domain and its sum
 __device__ __forceinline__ float paged_lse(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f; }
 __device__ __forceinline__ uint32_t paged_bf16x2(float a, float b) {

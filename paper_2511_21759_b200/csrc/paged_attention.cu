@@ -47,15 +47,6 @@ struct Barriers {
 };
 static_assert(sizeof(Barriers) <= 1024, "the barriers end inside the allocation");
 
-__device__ __forceinline__ void mbar_init(uint64_t* bar, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count));
-}
-__device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
 // a box of rows of the pool: all head dims of a row, 64 at a time
 __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* tmap, uint64_t* bar, int row) {
     asm volatile(
@@ -288,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attention_kernel(const __gr
                 for (int nb = 0; nb < NS; ++nb) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        s[nb][j] = paged_ex2(s[nb][j] - shift[j >> 1]);
+                        s[nb][j] = ex2_approx(s[nb][j] - shift[j >> 1]);
                         sum[j >> 1] += s[nb][j];
                     }
                     p[nb][0] = paged_bf16x2(s[nb][0], s[nb][1]);

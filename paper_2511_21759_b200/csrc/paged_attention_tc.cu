@@ -9,7 +9,7 @@
 // TMEM lane r = packed row r, so a row's maximum and sum never leave the thread.  The row's shift M is an integer in the log2
 // domain and moves only when a tile's maximum exceeds it by more than 8; O (in TMEM) and the sum are then multiplied by an exact
 // power of two (with 4 a row of every warp still moved now and then, some 1000 cycles for both Q tiles: a prompt 151 us, with 8 141).
-// P = exp2(S - M) < 256, rounded to bf16 (relative 2^-9 a key, independent from key to key; the sum keeps the unrounded
+// P = exp2(S - M) < 256, rounded to bf16 (up to 2^-8 of itself a key, independent from key to key; the sum keeps the unrounded
 // values), takes S's place in TMEM as the A operand of O += P V, with V taken MN-major from its [key][dim] tile.  A warp loads K and Q
 // (TMA boxes of a page's rows x 64 values, which land in the canonical swizzled layout whatever the page size) and one V (a single
 // warp both where two CTAs share the SM's registers), a warp a Q tile issues its MMAs, all meet through mbarriers with bounded waits;
@@ -26,7 +26,6 @@
 // tiles takes some 1700 cycles: the products alone 1374 (51 cycles for 128 x 64 x 16, which shared memory bounds, 72 for 128 x 128 x
 // 16), the exponentials 1024, a softmax warp's own chain from one score tile to the next some 1500.  An item costs 3 tiles beside its
 // own, the start 4 us, the parts' kernel 7 us.
-#include "attention_tc.cuh"
 #include "paged.cuh"
 
 namespace odb {
