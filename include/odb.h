@@ -508,7 +508,8 @@ int32_t odb_paged_norm_rope_store(odb_paged* h, int32_t layer, const odb_paged_b
 
 /* out[r][h] = sum_j softmax_j(scale * q[r][h] . K[j][h / group]) V[j][h / group] over the keys j that row r at position
  * p = first + (r - row_start) sees: j < len_after, j <= p + right, and j >= p - left or j < sinks (left, right: -1 = no
- * limit; causal: right = 0).  The row's own K and V are in the pool before (odb_paged_norm_rope_store).  scale 0 means
+ * limit; causal: right = 0).  Scores, maxima and sums are fp32; the weights are rounded to bf16 for the product with V, their sum
+ * is not.  The row's own K and V are in the pool before (odb_paged_norm_rope_store).  scale 0 means
  * 1 / sqrt(head_dim).  lse (fp32 [max_rows][n_heads], may be NULL): ln of the sum of exponentials.  A row that sees no key
  * gets zeros and -infinity.  What pages hold at positions nobody sees never reaches a result, not even as NaN.
  * Reads len_after, first, row_start, table; rows from row_start[n_seqs] on are left as they are.  q and out on 16-byte

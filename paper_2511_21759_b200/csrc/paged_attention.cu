@@ -13,9 +13,9 @@
 // CTAs, whoever it is: the same bits every time.
 //
 // Bound by HBM where there is work for all SMs (a pool read once; the products of 16 rows take a third of a tile's time): one token
-// of 48 requests, 905 MB, 153 us = 5.9 TB/s, of two of 131072 keys, 1.02 GB, 168 us = 6.1 TB/s; the rest is the start (a microsecond to
+// of 48 requests, 905 MB, 152 us = 6.0 TB/s, of two of 131072 keys, 1.02 GB, 167 us = 6.1 TB/s; the rest is the start (a microsecond to
 // find the share, two until the first tile is there), the parts and the slowest SMs' tail.  Small calls are bound by latency: one token
-// of 577 keys 9.2 us, 16 requests with a window of 4096 keys of 64 (67 MB) 23 us.
+// of 577 keys 9.2 us, 16 requests with a window of 4096 keys of 64 (67 MB) 21 us.
 //
 // Rows of V behind the last visible key are whatever the page held before: their P is zero, but zero times an infinity or NaN
 // there is not, so they are set to zero in shared memory first.  A key that some rows of the tile see and others do not is

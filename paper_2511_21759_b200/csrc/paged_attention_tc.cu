@@ -20,9 +20,9 @@
 // keys that only some rows see, and the softmax warps add those, from the pool, to O of the rows that see them, one TMEM column at a
 // time.
 //
-// Measured, 32 query and 8 K/V heads of 128: a causal prompt of 4096 rows 141 us = 975 TFLOP/s of its visible pairs (0.57 of what a
-// large matrix product reaches); blocks of 32 rows of 16 requests of up to 4096 keys 46 us = 3.7 TB/s; 4 requests of some 1300 rows, 32
-// K/V heads, 148 us.  Called without a pause the large ones run into the card's 1000 W, at 1.6 GHz: 164 and 174 us.  A tile of both Q
+// Measured, 32 query and 8 K/V heads of 128: a causal prompt of 4096 rows 140 us = 985 TFLOP/s of its visible pairs (0.58 of what a
+// large matrix product reaches); blocks of 32 rows of 16 requests of up to 4096 keys 45 us = 3.7 TB/s; 4 requests of some 1300 rows, 32
+// K/V heads, 140 us.  Called without a pause the large ones run into the card's 1000 W, at 1.6 GHz: 160 - 166 and 166 - 176 us.  A tile of both Q
 // tiles takes some 1700 cycles: the products alone 1374 (51 cycles for 128 x 64 x 16, which shared memory bounds, 72 for 128 x 128 x
 // 16), the exponentials 1024, a softmax warp's own chain from one score tile to the next some 1500.  An item costs 3 tiles beside its
 // own, the start 4 us, the parts' kernel 7 us.
