@@ -461,6 +461,18 @@ int32_t odb_paged_destroy(odb_paged* h);
  * norm_rope_store records nothing: a slot that is none is a row that is not stored. */
 int32_t odb_paged_status(odb_paged* h, void* stream);
 
+/* ---- pools of 8 bits ----
+ * The same handle over a pool of half the bytes: e4m3 [n_layers][2][n_pages][n_kv_heads][page_size][head_dim] with an fp32 scale for each
+ * block of 16 positions of a head, [n_layers][2][n_pages][n_kv_heads][page_size / 16]; K or V of a position is code * scale.  Scales are
+ * powers of two from 2^-100 to 2^119, so that what a code stands for is a number of bf16.  kv and scales on 256-byte boundaries, borrowed
+ * as kv is; the workspace is odb_paged_workspace_bytes'.  layout, attention, load, status and destroy are called as over a pool of bf16
+ * (an attention's weights are rounded to f16 or bf16 for the product with V); for the store see odb_paged_norm_rope_store. */
+enum { ODB_PAGED_SCALE_BLOCK = 16 };
+size_t odb_paged_e4m3_kv_bytes(const odb_paged_config* cfg);     /* 0: a configuration odb_paged_create_e4m3 would refuse */
+size_t odb_paged_e4m3_scale_bytes(const odb_paged_config* cfg);
+int32_t odb_paged_create_e4m3(const odb_paged_config* cfg, void* kv, size_t kv_bytes, void* scales, size_t scale_bytes, void* workspace,
+                              size_t ws_bytes, void* stream, odb_paged** out);
+
 /* Tables and maps of the forward: every request's table grows or shrinks from ceil(len_before / page_size) to
  * ceil(len_after / page_size) pages, and rows first .. first + count - 1 of every request get their places.
  * With n free pages, G given back (requests in order, then table order) and appended to them, T taken (requests in order,
@@ -502,7 +514,16 @@ typedef struct odb_rope {
 /* For every row r < max_rows with row_pos[r] >= 0: q_out = rotate(norm(q)), and K := rotate(norm(k)), V := v at
  * row_slot[r] (a slot that is none, -1 for one, stores nothing).  norm: x / sqrt(mean(x^2) + eps) * gain over a head's
  * head_dim values.  rotate: by position x frequency; values behind rot_dim pass.  fp32, rounded once.  Rows with
- * the same slot are written over one another, in no order and in pieces of 8 bytes.  Reads row_pos and row_slot. */
+ * the same slot are written over one another, in no order and in pieces of 8 bytes.  Reads row_pos and row_slot.
+ *
+ * Over a pool of 8 bits K and V are quantised as they are written, block by block (16 positions of a request from a multiple of 16 on, a
+ * head, K or V), from fp32 in one rounding.  e is the smallest integer, from -100 to 119, with max |x| <= 448 * 2^e over the finite values
+ * that the call writes of the block; where the block keeps positions, those below len_after that the call does not write, e is at least
+ * the block's exponent before, and their codes are rounded again, code := e4m3(code * 2^(before - e)).  The codes of the rows are
+ * e4m3(x * 2^-e), to the nearest, ties to even, NaN where x is not finite (beyond 448 * 2^119 the largest number); the scale is 2^e.
+ * Reads row_seq and len_after too, as odb_paged_layout leaves them: the rows of a request's block follow one another, with a position each,
+ * and their slots lie in one page at position % 16 (others are not stored).  No two requests write into a block in the same call (what
+ * it holds then is one's or the other's). */
 int32_t odb_paged_norm_rope_store(odb_paged* h, int32_t layer, const odb_paged_batch* b, const odb_paged_rows* rows, const odb_rope* rope,
                                   float eps, void* stream);
 
@@ -517,6 +538,12 @@ int32_t odb_paged_norm_rope_store(odb_paged* h, int32_t layer, const odb_paged_b
  * call gives the same bits. */
 int32_t odb_paged_attention(odb_paged* h, int32_t layer, const odb_paged_batch* b, const void* q, int64_t q_stride, void* out,
                             int64_t out_stride, float* lse, float scale, int32_t left, int32_t right, int32_t sinks, void* stream);
+
+/* Rows back from the pool as bf16, K and V: k[r], v[r] (bf16 [max_rows][n_kv_heads][head_dim] on 16-byte boundaries, strides in elements,
+ * multiples of 8; slices of one tensor's rows as they are, rows that overlap are refused) := what the layer holds at row_slot[r], exact from
+ * either pool.  A row whose slot is none is left as it is.  Reads row_slot. */
+int32_t odb_paged_load(odb_paged* h, int32_t layer, const odb_paged_batch* b, void* k, int64_t k_stride, void* v, int64_t v_stride,
+                       void* stream);
 
 #ifdef __cplusplus
 }

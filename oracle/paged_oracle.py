@@ -98,3 +98,51 @@ def attention(q, keys, values, pos, scale=None, left=-1, right=-1, sinks=0):
             lse[r, h] = m + np.log(e.sum())
             size[r, h] = (np.abs(k) @ np.abs(x)).max() * abs(scale)
     return out, lse, mag, size
+
+
+# ---- pools of 8 bits -----------------------------------------------------------------------------------------------------
+
+BLOCK, LOW_EXP, HIGH_EXP = 16, -100, 119        # positions of a scale, and its exponent's range
+
+
+def e4m3_values():
+    """What each of the 256 codes stands for: a sign, four bits of exponent, three of fraction; 0x7f and 0xff are none."""
+    c = np.arange(256)
+    e, f = (c >> 3) & 15, c & 7
+    v = np.where(e == 0, f / 8 * 2.0 ** -6, (1 + f / 8) * 2.0 ** (e - 7.0))
+    v = np.where((c & 127) == 127, np.nan, v)
+    return np.where(c >> 7 == 1, -v, v)
+
+
+def e4m3_round(x):
+    """The nearest value of a code, ties to the even fraction, beyond 448 the largest; what is not finite becomes NaN."""
+    x = np.asarray(x, np.float64)
+    fine = np.isfinite(x)
+    y = np.where(fine, x, 0.0)
+    step = 2.0 ** (np.maximum(np.frexp(y)[1] - 1.0, -6.0) - 3.0)
+    y = np.clip(np.rint(y / step) * step, -448, 448)
+    return np.where(fine, y, np.nan)
+
+
+def exponent_for(top):
+    """The smallest exponent with top <= 448 * 2^e, within the range."""
+    e = LOW_EXP
+    while e < HIGH_EXP and top > 448 * 2.0 ** e:
+        e += 1
+    return e
+
+
+def quantise_block(before, before_exp, rows, offsets, live: int):
+    """A block's values after rows [n][hd] have been written at `offsets`: before [16][hd] under exponent before_exp, of which the first
+    `live` positions that are not written are kept.  Returns values [16][hd] and the exponent; positions that are neither are as before."""
+    finite = np.where(np.isfinite(rows), np.abs(rows), 0.0)
+    e = exponent_for(finite.max(initial=0.0))
+    kept = [o for o in range(min(max(live, 0), BLOCK)) if o not in set(offsets)]
+    if kept:
+        e = max(e, before_exp)
+    out = before.copy()
+    for o in kept:
+        out[o] = e4m3_round(before[o] / 2.0 ** e) * 2.0 ** e
+    for o, x in zip(offsets, rows):
+        out[o] = e4m3_round(x / 2.0 ** e) * 2.0 ** e
+    return out, e

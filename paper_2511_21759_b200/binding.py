@@ -16,6 +16,7 @@ LIB_PATH = os.path.join(HERE, "libodb.so")
 ODB_OK, ODB_ERR_ARG, ODB_ERR_SHAPE, ODB_ERR_WORKSPACE, ODB_ERR_STATE, ODB_ERR_CUDA, ODB_ERR_TIMEOUT = 0, -1, -2, -3, -4, -5, -6
 ODB_MAX_COPIES, ODB_MAX_RANKS, ODB_MAX_CHAIN = 8, 4, 5
 ODB_STATIC_SCRATCH_BYTES = 8 << 20
+ODB_PAGED_SCALE_BLOCK = 16
 KINDS = ("gemm", "attention", "elementwise", "confidence", "control")
 
 
@@ -124,6 +125,10 @@ SIGNATURES = {
     "odb_paged_workspace_bytes": (C.c_size_t, [C.POINTER(odb_paged_config)]),
     "odb_paged_create": (C.c_int32, [C.POINTER(odb_paged_config), C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t, C.c_void_p,
                                      C.POINTER(C.c_void_p)]),
+    "odb_paged_e4m3_kv_bytes": (C.c_size_t, [C.POINTER(odb_paged_config)]),
+    "odb_paged_e4m3_scale_bytes": (C.c_size_t, [C.POINTER(odb_paged_config)]),
+    "odb_paged_create_e4m3": (C.c_int32, [C.POINTER(odb_paged_config), C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t,
+                                          C.c_void_p, C.POINTER(C.c_void_p)]),
     "odb_paged_destroy": (C.c_int32, [C.c_void_p]),
     "odb_paged_status": (C.c_int32, [C.c_void_p, C.c_void_p]),
     "odb_paged_layout": (C.c_int32, [C.c_void_p, C.POINTER(odb_paged_batch), C.c_void_p]),
@@ -133,6 +138,8 @@ SIGNATURES = {
                                               C.POINTER(odb_rope), C.c_float, C.c_void_p]),
     "odb_paged_attention": (C.c_int32, [C.c_void_p, C.c_int32, C.POINTER(odb_paged_batch), C.c_void_p, C.c_int64, C.c_void_p,
                                         C.c_int64, C.c_void_p, C.c_float, C.c_int32, C.c_int32, C.c_int32, C.c_void_p]),
+    "odb_paged_load": (C.c_int32, [C.c_void_p, C.c_int32, C.POINTER(odb_paged_batch), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                   C.c_void_p]),
 }
 
 _lib = None

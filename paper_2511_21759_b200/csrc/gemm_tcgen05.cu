@@ -611,6 +611,19 @@ cudaError_t make_pool_tmap(CUtensorMap* out, const void* kv, unsigned long long 
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+cudaError_t make_pool_e4m3_tmap(CUtensorMap* out, const void* codes, unsigned long long rows, int hd, int box_rows) {
+    EncodeTiledFn fn = get_encode_fn();
+    if (!fn) return cudaErrorNotSupported;
+    cuuint64_t dims[2] = {static_cast<cuuint64_t>(hd), rows};
+    cuuint64_t strides[1] = {static_cast<cuuint64_t>(hd)};
+    cuuint32_t box[2] = {static_cast<cuuint32_t>(hd), static_cast<cuuint32_t>(box_rows)};
+    cuuint32_t estr[2] = {1, 1};
+    CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(codes), dims, strides, box, estr,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, hd == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 cudaError_t make_group_tmap(CUtensorMap* out, const void* q, int rows, long long stride, int heads, int hd, int group, int tokens) {
     EncodeTiledFn fn = get_encode_fn();
     if (!fn) return cudaErrorNotSupported;

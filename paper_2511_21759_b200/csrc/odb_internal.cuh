@@ -379,6 +379,8 @@ cudaError_t make_rows_tmap(CUtensorMap* out, const void* base, int rows, int col
 // the K/V pool bf16 [rows][hd] as boxes of box_rows rows x atoms 64 values: in shared memory [atom][box_rows][64], 128-byte swizzle;
 // rows beyond `rows` read as zero
 cudaError_t make_pool_tmap(CUtensorMap* out, const void* kv, unsigned long long rows, int hd, int box_rows, int atoms);
+// codes of 8 bits [rows][hd] as boxes of `box_rows` whole rows, swizzled by their width
+cudaError_t make_pool_e4m3_tmap(CUtensorMap* out, const void* codes, unsigned long long rows, int hd, int box_rows);
 // query rows bf16 [rows][heads][hd], `stride` elements from row to row, as boxes of `tokens` rows x `group` heads x 64 values
 cudaError_t make_group_tmap(CUtensorMap* out, const void* q, int rows, long long stride, int heads, int hd, int group, int tokens);
 size_t packed_weight_bytes(int N, int K);

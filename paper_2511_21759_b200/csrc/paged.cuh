@@ -36,6 +36,30 @@ struct PagedStoreArgs {
 };
 cudaError_t launch_paged_store(const PagedStoreArgs& a, cudaStream_t st);
 
+// ---- pools of 8 bits: e4m3 and a scale, a power of two, for each block of 16 positions of a head (paged_e4m3_store.cu) ----
+constexpr int kPagedBlock = ODB_PAGED_SCALE_BLOCK;
+constexpr int kPagedLowExp = -100, kPagedHighExp = 119;   // of scales: what the codes stand for is then a number of bf16
+struct PagedE4m3StoreArgs {
+    PagedStoreArgs rows;                                  // KV = 0: as units it has those of q
+    const int32_t *row_seq, *len;
+    unsigned char *k_pool, *v_pool;                       // this layer's
+    float *k_scales, *v_scales;
+    int KV, n_seqs, window;                               // window: rows in which a warp looks for the beginnings of blocks, 1 or 16
+};
+cudaError_t launch_paged_e4m3_store(const PagedE4m3StoreArgs& a, cudaStream_t st);
+
+// ---- rows back from the pool (paged_load.cu) ----
+struct PagedLoadArgs {
+    const unsigned char *k_pool, *v_pool;                 // this layer's: codes, or bf16 where there are no scales
+    const float *k_scales, *v_scales;
+    const int32_t* row_slot;
+    __nv_bfloat16 *k_out, *v_out;
+    long long k_stride, v_stride;
+    int rows, KV, HD, page_shift, n_pages;
+    int per_row, block_rows;                              // pieces of 16 values of a row, K and V; rows of a block (the launcher's)
+};
+cudaError_t launch_paged_load(PagedLoadArgs a, cudaStream_t st);
+
 // ---- attention (paged_attention.cu) ----
 // n / d for 0 <= n < 2^31 by a product: with l = ceil(log2 d) and m = floor(2^(31 + l) / d) + 1, which fits 32 bits, n m 2^-(31 + l)
 // exceeds n / d by less than 1 / d (Granlund and Montgomery, PLDI 1994).
@@ -79,6 +103,7 @@ struct PagedAttnArgs {
     struct PagedShared* shared;                           // [kPagedMaxCtas], of the last launch that adds up in a kernel of its own
     PagedDiv by_group, by_rows, by_once;                  // divisions by G, by the packed rows of an item, by at_once
     int tile_rows, tile_tokens;                           // many rows: packed rows of an item, query rows of a Q tile
+    const float* scales;                                  // pools of 8 bits: [pool_rows / 16]
 };
 // the pool's two maps: boxes of whole rows, and of 64 values of a row
 struct PagedMaps {
@@ -93,6 +118,10 @@ cudaError_t launch_paged_attention_tc(PagedAttnArgs a, const PagedMaps& maps, in
 constexpr int kPagedTcMaxGroup = 128;   // heads of a group that fit a Q tile
 constexpr int kPagedTcItem = 3;         // key tiles that an item costs the many rows' kernel beside its own
 size_t paged_part_bytes(int hd);
+
+// ---- attention over a pool of 8 bits (paged_e4m3_attention.cu) ----
+int paged_e4m3_attention_kernel_of(int n_seqs, int max_rows, int max_new, int group, int kv_heads, long long longest, long long out_stride);
+cudaError_t launch_paged_e4m3_attention(PagedAttnArgs a, const CUtensorMap& map, int hd, int q_tiles, int sms, cudaStream_t st);
 
 #ifdef __CUDACC__
 // ---------------------------------------------------------------------------------------

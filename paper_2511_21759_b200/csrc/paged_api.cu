@@ -10,13 +10,20 @@ using namespace odb;
 struct odb_paged {
     odb_paged_config cfg;
     int device, sms, page_shift;
-    __nv_bfloat16* kv;
+    void* kv;
+    float* scales;                  // null: the pool is bf16
     int* status;
     unsigned int* arrivals;
     PagedShared* shared;
     float *part_o, *part_ml;
     int pool_rows, layer_rows;      // rows of head_dim values: of the whole pool, of the K or the V of a layer
-    PagedMaps maps;
+    PagedMaps maps;                 // pools of 8 bits: rows alone
+    int value_bytes() const { return scales ? 1 : 2; }
+    // the layer's K, and V behind it
+    char* k_of(int layer) const { return static_cast<char*>(kv) + static_cast<size_t>(2 * layer) * layer_rows * cfg.head_dim * value_bytes(); }
+    char* v_of(int layer) const { return k_of(layer) + static_cast<size_t>(layer_rows) * cfg.head_dim * value_bytes(); }
+    float* k_scales_of(int layer) const { return scales ? scales + static_cast<size_t>(2 * layer) * (layer_rows / kPagedBlock) : nullptr; }
+    float* v_scales_of(int layer) const { return scales ? k_scales_of(layer) + layer_rows / kPagedBlock : nullptr; }
 };
 
 namespace {
@@ -72,32 +79,19 @@ bool overlap(const Rows& a, const Rows& b, int32_t n) {
     return false;
 }
 
-int32_t enqueued(cudaError_t e) { return e == cudaSuccess ? ODB_OK : record_cuda_error(e); }
-
-}  // namespace
-
-extern "C" {
-
-size_t odb_paged_kv_bytes(const odb_paged_config* c) {
-    if (check_config(c) != ODB_OK) return 0;
-    return static_cast<size_t>(c->n_layers) * 2 * c->n_pages * c->n_kv_heads * c->page_size * c->head_dim * 2;
+size_t pool_values(const odb_paged_config* c) {
+    return static_cast<size_t>(c->n_layers) * 2 * c->n_pages * c->n_kv_heads * c->page_size * c->head_dim;
 }
 
-size_t odb_paged_workspace_bytes(const odb_paged_config* c) {
-    if (check_config(c) != ODB_OK) return 0;
-    return kStatusBytes + kArrivalBytes + kSharedBytes + paged_part_bytes(c->head_dim);
-}
-
-int32_t odb_paged_create(const odb_paged_config* cfg, void* kv, size_t kv_bytes, void* workspace, size_t ws_bytes, void* stream,
-                         odb_paged** out) {
-    const int32_t rc = check_config(cfg);
-    if (rc != ODB_OK) return rc;
+// a handle over a pool of bf16, or of codes with scales
+int32_t create(const odb_paged_config* cfg, void* kv, size_t kv_bytes, float* scales, void* workspace, size_t ws_bytes, cudaStream_t st, odb_paged** out) {
     if (!kv || !workspace || !out || !aligned(kv, 256) || !aligned(workspace, 256)) return ODB_ERR_ARG;
-    if (kv_bytes < odb_paged_kv_bytes(cfg) || ws_bytes < odb_paged_workspace_bytes(cfg)) return ODB_ERR_WORKSPACE;
+    if (kv_bytes < pool_values(cfg) * (scales ? 1 : 2) || ws_bytes < odb_paged_workspace_bytes(cfg)) return ODB_ERR_WORKSPACE;
     odb_paged* h = new (std::nothrow) odb_paged();
     if (!h) return ODB_ERR_ARG;
     h->cfg = *cfg;
-    h->kv = static_cast<__nv_bfloat16*>(kv);
+    h->kv = kv;
+    h->scales = scales;
     for (h->page_shift = 0; (1 << h->page_shift) < cfg->page_size;) ++h->page_shift;
     h->layer_rows = cfg->n_pages * cfg->n_kv_heads * cfg->page_size;
     h->pool_rows = h->layer_rows * 2 * cfg->n_layers;
@@ -110,9 +104,13 @@ int32_t odb_paged_create(const odb_paged_config* cfg, void* kv, size_t kv_bytes,
     cudaError_t e = cudaGetDevice(&h->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, h->device);
     if (e == cudaSuccess && h->sms > 148) h->sms = 148;         // what the workspace has parts for
-    if (e == cudaSuccess) e = make_pool_tmap(&h->maps.rows, kv, h->pool_rows, cfg->head_dim, cfg->page_size < 64 ? cfg->page_size : 64, cfg->head_dim / 64);
-    if (e == cudaSuccess) e = make_pool_tmap(&h->maps.atoms, kv, h->pool_rows, cfg->head_dim, cfg->page_size < 64 ? cfg->page_size : 64, 1);
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int box_rows = cfg->page_size < 64 ? cfg->page_size : 64;
+    if (scales) {
+        if (e == cudaSuccess) e = make_pool_e4m3_tmap(&h->maps.rows, kv, h->pool_rows, cfg->head_dim, box_rows);
+    } else {
+        if (e == cudaSuccess) e = make_pool_tmap(&h->maps.rows, kv, h->pool_rows, cfg->head_dim, box_rows, cfg->head_dim / 64);
+        if (e == cudaSuccess) e = make_pool_tmap(&h->maps.atoms, kv, h->pool_rows, cfg->head_dim, box_rows, 1);
+    }
     if (e == cudaSuccess) e = cudaMemsetAsync(ws, 0, kStatusBytes + kArrivalBytes, st);
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     if (e != cudaSuccess) {
@@ -121,6 +119,43 @@ int32_t odb_paged_create(const odb_paged_config* cfg, void* kv, size_t kv_bytes,
     }
     *out = h;
     return ODB_OK;
+}
+
+int32_t enqueued(cudaError_t e) { return e == cudaSuccess ? ODB_OK : record_cuda_error(e); }
+
+}  // namespace
+
+extern "C" {
+
+size_t odb_paged_kv_bytes(const odb_paged_config* c) {
+    if (check_config(c) != ODB_OK) return 0;
+    return pool_values(c) * 2;
+}
+
+size_t odb_paged_workspace_bytes(const odb_paged_config* c) {
+    if (check_config(c) != ODB_OK) return 0;
+    return kStatusBytes + kArrivalBytes + kSharedBytes + paged_part_bytes(c->head_dim);
+}
+
+int32_t odb_paged_create(const odb_paged_config* cfg, void* kv, size_t kv_bytes, void* workspace, size_t ws_bytes, void* stream,
+                         odb_paged** out) {
+    const int32_t rc = check_config(cfg);
+    return rc != ODB_OK ? rc : create(cfg, kv, kv_bytes, nullptr, workspace, ws_bytes, static_cast<cudaStream_t>(stream), out);
+}
+
+size_t odb_paged_e4m3_kv_bytes(const odb_paged_config* c) { return check_config(c) != ODB_OK ? 0 : pool_values(c); }
+
+size_t odb_paged_e4m3_scale_bytes(const odb_paged_config* c) {
+    return check_config(c) != ODB_OK ? 0 : pool_values(c) / c->head_dim / kPagedBlock * sizeof(float);
+}
+
+int32_t odb_paged_create_e4m3(const odb_paged_config* cfg, void* kv, size_t kv_bytes, void* scales, size_t scale_bytes, void* workspace,
+                              size_t ws_bytes, void* stream, odb_paged** out) {
+    const int32_t rc = check_config(cfg);
+    if (rc != ODB_OK) return rc;
+    if (!scales || !aligned(scales, 256)) return ODB_ERR_ARG;
+    if (scale_bytes < odb_paged_e4m3_scale_bytes(cfg)) return ODB_ERR_WORKSPACE;
+    return create(cfg, kv, kv_bytes, static_cast<float*>(scales), workspace, ws_bytes, static_cast<cudaStream_t>(stream), out);
 }
 
 int32_t odb_paged_destroy(odb_paged* h) {
@@ -186,6 +221,7 @@ int32_t odb_paged_norm_rope_store(odb_paged* h, int32_t layer, const odb_paged_b
     if (rope->rot_dim < 0 || rope->rot_dim > c.head_dim || rope->rot_dim % 8) return ODB_ERR_SHAPE;
     if (b->max_rows == 0) return ODB_OK;
     if (!r->q || !r->k || !r->v || !r->q_out || !b->row_pos || !b->row_slot || (rope->rot_dim && !rope->turns)) return ODB_ERR_ARG;
+    if (h->scales && (!b->row_seq || !b->len_after || b->n_seqs < 1)) return ODB_ERR_ARG;
     if (!(eps >= 0.f) || !isfinite(eps) || !isfinite(rope->magnitude)) return ODB_ERR_ARG;
     const int64_t qw = static_cast<int64_t>(c.n_heads) * c.head_dim, kw = static_cast<int64_t>(c.n_kv_heads) * c.head_dim;
     if (r->q_stride < qw || r->out_stride < qw || r->k_stride < kw || r->v_stride < kw) return ODB_ERR_ARG;
@@ -208,10 +244,20 @@ int32_t odb_paged_norm_rope_store(odb_paged* h, int32_t layer, const odb_paged_b
     a.turns = reinterpret_cast<const unsigned long long*>(rope->turns);
     a.magnitude = rope->magnitude;
     a.row_pos = b->row_pos; a.row_slot = b->row_slot;
-    a.k_pool = h->kv + static_cast<size_t>(2 * layer) * h->layer_rows * c.head_dim;
-    a.v_pool = a.k_pool + static_cast<size_t>(h->layer_rows) * c.head_dim;
     a.rows = b->max_rows; a.H = c.n_heads; a.KV = c.n_kv_heads; a.HD = c.head_dim;
     a.rot = rope->rot_dim; a.interleaved = rope->interleaved != 0; a.page_shift = h->page_shift; a.n_pages = c.n_pages;
+    if (h->scales) {
+        PagedE4m3StoreArgs p{};
+        p.rows = a;
+        p.rows.KV = 0;
+        p.row_seq = b->row_seq; p.len = b->len_after;
+        p.k_pool = reinterpret_cast<unsigned char*>(h->k_of(layer)); p.v_pool = reinterpret_cast<unsigned char*>(h->v_of(layer));
+        p.k_scales = h->k_scales_of(layer); p.v_scales = h->v_scales_of(layer);
+        p.KV = c.n_kv_heads; p.n_seqs = b->n_seqs;
+        p.window = b->max_rows / b->n_seqs >= kPagedBlock ? kPagedBlock : 1;
+        return enqueued(launch_paged_e4m3_store(p, static_cast<cudaStream_t>(stream)));
+    }
+    a.k_pool = reinterpret_cast<__nv_bfloat16*>(h->k_of(layer)); a.v_pool = reinterpret_cast<__nv_bfloat16*>(h->v_of(layer));
     return enqueued(launch_paged_store(a, static_cast<cudaStream_t>(stream)));
 }
 
@@ -231,7 +277,7 @@ int32_t odb_paged_attention(odb_paged* h, int32_t layer, const odb_paged_batch* 
     if (overlap({out, out_stride, qw}, {q, q_stride, qw}, b->max_rows)) return ODB_ERR_ARG;   // some CTAs read Q after others have written
     const int G = c.n_heads / c.n_kv_heads;
     if (static_cast<double>(b->max_rows) * c.n_heads >= 2147483648.0 - 65536) return ODB_ERR_SHAPE;   // packed rows are 32-bit numbers
-    const int q_tiles = paged_attention_kernel_of(b->n_seqs, b->max_rows, b->max_new, G, c.n_kv_heads, longest, out_stride);
+    const int q_tiles = (h->scales ? paged_e4m3_attention_kernel_of : paged_attention_kernel_of)(b->n_seqs, b->max_rows, b->max_new, G, c.n_kv_heads, longest, out_stride);
     if (q_tiles < 0) return ODB_ERR_SHAPE;
     PagedAttnArgs a{};
     a.q = static_cast<const __nv_bfloat16*>(q);
@@ -241,7 +287,8 @@ int32_t odb_paged_attention(odb_paged* h, int32_t layer, const odb_paged_batch* 
     a.table = b->table; a.len = b->len_after; a.first = b->first; a.row_start = b->row_start;
     a.n_seqs = b->n_seqs; a.max_rows = b->max_rows; a.H = c.n_heads; a.KV = c.n_kv_heads; a.G = G;
     a.page_shift = h->page_shift; a.n_pages = c.n_pages; a.table_stride = b->table_stride;
-    a.pool = reinterpret_cast<const unsigned short*>(h->kv);
+    a.pool = static_cast<const unsigned short*>(h->kv);
+    a.scales = h->scales;
     a.k_row0 = 2 * layer * h->layer_rows; a.v_row0 = a.k_row0 + h->layer_rows; a.pool_rows = h->pool_rows;
     a.left = left < 0 || left > kPagedUnlimited ? kPagedUnlimited : left;
     a.right = right < 0 || right > kPagedUnlimited ? kPagedUnlimited : right;
@@ -249,7 +296,28 @@ int32_t odb_paged_attention(odb_paged* h, int32_t layer, const odb_paged_batch* 
     a.scale_log2 = (scale != 0.f ? scale : 1.0f / sqrtf(static_cast<float>(c.head_dim))) * 1.4426950408889634f;
     a.status = h->status; a.arrivals = h->arrivals; a.part_o = h->part_o; a.part_ml = h->part_ml;
     a.shared = h->shared;
-    return enqueued(launch_paged_attention(a, h->maps, c.head_dim, q_tiles, h->sms, static_cast<cudaStream_t>(stream)));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (h->scales) return enqueued(launch_paged_e4m3_attention(a, h->maps.rows, c.head_dim, q_tiles, h->sms, st));
+    return enqueued(launch_paged_attention(a, h->maps, c.head_dim, q_tiles, h->sms, st));
+}
+
+int32_t odb_paged_load(odb_paged* h, int32_t layer, const odb_paged_batch* b, void* k, int64_t k_stride, void* v, int64_t v_stride, void* stream) {
+    const int32_t rc = check_call(h, layer);
+    if (rc != ODB_OK) return rc;
+    if (!b || b->max_rows < 0) return ODB_ERR_ARG;
+    if (b->max_rows == 0) return ODB_OK;
+    const odb_paged_config& c = h->cfg;
+    const int64_t width = static_cast<int64_t>(c.n_kv_heads) * c.head_dim;
+    if (!k || !v || !b->row_slot || k_stride < width || v_stride < width || ((k_stride | v_stride) & 7) || !aligned(k, 16) || !aligned(v, 16)) return ODB_ERR_ARG;
+    if (overlap({k, k_stride, width}, {v, v_stride, width}, b->max_rows)) return ODB_ERR_ARG;
+    PagedLoadArgs a{};
+    a.k_pool = reinterpret_cast<const unsigned char*>(h->k_of(layer)); a.v_pool = reinterpret_cast<const unsigned char*>(h->v_of(layer));
+    a.k_scales = h->k_scales_of(layer); a.v_scales = h->v_scales_of(layer);
+    a.row_slot = b->row_slot;
+    a.k_out = static_cast<__nv_bfloat16*>(k); a.v_out = static_cast<__nv_bfloat16*>(v);
+    a.k_stride = k_stride; a.v_stride = v_stride;
+    a.rows = b->max_rows; a.KV = c.n_kv_heads; a.HD = c.head_dim; a.page_shift = h->page_shift; a.n_pages = c.n_pages;
+    return enqueued(launch_paged_load(a, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

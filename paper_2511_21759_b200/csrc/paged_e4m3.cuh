@@ -1,0 +1,45 @@
+// Codes of 8 bits (e4m3: a sign, four bits of exponent, three behind the first; 0x7f and 0xff are NaN, the largest number is 448) and
+// the powers of two that they are scaled by.
+#pragma once
+
+#include "paged.cuh"
+
+namespace odb {
+
+namespace {
+
+// 2^e for -126 <= e <= 127
+__device__ __forceinline__ float exp2_int(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
+// the exponent of a scale: a power of two from a pool, whatever its memory holds
+__device__ __forceinline__ int e4m3_exponent(float scale) {
+    return min(max(static_cast<int>(__float_as_uint(scale) >> 23 & 255u) - 127, kPagedLowExp), kPagedHighExp);
+}
+// the smallest exponent with top <= 448 * 2^e: 448 = 1.75 * 2^8, and a fraction above 1.75 carries into the exponent
+__device__ __forceinline__ int e4m3_exponent_for(float top) {
+    return min(max(static_cast<int>((__float_as_uint(top) + 0x1fffffu) >> 23) - 127 - 8, kPagedLowExp), kPagedHighExp);
+}
+// two codes, to the nearest even, the first in the low byte; beyond 448 the largest number
+__device__ __forceinline__ unsigned short e4m3x2_of(float a, float b) {
+    unsigned short r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %2, %1;" : "=h"(r) : "f"(a), "f"(b));
+    return r;
+}
+// the values of two codes, exact, the low byte's in the low half
+__device__ __forceinline__ uint32_t f16x2_of(unsigned short codes) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(codes));
+    return r;
+}
+__device__ __forceinline__ float2 f32x2_of(unsigned short codes) {
+    const uint32_t h = f16x2_of(codes);
+    return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+// four codes times a power of two, rounded again
+__device__ __forceinline__ uint32_t e4m3x4_times(uint32_t codes, float by) {
+    const float2 a = f32x2_of(static_cast<unsigned short>(codes)), b = f32x2_of(static_cast<unsigned short>(codes >> 16));
+    return e4m3x2_of(a.x * by, a.y * by) | static_cast<uint32_t>(e4m3x2_of(b.x * by, b.y * by)) << 16;
+}
+
+}  // namespace
+
+}  // namespace odb

@@ -1,0 +1,79 @@
+// Rows back from the pool, by their slots, as bf16: out = code * scale, which a scale of 2^-100 .. 2^119 leaves exact (a code's three
+// bits, and 2^-9 * 2^-100 is no less than the smallest number of bf16); of a pool of bf16 the values themselves.
+//
+// A thread takes 16 values of a head, a warp's threads lie side by side along a row: reads of a head's values in one piece, writes of
+// whole rows.  Four of them are in flight at once.
+#include "paged_e4m3.cuh"
+
+namespace odb {
+
+namespace {
+
+constexpr int kThreads = 256, kAtOnce = 4;
+
+template <int HD, bool E4M3>
+__global__ void __launch_bounds__(kThreads) paged_load_kernel(const PagedLoadArgs p, const PagedDiv by_row) {
+    constexpr int kPieces = HD / 16;                            // of a head
+    pdl_launch_dependents();
+    pdl_wait();
+    const int r0 = blockIdx.x * p.block_rows, all = min(p.block_rows, p.rows - r0) * p.per_row, half = p.per_row / 2;
+    for (int u0 = threadIdx.x; u0 < all; u0 += kThreads * kAtOnce) {
+        uint4 v[kAtOnce][E4M3 ? 1 : 2];
+        float scale[kAtOnce];
+        __nv_bfloat16* out[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const int u = u0 + k * kThreads;
+            out[k] = nullptr;
+            if (u >= all) continue;
+            const int row = by_row(u), x = u - row * p.per_row;
+            const bool is_v = x >= half;
+            const int head = (is_v ? x - half : x) / kPieces, piece = x % kPieces, r = r0 + row;
+            const int slot = p.row_slot[r], page = slot >> p.page_shift;
+            if (slot < 0 || page >= p.n_pages) continue;
+            const size_t at = ((static_cast<size_t>(page) * p.KV + head) << p.page_shift) + (slot & ((1 << p.page_shift) - 1));
+            const unsigned char* src = (is_v ? p.v_pool : p.k_pool) + (at * HD + piece * 16) * (E4M3 ? 1 : 2);
+#pragma unroll
+            for (int i = 0; i < (E4M3 ? 1 : 2); ++i) v[k][i] = reinterpret_cast<const uint4*>(src)[i];
+            if (E4M3) scale[k] = (is_v ? p.v_scales : p.k_scales)[at / kPagedBlock];
+            out[k] = (is_v ? p.v_out + r * p.v_stride : p.k_out + r * p.k_stride) + head * HD + piece * 16;
+        }
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            if (!out[k]) continue;
+            uint4 y[2];
+            if constexpr (E4M3) {
+                const uint32_t c[4] = {v[k][0].x, v[k][0].y, v[k][0].z, v[k][0].w};
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float2 f = f32x2_of(static_cast<unsigned short>(c[i / 2] >> 16 * (i & 1)));
+                    w[i] = paged_bf16x2(f.x * scale[k], f.y * scale[k]);
+                }
+                y[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                y[1] = make_uint4(w[4], w[5], w[6], w[7]);
+            } else {
+                y[0] = v[k][0];
+                y[1] = v[k][1];
+            }
+            reinterpret_cast<uint4*>(out[k])[0] = y[0];
+            reinterpret_cast<uint4*>(out[k])[1] = y[1];
+        }
+    }
+}
+
+template <int HD, bool E4M3>
+cudaError_t launch(PagedLoadArgs a, cudaStream_t st) {
+    a.per_row = 2 * a.KV * (HD / 16);
+    a.block_rows = a.per_row >= kThreads * kAtOnce ? 1 : kThreads * kAtOnce / a.per_row;
+    return launch_kernel(paged_load_kernel<HD, E4M3>, dim3((a.rows + a.block_rows - 1) / a.block_rows), dim3(kThreads), 0, st, a, PagedDiv::by(a.per_row));
+}
+
+}  // namespace
+
+cudaError_t launch_paged_load(PagedLoadArgs a, cudaStream_t st) {
+    if (a.k_scales) return a.HD == 128 ? launch<128, true>(a, st) : launch<64, true>(a, st);
+    return a.HD == 128 ? launch<128, false>(a, st) : launch<64, false>(a, st);
+}
+
+}  // namespace odb

@@ -26,7 +26,7 @@ import torch
 
 from . import binding as B
 
-_BF16, _F32 = torch.bfloat16, torch.float32
+_BF16, _F32, _E4M3 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
 _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 _ROWS = struct.Struct("=QqQqQqQqQQ")          # odb_paged_rows, filled in one go
 SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
@@ -132,36 +132,58 @@ class Batch(_OnStream):
 
 
 class PagedCache(_OnStream):
-    """A pool of K/V pages (bf16 [n_layers][2][n_pages][n_kv_heads][page_size][head_dim]) and the calls over it.  kv: a
-    tensor of that shape to use; otherwise one is allocated (not cleared: what no request has written reaches no result)."""
+    """A pool of K/V pages ([n_layers][2][n_pages][n_kv_heads][page_size][head_dim]) and the calls over it, in bf16 or, dtype
+    torch.float8_e4m3fn, in half the memory: codes of 8 bits with a scale, a power of two, for each block of 16 positions of a head (float32
+    [n_layers][2][n_pages][n_kv_heads][page_size / 16]; K or V of a position is code * scale), which norm_rope_store writes and load and
+    attention read.  kv, and scales beside it: tensors of that shape to use; otherwise they are allocated (not cleared: what no request has
+    written reaches no result)."""
 
-    def __init__(self, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, *, kv=None, device=None):
+    def __init__(self, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, *, dtype=None, kv=None,
+                 scales=None, device=None):
         lib = B.lib()
         self.cfg = B.odb_paged_config(n_layers, n_heads, n_kv_heads, head_dim, page_size, n_pages)
         self.n_layers, self.n_heads, self.n_kv_heads, self.head_dim, self.page_size, self.n_pages = \
             n_layers, n_heads, n_kv_heads, head_dim, page_size, n_pages
         self.handle = C.c_void_p()
+        self.dtype = dtype or (kv.dtype if isinstance(kv, torch.Tensor) else _BF16)
+        if self.dtype not in (_BF16, _E4M3):
+            raise ValueError(f"dtype {self.dtype}: torch.bfloat16 or torch.float8_e4m3fn")
         if not lib.odb_paged_kv_bytes(C.byref(self.cfg)):
             raise B.OdbError(B.ODB_ERR_SHAPE, "odb_paged_create")
         shape = (n_layers, 2, n_pages, n_kv_heads, page_size, head_dim)
         if kv is None:
-            kv = torch.empty(shape, dtype=torch.bfloat16, device=device or "cuda")
-        elif tuple(kv.shape) != shape or kv.dtype != torch.bfloat16 or not kv.is_cuda or not kv.is_contiguous():
-            raise ValueError(f"kv: a contiguous bfloat16 CUDA tensor of shape {shape} is wanted")
+            kv = torch.empty(shape, dtype=self.dtype, device=device or "cuda")
+        elif tuple(kv.shape) != shape or kv.dtype != self.dtype or not kv.is_cuda or not kv.is_contiguous():
+            raise ValueError(f"kv: a contiguous {str(self.dtype)[6:]} CUDA tensor of shape {shape} is wanted")
         self.kv = kv
         self.device = kv.device
+        shape = shape[:4] + (page_size // B.ODB_PAGED_SCALE_BLOCK,)
+        if self.dtype is _BF16:
+            if scales is not None:
+                raise ValueError("scales: a pool of bfloat16 has none")
+        elif scales is None:
+            scales = torch.empty(shape, dtype=_F32, device=self.device)
+        elif tuple(scales.shape) != shape or scales.dtype != _F32 or scales.device != self.device or not scales.is_contiguous():
+            raise ValueError(f"scales: a contiguous float32 tensor of shape {shape} on {self.device} is wanted")
+        self.scales = scales
         self.workspace = torch.empty(lib.odb_paged_workspace_bytes(C.byref(self.cfg)), dtype=torch.uint8, device=self.device)
         self._index = self.device.index
-        self._made(self._index, (self.workspace, kv))
+        self._made(self._index, (self.workspace, kv, scales))
+        rest = (self.workspace.data_ptr(), self.workspace.numel(), C.c_void_p(self._raw), C.byref(self.handle))
         with torch.cuda.device(self.device):
-            B.check(lib.odb_paged_create(C.byref(self.cfg), kv.data_ptr(), kv.numel() * 2, self.workspace.data_ptr(),
-                                         self.workspace.numel(), C.c_void_p(self._raw), C.byref(self.handle)), "odb_paged_create")
+            if scales is None:
+                B.check(lib.odb_paged_create(C.byref(self.cfg), kv.data_ptr(), kv.numel() * 2, *rest), "odb_paged_create")
+            else:
+                B.check(lib.odb_paged_create_e4m3(C.byref(self.cfg), kv.data_ptr(), kv.numel(), scales.data_ptr(), scales.numel() * 4, *rest),
+                        "odb_paged_create_e4m3")
         self._shape = (self.device, n_heads, n_kv_heads, head_dim, page_size, n_pages)     # what a batch depends on
         self._gain_shape = torch.Size((head_dim,))
-        self._new, self._width = kv.new_empty, n_heads * head_dim       # outputs: bf16 on the cache's device (1.4 us; torch.empty 3.1)
+        # outputs: bf16 on the cache's device (1.4 us; torch.empty 3.1)
+        self._new, self._width = torch.empty(0, dtype=_BF16, device=self.device).new_empty, n_heads * head_dim
         self._rows_c = B.odb_paged_rows()
         self._rows_ref = C.byref(self._rows_c)
         self._layout, self._store, self._attention = lib.odb_paged_layout, lib.odb_paged_norm_rope_store, lib.odb_paged_attention
+        self._load = lib.odb_paged_load
 
     def close(self):
         if self.handle:
@@ -229,7 +251,8 @@ class PagedCache(_OnStream):
         """Norm of every q and k head (where a gain is given), rotation by row_pos, K and V into row_slot
         (odb_paged_norm_rope_store).  q, k, v: [max_rows][heads][head_dim] or [max_rows][heads * head_dim], slices of one
         projection's output as they are.  Returns q_out (a new tensor where none is given; q itself may be given, other rows that overlap
-        q, k or v are refused)."""
+        q, k or v are refused).  Over a pool of 8 bits K and V are quantised as they are written, under a scale that fits the largest value
+        of each block of 16 positions and what the block keeps of earlier calls; it then takes row_seq and len_after too."""
         if _current_device() != self._index:
             return self._there(self.norm_rope_store, layer, batch, q, k, v, rope, q_gain=q_gain, k_gain=k_gain, eps=eps, q_out=q_out)
         if batch.cache is not self:
@@ -274,6 +297,24 @@ class PagedCache(_OnStream):
         if status:
             raise B.OdbError(status, "odb_paged_attention")
         return out
+
+    def load(self, layer: int, batch: Batch, *, k_out=None, v_out=None):
+        """K and V of the batch's rows back from row_slot (odb_paged_load): bf16 [max_rows][n_kv_heads][head_dim] each, exact from either pool.
+        Returns (k, v), new tensors where none are given; a row whose slot is none is left as it is (of a new tensor: as the memory was)."""
+        if _current_device() != self._index:
+            return self._there(self.load, layer, batch, k_out=k_out, v_out=v_out)
+        if batch.cache is not self:
+            self._other(batch)
+        if k_out is None:
+            k_out = self._new(batch.max_rows, self.n_kv_heads, self.head_dim)
+        if v_out is None:
+            v_out = self._new(batch.max_rows, self.n_kv_heads, self.head_dim)
+        kp, ks = self._rows(k_out, "k_out", self.n_kv_heads, batch._kv)
+        vp, vs = self._rows(v_out, "v_out", self.n_kv_heads, batch._kv)
+        status = self._load(self.handle, layer, batch._ref, kp, ks, vp, vs, self._current(batch, batch))
+        if status:
+            raise B.OdbError(status, "odb_paged_load")
+        return k_out, v_out
 
     def status(self) -> int:
         """Waits for the current stream; ODB_OK or what the device has found since the last call (read and cleared)."""
