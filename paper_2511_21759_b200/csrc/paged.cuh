@@ -194,13 +194,13 @@ struct PagedShares {
     int size[kPagedWaves], at_once;
     __device__ __forceinline__ void divide(int total, int waves, int min_units, int full_units, const PagedDiv& by_once) {
         // 45, 27, 17 and 11 of a hundred: see the launcher of the few rows' kernel
-        constexpr int kPart[kPagedWaves] = {115, 69, 44, 28};
+        constexpr int kPart[kPagedWaves] = {115, 69, 44, 28}, kPartOfTwo = 180;
         const int most = by_once(total + at_once - 1), least = max(min_units, min(full_units, most));
         int left = total;
 #pragma unroll
         for (int w = 0; w < kPagedWaves; ++w) {
             const int all = by_once(left + at_once - 1);
-            const int part = w + 1 < waves ? static_cast<int>(static_cast<unsigned>(most) * kPart[w] / 256) + 1 : all;
+            const int part = w + 1 < waves ? static_cast<int>(static_cast<unsigned>(most) * (waves == 2 ? kPartOfTwo : kPart[w]) / 256) + 1 : all;
             size[w] = max(min(part, all), least);
             left -= min(left, size[w] * at_once);
         }
@@ -481,7 +481,17 @@ struct PagedPages {
             }
             if (TOGETHER) __syncwarp();
         }
-        const int page = __shfl_sync(0xffffffffu, entry, p - first);
+        return at(a, head, pos, base, __shfl_sync(0xffffffffu, entry, p - first));
+    }
+    // Position pos + more of each lane, of those that `wanted` says (others get the row behind the pool): at most 64 positions from pos on,
+    // which is a multiple of them, so that their pages are among the 32 entries with pos's.
+    template <bool ASK>
+    __device__ __forceinline__ int rows(const PagedAttnArgs& a, const PagedSeq& q, int s, int head, int pos, int more, bool wanted, int base) {
+        row<ASK, true>(a, q, s, head, pos, base);
+        const int p = pos + more, i = (p >> a.page_shift) - first, page = __shfl_sync(0xffffffffu, entry, i & 31);
+        return wanted && i < 32 ? at(a, head, p, base, page) : a.pool_rows;
+    }
+    __device__ __forceinline__ static int at(const PagedAttnArgs& a, int head, int pos, int base, int page) {
         return page >= 0 && page < a.n_pages ? base + ((page * a.KV + head) << a.page_shift) + (pos & ((1 << a.page_shift) - 1)) : a.pool_rows;
     }
 };

@@ -98,7 +98,7 @@ def _kernels(source):
 LAUNCHES = {  # source: {kernel: (threads, CTAs on an SM)}
     "paged_e4m3_store.cu": {("paged_e4m3_store_kernel", d, i, w): (64, 5) for d in (64, 128) for i in (0, 1) for w in (0, 1)},
     "paged_load.cu": {("paged_load_kernel", d, f): (256, 4) for d in (64, 128) for f in (0, 1)},
-    "paged_e4m3_attention.cu": {("paged_e4m3_attention_kernel", d): (160, 2) for d in (64, 128)},
+    "paged_e4m3_attention.cu": {("paged_e4m3_attention_kernel", d, n): (160, 4 if n == 8 else 2) for d in (64, 128) for n in (8, 16)},
 }
 
 
@@ -108,4 +108,5 @@ def test_kernels_fit_and_spill_nothing(source):
     assert set(seen) == set(LAUNCHES[source])
     for kernel, (threads, ctas) in LAUNCHES[source].items():
         registers, spills = seen[kernel]
-        assert ctas * threads * (-(-registers // 8) * 8) <= 65536 and spills == 0, (kernel, registers, spills)
+        # a scheduler's quarter of the registers goes to whole warps
+        assert -(-ctas * threads // 128) * 32 * (-(-registers // 8) * 8) <= 16384 and spills == 0, (kernel, registers, spills)
