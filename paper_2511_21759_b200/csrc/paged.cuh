@@ -194,13 +194,13 @@ struct PagedShares {
     int size[kPagedWaves], at_once;
     __device__ __forceinline__ void divide(int total, int waves, int min_units, int full_units, const PagedDiv& by_once) {
         // 45, 27, 17 and 11 of a hundred: see the launcher of the few rows' kernel
-        constexpr int kPart[kPagedWaves] = {115, 69, 44, 28}, kPartOfTwo = 180;
+        constexpr int kPart[kPagedWaves] = {115, 69, 44, 28};
         const int most = by_once(total + at_once - 1), least = max(min_units, min(full_units, most));
         int left = total;
 #pragma unroll
         for (int w = 0; w < kPagedWaves; ++w) {
             const int all = by_once(left + at_once - 1);
-            const int part = w + 1 < waves ? static_cast<int>(static_cast<unsigned>(most) * (waves == 2 ? kPartOfTwo : kPart[w]) / 256) + 1 : all;
+            const int part = w + 1 < waves ? static_cast<int>(static_cast<unsigned>(most) * kPart[w] / 256) + 1 : all;
             size[w] = max(min(part, all), least);
             left -= min(left, size[w] * at_once);
         }

@@ -29,10 +29,9 @@ constexpr int kFullUnits = 12;              // of a CTA where all places on the 
 constexpr int kMmaWarps = 4;                // 16 keys of a tile each
 constexpr int kThreads = 32 * (kMmaWarps + 1);
 constexpr int kBlocks = kKT / kPagedBlock;  // of a tile
-template <int NR> constexpr int kCtas = NR == 8 ? 4 : 2;                    // of an SM: a warp's chain is hidden by the other CTAs', and so is a CTA's start
-template <int NR> constexpr int kWaves = NR == 8 ? 2 : kPagedWaves;
+template <int NR> constexpr int kCtas = NR == 8 ? 3 : 2;                    // of an SM
 template <int HD> constexpr uint32_t kTileBytes = kKT * HD;                 // K or V of a tile
-template <int HD, int NR> constexpr int kStages = HD == 128 ? (NR == 8 ? 3 : 7) : (NR == 8 ? 6 : 13);   // K and V tiles on the way or in use
+template <int HD, int NR> constexpr int kStages = HD == 128 ? (NR == 8 ? 4 : 7) : (NR == 8 ? 8 : 13);   // K and V tiles on the way or in use
 
 template <int HD, int NR>
 struct Shared {
@@ -131,7 +130,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<NR>) paged_e4m3_attention_kern
     // the ring's memory holds the sums until the start is found
     static_assert(sizeof(PagedScratch) <= S * 2 * kT, "the scratch fits the rings");
     PagedStart start;
-    const bool any = paged_find_start<kThreads, kKT, kItem, true>(a, *reinterpret_cast<PagedScratch*>(smem), kWaves<NR>, kMinUnits, kFullUnits, start);
+    const bool any = paged_find_start<kThreads, kKT, kItem, true>(a, *reinterpret_cast<PagedScratch*>(smem), 1, kMinUnits, kFullUnits, start);
     if (!any) return;                                           // block-uniform
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the scratch's writes before the copies that take its place
     __syncthreads();
@@ -260,78 +259,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<NR>) paged_e4m3_attention_kern
             const uint32_t sk = tiles + stage * 2 * kT, sv = sk + kT;
             const bool any_key = k0 < w.k.hi && (k0 + KW > w.k.lo || k0 < a.sinks);   // some row of the item sees some key
             if (ok && any_key) {
-                float s[NG][4];                                 // keys lane / 4 and 8 behind it, each of two rows
-#pragma unroll
-                for (int n = 0; n < NG; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
-#pragma unroll
-                for (int c = 0; c < NC; c += 2) {
-                    uint32_t x[4];                              // keys 0 .. 7 of chunk c and the next, then keys 8 .. 15
-                    ldsm4(sk + chunk_at(warp * KW + (lane & 7) + ((lane >> 4) << 3), c + (lane >> 3 & 1)), x);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint32_t ka[4] = {low_codes(x[h]), low_codes(x[2 + h]), high_codes(x[h]), high_codes(x[2 + h])};
-#pragma unroll
-                        for (int n = 0; n < NG; ++n) mma(s[n], ka, qf[n][c + h][0], qf[n][c + h][1]);
-                    }
-                }
-                const float ks = sh->scale[stage][0][warp];
-                const float log_vs = static_cast<float>(static_cast<int>(__float_as_uint(sh->scale[stage][1][warp]) >> 23) - 127);
                 const bool whole = k0 + KW <= all_hi && (k0 >= all_lo || k0 + KW <= a.sinks);
-                float top[NE];
-#pragma unroll
-                for (int e = 0; e < NE; ++e) {
-                    float* x = &s[e >> 1][e & 1];               // x[0], x[2]
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        x[2 * h] *= unit[e] * ks;
-                        if (!whole) {
-                            const int key = k0 + h * 8 + (lane >> 2);
-                            const bool seen = key < w.q.len && key - a.right <= pos[e] && (key + a.left >= pos[e] || key < a.sinks);
-                            x[2 * h] = seen ? x[2 * h] : -INFINITY;
-                        }
-                    }
-                    top[e] = row_max(fmaxf(x[0], x[2]));
-                }
-                float factor[NE], shift[NE], more[NE];
-                bool same = true, far = false;                  // far: a block's weights might vanish that its sum needs
-#pragma unroll
-                for (int e = 0; e < NE; ++e) {
-                    factor[e] = 1.f;
-                    shift[e] = more[e] = 0.f;
-                    const float mn = fmaxf(m[e], top[e]);
-                    if (mn == -INFINITY) continue;              // the row has seen no key
-                    const float before = m[e] - mn + g[e], gn = fmaxf(before, top[e] - mn + log_vs);
-                    l[e] *= ex2_approx(m[e] - mn);
-                    factor[e] = ex2_approx(before - gn);
-                    shift[e] = mn;
-                    more[e] = log_vs - gn;
-                    m[e] = mn;
-                    g[e] = gn;
-                    same = same && factor[e] == 1.f;
-                    far = far || more[e] < -60.f;
-                }
-                far = __any_sync(0xffffffffu, far);
-#pragma unroll
-                for (int e = 0; e < NE; ++e) {
-                    float* x = &s[e >> 1][e & 1];
-                    const float y0 = x[0] - shift[e], y1 = x[2] - shift[e];
-                    x[0] = ex2_approx(y0 + more[e]);
-                    x[2] = ex2_approx(y1 + more[e]);
-                    l[e] += far ? ex2_approx(y0) + ex2_approx(y1) : (x[0] + x[2]) * ex2_approx(-more[e]);
-                }
-                uint32_t p[NG][2];
-#pragma unroll
-                for (int n = 0; n < NG; ++n)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) p[n][h] = turned(f16x2(s[n][2 * h], s[n][2 * h + 1]));
-                if (!__all_sync(0xffffffffu, same)) {
-#pragma unroll
-                    for (int n = 0; n < NG; ++n)
-#pragma unroll
-                        for (int c = 0; c < NC; ++c)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) o[n][c][j] *= factor[2 * n + (j & 1)];
-                }
                 if (!whole) {
                     // V in places that a row does not see: zero where no row sees it, by the element where it is NaN
                     constexpr int kChunks = KW * HD / 16 / 32;  // 16-byte chunks of a lane
@@ -385,18 +313,94 @@ __global__ void __launch_bounds__(kThreads, kCtas<NR>) paged_e4m3_attention_kern
                     }
                     __syncwarp();
                 }
+                uint32_t kx[NC / 2][4], vx[NC / 2][4];          // both tiles' words at once: V's become f16 while the scores are on their way
 #pragma unroll
-                for (int c = 0; c < NC; c += 2) {
-                    uint32_t x[4];                              // keys 0 .. 7 and 8 .. 15 of chunk c, then of the next
-                    ldsm4_t(sv + chunk_at(warp * KW + (lane & 15), c + (lane >> 4)), x);
+                for (int c = 0; c < NC / 2; ++c)                // keys 0 .. 7 of chunk 2 c and the next, then keys 8 .. 15
+                    ldsm4(sk + chunk_at(warp * KW + (lane & 7) + ((lane >> 4) << 3), 2 * c + (lane >> 3 & 1)), kx[c]);
+#pragma unroll
+                for (int c = 0; c < NC / 2; ++c)                // keys 0 .. 7 and 8 .. 15 of chunk 2 c, then of the next
+                    ldsm4_t(sv + chunk_at(warp * KW + (lane & 15), 2 * c + (lane >> 4)), vx[c]);
+                float s[NG][4], odd[NG][4];                     // keys lane / 4 and 8 behind it, each of two rows; every other step in sums of its own
+#pragma unroll
+                for (int n = 0; n < NG; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[n][j] = odd[n][j] = 0.f;
+#pragma unroll
+                for (int c = 0; c < NC / 2; ++c)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t ka[4] = {low_codes(kx[c][h]), low_codes(kx[c][2 + h]), high_codes(kx[c][h]), high_codes(kx[c][2 + h])};
+#pragma unroll
+                        for (int n = 0; n < NG; ++n) mma(h ? odd[n] : s[n], ka, qf[n][2 * c + h][0], qf[n][2 * c + h][1]);
+                    }
+                const float ks = sh->scale[stage][0][warp];
+                const float log_vs = static_cast<float>(static_cast<int>(__float_as_uint(sh->scale[stage][1][warp]) >> 23) - 127);
+                float top[NE];
+#pragma unroll
+                for (int e = 0; e < NE; ++e) {
+                    float* x = &s[e >> 1][e & 1];               // x[0], x[2]
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        x[2 * h] = (x[2 * h] + odd[e >> 1][2 * h + (e & 1)]) * (unit[e] * ks);
+                        if (!whole) {
+                            const int key = k0 + h * 8 + (lane >> 2);
+                            const bool seen = key < w.q.len && key - a.right <= pos[e] && (key + a.left >= pos[e] || key < a.sinks);
+                            x[2 * h] = seen ? x[2 * h] : -INFINITY;
+                        }
+                    }
+                    top[e] = row_max(fmaxf(x[0], x[2]));
+                }
+                float factor[NE], shift[NE], more[NE];
+                bool rare = false;                              // O has to be rescaled
+#pragma unroll
+                for (int e = 0; e < NE; ++e) {
+                    factor[e] = 1.f;
+                    shift[e] = more[e] = 0.f;
+                    const float mn = fmaxf(m[e], top[e]);
+                    if (mn == -INFINITY) continue;              // the row has seen no key
+                    const float before = m[e] - mn + g[e], gn = fmaxf(before, top[e] - mn + log_vs);
+                    l[e] *= ex2_approx(m[e] - mn);
+                    factor[e] = ex2_approx(before - gn);
+                    shift[e] = mn;
+                    more[e] = log_vs - gn;
+                    m[e] = mn;
+                    g[e] = gn;
+                    rare = rare || before != gn;
+                }
+                float sum[NE];
+#pragma unroll
+                for (int e = 0; e < NE; ++e) {
+                    float* x = &s[e >> 1][e & 1];
+                    const float y0 = x[0] - shift[e], y1 = x[2] - shift[e];
+                    x[0] = ex2_approx(y0 + more[e]);
+                    x[2] = ex2_approx(y1 + more[e]);
+                    // weights that a far larger scale elsewhere lets vanish still count in the sum
+                    sum[e] = more[e] < -60.f ? ex2_approx(y0) + ex2_approx(y1) : (x[0] + x[2]) * ex2_approx(-more[e]);
+                }
+#pragma unroll
+                for (int e = 0; e < NE; ++e) l[e] += sum[e];
+                uint32_t p[NG][2];
+#pragma unroll
+                for (int n = 0; n < NG; ++n)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) p[n][h] = turned(f16x2(s[n][2 * h], s[n][2 * h + 1]));
+                if (__any_sync(0xffffffffu, rare)) {
+#pragma unroll
+                    for (int n = 0; n < NG; ++n)
+#pragma unroll
+                        for (int c = 0; c < NC; ++c)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) o[n][c][j] *= factor[2 * n + (j & 1)];
+                }
+#pragma unroll
+                for (int c = 0; c < NC / 2; ++c)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {               // a word: two keys of an even dim, then of the odd one
-                        const uint32_t y = __byte_perm(x[2 * h], 0, 0x3120), z = __byte_perm(x[2 * h + 1], 0, 0x3120);
+                        const uint32_t y = __byte_perm(vx[c][2 * h], 0, 0x3120), z = __byte_perm(vx[c][2 * h + 1], 0, 0x3120);
                         const uint32_t va[4] = {low_codes(y), high_codes(y), low_codes(z), high_codes(z)};
 #pragma unroll
-                        for (int n = 0; n < NG; ++n) mma(o[n][c + h], va, p[n][0], p[n][1]);
+                        for (int n = 0; n < NG; ++n) mma(o[n][2 * c + h], va, p[n][0], p[n][1]);
                     }
-                }
                 if (!whole) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // this warp's writes to V before the next copy into it
             }
             if (t + 1 == w.t1) break;                 // the item's last V tile stays: its place is where the warps meet
@@ -533,7 +537,7 @@ cudaError_t launch(PagedAttnArgs a, const CUtensorMap& tmap, int sms, cudaStream
     const long long tiles = (static_cast<long long>(a.table_stride) << a.page_shift) / kKT + 1 + kItem,
                     most = (static_cast<long long>(a.max_rows) * a.G / NR + a.n_seqs) * a.KV * tiles / kMinUnits + 1;
     static_assert(kPagedMaxCtas * 16 <= kPagedPartRows, "parts");
-    const int grid = static_cast<int>(most < kWaves<NR> * a.at_once ? most : kWaves<NR> * a.at_once);
+    const int grid = static_cast<int>(most < a.at_once ? most : a.at_once);
     return launch_kernel(paged_e4m3_attention_kernel<HD, NR>, dim3(grid), dim3(kThreads), kSmem<HD, NR>, st, tmap, a);
 }
 

@@ -96,9 +96,9 @@ def _kernels(source):
 
 
 LAUNCHES = {  # source: {kernel: (threads, CTAs on an SM)}
-    "paged_e4m3_store.cu": {("paged_e4m3_store_kernel", d, i, w): (64, 5) for d in (64, 128) for i in (0, 1) for w in (0, 1)},
+    "paged_e4m3_store.cu": {("paged_e4m3_store_kernel", d, i, w): (64, 4) for d in (64, 128) for i in (0, 1) for w in (0, 1)},
     "paged_load.cu": {("paged_load_kernel", d, f): (256, 4) for d in (64, 128) for f in (0, 1)},
-    "paged_e4m3_attention.cu": {("paged_e4m3_attention_kernel", d, n): (160, 4 if n == 8 else 2) for d in (64, 128) for n in (8, 16)},
+    "paged_e4m3_attention.cu": {("paged_e4m3_attention_kernel", d, n): (160, 3 if n == 8 else 2) for d in (64, 128) for n in (8, 16)},
 }
 
 
