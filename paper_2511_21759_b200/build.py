@@ -9,7 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libodb.so")
 SOURCES = ["gemm_tcgen05.cu", "gemm_rows.cu", "gemm_static.cu", "elementwise.cu", "first_norm.cu", "attention.cu", "attention_tc.cu", "control.cu", "tensor_parallel.cu", "step_persistent.cu",
            "paged_layout.cu", "paged_store.cu", "paged_attention.cu", "paged_attention_tc.cu", "paged_e4m3_store.cu",
-           "paged_load.cu", "paged_e4m3_attention.cu", "paged_api.cu", "odb_api.cu"]
+           "paged_load.cu", "paged_e4m3_attention.cu", "paged_e4m3_attention_tc.cu", "paged_api.cu", "odb_api.cu"]
 
 
 def _stale() -> bool:

@@ -121,6 +121,7 @@ size_t paged_part_bytes(int hd);
 
 // ---- attention over a pool of 8 bits (paged_e4m3_attention.cu) ----
 int paged_e4m3_attention_kernel_of(int n_seqs, int max_rows, int max_new, int group, int kv_heads, long long longest, long long out_stride);
+cudaError_t launch_paged_e4m3_attention_tc(PagedAttnArgs a, const CUtensorMap& map, int hd, int q_tiles, int sms, cudaStream_t st);
 cudaError_t launch_paged_e4m3_attention(PagedAttnArgs a, const CUtensorMap& map, int hd, int q_tiles, int sms, cudaStream_t st);
 
 #ifdef __CUDACC__

@@ -40,6 +40,20 @@ __device__ __forceinline__ uint32_t e4m3x4_times(uint32_t codes, float by) {
     return e4m3x2_of(a.x * by, a.y * by) | static_cast<uint32_t>(e4m3x2_of(b.x * by, b.y * by)) << 16;
 }
 
+// a box of rows of the pool
+__device__ __forceinline__ void tma_codes(uint32_t dst, const CUtensorMap* tmap, uint64_t* bar, int row) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
+                 "l"(reinterpret_cast<uint64_t>(tmap)), "r"(smem_u32(bar)), "r"(0), "r"(row)
+                 : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+// an arrival once this thread's copies so far have landed; counted among the barrier's
+__device__ __forceinline__ void copies_arrive(uint64_t* bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
 }  // namespace
 
 }  // namespace odb

@@ -26,6 +26,8 @@ constexpr int kItem = 1;                    // key tiles that an item costs besi
 constexpr int kMinUnits = 2;                // units of a CTA, at least
 constexpr int kKT = 64;                     // keys per tile
 constexpr int kFullUnits = 12;              // of a CTA where all places on the SMs have work
+constexpr int kSmallUnits = 1024;           // up to here few rows' kernel for any number of rows
+constexpr int kManyRows = 1024;             // packed rows a request, on average, from which two Q tiles are right whatever the longest
 constexpr int kMmaWarps = 4;                // 16 keys of a tile each
 constexpr int kThreads = 32 * (kMmaWarps + 1);
 constexpr int kBlocks = kKT / kPagedBlock;  // of a tile
@@ -44,19 +46,6 @@ template <int HD, int NR> constexpr uint32_t kSmem = kStages<HD, NR> * 2 * kTile
 template <int HD, int NR> constexpr bool kFits = kCtas<NR> * (kSmem<HD, NR> + 1024) <= 228 * 1024;
 static_assert(kFits<128, 8> && kFits<64, 8> && kFits<128, 16> && kFits<64, 16>, "the CTAs share an SM");
 
-// a box of rows of the pool
-__device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* tmap, uint64_t* bar, int row) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
-                 "l"(reinterpret_cast<uint64_t>(tmap)), "r"(smem_u32(bar)), "r"(0), "r"(row)
-                 : "memory");
-}
-__device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
-}
-// an arrival once this thread's copies so far have landed; counted among the barrier's
-__device__ __forceinline__ void copies_arrive(uint64_t* bar) {
-    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -164,8 +153,8 @@ __global__ void __launch_bounds__(kThreads, kCtas<NR>) paged_e4m3_attention_kern
                 for (int c = 0; c < boxes; ++c) {
                     const int r = __shfl_sync(0xffffffffu, row, c << box_shift >> 4);
                     if (paged_elect()) {
-                        tma_rows(to + c * box * HD, &tm, full, r);
-                        tma_rows(to + kT + c * box * HD, &tm, full, r < a.pool_rows ? r + a.v_row0 - a.k_row0 : r);
+                        tma_codes(to + c * box * HD, &tm, full, r);
+                        tma_codes(to + kT + c * box * HD, &tm, full, r < a.pool_rows ? r + a.v_row0 - a.k_row0 : r);
                     }
                     __syncwarp();
                 }
@@ -543,16 +532,35 @@ cudaError_t launch(PagedAttnArgs a, const CUtensorMap& tmap, int sms, cudaStream
 
 }  // namespace
 
-int paged_e4m3_attention_kernel_of(int n_seqs, int max_rows, int max_new, int group, int kv_heads, long long longest, long long) {
-    const long long all = static_cast<long long>(max_rows) * group, tiles = longest / kKT + 1;
-    return (static_cast<double>(all / 8) + n_seqs) * kv_heads * static_cast<double>(tiles + kItem) < 2147483648.0 - 65536 ? (max_new > 0 ? max_new * group > 8 : all > 8 * n_seqs) : -1;
+// Which kernel, as for a pool of bf16 (paged_attention_kernel_of): 8 or 16, the packed rows of the few rows' items; 1 or 2, the Q tiles of the
+// many rows'; -1, none.
+int paged_e4m3_attention_kernel_of(int n_seqs, int max_rows, int max_new, int group, int kv_heads, long long longest, long long out_stride) {
+    const long long all = static_cast<long long>(max_rows) * group, mean = (max_rows + n_seqs - 1ll) / n_seqs * group,
+                    mine = max_new > 0 ? static_cast<long long>(max_new) * group : mean, tiles = longest / kKT + 1;
+    // units of all items together and what is added to them on the way, with rows that follow one another
+    auto fits = [&](int tile_rows, int item) {
+        return (static_cast<double>(all / tile_rows) + n_seqs) * kv_heads * static_cast<double>(tiles + item) < 2147483648.0 - 65536;
+    };
+    const int few = mine <= 8 && fits(8, kItem) ? 8 : fits(16, kItem) ? 16 : -1;
+    if (group <= kPagedTcMaxGroup && out_stride <= 1ll << 27) {
+        const int tile = kPagedTcMaxGroup / group * group;
+        const double units = static_cast<double>((all + 15ll * n_seqs) / 16) * kv_heads * static_cast<double>(tiles + kItem);
+        if ((mine > 16 && units > kSmallUnits) || few < 0) {
+            const bool alike = max_new > 0 ? static_cast<long long>(max_new) * n_seqs <= 3ll * max_rows : n_seqs == 1 || mean >= kManyRows;
+            const int q_tiles = mine > 128 && alike ? 2 : 1;
+            if (fits(q_tiles * tile, kPagedTcItem)) return q_tiles;
+            return fits(2 * tile, kPagedTcItem) ? 2 : -1;
+        }
+    }
+    return few;
 }
 
 cudaError_t launch_paged_e4m3_attention(PagedAttnArgs a, const CUtensorMap& map, int hd, int kernel, int sms, cudaStream_t st) {
-    if (sms < 1 || 2 * sms * 128 > kPagedPartRows || kPagedWaves * 2 * sms > kPagedMaxCtas) return cudaErrorInvalidValue;   // the workspace's size
+    if (sms < 1 || 2 * sms * 128 > kPagedPartRows || 3 * sms > kPagedMaxCtas) return cudaErrorInvalidValue;   // the workspace's size
     a.by_group = PagedDiv::by(a.G);
-    if (kernel == 0) return hd == 128 ? launch<128, 8>(a, map, sms, st) : launch<64, 8>(a, map, sms, st);
-    return hd == 128 ? launch<128, 16>(a, map, sms, st) : launch<64, 16>(a, map, sms, st);
+    if (kernel == 8) return hd == 128 ? launch<128, 8>(a, map, sms, st) : launch<64, 8>(a, map, sms, st);
+    if (kernel == 16) return hd == 128 ? launch<128, 16>(a, map, sms, st) : launch<64, 16>(a, map, sms, st);
+    return launch_paged_e4m3_attention_tc(a, map, hd, kernel, sms, st);
 }
 
 }  // namespace odb

@@ -1,0 +1,380 @@
+// Attention over a pool of 8 bits: many packed rows, on the tcgen05 tensor cores.  Formulas, masks, the division of the work, products,
+// softmax and results: paged_attention_tc.cu, whose kernel this is behind the K and V tiles in shared memory; K and V of a position are
+// code * scale, numbers of bf16.
+//
+// What is its own is the way there: TMA brings codes into a ring of staging tiles, and converter warps write them as bf16, scaled, into
+// the places of the operands' canonical layout (16 codes of a lane become two pieces of 16 bytes).  A code's fields are moved into
+// place as integers, which leaves its value times 2^-120, and one product in bf16, exact, brings that and the block's scale together:
+// six instructions for two codes.  (By way of f16, where the conversion is one instruction, P and the softmax would have had to take
+// the scales in.)  NaN is found by the largest fields of a tile and put in afterwards.  The converters also do what the loader of bf16
+// does with V at keys that not all rows see: zeros where no row sees them, and NaN is kept for the softmax warps.
+//
+// Registers: the softmax warps take 160, all others 96 of the 128 that a thread is launched with.
+#include "paged_attention_tc.cuh"
+#include "paged_e4m3.cuh"
+
+namespace odb {
+
+namespace {
+
+template <int QT> constexpr int kConvWarps = 2 * QT;
+template <int QT> constexpr int kThreads = 256 * QT;         // 4 QT softmax warps; QT MMA warps, the loader, (two Q tiles: one that idles,) converters
+constexpr int kLaunchRegs = 128, kSoftmaxRegs = 160, kOtherRegs = 96;   // as many warpgroups of the one as of the other
+static_assert(kSoftmaxRegs + kOtherRegs <= 2 * kLaunchRegs, "the split fits what the block was launched with");
+template <int HD, int QT> constexpr int kQBufs = HD == 128 && QT == 1 ? 1 : 2;
+template <int HD, int QT> constexpr int kSlots = HD == 128 ? 2 : (QT == 1 ? 3 : 4);    // K tiles, and V tiles, as operands
+template <int HD, int QT> constexpr int kStaging = HD == 128 ? (QT == 1 ? 2 : 4) : 6;  // tiles of codes
+template <int HD> constexpr uint32_t kCodeBytes = kKT * HD;
+template <int HD, int QT>
+constexpr uint32_t kSmem = kQBufs<HD, QT> * QT * kQBytes<HD> + 2 * kSlots<HD, QT> * kTileBytes<HD> + kStaging<HD, QT> * kCodeBytes<HD> + 1024;
+static_assert(2 * (kSmem<128, 1> + 1024) <= 228 * 1024 && 2 * (kSmem<64, 1> + 1024) <= 228 * 1024 && kSmem<128, 2> <= 227 * 1024 && kSmem<64, 2> <= 227 * 1024, "the CTAs share an SM");
+
+struct alignas(8) SharedE4m3 {
+    uint64_t q_full[2];                // an item's Q tiles landed in the buffer          (loader -> MMA)
+    uint64_t st_full[6];               // a tile of codes and its scales landed           (loader -> converters)
+    uint64_t st_empty[6];              // the converters have read it                     (converters -> loader)
+    uint64_t k_full[4], v_full[4];     // K or V tile written, V looked at                (converters -> MMA; V -> softmax)
+    uint64_t k_empty[4], v_empty[4];   // the MMAs have read the slot                     (MMA -> converters, QT arrivals)
+    uint64_t s_full[2][3];             // S of Q tile g into buffer i has completed       (MMA -> softmax)
+    uint64_t p_full[2][3];             // P has taken its place                           (softmax -> MMA, 4 arrivals)
+    uint64_t pv_done[2][2];            // O += P V of an even / odd tile has completed    (MMA -> MMA, softmax)
+    uint64_t o_full[2];                // the item's last one has                         (MMA -> softmax)
+    uint64_t item_done[2];             // the Q buffer may be overwritten                 (softmax -> loader, 4 QT arrivals)
+    uint32_t tmem_base;
+    int abort, keep_o[2];
+    float scale[6][kKT / kPagedBlock]; // of a staging tile's blocks
+    int odd[4][4];                     // V in the slot has NaN where only some rows see it, by converter
+};
+static_assert(sizeof(SharedE4m3) <= 1024, "the barriers end inside the allocation");
+
+template <int HD_, int QT_>
+struct TcE4m3 {
+    static constexpr int HD = HD_, QT = QT_, NQ = kQBufs<HD, QT>, KS = kSlots<HD, QT>, VS = kSlots<HD, QT>;
+    using Shared = SharedE4m3;
+    // V of the slot has been looked at; it has NaN where only some rows see it; whether this is one (0: it is not)
+    static __device__ __forceinline__ uint64_t* v_seen(Shared* sh, uint32_t slot) { return &sh->v_full[slot]; }
+    static __device__ __forceinline__ bool odd(Shared* sh, uint32_t slot) {
+        int any = 0;
+#pragma unroll
+        for (int i = 0; i < kConvWarps<QT>; ++i) any |= *const_cast<volatile int*>(&sh->odd[slot][i]);
+        return any != 0;
+    }
+    static __device__ __forceinline__ float odd_value(const PagedAttnArgs& a, int row, int d) {
+        const unsigned char code = reinterpret_cast<const unsigned char*>(a.pool)[static_cast<size_t>(row) * HD + d];
+        return (code & 0x7f) == 0x7f ? __uint_as_float(0x7fffffffu) : 0.f;
+    }
+};
+
+// two codes in the upper bytes of the halves -> their values times 2^-120 as bf16; top: the largest fields so far
+__device__ __forceinline__ uint32_t widen_codes(uint32_t x, uint32_t& top) {
+    const uint32_t m = (x >> 4) & 0x07f007f0u;
+    top = max_u16x2(top, m);
+    return m | (x & 0x80008000u);
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t exp2_bf16x2(int e) { return static_cast<uint32_t>(e + 127) * 0x00800080u; }
+
+template <int HD, int QT>
+__global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
+    paged_e4m3_attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_codes,
+                                   const __grid_constant__ CUtensorMap tm_out, const PagedAttnArgs a) {
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    using T = TcE4m3<HD, QT>;
+    constexpr int NQ = T::NQ, SL = kSlots<HD, QT>, ST = kStaging<HD, QT>, CW = kConvWarps<QT>, kFirst = kBufs<HD> - 1, kAtoms = HD / 64;
+    constexpr uint32_t kT = kTileBytes<HD>, kC = kCodeBytes<HD>;
+    constexpr int kSoftmaxWarps = 4 * QT, kLoader = kSoftmaxWarps + QT, kConv = kThreads<QT> / 32 - CW, kBlocks = kKT / kPagedBlock;
+    uint8_t* sQ = smem_raw;                                  // [buffer][Q tile]
+    uint8_t* sK = sQ + NQ * QT * kQBytes<HD>;
+    uint8_t* sV = sK + SL * kT;
+    uint8_t* sC = sV + SL * kT;
+    SharedE4m3* sh = reinterpret_cast<SharedE4m3*>(sC + ST * kC);
+    static_assert(SL <= 4 && ST <= 6 && kBufs<HD> * kKT + HD <= static_cast<int>(kCols) && 4 * kPatch <= kQBytes<HD>, "rings, TMEM columns, patches");
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+    volatile int* cta_abort = &sh->abort;
+
+    if ((smem_u32(smem_raw) & 1023u) != 0) {                // the swizzled tiles need 1024-byte alignment
+        if (tid == 0) atomicExch(a.status, ODB_ERR_CUDA);
+        pdl_wait();
+        return;
+    }
+    if (tid == 0) {
+        tma_prefetch_map(&tm_q);
+        tma_prefetch_map(&tm_codes);
+        for (int i = 0; i < NQ; ++i) {
+            mbar_init(&sh->q_full[i], 1);
+            mbar_init(&sh->item_done[i], kSoftmaxWarps);
+        }
+        for (int i = 0; i < ST; ++i) {
+            mbar_init(&sh->st_full[i], 1 + kBlocks);
+            mbar_init(&sh->st_empty[i], CW);
+        }
+        for (int i = 0; i < SL; ++i) {
+            mbar_init(&sh->k_full[i], CW);
+            mbar_init(&sh->v_full[i], CW);
+            mbar_init(&sh->k_empty[i], QT);
+            mbar_init(&sh->v_empty[i], QT);
+        }
+        for (int g = 0; g < QT; ++g) {
+            for (int b = 0; b < kBufs<HD>; ++b) {
+                mbar_init(&sh->s_full[g][b], 1);
+                mbar_init(&sh->p_full[g][b], 4);
+            }
+            for (int i = 0; i < 2; ++i) mbar_init(&sh->pv_done[g][i], 1);
+            mbar_init(&sh->o_full[g], 1);
+            sh->keep_o[g] = 0;
+        }
+        sh->abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kSoftmaxWarps) paged_tc_alloc(&sh->tmem_base, QT * kCols);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    pdl_launch_dependents();                                // behind the TMEM allocation
+    pdl_wait();
+
+    PagedStart start;
+    static_assert(sizeof(PagedScratch) <= kSmem<64, 1> - 1024, "the scratch fits the tiles");
+    const bool any = paged_find_start<kThreads<QT>, kKT, kItem, false>(a, *reinterpret_cast<PagedScratch*>(sQ), 1, kItem + 2, 0, start);
+    proxy_fence();                                          // the scratch's writes before the copies that take its place
+    __syncthreads();
+
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait_bounded(bar, parity, cta_abort, a.status); };
+    auto all_wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
+    const uint32_t tmem = __shfl_sync(0xffffffffu, sh->tmem_base, 0);
+    if (tid == 0) a.shared[blockIdx.x].rows = 0;            // thread 0 writes it again where an item begins here and ends elsewhere
+    // K and V tiles of the share as loader and converters take them: K kFirst tiles ahead, then one of each by turns
+    struct Tiles {
+        PagedWalk<kKT, kItem> w;
+        int t;
+        bool have = true;
+        __device__ __forceinline__ void next() {
+            if (++t == w.t1) {
+                have = w.next();
+                t = w.t0;
+            }
+        }
+    };
+
+    if (!any) {
+        // nothing to do for this CTA
+    } else if (warp < kSoftmaxWarps) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+        paged_tc_softmax<T>(a, start, tm_out, sh, sQ, tmem);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if (warp < kLoader) {
+            paged_tc_mma<T>(a, start, sh, sQ, sK, sV, tmem, warp - kSoftmaxWarps);
+        } else if (warp == kLoader) {
+            // ================= loader: codes and scales; Q before its item's first tile or (one Q buffer) where the item in front has ended
+            const int box_shift = min(a.page_shift, 6), box = 1 << box_shift;
+            bool ok = true;
+            Tiles k{PagedWalk<kKT, kItem>(a, start)}, v{PagedWalk<kKT, kItem>(a, start)};
+            k.t = v.t = k.w.t0;
+            PagedPages k_pages, v_pages;
+            uint32_t slot = 0, ph = 1, issued = 0, nq = 0;
+            const uint32_t codes = __shfl_sync(0xffffffffu, smem_u32(sC), 0);
+            auto load = [&](Tiles& x, PagedPages& pages, int base, auto ask) {
+                if (!ok || !x.have) return;
+                const int k0 = x.w.k.tile(x.t) << 6, b = lane & (kBlocks - 1);
+                const int boxes = max(0, (min(kKT, x.w.k.hi - k0) + box - 1) >> box_shift), n_blocks = boxes << box_shift >> 4;
+                const int row = pages.template rows<decltype(ask)::value>(a, x.w.q, x.w.seq, x.w.head, k0, b * kPagedBlock, b < n_blocks, base);
+                if (issued >= static_cast<uint32_t>(ST)) ok = all_wait(&sh->st_empty[slot], ph);
+                if (!ok) return;
+                uint64_t* full = &sh->st_full[slot];
+                if (paged_elect()) mbar_expect_tx(full, static_cast<uint32_t>(boxes) * box * HD);
+                __syncwarp();
+                for (int c = 0; c < boxes; ++c) {
+                    const int r = __shfl_sync(0xffffffffu, row, c << box_shift >> 4);
+                    if (paged_elect()) tma_codes(codes + slot * kC + c * box * HD, &tm_codes, full, r);
+                    __syncwarp();
+                }
+                if (lane < kBlocks) {                        // a page that is none reads as zeros
+                    if (b < n_blocks) {
+                        if (row < a.pool_rows) copy4(smem_u32(&sh->scale[slot][b]), a.scales + row / kPagedBlock);
+                        else sh->scale[slot][b] = 1.f;
+                    }
+                    copies_arrive(full);
+                }
+                __syncwarp();
+                ++issued;
+                if (++slot == static_cast<uint32_t>(ST)) { slot = 0; ph ^= 1u; }
+                x.next();
+            };
+            PagedWalk<kKT, kItem> wq(a, start);
+            bool have_q = true;
+            auto next_q = [&]() {
+                if (!have_q) return;
+                const uint32_t buf = nq % NQ;
+                if (nq >= NQ) ok = ok && all_wait(&sh->item_done[buf], (nq / NQ - 1) & 1u);
+                if (!ok) return;
+                const uint32_t dst = __shfl_sync(0xffffffffu, smem_u32(sQ) + buf * QT * kQBytes<HD>, 0);
+                const int row = wq.q.row0 + wq.rt * QT * a.tile_tokens;
+                if (paged_elect()) {
+                    mbar_expect_tx(&sh->q_full[buf], QT * kAtoms * static_cast<uint32_t>(a.tile_tokens) * a.G * 128);
+#pragma unroll
+                    for (int g = 0; g < QT; ++g)
+#pragma unroll
+                        for (int at = 0; at < kAtoms; ++at)
+                            tma_box_3d(dst + g * kQBytes<HD> + at * kTQ * 128, &tm_q, &sh->q_full[buf], 64 * at, wq.head * a.G, row + g * a.tile_tokens);
+                }
+                __syncwarp();
+                ++nq;
+                have_q = wq.next();
+            };
+            for (int i = 0; i < kFirst; ++i) load(k, k_pages, a.k_row0, std::false_type());
+            if (NQ == 2) next_q();
+            while (ok && v.have) {
+                if (NQ == 1 && v.t == v.w.t0) next_q();
+                // behind the item's third tile: the epilogue in front of it, which frees the buffer, is on its way by then
+                const bool then_q = NQ == 2 && v.t == min(v.w.t0 + 2, v.w.t1 - 1);
+                load(k, k_pages, a.k_row0, std::false_type());
+                load(v, v_pages, a.v_row0, std::true_type());
+                if (then_q) next_q();
+            }
+            if (*cta_abort && lane == 0) {   // copies in flight land before the CTA's shared memory goes away
+                const long long t0 = clock64();
+                auto land = [&](uint64_t* bars, uint32_t n, uint32_t slots) {
+                    for (uint32_t j = n > slots ? n - slots : 0; j < n; ++j)
+                        while (!mbar_try_wait_parity(&bars[j % slots], (j / slots) & 1u) && clock64() - t0 < kWaitLimitCycles / 8) {
+                        }
+                };
+                land(sh->q_full, nq, NQ);
+                land(sh->st_full, issued, ST);
+            }
+        } else if (warp >= kConv) {
+            // ================= converters: each the same keys of every tile =================
+            constexpr int kKeys = kKT / CW, kPieces = HD / 16, kAtOnce = 32 / kPieces, kSteps = kKeys / kAtOnce,
+                          kGroup = kSteps < 4 ? kSteps : 4;    // keys of a warp; of a step; steps in flight
+            const int cw = warp - kConv, piece = lane % kPieces, atom = piece >> 2, first = (piece & 3) * 2 + (atom & 1);   // the two halves of a lane's piece: banks
+            bool ok = true;
+            Tiles k{PagedWalk<kKT, kItem>(a, start)}, v{PagedWalk<kKT, kItem>(a, start)};
+            k.t = v.t = k.w.t0;
+            uint32_t st = 0, st_ph = 0, k_slot = 0, k_n = 0, v_slot = 0, v_n = 0;
+            auto convert = [&](Tiles& x, uint8_t* tiles, uint64_t* full, uint64_t* empty, uint32_t& slot, uint32_t& n, auto is_v) {
+                if (!ok || !x.have) return;
+                const int k0 = x.w.k.tile(x.t) << 6;
+                const bool care = decltype(is_v)::value && !SeenByAll(a, x.w.q, x.w.rt * QT * a.tile_tokens, QT * a.tile_tokens).tile(a, k0);
+                ok = all_wait(&sh->st_full[st], st_ph);
+                if (ok && n >= static_cast<uint32_t>(SL)) ok = all_wait(&empty[slot], (n / SL - 1) & 1u);
+                if (!ok) return;
+                const uint32_t from = smem_u32(sC) + st * kC, to = smem_u32(tiles) + slot * kT + atom * kKT * 128;
+                auto code_at = [&](int key) -> uint32_t {
+                    return HD == 128 ? from + key * 128 + ((piece ^ (key & 7)) << 4) : from + key * 64 + ((piece ^ (key >> 1 & 3)) << 4);
+                };
+                auto key_of = [&](int i) { return cw * kKeys + i * kAtOnce + lane / kPieces; };
+                uint32_t top = 0;
+#pragma unroll 1
+                for (int i0 = 0; i0 < kSteps; i0 += kGroup) {
+                    uint32_t w[kGroup][4];
+#pragma unroll
+                    for (int i = 0; i < kGroup; ++i)
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i][0]), "=r"(w[i][1]), "=r"(w[i][2]), "=r"(w[i][3]) : "r"(code_at(key_of(i0 + i))) : "memory");
+#pragma unroll
+                    for (int i = 0; i < kGroup; ++i) {
+                        const int key = key_of(i0 + i), e = e4m3_exponent(sh->scale[st][key / kPagedBlock]);
+                        const bool hidden = care && (k0 + key >= x.w.k.hi || (k0 + key < x.w.k.lo && k0 + key >= a.sinks));
+                        const uint32_t by = hidden ? 0u : exp2_bf16x2(min(e, 7) + 120);
+                        uint32_t y[8], mine = 0;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            y[2 * j] = mul_bf16x2(widen_codes(__byte_perm(w[i][j], 0, 0x1404), mine), by);
+                            y[2 * j + 1] = mul_bf16x2(widen_codes(__byte_perm(w[i][j], 0, 0x3424), mine), by);
+                        }
+                        if (!hidden) top = max_u16x2(top, mine);
+                        if (__any_sync(0xffffffffu, e > 7)) {     // 2^(e + 120) is no number of bf16
+                            const uint32_t more = exp2_bf16x2(max(e - 7, 0));
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) y[j] = mul_bf16x2(y[j], more);
+                        }
+                        const uint32_t row = to + key * 128;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {             // the half `first` first: eight lanes at a time meet all banks
+                            const int odd = (first ^ h) & 1;
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + (((first ^ h) ^ (key & 7)) << 4)), "r"(odd ? y[4] : y[0]), "r"(odd ? y[5] : y[1]),
+                                         "r"(odd ? y[6] : y[2]), "r"(odd ? y[7] : y[3])
+                                         : "memory");
+                        }
+                    }
+                }
+                const bool nan = __any_sync(0xffffffffu, (top & 0xffffu) == 0x07f0u || top >> 16 == 0x07f0u);
+                if (nan) {                                    // rare
+#pragma unroll 1
+                    for (int i = 0; i < kSteps; ++i) {
+                        const int key = key_of(i);
+                        if (care && (k0 + key >= x.w.k.hi || (k0 + key < x.w.k.lo && k0 + key >= a.sinks))) continue;
+#pragma unroll 1
+                        for (int j = 0; j < 16; ++j) {
+                            uint32_t c;
+                            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(c) : "r"(code_at(key) + j) : "memory");
+                            if ((c & 0x7fu) == 0x7fu)         // where only some rows see it the softmax warps give it to them
+                                asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + key * 128 + ((((piece & 3) * 2 + (j >> 3)) ^ (key & 7)) << 4) + (j & 7) * 2),
+                                             "h"(static_cast<unsigned short>(care ? 0 : 0x7fff))
+                                             : "memory");
+                        }
+                    }
+                }
+                if (care && lane == 0) *const_cast<volatile int*>(&sh->odd[slot][cw]) = nan;
+                proxy_fence();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&sh->st_empty[st]);
+                    mbar_arrive(&full[slot]);
+                }
+                __syncwarp();
+                if (++st == static_cast<uint32_t>(ST)) { st = 0; st_ph ^= 1u; }
+                if (++slot == static_cast<uint32_t>(SL)) slot = 0;
+                ++n;
+                x.next();
+            };
+            auto convert_k = [&]() { convert(k, sK, sh->k_full, sh->k_empty, k_slot, k_n, std::false_type()); };
+            for (int i = 0; i < kFirst; ++i) convert_k();
+            while (ok && v.have) {
+                convert_k();
+                convert(v, sV, sh->v_full, sh->v_empty, v_slot, v_n, std::true_type());
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kSoftmaxWarps) {
+        __syncwarp();
+        tc_fence_after();
+        tmem_free(tmem, QT * kCols);
+    }
+}
+
+template <int HD, int QT>
+cudaError_t launch(const PagedAttnArgs& a, const CUtensorMap& tm_q, const CUtensorMap& tm_out, const CUtensorMap& map, cudaStream_t st) {
+    static std::atomic<unsigned long long> attr_done{0};
+    cudaError_t e = set_smem_limit_once(attr_done, paged_e4m3_attention_tc_kernel<HD, QT>, static_cast<int>(kSmem<HD, QT>));
+    if (e != cudaSuccess) return e;
+    static std::atomic<int> regs{0};
+    if (regs.load(std::memory_order_relaxed) != kLaunchRegs) {   // with fewer the softmax warps would wait for the others' without end
+        cudaFuncAttributes f;
+        e = cudaFuncGetAttributes(&f, paged_e4m3_attention_tc_kernel<HD, QT>);
+        if (e != cudaSuccess) return e;
+        if (f.numRegs != kLaunchRegs) return cudaErrorInvalidConfiguration;
+        regs.store(f.numRegs, std::memory_order_relaxed);
+    }
+    const dim3 grid(a.at_once);
+    e = launch_kernel(paged_e4m3_attention_tc_kernel<HD, QT>, grid, dim3(kThreads<QT>), kSmem<HD, QT>, st, tm_q, map, tm_out, a);
+    if (e != cudaSuccess) return e;
+    return launch_kernel(paged_merge_kernel<HD>, dim3(grid.x, QT * HD / kMergeDims), dim3(kTQ), 0, st, a);
+}
+
+}  // namespace
+
+cudaError_t launch_paged_e4m3_attention_tc(PagedAttnArgs a, const CUtensorMap& map, int hd, int q_tiles, int sms, cudaStream_t st) {
+    CUtensorMap tm_q, tm_out;
+    const cudaError_t e = paged_tc_args(a, hd, q_tiles, sms, &tm_q, &tm_out);
+    if (e != cudaSuccess) return e;
+    if (q_tiles == 1) return hd == 128 ? launch<128, 1>(a, tm_q, tm_out, map, st) : launch<64, 1>(a, tm_q, tm_out, map, st);
+    return hd == 128 ? launch<128, 2>(a, tm_q, tm_out, map, st) : launch<64, 2>(a, tm_q, tm_out, map, st);
+}
+
+}  // namespace odb
