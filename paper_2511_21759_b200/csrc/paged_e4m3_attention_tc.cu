@@ -17,22 +17,23 @@ namespace odb {
 
 namespace {
 
-template <int QT> constexpr int kConvWarps = 2 * QT;
+template <int QT> constexpr int kConvWarps = QT;             // converters of K, and of V
 template <int QT> constexpr int kThreads = 256 * QT;         // 4 QT softmax warps; QT MMA warps, the loader, (two Q tiles: one that idles,) converters
 constexpr int kLaunchRegs = 128, kSoftmaxRegs = 160, kOtherRegs = 96;   // as many warpgroups of the one as of the other
 static_assert(kSoftmaxRegs + kOtherRegs <= 2 * kLaunchRegs, "the split fits what the block was launched with");
 template <int HD, int QT> constexpr int kQBufs = HD == 128 && QT == 1 ? 1 : 2;
-template <int HD, int QT> constexpr int kSlots = HD == 128 ? 2 : (QT == 1 ? 3 : 4);    // K tiles, and V tiles, as operands
-template <int HD, int QT> constexpr int kStaging = HD == 128 ? (QT == 1 ? 2 : 4) : 6;  // tiles of codes
+template <int HD, int QT> constexpr int kKSlots = HD == 128 ? QT : (QT == 1 ? 3 : 4);  // K tiles as operands
+template <int HD, int QT> constexpr int kVSlots = HD == 128 ? 2 : (QT == 1 ? 3 : 4);   // V tiles
+template <int HD, int QT> constexpr int kStaging = HD == 128 ? 2 : 3;                  // tiles of codes, of K and of V
 template <int HD> constexpr uint32_t kCodeBytes = kKT * HD;
 template <int HD, int QT>
-constexpr uint32_t kSmem = kQBufs<HD, QT> * QT * kQBytes<HD> + 2 * kSlots<HD, QT> * kTileBytes<HD> + kStaging<HD, QT> * kCodeBytes<HD> + 1024;
+constexpr uint32_t kSmem = kQBufs<HD, QT> * QT * kQBytes<HD> + (kKSlots<HD, QT> + kVSlots<HD, QT>) * kTileBytes<HD> + 2 * kStaging<HD, QT> * kCodeBytes<HD> + 1024;
 static_assert(2 * (kSmem<128, 1> + 1024) <= 228 * 1024 && 2 * (kSmem<64, 1> + 1024) <= 228 * 1024 && kSmem<128, 2> <= 227 * 1024 && kSmem<64, 2> <= 227 * 1024, "the CTAs share an SM");
 
 struct alignas(8) SharedE4m3 {
     uint64_t q_full[2];                // an item's Q tiles landed in the buffer          (loader -> MMA)
-    uint64_t st_full[6];               // a tile of codes and its scales landed           (loader -> converters)
-    uint64_t st_empty[6];              // the converters have read it                     (converters -> loader)
+    uint64_t st_full[2][3];            // a tile of codes of K / V and its scales landed  (loader -> converters)
+    uint64_t st_empty[2][3];           // the converters have read it                     (converters -> loader)
     uint64_t k_full[4], v_full[4];     // K or V tile written, V looked at                (converters -> MMA; V -> softmax)
     uint64_t k_empty[4], v_empty[4];   // the MMAs have read the slot                     (MMA -> converters, QT arrivals)
     uint64_t s_full[2][3];             // S of Q tile g into buffer i has completed       (MMA -> softmax)
@@ -42,14 +43,14 @@ struct alignas(8) SharedE4m3 {
     uint64_t item_done[2];             // the Q buffer may be overwritten                 (softmax -> loader, 4 QT arrivals)
     uint32_t tmem_base;
     int abort, keep_o[2];
-    float scale[6][kKT / kPagedBlock]; // of a staging tile's blocks
-    int odd[4][4];                     // V in the slot has NaN where only some rows see it, by converter
+    float scale[2][3][kKT / kPagedBlock];   // of a staging tile's blocks
+    int odd[4][2];                     // V in the slot has NaN where only some rows see it, by converter
 };
 static_assert(sizeof(SharedE4m3) <= 1024, "the barriers end inside the allocation");
 
 template <int HD_, int QT_>
 struct TcE4m3 {
-    static constexpr int HD = HD_, QT = QT_, NQ = kQBufs<HD, QT>, KS = kSlots<HD, QT>, VS = kSlots<HD, QT>;
+    static constexpr int HD = HD_, QT = QT_, NQ = kQBufs<HD, QT>, KS = kKSlots<HD, QT>, VS = kVSlots<HD, QT>;
     using Shared = SharedE4m3;
     // V of the slot has been looked at; it has NaN where only some rows see it; whether this is one (0: it is not)
     static __device__ __forceinline__ uint64_t* v_seen(Shared* sh, uint32_t slot) { return &sh->v_full[slot]; }
@@ -84,15 +85,16 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                                    const __grid_constant__ CUtensorMap tm_out, const PagedAttnArgs a) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     using T = TcE4m3<HD, QT>;
-    constexpr int NQ = T::NQ, SL = kSlots<HD, QT>, ST = kStaging<HD, QT>, CW = kConvWarps<QT>, kFirst = kBufs<HD> - 1, kAtoms = HD / 64;
+    constexpr int NQ = T::NQ, KS = T::KS, VS = T::VS, ST = kStaging<HD, QT>, CW = kConvWarps<QT>, kFirst = kBufs<HD> - 1, kAtoms = HD / 64;
     constexpr uint32_t kT = kTileBytes<HD>, kC = kCodeBytes<HD>;
-    constexpr int kSoftmaxWarps = 4 * QT, kLoader = kSoftmaxWarps + QT, kConv = kThreads<QT> / 32 - CW, kBlocks = kKT / kPagedBlock;
+    constexpr int kSoftmaxWarps = 4 * QT, kLoader = kSoftmaxWarps + QT, kConv = kThreads<QT> / 32 - 2 * CW, kBlocks = kKT / kPagedBlock;
     uint8_t* sQ = smem_raw;                                  // [buffer][Q tile]
     uint8_t* sK = sQ + NQ * QT * kQBytes<HD>;
-    uint8_t* sV = sK + SL * kT;
-    uint8_t* sC = sV + SL * kT;
-    SharedE4m3* sh = reinterpret_cast<SharedE4m3*>(sC + ST * kC);
-    static_assert(SL <= 4 && ST <= 6 && kBufs<HD> * kKT + HD <= static_cast<int>(kCols) && 4 * kPatch <= kQBytes<HD>, "rings, TMEM columns, patches");
+    uint8_t* sV = sK + KS * kT;
+    uint8_t* sC = sV + VS * kT;                              // [K, V][tile]
+    SharedE4m3* sh = reinterpret_cast<SharedE4m3*>(sC + 2 * ST * kC);
+    static_assert(VS >= kBufs<HD>, "the tile before in a slot of V has been multiplied when the softmax asks for this one");
+    static_assert(KS <= 4 && VS <= 4 && ST <= 3 && kBufs<HD> * kKT + HD <= static_cast<int>(kCols) && 4 * kPatch <= kQBytes<HD>, "rings, TMEM columns, patches");
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     volatile int* cta_abort = &sh->abort;
 
@@ -108,14 +110,16 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
             mbar_init(&sh->q_full[i], 1);
             mbar_init(&sh->item_done[i], kSoftmaxWarps);
         }
-        for (int i = 0; i < ST; ++i) {
-            mbar_init(&sh->st_full[i], 1 + kBlocks);
-            mbar_init(&sh->st_empty[i], CW);
+        for (int i = 0; i < 2 * ST; ++i) {
+            mbar_init(&sh->st_full[i & 1][i >> 1], 1 + kBlocks);
+            mbar_init(&sh->st_empty[i & 1][i >> 1], CW);
         }
-        for (int i = 0; i < SL; ++i) {
+        for (int i = 0; i < KS; ++i) {
             mbar_init(&sh->k_full[i], CW);
-            mbar_init(&sh->v_full[i], CW);
             mbar_init(&sh->k_empty[i], QT);
+        }
+        for (int i = 0; i < VS; ++i) {
+            mbar_init(&sh->v_full[i], CW);
             mbar_init(&sh->v_empty[i], QT);
         }
         for (int g = 0; g < QT; ++g) {
@@ -147,12 +151,16 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
     auto all_wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
     const uint32_t tmem = __shfl_sync(0xffffffffu, sh->tmem_base, 0);
     if (tid == 0) a.shared[blockIdx.x].rows = 0;            // thread 0 writes it again where an item begins here and ends elsewhere
-    // K and V tiles of the share as loader and converters take them: K kFirst tiles ahead, then one of each by turns
+    // K or V tiles of the share, and the staging ring that they go through
     struct Tiles {
         PagedWalk<kKT, kItem> w;
         int t;
+        uint32_t slot = 0, ph = 0, n = 0;
         bool have = true;
+        __device__ __forceinline__ Tiles(const PagedAttnArgs& args, const PagedStart& st) : w(args, st), t(w.t0) {}
         __device__ __forceinline__ void next() {
+            ++n;
+            if (++slot == static_cast<uint32_t>(ST)) { slot = 0; ph ^= 1u; }
             if (++t == w.t1) {
                 have = w.next();
                 t = w.t0;
@@ -173,36 +181,34 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
             // ================= loader: codes and scales; Q before its item's first tile or (one Q buffer) where the item in front has ended
             const int box_shift = min(a.page_shift, 6), box = 1 << box_shift;
             bool ok = true;
-            Tiles k{PagedWalk<kKT, kItem>(a, start)}, v{PagedWalk<kKT, kItem>(a, start)};
-            k.t = v.t = k.w.t0;
+            Tiles k(a, start), v(a, start);
             PagedPages k_pages, v_pages;
-            uint32_t slot = 0, ph = 1, issued = 0, nq = 0;
+            uint32_t nq = 0;
             const uint32_t codes = __shfl_sync(0xffffffffu, smem_u32(sC), 0);
-            auto load = [&](Tiles& x, PagedPages& pages, int base, auto ask) {
+            auto load = [&](Tiles& x, PagedPages& pages, auto is_v) {
+                constexpr int V = decltype(is_v)::value;
                 if (!ok || !x.have) return;
                 const int k0 = x.w.k.tile(x.t) << 6, b = lane & (kBlocks - 1);
                 const int boxes = max(0, (min(kKT, x.w.k.hi - k0) + box - 1) >> box_shift), n_blocks = boxes << box_shift >> 4;
-                const int row = pages.template rows<decltype(ask)::value>(a, x.w.q, x.w.seq, x.w.head, k0, b * kPagedBlock, b < n_blocks, base);
-                if (issued >= static_cast<uint32_t>(ST)) ok = all_wait(&sh->st_empty[slot], ph);
+                const int row = pages.rows<V != 0>(a, x.w.q, x.w.seq, x.w.head, k0, b * kPagedBlock, b < n_blocks, V ? a.v_row0 : a.k_row0);
+                if (x.n >= static_cast<uint32_t>(ST)) ok = all_wait(&sh->st_empty[V][x.slot], x.ph ^ 1u);
                 if (!ok) return;
-                uint64_t* full = &sh->st_full[slot];
+                uint64_t* full = &sh->st_full[V][x.slot];
                 if (paged_elect()) mbar_expect_tx(full, static_cast<uint32_t>(boxes) * box * HD);
                 __syncwarp();
                 for (int c = 0; c < boxes; ++c) {
                     const int r = __shfl_sync(0xffffffffu, row, c << box_shift >> 4);
-                    if (paged_elect()) tma_codes(codes + slot * kC + c * box * HD, &tm_codes, full, r);
+                    if (paged_elect()) tma_codes(codes + (V * ST + x.slot) * kC + c * box * HD, &tm_codes, full, r);
                     __syncwarp();
                 }
                 if (lane < kBlocks) {                        // a page that is none reads as zeros
                     if (b < n_blocks) {
-                        if (row < a.pool_rows) copy4(smem_u32(&sh->scale[slot][b]), a.scales + row / kPagedBlock);
-                        else sh->scale[slot][b] = 1.f;
+                        if (row < a.pool_rows) copy4(smem_u32(&sh->scale[V][x.slot][b]), a.scales + row / kPagedBlock);
+                        else sh->scale[V][x.slot][b] = 1.f;
                     }
                     copies_arrive(full);
                 }
                 __syncwarp();
-                ++issued;
-                if (++slot == static_cast<uint32_t>(ST)) { slot = 0; ph ^= 1u; }
                 x.next();
             };
             PagedWalk<kKT, kItem> wq(a, start);
@@ -226,14 +232,14 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                 ++nq;
                 have_q = wq.next();
             };
-            for (int i = 0; i < kFirst; ++i) load(k, k_pages, a.k_row0, std::false_type());
+            for (int i = 0; i < kFirst; ++i) load(k, k_pages, std::false_type());
             if (NQ == 2) next_q();
             while (ok && v.have) {
                 if (NQ == 1 && v.t == v.w.t0) next_q();
                 // behind the item's third tile: the epilogue in front of it, which frees the buffer, is on its way by then
                 const bool then_q = NQ == 2 && v.t == min(v.w.t0 + 2, v.w.t1 - 1);
-                load(k, k_pages, a.k_row0, std::false_type());
-                load(v, v_pages, a.v_row0, std::true_type());
+                load(k, k_pages, std::false_type());
+                load(v, v_pages, std::true_type());
                 if (then_q) next_q();
             }
             if (*cta_abort && lane == 0) {   // copies in flight land before the CTA's shared memory goes away
@@ -244,99 +250,97 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                         }
                 };
                 land(sh->q_full, nq, NQ);
-                land(sh->st_full, issued, ST);
+                land(sh->st_full[0], k.n, ST);
+                land(sh->st_full[1], v.n, ST);
             }
         } else if (warp >= kConv) {
-            // ================= converters: each the same keys of every tile =================
-            constexpr int kKeys = kKT / CW, kPieces = HD / 16, kAtOnce = 32 / kPieces, kSteps = kKeys / kAtOnce,
-                          kGroup = kSteps < 4 ? kSteps : 4;    // keys of a warp; of a step; steps in flight
-            const int cw = warp - kConv, piece = lane % kPieces, atom = piece >> 2, first = (piece & 3) * 2 + (atom & 1);   // the two halves of a lane's piece: banks
-            bool ok = true;
-            Tiles k{PagedWalk<kKT, kItem>(a, start)}, v{PagedWalk<kKT, kItem>(a, start)};
-            k.t = v.t = k.w.t0;
-            uint32_t st = 0, st_ph = 0, k_slot = 0, k_n = 0, v_slot = 0, v_n = 0;
-            auto convert = [&](Tiles& x, uint8_t* tiles, uint64_t* full, uint64_t* empty, uint32_t& slot, uint32_t& n, auto is_v) {
-                if (!ok || !x.have) return;
-                const int k0 = x.w.k.tile(x.t) << 6;
-                const bool care = decltype(is_v)::value && !SeenByAll(a, x.w.q, x.w.rt * QT * a.tile_tokens, QT * a.tile_tokens).tile(a, k0);
-                ok = all_wait(&sh->st_full[st], st_ph);
-                if (ok && n >= static_cast<uint32_t>(SL)) ok = all_wait(&empty[slot], (n / SL - 1) & 1u);
-                if (!ok) return;
-                const uint32_t from = smem_u32(sC) + st * kC, to = smem_u32(tiles) + slot * kT + atom * kKT * 128;
-                auto code_at = [&](int key) -> uint32_t {
-                    return HD == 128 ? from + key * 128 + ((piece ^ (key & 7)) << 4) : from + key * 64 + ((piece ^ (key >> 1 & 3)) << 4);
-                };
-                auto key_of = [&](int i) { return cw * kKeys + i * kAtOnce + lane / kPieces; };
-                uint32_t top = 0;
+            // ================= converters of K, then of V: each the same keys of every tile =================
+            constexpr int kKeys = kKT / CW, kPieces = HD / 16, kAtOnce = 32 / kPieces, kSteps = kPagedBlock / kAtOnce;   // keys of a warp, of a step; steps of a block
+            const int cw = (warp - kConv) % CW, piece = lane % kPieces, atom = piece >> 2;
+            const int first = (piece & 3) * 2 + (atom & 1);  // of a lane's two halves the one that it stores first: eight lanes at a time meet all banks
+            auto convert = [&](uint8_t* tiles, uint64_t* full, uint64_t* empty, auto is_v) {
+                constexpr int V = decltype(is_v)::value, SL = V ? VS : KS;
+                Tiles x(a, start);
+                uint32_t slot = 0, empty_ph = 1;
+                while (x.have) {
+                    const int k0 = x.w.k.tile(x.t) << 6;
+                    const bool care = V && !SeenByAll(a, x.w.q, x.w.rt * QT * a.tile_tokens, QT * a.tile_tokens).tile(a, k0);
+                    bool ok = all_wait(&sh->st_full[V][x.slot], x.ph);
+                    if (ok && x.n >= static_cast<uint32_t>(SL)) ok = all_wait(&empty[slot], empty_ph);
+                    if (!ok) break;
+                    const uint32_t from = smem_u32(sC) + (V * ST + x.slot) * kC, to = smem_u32(tiles) + slot * kT + atom * kKT * 128;
+                    auto code_at = [&](int key) -> uint32_t {
+                        return HD == 128 ? from + key * 128 + ((piece ^ (key & 7)) << 4) : from + key * 64 + ((piece ^ (key >> 1 & 3)) << 4);
+                    };
+                    auto hidden = [&](int key) { return care && (k0 + key >= x.w.k.hi || (k0 + key < x.w.k.lo && k0 + key >= a.sinks)); };
+                    uint32_t top = 0;
 #pragma unroll 1
-                for (int i0 = 0; i0 < kSteps; i0 += kGroup) {
-                    uint32_t w[kGroup][4];
+                    for (int key0 = cw * kKeys; key0 < (cw + 1) * kKeys; key0 += kPagedBlock) {      // a block, one scale
+                        const int e = e4m3_exponent(sh->scale[V][x.slot][key0 / kPagedBlock]), key1 = key0 + lane / kPieces;
+                        const uint32_t by = exp2_bf16x2(min(e, 7) + 120);
+                        uint32_t w[kSteps][4], y[kSteps][8];
 #pragma unroll
-                    for (int i = 0; i < kGroup; ++i)
-                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i][0]), "=r"(w[i][1]), "=r"(w[i][2]), "=r"(w[i][3]) : "r"(code_at(key_of(i0 + i))) : "memory");
+                        for (int i = 0; i < kSteps; ++i)
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                         : "=r"(w[i][0]), "=r"(w[i][1]), "=r"(w[i][2]), "=r"(w[i][3]) : "r"(code_at(key1 + i * kAtOnce)) : "memory");
 #pragma unroll
-                    for (int i = 0; i < kGroup; ++i) {
-                        const int key = key_of(i0 + i), e = e4m3_exponent(sh->scale[st][key / kPagedBlock]);
-                        const bool hidden = care && (k0 + key >= x.w.k.hi || (k0 + key < x.w.k.lo && k0 + key >= a.sinks));
-                        const uint32_t by = hidden ? 0u : exp2_bf16x2(min(e, 7) + 120);
-                        uint32_t y[8], mine = 0;
+                        for (int i = 0; i < kSteps; ++i) {
+                            if (care && hidden(key1 + i * kAtOnce)) w[i][0] = w[i][1] = w[i][2] = w[i][3] = 0u;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            y[2 * j] = mul_bf16x2(widen_codes(__byte_perm(w[i][j], 0, 0x1404), mine), by);
-                            y[2 * j + 1] = mul_bf16x2(widen_codes(__byte_perm(w[i][j], 0, 0x3424), mine), by);
+                            for (int j = 0; j < 4; ++j) {
+                                y[i][2 * j] = mul_bf16x2(widen_codes(__byte_perm(w[i][j], 0, 0x1404), top), by);
+                                y[i][2 * j + 1] = mul_bf16x2(widen_codes(__byte_perm(w[i][j], 0, 0x3424), top), by);
+                            }
                         }
-                        if (!hidden) top = max_u16x2(top, mine);
-                        if (__any_sync(0xffffffffu, e > 7)) {     // 2^(e + 120) is no number of bf16
-                            const uint32_t more = exp2_bf16x2(max(e - 7, 0));
+                        if (e > 7) {                          // 2^(e + 120) is no number of bf16
+                            const uint32_t more = exp2_bf16x2(e - 7);
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) y[j] = mul_bf16x2(y[j], more);
-                        }
-                        const uint32_t row = to + key * 128;
+                            for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {             // the half `first` first: eight lanes at a time meet all banks
-                            const int odd = (first ^ h) & 1;
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + (((first ^ h) ^ (key & 7)) << 4)), "r"(odd ? y[4] : y[0]), "r"(odd ? y[5] : y[1]),
-                                         "r"(odd ? y[6] : y[2]), "r"(odd ? y[7] : y[3])
-                                         : "memory");
+                                for (int j = 0; j < 8; ++j) y[i][j] = mul_bf16x2(y[i][j], more);
                         }
-                    }
-                }
-                const bool nan = __any_sync(0xffffffffu, (top & 0xffffu) == 0x07f0u || top >> 16 == 0x07f0u);
-                if (nan) {                                    // rare
-#pragma unroll 1
-                    for (int i = 0; i < kSteps; ++i) {
-                        const int key = key_of(i);
-                        if (care && (k0 + key >= x.w.k.hi || (k0 + key < x.w.k.lo && k0 + key >= a.sinks))) continue;
-#pragma unroll 1
-                        for (int j = 0; j < 16; ++j) {
-                            uint32_t c;
-                            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(c) : "r"(code_at(key) + j) : "memory");
-                            if ((c & 0x7fu) == 0x7fu)         // where only some rows see it the softmax warps give it to them
-                                asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + key * 128 + ((((piece & 3) * 2 + (j >> 3)) ^ (key & 7)) << 4) + (j & 7) * 2),
-                                             "h"(static_cast<unsigned short>(care ? 0 : 0x7fff))
+#pragma unroll
+                        for (int i = 0; i < kSteps; ++i) {
+                            const int key = key1 + i * kAtOnce;
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const int odd = (first ^ h) & 1;
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + key * 128 + (((first ^ h) ^ (key & 7)) << 4)),
+                                             "r"(odd ? y[i][4] : y[i][0]), "r"(odd ? y[i][5] : y[i][1]), "r"(odd ? y[i][6] : y[i][2]), "r"(odd ? y[i][7] : y[i][3])
                                              : "memory");
+                            }
                         }
                     }
+                    const bool nan = __any_sync(0xffffffffu, (top & 0xffffu) == 0x07f0u || top >> 16 == 0x07f0u);
+                    if (nan) {                                // rare
+#pragma unroll 1
+                        for (int key = cw * kKeys + lane / kPieces; key < (cw + 1) * kKeys; key += kAtOnce) {
+                            if (hidden(key)) continue;
+#pragma unroll 1
+                            for (int j = 0; j < 16; ++j) {
+                                uint32_t c;
+                                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(c) : "r"(code_at(key) + j) : "memory");
+                                if ((c & 0x7fu) == 0x7fu)     // where only some rows see it the softmax warps give it to them
+                                    asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + key * 128 + ((((piece & 3) * 2 + (j >> 3)) ^ (key & 7)) << 4) + (j & 7) * 2),
+                                                 "h"(static_cast<unsigned short>(care ? 0 : 0x7fff))
+                                                 : "memory");
+                            }
+                        }
+                    }
+                    if (care && lane == 0) *const_cast<volatile int*>(&sh->odd[slot][cw]) = nan;
+                    proxy_fence();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(&full[slot]);
+                        mbar_arrive(&sh->st_empty[V][x.slot]);
+                    }
+                    __syncwarp();
+                    if (++slot == static_cast<uint32_t>(SL)) { slot = 0; empty_ph ^= 1u; }
+                    x.next();
                 }
-                if (care && lane == 0) *const_cast<volatile int*>(&sh->odd[slot][cw]) = nan;
-                proxy_fence();
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(&sh->st_empty[st]);
-                    mbar_arrive(&full[slot]);
-                }
-                __syncwarp();
-                if (++st == static_cast<uint32_t>(ST)) { st = 0; st_ph ^= 1u; }
-                if (++slot == static_cast<uint32_t>(SL)) slot = 0;
-                ++n;
-                x.next();
             };
-            auto convert_k = [&]() { convert(k, sK, sh->k_full, sh->k_empty, k_slot, k_n, std::false_type()); };
-            for (int i = 0; i < kFirst; ++i) convert_k();
-            while (ok && v.have) {
-                convert_k();
-                convert(v, sV, sh->v_full, sh->v_empty, v_slot, v_n, std::true_type());
-            }
+            if (warp < kConv + CW) convert(sK, sh->k_full, sh->k_empty, std::false_type());
+            else convert(sV, sh->v_full, sh->v_empty, std::true_type());
         }
     }
     tc_fence_before();
