@@ -2,6 +2,8 @@
 // attention's work, which the kernels of few and of many rows have in common.
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include "attention_tc.cuh"
 
 namespace odb {
@@ -512,6 +514,11 @@ __device__ __forceinline__ float paged_weight(float m, float M) { return m == -I
 __device__ __forceinline__ float paged_lse(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f; }
 __device__ __forceinline__ uint32_t paged_bf16x2(float a, float b) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+__device__ __forceinline__ uint32_t paged_f16x2(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 

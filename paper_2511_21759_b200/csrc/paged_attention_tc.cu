@@ -61,7 +61,9 @@ static_assert(sizeof(Shared) <= 1024, "the barriers end inside the allocation");
 template <int HD_, int QT_>
 struct Tc {
     static constexpr int HD = HD_, QT = QT_, NQ = kQBufs<HD, QT>, KS = kKSlots<HD, QT>, VS = kVSlots<HD, QT>;
+    static constexpr bool kCodes = false;
     using Shared = odb::Shared;
+    static __device__ __forceinline__ uint64_t* q_ready(Shared* sh, int) { return sh->q_full; }
     // V of the slot has been looked at; it has values that are not finite where only some rows see them; one of them (0: finite)
     static __device__ __forceinline__ uint64_t* v_seen(Shared* sh, uint32_t slot) { return &sh->v_seen[slot]; }
     static __device__ __forceinline__ bool odd(Shared* sh, uint32_t slot) { return *const_cast<volatile int*>(&sh->odd[slot]) != 0; }

@@ -165,7 +165,7 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16
 }
 
 // The MMAs of Q tile g: the whole warp walks and waits, one lane issues.
-// T: HD, QT; NQ Q buffers, KS and VS places of the K and V rings, and the barriers' struct.
+// T: HD, QT; NQ Q buffers, KS and VS places of the K and V rings, and the barriers' struct; kCodes: the operands are f16 (paged_e4m3_attention_tc.cu).
 template <class T>
 __device__ __forceinline__ void paged_tc_mma(const PagedAttnArgs& a, const PagedStart& start, typename T::Shared* sh, const uint8_t* sQ, const uint8_t* sK,
                                              const uint8_t* sV, uint32_t tmem, int g) {
@@ -176,8 +176,10 @@ __device__ __forceinline__ void paged_tc_mma(const PagedAttnArgs& a, const Paged
     // S of tile i + kFirst, P V of tile i by turns; with two Q buffers into the next item, so that its first scores are ready when
     // the softmax warps have written the one in front of it.  (P of an item's first tile says that O has been read.)
     PagedWalk<kKT, kItem> ws(a, start), wv(a, start);
-    const uint32_t idesc_s = instr_desc(kTQ, kKT, 0) | (a.negate ? 1u << 13 : 0u);   // bit 13: the product's A is taken with its sign turned
-    constexpr uint32_t idesc_o = instr_desc(kTQ, HD, 1);
+    constexpr int kItems = T::kCodes ? 1 : NQ;               // kCodes: the next item's Q becomes f16 when this one has been written
+    constexpr uint32_t kTypes = T::kCodes ? ~((7u << 7) | (7u << 10)) : ~0u;               // f16: both types zero
+    const uint32_t idesc_s = (instr_desc(kTQ, kKT, 0) & kTypes) | (a.negate ? 1u << 13 : 0u);   // bit 13: the product's A is taken with its sign turned
+    constexpr uint32_t idesc_o = instr_desc(kTQ, HD, 1) & kTypes;
     const uint32_t cols = tmem + g * kCols;
     const uint32_t q_lo = static_cast<uint32_t>(desc_k_major(smem_u32(sQ) + g * kQBytes<HD>)), k_lo = static_cast<uint32_t>(desc_k_major(smem_u32(sK))),
                    v_lo = static_cast<uint32_t>(desc_mn_major(smem_u32(sV), kKT * 128));
@@ -197,7 +199,7 @@ __device__ __forceinline__ void paged_tc_mma(const PagedAttnArgs& a, const Paged
     auto issue_s = [&](bool first_pv) {
         const uint32_t q = q_lo + q_buf * (QT * kQBytes<HD> >> 4), k = k_lo + k_slot * (kT >> 4), d = cols + s_buf * kKT;
         const uint32_t full = bar_of(sh->s_full[g], s_buf), empty = bar_of(sh->k_empty, k_slot);
-        if (ts == ws.t0) all_wait(sh->q_full, q_buf, q_ph);
+        if (ts == ws.t0) all_wait(T::q_ready(sh, g), q_buf, q_ph);
         if (ok) all_wait(sh->k_full, k_slot, k_ph);
         // the last P V has been done, and with it the one that read P in this S's place
         if (ok && !first_pv) all_wait(sh->pv_done[g], pv_bar, pv_ph);
@@ -227,7 +229,7 @@ __device__ __forceinline__ void paged_tc_mma(const PagedAttnArgs& a, const Paged
     do {
         const int n = wv.t1 - wv.t0;
         for (int t = 0; t < n && ok; ++t) {
-            while (ok && have_s && s_ahead <= kFirst && i_ahead < NQ) issue_s(first_pv);
+            while (ok && have_s && s_ahead <= kFirst && i_ahead < kItems) issue_s(first_pv);
             const uint32_t v = v_lo + v_slot * (kT >> 4), o = paged_tc_o<HD>(tmem, g), pa = cols + p_buf * kKT;
             pv_bar ^= 1u;
             if (pv_bar == 0) pv_ph ^= 1u;
@@ -267,7 +269,7 @@ __device__ __forceinline__ void paged_tc_softmax(const PagedAttnArgs& a, const P
     const uint32_t s_base = tmem + g * kCols + lane_base, o_base = paged_tc_o<HD>(tmem, g) + lane_base;
     const int rows_g = a.tile_tokens * a.G;                  // packed rows of a Q tile
     constexpr float kSlack = 8.0f;
-    const uint64_t scale2 = pack2f(a.scale_log2, a.scale_log2);
+    float scale = a.scale_log2;                              // of the row's scores
     bool ok = true;
     uint32_t item = 0, done = 0;                             // key tiles of the items before
     bool storing = false;                                    // the last item's output is on its way from the Q tile's place
@@ -288,7 +290,8 @@ __device__ __forceinline__ void paged_tc_softmax(const PagedAttnArgs& a, const P
         const SeenByAll by_tile(a, w.q, tok0, a.tile_tokens), by_item(a, w.q, w.rt * QT * a.tile_tokens, QT * a.tile_tokens);
         const int left = min(rows_g, (w.q.n - tok0) * a.G);          // rows of the Q tile (may be negative); others hold anything
         const bool mine = r < left;
-        float M_row = -INFINITY, l_row = 0.f;
+        if constexpr (T::kCodes) scale = a.scale_log2 * T::template own_q<kTQ>(sh, sQ, item, g, r, ok, wait);
+        float M_row = -INFINITY, l_row = 0.f, G_row = 0.f;           // the row's shift, M (kCodes: M + G), and its sum
         uint32_t sv[64];                                             // the row's scores of the tile at hand
         auto ask = [&](int t) {                                      // for those of tile t, once they are there
             const uint32_t gt = done + t, b = gt % kB;
@@ -311,32 +314,72 @@ __device__ __forceinline__ void paged_tc_softmax(const PagedAttnArgs& a, const P
                     if (!((mask >> j) & 1ull)) sv[j] = 0xff800000u;
             }
             float mx[4];                                             // largest visible score of the tile, in four chains
+            float mul[4], up[4], weight[4];                          // kCodes: of the tile's blocks: K's scale and the row's, log2 of V's, and 1 / V's
+            bool wide = false;                                       // V's scales lie far from 1: see the sum
+            if constexpr (T::kCodes) {
+                wide = T::scales(sh, gt, mul, up, weight);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) mul[c] = fminf(fmaxf(mul[c] * scale, 0x1p-126f), 0x1.fffffep127f);   // masked scores, and zeros, stay what they are
+            }
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 mx[c] = __uint_as_float(sv[16 * c]);
 #pragma unroll
                 for (int j = 1; j < 15; j += 2) mx[c] = max3(mx[c], __uint_as_float(sv[16 * c + j]), __uint_as_float(sv[16 * c + j + 1]));
             }
-            float m0 = fmaxf(max3(mx[0], mx[1], __uint_as_float(sv[15])), max3(mx[2], mx[3], __uint_as_float(sv[31])));
-            m0 = max3(m0, __uint_as_float(sv[47]), __uint_as_float(sv[63]));
-            const float mt_log2 = mine && mask ? m0 * a.scale_log2 : -INFINITY;   // rows that are none turn nothing for the warp's others
+            // Whether the shift has to move, for a tile that exceeds it by more than kSlack or holds the first visible key.
             // The exponentials take a score's exact product with the scale, the shift comes from the rounded one: from 2^22 on
-            // they lie up to 0.25 and more apart, and the scores are rounded first.
-            const bool far = fabsf(mt_log2) >= 0x1p22f && mt_log2 != -INFINITY;
-            uint64_t mult2 = scale2;
+            // they lie up to 0.25 and more apart, and the scores are rounded first (in products of their own, here and below).
+            bool far, move;
+            float M_new;
+            if constexpr (T::kCodes) {
+                float most = -INFINITY, exceeds = -INFINITY;
+                const float M = M_row == -INFINITY ? 0.f : M_row;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    mx[c] = __fmul_rn(fmaxf(mx[c], __uint_as_float(sv[16 * c + 15])), mul[c]);
+                    most = fmaxf(most, mx[c]);
+                    exceeds = fmaxf(exceeds, mx[c] - M + up[c]);
+                }
+                const bool seen = mine && mask && most != -INFINITY;
+                far = seen && fabsf(most) >= 0x1p22f;
+                move = seen && (M_row == -INFINITY || exceeds > G_row + kSlack || most > M_row + 60.f);
+                M_new = fmaxf(M_row, ceilf(most));
+            } else {
+                float m0 = fmaxf(max3(mx[0], mx[1], __uint_as_float(sv[15])), max3(mx[2], mx[3], __uint_as_float(sv[31])));
+                m0 = max3(m0, __uint_as_float(sv[47]), __uint_as_float(sv[63]));
+                const float mt_log2 = mine && mask ? m0 * scale : -INFINITY;   // rows that are none turn nothing for the warp's others
+                far = fabsf(mt_log2) >= 0x1p22f && mt_log2 != -INFINITY;
+                move = mt_log2 > M_row + kSlack;                     // also the first visible key (M_row = -inf)
+                M_new = ceilf(mt_log2);
+            }
+            uint64_t mult2[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) mult2[c] = T::kCodes ? pack2f(mul[c], mul[c]) : pack2f(scale, scale);
             float factor = 1.0f;                                     // what O and the row sum so far are multiplied by
-            bool rescale = false;
-            if (__any_sync(0xffffffffu, mt_log2 > M_row + kSlack || far)) {
-                if (mt_log2 > M_row + kSlack) {                      // also the first visible key (M_row = -inf)
-                    const float M_new = ceilf(mt_log2);
-                    if (M_row != -INFINITY) factor = exp2f(M_row - M_new);   // an exact power of two
+            bool rescale = false, rounded = false;                   // rounded: the scores stand as x, kCodes: as x - M
+            if (__any_sync(0xffffffffu, move || far)) {
+                if (move) {
+                    float G_new = 0.f;
+                    if constexpr (T::kCodes) {
+                        G_new = mx[0] - M_new + up[0];
+#pragma unroll
+                        for (int c = 1; c < 4; ++c) G_new = fmaxf(G_new, mx[c] - M_new + up[c]);
+                        G_new = ceilf(G_new);
+                        if (M_row != -INFINITY) G_new = fmaxf(G_new, M_row - M_new + G_row);   // M + G never falls
+                    }
+                    if (M_row != -INFINITY) factor = exp2f(M_row - M_new + (G_row - G_new));   // an exact power of two
                     M_row = M_new;
+                    G_row = G_new;
                 }
                 rescale = __any_sync(0xffffffffu, factor != 1.0f);
-                if (__any_sync(0xffffffffu, far)) {
+                rounded = __any_sync(0xffffffffu, far);
+                if (rounded) {
 #pragma unroll
-                    for (int j = 0; j < 64; ++j) sv[j] = __float_as_uint(__uint_as_float(sv[j]) * a.scale_log2);
-                    mult2 = pack2f(1.0f, 1.0f);
+                    for (int j = 0; j < 64; ++j)
+                        sv[j] = __float_as_uint(T::kCodes ? __fmul_rn(__uint_as_float(sv[j]), mul[j / 16]) - (M_row == -INFINITY ? 0.f : M_row) : __uint_as_float(sv[j]) * scale);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) mult2[c] = pack2f(1.0f, 1.0f);
                 }
                 if (rescale && t > 0) {                              // warp-uniform; rows that keep their shift multiply by 1
                     // P V(t - 1) has been added to O.  The parity is not ambiguous: S(t) was issued behind P V(t - kB), so P V(t - 3),
@@ -355,26 +398,47 @@ __device__ __forceinline__ void paged_tc_softmax(const PagedAttnArgs& a, const P
                 }
             }
             const float m_log2 = M_row == -INFINITY ? 0.f : M_row;   // a row that has seen no key: every P is 0
-            const uint64_t shift2 = pack2f(-m_log2, -m_log2);
+            uint64_t shift2[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const float shift = T::kCodes ? up[c] - G_row - (rounded ? 0.f : m_log2) : -m_log2;
+                shift2[c] = pack2f(shift, shift);
+            }
             uint64_t sum[4] = {0ull, 0ull, 0ull, 0ull};
             // The two softmax warps of a scheduler take turns at the exponentials: left alone they fall into step, share the
             // special-function unit for twice as long and leave it idle together for the rest of the tile.
             if (QT == 2) turn_begin(g, gw);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                uint32_t pb[16];                                     // P of 32 keys as bf16 pairs
+                uint32_t pb[16];                                     // P of 32 keys as pairs
 #pragma unroll
                 for (int u = 0; u < 16; ++u) {
-                    const float2 x = unpack2f(fma2(pack2u(sv[32 * half + 2 * u], sv[32 * half + 2 * u + 1]), mult2, shift2));
+                    const int c = 2 * half + u / 8, chain = T::kCodes ? c : u & 3;
+                    const float2 x = unpack2f(fma2(pack2u(sv[32 * half + 2 * u], sv[32 * half + 2 * u + 1]), mult2[c], shift2[c]));
                     const float p0 = ex2_approx(x.x), p1 = ex2_approx(x.y);
-                    sum[u & 3] = add2(sum[u & 3], pack2f(p0, p1));
-                    pb[u] = paged_bf16x2(p0, p1);
+                    sum[chain] = add2(sum[chain], pack2f(p0, p1));
+                    pb[u] = T::kCodes ? paged_f16x2(p0, p1) : paged_bf16x2(p0, p1);
                 }
                 tmem_st16(ts + 16 * half, pb);
             }
             if (QT == 2) turn_end(g, gw);
-            const float2 s0 = unpack2f(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
-            l_row += s0.x + s0.y;
+            if constexpr (T::kCodes) {
+                if (wide) {                                          // weights that a scale lets vanish still count in the sum
+                    float all = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 64; ++j) all += ex2_approx(__uint_as_float(sv[j]) * unpack2f(mult2[j / 16]).x - (rounded ? 0.f : m_log2));
+                    l_row += all * exp2f(-G_row);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const float2 s0 = unpack2f(sum[c]);
+                        l_row += (s0.x + s0.y) * weight[c];
+                    }
+                }
+            } else {
+                const float2 s0 = unpack2f(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
+                l_row += s0.x + s0.y;
+            }
             if (care) {
                 // The parity is not ambiguous: the tile before it in this slot was multiplied before S(t) was, the one behind it waits
                 // for P V(t).
@@ -438,7 +502,7 @@ __device__ __forceinline__ void paged_tc_softmax(const PagedAttnArgs& a, const P
         const float inv = l_row == 0.f ? 0.f : 1.0f / l_row;
         if (final && a.lse && row_w + lane < left) {
             const int idx = row_w + lane, i = a.by_group(idx);
-            a.lse[static_cast<size_t>(w.q.row0 + tok0 + i) * a.H + w.head * a.G + idx - i * a.G] = paged_lse(m_log2, l_row);
+            a.lse[static_cast<size_t>(w.q.row0 + tok0 + i) * a.H + w.head * a.G + idx - i * a.G] = paged_lse(m_log2, T::kCodes ? l_row * exp2f(G_row) : l_row);   // the logarithm of a number near 1 where one key takes most
         }
         // 64 values of the row as pairs of bf16
         auto result = [&](int c, uint32_t (&x)[32]) {
@@ -489,11 +553,15 @@ __device__ __forceinline__ void paged_tc_softmax(const PagedAttnArgs& a, const P
             // [16 bytes of a row][row]: a warp's store is 512 bytes in one piece, and so is a load of the kernel that adds up
             const size_t part = paged_part(a, blockIdx.x, w.t0 == 0) + g * kTQ;
             float* po = a.part_o + part * HD + r * 4;
-            if (r < left) *reinterpret_cast<float2*>(a.part_ml + (part + r) * 2) = make_float2(M_row, l_row);
+            const float unit = T::kCodes ? exp2f(G_row) : 1.f;       // a part's unit is 2^M
+            if (r < left) *reinterpret_cast<float2*>(a.part_ml + (part + r) * 2) = make_float2(M_row, l_row * unit);
 #pragma unroll 1
             for (int c = 0; c < HD / 32; ++c) {
                 uint32_t v[32];
                 tmem_ld32(o_base + c * 32, v);
+                if (T::kCodes)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * unit);
                 if (l_row == 0.f)
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] = 0u;

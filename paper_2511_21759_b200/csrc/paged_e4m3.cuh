@@ -30,6 +30,14 @@ __device__ __forceinline__ uint32_t f16x2_of(unsigned short codes) {
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(codes));
     return r;
 }
+__device__ __forceinline__ uint32_t low_codes(uint32_t w) { return f16x2_of(static_cast<unsigned short>(w)); }
+__device__ __forceinline__ uint32_t high_codes(uint32_t w) { return f16x2_of(static_cast<unsigned short>(w >> 16)); }
+// some code of the four is NaN: 0x7f + 1 carries into the sign's place
+__device__ __forceinline__ bool odd_codes(uint32_t four) { return ((four & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+__device__ __forceinline__ uint32_t without_nan(uint32_t four) {   // zero in their places
+    const uint32_t nan = ((four & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+    return four & ~(nan | (nan - (nan >> 7)));
+}
 __device__ __forceinline__ float2 f32x2_of(unsigned short codes) {
     const uint32_t h = f16x2_of(codes);
     return __half22float2(*reinterpret_cast<const __half2*>(&h));

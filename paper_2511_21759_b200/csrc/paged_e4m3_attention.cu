@@ -77,15 +77,6 @@ __device__ __forceinline__ uint32_t turned(uint32_t x) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
     return r;
 }
-__device__ __forceinline__ uint32_t f16x2(float a, float b) {
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ uint32_t low_codes(uint32_t w) { return f16x2_of(static_cast<unsigned short>(w)); }
-__device__ __forceinline__ uint32_t high_codes(uint32_t w) { return f16x2_of(static_cast<unsigned short>(w >> 16)); }
-// some code of the four is NaN: 0x7f + 1 carries into the sign's place
-__device__ __forceinline__ bool odd_codes(uint32_t four) { return ((four & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
-
 template <int HD, int NR>
 __global__ void __launch_bounds__(kThreads, kCtas<NR>) paged_e4m3_attention_kernel(const __grid_constant__ CUtensorMap tm, const PagedAttnArgs a) {
     constexpr int KW = kKT / kMmaWarps;                         // keys of a warp
@@ -211,8 +202,8 @@ __global__ void __launch_bounds__(kThreads, kCtas<NR>) paged_e4m3_attention_kern
             const float by = exp2_int(-ex), mine = exp2_int(ex) * a.scale_log2;
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
-                qf[n][c][0] = f16x2(__uint_as_float(x[c].x << 16) * by, __uint_as_float(x[c].x & 0xffff0000u) * by);
-                qf[n][c][1] = f16x2(__uint_as_float(x[c].y << 16) * by, __uint_as_float(x[c].y & 0xffff0000u) * by);
+                qf[n][c][0] = paged_f16x2(__uint_as_float(x[c].x << 16) * by, __uint_as_float(x[c].x & 0xffff0000u) * by);
+                qf[n][c][1] = paged_f16x2(__uint_as_float(x[c].y << 16) * by, __uint_as_float(x[c].y & 0xffff0000u) * by);
             }
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
@@ -293,10 +284,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<NR>) paged_e4m3_attention_kern
                             const uint32_t ad = sv + chunk_at(warp * KW + kc, dd >> 2) + (dd & 3) * 4;
                             uint32_t v;
                             asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(ad) : "memory");
-#pragma unroll
-                            for (int b = 0; b < 4; ++b)
-                                if ((v >> 8 * b & 0x7fu) == 0x7fu) v &= ~(0xffu << 8 * b);
-                            asm volatile("st.shared.b32 [%0], %1;" ::"r"(ad), "r"(v) : "memory");
+                            asm volatile("st.shared.b32 [%0], %1;" ::"r"(ad), "r"(without_nan(v)) : "memory");
                         }
                         __syncwarp();
                     }
@@ -330,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<NR>) paged_e4m3_attention_kern
                     float* x = &s[e >> 1][e & 1];               // x[0], x[2]
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        x[2 * h] = (x[2 * h] + odd[e >> 1][2 * h + (e & 1)]) * (unit[e] * ks);
+                        x[2 * h] = __fmul_rn(x[2 * h] + odd[e >> 1][2 * h + (e & 1)], fminf(unit[e] * ks, 0x1.fffffep127f));   // rounded as the maximum is
                         if (!whole) {
                             const int key = k0 + h * 8 + (lane >> 2);
                             const bool seen = key < w.q.len && key - a.right <= pos[e] && (key + a.left >= pos[e] || key < a.sinks);
@@ -372,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<NR>) paged_e4m3_attention_kern
 #pragma unroll
                 for (int n = 0; n < NG; ++n)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) p[n][h] = turned(f16x2(s[n][2 * h], s[n][2 * h + 1]));
+                    for (int h = 0; h < 2; ++h) p[n][h] = turned(paged_f16x2(s[n][2 * h], s[n][2 * h + 1]));
                 if (__any_sync(0xffffffffu, rare)) {
 #pragma unroll
                     for (int n = 0; n < NG; ++n)

@@ -2,12 +2,18 @@
 // softmax and results: paged_attention_tc.cu, whose kernel this is behind the K and V tiles in shared memory; K and V of a position are
 // code * scale, numbers of bf16.
 //
-// What is its own is the way there: TMA brings codes into a ring of staging tiles, and converter warps write them as bf16, scaled, into
-// the places of the operands' canonical layout (16 codes of a lane become two pieces of 16 bytes).  A code's fields are moved into
-// place as integers, which leaves its value times 2^-120, and one product in bf16, exact, brings that and the block's scale together:
-// six instructions for two codes.  (By way of f16, where the conversion is one instruction, P and the softmax would have had to take
-// the scales in.)  NaN is found by the largest fields of a tile and put in afterwards.  The converters also do what the loader of bf16
-// does with V at keys that not all rows see: zeros where no row sees them, and NaN is kept for the softmax warps.
+// Both products are f16: a code is a number of f16, and one instruction makes an operand's word of two codes (as bf16 with its scale a code
+// took five times the work, and the converters were what the kernel waited for).  TMA brings codes into staging tiles, and converter
+// warps write them into the places of the operands' canonical layout.  Scales stay outside, as in the kernel of few rows:
+//   S: each softmax thread brings its row of Q into 1 .. 2 by a power of two, as f16, before the item's first product; a score is
+//      multiplied by that power, the softmax scale and its block's.
+//   P V: the weights that multiply codes are 2^(x - M + log2(V's scale) - G), with M + G, both whole numbers, moved as the shift of bf16
+//      is, by the largest x + log2 of a tile (apart, so that large scores do not lose the scales); in f16, up to 2^-11 of themselves
+//      or 2^-24 of the row's largest (the shift is rounded up).  The sum takes them block by block over V's scale, so that sum and
+//      output have the same unit, 2^(M + G), and the rest is as for bf16.  Where V's scales are beyond 2^+-40 weights may vanish that
+//      count in the sum, which then has exponentials of its own.
+// The converters also do what the loader of bf16 does with V at keys that not all rows see: zeros where no row sees them, and NaN is
+// kept for the softmax warps.
 //
 // Registers: the softmax warps take 160, all others 96 of the 128 that a thread is launched with.
 #include "paged_attention_tc.cuh"
@@ -18,7 +24,7 @@ namespace odb {
 namespace {
 
 template <int QT> constexpr int kConvWarps = QT;             // converters of K, and of V
-template <int QT> constexpr int kThreads = 256 * QT;         // 4 QT softmax warps; QT MMA warps, the loader, (two Q tiles: one that idles,) converters
+template <int QT> constexpr int kThreads = 256 * QT;         // 4 QT softmax warps, QT each of MMA warps, loaders, converters of K and of V
 constexpr int kLaunchRegs = 128, kSoftmaxRegs = 160, kOtherRegs = 96;   // as many warpgroups of the one as of the other
 static_assert(kSoftmaxRegs + kOtherRegs <= 2 * kLaunchRegs, "the split fits what the block was launched with");
 template <int HD, int QT> constexpr int kQBufs = HD == 128 && QT == 1 ? 1 : 2;
@@ -30,9 +36,13 @@ template <int HD, int QT>
 constexpr uint32_t kSmem = kQBufs<HD, QT> * QT * kQBytes<HD> + (kKSlots<HD, QT> + kVSlots<HD, QT>) * kTileBytes<HD> + 2 * kStaging<HD, QT> * kCodeBytes<HD> + 1024;
 static_assert(2 * (kSmem<128, 1> + 1024) <= 228 * 1024 && 2 * (kSmem<64, 1> + 1024) <= 228 * 1024 && kSmem<128, 2> <= 227 * 1024 && kSmem<64, 2> <= 227 * 1024, "the CTAs share an SM");
 
-struct alignas(8) SharedE4m3 {
+constexpr int kBlocks = kKT / kPagedBlock;   // of a tile
+constexpr int kAhead = 8;                    // a tile of K is converted less than that many tiles ahead of the softmax: kBufs - 1 scores, the slots of K
+
+struct alignas(16) SharedE4m3 {
     uint64_t q_full[2];                // an item's Q tiles landed in the buffer          (loader -> MMA)
-    uint64_t st_full[2][3];            // a tile of codes of K / V and its scales landed  (loader -> converters)
+    uint64_t q_ready[2][2];            // Q tile g in the buffer is f16                   (softmax -> MMA, 4 arrivals)
+    uint64_t st_full[2][3];            // a tile of codes of K, with all scales, / V landed (loader -> converters)
     uint64_t st_empty[2][3];           // the converters have read it                     (converters -> loader)
     uint64_t k_full[4], v_full[4];     // K or V tile written, V looked at                (converters -> MMA; V -> softmax)
     uint64_t k_empty[4], v_empty[4];   // the MMAs have read the slot                     (MMA -> converters, QT arrivals)
@@ -43,7 +53,9 @@ struct alignas(8) SharedE4m3 {
     uint64_t item_done[2];             // the Q buffer may be overwritten                 (softmax -> loader, 4 QT arrivals)
     uint32_t tmem_base;
     int abort, keep_o[2];
-    float scale[2][3][kKT / kPagedBlock];   // of a staging tile's blocks
+    float scale[3][2][kBlocks];        // of a staging tile's blocks of K, of V
+    alignas(16) float scales[kAhead][3][kBlocks];   // of the tiles at work: K's scale, log2 of V's, 1 / V's (converter of K -> softmax)
+    int wide[kAhead];                  // some log2 of V's scales is beyond +-40
     int odd[4][2];                     // V in the slot has NaN where only some rows see it, by converter
 };
 static_assert(sizeof(SharedE4m3) <= 1024, "the barriers end inside the allocation");
@@ -51,7 +63,46 @@ static_assert(sizeof(SharedE4m3) <= 1024, "the barriers end inside the allocatio
 template <int HD_, int QT_>
 struct TcE4m3 {
     static constexpr int HD = HD_, QT = QT_, NQ = kQBufs<HD, QT>, KS = kKSlots<HD, QT>, VS = kVSlots<HD, QT>;
+    static constexpr bool kCodes = true;
     using Shared = SharedE4m3;
+    static __device__ __forceinline__ uint64_t* q_ready(Shared* sh, int g) { return sh->q_ready[g]; }
+    // The thread's row of the item's Q tile as f16 in 1 .. 2: what its scores are multiplied by.
+    template <int ROWS, class Wait>
+    static __device__ __forceinline__ float own_q(Shared* sh, uint8_t* sQ, uint32_t item, int g, int r, bool& ok, Wait& wait) {
+        const uint32_t buf = item % NQ, row = smem_u32(sQ) + (buf * QT + g) * kQBytes<HD> + r * 128;
+        ok = __all_sync(0xffffffffu, wait(&sh->q_full[buf], (item / NQ) & 1u)) && ok;
+        auto at = [&](int c) { return row + (c >> 3) * (ROWS * 128) + (((c & 7) ^ (r & 7)) << 4); };
+        uint32_t x[HD / 8][4], top = 0;
+#pragma unroll
+        for (int c = 0; c < HD / 8; ++c)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[c][0]), "=r"(x[c][1]), "=r"(x[c][2]), "=r"(x[c][3]) : "r"(at(c)) : "memory");
+#pragma unroll
+        for (int c = 0; c < HD / 8; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = max_u16x2(top, x[c][j] & 0x7fff7fffu);
+        top = max(top & 0xffffu, top >> 16);
+        const int ex = min(max(static_cast<int>(top >> 7) - 127, -126), 126);     // an infinity stays one
+        const float by = exp2_int(-ex);
+#pragma unroll
+        for (int c = 0; c < HD / 8; ++c) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[c][j] = paged_f16x2(__uint_as_float(x[c][j] << 16) * by, __uint_as_float(x[c][j] & 0xffff0000u) * by);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at(c)), "r"(x[c][0]), "r"(x[c][1]), "r"(x[c][2]), "r"(x[c][3]) : "memory");
+        }
+        proxy_fence();
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(&sh->q_ready[g][buf]);
+        return exp2_int(ex);
+    }
+    // The scales of tile n's blocks; whether V's are wide.
+    static __device__ __forceinline__ bool scales(Shared* sh, uint32_t n, float (&k)[kBlocks], float (&log_v)[kBlocks], float (&by_v)[kBlocks]) {
+        const float4* s = reinterpret_cast<const float4*>(sh->scales[n % kAhead]);
+        const float4 x = s[0], y = s[1], z = s[2];
+        k[0] = x.x; k[1] = x.y; k[2] = x.z; k[3] = x.w;
+        log_v[0] = y.x; log_v[1] = y.y; log_v[2] = y.z; log_v[3] = y.w;
+        by_v[0] = z.x; by_v[1] = z.y; by_v[2] = z.z; by_v[3] = z.w;
+        return sh->wide[n % kAhead] != 0;
+    }
     // V of the slot has been looked at; it has NaN where only some rows see it; whether this is one (0: it is not)
     static __device__ __forceinline__ uint64_t* v_seen(Shared* sh, uint32_t slot) { return &sh->v_full[slot]; }
     static __device__ __forceinline__ bool odd(Shared* sh, uint32_t slot) {
@@ -66,19 +117,6 @@ struct TcE4m3 {
     }
 };
 
-// two codes in the upper bytes of the halves -> their values times 2^-120 as bf16; top: the largest fields so far
-__device__ __forceinline__ uint32_t widen_codes(uint32_t x, uint32_t& top) {
-    const uint32_t m = (x >> 4) & 0x07f007f0u;
-    top = max_u16x2(top, m);
-    return m | (x & 0x80008000u);
-}
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-__device__ __forceinline__ uint32_t exp2_bf16x2(int e) { return static_cast<uint32_t>(e + 127) * 0x00800080u; }
-
 template <int HD, int QT>
 __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
     paged_e4m3_attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_codes,
@@ -87,13 +125,14 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
     using T = TcE4m3<HD, QT>;
     constexpr int NQ = T::NQ, KS = T::KS, VS = T::VS, ST = kStaging<HD, QT>, CW = kConvWarps<QT>, kFirst = kBufs<HD> - 1, kAtoms = HD / 64;
     constexpr uint32_t kT = kTileBytes<HD>, kC = kCodeBytes<HD>;
-    constexpr int kSoftmaxWarps = 4 * QT, kLoader = kSoftmaxWarps + QT, kConv = kThreads<QT> / 32 - 2 * CW, kBlocks = kKT / kPagedBlock;
+    constexpr int kSoftmaxWarps = 4 * QT, kLoader = kSoftmaxWarps + QT, kConv = kThreads<QT> / 32 - 2 * CW;
     uint8_t* sQ = smem_raw;                                  // [buffer][Q tile]
     uint8_t* sK = sQ + NQ * QT * kQBytes<HD>;
     uint8_t* sV = sK + KS * kT;
     uint8_t* sC = sV + VS * kT;                              // [K, V][tile]
     SharedE4m3* sh = reinterpret_cast<SharedE4m3*>(sC + 2 * ST * kC);
     static_assert(VS >= kBufs<HD>, "the tile before in a slot of V has been multiplied when the softmax asks for this one");
+    static_assert(kBufs<HD> - 1 + KS < kAhead, "a tile's scales stay until the softmax has read them");
     static_assert(KS <= 4 && VS <= 4 && ST <= 3 && kBufs<HD> * kKT + HD <= static_cast<int>(kCols) && 4 * kPatch <= kQBytes<HD>, "rings, TMEM columns, patches");
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     volatile int* cta_abort = &sh->abort;
@@ -111,7 +150,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
             mbar_init(&sh->item_done[i], kSoftmaxWarps);
         }
         for (int i = 0; i < 2 * ST; ++i) {
-            mbar_init(&sh->st_full[i & 1][i >> 1], 1 + kBlocks);
+            mbar_init(&sh->st_full[i & 1][i >> 1], i & 1 ? 1 : 1 + 2 * kBlocks);   // the tile, and the lanes that copy scales
             mbar_init(&sh->st_empty[i & 1][i >> 1], CW);
         }
         for (int i = 0; i < KS; ++i) {
@@ -129,6 +168,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
             }
             for (int i = 0; i < 2; ++i) mbar_init(&sh->pv_done[g][i], 1);
             mbar_init(&sh->o_full[g], 1);
+            for (int i = 0; i < NQ; ++i) mbar_init(&sh->q_ready[g][i], 4);
             sh->keep_o[g] = 0;
         }
         sh->abort = 0;
@@ -177,8 +217,8 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         if (warp < kLoader) {
             paged_tc_mma<T>(a, start, sh, sQ, sK, sV, tmem, warp - kSoftmaxWarps);
-        } else if (warp == kLoader) {
-            // ================= loader: codes and scales; Q before its item's first tile or (one Q buffer) where the item in front has ended
+        } else if (warp < kLoader + QT) {
+            // ================= loader, or (two Q tiles) one of K and Q and one of V: codes and scales; Q before its item's first tile or (one Q buffer) where the item in front has ended
             const int box_shift = min(a.page_shift, 6), box = 1 << box_shift;
             bool ok = true;
             Tiles k(a, start), v(a, start);
@@ -201,10 +241,11 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                     if (paged_elect()) tma_codes(codes + (V * ST + x.slot) * kC + c * box * HD, &tm_codes, full, r);
                     __syncwarp();
                 }
-                if (lane < kBlocks) {                        // a page that is none reads as zeros
+                if (!V && lane < 2 * kBlocks) {              // K's scales, then V's; a page that is none reads as zeros
+                    float* scale = &sh->scale[x.slot][0][lane];
                     if (b < n_blocks) {
-                        if (row < a.pool_rows) copy4(smem_u32(&sh->scale[V][x.slot][b]), a.scales + row / kPagedBlock);
-                        else sh->scale[V][x.slot][b] = 1.f;
+                        if (row < a.pool_rows) copy4(smem_u32(scale), a.scales + (row + (lane < kBlocks ? 0 : a.v_row0 - a.k_row0)) / kPagedBlock);
+                        else *scale = 1.f;
                     }
                     copies_arrive(full);
                 }
@@ -232,8 +273,19 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                 ++nq;
                 have_q = wq.next();
             };
+            if (QT == 2) {
+                static_assert(QT == 1 || NQ == 2, "K waits for its item's Q buffer, V does not");
+                if (warp == kLoader)
+                    while (ok && k.have) {
+                        if (k.t == k.w.t0) next_q();
+                        load(k, k_pages, std::false_type());
+                    }
+                else
+                    while (ok && v.have) load(v, v_pages, std::true_type());
+                k.have = v.have = false;
+            }
             for (int i = 0; i < kFirst; ++i) load(k, k_pages, std::false_type());
-            if (NQ == 2) next_q();
+            if (QT == 1 && NQ == 2) next_q();
             while (ok && v.have) {
                 if (NQ == 1 && v.t == v.w.t0) next_q();
                 // behind the item's third tile: the epilogue in front of it, which frees the buffer, is on its way by then
@@ -256,8 +308,10 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
         } else if (warp >= kConv) {
             // ================= converters of K, then of V: each the same keys of every tile =================
             constexpr int kKeys = kKT / CW, kPieces = HD / 16, kAtOnce = 32 / kPieces, kSteps = kPagedBlock / kAtOnce;   // keys of a warp, of a step; steps of a block
-            const int cw = (warp - kConv) % CW, piece = lane % kPieces, atom = piece >> 2;
-            const int first = (piece & 3) * 2 + (atom & 1);  // of a lane's two halves the one that it stores first: eight lanes at a time meet all banks
+            // Of eight lanes at a time, which a store of 16 bytes takes together, four have neighbouring pieces of one key and four those of the
+            // next: all banks, by the swizzle.
+            const int cw = (warp - kConv) % CW, piece = HD == 128 ? (lane & 3) + (lane >> 3 & 1) * 4 : lane & 3, atom = piece >> 2;
+            const int mine = HD == 128 ? (lane >> 2 & 1) + (lane >> 4) * 2 : lane >> 2;          // of a step's keys
             auto convert = [&](uint8_t* tiles, uint64_t* full, uint64_t* empty, auto is_v) {
                 constexpr int V = decltype(is_v)::value, SL = V ? VS : KS;
                 Tiles x(a, start);
@@ -273,60 +327,50 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                         return HD == 128 ? from + key * 128 + ((piece ^ (key & 7)) << 4) : from + key * 64 + ((piece ^ (key >> 1 & 3)) << 4);
                     };
                     auto hidden = [&](int key) { return care && (k0 + key >= x.w.k.hi || (k0 + key < x.w.k.lo && k0 + key >= a.sinks)); };
-                    uint32_t top = 0;
+                    if (!V && cw == 0) {                      // the tile's scales to the softmax warps
+                        const int first = k0 + (lane & (kBlocks - 1)) * kPagedBlock;
+                        const bool unseen = first >= x.w.k.hi || (first + kPagedBlock <= x.w.k.lo && first >= a.sinks);   // by all rows of the item
+                        const int e = unseen ? 0 : e4m3_exponent((&sh->scale[x.slot][0][0])[lane & (2 * kBlocks - 1)]);
+                        float* s = &sh->scales[x.n % kAhead][0][0];
+                        if (lane < kBlocks) s[lane] = exp2_int(e);
+                        else if (lane < 2 * kBlocks) {
+                            s[lane] = static_cast<float>(e);
+                            s[lane + kBlocks] = exp2_int(-e);
+                        }
+                        const bool wide = __any_sync(0xffffffffu, lane >= kBlocks && lane < 2 * kBlocks && (e < -40 || e > 40));
+                        if (lane == 0) sh->wide[x.n % kAhead] = wide;
+                    }
+                    bool nan = false;
 #pragma unroll 1
-                    for (int key0 = cw * kKeys; key0 < (cw + 1) * kKeys; key0 += kPagedBlock) {      // a block, one scale
-                        const int e = e4m3_exponent(sh->scale[V][x.slot][key0 / kPagedBlock]), key1 = key0 + lane / kPieces;
-                        const uint32_t by = exp2_bf16x2(min(e, 7) + 120);
-                        uint32_t w[kSteps][4], y[kSteps][8];
+                    for (int key0 = cw * kKeys + mine; key0 < (cw + 1) * kKeys; key0 += kPagedBlock) {
+                        uint32_t w[kSteps][4];
 #pragma unroll
                         for (int i = 0; i < kSteps; ++i)
                             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                         : "=r"(w[i][0]), "=r"(w[i][1]), "=r"(w[i][2]), "=r"(w[i][3]) : "r"(code_at(key1 + i * kAtOnce)) : "memory");
-#pragma unroll
-                        for (int i = 0; i < kSteps; ++i) {
-                            if (care && hidden(key1 + i * kAtOnce)) w[i][0] = w[i][1] = w[i][2] = w[i][3] = 0u;
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                y[i][2 * j] = mul_bf16x2(widen_codes(__byte_perm(w[i][j], 0, 0x1404), top), by);
-                                y[i][2 * j + 1] = mul_bf16x2(widen_codes(__byte_perm(w[i][j], 0, 0x3424), top), by);
-                            }
-                        }
-                        if (e > 7) {                          // 2^(e + 120) is no number of bf16
-                            const uint32_t more = exp2_bf16x2(e - 7);
+                                         : "=r"(w[i][0]), "=r"(w[i][1]), "=r"(w[i][2]), "=r"(w[i][3]) : "r"(code_at(key0 + i * kAtOnce)) : "memory");
+                        if (care) {
 #pragma unroll
                             for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-                                for (int j = 0; j < 8; ++j) y[i][j] = mul_bf16x2(y[i][j], more);
+                                for (int j = 0; j < 4; ++j) {
+                                    if (hidden(key0 + i * kAtOnce)) w[i][j] = 0u;
+                                    if (odd_codes(w[i][j])) {         // rare: the softmax warps give it to the rows that see it
+                                        nan = true;
+                                        w[i][j] = without_nan(w[i][j]);
+                                    }
+                                }
                         }
 #pragma unroll
                         for (int i = 0; i < kSteps; ++i) {
-                            const int key = key1 + i * kAtOnce;
+                            const int key = key0 + i * kAtOnce;
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const int odd = (first ^ h) & 1;
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + key * 128 + (((first ^ h) ^ (key & 7)) << 4)),
-                                             "r"(odd ? y[i][4] : y[i][0]), "r"(odd ? y[i][5] : y[i][1]), "r"(odd ? y[i][6] : y[i][2]), "r"(odd ? y[i][7] : y[i][3])
+                            for (int h = 0; h < 2; ++h)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + key * 128 + ((((piece & 3) * 2 + h) ^ (key & 7)) << 4)),
+                                             "r"(low_codes(w[i][2 * h])), "r"(high_codes(w[i][2 * h])), "r"(low_codes(w[i][2 * h + 1])), "r"(high_codes(w[i][2 * h + 1]))
                                              : "memory");
-                            }
                         }
                     }
-                    const bool nan = __any_sync(0xffffffffu, (top & 0xffffu) == 0x07f0u || top >> 16 == 0x07f0u);
-                    if (nan) {                                // rare
-#pragma unroll 1
-                        for (int key = cw * kKeys + lane / kPieces; key < (cw + 1) * kKeys; key += kAtOnce) {
-                            if (hidden(key)) continue;
-#pragma unroll 1
-                            for (int j = 0; j < 16; ++j) {
-                                uint32_t c;
-                                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(c) : "r"(code_at(key) + j) : "memory");
-                                if ((c & 0x7fu) == 0x7fu)     // where only some rows see it the softmax warps give it to them
-                                    asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + key * 128 + ((((piece & 3) * 2 + (j >> 3)) ^ (key & 7)) << 4) + (j & 7) * 2),
-                                                 "h"(static_cast<unsigned short>(care ? 0 : 0x7fff))
-                                                 : "memory");
-                            }
-                        }
-                    }
+                    nan = __any_sync(0xffffffffu, nan);
                     if (care && lane == 0) *const_cast<volatile int*>(&sh->odd[slot][cw]) = nan;
                     proxy_fence();
                     __syncwarp();

@@ -7,8 +7,9 @@ Bounds, derived before the first run.
   the oracle's, under the exponent that the block got.
   load: exact.
   attention, over the values that the codes stand for: the output's rounding to bf16, 2^-8 of its value (half a step is 2^-9; the double is
-  kept for the sums in front of it); a weight's rounding, 2^-8 (bf16) or 2^-11 (f16) of itself, and in f16 no less than 2^-25 of the row's
-  largest product of weight and scale: at most the weight itself; a score's fp32 sum of head_dim exact products, head_dim 2^-24 sum|q k|
+  kept for the sums in front of it); a weight's rounding to f16, 2^-11 of itself (2^-8 is allowed, as for the pool of bf16), and no less
+  than 2^-24 of the row's largest product of weight and scale (half a step of 2^-24 where that is rounded up to a power of two): at most
+  the weight itself; a score's fp32 sum of head_dim exact products, head_dim 2^-24 sum|q k|
   scale, and Q in f16 under a power of two, 2^-25 of its largest value per dim: together d, which moves numerator and denominator by a
   factor e^d each; log-sum-exp by d and a rounding of fp32."""
 import numpy as np
@@ -430,8 +431,8 @@ def check(out, lse, qf, keys, values, vscale, start, firsts, D, scale=None, scal
                 want, mag = w @ v, w @ np.abs(v)
                 size = (np.abs(q) @ np.abs(k).T).max(1) * abs(sc)
                 d = D * 2.0 ** -24 * size + 2.0 ** -25 * np.abs(q).max(1) * np.abs(k).sum(1).max() * abs(sc)
-                # f16: no less than 2^-25 of the row's largest product of weight and scale
-                least = np.minimum(w * vs, 2.0 ** -25 * (w * vs).max(1, keepdims=True)) @ (np.abs(v) / vs[:, None])
+                # f16: no less than 2^-24 of the row's largest product of weight and scale
+                least = np.minimum(w * vs, 2.0 ** -24 * (w * vs).max(1, keepdims=True)) @ (np.abs(v) / vs[:, None])
                 if scaled:
                     d = d + 2.0 ** -23 * size
                     grow = np.minimum(np.expm1(np.minimum(2 * d, 50.0)), 1e6)[:, None]
