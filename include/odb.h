@@ -465,11 +465,15 @@ int32_t odb_paged_status(odb_paged* h, void* stream);
  * The same handle over a pool of half the bytes: e4m3 [n_layers][2][n_pages][n_kv_heads][page_size][head_dim] with an fp32 scale for each
  * block of 16 positions of a head, [n_layers][2][n_pages][n_kv_heads][page_size / 16]; K or V of a position is code * scale.  Scales are
  * powers of two from 2^-100 to 2^119, so that what a code stands for is a number of bf16.  kv and scales on 256-byte boundaries, borrowed
- * as kv is; the workspace is odb_paged_workspace_bytes'.  layout, attention, load, status and destroy are called as over a pool of bf16
+ * as kv is; the workspace is odb_paged_workspace_bytes', or more (below).  layout, attention, load, status and destroy are called as over a pool of bf16
  * (an attention's weights are rounded to f16 or bf16 for the product with V); for the store see odb_paged_norm_rope_store. */
 enum { ODB_PAGED_SCALE_BLOCK = 16 };
 size_t odb_paged_e4m3_kv_bytes(const odb_paged_config* cfg);     /* 0: a configuration odb_paged_create_e4m3 would refuse */
 size_t odb_paged_e4m3_scale_bytes(const odb_paged_config* cfg);
+/* A workspace of odb_paged_workspace_bytes + this many bytes has room for the K and V of one layer in bf16: prompts (requests of more than
+ * 128 packed rows that are alike) are then read from a copy of their pages, made in the call, which takes half the time.  Without it they
+ * are read as all others are. */
+size_t odb_paged_e4m3_layer_bytes(const odb_paged_config* cfg);
 int32_t odb_paged_create_e4m3(const odb_paged_config* cfg, void* kv, size_t kv_bytes, void* scales, size_t scale_bytes, void* workspace,
                               size_t ws_bytes, void* stream, odb_paged** out);
 

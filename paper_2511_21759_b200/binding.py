@@ -127,6 +127,7 @@ SIGNATURES = {
                                      C.POINTER(C.c_void_p)]),
     "odb_paged_e4m3_kv_bytes": (C.c_size_t, [C.POINTER(odb_paged_config)]),
     "odb_paged_e4m3_scale_bytes": (C.c_size_t, [C.POINTER(odb_paged_config)]),
+    "odb_paged_e4m3_layer_bytes": (C.c_size_t, [C.POINTER(odb_paged_config)]),
     "odb_paged_create_e4m3": (C.c_int32, [C.POINTER(odb_paged_config), C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t,
                                           C.c_void_p, C.POINTER(C.c_void_p)]),
     "odb_paged_destroy": (C.c_int32, [C.c_void_p]),

@@ -122,9 +122,13 @@ constexpr int kPagedTcItem = 3;         // key tiles that an item costs the many
 size_t paged_part_bytes(int hd);
 
 // ---- attention over a pool of 8 bits (paged_e4m3_attention.cu) ----
-int paged_e4m3_attention_kernel_of(int n_seqs, int max_rows, int max_new, int group, int kv_heads, long long longest, long long out_stride);
-cudaError_t launch_paged_e4m3_attention_tc(PagedAttnArgs a, const CUtensorMap& map, int hd, int q_tiles, int sms, cudaStream_t st);
-cudaError_t launch_paged_e4m3_attention(PagedAttnArgs a, const CUtensorMap& map, int hd, int q_tiles, int sms, cudaStream_t st);
+// The kernel: 8 or 16, the packed rows of the few rows' items; 1, the many rows' over the codes; 2, that of bf16 with two Q tiles, over a copy of
+// the pages (room: there is memory for one); -1: none, its sums would pass 32 bits.
+int paged_e4m3_attention_kernel_of(int n_seqs, int max_rows, int max_new, int group, int kv_heads, long long longest, long long out_stride, bool room);
+cudaError_t launch_paged_e4m3_attention_tc(PagedAttnArgs a, const CUtensorMap& map, int hd, int sms, cudaStream_t st);
+cudaError_t launch_paged_e4m3_attention(PagedAttnArgs a, const CUtensorMap& map, int hd, int kernel, int sms, cudaStream_t st);
+// The pages that an attention's rows see, as bf16 in their places of one layer's K and V (paged_load.cu).
+cudaError_t launch_paged_expand(const PagedAttnArgs& a, __nv_bfloat16* layer, int layer_rows, int hd, cudaStream_t st);
 
 #ifdef __CUDACC__
 // ---------------------------------------------------------------------------------------

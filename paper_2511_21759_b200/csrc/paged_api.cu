@@ -18,6 +18,8 @@ struct odb_paged {
     float *part_o, *part_ml;
     int pool_rows, layer_rows;      // rows of head_dim values: of the whole pool, of the K or the V of a layer
     PagedMaps maps;                 // pools of 8 bits: rows alone
+    __nv_bfloat16* layer;           // pools of 8 bits: room for a layer's K and V in bf16, null: there is none
+    PagedMaps layer_maps;
     int value_bytes() const { return scales ? 1 : 2; }
     // the layer's K, and V behind it
     char* k_of(int layer) const { return static_cast<char*>(kv) + static_cast<size_t>(2 * layer) * layer_rows * cfg.head_dim * value_bytes(); }
@@ -107,6 +109,11 @@ int32_t create(const odb_paged_config* cfg, void* kv, size_t kv_bytes, float* sc
     const int box_rows = cfg->page_size < 64 ? cfg->page_size : 64;
     if (scales) {
         if (e == cudaSuccess) e = make_pool_e4m3_tmap(&h->maps.rows, kv, h->pool_rows, cfg->head_dim, box_rows);
+        if (ws_bytes >= odb_paged_workspace_bytes(cfg) + odb_paged_e4m3_layer_bytes(cfg)) {
+            h->layer = reinterpret_cast<__nv_bfloat16*>(ws + odb_paged_workspace_bytes(cfg));
+            if (e == cudaSuccess) e = make_pool_tmap(&h->layer_maps.rows, h->layer, 2ull * h->layer_rows, cfg->head_dim, box_rows, cfg->head_dim / 64);
+            if (e == cudaSuccess) e = make_pool_tmap(&h->layer_maps.atoms, h->layer, 2ull * h->layer_rows, cfg->head_dim, box_rows, 1);
+        }
     } else {
         if (e == cudaSuccess) e = make_pool_tmap(&h->maps.rows, kv, h->pool_rows, cfg->head_dim, box_rows, cfg->head_dim / 64);
         if (e == cudaSuccess) e = make_pool_tmap(&h->maps.atoms, kv, h->pool_rows, cfg->head_dim, box_rows, 1);
@@ -147,6 +154,10 @@ size_t odb_paged_e4m3_kv_bytes(const odb_paged_config* c) { return check_config(
 
 size_t odb_paged_e4m3_scale_bytes(const odb_paged_config* c) {
     return check_config(c) != ODB_OK ? 0 : pool_values(c) / c->head_dim / kPagedBlock * sizeof(float);
+}
+
+size_t odb_paged_e4m3_layer_bytes(const odb_paged_config* c) {
+    return check_config(c) != ODB_OK ? 0 : pool_values(c) / c->n_layers * sizeof(__nv_bfloat16);
 }
 
 int32_t odb_paged_create_e4m3(const odb_paged_config* cfg, void* kv, size_t kv_bytes, void* scales, size_t scale_bytes, void* workspace,
@@ -277,8 +288,9 @@ int32_t odb_paged_attention(odb_paged* h, int32_t layer, const odb_paged_batch* 
     if (overlap({out, out_stride, qw}, {q, q_stride, qw}, b->max_rows)) return ODB_ERR_ARG;   // some CTAs read Q after others have written
     const int G = c.n_heads / c.n_kv_heads;
     if (static_cast<double>(b->max_rows) * c.n_heads >= 2147483648.0 - 65536) return ODB_ERR_SHAPE;   // packed rows are 32-bit numbers
-    const int q_tiles = (h->scales ? paged_e4m3_attention_kernel_of : paged_attention_kernel_of)(b->n_seqs, b->max_rows, b->max_new, G, c.n_kv_heads, longest, out_stride);
-    if (q_tiles < 0) return ODB_ERR_SHAPE;
+    const int kernel = h->scales ? paged_e4m3_attention_kernel_of(b->n_seqs, b->max_rows, b->max_new, G, c.n_kv_heads, longest, out_stride, h->layer != nullptr)
+                                 : paged_attention_kernel_of(b->n_seqs, b->max_rows, b->max_new, G, c.n_kv_heads, longest, out_stride);
+    if (kernel < 0) return ODB_ERR_SHAPE;
     PagedAttnArgs a{};
     a.q = static_cast<const __nv_bfloat16*>(q);
     a.out = static_cast<__nv_bfloat16*>(out);
@@ -297,8 +309,16 @@ int32_t odb_paged_attention(odb_paged* h, int32_t layer, const odb_paged_batch* 
     a.status = h->status; a.arrivals = h->arrivals; a.part_o = h->part_o; a.part_ml = h->part_ml;
     a.shared = h->shared;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (h->scales) return enqueued(launch_paged_e4m3_attention(a, h->maps.rows, c.head_dim, q_tiles, h->sms, st));
-    return enqueued(launch_paged_attention(a, h->maps, c.head_dim, q_tiles, h->sms, st));
+    if (!h->scales) return enqueued(launch_paged_attention(a, h->maps, c.head_dim, kernel, h->sms, st));
+    if (kernel != 2) return enqueued(launch_paged_e4m3_attention(a, h->maps.rows, c.head_dim, kernel, h->sms, st));
+    a.by_rows = PagedDiv::by(1);                            // of no use to the copy, but read
+    a.by_group = a.by_rows;
+    const cudaError_t e = launch_paged_expand(a, h->layer, h->layer_rows, c.head_dim, st);
+    if (e != cudaSuccess) return record_cuda_error(e);
+    a.pool = reinterpret_cast<const unsigned short*>(h->layer);
+    a.scales = nullptr;
+    a.k_row0 = 0; a.v_row0 = h->layer_rows; a.pool_rows = 2 * h->layer_rows;
+    return enqueued(launch_paged_attention(a, h->layer_maps, c.head_dim, kernel, h->sms, st));
 }
 
 int32_t odb_paged_load(odb_paged* h, int32_t layer, const odb_paged_batch* b, void* k, int64_t k_stride, void* v, int64_t v_stride, void* stream) {

@@ -290,7 +290,7 @@ __device__ __forceinline__ void paged_tc_softmax(const PagedAttnArgs& a, const P
         const SeenByAll by_tile(a, w.q, tok0, a.tile_tokens), by_item(a, w.q, w.rt * QT * a.tile_tokens, QT * a.tile_tokens);
         const int left = min(rows_g, (w.q.n - tok0) * a.G);          // rows of the Q tile (may be negative); others hold anything
         const bool mine = r < left;
-        if constexpr (T::kCodes) scale = a.scale_log2 * T::template own_q<kTQ>(sh, sQ, item, g, r, ok, wait);
+        if constexpr (T::kCodes) scale = a.scale_log2 * T::template own_q<kTQ>(sh, sQ, item, r, ok, wait);
         float M_row = -INFINITY, l_row = 0.f, G_row = 0.f;           // the row's shift, M (kCodes: M + G), and its sum
         uint32_t sv[64];                                             // the row's scores of the tile at hand
         auto ask = [&](int t) {                                      // for those of tile t, once they are there
@@ -319,7 +319,7 @@ __device__ __forceinline__ void paged_tc_softmax(const PagedAttnArgs& a, const P
             if constexpr (T::kCodes) {
                 wide = T::scales(sh, gt, mul, up, weight);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) mul[c] = fminf(fmaxf(mul[c] * scale, 0x1p-126f), 0x1.fffffep127f);   // masked scores, and zeros, stay what they are
+                for (int c = 0; c < 4; ++c) mul[c] = fmaxf(mul[c] * scale, 0x1p-126f);   // not zero: masked scores stay what they are
             }
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
@@ -358,7 +358,7 @@ __device__ __forceinline__ void paged_tc_softmax(const PagedAttnArgs& a, const P
             for (int c = 0; c < 4; ++c) mult2[c] = T::kCodes ? pack2f(mul[c], mul[c]) : pack2f(scale, scale);
             float factor = 1.0f;                                     // what O and the row sum so far are multiplied by
             bool rescale = false, rounded = false;                   // rounded: the scores stand as x, kCodes: as x - M
-            if (__any_sync(0xffffffffu, move || far)) {
+            if (__builtin_expect(__any_sync(0xffffffffu, move || far), 0)) {
                 if (move) {
                     float G_new = 0.f;
                     if constexpr (T::kCodes) {
@@ -423,7 +423,7 @@ __device__ __forceinline__ void paged_tc_softmax(const PagedAttnArgs& a, const P
             }
             if (QT == 2) turn_end(g, gw);
             if constexpr (T::kCodes) {
-                if (wide) {                                          // weights that a scale lets vanish still count in the sum
+                if (__builtin_expect(wide, 0)) {                                // weights that a scale lets vanish still count in the sum
                     float all = 0.f;
 #pragma unroll
                     for (int j = 0; j < 64; ++j) all += ex2_approx(__uint_as_float(sv[j]) * unpack2f(mult2[j / 16]).x - (rounded ? 0.f : m_log2));

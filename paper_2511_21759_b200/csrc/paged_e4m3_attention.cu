@@ -27,6 +27,7 @@ constexpr int kMinUnits = 2;                // units of a CTA, at least
 constexpr int kKT = 64;                     // keys per tile
 constexpr int kFullUnits = 12;              // of a CTA where all places on the SMs have work
 constexpr int kSmallUnits = 1024;           // up to here few rows' kernel for any number of rows
+constexpr int kCopiedRows = 128;            // packed rows of the longest request from which requests that are alike take a copy in bf16
 constexpr int kManyRows = 1024;             // packed rows a request, on average, from which two Q tiles are right whatever the longest
 constexpr int kMmaWarps = 4;                // 16 keys of a tile each
 constexpr int kThreads = 32 * (kMmaWarps + 1);
@@ -520,9 +521,8 @@ cudaError_t launch(PagedAttnArgs a, const CUtensorMap& tmap, int sms, cudaStream
 
 }  // namespace
 
-// Which kernel, as for a pool of bf16 (paged_attention_kernel_of): 8 or 16, the packed rows of the few rows' items; 1 or 2, the Q tiles of the
-// many rows'; -1, none.
-int paged_e4m3_attention_kernel_of(int n_seqs, int max_rows, int max_new, int group, int kv_heads, long long longest, long long out_stride) {
+// Which kernel, as for a pool of bf16 (paged_attention_kernel_of).
+int paged_e4m3_attention_kernel_of(int n_seqs, int max_rows, int max_new, int group, int kv_heads, long long longest, long long out_stride, bool room) {
     const long long all = static_cast<long long>(max_rows) * group, mean = (max_rows + n_seqs - 1ll) / n_seqs * group,
                     mine = max_new > 0 ? static_cast<long long>(max_new) * group : mean, tiles = longest / kKT + 1;
     // units of all items together and what is added to them on the way, with rows that follow one another
@@ -535,9 +535,8 @@ int paged_e4m3_attention_kernel_of(int n_seqs, int max_rows, int max_new, int gr
         const double units = static_cast<double>((all + 15ll * n_seqs) / 16) * kv_heads * static_cast<double>(tiles + kItem);
         if ((mine > 16 && units > kSmallUnits) || few < 0) {
             const bool alike = max_new > 0 ? static_cast<long long>(max_new) * n_seqs <= 3ll * max_rows : n_seqs == 1 || mean >= kManyRows;
-            const int q_tiles = mine > 128 && alike ? 2 : 1;
-            if (fits(q_tiles * tile, kPagedTcItem)) return q_tiles;
-            return fits(2 * tile, kPagedTcItem) ? 2 : -1;
+            if (room && ((mine > kCopiedRows && alike) || !fits(tile, kPagedTcItem)) && fits(2 * tile, kPagedTcItem)) return 2;
+            return fits(tile, kPagedTcItem) ? 1 : few;
         }
     }
     return few;
@@ -548,7 +547,7 @@ cudaError_t launch_paged_e4m3_attention(PagedAttnArgs a, const CUtensorMap& map,
     a.by_group = PagedDiv::by(a.G);
     if (kernel == 8) return hd == 128 ? launch<128, 8>(a, map, sms, st) : launch<64, 8>(a, map, sms, st);
     if (kernel == 16) return hd == 128 ? launch<128, 16>(a, map, sms, st) : launch<64, 16>(a, map, sms, st);
-    return launch_paged_e4m3_attention_tc(a, map, hd, kernel, sms, st);
+    return launch_paged_e4m3_attention_tc(a, map, hd, sms, st);
 }
 
 }  // namespace odb

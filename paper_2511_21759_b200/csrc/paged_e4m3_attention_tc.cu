@@ -2,9 +2,14 @@
 // softmax and results: paged_attention_tc.cu, whose kernel this is behind the K and V tiles in shared memory; K and V of a position are
 // code * scale, numbers of bf16.
 //
+// An item is one Q tile, and every item writes its K and V tiles as operands for itself: this kernel is for requests of one row tile
+// (block steps) and for mixtures; prompts, whose row tiles would all do that again, take the pool's bf16 copy where there is memory for it
+// (paged_load.cu).
+//
 // Both products are f16: a code is a number of f16, and one instruction makes an operand's word of two codes (as bf16 with its scale a code
-// took five times the work, and the converters were what the kernel waited for).  TMA brings codes into staging tiles, and converter
-// warps write them into the places of the operands' canonical layout.  Scales stay outside, as in the kernel of few rows:
+// took five times the work, and the converters were what the kernel waited for: blocks of 32 rows 92 us instead of 67).  TMA brings codes
+// into staging tiles, and converter warps write them into the places of the operands' canonical layout.  Scales stay outside, as in the
+// kernel of few rows:
 //   S: each softmax thread brings its row of Q into 1 .. 2 by a power of two, as f16, before the item's first product; a score is
 //      multiplied by that power, the softmax scale and its block's.
 //   P V: the weights that multiply codes are 2^(x - M + log2(V's scale) - G), with M + G, both whole numbers, moved as the shift of bf16
@@ -23,53 +28,52 @@ namespace odb {
 
 namespace {
 
-template <int QT> constexpr int kConvWarps = QT;             // converters of K, and of V
-template <int QT> constexpr int kThreads = 256 * QT;         // 4 QT softmax warps, QT each of MMA warps, loaders, converters of K and of V
+constexpr int kThreads = 256;                               // four softmax warps; an MMA warp, the loader, a converter of K and one of V
 constexpr int kLaunchRegs = 128, kSoftmaxRegs = 160, kOtherRegs = 96;   // as many warpgroups of the one as of the other
 static_assert(kSoftmaxRegs + kOtherRegs <= 2 * kLaunchRegs, "the split fits what the block was launched with");
-template <int HD, int QT> constexpr int kQBufs = HD == 128 && QT == 1 ? 1 : 2;
-template <int HD, int QT> constexpr int kKSlots = HD == 128 ? QT : (QT == 1 ? 3 : 4);  // K tiles as operands
-template <int HD, int QT> constexpr int kVSlots = HD == 128 ? 2 : (QT == 1 ? 3 : 4);   // V tiles
-template <int HD, int QT> constexpr int kStaging = HD == 128 ? 2 : 3;                  // tiles of codes, of K and of V
+template <int HD> constexpr int kQBufs = HD == 128 ? 1 : 2;
+template <int HD> constexpr int kKSlots = HD == 128 ? 1 : 3;                                // K tiles as operands
+template <int HD> constexpr int kVSlots = HD == 128 ? 2 : 3;                                // V tiles
+template <int HD> constexpr int kStaging = HD == 128 ? 2 : 3;                               // tiles of codes, of K and of V
 template <int HD> constexpr uint32_t kCodeBytes = kKT * HD;
-template <int HD, int QT>
-constexpr uint32_t kSmem = kQBufs<HD, QT> * QT * kQBytes<HD> + (kKSlots<HD, QT> + kVSlots<HD, QT>) * kTileBytes<HD> + 2 * kStaging<HD, QT> * kCodeBytes<HD> + 1024;
-static_assert(2 * (kSmem<128, 1> + 1024) <= 228 * 1024 && 2 * (kSmem<64, 1> + 1024) <= 228 * 1024 && kSmem<128, 2> <= 227 * 1024 && kSmem<64, 2> <= 227 * 1024, "the CTAs share an SM");
+template <int HD>
+constexpr uint32_t kSmem = kQBufs<HD> * kQBytes<HD> + (kKSlots<HD> + kVSlots<HD>) * kTileBytes<HD> + 2 * kStaging<HD> * kCodeBytes<HD> + 1024;
+static_assert(2 * (kSmem<128> + 1024) <= 228 * 1024 && 2 * (kSmem<64> + 1024) <= 228 * 1024, "two CTAs share an SM");
 
 constexpr int kBlocks = kKT / kPagedBlock;   // of a tile
 constexpr int kAhead = 8;                    // a tile of K is converted less than that many tiles ahead of the softmax: kBufs - 1 scores, the slots of K
 
 struct alignas(16) SharedE4m3 {
     uint64_t q_full[2];                // an item's Q tiles landed in the buffer          (loader -> MMA)
-    uint64_t q_ready[2][2];            // Q tile g in the buffer is f16                   (softmax -> MMA, 4 arrivals)
+    uint64_t q_ready[2];               // the Q tile in the buffer is f16                 (softmax -> MMA, 4 arrivals)
     uint64_t st_full[2][3];            // a tile of codes of K, with all scales, / V landed (loader -> converters)
     uint64_t st_empty[2][3];           // the converters have read it                     (converters -> loader)
-    uint64_t k_full[4], v_full[4];     // K or V tile written, V looked at                (converters -> MMA; V -> softmax)
-    uint64_t k_empty[4], v_empty[4];   // the MMAs have read the slot                     (MMA -> converters, QT arrivals)
-    uint64_t s_full[2][3];             // S of Q tile g into buffer i has completed       (MMA -> softmax)
-    uint64_t p_full[2][3];             // P has taken its place                           (softmax -> MMA, 4 arrivals)
-    uint64_t pv_done[2][2];            // O += P V of an even / odd tile has completed    (MMA -> MMA, softmax)
-    uint64_t o_full[2];                // the item's last one has                         (MMA -> softmax)
-    uint64_t item_done[2];             // the Q buffer may be overwritten                 (softmax -> loader, 4 QT arrivals)
+    uint64_t k_full[3], v_full[3];     // K or V tile written, V looked at                (converters -> MMA; V -> softmax)
+    uint64_t k_empty[3], v_empty[3];   // the MMAs have read the slot                     (MMA -> converters)
+    uint64_t s_full[1][3];             // S into buffer i has completed       (MMA -> softmax)
+    uint64_t p_full[1][3];             // P has taken its place                           (softmax -> MMA, 4 arrivals)
+    uint64_t pv_done[1][2];            // O += P V of an even / odd tile has completed    (MMA -> MMA, softmax)
+    uint64_t o_full[1];                // the item's last one has                         (MMA -> softmax)
+    uint64_t item_done[2];             // the Q buffer may be overwritten                 (softmax -> loader, 4 arrivals)
     uint32_t tmem_base;
-    int abort, keep_o[2];
+    int abort, keep_o[1];
     float scale[3][2][kBlocks];        // of a staging tile's blocks of K, of V
     alignas(16) float scales[kAhead][3][kBlocks];   // of the tiles at work: K's scale, log2 of V's, 1 / V's (converter of K -> softmax)
     int wide[kAhead];                  // some log2 of V's scales is beyond +-40
-    int odd[4][2];                     // V in the slot has NaN where only some rows see it, by converter
+    int odd[3];                        // V in the slot has NaN where only some rows see it
 };
 static_assert(sizeof(SharedE4m3) <= 1024, "the barriers end inside the allocation");
 
-template <int HD_, int QT_>
+template <int HD_>
 struct TcE4m3 {
-    static constexpr int HD = HD_, QT = QT_, NQ = kQBufs<HD, QT>, KS = kKSlots<HD, QT>, VS = kVSlots<HD, QT>;
+    static constexpr int HD = HD_, QT = 1, NQ = kQBufs<HD>, KS = kKSlots<HD>, VS = kVSlots<HD>;
     static constexpr bool kCodes = true;
     using Shared = SharedE4m3;
-    static __device__ __forceinline__ uint64_t* q_ready(Shared* sh, int g) { return sh->q_ready[g]; }
+    static __device__ __forceinline__ uint64_t* q_ready(Shared* sh, int) { return sh->q_ready; }
     // The thread's row of the item's Q tile as f16 in 1 .. 2: what its scores are multiplied by.
     template <int ROWS, class Wait>
-    static __device__ __forceinline__ float own_q(Shared* sh, uint8_t* sQ, uint32_t item, int g, int r, bool& ok, Wait& wait) {
-        const uint32_t buf = item % NQ, row = smem_u32(sQ) + (buf * QT + g) * kQBytes<HD> + r * 128;
+    static __device__ __forceinline__ float own_q(Shared* sh, uint8_t* sQ, uint32_t item, int r, bool& ok, Wait& wait) {
+        const uint32_t buf = item % NQ, row = smem_u32(sQ) + buf * kQBytes<HD> + r * 128;
         ok = __all_sync(0xffffffffu, wait(&sh->q_full[buf], (item / NQ) & 1u)) && ok;
         auto at = [&](int c) { return row + (c >> 3) * (ROWS * 128) + (((c & 7) ^ (r & 7)) << 4); };
         uint32_t x[HD / 8][4], top = 0;
@@ -91,7 +95,7 @@ struct TcE4m3 {
         }
         proxy_fence();
         __syncwarp();
-        if ((threadIdx.x & 31) == 0) mbar_arrive(&sh->q_ready[g][buf]);
+        if ((threadIdx.x & 31) == 0) mbar_arrive(&sh->q_ready[buf]);
         return exp2_int(ex);
     }
     // The scales of tile n's blocks; whether V's are wide.
@@ -105,35 +109,30 @@ struct TcE4m3 {
     }
     // V of the slot has been looked at; it has NaN where only some rows see it; whether this is one (0: it is not)
     static __device__ __forceinline__ uint64_t* v_seen(Shared* sh, uint32_t slot) { return &sh->v_full[slot]; }
-    static __device__ __forceinline__ bool odd(Shared* sh, uint32_t slot) {
-        int any = 0;
-#pragma unroll
-        for (int i = 0; i < kConvWarps<QT>; ++i) any |= *const_cast<volatile int*>(&sh->odd[slot][i]);
-        return any != 0;
-    }
+    static __device__ __forceinline__ bool odd(Shared* sh, uint32_t slot) { return *const_cast<volatile int*>(&sh->odd[slot]) != 0; }
     static __device__ __forceinline__ float odd_value(const PagedAttnArgs& a, int row, int d) {
         const unsigned char code = reinterpret_cast<const unsigned char*>(a.pool)[static_cast<size_t>(row) * HD + d];
         return (code & 0x7f) == 0x7f ? __uint_as_float(0x7fffffffu) : 0.f;
     }
 };
 
-template <int HD, int QT>
-__global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
+template <int HD>
+__global__ void __launch_bounds__(kThreads, 2)
     paged_e4m3_attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_codes,
                                    const __grid_constant__ CUtensorMap tm_out, const PagedAttnArgs a) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
-    using T = TcE4m3<HD, QT>;
-    constexpr int NQ = T::NQ, KS = T::KS, VS = T::VS, ST = kStaging<HD, QT>, CW = kConvWarps<QT>, kFirst = kBufs<HD> - 1, kAtoms = HD / 64;
+    using T = TcE4m3<HD>;
+    constexpr int NQ = T::NQ, KS = T::KS, VS = T::VS, ST = kStaging<HD>, kFirst = kBufs<HD> - 1, kAtoms = HD / 64;
     constexpr uint32_t kT = kTileBytes<HD>, kC = kCodeBytes<HD>;
-    constexpr int kSoftmaxWarps = 4 * QT, kLoader = kSoftmaxWarps + QT, kConv = kThreads<QT> / 32 - 2 * CW;
-    uint8_t* sQ = smem_raw;                                  // [buffer][Q tile]
-    uint8_t* sK = sQ + NQ * QT * kQBytes<HD>;
+    constexpr int kSoftmaxWarps = 4, kLoader = 5, kConvK = 6;
+    uint8_t* sQ = smem_raw;
+    uint8_t* sK = sQ + NQ * kQBytes<HD>;
     uint8_t* sV = sK + KS * kT;
     uint8_t* sC = sV + VS * kT;                              // [K, V][tile]
     SharedE4m3* sh = reinterpret_cast<SharedE4m3*>(sC + 2 * ST * kC);
     static_assert(VS >= kBufs<HD>, "the tile before in a slot of V has been multiplied when the softmax asks for this one");
     static_assert(kBufs<HD> - 1 + KS < kAhead, "a tile's scales stay until the softmax has read them");
-    static_assert(KS <= 4 && VS <= 4 && ST <= 3 && kBufs<HD> * kKT + HD <= static_cast<int>(kCols) && 4 * kPatch <= kQBytes<HD>, "rings, TMEM columns, patches");
+    static_assert(KS <= 3 && VS <= 3 && ST <= 3 && kBufs<HD> * kKT + HD <= static_cast<int>(kCols) && 4 * kPatch <= kQBytes<HD>, "rings, TMEM columns, patches");
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     volatile int* cta_abort = &sh->abort;
 
@@ -151,30 +150,28 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
         }
         for (int i = 0; i < 2 * ST; ++i) {
             mbar_init(&sh->st_full[i & 1][i >> 1], i & 1 ? 1 : 1 + 2 * kBlocks);   // the tile, and the lanes that copy scales
-            mbar_init(&sh->st_empty[i & 1][i >> 1], CW);
+            mbar_init(&sh->st_empty[i & 1][i >> 1], 1);
         }
         for (int i = 0; i < KS; ++i) {
-            mbar_init(&sh->k_full[i], CW);
-            mbar_init(&sh->k_empty[i], QT);
+            mbar_init(&sh->k_full[i], 1);
+            mbar_init(&sh->k_empty[i], 1);
         }
         for (int i = 0; i < VS; ++i) {
-            mbar_init(&sh->v_full[i], CW);
-            mbar_init(&sh->v_empty[i], QT);
+            mbar_init(&sh->v_full[i], 1);
+            mbar_init(&sh->v_empty[i], 1);
         }
-        for (int g = 0; g < QT; ++g) {
-            for (int b = 0; b < kBufs<HD>; ++b) {
-                mbar_init(&sh->s_full[g][b], 1);
-                mbar_init(&sh->p_full[g][b], 4);
-            }
-            for (int i = 0; i < 2; ++i) mbar_init(&sh->pv_done[g][i], 1);
-            mbar_init(&sh->o_full[g], 1);
-            for (int i = 0; i < NQ; ++i) mbar_init(&sh->q_ready[g][i], 4);
-            sh->keep_o[g] = 0;
+        for (int b = 0; b < kBufs<HD>; ++b) {
+            mbar_init(&sh->s_full[0][b], 1);
+            mbar_init(&sh->p_full[0][b], 4);
         }
+        for (int i = 0; i < 2; ++i) mbar_init(&sh->pv_done[0][i], 1);
+        mbar_init(&sh->o_full[0], 1);
+        for (int i = 0; i < NQ; ++i) mbar_init(&sh->q_ready[i], 4);
+        sh->keep_o[0] = 0;
         sh->abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == kSoftmaxWarps) paged_tc_alloc(&sh->tmem_base, QT * kCols);
+    if (warp == kSoftmaxWarps) paged_tc_alloc(&sh->tmem_base, kCols);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -182,8 +179,8 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
     pdl_wait();
 
     PagedStart start;
-    static_assert(sizeof(PagedScratch) <= kSmem<64, 1> - 1024, "the scratch fits the tiles");
-    const bool any = paged_find_start<kThreads<QT>, kKT, kItem, false>(a, *reinterpret_cast<PagedScratch*>(sQ), 1, kItem + 2, 0, start);
+    static_assert(sizeof(PagedScratch) <= kSmem<64> - 1024, "the scratch fits the tiles");
+    const bool any = paged_find_start<kThreads, kKT, kItem, false>(a, *reinterpret_cast<PagedScratch*>(sQ), 1, kItem + 2, 0, start);
     proxy_fence();                                          // the scratch's writes before the copies that take its place
     __syncthreads();
 
@@ -217,8 +214,8 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         if (warp < kLoader) {
             paged_tc_mma<T>(a, start, sh, sQ, sK, sV, tmem, warp - kSoftmaxWarps);
-        } else if (warp < kLoader + QT) {
-            // ================= loader, or (two Q tiles) one of K and Q and one of V: codes and scales; Q before its item's first tile or (one Q buffer) where the item in front has ended
+        } else if (warp == kLoader) {
+            // ================= loader: codes and scales; Q before its item's first tile or (one Q buffer) where the item in front has ended
             const int box_shift = min(a.page_shift, 6), box = 1 << box_shift;
             bool ok = true;
             Tiles k(a, start), v(a, start);
@@ -259,33 +256,19 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                 const uint32_t buf = nq % NQ;
                 if (nq >= NQ) ok = ok && all_wait(&sh->item_done[buf], (nq / NQ - 1) & 1u);
                 if (!ok) return;
-                const uint32_t dst = __shfl_sync(0xffffffffu, smem_u32(sQ) + buf * QT * kQBytes<HD>, 0);
-                const int row = wq.q.row0 + wq.rt * QT * a.tile_tokens;
+                const uint32_t dst = __shfl_sync(0xffffffffu, smem_u32(sQ) + buf * kQBytes<HD>, 0);
+                const int row = wq.q.row0 + wq.rt * a.tile_tokens;
                 if (paged_elect()) {
-                    mbar_expect_tx(&sh->q_full[buf], QT * kAtoms * static_cast<uint32_t>(a.tile_tokens) * a.G * 128);
+                    mbar_expect_tx(&sh->q_full[buf], kAtoms * static_cast<uint32_t>(a.tile_tokens) * a.G * 128);
 #pragma unroll
-                    for (int g = 0; g < QT; ++g)
-#pragma unroll
-                        for (int at = 0; at < kAtoms; ++at)
-                            tma_box_3d(dst + g * kQBytes<HD> + at * kTQ * 128, &tm_q, &sh->q_full[buf], 64 * at, wq.head * a.G, row + g * a.tile_tokens);
+                    for (int at = 0; at < kAtoms; ++at) tma_box_3d(dst + at * kTQ * 128, &tm_q, &sh->q_full[buf], 64 * at, wq.head * a.G, row);
                 }
                 __syncwarp();
                 ++nq;
                 have_q = wq.next();
             };
-            if (QT == 2) {
-                static_assert(QT == 1 || NQ == 2, "K waits for its item's Q buffer, V does not");
-                if (warp == kLoader)
-                    while (ok && k.have) {
-                        if (k.t == k.w.t0) next_q();
-                        load(k, k_pages, std::false_type());
-                    }
-                else
-                    while (ok && v.have) load(v, v_pages, std::true_type());
-                k.have = v.have = false;
-            }
             for (int i = 0; i < kFirst; ++i) load(k, k_pages, std::false_type());
-            if (QT == 1 && NQ == 2) next_q();
+            if (NQ == 2) next_q();
             while (ok && v.have) {
                 if (NQ == 1 && v.t == v.w.t0) next_q();
                 // behind the item's third tile: the epilogue in front of it, which frees the buffer, is on its way by then
@@ -305,20 +288,20 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                 land(sh->st_full[0], k.n, ST);
                 land(sh->st_full[1], v.n, ST);
             }
-        } else if (warp >= kConv) {
-            // ================= converters of K, then of V: each the same keys of every tile =================
-            constexpr int kKeys = kKT / CW, kPieces = HD / 16, kAtOnce = 32 / kPieces, kSteps = kPagedBlock / kAtOnce;   // keys of a warp, of a step; steps of a block
-            // Of eight lanes at a time, which a store of 16 bytes takes together, four have neighbouring pieces of one key and four those of the
-            // next: all banks, by the swizzle.
-            const int cw = (warp - kConv) % CW, piece = HD == 128 ? (lane & 3) + (lane >> 3 & 1) * 4 : lane & 3, atom = piece >> 2;
-            const int mine = HD == 128 ? (lane >> 2 & 1) + (lane >> 4) * 2 : lane >> 2;          // of a step's keys
+        } else {
+            // ================= converters of K and of V =================
+            constexpr int kPieces = HD / 16, kSteps = kKT * kPieces / 32;
+            // Of eight lanes at a time, which 16 bytes a lane take together, four have neighbouring pieces of key k and four those of key k ^ 5 (head
+            // dim 64: k ^ 1): by the swizzles their loads and their stores meet all banks.  Steps 0 and 1 take four each of eight keys.
+            const int piece = HD == 128 ? (lane & 3) + (lane >> 3 & 1) * 4 : lane & 3, atom = piece >> 2;
+            auto key_of = [&](int step) { return HD == 128 ? (step >> 1) * 8 + (((lane >> 4) + 2 * (step & 1)) ^ (5 * (lane >> 2 & 1))) : step * 8 + (lane >> 2); };
             auto convert = [&](uint8_t* tiles, uint64_t* full, uint64_t* empty, auto is_v) {
                 constexpr int V = decltype(is_v)::value, SL = V ? VS : KS;
                 Tiles x(a, start);
                 uint32_t slot = 0, empty_ph = 1;
                 while (x.have) {
                     const int k0 = x.w.k.tile(x.t) << 6;
-                    const bool care = V && !SeenByAll(a, x.w.q, x.w.rt * QT * a.tile_tokens, QT * a.tile_tokens).tile(a, k0);
+                    const bool care = V && !SeenByAll(a, x.w.q, x.w.rt * a.tile_tokens, a.tile_tokens).tile(a, k0);
                     bool ok = all_wait(&sh->st_full[V][x.slot], x.ph);
                     if (ok && x.n >= static_cast<uint32_t>(SL)) ok = all_wait(&empty[slot], empty_ph);
                     if (!ok) break;
@@ -327,7 +310,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                         return HD == 128 ? from + key * 128 + ((piece ^ (key & 7)) << 4) : from + key * 64 + ((piece ^ (key >> 1 & 3)) << 4);
                     };
                     auto hidden = [&](int key) { return care && (k0 + key >= x.w.k.hi || (k0 + key < x.w.k.lo && k0 + key >= a.sinks)); };
-                    if (!V && cw == 0) {                      // the tile's scales to the softmax warps
+                    if (!V) {                      // the tile's scales to the softmax warps
                         const int first = k0 + (lane & (kBlocks - 1)) * kPagedBlock;
                         const bool unseen = first >= x.w.k.hi || (first + kPagedBlock <= x.w.k.lo && first >= a.sinks);   // by all rows of the item
                         const int e = unseen ? 0 : e4m3_exponent((&sh->scale[x.slot][0][0])[lane & (2 * kBlocks - 1)]);
@@ -341,37 +324,29 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                         if (lane == 0) sh->wide[x.n % kAhead] = wide;
                     }
                     bool nan = false;
+                    // few instructions, in a loop that is not unrolled far: what the softmax warps beside it run has to stay in the instruction cache
 #pragma unroll 1
-                    for (int key0 = cw * kKeys + mine; key0 < (cw + 1) * kKeys; key0 += kPagedBlock) {
-                        uint32_t w[kSteps][4];
-#pragma unroll
-                        for (int i = 0; i < kSteps; ++i)
-                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                         : "=r"(w[i][0]), "=r"(w[i][1]), "=r"(w[i][2]), "=r"(w[i][3]) : "r"(code_at(key0 + i * kAtOnce)) : "memory");
+                    for (int step = 0; step < kSteps; ++step) {
+                        const int key = key_of(step);
+                        uint32_t w[4];
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(code_at(key)) : "memory");
                         if (care) {
+                            const bool out = hidden(key);
 #pragma unroll
-                            for (int i = 0; i < kSteps; ++i)
-#pragma unroll
-                                for (int j = 0; j < 4; ++j) {
-                                    if (hidden(key0 + i * kAtOnce)) w[i][j] = 0u;
-                                    if (odd_codes(w[i][j])) {         // rare: the softmax warps give it to the rows that see it
-                                        nan = true;
-                                        w[i][j] = without_nan(w[i][j]);
-                                    }
-                                }
+                            for (int j = 0; j < 4; ++j) {
+                                if (out) w[j] = 0u;
+                                nan = nan || odd_codes(w[j]);             // rare: the softmax warps give it to the rows that see it
+                                w[j] = without_nan(w[j]);
+                            }
                         }
 #pragma unroll
-                        for (int i = 0; i < kSteps; ++i) {
-                            const int key = key0 + i * kAtOnce;
-#pragma unroll
-                            for (int h = 0; h < 2; ++h)
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + key * 128 + ((((piece & 3) * 2 + h) ^ (key & 7)) << 4)),
-                                             "r"(low_codes(w[i][2 * h])), "r"(high_codes(w[i][2 * h])), "r"(low_codes(w[i][2 * h + 1])), "r"(high_codes(w[i][2 * h + 1]))
-                                             : "memory");
-                        }
+                        for (int h = 0; h < 2; ++h)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + key * 128 + ((((piece & 3) * 2 + h) ^ (key & 7)) << 4)),
+                                         "r"(low_codes(w[2 * h])), "r"(high_codes(w[2 * h])), "r"(low_codes(w[2 * h + 1])), "r"(high_codes(w[2 * h + 1]))
+                                         : "memory");
                     }
                     nan = __any_sync(0xffffffffu, nan);
-                    if (care && lane == 0) *const_cast<volatile int*>(&sh->odd[slot][cw]) = nan;
+                    if (care && lane == 0) *const_cast<volatile int*>(&sh->odd[slot]) = nan;
                     proxy_fence();
                     __syncwarp();
                     if (lane == 0) {
@@ -383,7 +358,7 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
                     x.next();
                 }
             };
-            if (warp < kConv + CW) convert(sK, sh->k_full, sh->k_empty, std::false_type());
+            if (warp == kConvK) convert(sK, sh->k_full, sh->k_empty, std::false_type());
             else convert(sV, sh->v_full, sh->v_empty, std::true_type());
         }
     }
@@ -392,37 +367,36 @@ __global__ void __launch_bounds__(kThreads<QT>, QT == 1 ? 2 : 1)
     if (warp == kSoftmaxWarps) {
         __syncwarp();
         tc_fence_after();
-        tmem_free(tmem, QT * kCols);
+        tmem_free(tmem, kCols);
     }
 }
 
-template <int HD, int QT>
+template <int HD>
 cudaError_t launch(const PagedAttnArgs& a, const CUtensorMap& tm_q, const CUtensorMap& tm_out, const CUtensorMap& map, cudaStream_t st) {
     static std::atomic<unsigned long long> attr_done{0};
-    cudaError_t e = set_smem_limit_once(attr_done, paged_e4m3_attention_tc_kernel<HD, QT>, static_cast<int>(kSmem<HD, QT>));
+    cudaError_t e = set_smem_limit_once(attr_done, paged_e4m3_attention_tc_kernel<HD>, static_cast<int>(kSmem<HD>));
     if (e != cudaSuccess) return e;
     static std::atomic<int> regs{0};
     if (regs.load(std::memory_order_relaxed) != kLaunchRegs) {   // with fewer the softmax warps would wait for the others' without end
         cudaFuncAttributes f;
-        e = cudaFuncGetAttributes(&f, paged_e4m3_attention_tc_kernel<HD, QT>);
+        e = cudaFuncGetAttributes(&f, paged_e4m3_attention_tc_kernel<HD>);
         if (e != cudaSuccess) return e;
         if (f.numRegs != kLaunchRegs) return cudaErrorInvalidConfiguration;
         regs.store(f.numRegs, std::memory_order_relaxed);
     }
     const dim3 grid(a.at_once);
-    e = launch_kernel(paged_e4m3_attention_tc_kernel<HD, QT>, grid, dim3(kThreads<QT>), kSmem<HD, QT>, st, tm_q, map, tm_out, a);
+    e = launch_kernel(paged_e4m3_attention_tc_kernel<HD>, grid, dim3(kThreads), kSmem<HD>, st, tm_q, map, tm_out, a);
     if (e != cudaSuccess) return e;
-    return launch_kernel(paged_merge_kernel<HD>, dim3(grid.x, QT * HD / kMergeDims), dim3(kTQ), 0, st, a);
+    return launch_kernel(paged_merge_kernel<HD>, dim3(grid.x, HD / kMergeDims), dim3(kTQ), 0, st, a);
 }
 
 }  // namespace
 
-cudaError_t launch_paged_e4m3_attention_tc(PagedAttnArgs a, const CUtensorMap& map, int hd, int q_tiles, int sms, cudaStream_t st) {
+cudaError_t launch_paged_e4m3_attention_tc(PagedAttnArgs a, const CUtensorMap& map, int hd, int sms, cudaStream_t st) {
     CUtensorMap tm_q, tm_out;
-    const cudaError_t e = paged_tc_args(a, hd, q_tiles, sms, &tm_q, &tm_out);
+    const cudaError_t e = paged_tc_args(a, hd, 1, sms, &tm_q, &tm_out);
     if (e != cudaSuccess) return e;
-    if (q_tiles == 1) return hd == 128 ? launch<128, 1>(a, tm_q, tm_out, map, st) : launch<64, 1>(a, tm_q, tm_out, map, st);
-    return hd == 128 ? launch<128, 2>(a, tm_q, tm_out, map, st) : launch<64, 2>(a, tm_q, tm_out, map, st);
+    return hd == 128 ? launch<128>(a, tm_q, tm_out, map, st) : launch<64>(a, tm_q, tm_out, map, st);
 }
 
 }  // namespace odb

@@ -11,6 +11,19 @@ namespace {
 
 constexpr int kThreads = 256, kAtOnce = 4;
 
+// 16 codes as bf16
+__device__ __forceinline__ void expand16(const uint4& codes, float scale, uint4 (&y)[2]) {
+    const uint32_t c[4] = {codes.x, codes.y, codes.z, codes.w};
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float2 f = f32x2_of(static_cast<unsigned short>(c[i / 2] >> 16 * (i & 1)));
+        w[i] = paged_bf16x2(f.x * scale, f.y * scale);
+    }
+    y[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    y[1] = make_uint4(w[4], w[5], w[6], w[7]);
+}
+
 template <int HD, bool E4M3>
 __global__ void __launch_bounds__(kThreads) paged_load_kernel(const PagedLoadArgs p, const PagedDiv by_row) {
     constexpr int kPieces = HD / 16;                            // of a head
@@ -43,21 +56,43 @@ __global__ void __launch_bounds__(kThreads) paged_load_kernel(const PagedLoadArg
             if (!out[k]) continue;
             uint4 y[2];
             if constexpr (E4M3) {
-                const uint32_t c[4] = {v[k][0].x, v[k][0].y, v[k][0].z, v[k][0].w};
-                uint32_t w[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float2 f = f32x2_of(static_cast<unsigned short>(c[i / 2] >> 16 * (i & 1)));
-                    w[i] = paged_bf16x2(f.x * scale[k], f.y * scale[k]);
-                }
-                y[0] = make_uint4(w[0], w[1], w[2], w[3]);
-                y[1] = make_uint4(w[4], w[5], w[6], w[7]);
+                expand16(v[k][0], scale[k], y);
             } else {
                 y[0] = v[k][0];
                 y[1] = v[k][1];
             }
             reinterpret_cast<uint4*>(out[k])[0] = y[0];
             reinterpret_cast<uint4*>(out[k])[1] = y[1];
+        }
+    }
+}
+
+// The pages that the attention's rows see, one head of K or V a block at a time, from their codes into the same places of a pool of one layer
+// in bf16, which the attention's kernel for pools of bf16 then reads: for prompts, whose row tiles would otherwise each turn the same codes
+// into operands.
+template <int HD>
+__global__ void __launch_bounds__(kThreads) paged_expand_kernel(const PagedAttnArgs a, __nv_bfloat16* __restrict__ layer, const int layer_rows) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int s = blockIdx.y, head = blockIdx.z % a.KV;
+    const bool is_v = static_cast<int>(blockIdx.z) >= a.KV;
+    const PagedSeq q = paged_seq(a, s);
+    if (q.n == 0) return;
+    const long long top = min(static_cast<long long>(q.len), static_cast<long long>(q.first) + q.n + a.right), low = static_cast<long long>(q.first) - a.left;
+    for (long long p = blockIdx.x; p << a.page_shift < top; p += gridDim.x) {
+        const long long from = p << a.page_shift;
+        if (from + (1 << a.page_shift) <= low && from >= a.sinks) continue;
+        const int page = a.table[static_cast<size_t>(s) * a.table_stride + p];
+        if (page < 0 || page >= a.n_pages) continue;
+        const size_t row = static_cast<size_t>(page * a.KV + head) << a.page_shift, at = row + (is_v ? a.v_row0 : a.k_row0);
+        const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const unsigned char*>(a.pool) + at * HD);
+        const float* scale = a.scales + at / kPagedBlock;
+        uint4* dst = reinterpret_cast<uint4*>(layer + (row + (is_v ? layer_rows : 0)) * HD);
+        for (int i = threadIdx.x; i < (HD / 16) << a.page_shift; i += kThreads) {
+            uint4 y[2];
+            expand16(__ldg(src + i), __ldg(scale + i / HD), y);       // 16 positions of HD / 16 pieces each have a scale
+            dst[2 * i] = y[0];
+            dst[2 * i + 1] = y[1];
         }
     }
 }
@@ -74,6 +109,14 @@ cudaError_t launch(PagedLoadArgs a, cudaStream_t st) {
 cudaError_t launch_paged_load(PagedLoadArgs a, cudaStream_t st) {
     if (a.k_scales) return a.HD == 128 ? launch<128, true>(a, st) : launch<64, true>(a, st);
     return a.HD == 128 ? launch<128, false>(a, st) : launch<64, false>(a, st);
+}
+
+cudaError_t launch_paged_expand(const PagedAttnArgs& a, __nv_bfloat16* layer, int layer_rows, int hd, cudaStream_t st) {
+    // some 4096 blocks, whatever the requests
+    const long long others = static_cast<long long>(a.n_seqs) * 2 * a.KV, stripes = (4096 + others - 1) / others;
+    const dim3 grid(static_cast<unsigned>(stripes < a.table_stride ? stripes : a.table_stride), a.n_seqs, 2 * a.KV);
+    return hd == 128 ? launch_kernel(paged_expand_kernel<128>, grid, dim3(kThreads), 0, st, a, layer, layer_rows)
+                     : launch_kernel(paged_expand_kernel<64>, grid, dim3(kThreads), 0, st, a, layer, layer_rows);
 }
 
 }  // namespace odb

@@ -136,10 +136,11 @@ class PagedCache(_OnStream):
     torch.float8_e4m3fn, in half the memory: codes of 8 bits with a scale, a power of two, for each block of 16 positions of a head (float32
     [n_layers][2][n_pages][n_kv_heads][page_size / 16]; K or V of a position is code * scale), which norm_rope_store writes and load and
     attention read.  kv, and scales beside it: tensors of that shape to use; otherwise they are allocated (not cleared: what no request has
-    written reaches no result)."""
+    written reaches no result).  room: over codes, whether the workspace has room for the K and V of one layer in bf16, with which the
+    attention of prompts takes half the time (a layer in bf16 is as large as two of codes: of little account with many layers)."""
 
     def __init__(self, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, *, dtype=None, kv=None,
-                 scales=None, device=None):
+                 scales=None, room: bool = True, device=None):
         lib = B.lib()
         self.cfg = B.odb_paged_config(n_layers, n_heads, n_kv_heads, head_dim, page_size, n_pages)
         self.n_layers, self.n_heads, self.n_kv_heads, self.head_dim, self.page_size, self.n_pages = \
@@ -166,7 +167,8 @@ class PagedCache(_OnStream):
         elif tuple(scales.shape) != shape or scales.dtype != _F32 or scales.device != self.device or not scales.is_contiguous():
             raise ValueError(f"scales: a contiguous float32 tensor of shape {shape} on {self.device} is wanted")
         self.scales = scales
-        self.workspace = torch.empty(lib.odb_paged_workspace_bytes(C.byref(self.cfg)), dtype=torch.uint8, device=self.device)
+        size = lib.odb_paged_workspace_bytes(C.byref(self.cfg)) + (lib.odb_paged_e4m3_layer_bytes(C.byref(self.cfg)) if room and scales is not None else 0)
+        self.workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
         self._index = self.device.index
         self._made(self._index, (self.workspace, kv, scales))
         rest = (self.workspace.data_ptr(), self.workspace.numel(), C.c_void_p(self._raw), C.byref(self.handle))

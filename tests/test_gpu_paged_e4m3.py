@@ -7,7 +7,7 @@ Bounds, derived before the first run.
   the oracle's, under the exponent that the block got.
   load: exact.
   attention, over the values that the codes stand for: the output's rounding to bf16, 2^-8 of its value (half a step is 2^-9; the double is
-  kept for the sums in front of it); a weight's rounding to f16, 2^-11 of itself (2^-8 is allowed, as for the pool of bf16), and no less
+  kept for the sums in front of it); a weight's rounding, 2^-8 (bf16, over a copy) or 2^-11 (f16) of itself, and in f16 no less
   than 2^-24 of the row's largest product of weight and scale (half a step of 2^-24 where that is rounded up to a power of two): at most
   the weight itself; a score's fp32 sum of head_dim exact products, head_dim 2^-24 sum|q k|
   scale, and Q in f16 under a power of two, 2^-25 of its largest value per dim: together d, which moves numerator and denominator by a
@@ -50,8 +50,8 @@ def random_pool(rng, layers, n_pages, KV, page, D, low=-3, high=4, poison=False)
     return torch.from_numpy(c), torch.from_numpy(s.astype(np.float32))
 
 
-def make(layers, H, KV, D, page, n_pages, pool):
-    return paged().PagedCache(layers, H, KV, D, page, n_pages, kv=pool[0].cuda().view(E4M3), scales=pool[1].cuda())
+def make(layers, H, KV, D, page, n_pages, pool, room=True):
+    return paged().PagedCache(layers, H, KV, D, page, n_pages, kv=pool[0].cuda().view(E4M3), scales=pool[1].cuda(), room=room)
 
 
 # ---- store ------------------------------------------------------------------------------------------------------------
@@ -352,9 +352,10 @@ def test_load_of_every_code_under_every_scale():
 
 # ---- attention --------------------------------------------------------------------------------------------------------
 
-@pytest.fixture(params=["narrow", "wide"])
+# As for the pool of bf16, the table's width picks the kernel; in a wide one prompts are read from a copy in bf16 where there is room for it.
+@pytest.fixture(params=["narrow", "wide", "wide without room"])
 def columns(request):
-    return {"narrow": 1, "wide": 5000}[request.param]
+    return {"narrow": 1, "wide": 5000, "wide without room": -5000}[request.param]
 
 
 def setup(rng, lens, counts, firsts, H, KV, D, page, layers=1, layer=0, scale=1.0, spare=2, columns=1, spread=2, hidden=None):
@@ -366,7 +367,7 @@ def setup(rng, lens, counts, firsts, H, KV, D, page, layers=1, layer=0, scale=1.
     codes, scales = random_pool(rng, layers, n_pages, KV, page, D, poison=True)
     codes, scales = codes.numpy(), scales.numpy()
     order = rng.permutation(n_pages)
-    width = max(held + [1]) + columns
+    width = max(held + [1]) + abs(columns)
     table = np.full((len(lens), width), 10 ** 6, np.int32)
     keys, values, vscale = [], [], []
     at = 0
@@ -395,7 +396,7 @@ def setup(rng, lens, counts, firsts, H, KV, D, page, layers=1, layer=0, scale=1.
     rows = sum(counts)
     q, qf = bf16(rng, rows, H, D, scale=scale)
     start = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
-    cache = make(layers, H, KV, D, page, n_pages, (torch.from_numpy(codes), torch.from_numpy(scales)))
+    cache = make(layers, H, KV, D, page, n_pages, (torch.from_numpy(codes), torch.from_numpy(scales)), room=columns > 0)
     batch = P.Batch(cache, table=dev(table), len_after=i32(lens), first=i32(firsts), row_start=dev(start), max_rows=rows, max_new=max(counts))
     return cache, batch, q.cuda(), qf, keys, values, vscale, start
 
