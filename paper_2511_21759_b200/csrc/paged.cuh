@@ -46,7 +46,7 @@ struct PagedE4m3StoreArgs {
     const int32_t *row_seq, *len;
     unsigned char *k_pool, *v_pool;                       // this layer's
     float *k_scales, *v_scales;
-    int KV, n_seqs, window;                               // window: rows in which a warp looks for the beginnings of blocks, 1 or 16
+    int KV, n_seqs, window, heads;                        // window: rows in which a warp looks for the beginnings of blocks, 1 or 16; heads: of a unit
 };
 cudaError_t launch_paged_e4m3_store(const PagedE4m3StoreArgs& a, cudaStream_t st);
 

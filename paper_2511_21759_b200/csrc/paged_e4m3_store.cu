@@ -10,10 +10,16 @@
 // nothing but for the few values below 2^-6 of it; and what a code stands for is a number of bf16, kept codes of 2^-6 and more change
 // their exponent without a rounding, and x * 2^-e has none.
 //
-// A warp takes a block and one head of K or of V: HD / 8 threads a row, each the places that the store of bf16 gives it, all 16 rows'
-// loads in flight before the largest value is known.  Blocks begin where a row's request or block differs from the row's before it: a warp
-// looks for them among `window` rows (16 where requests have that many on average, otherwise 1), with all their maps in one load.
-// Units of q as in the store of bf16.
+// Four warps take a block of K or of V, four rows each, HD / 8 threads a row, each the places that the
+// store of bf16 gives it, and `heads` heads one after the other, the next one's rows in flight while the one before is turned: the block's
+// sines, its table and its slots are found once.  Blocks begin where a row's request or block differs from the row's before it: every warp
+// looks for them among `window` rows, with all their maps in one load.  Units of q as in the store of bf16, behind the blocks.
+//
+// What bounds it: the rows of a refresh of 4 requests x 4096 positions, 32 + 8 heads of 128, are 302 MB in and 168 MB out with q, 72 us at
+// the copy rate; it takes 111 us, 63 of them for q and 48 for K and V (75 with a warp to a block and head).  A thread holds two rows' values,
+// angles and loads in flight: the registers limit the warps of an SM, and seven CTAs of four (72 registers; up to 20 bytes spilled in some
+// forms) take 111 us where six (80, none spilled) take 121, at 16 x 32 rows 11.1 and 11.2.  48 tokens take 4.3 us in a graph, a
+// launch and three dependent reads (map, table, row).
 #include "paged_rows.cuh"
 
 #include "paged_e4m3.cuh"
@@ -22,7 +28,8 @@ namespace odb {
 
 namespace {
 
-constexpr int kThreads = 64;
+constexpr int kWarps = 4;                                     // of a block of positions
+constexpr int kThreads = 32 * kWarps;
 
 // codes of four values; those that are not finite become NaN
 __device__ __forceinline__ uint32_t codes4(f2 u, f2 v, f2 by) {
@@ -35,15 +42,16 @@ __device__ __forceinline__ float finite_max(float top, f2 x) {
     return fmaxf(top, fmaxf(fabsf(y.x), fabsf(y.y)));
 }
 
-template <int HD, bool INTER, bool ALL>
-__device__ __forceinline__ void block_unit(const PagedE4m3StoreArgs& p, int unit) {
-    constexpr int kLanes = HD / 8, kAtOnce = 32 / kLanes, kSteps = kPagedBlock / kAtOnce;
+// V: the blocks are of V
+template <int HD, bool INTER, bool ALL, bool V>
+__device__ __forceinline__ void block_unit(const PagedE4m3StoreArgs& p, int w, int head0) {
+    constexpr int kLanes = HD / 8, kAtOnce = kThreads / kLanes, kSteps = kPagedBlock / kAtOnce;
     constexpr unsigned kFull = 0xffffffffu;
     const PagedStoreArgs& rows = p.rows;
-    const int lane = threadIdx.x & 31, l = lane % kLanes, sub = lane / kLanes;
-    const int w = unit / (2 * p.KV), part = unit - w * 2 * p.KV;
-    const bool is_v = part >= p.KV;
-    const int head = is_v ? part - p.KV : part;
+    const int lane = threadIdx.x & 31, l = lane % kLanes, sub = threadIdx.x / kLanes;
+    __shared__ float tops[2][kWarps];
+    int turn = 0;
+    const int heads = min(p.heads, p.KV - head0);
     // lane i: row r0 + i, the one in front of the window first
     const int r0 = w * p.window - 1;
     int seq = -1, pos = -1, slot = -1;
@@ -57,14 +65,16 @@ __device__ __forceinline__ void block_unit(const PagedE4m3StoreArgs& p, int unit
     const int seq_before = __shfl_up_sync(kFull, seq, 1), mine_before = __shfl_up_sync(kFull, mine, 1);
     const unsigned same = __ballot_sync(kFull, lane > 0 && known && mine == mine_before && seq == seq_before);
     unsigned begins = __ballot_sync(kFull, known && lane > 0 && lane <= p.window) & ~same;
-    const int within = pos % kPagedBlock;
-    const bool has_slot = known && slot >= 0 && slot >> rows.page_shift < rows.n_pages && slot % kPagedBlock == within;
+    const int to_end = known ? min(max(p.len[seq], 0), 0x7fffffff - kPagedBlock) - (pos & ~(kPagedBlock - 1)) : 0;   // what the request has from the block's first position on
+    // the slot of the block's first position, -1 where the row has none
+    const int first = known && slot >= 0 && slot >> rows.page_shift < rows.n_pages && !((slot ^ pos) % kPagedBlock) ? slot & ~(kPagedBlock - 1) : -1;
 
-    const bool turned = !is_v && (ALL || l < rows.rot / 8);
-    const int ca = is_v || (turned && !INTER) ? 4 * l : 8 * l,
-              cb = is_v ? HD / 2 + 4 * l : turned && !INTER ? (ALL ? HD : rows.rot) / 2 + 4 * l : 8 * l + 4;
+    const bool turned = !V && (ALL || l < rows.rot / 8);
+    const int ca = V || (turned && !INTER) ? 4 * l : 8 * l,
+              cb = V ? HD / 2 + 4 * l : turned && !INTER ? (ALL ? HD : rows.rot) / 2 + 4 * l : 8 * l + 4;
     StoreTurn<INTER> t;
-    const bool normed = !is_v && rows.k_gain;
+    f2 cosines[kSteps][2], sines[kSteps][2];                    // of a thread's rows
+    const bool normed = !V && rows.k_gain;
     if (normed) t.gains(rows.k_gain, ca, cb);
 
     while (begins) {
@@ -72,89 +82,127 @@ __device__ __forceinline__ void block_unit(const PagedE4m3StoreArgs& p, int unit
         begins &= begins - 1;
         // its rows are lanes a .. a + n - 1; those with a slot in the same place of the pool are written
         const int n = min(kPagedBlock, __ffs(~(same >> 1 >> a)));
-        const bool in = lane >= a && lane < a + n && has_slot;
+        const bool in = lane >= a && lane < a + n && first >= 0;
         const unsigned any = __ballot_sync(kFull, in);
         if (!any) continue;
-        const int f = __ffs(any) - 1, base = __shfl_sync(kFull, slot - within, f), from = __shfl_sync(kFull, pos - within, f), s = __shfl_sync(kFull, seq, f);
-        const unsigned stored = __ballot_sync(kFull, in && slot - within == base);
-        const unsigned written = __reduce_or_sync(kFull, (stored >> lane) & 1u ? 1u << within : 0u);
-        const int live = min(max(p.len[s], 0), 0x7fffffff - kPagedBlock) - from;
+        const int f = __ffs(any) - 1, base = __shfl_sync(kFull, first, f), live = __shfl_sync(kFull, to_end, f);
+        const unsigned stored = __ballot_sync(kFull, in && first == base);
+        const unsigned written = __reduce_or_sync(kFull, (stored >> lane) & 1u ? 1u << pos % kPagedBlock : 0u);
         const unsigned kept = ((1u << min(max(live, 0), kPagedBlock)) - 1u) & ~written;
         const int page = base >> rows.page_shift;
-        const size_t at = ((static_cast<size_t>(page) * p.KV + head) << rows.page_shift) + (base & ((1 << rows.page_shift) - 1));
-        unsigned char* dst = (is_v ? p.v_pool : p.k_pool) + at * HD;
-        float* scale = (is_v ? p.v_scales : p.k_scales) + at / kPagedBlock;
-        const int before = kept ? e4m3_exponent(*scale) : kPagedLowExp;
+        const unsigned at = (static_cast<unsigned>(page * p.KV + head0) << rows.page_shift) + (base & ((1 << rows.page_shift) - 1));   // row of the layer's pool: below 2^31
 
-        const __nv_bfloat16* src = is_v ? rows.v + (r0 + a) * rows.v_stride + head * HD : rows.k + (r0 + a) * rows.k_stride + head * HD;
-        const long long stride = is_v ? rows.v_stride : rows.k_stride;
+        const long long stride = V ? rows.v_stride : rows.k_stride;
+        const __nv_bfloat16* src = (V ? rows.v : rows.k) + (r0 + a + sub) * stride + head0 * HD;
         uint2 va[kSteps], vb[kSteps];
+        auto load = [&]() {
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const int j = i * kAtOnce + sub;
-            va[i] = vb[i] = make_uint2(0u, 0u);
-            if ((stored >> a >> j) & 1u) {
-                va[i] = *reinterpret_cast<const uint2*>(src + j * stride + ca);
-                vb[i] = *reinterpret_cast<const uint2*>(src + j * stride + cb);
-            }
-        }
-        f2 x[kSteps][4];
-        float top = 0.f;
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            f2 u[2], v[2];
-            if (is_v) {
-                widen<false>(va[i], vb[i], u, v);
-            } else {
-                widen<INTER>(va[i], vb[i], u, v);
-                if (normed) t.template norm<HD>(u, v, rows.eps, kFull);
-                t.angles(rows, __shfl_sync(kFull, pos, min(a + i * kAtOnce + sub, 31)), l, turned);
-                t.turn(u, v, turned);
-            }
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                x[i][k] = u[k];
-                x[i][2 + k] = v[k];
-                top = finite_max(finite_max(top, u[k]), v[k]);
-            }
-        }
-        const int e = max(e4m3_exponent_for(__uint_as_float(__reduce_max_sync(kFull, __float_as_uint(top)))), before);
-        const float by = exp2_int(-e);
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const int off = __shfl_sync(kFull, within, min(a + i * kAtOnce + sub, 31));
-            if (!((stored >> a >> (i * kAtOnce + sub)) & 1u)) continue;
-            f2 u0 = x[i][0], u1 = x[i][1], v0 = x[i][2], v1 = x[i][3];
-            if (INTER && !is_v) {                               // the pairs back in their places
-                const float2 a0 = floats(u0), a1 = floats(u1), b0 = floats(v0), b1 = floats(v1);
-                u0 = pair(a0.x, b0.x); u1 = pair(a0.y, b0.y);
-                v0 = pair(a1.x, b1.x); v1 = pair(a1.y, b1.y);
-            }
-            *reinterpret_cast<uint32_t*>(dst + off * HD + ca) = codes4(u0, u1, pair(by, by));
-            *reinterpret_cast<uint32_t*>(dst + off * HD + cb) = codes4(v0, v1, pair(by, by));
-        }
-        if (kept && e > before) {                               // the scale has grown: what stays is rounded again under it
-            const float down = exp2_int(max(before - e, -126));
-#pragma unroll 1
             for (int i = 0; i < kSteps; ++i) {
-                const int off = i * kAtOnce + sub;
-                if (!((kept >> off) & 1u)) continue;
-                uint2* c = reinterpret_cast<uint2*>(dst + off * HD + 8 * l);
-                const uint2 old = *c;
-                *c = make_uint2(e4m3x4_times(old.x, down), e4m3x4_times(old.y, down));
+                va[i] = vb[i] = make_uint2(0u, 0u);
+                if ((stored >> a >> (i * kAtOnce + sub)) & 1u) {
+                    va[i] = *reinterpret_cast<const uint2*>(src + i * kAtOnce * stride + ca);
+                    vb[i] = *reinterpret_cast<const uint2*>(src + i * kAtOnce * stride + cb);
+                }
+            }
+            src += HD;
+        };
+        load();
+        if (!V) {
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                t.angles(rows, __shfl_sync(kFull, pos, min(a + i * kAtOnce + sub, 31)), l, turned);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    cosines[i][k] = t.c[k];
+                    sines[i][k] = t.s[k];
+                }
             }
         }
-        if (lane == 0) *scale = exp2_int(e);
+#pragma unroll 1
+        for (int h = 0; h < heads; ++h) {
+            const unsigned row = at + (static_cast<unsigned>(h) << rows.page_shift);
+            unsigned char* dst = (V ? p.v_pool : p.k_pool) + static_cast<size_t>(row) * HD;
+            float* scale = (V ? p.v_scales : p.k_scales) + row / kPagedBlock;
+            const int before = kept ? e4m3_exponent(*scale) : kPagedLowExp;
+            f2 x[kSteps][4];
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                f2 u[2], v[2];
+                if (V) widen<false>(va[i], vb[i], u, v);
+                else widen<INTER>(va[i], vb[i], u, v);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    x[i][k] = u[k];
+                    x[i][2 + k] = v[k];
+                }
+            }
+            if (h + 1 < heads) load();                          // the next head's rows while these are at work
+            float top = 0.f;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                f2 u[2] = {x[i][0], x[i][1]}, v[2] = {x[i][2], x[i][3]};
+                if (!V) {
+                    if (normed) t.template norm<HD>(u, v, rows.eps, kFull);
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        t.c[k] = cosines[i][k];
+                        t.s[k] = sines[i][k];
+                        t.ms[k] = sines[i][k] ^ 0x8000000080000000ull;      // both signs turned: registers are what limits the warps of an SM
+                    }
+                    t.turn(u, v, turned);
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    x[i][k] = u[k];
+                    x[i][2 + k] = v[k];
+                    top = finite_max(finite_max(top, u[k]), v[k]);
+                }
+            }
+            top = __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(top)));
+            if (lane == 0) tops[turn][threadIdx.x >> 5] = top;
+            __syncthreads();                                    // all have the block's exponent from before, too
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) top = fmaxf(top, tops[turn][i]);
+            turn ^= 1;
+            const int e = max(e4m3_exponent_for(top), before);
+            const float by = exp2_int(-e);
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int off = __shfl_sync(kFull, pos, min(a + i * kAtOnce + sub, 31)) % kPagedBlock;
+                if (!((stored >> a >> (i * kAtOnce + sub)) & 1u)) continue;
+                f2 u0 = x[i][0], u1 = x[i][1], v0 = x[i][2], v1 = x[i][3];
+                if (INTER && !V) {                           // the pairs back in their places
+                    const float2 a0 = floats(u0), a1 = floats(u1), b0 = floats(v0), b1 = floats(v1);
+                    u0 = pair(a0.x, b0.x); u1 = pair(a0.y, b0.y);
+                    v0 = pair(a1.x, b1.x); v1 = pair(a1.y, b1.y);
+                }
+                *reinterpret_cast<uint32_t*>(dst + off * HD + ca) = codes4(u0, u1, pair(by, by));
+                *reinterpret_cast<uint32_t*>(dst + off * HD + cb) = codes4(v0, v1, pair(by, by));
+            }
+            if (kept && e > before) {                           // the scale has grown: what stays is rounded again under it
+                const float down = exp2_int(max(before - e, -126));
+#pragma unroll 1
+                for (int i = 0; i < kSteps; ++i) {
+                    const int off = i * kAtOnce + sub;
+                    if (!((kept >> off) & 1u)) continue;
+                    uint2* c = reinterpret_cast<uint2*>(dst + off * HD + 8 * l);
+                    const uint2 old = *c;
+                    *c = make_uint2(e4m3x4_times(old.x, down), e4m3x4_times(old.y, down));
+                }
+            }
+            if (threadIdx.x == 0) *scale = exp2_int(e);
+        }
     }
 }
 
 template <int HD, bool INTER, bool ALL>
-__global__ void __launch_bounds__(kThreads) paged_e4m3_store_kernel(const PagedE4m3StoreArgs p, const int blocks, const int units) {
+__global__ void __launch_bounds__(kThreads, 7) paged_e4m3_store_kernel(const PagedE4m3StoreArgs p, const int blocks) {
     pdl_launch_dependents();
     pdl_wait();
     if (static_cast<int>(blockIdx.x) < blocks) {
-        const int unit = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-        if (unit < units) block_unit<HD, INTER, ALL>(p, unit);
+        const int groups = (p.KV + p.heads - 1) / p.heads, w = blockIdx.x / (2 * groups), part = blockIdx.x - w * 2 * groups;
+        if (part < groups) block_unit<HD, INTER, ALL, false>(p, w, part * p.heads);
+        else block_unit<HD, INTER, ALL, true>(p, w, (part - groups) * p.heads);
     } else {
         constexpr int kLanes = HD / 8;
         store_unit<HD, INTER, ALL>(p.rows, static_cast<long long>(blockIdx.x - blocks) * (kThreads / kLanes) + threadIdx.x / kLanes);
@@ -163,10 +211,10 @@ __global__ void __launch_bounds__(kThreads) paged_e4m3_store_kernel(const PagedE
 
 template <int HD, bool INTER, bool ALL>
 cudaError_t launch(const PagedE4m3StoreArgs& a, cudaStream_t st) {
-    const int units = (a.rows.rows + a.window - 1) / a.window * 2 * a.KV, blocks = (units + kThreads / 32 - 1) / (kThreads / 32);
+    const int blocks = (a.rows.rows + a.window - 1) / a.window * 2 * ((a.KV + a.heads - 1) / a.heads);
     const long long q_units = static_cast<long long>(a.rows.rows) * ((a.rows.H + kStoreHeads - 1) / kStoreHeads), per = kThreads / (HD / 8);
     return launch_kernel(paged_e4m3_store_kernel<HD, INTER, ALL>, dim3(static_cast<unsigned>(blocks + (q_units + per - 1) / per)), dim3(kThreads), 0, st, a,
-                         blocks, units);
+                         blocks);
 }
 
 }  // namespace
