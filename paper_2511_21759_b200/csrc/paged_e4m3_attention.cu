@@ -26,9 +26,10 @@ constexpr int kItem = 1;                    // key tiles that an item costs besi
 constexpr int kMinUnits = 2;                // units of a CTA, at least
 constexpr int kKT = 64;                     // keys per tile
 constexpr int kFullUnits = 12;              // of a CTA where all places on the SMs have work
-constexpr int kSmallUnits = 1024;           // up to here few rows' kernel for any number of rows
-constexpr int kCopiedRows = 128;            // packed rows of the longest request from which requests that are alike take a copy in bf16
-constexpr int kManyRows = 1024;             // packed rows a request, on average, from which two Q tiles are right whatever the longest
+constexpr int kFewRows = 32;                // packed rows of the longest request, up to which few rows' kernel takes them
+constexpr int kSmallUnits = 2304;           // up to here few rows' kernel for any number of rows
+constexpr int kCopiedRows = 384;            // packed rows of the longest request above which requests that are alike take a copy in bf16
+constexpr int kManyRows = 1024;             // packed rows a request, on average, from which the copy is right whatever the longest
 constexpr int kMmaWarps = 4;                // 16 keys of a tile each
 constexpr int kThreads = 32 * (kMmaWarps + 1);
 constexpr int kBlocks = kKT / kPagedBlock;  // of a tile
@@ -521,7 +522,15 @@ cudaError_t launch(PagedAttnArgs a, const CUtensorMap& tmap, int sms, cudaStream
 
 }  // namespace
 
-// Which kernel, as for a pool of bf16 (paged_attention_kernel_of).
+// Which kernel (8, 16: few rows' for items of so many; 1: one Q tile of the tensor cores; 2: the copy in bf16), by the packed rows of the
+// longest request and by the work, as for a pool of bf16 (paged_attention_kernel_of).  Both sides, 8 K/V heads of 128, in us:
+//   items of 8 or 16 rows: tokens of 16 requests x 8192 keys, groups of 8 heads: 33 | 43, of 12: 52 | 46; 20 packed rows, 4096 keys: 73 | 78,
+//     32 rows: 90 | 80 (a third item of 8 costs less than a second of 16 does)
+//   kFewRows, 16 requests, 4096 keys: 32 packed rows 80 | 92 on the tensor cores, 48 rows 112 | 92
+//   kSmallUnits, blocks of 32 rows x group 4: 1536 units (4 requests of 256 keys) 12.5 | 23.4, 2304 (2 of 1024) 22.7 | 24.8, 3072 (16 of 64)
+//     22.9 | 21.6, 4608 (4 of 1024) 31 | 26
+//   kCopiedRows, 16 requests, 4096 keys: 384 packed rows 247 | 287 with the copy, 512 rows 321 | 291, 1024 rows 616 | 463
+// The copy wants the requests alike: a prompt among single tokens would have all their pages copied.
 int paged_e4m3_attention_kernel_of(int n_seqs, int max_rows, int max_new, int group, int kv_heads, long long longest, long long out_stride, bool room) {
     const long long all = static_cast<long long>(max_rows) * group, mean = (max_rows + n_seqs - 1ll) / n_seqs * group,
                     mine = max_new > 0 ? static_cast<long long>(max_new) * group : mean, tiles = longest / kKT + 1;
@@ -529,11 +538,11 @@ int paged_e4m3_attention_kernel_of(int n_seqs, int max_rows, int max_new, int gr
     auto fits = [&](int tile_rows, int item) {
         return (static_cast<double>(all / tile_rows) + n_seqs) * kv_heads * static_cast<double>(tiles + item) < 2147483648.0 - 65536;
     };
-    const int few = mine <= 8 && fits(8, kItem) ? 8 : fits(16, kItem) ? 16 : -1;
+    const int few = (mine <= 8 || (mine > 16 && mine <= 24)) && fits(8, kItem) ? 8 : fits(16, kItem) ? 16 : -1;
     if (group <= kPagedTcMaxGroup && out_stride <= 1ll << 27) {
         const int tile = kPagedTcMaxGroup / group * group;
         const double units = static_cast<double>((all + 15ll * n_seqs) / 16) * kv_heads * static_cast<double>(tiles + kItem);
-        if ((mine > 16 && units > kSmallUnits) || few < 0) {
+        if ((mine > kFewRows && units > kSmallUnits) || few < 0) {
             const bool alike = max_new > 0 ? static_cast<long long>(max_new) * n_seqs <= 3ll * max_rows : n_seqs == 1 || mean >= kManyRows;
             if (room && ((mine > kCopiedRows && alike) || !fits(tile, kPagedTcItem)) && fits(2 * tile, kPagedTcItem)) return 2;
             return fits(tile, kPagedTcItem) ? 1 : few;

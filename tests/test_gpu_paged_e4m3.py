@@ -68,6 +68,10 @@ STORE = [  # requests (first, rows, length), H, KV, D, page, rot, interleaved, n
     ([(100000, 47, 100100), (0, 16, 16)], 16, 4, 128, 64, 128, True, False, "yarn", 32.0),
     ([(0, 700, 700), (300, 418, 718)], 4, 4, 64, 64, 64, False, True, "none", 1.0),
     ([(i * 3, 1, i * 3 + 1) for i in range(70)], 4, 2, 64, 16, 64, False, True, "none", 1.0),
+    # enough work for units of 4, of 8 and of 2 heads, the last of fewer; rows of two and more blocks in a window
+    ([(i * 3, 1, i * 3 + 1) for i in range(90)], 26, 26, 64, 32, 64, False, True, "none", 1.0),
+    ([(5, 1000, 1005)], 70, 70, 64, 64, 64, True, True, "none", 1.0),
+    ([(i * 7 + 3, 9, i * 7 + 12) for i in range(60)], 31, 31, 128, 16, 128, False, False, "none", 1.0),
 ]
 
 
@@ -489,7 +493,7 @@ def test_attention_of_many_requests_of_a_tile_or_two(new, G, D, columns):
 
 
 @requires_gpu
-@pytest.mark.parametrize("new", [1, 3, 20, 40])
+@pytest.mark.parametrize("new", [1, 3, 10, 20, 40, 250])
 @pytest.mark.parametrize("D", [64, 128])
 def test_attention_rows_that_see_nothing_and_requests_without_rows_or_keys(new, D, columns):
     rng = np.random.default_rng(new + D)
@@ -507,7 +511,7 @@ def test_attention_rows_that_see_nothing_and_requests_without_rows_or_keys(new, 
 
 
 @requires_gpu
-@pytest.mark.parametrize("new,G", [(1, 4), (5, 2), (20, 1), (9, 4), (20, 4), (70, 1), (100, 3)])
+@pytest.mark.parametrize("new,G", [(1, 4), (5, 2), (5, 4), (20, 1), (9, 4), (20, 4), (70, 1), (100, 3), (130, 3)])
 @pytest.mark.parametrize("D", [64, 128])
 def test_attention_nan_codes_reach_only_the_rows_that_see_them(new, G, D, columns):
     rng = np.random.default_rng(new + D)
@@ -553,7 +557,7 @@ def test_attention_nan_codes_reach_only_the_rows_that_see_them(new, G, D, column
 
 @requires_gpu
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("new", [3, 45, 90])
+@pytest.mark.parametrize("new", [3, 5, 45, 90, 240])
 def test_attention_of_large_scores_and_another_scale(new, D, columns):
     rng = np.random.default_rng(21)
     lens, counts = [333, 94], [new, new]
