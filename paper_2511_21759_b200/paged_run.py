@@ -1,4 +1,4 @@
-"""A small server loop over the paged cache: python -m paper_2511_21759_b200.paged_run [--layers N] [--requests N] [--blocks N]
+"""A small server loop over the paged cache: python -m paper_2511_21759_b200.paged_run [--layers N] [--requests N] [--blocks N] [--kv bf16|e4m3]
 
 Attention layers with grouped heads over requests of different lengths, decoded block by block as the method does: a refresh of
 every request at the start of its block (all rows, keys in both directions), a few steps of the block's rows against the cached
@@ -8,6 +8,7 @@ request ends, a new one takes its place and its pages.  Per forward
     layout                                     once: block tables, slots, rows
     QKV projection -> norm_rope_store -> attention -> output projection        per layer
 
+The cache is of bf16 or (--kv e4m3) of 8 bits, quantised as it is written: twice the requests in the same memory.
 The projections are the library's GEMM; weights and inputs are synthetic (seeded).  Prints what every forward held and took.
 """
 from __future__ import annotations
@@ -67,11 +68,11 @@ class Layers:
 
 
 class Server:
-    """Requests with a prompt and a response in blocks, their pages in one pool."""
+    """Requests with a prompt and a response in blocks, their pages in one pool (of bf16, or in 8 bits: dtype torch.float8_e4m3fn)."""
 
-    def __init__(self, layers: Layers, page_size: int, n_pages: int, longest: int, block: int):
+    def __init__(self, layers: Layers, page_size: int, n_pages: int, longest: int, block: int, dtype=torch.bfloat16):
         self.layers, self.block, self.page_size = layers, block, page_size
-        self.cache = paged.PagedCache(layers.n_layers, layers.n_heads, layers.n_kv_heads, layers.head_dim, page_size, n_pages)
+        self.cache = paged.PagedCache(layers.n_layers, layers.n_heads, layers.n_kv_heads, layers.head_dim, page_size, n_pages, dtype=dtype)
         self.rope = paged.Rope(layers.head_dim)
         self.width = -(-longest // page_size)
         self.free = torch.arange(n_pages, dtype=torch.int32, device="cuda")
@@ -114,10 +115,11 @@ class Server:
         return batch, h
 
 
-def run(layers: Layers, requests: int = 6, blocks: int = 3, block: int = 32, page_size: int = 16, steps: int = 2, seen=None, say=print):
+def run(layers: Layers, requests: int = 6, blocks: int = 3, block: int = 32, page_size: int = 16, steps: int = 2, seen=None, say=print,
+        dtype=torch.bfloat16):
     """The loop of this file's heading; every request has `blocks` blocks of response.  Returns the server."""
     longest = 40 * requests + 64 + blocks * block
-    server = Server(layers, page_size, requests * (-(-longest // page_size)), longest, block)
+    server = Server(layers, page_size, requests * (-(-longest // page_size)), longest, block, dtype)
     for i in range(requests):
         server.add(40 * i + 17, blocks * block)
     held = lambda: sum(-(-n // page_size) for n in server.length)
@@ -143,8 +145,9 @@ def main():
     ap.add_argument("--layers", type=int, default=4)
     ap.add_argument("--requests", type=int, default=6)
     ap.add_argument("--blocks", type=int, default=3)
+    ap.add_argument("--kv", choices=["bf16", "e4m3"], default="bf16", help="the cache's values")
     a = ap.parse_args()
-    run(Layers(a.layers, 32, 8, 128), a.requests, a.blocks)
+    run(Layers(a.layers, 32, 8, 128), a.requests, a.blocks, dtype=torch.bfloat16 if a.kv == "bf16" else torch.float8_e4m3fn)
 
 
 if __name__ == "__main__":
