@@ -12,6 +12,8 @@ Bounds, derived before the first run.
   the weight itself; a score's fp32 sum of head_dim exact products, head_dim 2^-24 sum|q k|
   scale, and Q in f16 under a power of two, 2^-25 of its largest value per dim: together d, which moves numerator and denominator by a
   factor e^d each; log-sum-exp by d and a rounding of fp32."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -129,6 +131,7 @@ def _check_store(case, seed, layers=2, layer=1, size=1.0):
     exps = np.log2(scales).round().astype(int)
     assert np.array_equal(2.0 ** exps, scales)
     want_pool, want_exps = before.copy(), before_exp.copy()
+    codes_before, codes_after = pool[0].numpy(), codes_of(cache.kv)
     blocks = {}
     for r in range(len(seq)):
         blocks.setdefault((seq[r], pos[r] // O.BLOCK), []).append(r)
@@ -158,8 +161,8 @@ def _check_store(case, seed, layers=2, layer=1, size=1.0):
             want_pool[place], want_exps[layer, :, pg, h, o0 // O.BLOCK] = got, ge
             for i in range(2):                                 # positions that are neither written nor kept: their codes stay
                 rest = [o for o in range(O.BLOCK) if o not in offs + kept]
-                old = pool[0].numpy()[layer, i, pg, h, o0:o0 + O.BLOCK]
-                now = codes_of(cache.kv)[layer, i, pg, h, o0:o0 + O.BLOCK] if rest else old
+                old = codes_before[layer, i, pg, h, o0:o0 + O.BLOCK]
+                now = codes_after[layer, i, pg, h, o0:o0 + O.BLOCK] if rest else old
                 assert np.array_equal(now[rest], old[rest])
     assert np.array_equal(after, want_pool) and np.array_equal(exps, want_exps)     # nothing else has changed
     # the same call again finds its own scales and changes nothing
@@ -726,6 +729,55 @@ def test_streams_and_graphs():
     cache.close()
 
 
+@requires_gpu
+def test_prompts_copies_are_made_in_every_call():
+    """Layers after one another through one copy's place, eagerly and replayed, with the pool changed in between."""
+    rng = np.random.default_rng(31)
+    cache, b, q, *_ = setup(rng, [300, 260], [250, 250], [50, 10], 4, 2, 64, 32, layers=2, layer=0, columns=5000)
+    raw = cache.kv.view(torch.uint8)
+    raw[1].copy_(raw[0].flip(-1))
+    cache.scales[1].copy_(cache.scales[0])
+    run = lambda: [cache.attention(i, b, q, right=0) for i in (0, 1, 0)]
+    want = run()
+    assert cache.status() == 0 and bool(torch.isfinite(want[0]).all()) and not torch.equal(want[0], want[1]) and torch.equal(want[0], want[2])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = run()
+    g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    raw[0, 1] ^= 0x80                                             # the signs of V of layer 0
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], -want[0]) and torch.equal(got[1], want[1]) and torch.equal(got[2], -want[0])
+    raw[0, 1] ^= 0x80
+    assert all(torch.equal(x, y) for x, y in zip(run(), want))
+    cache.close()
+
+
+@requires_gpu
+def test_prompts_with_a_table_of_nonsense_stay_inside_the_pool():
+    from paper_2511_21759_b200 import binding as B
+    rng = np.random.default_rng(8)
+    cache, b, q, *_ = setup(rng, [300, 300], [250, 250], [50, 50], 2, 1, 64, 16, columns=5000)
+    table, length = b.table.clone(), b.len_after.clone()
+    want = cache.attention(0, b, q, right=0)
+    b.table.fill_(-5)
+    b.table[1] = 2 ** 31 - 1
+    assert bool((cache.attention(0, b, q) == 0).all()) and cache.status() == B.ODB_ERR_STATE
+    b.len_after.fill_(2 ** 31 - 1)
+    b.first.fill_(-2 ** 31)
+    assert bool((cache.attention(0, b, q, right=0) == 0).all()) and cache.status() == B.ODB_ERR_ARG
+    starts = b.row_start.clone()
+    for bad in ([0, 1, 2 ** 31 - 1], [-9, -3, -1], [1, 0, 2]):
+        b.row_start.copy_(torch.tensor(bad, dtype=torch.int32))
+        cache.attention(0, b, q)
+        assert cache.status() == B.ODB_ERR_ARG
+    b.row_start.copy_(starts), b.table.copy_(table), b.len_after.copy_(length), b.first.fill_(50)
+    assert torch.equal(cache.attention(0, b, q, right=0), want) and cache.status() == 0
+    cache.close()
+
+
 # ---- refusals ---------------------------------------------------------------------------------------------------------
 
 @requires_gpu
@@ -768,6 +820,8 @@ def test_calls_that_are_refused():
         with pytest.raises(B.OdbError) as e:
             cache.load(layer, rows)
         assert e.value.status == B.ODB_ERR_ARG
+    many = B.odb_paged_batch(max_rows=2 ** 29, row_slot=rows.row_slot.data_ptr())      # 32-bit numbers: refused before anything is read
+    assert B.lib().odb_paged_load(cache.handle, 0, C.byref(many), flat.data_ptr(), 128, flat.data_ptr() + 2 ** 50, 128, None) == B.ODB_ERR_SHAPE
     other = P.PagedCache(1, 4, 2, 64, 16, 5, dtype=E4M3)
     with pytest.raises(ValueError):
         other.load(0, rows)
