@@ -337,6 +337,7 @@ int32_t odb_paged_load(odb_paged* h, int32_t layer, const odb_paged_batch* b, vo
     const int64_t width = static_cast<int64_t>(c.n_kv_heads) * c.head_dim;
     if (!k || !v || !b->row_slot || k_stride < width || v_stride < width || ((k_stride | v_stride) & 7) || !aligned(k, 16) || !aligned(v, 16)) return ODB_ERR_ARG;
     if (overlap({k, k_stride, width}, {v, v_stride, width}, b->max_rows)) return ODB_ERR_ARG;
+    if (static_cast<double>(b->max_rows) * c.n_kv_heads >= 1073741824.0) return ODB_ERR_SHAPE;   // blocks' rows are 32-bit numbers
     PagedLoadArgs a{};
     a.k_pool = reinterpret_cast<const unsigned char*>(h->k_of(layer)); a.v_pool = reinterpret_cast<const unsigned char*>(h->v_of(layer));
     a.k_scales = h->k_scales_of(layer); a.v_scales = h->v_scales_of(layer);
