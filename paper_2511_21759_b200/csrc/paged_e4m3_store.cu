@@ -15,8 +15,8 @@
 // sines, its table and its slots are found once.  Blocks begin where a row's request or block differs from the row's before it: every warp
 // looks for them among `window` rows, with all their maps in one load.  Units of q as in the store of bf16, behind the blocks.
 //
-// What bounds it: the rows of a refresh of 4 requests x 4096 positions, 32 + 8 heads of 128, are 302 MB in and 168 MB out with q, 72 us at
-// the copy rate; it takes 111 us, 63 of them for q and 48 for K and V (75 with a warp to a block and head).  A thread holds two rows' values,
+// What bounds it: a refresh of 16 requests of 1200 to 1999 rows, 32 + 8 heads of 128, reads 317 MB and writes 264 with q, 88 us at the copy
+// rate; it takes 111 us, 63 of them for q and 48 for K and V (75 with a warp to a block and head).  A thread holds two rows' values,
 // angles and loads in flight: the registers limit the warps of an SM, and seven CTAs of four (72 registers; up to 20 bytes spilled in some
 // forms) take 111 us where six (80, none spilled) take 121, at 16 x 32 rows 11.1 and 11.2.  48 tokens take 4.3 us in a graph, a
 // launch and three dependent reads (map, table, row).
