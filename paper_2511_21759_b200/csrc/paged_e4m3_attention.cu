@@ -534,8 +534,8 @@ cudaError_t launch(PagedAttnArgs a, const CUtensorMap& tmap, int sms, cudaStream
 //   items of 8 or 16 rows: tokens of 16 requests x 8192 keys, groups of 8 heads: 33 | 43, of 12: 52 | 46; 20 packed rows, 4096 keys: 73 | 78,
 //     32 rows: 90 | 80 (a third item of 8 costs less than a second of 16 does)
 //   kFewRows, 16 requests, 4096 keys: 32 packed rows 80 | 92 on the tensor cores, 48 rows 112 | 92
-//   kSmallUnits, blocks of 32 rows x group 4: 1536 units (4 requests of 256 keys) 12.5 | 23.4, 2304 (2 of 1024) 22.7 | 24.8, 3072 (16 of 64)
-//     22.9 | 21.6, 4608 (4 of 1024) 31 | 26
+//   kSmallUnits, blocks of 32 rows x group 4: 1536 units (4 requests of 256 keys) 12.5 | 23.4, 2304 (2 of 1024) 22.7 | 24.8, 4608 (4 of 1024)
+//     31 | 26
 //   kCopiedRows, 16 requests, 4096 keys: 384 packed rows 247 | 287 with the copy, 512 rows 321 | 291, 1024 rows 616 | 463
 // The copy wants the requests alike: a prompt among single tokens would have all their pages copied.
 int paged_e4m3_attention_kernel_of(int n_seqs, int max_rows, int max_new, int group, int kv_heads, long long longest, long long out_stride, bool room) {
