@@ -14,7 +14,7 @@ namespace odb {
 
 namespace {
 
-constexpr int kThreads = 256, kAtOnce = 4;
+constexpr int kThreads = 256, kAtOnce = 4, kCopied = 2;   // loads in flight of a thread: of the load's, of the copy's, which has eight blocks on an SM
 
 // 8 codes as bf16
 __device__ __forceinline__ uint4 expand8(const uint2& codes, float scale) {
@@ -65,9 +65,10 @@ __global__ void __launch_bounds__(kThreads) paged_load_kernel(const PagedLoadArg
 
 // The pages that the attention's rows see, one head of K or V a block at a time, from their codes into the same places of a pool of one layer
 // in bf16, which the attention's kernel for pools of bf16 then reads: for prompts, whose row tiles would otherwise each turn the same codes
-// into operands.
+// into operands.  The reads are ordinary loads: a block is resident while the store in front of it still writes the pool, and the loads for
+// memory that is constant promise nothing about what is written in a kernel's lifetime, be it in front of its wait.
 template <int HD>
-__global__ void __launch_bounds__(kThreads) paged_expand_kernel(const PagedAttnArgs a, __nv_bfloat16* __restrict__ layer, const int layer_rows) {
+__global__ void __launch_bounds__(kThreads, 8) paged_expand_kernel(const PagedAttnArgs a, __nv_bfloat16* layer, const int layer_rows) {
     pdl_launch_dependents();
     pdl_wait();
     const int s = blockIdx.y, head = blockIdx.z % a.KV;
@@ -84,8 +85,23 @@ __global__ void __launch_bounds__(kThreads) paged_expand_kernel(const PagedAttnA
         const uint2* src = reinterpret_cast<const uint2*>(reinterpret_cast<const unsigned char*>(a.pool) + at * HD);
         const float* scale = a.scales + at / kPagedBlock;
         uint4* dst = reinterpret_cast<uint4*>(layer + (row + (is_v ? layer_rows : 0)) * HD);
-        for (int i = threadIdx.x; i < (HD / 8) << a.page_shift; i += kThreads)
-            dst[i] = expand8(__ldg(src + i), __ldg(scale + i / (2 * HD)));   // 16 positions of HD / 8 pieces each have a scale
+        const int all = (HD / 8) << a.page_shift;
+        for (int i0 = threadIdx.x; i0 < all; i0 += kThreads * kCopied) {
+            uint2 codes[kCopied];
+            float by[kCopied];
+#pragma unroll
+            for (int k = 0; k < kCopied; ++k) {
+                const int i = i0 + k * kThreads;
+                if (i >= all) break;
+                codes[k] = src[i];
+                by[k] = scale[i / (2 * HD)];                    // 16 positions of HD / 8 pieces each have a scale
+            }
+#pragma unroll
+            for (int k = 0; k < kCopied; ++k) {
+                const int i = i0 + k * kThreads;
+                if (i < all) dst[i] = expand8(codes[k], by[k]);
+            }
+        }
     }
 }
 
