@@ -57,7 +57,7 @@ __device__ __forceinline__ void tma_codes(uint32_t dst, const CUtensorMap* tmap,
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
-// an arrival once this thread's copies so far have landed; counted among the barrier's
+// an arrival once this thread's copies so far have landed; counted among the barrier's.  It says nothing of what the thread has stored itself.
 __device__ __forceinline__ void copies_arrive(uint64_t* bar) {
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }

@@ -160,11 +160,13 @@ __global__ void __launch_bounds__(kThreads, kCtas<NR>) paged_e4m3_attention_kern
                 }
                 if (lane < 2 * kBlocks) {                       // K's scales, then V's; a page that is none reads as zeros
                     float* scale = &sh->scale[s][0][lane];
-                    if (b < n_blocks) {
-                        if (there) copy4(smem_u32(scale), a.scales + (row + (lane < kBlocks ? 0 : a.v_row0 - a.k_row0)) / kPagedBlock);
-                        else *scale = 1.f;
+                    if (b < n_blocks && !there) {
+                        *scale = 1.f;
+                        mbar_arrive(full);                      // a copy's arrival would not wait for this lane's own write
+                    } else {
+                        if (b < n_blocks) copy4(smem_u32(scale), a.scales + (row + (lane < kBlocks ? 0 : a.v_row0 - a.k_row0)) / kPagedBlock);
+                        copies_arrive(full);
                     }
-                    copies_arrive(full);
                 }
                 __syncwarp();
                 next_stage();

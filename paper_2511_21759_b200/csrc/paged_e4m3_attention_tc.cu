@@ -240,11 +240,13 @@ __global__ void __launch_bounds__(kThreads, 2)
                 }
                 if (!V && lane < 2 * kBlocks) {              // K's scales, then V's; a page that is none reads as zeros
                     float* scale = &sh->scale[x.slot][0][lane];
-                    if (b < n_blocks) {
-                        if (row < a.pool_rows) copy4(smem_u32(scale), a.scales + (row + (lane < kBlocks ? 0 : a.v_row0 - a.k_row0)) / kPagedBlock);
-                        else *scale = 1.f;
+                    if (b < n_blocks && row >= a.pool_rows) {
+                        *scale = 1.f;
+                        mbar_arrive(full);                   // a copy's arrival would not wait for this lane's own write
+                    } else {
+                        if (b < n_blocks) copy4(smem_u32(scale), a.scales + (row + (lane < kBlocks ? 0 : a.v_row0 - a.k_row0)) / kPagedBlock);
+                        copies_arrive(full);
                     }
-                    copies_arrive(full);
                 }
                 __syncwarp();
                 x.next();

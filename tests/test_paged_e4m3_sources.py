@@ -1,7 +1,12 @@
-"""What the sources of the paged cache say of memory that a kernel in front of them writes: a kernel of this library is resident, by programmatic
+"""What the sources of the paged cache say of memory that others write.
+
+Of the kernel in front: a kernel of this library is resident, by programmatic
 dependent launch, while the one in front of it still runs, and what it reads has been written in its lifetime.  Loads for memory that is
 constant as long as the kernel lives (ld.global.nc, __ldg, and what the compiler may make of pointers that share nothing with others) promise
-nothing about such memory."""
+nothing about such memory.
+
+Of other threads: the arrival that follows a thread's asynchronous copies (cp.async.mbarrier.arrive) is made when they have landed and orders
+nothing that the thread has stored itself."""
 import glob
 import os
 import re
@@ -21,3 +26,12 @@ def test_nothing_is_read_as_if_it_were_constant(name):
     text = code_of(name)
     for word in ("__ldg", "ld.global.nc", "ldu.", "__restrict__"):
         assert word not in text, word
+
+
+@pytest.mark.parametrize("name", ["paged_e4m3_attention.cu", "paged_e4m3_attention_tc.cu"])
+def test_a_scale_that_a_lane_writes_itself_is_followed_by_its_own_arrival(name):
+    text = code_of(name)
+    stores = [m.end() for m in re.finditer(r"\*scale = 1\.f;", text)]
+    assert len(stores) == 1
+    then = re.search(r"\b(mbar_arrive|copies_arrive)\(", text[stores[0]:])
+    assert then.group(1) == "mbar_arrive"
