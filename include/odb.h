@@ -468,7 +468,7 @@ int32_t odb_paged_status(odb_paged* h, void* stream);
  * powers of two from 2^-100 to 2^119, so that what a code stands for is a number of bf16.  kv and scales on 256-byte boundaries, borrowed
  * as kv is; the workspace is odb_paged_workspace_bytes', or more (below).  layout, attention, load, status and destroy are called as over a pool of bf16
  * (an attention's weights are rounded to f16 or bf16 for the product with V); for the store see odb_paged_norm_rope_store. */
-enum { ODB_PAGED_SCALE_BLOCK = 16 };
+enum { ODB_PAGED_SCALE_BLOCK = 16, ODB_PAGED_LEAST_SCALE = -100 };   /* positions of a scale; the smallest scale's exponent */
 size_t odb_paged_e4m3_kv_bytes(const odb_paged_config* cfg);     /* 0: a configuration odb_paged_create_e4m3 would refuse */
 size_t odb_paged_e4m3_scale_bytes(const odb_paged_config* cfg);
 /* A workspace of odb_paged_workspace_bytes + this many bytes has room for the K and V of one layer in bf16: prompts (requests that are
@@ -484,7 +484,10 @@ int32_t odb_paged_create_e4m3(const odb_paged_config* cfg, void* kv, size_t kv_b
  * then table order): page j that is taken is entry n + G - 1 - j; the first n + G - T entries remain.  Table entries
  * behind the pages held are left as they are.  Reads len_before, len_after, first, count; updates table, free_pages;
  * writes row_start, row_seq, row_pos, row_slot.  A forward that does not fit changes no table and has no rows (row_start
- * all zero), see odb_paged_status.  The next call's len_before is this one's len_after. */
+ * all zero), see odb_paged_status.  The next call's len_before is this one's len_after.
+ * Over a pool of 8 bits the scales of the pages taken, of all layers and heads, become 2^ODB_PAGED_LEAST_SCALE: what they hold of others
+ * has no say in the blocks that are then filled, be it part by part (odb_paged_norm_rope_store).  Of the handle that is called: with
+ * another one over the same tables, or pages that are handed out without this call, the caller writes them. */
 int32_t odb_paged_layout(odb_paged* h, const odb_paged_batch* b, void* stream);
 
 /* Rotation frequencies.  plain: theta^(-2i / rot_dim) radians per position for pair i; linear: divided by factor
@@ -523,8 +526,9 @@ typedef struct odb_rope {
  *
  * Over a pool of 8 bits K and V are quantised as they are written, block by block (16 positions of a request from a multiple of 16 on, a
  * head, K or V), from fp32 in one rounding.  e is the smallest integer, from -100 to 119, with max |x| <= 448 * 2^e over the finite values
- * that the call writes of the block; where the block keeps positions, those below len_after that the call does not write, e is at least
- * the block's exponent before, and their codes are rounded again, code := e4m3(code * 2^(before - e)).  The codes of the rows are
+ * that the call writes of the block; where the block keeps positions, those below len_after that the call does not write, whether or not
+ * anyone has written them, e is at least the block's exponent before (the smallest in a page that odb_paged_layout has handed out and
+ * nobody has written to), and their codes are rounded again, code := e4m3(code * 2^(before - e)).  The codes of the rows are
  * e4m3(x * 2^-e), to the nearest, ties to even, NaN where x is not finite (beyond 448 * 2^119 the largest number); the scale is 2^e.
  * Reads row_seq and len_after too, as odb_paged_layout leaves them: the rows of a request's block follow one another, with a position each,
  * and their slots lie in one page at position % 16 (others are not stored).  No two requests write into a block in the same call (what

@@ -16,7 +16,7 @@ LIB_PATH = os.path.join(HERE, "libodb.so")
 ODB_OK, ODB_ERR_ARG, ODB_ERR_SHAPE, ODB_ERR_WORKSPACE, ODB_ERR_STATE, ODB_ERR_CUDA, ODB_ERR_TIMEOUT = 0, -1, -2, -3, -4, -5, -6
 ODB_MAX_COPIES, ODB_MAX_RANKS, ODB_MAX_CHAIN = 8, 4, 5
 ODB_STATIC_SCRATCH_BYTES = 8 << 20
-ODB_PAGED_SCALE_BLOCK = 16
+ODB_PAGED_SCALE_BLOCK, ODB_PAGED_LEAST_SCALE = 16, -100
 KINDS = ("gemm", "attention", "elementwise", "confidence", "control")
 
 

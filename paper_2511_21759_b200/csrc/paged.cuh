@@ -21,6 +21,8 @@ struct PagedLayoutArgs {
     int32_t *row_start, *row_seq, *row_pos, *row_slot;
     int n_seqs, max_rows, page_shift, n_pages, table_stride;
     int* status;
+    float* scales;                                        // [parts][n_pages][page_scales], null: a pool of bf16
+    int parts, page_scales;                               // K and V of every layer; scales of a page in one of them
 };
 cudaError_t launch_paged_layout(const PagedLayoutArgs& a, cudaStream_t st);
 
@@ -40,7 +42,7 @@ cudaError_t launch_paged_store(const PagedStoreArgs& a, cudaStream_t st);
 
 // ---- pools of 8 bits: e4m3 and a scale, a power of two, for each block of 16 positions of a head (paged_e4m3_store.cu) ----
 constexpr int kPagedBlock = ODB_PAGED_SCALE_BLOCK;
-constexpr int kPagedLowExp = -100, kPagedHighExp = 119;   // of scales: what the codes stand for is then a number of bf16
+constexpr int kPagedLowExp = ODB_PAGED_LEAST_SCALE, kPagedHighExp = 119;   // of scales: what the codes stand for is then a number of bf16
 struct PagedE4m3StoreArgs {
     PagedStoreArgs rows;                                  // KV = 0: as units it has those of q
     const int32_t *row_seq, *len;

@@ -193,7 +193,8 @@ int32_t odb_paged_layout(odb_paged* h, const odb_paged_batch* b, void* stream) {
         (b->max_rows && (!b->row_seq || !b->row_pos || !b->row_slot)))
         return ODB_ERR_ARG;
     PagedLayoutArgs a{b->len_before, b->len_after, b->first, b->count, b->table, b->free_pages, b->row_start, b->row_seq, b->row_pos,
-                      b->row_slot, b->n_seqs, b->max_rows, h->page_shift, h->cfg.n_pages, b->table_stride, h->status};
+                      b->row_slot, b->n_seqs, b->max_rows, h->page_shift, h->cfg.n_pages, b->table_stride, h->status,
+                      h->scales, 2 * h->cfg.n_layers, h->cfg.n_kv_heads * (h->cfg.page_size / kPagedBlock)};
     return enqueued(launch_paged_layout(a, static_cast<cudaStream_t>(stream)));
 }
 

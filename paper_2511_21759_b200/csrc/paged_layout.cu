@@ -20,6 +20,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kPer = kPagedMaxSeqs / kThreads;   // requests of a thread
+constexpr int kScaleBlocks = 148;                // blocks at least, over a pool of 8 bits: pages may be taken for many more rows than the forward has
 
 struct Sums {
     int row0[kPagedMaxSeqs + 1], take0[kPagedMaxSeqs + 1], give0[kPagedMaxSeqs + 1];
@@ -157,13 +158,25 @@ __global__ void __launch_bounds__(kThreads) paged_layout_kernel(const PagedLayou
         *entry(s, sm.held[s] + j - sm.take0[s]) = taken(j);
     }
     for (int g = t0; g < G - T; g += step) a.free_pages[n_free + g] = given(g);
+    if (a.scales) {
+        // a block to a page: its scales become the smallest, under which what is left there of others counts as nothing
+        const float least = __uint_as_float(static_cast<uint32_t>(kPagedLowExp + 127) << 23);
+        for (int j = blockIdx.x; j < T; j += gridDim.x) {
+            const int page = taken(j);
+            if (page < 0 || page >= a.n_pages) continue;
+            for (int i = tid; i < a.parts * a.page_scales; i += kThreads) {
+                const int part = i / a.page_scales;
+                a.scales[(static_cast<size_t>(part) * a.n_pages + page) * a.page_scales + (i - part * a.page_scales)] = least;
+            }
+        }
+    }
 }
 
 }  // namespace
 
 cudaError_t launch_paged_layout(const PagedLayoutArgs& a, cudaStream_t st) {
-    const int blocks = (a.max_rows + kThreads - 1) / kThreads;
-    return launch_kernel(paged_layout_kernel, dim3(blocks < 1 ? 1 : blocks > 296 ? 296 : blocks), dim3(kThreads), 0, st, a);
+    const int rows = (a.max_rows + kThreads - 1) / kThreads, least = a.scales ? kScaleBlocks : 1, blocks = rows < least ? least : rows;
+    return launch_kernel(paged_layout_kernel, dim3(blocks > 296 ? 296 : blocks), dim3(kThreads), 0, st, a);
 }
 
 }  // namespace odb

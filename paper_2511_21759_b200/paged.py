@@ -136,8 +136,11 @@ class PagedCache(_OnStream):
     torch.float8_e4m3fn, in half the memory: codes of 8 bits with a scale, a power of two, for each block of 16 positions of a head (float32
     [n_layers][2][n_pages][n_kv_heads][page_size / 16]; K or V of a position is code * scale), which norm_rope_store writes and load and
     attention read.  kv, and scales beside it: tensors of that shape to use; otherwise they are allocated (not cleared: what no request has
-    written reaches no result).  room: over codes, whether the workspace has room for the K and V of one layer in bf16, with which the
-    attention of prompts takes half the time (a layer in bf16 is as large as two of codes: of little account with many layers)."""
+    written reaches no result).  Where a part of a block is written, its scale is no less than before as long as the request goes further:
+    a cache's own scales begin at 2 ** ODB_PAGED_LEAST_SCALE, and layout puts that into the pages it hands out; a caller that brings scales,
+    or hands out pages without this cache's layout, writes it there.  room: over codes, whether the workspace has room for the K and V of one
+    layer in bf16, with which the attention of prompts takes half the time (a layer in bf16 is as large as two of codes: of little account
+    with many layers)."""
 
     def __init__(self, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, *, dtype=None, kv=None,
                  scales=None, room: bool = True, device=None):
@@ -163,7 +166,7 @@ class PagedCache(_OnStream):
             if scales is not None:
                 raise ValueError("scales: a pool of bfloat16 has none")
         elif scales is None:
-            scales = torch.empty(shape, dtype=_F32, device=self.device)
+            scales = torch.full(shape, 2.0 ** B.ODB_PAGED_LEAST_SCALE, dtype=_F32, device=self.device)
         elif tuple(scales.shape) != shape or scales.dtype != _F32 or scales.device != self.device or not scales.is_contiguous():
             raise ValueError(f"scales: a contiguous float32 tensor of shape {shape} on {self.device} is wanted")
         self.scales = scales
@@ -240,7 +243,8 @@ class PagedCache(_OnStream):
         raise ValueError(f"{what}: a contiguous float32 tensor of {self.head_dim} values on {self.device} is wanted")
 
     def layout(self, batch: Batch):
-        """Block tables, free list and row maps of the forward (odb_paged_layout); the batch's arrays are updated."""
+        """Block tables, free list and row maps of the forward (odb_paged_layout); the batch's arrays are updated, and so are, over a pool of
+        8 bits, this cache's scales of the pages that are handed out."""
         if batch.cache is not self:
             self._other(batch)
         if _current_device() != self._index:
