@@ -319,7 +319,7 @@ __device__ __forceinline__ void paged_tc_softmax(const PagedAttnArgs& a, const P
             if constexpr (T::kCodes) {
                 wide = T::scales(sh, gt, mul, up, weight);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) mul[c] = fmaxf(mul[c] * scale, 0x1p-126f);   // not zero: masked scores stay what they are
+                for (int c = 0; c < 4; ++c) mul[c] = fminf(fmaxf(mul[c] * scale, 0x1p-126f), 0x1.fffffep127f);   // not zero: masked scores stay what they are; finite: scores of zero do
             }
 #pragma unroll
             for (int c = 0; c < 4; ++c) {

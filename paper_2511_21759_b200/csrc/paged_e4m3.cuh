@@ -18,6 +18,11 @@ __device__ __forceinline__ int e4m3_exponent(float scale) {
 __device__ __forceinline__ int e4m3_exponent_for(float top) {
     return min(max(static_cast<int>((__float_as_uint(top) + 0x1fffffu) >> 23) - 127 - 8, kPagedLowExp), kPagedHighExp);
 }
+// The exponent of the power of two that a row of Q is divided by, from its largest value's bits as bf16: that value is then in 1 .. 2, or, of
+// the largest there are, below f16's 2^16, so that the power times a softmax scale stays a number of fp32.  An infinity stays one.
+__device__ __forceinline__ int q_exponent(uint32_t top) { return min(max(static_cast<int>(top >> 7) - 127, -126), 112); }
+// What a score's product is multiplied by, beyond fp32 its largest number: products that are zero stay zero.
+__device__ __forceinline__ float finite_factor(float x) { return fmaxf(fminf(x, 0x1.fffffep127f), -0x1.fffffep127f); }
 // two codes, to the nearest even, the first in the low byte; beyond 448 the largest number
 __device__ __forceinline__ unsigned short e4m3x2_of(float a, float b) {
     unsigned short r;

@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<NR>) paged_e4m3_attention_kern
             }
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const int ex = min(max(static_cast<int>(top >> 7) - 127, -126), 126);     // an infinity stays one
+            const int ex = q_exponent(top);
             const float by = exp2_int(-ex), mine = exp2_int(ex) * a.scale_log2;
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
@@ -327,9 +327,10 @@ __global__ void __launch_bounds__(kThreads, kCtas<NR>) paged_e4m3_attention_kern
 #pragma unroll
                 for (int e = 0; e < NE; ++e) {
                     float* x = &s[e >> 1][e & 1];               // x[0], x[2]
+                    const float by = finite_factor(unit[e] * ks);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        x[2 * h] = __fmul_rn(x[2 * h] + odd[e >> 1][2 * h + (e & 1)], fminf(unit[e] * ks, 0x1.fffffep127f));   // rounded as the maximum is
+                        x[2 * h] = __fmul_rn(x[2 * h] + odd[e >> 1][2 * h + (e & 1)], by);   // rounded as the maximum is
                         if (!whole) {
                             const int key = k0 + h * 8 + (lane >> 2);
                             const bool seen = key < w.q.len && key - a.right <= pos[e] && (key + a.left >= pos[e] || key < a.sinks);

@@ -85,7 +85,7 @@ struct TcE4m3 {
 #pragma unroll
             for (int j = 0; j < 4; ++j) top = max_u16x2(top, x[c][j] & 0x7fff7fffu);
         top = max(top & 0xffffu, top >> 16);
-        const int ex = min(max(static_cast<int>(top >> 7) - 127, -126), 126);     // an infinity stays one
+        const int ex = q_exponent(top);
         const float by = exp2_int(-ex);
 #pragma unroll
         for (int c = 0; c < HD / 8; ++c) {

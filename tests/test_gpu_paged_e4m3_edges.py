@@ -7,7 +7,7 @@ import torch
 from gpu_common import requires_gpu
 from oracle import paged_oracle as O
 from test_gpu_paged import dev, paged
-from test_gpu_paged_e4m3 import E4M3, VALUES, codes_of, i32, make, pool_values, random_pool, setup
+from test_gpu_paged_e4m3 import E4M3, VALUES, check, codes_of, i32, make, pool_values, random_pool, setup
 from test_paged_e4m3_host import kernel
 
 LOW = 2.0 ** O.LOW_EXP
@@ -133,6 +133,125 @@ def test_layout_touches_the_scales_of_the_pages_it_hands_out_and_no_others(layer
     want = scales.clone()
     want[:, :, taken] = LOW
     assert torch.equal(bits(cache.scales), bits(want))
+    cache.close()
+
+
+# ---- scores at the end of their range -----------------------------------------------------------------------------------
+
+@pytest.fixture(params=["narrow", "wide", "wide without room"])
+def columns(request):
+    return {"narrow": 1, "wide": 5000, "wide without room": -5000}[request.param]
+
+
+def exact_setup(rng, n, new, G, D, columns, k, v, k_exp, v_exp, q):
+    """One request of n positions, 2 K/V heads: values k, v [n][2][D] as codes under the blocks' exponents k_exp, v_exp [blocks][2] (all of
+    them exact); q [new][2 G][D] at the last positions."""
+    P = paged()
+    page, blocks = 16, O.pages_of(n, 16)
+    n_pages = blocks + 2
+    codes, scales = (t.numpy() for t in random_pool(rng, 1, n_pages, 2, page, D, poison=True))
+    order = rng.permutation(n_pages)[:blocks]
+    for i, (x, e) in enumerate(((k, k_exp), (v, v_exp))):
+        for blk in range(blocks):
+            part = x[blk * 16:(blk + 1) * 16]
+            for h in range(2):
+                y = part[:, h] / 2.0 ** e[blk, h]
+                assert np.array_equal(O.e4m3_round(y), y)
+                c = np.searchsorted(VALUES[:127], np.abs(y)).astype(np.uint8) | np.where(np.signbit(y), 128, 0).astype(np.uint8)
+                codes[0, i, order[blk], h, :len(part)] = c
+                scales[0, i, order[blk], h, 0] = 2.0 ** e[blk, h]
+    cache = make(1, 2 * G, 2, D, page, n_pages, (torch.from_numpy(codes), torch.from_numpy(scales)), room=columns > 0)
+    table = np.full((1, blocks + abs(columns)), 10 ** 6, np.int32)
+    table[0, :blocks] = order
+    b = P.Batch(cache, table=dev(table), len_after=i32([n]), first=i32([n - new]), row_start=i32([0, new]), max_rows=new, max_new=new)
+    qb = torch.from_numpy(q.astype(np.float32)).to(torch.bfloat16)
+    assert np.array_equal(qb.double().numpy(), q)
+    return cache, b, qb.cuda()
+
+
+@requires_gpu
+@pytest.mark.parametrize("new", [2, 3, 40, 250])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("scale", [0.25, -0.25])
+def test_a_score_of_zero_stays_zero_whatever_factors_it(new, D, scale, columns):
+    """Queries of 2^100 in one dim, keys under a scale of 2^119 that are zero there: all scores are zero, a row's output is the mean of what
+    it sees (weights are equal, so that their rounding is none of the mean's): rounded to bf16, and the sums in fp32."""
+    rng = np.random.default_rng(new + D)
+    n, G = 300, 4
+    k = rng.integers(-7, 8, (n, 2, D)) * 2.0 ** 119
+    k[..., 5] = 0.0
+    v = rng.integers(-8, 9, (n, 2, D)) * 1.0
+    q = np.zeros((new, 2 * G, D))
+    q[..., 5] = 2.0 ** 100
+    blocks = O.pages_of(n, 16)
+    cache, b, qb = exact_setup(rng, n, new, G, D, columns, k, v, np.full((blocks, 2), 119), np.zeros((blocks, 2), int), q)
+    lse = torch.empty(new, 2 * G, device="cuda")
+    out = cache.attention(0, b, qb, scale=scale, right=0, lse=lse).double().cpu().numpy()
+    assert cache.status() == 0
+    for r in range(new):
+        ok = n - new + r + 1
+        want = np.repeat(v[:ok].mean(0), G, 0)
+        assert (np.abs(out[r] - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -20 * 8).all(), r
+        assert np.allclose(lse[r].cpu().numpy(), np.log(ok), rtol=2.0 ** -21, atol=0), r
+    cache.close()
+
+
+@requires_gpu
+@pytest.mark.parametrize("new,G,columns", [(4, 4, 1), (40, 4, 1), (40, 4, 5000), (40, 4, -5000), (250, 4, 5000), (250, 4, -5000)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_queries_that_are_large_small_zero_or_not_finite_in_every_kernel(new, G, columns, D):
+    """A row's queries are its own matter.  (Many rows' kernels round the scores of 32 packed rows first where one of them is beyond 2^22: the
+    others keep their values, not their last bits.)"""
+    rng = np.random.default_rng(24)
+    cache, b, q, qf, *rest = setup(rng, [400], [new], [400 - new], 2 * G, 2, D, 16, columns=columns)
+    assert kernel_of(b, cache) == {(4, 1): 16, (40, 1): 16, (40, 5000): 1, (40, -5000): 1, (250, 5000): 2, (250, -5000): 1}[new, columns]
+    x = q.clone()
+    x[0] *= 2.0 ** 100
+    x[1] *= 2.0 ** -120
+    x[2] = 0.0
+    x[3, 1, 5] = float("inf")
+    x[3, 2, 6] = float("nan")
+    out = cache.attention(0, b, x, right=0)
+    assert cache.status() == 0
+    assert bool(torch.isnan(out[3, 2]).all()) and bool(torch.isfinite(out[:3]).all()) and bool(torch.isfinite(out[4:]).all())
+    check(out[1:3], None, x[1:3].float().cpu().numpy(), *rest[:3], np.array([0, 2]), [400 - new + 1], D, right=0)
+    x[3, 1:3] = 0.0                                               # the row's other heads against the oracle, and its two by themselves
+    check(cache.attention(0, b, x, right=0)[3:4], None, x[3:4].float().cpu().numpy(), *rest[:3], np.array([0, 1]), [400 - new + 3], D, right=0)
+    keep = [0] + list(range(3, 2 * G))
+    same = cache.attention(0, b, x, right=0)[3, keep]
+    assert bool(torch.isfinite(out[3, keep]).all()) and torch.allclose(out[3, keep].float(), same.float(), rtol=2.0 ** -7, atol=2.0 ** -16)   # a step, and a sum's roundings
+    if new > 4:
+        check(out[4:20], None, x[4:20].float().cpu().numpy(), *rest[:3], np.array([0, 16]), [400 - new + 4], D, right=0)
+    cache.close()
+
+
+@requires_gpu
+@pytest.mark.parametrize("new", [2, 40, 250])
+@pytest.mark.parametrize("scale", [8.0, -2.0 ** -8])
+def test_queries_of_the_largest_numbers_meet_keys_of_the_smallest(new, scale, columns):
+    """Queries of 2^127, keys under the smallest scales: scores of some 2^20 and 2^30, exact but for the scale's rounding.  A tie's
+    weights round alike (by 2^-9 in bf16), the output by 2^-9; the others' weights are 0.  The log-sum-exp: the scale's rounding, a product's and
+    the two of its way to base e, 2^-24 each."""
+    rng = np.random.default_rng(new)
+    n, G, D = 333, 4, 64
+    blocks = O.pages_of(n, 16)
+    k = rng.integers(-1, 2, (n, 2, D)) * (rng.random((n, 2, D)) < 0.1) * 2.0 ** -98
+    e = np.stack([rng.integers(-100, -97, (blocks, 2)), np.zeros((blocks, 2), int)])
+    v = rng.integers(-8, 9, (n, 2, D)) * 1.0
+    q = rng.integers(-1, 2, (new, 2 * G, D)) * 2.0 ** 127
+    cache, b, qb = exact_setup(rng, n, new, G, D, columns, k, v, e[0], e[1], q)
+    lse = torch.empty(new, 2 * G, device="cuda")
+    out = cache.attention(0, b, qb, scale=scale, right=0, lse=lse).double().cpu().numpy()
+    lse = lse.double().cpu().numpy()
+    assert cache.status() == 0
+    for r in range(new):
+        ok = n - new + r + 1
+        for h in range(2 * G):
+            x = k[:ok, h // G] @ q[r, h] * scale
+            win = x == x.max()
+            want, mag = v[:ok, h // G][win].mean(0), np.abs(v[:ok, h // G][win]).mean(0)
+            assert (np.abs(out[r, h] - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -8 * mag).all(), (r, h)
+            assert abs(lse[r, h] - (x.max() + np.log(win.sum()))) <= 2.0 ** -21 * (1 + abs(x.max())), (r, h)
     cache.close()
 
 
