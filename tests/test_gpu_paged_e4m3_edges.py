@@ -226,6 +226,43 @@ def test_queries_that_are_large_small_zero_or_not_finite_in_every_kernel(new, G,
 
 
 @requires_gpu
+@pytest.mark.parametrize("new", [2, 5, 45, 240])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("scale", [2.0 ** 20, -2.0 ** 20, 2.0 ** 23])
+def test_scores_beyond_2_to_22_with_winners_and_ties(new, D, scale, columns):
+    """Whole numbers times a power of two: every product and sum is exact, and rows have the mean of their winners, whose blocks have different
+    scales of K and of V.  A tie's weights round alike (by 2^-9 in bf16), the output by 2^-9; the others' weights are 0.  The log-sum-exp: the
+    scale's rounding, a product's and the two of its way to base e, 2^-24 each."""
+    rng = np.random.default_rng(new + D)
+    n, G = 333, 4
+    blocks = O.pages_of(n, 16)
+    k = rng.integers(-1, 2, (n, 2, D)) * (rng.random((n, 2, D)) < 0.1) * 1.0
+    for j in rng.integers(0, n, 60):                              # the same key in many blocks
+        k[j] = k[3]
+    v = rng.integers(-8, 9, (n, 2, D)) * 1.0
+    e = rng.integers(-4, 1, (2, blocks, 2))
+    v = v * 2.0 ** np.repeat(e[1], 16, 0)[:n][..., None]
+    q = rng.integers(-2, 3, (new, 2 * G, D)) * 1.0
+    cache, b, qb = exact_setup(rng, n, new, G, D, columns, k, v, e[0], e[1], q)
+    lse = torch.empty(new, 2 * G, device="cuda")
+    out = cache.attention(0, b, qb, scale=scale, right=0, lse=lse).double().cpu().numpy()
+    lse = lse.double().cpu().numpy()
+    assert cache.status() == 0
+    ties = 0
+    for r in range(new):
+        ok = n - new + r + 1
+        for h in range(2 * G):
+            x = k[:ok, h // G] @ q[r, h] * scale
+            win = x == x.max()
+            ties += win.sum() > 1
+            want, mag = v[:ok, h // G][win].mean(0), np.abs(v[:ok, h // G][win]).mean(0)
+            assert (np.abs(out[r, h] - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -8 * mag).all(), (r, h)
+            assert abs(lse[r, h] - (x.max() + np.log(win.sum()))) <= 2.0 ** -21 * (1 + abs(x.max())), (r, h)
+    assert ties
+    cache.close()
+
+
+@requires_gpu
 @pytest.mark.parametrize("new", [2, 40, 250])
 @pytest.mark.parametrize("scale", [8.0, -2.0 ** -8])
 def test_queries_of_the_largest_numbers_meet_keys_of_the_smallest(new, scale, columns):
