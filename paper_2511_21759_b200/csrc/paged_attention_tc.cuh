@@ -15,6 +15,9 @@ template <int HD> constexpr uint32_t kQBytes = kTQ * HD * 2;
 template <int HD> constexpr uint32_t kTileBytes = kKT * HD * 2;             // K or V of a tile, as the products take it
 template <int HD> constexpr int kBufs = HD == 128 ? 2 : 3;   // S / P buffers of a Q tile: 256 columns, of which O takes HD
 constexpr uint32_t kCols = 256;
+// kCodes: a tile that moves the shift has weights up to 2^kRoom, those behind it up to 2^(kRoom + kSlack), where f16 ends below 2^16, so that few
+// are too small for f16.  The row's sum stands without it, over 2^kRoom: where V's scales are the smallest it is near the end of fp32.
+constexpr float kSlack = 8.0f, kRoom = 7.0f;
 constexpr uint32_t kPatch = 4096;                            // per softmax warp, in the Q tile: 32 rows x 128 bytes of output
 
 // The launch's numbers and the maps of Q and of the outputs.
@@ -268,7 +271,6 @@ __device__ __forceinline__ void paged_tc_softmax(const PagedAttnArgs& a, const P
     const uint32_t lane_base = static_cast<uint32_t>(gw * 32) << 16;   // this warp's TMEM lanes
     const uint32_t s_base = tmem + g * kCols + lane_base, o_base = paged_tc_o<HD>(tmem, g) + lane_base;
     const int rows_g = a.tile_tokens * a.G;                  // packed rows of a Q tile
-    constexpr float kSlack = 8.0f;
     float scale = a.scale_log2;                              // of the row's scores
     bool ok = true;
     uint32_t item = 0, done = 0;                             // key tiles of the items before
@@ -291,7 +293,7 @@ __device__ __forceinline__ void paged_tc_softmax(const PagedAttnArgs& a, const P
         const int left = min(rows_g, (w.q.n - tok0) * a.G);          // rows of the Q tile (may be negative); others hold anything
         const bool mine = r < left;
         if constexpr (T::kCodes) scale = a.scale_log2 * T::template own_q<kTQ>(sh, sQ, item, r, ok, wait);
-        float M_row = -INFINITY, l_row = 0.f, G_row = 0.f;           // the row's shift, M (kCodes: M + G), and its sum
+        float M_row = -INFINITY, l_row = 0.f, G_row = 0.f;           // the row's shift, M (kCodes: M + G), and its sum (kCodes: over 2^kRoom)
         uint32_t sv[64];                                             // the row's scores of the tile at hand
         auto ask = [&](int t) {                                      // for those of tile t, once they are there
             const uint32_t gt = done + t, b = gt % kB;
@@ -314,7 +316,7 @@ __device__ __forceinline__ void paged_tc_softmax(const PagedAttnArgs& a, const P
                     if (!((mask >> j) & 1ull)) sv[j] = 0xff800000u;
             }
             float mx[4];                                             // largest visible score of the tile, in four chains
-            float mul[4], up[4], weight[4];                          // kCodes: of the tile's blocks: K's scale and the row's, log2 of V's, and 1 / V's
+            float mul[4], up[4], weight[4];                          // kCodes: of the tile's blocks: K's scale and the row's, log2 of V's, and 2^-kRoom / V's
             bool wide = false;                                       // V's scales lie far from 1: see the sum
             if constexpr (T::kCodes) {
                 wide = T::scales(sh, gt, mul, up, weight);
@@ -343,7 +345,7 @@ __device__ __forceinline__ void paged_tc_softmax(const PagedAttnArgs& a, const P
                 }
                 const bool seen = mine && mask && most != -INFINITY;
                 far = seen && fabsf(most) >= 0x1p22f;
-                move = seen && (M_row == -INFINITY || exceeds > G_row + kSlack || most > M_row + 60.f);
+                move = seen && (M_row == -INFINITY || exceeds > G_row + (kSlack + kRoom) || most > M_row + 60.f);
                 M_new = fmaxf(M_row, ceilf(most));
             } else {
                 float m0 = fmaxf(max3(mx[0], mx[1], __uint_as_float(sv[15])), max3(mx[2], mx[3], __uint_as_float(sv[31])));
@@ -365,7 +367,7 @@ __device__ __forceinline__ void paged_tc_softmax(const PagedAttnArgs& a, const P
                         G_new = mx[0] - M_new + up[0];
 #pragma unroll
                         for (int c = 1; c < 4; ++c) G_new = fmaxf(G_new, mx[c] - M_new + up[c]);
-                        G_new = ceilf(G_new);
+                        G_new = ceilf(G_new) - kRoom;
                         if (M_row != -INFINITY) G_new = fmaxf(G_new, M_row - M_new + G_row);   // M + G never falls
                     }
                     if (M_row != -INFINITY) factor = exp2f(M_row - M_new + (G_row - G_new));   // an exact power of two
@@ -427,7 +429,7 @@ __device__ __forceinline__ void paged_tc_softmax(const PagedAttnArgs& a, const P
                     float all = 0.f;
 #pragma unroll
                     for (int j = 0; j < 64; ++j) all += ex2_approx(__uint_as_float(sv[j]) * unpack2f(mult2[j / 16]).x - (rounded ? 0.f : m_log2));
-                    l_row += all * exp2f(-G_row);
+                    l_row += all * exp2f(-G_row - kRoom);
                 } else {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
@@ -499,10 +501,10 @@ __device__ __forceinline__ void paged_tc_softmax(const PagedAttnArgs& a, const P
         const uint32_t place = smem_u32(sQ) + ((item % NQ) * QT + g) * kQBytes<HD>;   // every MMA that reads this Q tile has completed
         const uint32_t patch = place + gw * kPatch;
         const bool final = w.whole();
-        const float inv = l_row == 0.f ? 0.f : 1.0f / l_row;
+        const float inv = l_row == 0.f ? 0.f : (T::kCodes ? exp2f(-kRoom) : 1.0f) / l_row;
         if (final && a.lse && row_w + lane < left) {
             const int idx = row_w + lane, i = a.by_group(idx);
-            a.lse[static_cast<size_t>(w.q.row0 + tok0 + i) * a.H + w.head * a.G + idx - i * a.G] = paged_lse(m_log2, T::kCodes ? l_row * exp2f(G_row) : l_row);   // the logarithm of a number near 1 where one key takes most
+            a.lse[static_cast<size_t>(w.q.row0 + tok0 + i) * a.H + w.head * a.G + idx - i * a.G] = paged_lse(m_log2, T::kCodes ? l_row * exp2f(G_row + kRoom) : l_row);   // the logarithm of a number near 1 where one key takes most
         }
         // 64 values of the row as pairs of bf16
         auto result = [&](int c, uint32_t (&x)[32]) {
@@ -554,7 +556,7 @@ __device__ __forceinline__ void paged_tc_softmax(const PagedAttnArgs& a, const P
             const size_t part = paged_part(a, blockIdx.x, w.t0 == 0) + g * kTQ;
             float* po = a.part_o + part * HD + r * 4;
             const float unit = T::kCodes ? exp2f(G_row) : 1.f;       // a part's unit is 2^M
-            if (r < left) *reinterpret_cast<float2*>(a.part_ml + (part + r) * 2) = make_float2(M_row, l_row * unit);
+            if (r < left) *reinterpret_cast<float2*>(a.part_ml + (part + r) * 2) = make_float2(M_row, T::kCodes ? l_row * exp2f(G_row + kRoom) : l_row);
 #pragma unroll 1
             for (int c = 0; c < HD / 32; ++c) {
                 uint32_t v[32];

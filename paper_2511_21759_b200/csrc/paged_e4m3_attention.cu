@@ -7,10 +7,12 @@
 // of four heads, fill a quarter of each product and of the softmax.  NR: 8 or 16 packed rows an item, whose products share the codes.
 //   S: a row of Q is brought into 1 .. 2 by a power of two first (f16 keeps 2^-25 of its largest value; the sums of products are fp32);
 //      the scores are multiplied by that power, the softmax scale and the block's scale, all at once.
-//   P V: beside the running maximum m of a row's scores x stands g, so that m + g is the running maximum of x + log2(V's scale).  The
-//      weights that multiply codes are 2^(x - m + log2(scale) - g) <= 1, in f16 (up to 2^-11 of themselves, or 2^-25 of the row's
-//      largest); the sum takes them in fp32, block by block, times 2^(g - log2(scale)): whatever the scales, the largest product of a
-//      weight and a scale keeps its precision.  (g and not the maximum itself, which would lose the scales in large scores' last bits.)
+//   P V: beside the running maximum m of a row's scores x stands g, so that m + g + 15 is the running maximum of x + log2(V's scale).  The
+//      weights that multiply codes are 2^(x - m + log2(scale) - g) <= 2^15, in f16: off by up to 2^-11 of themselves, or 2^-40 of the
+//      row's largest.  The 15 are for contexts in which one key takes most (with weights up to 1 all that are 2^-25 of the largest
+//      vanished, up to 2^-8 of the sum of 131072 keys, and all of the output where the one key's V is zero).  The sum takes them in fp32, block
+//      by block, times 2^(g - log2(scale)): whatever the scales, the largest product of a weight and a scale keeps its precision.  (g and
+//      not the maximum itself, which would lose the scales in large scores' last bits.)
 // A warp multiplies 16 positions of a tile of 64: a block, with one scale of K and one of V.
 //
 // Places in a fragment are the dims that they have in memory: of 16 dims a lane has the four that ldmatrix gives it as one word, the same
@@ -40,6 +42,7 @@ constexpr int kManyRows = 1024;             // packed rows a request, on average
 constexpr int kMmaWarps = 4;                // 16 keys of a tile each
 constexpr int kThreads = 32 * (kMmaWarps + 1);
 constexpr int kBlocks = kKT / kPagedBlock;  // of a tile
+constexpr float kRoom = 15.f;               // log2 of the largest weight, whose f16 ends below 2^16
 template <int NR> constexpr int kCtas = NR == 8 ? 3 : 2;                    // of an SM
 template <int HD> constexpr uint32_t kTileBytes = kKT * HD;                 // K or V of a tile
 template <int HD, int NR> constexpr int kStages = HD == 128 ? (NR == 8 ? 4 : 7) : (NR == 8 ? 8 : 13);   // K and V tiles on the way or in use
@@ -347,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<NR>) paged_e4m3_attention_kern
                     shift[e] = more[e] = 0.f;
                     const float mn = fmaxf(m[e], top[e]);
                     if (mn == -INFINITY) continue;              // the row has seen no key
-                    const float before = m[e] - mn + g[e], gn = fmaxf(before, top[e] - mn + log_vs);
+                    const float before = m[e] - mn + g[e], gn = fmaxf(before, top[e] - mn + (log_vs - kRoom));
                     l[e] *= ex2_approx(m[e] - mn);
                     factor[e] = ex2_approx(before - gn);
                     shift[e] = mn;
@@ -422,7 +425,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<NR>) paged_e4m3_attention_kern
                     const float* x = sh->ml[i][row_of(e)];
                     L += paged_weight(x[0], M) * x[1];
                 }
-                const float f = g[e] == -INFINITY ? 0.f : ex2_approx(m[e] - M + g[e]);   // from here on in units of 2^M, without scales
+                const float f = g[e] == -INFINITY ? 0.f : ex2_approx(m[e] - M + (g[e] + kRoom)) * 0x1p-15f;   // from here on in units of 2^M, without scales
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
                     o[e >> 1][c][e & 1] *= f;

@@ -13,10 +13,12 @@
 //   S: each softmax thread brings its row of Q into 1 .. 2 by a power of two, as f16, before the item's first product; a score is
 //      multiplied by that power, the softmax scale and its block's.
 //   P V: the weights that multiply codes are 2^(x - M + log2(V's scale) - G), with M + G, both whole numbers, moved as the shift of bf16
-//      is, by the largest x + log2 of a tile (apart, so that large scores do not lose the scales); in f16, up to 2^-11 of themselves
-//      or 2^-24 of the row's largest (the shift is rounded up).  The sum takes them block by block over V's scale, so that sum and
-//      output have the same unit, 2^(M + G), and the rest is as for bf16.  Where V's scales are beyond 2^+-40 weights may vanish that
-//      count in the sum, which then has exponentials of its own.
+//      is, by the largest x + log2 of a tile (apart, so that large scores do not lose the scales), whose weight is then 2^6 to 2^7 and
+//      later ones' up to 2^15; in f16, off by up to 2^-11 of themselves or 2^-31 of the row's largest (with weights of 1 for the largest
+//      it was 2^-24, and thousands of keys beside one that takes most lost a tenth and more of their part).  The sum takes them block by
+//      block over V's scale, so that sum and output move together (the sum's unit is 2^(M + G + kRoom), the output's 2^(M + G)), and the
+//      rest is as for bf16.  Where V's scales are beyond 2^+-40 weights may vanish that count in the sum, which then has exponentials of
+//      its own.
 // The converters also do what the loader of bf16 does with V at keys that not all rows see: zeros where no row sees them, and NaN is
 // kept for the softmax warps.
 //
@@ -58,7 +60,7 @@ struct alignas(16) SharedE4m3 {
     uint32_t tmem_base;
     int abort, keep_o[1];
     float scale[3][2][kBlocks];        // of a staging tile's blocks of K, of V
-    alignas(16) float scales[kAhead][3][kBlocks];   // of the tiles at work: K's scale, log2 of V's, 1 / V's (converter of K -> softmax)
+    alignas(16) float scales[kAhead][3][kBlocks];   // of the tiles at work: K's scale, log2 of V's, 2^-kRoom / V's (converter of K -> softmax)
     int wide[kAhead];                  // some log2 of V's scales is beyond +-40
     int odd[3];                        // V in the slot has NaN where only some rows see it
 };
@@ -320,7 +322,7 @@ __global__ void __launch_bounds__(kThreads, 2)
                         if (lane < kBlocks) s[lane] = exp2_int(e);
                         else if (lane < 2 * kBlocks) {
                             s[lane] = static_cast<float>(e);
-                            s[lane + kBlocks] = exp2_int(-e);
+                            s[lane + kBlocks] = exp2_int(-e - static_cast<int>(kRoom));
                         }
                         const bool wide = __any_sync(0xffffffffu, lane >= kBlocks && lane < 2 * kBlocks && (e < -40 || e > 40));
                         if (lane == 0) sh->wide[x.n % kAhead] = wide;

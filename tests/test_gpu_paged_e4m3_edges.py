@@ -266,9 +266,7 @@ def test_scores_beyond_2_to_22_with_winners_and_ties(new, D, scale, columns):
 @pytest.mark.parametrize("new", [2, 40, 250])
 @pytest.mark.parametrize("scale", [8.0, -2.0 ** -8])
 def test_queries_of_the_largest_numbers_meet_keys_of_the_smallest(new, scale, columns):
-    """Queries of 2^127, keys under the smallest scales: scores of some 2^20 and 2^30, exact but for the scale's rounding.  A tie's
-    weights round alike (by 2^-9 in bf16), the output by 2^-9; the others' weights are 0.  The log-sum-exp: the scale's rounding, a product's and
-    the two of its way to base e, 2^-24 each."""
+    """Queries of 2^127, keys under the smallest scales: scores of some 2^20 and 2^30, exact but for the scale's rounding; bounds as above."""
     rng = np.random.default_rng(new)
     n, G, D = 333, 4, 64
     blocks = O.pages_of(n, 16)
@@ -289,6 +287,60 @@ def test_queries_of_the_largest_numbers_meet_keys_of_the_smallest(new, scale, co
             want, mag = v[:ok, h // G][win].mean(0), np.abs(v[:ok, h // G][win]).mean(0)
             assert (np.abs(out[r, h] - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -8 * mag).all(), (r, h)
             assert abs(lse[r, h] - (x.max() + np.log(win.sum()))) <= 2.0 ** -21 * (1 + abs(x.max())), (r, h)
+    cache.close()
+
+
+# ---- many small weights beside a large one ------------------------------------------------------------------------------
+
+@requires_gpu
+@pytest.mark.parametrize("new", [1, 2, 4, 40, 250])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("gap", [20, 24, 27])
+@pytest.mark.parametrize("at", [0, 2000])
+def test_small_weights_beside_a_large_one_reach_the_output(new, D, gap, at, columns):
+    """One key, whose V is zero, takes a weight 2^gap times that of each of 4000 others, whose V are one.  Weights in f16: off by 2^-11 of
+    themselves or by half of 2^-24, in a unit in which the row's largest product of weight and scale is 2^6 at least: 2^-31 of it a weight.
+    In bf16, 2^-9.  The gap's own roundings, in fp32 at 27, are below 2^-17; the output's, 2^-9."""
+    rng = np.random.default_rng(new + D)
+    n, G = 4001 + new, 4
+    blocks = O.pages_of(n, 16)
+    k, v = np.zeros((n, 2, D)), np.ones((n, 2, D))
+    k[at, :, 3], v[at] = 1.0, 0.0
+    q = np.zeros((new, 2 * G, D))
+    q[..., 3] = 1.0
+    cache, b, qb = exact_setup(rng, n, new, G, D, columns, k, v, np.full((blocks, 2), -8), np.full((blocks, 2), -8), q)
+    out = cache.attention(0, b, qb, scale=gap * float(np.log(2.0)), right=0).double().cpu().numpy()
+    assert cache.status() == 0
+    others = n - new + np.arange(new)
+    small = others * 2.0 ** -gap
+    want = small / (1 + small)
+    tol = want * (2.0 ** -9 + 2.0 ** -9 + 2.0 ** -17) + others * 2.0 ** -31
+    assert (np.abs(out - want[:, None, None]) <= tol[:, None, None]).all(), (np.abs(out - want[:, None, None]).max(), want.max())
+    cache.close()
+
+
+@requires_gpu
+@pytest.mark.parametrize("new,G,takes", [(1, 4, 8), (4, 4, 16), (1, 1, 8)])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("gap", [27, 34])
+def test_small_weights_in_shares_of_many_keys(new, G, takes, D, gap):
+    """The same for many requests over the same pages, whose CTAs have long shares: in the kernel of few rows half of f16's last step is 2^-40 of
+    the row's largest product of weight and scale."""
+    P = paged()
+    n, seqs = 8001, 100
+    blocks = O.pages_of(n, 16)
+    k, v = np.zeros((n, 2, D)), np.ones((n, 2, D))
+    k[40, :, 3], v[40] = 1.0, 0.0
+    q = np.zeros((new, 2 * G, D))
+    q[..., 3] = 1.0
+    cache, b, qb = exact_setup(np.random.default_rng(D), n, new, G, D, 1, k, v, np.full((blocks, 2), -8), np.full((blocks, 2), -8), q)
+    many = P.Batch(cache, table=b.table.repeat(seqs, 1), len_after=i32([n] * seqs), first=i32([n - new] * seqs), row_start=i32(np.arange(seqs + 1) * new),
+                   max_rows=seqs * new, max_new=new)
+    assert kernel_of(many, cache) == takes
+    out = cache.attention(0, many, qb.repeat(seqs, 1, 1), scale=gap * float(np.log(2.0))).double().cpu().numpy()
+    assert cache.status() == 0
+    want = (n - 1) * 2.0 ** -gap / (1 + (n - 1) * 2.0 ** -gap)
+    assert (np.abs(out - want) <= want * (2.0 ** -9 + 2.0 ** -11 + 2.0 ** -17) + (n - 1) * 2.0 ** -40).all(), (np.abs(out - want).max(), want)
     cache.close()
 
 
