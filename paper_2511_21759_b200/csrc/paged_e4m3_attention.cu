@@ -34,7 +34,6 @@ namespace {
 constexpr int kItem = 1;                    // key tiles that an item costs beside its own
 constexpr int kMinUnits = 2;                // units of a CTA, at least
 constexpr int kKT = 64;                     // keys per tile
-constexpr int kFullUnits = 12;              // of a CTA where all places on the SMs have work
 constexpr int kFewRows = 32;                // packed rows of the longest request, up to which few rows' kernel takes them
 constexpr int kSmallUnits = 2304;           // up to here few rows' kernel for any number of rows
 constexpr int kCopiedRows = 384;            // packed rows of the longest request above which requests that are alike take a copy in bf16
@@ -122,7 +121,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<NR>) paged_e4m3_attention_kern
     // the ring's memory holds the sums until the start is found
     static_assert(sizeof(PagedScratch) <= S * 2 * kT, "the scratch fits the rings");
     PagedStart start;
-    const bool any = paged_find_start<kThreads, kKT, kItem, true>(a, *reinterpret_cast<PagedScratch*>(smem), 1, kMinUnits, kFullUnits, start);
+    const bool any = paged_find_start<kThreads, kKT, kItem, true>(a, *reinterpret_cast<PagedScratch*>(smem), 1, kMinUnits, 0, start);
     if (!any) return;                                           // block-uniform
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the scratch's writes before the copies that take its place
     __syncthreads();
@@ -525,7 +524,7 @@ cudaError_t launch(PagedAttnArgs a, const CUtensorMap& tmap, int sms, cudaStream
     a.part_rows = NR;
     a.at_once = kCtas<NR> * sms;
     a.by_once = PagedDiv::by(a.at_once);
-    // waves of CTAs, as for a pool of bf16; no more than the table's width leaves work for
+    // one wave of CTAs with equal shares; no more than the table's width leaves work for
     const long long tiles = (static_cast<long long>(a.table_stride) << a.page_shift) / kKT + 1 + kItem,
                     most = (static_cast<long long>(a.max_rows) * a.G / NR + a.n_seqs) * a.KV * tiles / kMinUnits + 1;
     static_assert(kPagedMaxCtas * 16 <= kPagedPartRows, "parts");

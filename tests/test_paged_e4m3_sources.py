@@ -1,4 +1,4 @@
-"""What the sources of the paged cache say of memory that others write.
+"""What the sources of the paged cache say, of memory that others write for the most part.
 
 Of the kernel in front: a kernel of this library is resident, by programmatic
 dependent launch, while the one in front of it still runs, and what it reads has been written in its lifetime.  Loads for memory that is
@@ -6,7 +6,9 @@ constant as long as the kernel lives (ld.global.nc, __ldg, and what the compiler
 nothing about such memory.
 
 Of other threads: the arrival that follows a thread's asynchronous copies (cp.async.mbarrier.arrive) is made when they have landed and orders
-nothing that the thread has stored itself."""
+nothing that the thread has stored itself.
+
+And of a call that has one wave of CTAs: what its shares are at least as long as all places have work decides nothing."""
 import glob
 import os
 import re
@@ -35,3 +37,9 @@ def test_a_scale_that_a_lane_writes_itself_is_followed_by_its_own_arrival(name):
     assert len(stores) == 1
     then = re.search(r"\b(mbar_arrive|copies_arrive)\(", text[stores[0]:])
     assert then.group(1) == "mbar_arrive"
+
+
+@pytest.mark.parametrize("name", ["paged_e4m3_attention.cu", "paged_e4m3_attention_tc.cu"])
+def test_one_wave_of_equal_shares_has_no_numbers_without_effect(name):
+    calls = re.findall(r"paged_find_start<[^>]*>\(a, [^;]*?, (\d+), (\w+(?: \+ \d+)?), (\w+), start\);", code_of(name))
+    assert calls and all(waves == "1" and full == "0" for waves, _, full in calls), calls
