@@ -472,8 +472,9 @@ enum { ODB_PAGED_SCALE_BLOCK = 16, ODB_PAGED_LEAST_SCALE = -100 };   /* position
 size_t odb_paged_e4m3_kv_bytes(const odb_paged_config* cfg);     /* 0: a configuration odb_paged_create_e4m3 would refuse */
 size_t odb_paged_e4m3_scale_bytes(const odb_paged_config* cfg);
 /* A workspace of odb_paged_workspace_bytes + this many bytes has room for the K and V of one layer in bf16: prompts (requests that are
- * alike, of more than 384 packed rows) are then read from a copy of their pages, made in the call, which takes half the time (4096 causal
- * rows 168 us instead of 328).  Without it they are read as all others are. */
+ * alike, the longest of more than 384 packed rows and up to three times the mean) are then read from a copy of all requests' pages, made in
+ * the call, which takes half the time (4096 causal rows 171 us instead of 344; beside one or two single tokens of more than some 30000 keys,
+ * which count as alike, it takes longer).  Without it they are read as all others are. */
 size_t odb_paged_e4m3_layer_bytes(const odb_paged_config* cfg);
 int32_t odb_paged_create_e4m3(const odb_paged_config* cfg, void* kv, size_t kv_bytes, void* scales, size_t scale_bytes, void* workspace,
                               size_t ws_bytes, void* stream, odb_paged** out);

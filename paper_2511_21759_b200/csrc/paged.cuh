@@ -60,7 +60,7 @@ struct PagedLoadArgs {
     __nv_bfloat16 *k_out, *v_out;
     long long k_stride, v_stride;
     int rows, KV, HD, page_shift, n_pages;
-    int per_row, block_rows;                              // pieces of 16 values of a row, K and V; rows of a block (the launcher's)
+    int per_row, block_rows;                              // pieces of 8 values of a row, K and V; rows of a block (the launcher's)
 };
 cudaError_t launch_paged_load(PagedLoadArgs a, cudaStream_t st);
 

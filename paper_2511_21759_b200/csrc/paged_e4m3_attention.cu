@@ -19,8 +19,8 @@
 // four of Q; V's words (transposed by pairs of bytes) hold two keys of two dims, the even ones for rows 0 .. 7 of the product and the odd
 // ones for rows 8 .. 15.  P's fragments are S's, turned 8 x 8 at a time (movmatrix).
 //
-// What bounds it: the codes' way from memory.  A token of 48 requests of up to 8192 keys (32 + 8 heads of 128, 454 MB) takes 83.4 us, 0.83 of
-// the copy rate, of two of up to 131072 keys 90, 0.86; the rest is the CTAs' start, their last tiles and the meeting of parts (one wave of
+// What bounds it: the codes' way from memory.  A token of 48 requests of up to 8192 keys (32 + 8 heads of 128, 454 MB) takes 83 to 90 us by the
+// box, 0.77 to 0.83 of the copy rate, of two of up to 131072 keys 90 to 96, 0.81 to 0.86; the rest is the CTAs' start, their last tiles and the meeting of parts (one wave of
 // CTAs with equal shares; the four waves that pays for bf16 took 89.8, half the bytes leave half the time to hide a start in).  A loader
 // warp issues a box a page and a copy of scales a block, whose number a tile was the bound while K and V had a barrier each (153 us).  Three
 // CTAs an SM with four stages of K and V 83.4, four CTAs with three stages 89.8; with items of 16, whose registers leave two CTAs, seven.
@@ -542,7 +542,12 @@ cudaError_t launch(PagedAttnArgs a, const CUtensorMap& tmap, int sms, cudaStream
 //   kSmallUnits, blocks of 32 rows x group 4: 1536 units (4 requests of 256 keys) 12.5 | 23.4, 2304 (2 of 1024) 22.7 | 24.8, 4608 (4 of 1024)
 //     31 | 26
 //   kCopiedRows, 16 requests, 4096 keys: 384 packed rows 247 | 287 with the copy, 512 rows 321 | 291, 1024 rows 616 | 463
-// The copy wants the requests alike: a prompt among single tokens would have all their pages copied.
+// The copy wants the requests alike, for all pages are copied, those of single tokens too.  Alike is what the kernel over bf16 calls so (the
+// longest up to three times the mean), where that costs no copy: a prompt beside one or two tokens counts, and where they have long contexts
+// the copy is the slower side.  A chunk of 512 rows at 4096 keys x group 4, copy | tensor cores over codes (those with more tokens take the
+// latter): beside one token of 32768 keys 112 | 116, beside two 172 | 145; beside one of 131072 keys 310 | 220, beside two 557 | 324.
+// Head dim 64 takes the same limits, none of which was looked for there; the copy against the codes: a refresh of 4 x 900 - 1536 rows, 32 K/V
+// heads, 82 | 167, the chunk beside a token of 32768 keys 82 | 100, of 131072 205 | 186.
 int paged_e4m3_attention_kernel_of(int n_seqs, int max_rows, int max_new, int group, int kv_heads, long long longest, long long out_stride, bool room) {
     const long long all = static_cast<long long>(max_rows) * group, mean = (max_rows + n_seqs - 1ll) / n_seqs * group,
                     mine = max_new > 0 ? static_cast<long long>(max_new) * group : mean, tiles = longest / kKT + 1;

@@ -9,7 +9,9 @@
 // meet.
 //
 // Bound by latency: a chain of loads, one scan of four sums and a search; 16 requests take 3.5 us a call among others, 1000
-// requests, long prompts among them, 9.7 us.  Lengths that do not fit (negative, longer than a table
+// requests, long prompts among them, 9.7 us.  Over a pool of 8 bits the scales of the pages taken become the smallest, a block to a page, all
+// layers (32 layers of 8 heads: 48 requests that take a page each 2.8 -> 3.5 us in a graph, a prompt of 4096 rows 2.5 -> 3.2, of 16 x 2000 6.0).
+// Lengths that do not fit (negative, longer than a table
 // row, more pages than there are, rows behind the length) change no table: there are no rows then, and the status word
 // says why.
 #include "paged.cuh"

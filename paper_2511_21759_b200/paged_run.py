@@ -8,7 +8,8 @@ request ends, a new one takes its place and its pages.  Per forward
     layout                                     once: block tables, slots, rows
     QKV projection -> norm_rope_store -> attention -> output projection        per layer
 
-The cache is of bf16 or (--kv e4m3) of 8 bits, quantised as it is written: twice the requests in the same memory.
+The cache is of bf16 or (--kv e4m3) of 8 bits, quantised as it is written, in half the memory and, for the attention of prompts, room for
+one layer in bf16 beside it.  Single tokens are then attended to in half the time; this loop's blocks and refreshes take longer than over bf16.
 The projections are the library's GEMM; weights and inputs are synthetic (seeded).  Prints what every forward held and took.
 """
 from __future__ import annotations

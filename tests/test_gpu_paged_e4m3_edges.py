@@ -136,6 +136,20 @@ def test_layout_touches_the_scales_of_the_pages_it_hands_out_and_no_others(layer
     cache.close()
 
 
+@requires_gpu
+def test_layout_of_a_free_list_of_nonsense_touches_no_scales():
+    P, B = paged(), binding()
+    rng = np.random.default_rng(6)
+    scales = dirty_scales(rng, (2, 2, 6, 2, 2))
+    cache = make(2, 2, 2, 64, 32, 6, (random_pool(rng, 2, 6, 2, 32, 64)[0], scales))
+    for page in (-1, 6, 2 ** 31 - 1, -2 ** 31):
+        b = P.Batch(cache, table=i32([[-1] * 4]), free_pages=i32([page] * 6), len_before=i32([0]), len_after=i32([100]), first=i32([0]), count=i32([100]), max_rows=100)
+        cache.layout(b)
+        assert cache.status() == B.ODB_ERR_STATE and bool((b.row_slot == -1).all())
+        assert torch.equal(cache.scales.cpu().view(torch.int32), scales.view(torch.int32))
+    cache.close()
+
+
 # ---- scores at the end of their range -----------------------------------------------------------------------------------
 
 @pytest.fixture(params=["narrow", "wide", "wide without room"])
