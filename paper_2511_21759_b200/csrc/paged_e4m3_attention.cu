@@ -19,8 +19,8 @@
 // four of Q; V's words (transposed by pairs of bytes) hold two keys of two dims, the even ones for rows 0 .. 7 of the product and the odd
 // ones for rows 8 .. 15.  P's fragments are S's, turned 8 x 8 at a time (movmatrix).
 //
-// What bounds it: the codes' way from memory.  A token of 48 requests of up to 8192 keys (32 + 8 heads of 128, 454 MB) takes 83 to 90 us by the
-// box, 0.77 to 0.83 of the copy rate, of two of up to 131072 keys 90 to 96, 0.81 to 0.86; the rest is the CTAs' start, their last tiles and the meeting of parts (one wave of
+// What bounds it: the codes' way from memory.  A token of 48 requests of up to 8192 keys (32 + 8 heads of 128, 454 MB) takes 83 to 90 us from card
+// to card, 0.77 to 0.83 of the copy rate, of two of up to 131072 keys 90 to 96, 0.81 to 0.86; the rest is the CTAs' start, their last tiles and the meeting of parts (one wave of
 // CTAs with equal shares; the four waves that pays for bf16 took 89.8, half the bytes leave half the time to hide a start in).  A loader
 // warp issues a box a page and a copy of scales a block, whose number a tile was the bound while K and V had a barrier each (153 us).  Three
 // CTAs an SM with four stages of K and V 83.4, four CTAs with three stages 89.8; with items of 16, whose registers leave two CTAs, seven.

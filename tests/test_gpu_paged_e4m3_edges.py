@@ -245,7 +245,7 @@ def test_queries_that_are_large_small_zero_or_not_finite_in_every_kernel(new, G,
 @pytest.mark.parametrize("scale", [2.0 ** 20, -2.0 ** 20, 2.0 ** 23])
 def test_scores_beyond_2_to_22_with_winners_and_ties(new, D, scale, columns):
     """Whole numbers times a power of two: every product and sum is exact, and rows have the mean of their winners, whose blocks have different
-    scales of K and of V.  A tie's weights round alike (by 2^-9 in bf16), the output by 2^-9; the others' weights are 0.  The log-sum-exp: the
+    scales of K and of V.  A tie's weights round alike (by 2^-8 in bf16), the output by 2^-8; the others' weights are 0.  The log-sum-exp: the
     scale's rounding, a product's and the two of its way to base e, 2^-24 each."""
     rng = np.random.default_rng(new + D)
     n, G = 333, 4
@@ -314,7 +314,7 @@ def test_queries_of_the_largest_numbers_meet_keys_of_the_smallest(new, scale, co
 def test_small_weights_beside_a_large_one_reach_the_output(new, D, gap, at, columns):
     """One key, whose V is zero, takes a weight 2^gap times that of each of 4000 others, whose V are one.  Weights in f16: off by 2^-11 of
     themselves or by half of 2^-24, in a unit in which the row's largest product of weight and scale is 2^6 at least: 2^-31 of it a weight.
-    In bf16, 2^-9.  The gap's own roundings, in fp32 at 27, are below 2^-17; the output's, 2^-9."""
+    In bf16, 2^-8.  The gap's own roundings, in fp32 at 27, are below 2^-17; the output's, 2^-8."""
     rng = np.random.default_rng(new + D)
     n, G = 4001 + new, 4
     blocks = O.pages_of(n, 16)
@@ -328,7 +328,7 @@ def test_small_weights_beside_a_large_one_reach_the_output(new, D, gap, at, colu
     others = n - new + np.arange(new)
     small = others * 2.0 ** -gap
     want = small / (1 + small)
-    tol = want * (2.0 ** -9 + 2.0 ** -9 + 2.0 ** -17) + others * 2.0 ** -31
+    tol = want * (2.0 ** -8 + 2.0 ** -8 + 2.0 ** -17) + others * 2.0 ** -31
     assert (np.abs(out - want[:, None, None]) <= tol[:, None, None]).all(), (np.abs(out - want[:, None, None]).max(), want.max())
     cache.close()
 
@@ -354,7 +354,41 @@ def test_small_weights_in_shares_of_many_keys(new, G, takes, D, gap):
     out = cache.attention(0, many, qb.repeat(seqs, 1, 1), scale=gap * float(np.log(2.0))).double().cpu().numpy()
     assert cache.status() == 0
     want = (n - 1) * 2.0 ** -gap / (1 + (n - 1) * 2.0 ** -gap)
-    assert (np.abs(out - want) <= want * (2.0 ** -9 + 2.0 ** -11 + 2.0 ** -17) + (n - 1) * 2.0 ** -40).all(), (np.abs(out - want).max(), want)
+    assert (np.abs(out - want) <= want * (2.0 ** -8 + 2.0 ** -11 + 2.0 ** -17) + (n - 1) * 2.0 ** -40).all(), (np.abs(out - want).max(), want)
+    cache.close()
+
+
+@requires_gpu
+@pytest.mark.parametrize("new", [1, 4, 40, 250])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("exp", [-100, 105, "zeros"])
+def test_values_under_the_smallest_and_under_large_scales(new, D, exp, columns):
+    """V of whole numbers under one exponent, or zeros, whose blocks have the smallest scale; scores that rise by 20 along the keys.  bf16 has
+    eight significant bits, steps of 2^-7 from 1 on: a weight's rounding behind the copy is half of that, 2^-8 of the weight, and so is the
+    output's (2^-9, half a step at the end of an octave, is not the bound).  A score's roundings, fp32 at 30, stay below 2^-13 of a weight."""
+    rng = np.random.default_rng(new + D)
+    n, G = 700, 4
+    blocks, e = O.pages_of(n, 16), -100 if exp == "zeros" else exp
+    k = rng.integers(-1, 2, (n, 2, D)) * (rng.random((n, 2, D)) < 0.2) * 1.0
+    k[..., 3] = (np.arange(n) // 47)[:, None]                      # 0 .. 14, by which the scores rise
+    k_exp = np.zeros((blocks, 2), int)
+    v = rng.integers(-8, 9, (n, 2, D)) * 2.0 ** e * (exp != "zeros")
+    q = rng.integers(-2, 3, (new, 2 * G, D)) * 0.25
+    q[..., 3] = 1.5
+    cache, b, qb = exact_setup(rng, n, new, G, D, columns, k, v, k_exp, np.full((blocks, 2), e), q)
+    lse = torch.empty(new, 2 * G, device="cuda")
+    out = cache.attention(0, b, qb, scale=1.0, right=0, lse=lse).double().cpu().numpy()
+    lse = lse.double().cpu().numpy()
+    assert cache.status() == 0
+    for r in range(new):
+        ok = n - new + r + 1
+        for h in range(2 * G):
+            x = k[:ok, h // G] @ q[r, h]
+            z = x.max() + np.log(np.exp(x - x.max()).sum())
+            w = np.exp(x - z)
+            want, mag = w @ v[:ok, h // G], w @ np.abs(v[:ok, h // G])
+            assert (np.abs(out[r, h] - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -12) * mag).all(), (r, h)
+            assert abs(lse[r, h] - z) <= 2.0 ** -16, (r, h)
     cache.close()
 
 
